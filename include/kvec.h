@@ -270,6 +270,112 @@ KVEC_API kvec_status kvec_decode_attention(kvec_handle* h, int batch, const void
                                            const int32_t* lens, int cap, float* out,
                                            kvec_stream_t stream);
 
+/* ------------------------------------------------------------------ decoding over pages
+ *
+ * The cache that decoding grows: keys and values in pages of a pool that a caller hands
+ * out, each page holding page_size slots of every KV head.  Slot j of sequence s and KV
+ * head h is row j % page_size of page page_table[s][j / page_size].  A head's slots are in
+ * the order of their tokens, but after an eviction the heads of a sequence hold different
+ * tokens in a slot.  An entry of page_table outside [0, num_pages) is no page: what would
+ * be stored there is dropped, and what would be read there is not visible. */
+typedef enum { KVEC_BF16 = 0, KVEC_FP16 = 1 } kvec_dtype;
+
+typedef struct {
+    int   dtype;          /* kvec_dtype of the keys and values (and of q and out) */
+    int   page_size;      /* slots of a page: 16, 32, 64, 128 or 256 */
+    int   num_pages;      /* pages of the pool; num_pages * H_kv * page_size <= 2^31 - 1 */
+    int   max_pages;      /* entries of a page_table row: a sequence holds up to
+                             max_pages * page_size <= 2^20 slots */
+    void* k_pages;        /* device [num_pages][H_kv][page_size][d], 16-byte aligned */
+    void* v_pages;        /* the same */
+    float* weights;       /* device fp32 [num_pages][H_kv][page_size], accumulated attention
+                             weights of the slots; NULL: none are kept */
+    const int32_t* page_table;   /* device [batch][max_pages] */
+    const int32_t* lens;         /* device [batch]: slots in use, clamped to [0, max_pages * page_size] */
+} kvec_paged_cache;
+
+/* Queries, keys and values of T new tokens made ready for attention, in one pass:
+ * the norm of every query and key head, its rotation by the token's position, and the
+ * store of keys and values into the cache.  For a query or key row x of d values, in fp32:
+ *   y = x * (mean(x^2) + eps)^-1/2 * w      (w: q_norm or k_norm; NULL: y = x)
+ *   pairs (a, b) of the first rot_dim values become (a c - b s, b c + a s), with the
+ *   pair's c and s from row positions[t] of rot_table; the other values stay.
+ * Pairs are (i, i + rot_dim / 2), or (2 i, 2 i + 1) with interleaved = 1.  Results are
+ * rounded once, to dtype.
+ *   q, k, v   device dtype, token t's heads at q + t * q_stride elements, d apart (strides
+ *             are multiples of 8 elements; one projection's output can hold all three).
+ *   positions device int32 [T]; a token whose position lies outside [0, max_positions) is
+ *             padding: nothing is written for it.
+ *   rot_table device fp32 [max_positions][rot_dim]: cosines of the rot_dim / 2 pairs, then
+ *             their sines.  rot_dim is a multiple of 16 up to d (0: no rotation; the table
+ *             may then be NULL and positions below 2^31 - 1 are valid).
+ *   q_out     device dtype [T][H_q][d]; may be q itself where q_stride = H_q * d.
+ *   k_out     device dtype [T][H_kv][d] (may be k in the same way), or NULL.
+ * With a cache (NULL: none; k_out is then needed) sequence s's tokens take its last slots:
+ * its lens already counts them, and token t of cu_tokens[s] <= t < cu_tokens[s + 1] goes to
+ * slot lens[s] - (cu_tokens[s + 1] - t).  The slot's accumulated weight becomes 0.
+ * cu_tokens is device int32 [batch + 1], ascending from 0 (NULL: token t is sequence t's
+ * only new one, batch = T); tokens from cu_tokens[batch] on are padding.  A slot below 0 or past the
+ * sequence's capacity is not stored.  v may be NULL without a cache.
+ * No two tokens may share a slot.  0 <= T; T = 0 does nothing. */
+typedef struct {
+    int dtype;                 /* kvec_dtype of q, k, v, the norms and the outputs */
+    int num_tokens;            /* T */
+    const void *q, *k, *v;
+    int64_t q_stride, k_stride, v_stride;   /* elements from a token to the next */
+    const void *q_norm, *k_norm;            /* device dtype [d], or NULL */
+    float eps;                 /* >= 0, finite */
+    int rot_dim, interleaved;
+    int max_positions;         /* rows of rot_table */
+    const float* rot_table;
+    const int32_t* positions;
+    void *q_out, *k_out;
+} kvec_rotate_args;
+KVEC_API kvec_status kvec_rotate_append(kvec_handle* h, const kvec_rotate_args* args, int batch,
+                                        const int32_t* cu_tokens, const kvec_paged_cache* cache,
+                                        kvec_stream_t stream);
+
+/* Bytes of scratch that kvec_paged_decode needs for these sizes (0 if they are invalid).
+ * with_weights: the cache keeps accumulated weights.  Host only; needs the handle for
+ * the device's size. */
+KVEC_API size_t kvec_paged_decode_bytes(kvec_handle* h, int batch, int max_len, int with_weights);
+
+/* Attention of one new token per sequence over the paged cache.  The token's own key is
+ * the last slot (kvec_rotate_append with lens counting it).  With n = lens[s] clamped to
+ * [0, min(max_len, capacity)], slot j < n is visible if window = 0, or j >= n - window, or
+ * j < sinks (the first slots that stay visible beside a sliding window):
+ *   out[s][hq] = sum_j p_j v_j,  p_j = softmax over the visible j of scale * <q[s][hq], k_j>;
+ * no visible slot (or every logit minus infinity): a zero row.  With cache.weights every
+ * visible slot's weight grows by the p_j of the group's query heads:
+ *   weights[slot j of head h] += sum over hq of h's group of p_j,
+ * which is what kvec_paged_evict ranks by.
+ *   q        device cache.dtype [batch][H_q][d]; out the same shape and type.
+ *   max_len  host bound on the lengths; the work is divided over the device by it.
+ *   scratch  device, kvec_paged_decode_bytes bytes, 16-byte aligned: written and read
+ *            within the call; calls that may overlap need one each.
+ * No two sequences may share a page when weights are kept (their additions would race).
+ * 1 <= batch <= max_batch, H_q/H_kv <= 8. */
+KVEC_API kvec_status kvec_paged_decode(kvec_handle* h, int batch, const void* q,
+                                       const kvec_paged_cache* cache, int max_len, int window, int sinks,
+                                       void* out, void* scratch, size_t scratch_bytes, kvec_stream_t stream);
+
+/* Eviction by accumulated attention weight.  Of a sequence with n = lens[s] slots (clamped
+ * to [0, min(max_len, capacity)]) every KV head keeps m = min(n, budget): its first `sinks`
+ * slots, its last `recent` slots (sinks + recent <= budget), and the best of the others by
+ * cache.weights (higher first, then the lower slot; NaN counts as minus infinity).  The
+ * kept rows of K, V and weights are copied, in ascending order of their slots, to slots
+ * 0 .. m - 1 of the pages of new_table; the old pages are not changed.
+ *   new_table device int32 [batch][new_max_pages], new_max_pages * page_size >=
+ *             min(budget, max_len): pages of the same pool, none of them in use by
+ *             page_table and none twice (the copies of a page that is would race).
+ *   new_lens  device int32 [batch]: m.
+ *   kept      device int32 [batch][H_kv][budget]: the kept slots, ascending; -1 past m.
+ * A slot on no page ranks as NaN does; kept, its row is left as the new page has it. */
+KVEC_API kvec_status kvec_paged_evict(kvec_handle* h, int batch, const kvec_paged_cache* cache,
+                                      const int32_t* new_table, int new_max_pages, int max_len, int budget,
+                                      int sinks, int recent, int32_t* new_lens, int32_t* kept,
+                                      kvec_stream_t stream);
+
 /* Device views of the last processed layer's intermediates (valid until the
  * next call on the handle; read after synchronising the stream).  Row strides
  * use ML = max_seqlen + 4 rounded up to a multiple of 32 (reported in max_seqlen).

@@ -739,6 +739,7 @@ kvec_status kvec_create(const kvec_params* params, kvec_handle** out) {
     if (e == cudaSuccess) e = configure_select();
     if (e == cudaSuccess) e = configure_chain();
     if (e == cudaSuccess) e = configure_decode();
+    if (e == cudaSuccess) e = configure_paged_decode();
     if (e == cudaSuccess) e = cudaDeviceGetStreamPriorityRange(&h->prio_lo, &h->prio_hi);
     for (cudaStream_t* st : {&h->s_score, &h->s_gather, &h->s_cap})
         if (e == cudaSuccess) e = cudaStreamCreateWithPriority(st, cudaStreamNonBlocking, h->prio_lo);
@@ -1155,6 +1156,225 @@ kvec_status kvec_decode_attention(kvec_handle* h, int batch, const void* q, cons
     io.scale = p.softmax_scale > 0.f ? p.softmax_scale : (float)(1.0 / sqrt((double)p.head_dim));
     cudaError_t e = launch_decode(io, h->num_sms, reinterpret_cast<cudaStream_t>(stream));
     if (e != cudaSuccess) return cuda_fail(e, "decode attention launch");
+    return KVEC_OK;
+}
+
+// ------------------------------------------------------------------ decoding over pages
+
+namespace {
+
+constexpr int kPagedMaxLen = 1 << 20;    // slots of a sequence, rows of a prefill sequence
+constexpr int kMaxGridBatch = 65535;     // sequences are a grid's z dimension
+
+// The checks of a call that do not need the handle come first, so that they hold without a device.
+kvec_status view_cache(const kvec_paged_cache* c, PagedCacheView* v) {
+    if (!c) return fail(KVEC_ERR_INVALID_ARG, "cache is NULL");
+    if (c->dtype != KVEC_BF16 && c->dtype != KVEC_FP16)
+        return fail(KVEC_ERR_INVALID_ARG, "cache dtype %d is neither KVEC_BF16 nor KVEC_FP16", c->dtype);
+    int log_page = 4;
+    while (log_page <= 8 && (1 << log_page) != c->page_size) ++log_page;
+    if (log_page > 8)
+        return fail(KVEC_ERR_UNSUPPORTED, "page_size %d is none of 16, 32, 64, 128, 256", c->page_size);
+    if (c->num_pages < 1 || c->max_pages < 1 || ((long long)c->max_pages << log_page) > kPagedMaxLen)
+        return fail(KVEC_ERR_INVALID_ARG, "need num_pages >= 1 and 1 <= max_pages * page_size <= %d", kPagedMaxLen);
+    if (!c->k_pages || !c->v_pages || !c->page_table || !c->lens)
+        return fail(KVEC_ERR_INVALID_ARG, "a device pointer of the cache is NULL");
+    if (!aligned16(c->k_pages) || !aligned16(c->v_pages) || !aligned16(c->weights))
+        return fail(KVEC_ERR_INVALID_ARG, "k_pages, v_pages and weights must be 16-byte aligned");
+    if (reinterpret_cast<uintptr_t>(c->page_table) % 4 || reinterpret_cast<uintptr_t>(c->lens) % 4)
+        return fail(KVEC_ERR_INVALID_ARG, "page_table and lens must be 4-byte aligned");
+    v->k = static_cast<uint16_t*>(c->k_pages);
+    v->v = static_cast<uint16_t*>(c->v_pages);
+    v->weights = c->weights;
+    v->table = c->page_table;
+    v->lens = c->lens;
+    v->dtype = c->dtype;
+    v->log_page = log_page;
+    v->num_pages = c->num_pages;
+    v->max_pages = c->max_pages;
+    v->capacity = c->max_pages << log_page;
+    return KVEC_OK;
+}
+
+// What a call over pages asks of its handle.
+kvec_status check_paged_handle(kvec_handle* h, int batch, const PagedCacheView* v) {
+    if (!h) return fail(KVEC_ERR_INVALID_ARG, "handle is NULL");
+    if (batch < 1 || batch > h->p.max_batch || batch > kMaxGridBatch)
+        return fail(KVEC_ERR_INVALID_ARG, "batch %d outside [1, max_batch = %d]", batch,
+                    std::min(h->p.max_batch, kMaxGridBatch));
+    if (v && (((long long)v->num_pages * h->p.num_kv_heads) << v->log_page) > 0x7fffffffll)
+        return fail(KVEC_ERR_UNSUPPORTED, "num_pages * num_kv_heads * page_size exceeds 2^31 - 1 rows");
+    return KVEC_OK;
+}
+
+kvec_status check_window(int window, int sinks) {
+    if (window < 0 || sinks < 0) return fail(KVEC_ERR_INVALID_ARG, "window and sinks must not be negative");
+    return KVEC_OK;
+}
+
+float softmax_scale_of(const kvec_params& p) {
+    return p.softmax_scale > 0.f ? p.softmax_scale : (float)(1.0 / sqrt((double)p.head_dim));
+}
+
+bool stride_ok(int64_t s) { return s >= 0 && s % 8 == 0 && s < ((int64_t)1 << 40); }
+
+}  // namespace
+
+kvec_status kvec_rotate_append(kvec_handle* h, const kvec_rotate_args* a, int batch, const int32_t* cu_tokens,
+                               const kvec_paged_cache* cache, kvec_stream_t stream) {
+    if (!a) return fail(KVEC_ERR_INVALID_ARG, "args is NULL");
+    PagedCacheView v{};
+    if (cache) {
+        kvec_status s = view_cache(cache, &v);
+        if (s != KVEC_OK) return s;
+        if (cache->dtype != a->dtype) return fail(KVEC_ERR_INVALID_ARG, "the cache's dtype differs from the inputs'");
+    }
+    if (a->dtype != KVEC_BF16 && a->dtype != KVEC_FP16)
+        return fail(KVEC_ERR_INVALID_ARG, "dtype %d is neither KVEC_BF16 nor KVEC_FP16", a->dtype);
+    if (a->num_tokens < 0) return fail(KVEC_ERR_INVALID_ARG, "num_tokens %d < 0", a->num_tokens);
+    if (!(a->eps >= 0.f) || !isfinite(a->eps)) return fail(KVEC_ERR_INVALID_ARG, "eps must be finite and not negative");
+    if (a->rot_dim < 0 || a->rot_dim > kHeadDim || a->rot_dim % 16)
+        return fail(KVEC_ERR_INVALID_ARG, "rot_dim %d must be a multiple of 16 in [0, %d]", a->rot_dim, kHeadDim);
+    if (a->interleaved != 0 && a->interleaved != 1) return fail(KVEC_ERR_INVALID_ARG, "interleaved must be 0 or 1");
+    if (a->rot_dim && (a->max_positions < 1 || !a->rot_table))
+        return fail(KVEC_ERR_INVALID_ARG, "a rotation needs rot_table and max_positions >= 1");
+    if (!stride_ok(a->q_stride) || !stride_ok(a->k_stride) || !stride_ok(a->v_stride))
+        return fail(KVEC_ERR_INVALID_ARG, "strides must be non-negative multiples of 8 elements");
+    kvec_status s = check_paged_handle(h, batch, cache ? &v : nullptr);
+    if (s != KVEC_OK) return s;
+    if (a->num_tokens == 0) return KVEC_OK;
+    if (!cu_tokens && a->num_tokens != batch)
+        return fail(KVEC_ERR_INVALID_ARG, "without cu_tokens every sequence has one token: num_tokens %d, batch %d",
+                    a->num_tokens, batch);
+    if (!a->q || !a->k || !a->positions || !a->q_out || (cache && !a->v) || (!cache && !a->k_out))
+        return fail(KVEC_ERR_INVALID_ARG, "a device pointer is NULL");
+    for (const void* p : {a->q, a->k, a->v, a->q_norm, a->k_norm, (const void*)a->rot_table, (const void*)a->q_out,
+                          (const void*)a->k_out})
+        if (!aligned16(p))
+            return fail(KVEC_ERR_INVALID_ARG, "q, k, v, the norms, rot_table and the outputs must be 16-byte aligned");
+    if (reinterpret_cast<uintptr_t>(a->positions) % 4 || reinterpret_cast<uintptr_t>(cu_tokens) % 4)
+        return fail(KVEC_ERR_INVALID_ARG, "positions and cu_tokens must be 4-byte aligned");
+    const kvec_params& p = h->p;
+    if ((a->q_out == a->q && a->q_stride != (int64_t)p.num_q_heads * kHeadDim) ||
+        (a->k_out == a->k && a->k_out && a->k_stride != (int64_t)p.num_kv_heads * kHeadDim))
+        return fail(KVEC_ERR_INVALID_ARG, "an output may be its input only where the input's tokens are packed");
+    RotateIO io{};
+    io.q = static_cast<const uint16_t*>(a->q);
+    io.k = static_cast<const uint16_t*>(a->k);
+    io.v = static_cast<const uint16_t*>(a->v);
+    io.q_stride = a->q_stride;
+    io.k_stride = a->k_stride;
+    io.v_stride = a->v_stride;
+    io.q_norm = static_cast<const uint16_t*>(a->q_norm);
+    io.k_norm = static_cast<const uint16_t*>(a->k_norm);
+    io.rot_table = a->rot_table;
+    io.positions = a->positions;
+    io.cu = cu_tokens;
+    io.q_out = static_cast<uint16_t*>(a->q_out);
+    io.k_out = static_cast<uint16_t*>(a->k_out);
+    io.eps = a->eps;
+    io.dtype = a->dtype;
+    io.num_tokens = a->num_tokens;
+    io.batch = batch;
+    io.Hq = p.num_q_heads;
+    io.Hkv = p.num_kv_heads;
+    io.rot_dim = a->rot_dim;
+    io.interleaved = a->interleaved;
+    io.max_positions = a->rot_dim ? a->max_positions : 0x7fffffff;
+    int prev = 0;
+    s = set_device(h, &prev);
+    if (s != KVEC_OK) return s;
+    DeviceGuard guard{prev, h->device};
+    cudaError_t e = launch_rotate(io, v, reinterpret_cast<cudaStream_t>(stream));
+    if (e != cudaSuccess) return cuda_fail(e, "rotate launch");
+    return KVEC_OK;
+}
+
+size_t kvec_paged_decode_bytes(kvec_handle* h, int batch, int max_len, int with_weights) {
+    if (!h || batch < 1 || batch > h->p.max_batch || max_len < 1 || max_len > kPagedMaxLen) return 0;
+    return paged_decode_scratch(batch, h->p.num_q_heads, h->p.num_kv_heads, max_len, with_weights != 0, h->num_sms);
+}
+
+kvec_status kvec_paged_decode(kvec_handle* h, int batch, const void* q, const kvec_paged_cache* cache, int max_len,
+                              int window, int sinks, void* out, void* scratch, size_t scratch_bytes,
+                              kvec_stream_t stream) {
+    PagedCacheView v{};
+    kvec_status s = view_cache(cache, &v);
+    if (s == KVEC_OK) s = check_window(window, sinks);
+    if (s != KVEC_OK) return s;
+    if (max_len < 1 || max_len > v.capacity)
+        return fail(KVEC_ERR_INVALID_ARG, "max_len %d outside [1, max_pages * page_size = %d]", max_len, v.capacity);
+    s = check_paged_handle(h, batch, &v);
+    if (s != KVEC_OK) return s;
+    if (h->g > 8)
+        return fail(KVEC_ERR_UNSUPPORTED, "decode attention supports up to 8 query heads per KV head (g = %d)", h->g);
+    if (!q || !out || !scratch) return fail(KVEC_ERR_INVALID_ARG, "a device pointer is NULL");
+    if (!aligned16(q) || !aligned16(out) || !aligned16(scratch))
+        return fail(KVEC_ERR_INVALID_ARG, "q, out and scratch must be 16-byte aligned");
+    const size_t need = kvec_paged_decode_bytes(h, batch, max_len, v.weights != nullptr);
+    if (scratch_bytes < need)
+        return fail(KVEC_ERR_INVALID_ARG, "scratch of %zu bytes, %zu are needed", scratch_bytes, need);
+    PagedDecodeIO io{};
+    io.q = static_cast<const uint16_t*>(q);
+    io.out = static_cast<uint16_t*>(out);
+    io.scratch = scratch;
+    io.err = h->sc.err;
+    io.batch = batch;
+    io.Hq = h->p.num_q_heads;
+    io.Hkv = h->p.num_kv_heads;
+    io.max_len = max_len;
+    io.window = window;
+    io.sinks = sinks;
+    io.scale = softmax_scale_of(h->p);
+    int prev = 0;
+    s = set_device(h, &prev);
+    if (s != KVEC_OK) return s;
+    DeviceGuard guard{prev, h->device};
+    cudaError_t e = launch_paged_decode(io, v, h->num_sms, reinterpret_cast<cudaStream_t>(stream));
+    if (e != cudaSuccess) return cuda_fail(e, "paged decode launch");
+    return KVEC_OK;
+}
+
+kvec_status kvec_paged_evict(kvec_handle* h, int batch, const kvec_paged_cache* cache, const int32_t* new_table,
+                             int new_max_pages, int max_len, int budget, int sinks, int recent, int32_t* new_lens,
+                             int32_t* kept, kvec_stream_t stream) {
+    PagedCacheView v{};
+    kvec_status s = view_cache(cache, &v);
+    if (s != KVEC_OK) return s;
+    if (!v.weights) return fail(KVEC_ERR_INVALID_ARG, "the cache keeps no weights to rank by");
+    if (max_len < 1 || max_len > v.capacity)
+        return fail(KVEC_ERR_INVALID_ARG, "max_len %d outside [1, max_pages * page_size = %d]", max_len, v.capacity);
+    if (budget < 1 || budget > kPagedMaxLen) return fail(KVEC_ERR_INVALID_ARG, "budget %d outside [1, %d]", budget, kPagedMaxLen);
+    if (sinks < 0 || recent < 0 || (long long)sinks + recent > budget)
+        return fail(KVEC_ERR_INVALID_ARG, "need sinks, recent >= 0 and sinks + recent <= budget");
+    if (new_max_pages < 1 || ((long long)new_max_pages << v.log_page) < std::min(budget, max_len))
+        return fail(KVEC_ERR_INVALID_ARG, "new_table's %d pages of a sequence hold fewer than min(budget, max_len) slots",
+                    new_max_pages);
+    s = check_paged_handle(h, batch, &v);
+    if (s != KVEC_OK) return s;
+    if (!new_table || !new_lens || !kept) return fail(KVEC_ERR_INVALID_ARG, "a device pointer is NULL");
+    if (new_table == v.table || new_lens == v.lens)
+        return fail(KVEC_ERR_INVALID_ARG, "new_table and new_lens must not be the cache's");
+    for (const int32_t* p : {new_table, static_cast<const int32_t*>(new_lens), static_cast<const int32_t*>(kept)})
+        if (reinterpret_cast<uintptr_t>(p) % 4)
+            return fail(KVEC_ERR_INVALID_ARG, "new_table, new_lens and kept must be 4-byte aligned");
+    EvictIO io{};
+    io.new_table = new_table;
+    io.new_lens = new_lens;
+    io.kept = kept;
+    io.batch = batch;
+    io.Hkv = h->p.num_kv_heads;
+    io.new_max_pages = new_max_pages;
+    io.max_len = max_len;
+    io.budget = budget;
+    io.sinks = sinks;
+    io.recent = recent;
+    int prev = 0;
+    s = set_device(h, &prev);
+    if (s != KVEC_OK) return s;
+    DeviceGuard guard{prev, h->device};
+    cudaError_t e = launch_evict(io, v, reinterpret_cast<cudaStream_t>(stream));
+    if (e != cudaSuccess) return cuda_fail(e, "evict launch");
     return KVEC_OK;
 }
 

@@ -112,6 +112,54 @@ struct DecodeIO {
     float scale;              // softmax scale
 };
 
+// A paged cache as its kernels see it (kvec_paged_cache): rows of kHeadDim values, row
+// (page * Hkv + h) << log_page | slot within the page.
+struct PagedCacheView {
+    uint16_t* k;              // null: no cache
+    uint16_t* v;
+    float* weights;           // null: none kept
+    const int* table;         // [batch][max_pages]
+    const int* lens;          // [batch]
+    int dtype;                // kvec_dtype
+    int log_page, num_pages, max_pages;
+    int capacity;             // max_pages << log_page
+};
+
+// New tokens' norms, rotation and store (rotate_kernel.cu).
+struct RotateIO {
+    const uint16_t *q, *k, *v;
+    long long q_stride, k_stride, v_stride;   // elements
+    const uint16_t *q_norm, *k_norm;          // [d] or null
+    const float* rot_table;                   // [max_positions][rot_dim]
+    const int* positions;
+    const int* cu;                            // [batch + 1], or null: a token a sequence
+    uint16_t *q_out, *k_out;
+    float eps;
+    int dtype, num_tokens, batch, Hq, Hkv, rot_dim, interleaved, max_positions;
+};
+
+// One new token's attention over a paged cache (paged_decode_kernel.cu).
+struct PagedDecodeIO {
+    const uint16_t* q;        // [batch][Hq][d]
+    uint16_t* out;            // [batch][Hq][d]
+    void* scratch;
+    int* err;
+    int batch, Hq, Hkv;
+    int max_len;              // bound on the lengths, within the cache's capacity
+    int window, sinks;
+    float scale;
+};
+
+// Eviction by accumulated weight (evict_kernel.cu).
+struct EvictIO {
+    const int* new_table;     // [batch][new_max_pages]
+    int* new_lens;            // [batch]
+    int* kept;                // [batch][Hkv][budget]
+    int batch, Hkv, new_max_pages;
+    int max_len;              // bound on the lengths, within the cache's capacity
+    int budget, sinks, recent;
+};
+
 // ---------------------------------------------------------------- helpers
 
 __device__ __forceinline__ uint32_t float_order_key(float f) {
@@ -234,6 +282,10 @@ cudaError_t launch_finalize(const Geometry& g, const LayerIO& io, const Scratch&
 cudaError_t launch_ada(const Geometry& g, const LayerIO& io, const Scratch& sc, const Slot& sl, cudaStream_t st,
                        int priority, int ncall);
 cudaError_t launch_decode(const DecodeIO& io, int num_sms, cudaStream_t st);
+cudaError_t launch_rotate(const RotateIO& io, const PagedCacheView& c, cudaStream_t st);
+cudaError_t launch_paged_decode(const PagedDecodeIO& io, const PagedCacheView& c, int num_sms, cudaStream_t st);
+size_t paged_decode_scratch(int batch, int Hq, int Hkv, int max_len, bool weights, int num_sms);
+cudaError_t launch_evict(const EvictIO& io, const PagedCacheView& c, cudaStream_t st);
 // out_idx from the slot's kept-position bits, then the K/V rows.
 cudaError_t launch_gather(const Geometry& g, const Group& gr, cudaStream_t st, int priority, bool programmatic);
 
@@ -249,5 +301,10 @@ cudaError_t configure_window(const Geometry& g);
 cudaError_t configure_select();
 cudaError_t configure_chain();
 cudaError_t configure_decode();
+cudaError_t configure_paged_decode();
+
+// A tiled tensor map of 16-bit elements with the 128-byte swizzle; strides in bytes, of dimensions 1 up.
+cudaError_t encode_tensor_map(CUtensorMap* map, int dtype, int rank, const void* base, const uint64_t* dims,
+                              const uint64_t* strides, const uint32_t* box);
 
 }  // namespace kvec

@@ -29,7 +29,11 @@ EXPORTED = ("kvec_create", "kvec_destroy", "kvec_state_bytes", "kvec_reset", "kv
             "kvec_select_layers", "kvec_debug_scores", "kvec_sync_status", "kvec_set_profiling",
             "kvec_kernel_time", "kvec_status_string", "kvec_last_error", "kvec_select_layer_noalloc",
             "kvec_select_layer_lse", "kvec_select_layers_lse", "kvec_decode_attention",
-            "kvec_noalloc_sync_status", "kvec_set_test_fault", "kvec_output_capacity")
+            "kvec_noalloc_sync_status", "kvec_set_test_fault", "kvec_output_capacity",
+            "kvec_rotate_append", "kvec_paged_decode_bytes", "kvec_paged_decode", "kvec_paged_evict")
+
+KVEC_BF16 = 0
+KVEC_FP16 = 1
 
 
 class KvecUnavailable(ImportError):
@@ -60,6 +64,26 @@ class kvec_debug_view(ctypes.Structure):
         ("sigma", ctypes.c_void_p), ("htop", ctypes.c_void_p), ("pres_bits", ctypes.c_void_p),
         ("Pprime", ctypes.c_void_p), ("row_stats", ctypes.c_void_p),
         ("max_seqlen", ctypes.c_int), ("words_per_row", ctypes.c_int),
+    ]
+
+
+class kvec_paged_cache(ctypes.Structure):
+    _fields_ = [
+        ("dtype", ctypes.c_int), ("page_size", ctypes.c_int), ("num_pages", ctypes.c_int), ("max_pages", ctypes.c_int),
+        ("k_pages", ctypes.c_void_p), ("v_pages", ctypes.c_void_p), ("weights", ctypes.c_void_p),
+        ("page_table", ctypes.c_void_p), ("lens", ctypes.c_void_p),
+    ]
+
+
+class kvec_rotate_args(ctypes.Structure):
+    _fields_ = [
+        ("dtype", ctypes.c_int), ("num_tokens", ctypes.c_int),
+        ("q", ctypes.c_void_p), ("k", ctypes.c_void_p), ("v", ctypes.c_void_p),
+        ("q_stride", ctypes.c_int64), ("k_stride", ctypes.c_int64), ("v_stride", ctypes.c_int64),
+        ("q_norm", ctypes.c_void_p), ("k_norm", ctypes.c_void_p), ("eps", ctypes.c_float),
+        ("rot_dim", ctypes.c_int), ("interleaved", ctypes.c_int), ("max_positions", ctypes.c_int),
+        ("rot_table", ctypes.c_void_p), ("positions", ctypes.c_void_p),
+        ("q_out", ctypes.c_void_p), ("k_out", ctypes.c_void_p),
     ]
 
 
@@ -101,6 +125,12 @@ def load() -> ctypes.CDLL:
             "kvec_noalloc_sync_status": ([_vp], st),
             "kvec_set_test_fault": ([i], None),
             "kvec_output_capacity": ([ctypes.POINTER(kvec_params), i], i),
+            "kvec_rotate_append": ([_vp, ctypes.POINTER(kvec_rotate_args), i, _vp, ctypes.POINTER(kvec_paged_cache),
+                                    _vp], st),
+            "kvec_paged_decode_bytes": ([_vp, i, i, i], ctypes.c_size_t),
+            "kvec_paged_decode": ([_vp, i, _vp, ctypes.POINTER(kvec_paged_cache), i, i, i, _vp, _vp, ctypes.c_size_t,
+                                   _vp], st),
+            "kvec_paged_evict": ([_vp, i, ctypes.POINTER(kvec_paged_cache), _vp, i, i, i, i, i, _vp, _vp, _vp], st),
         }
         for name, (args, res) in sig.items():
             fn = getattr(lib, name)
@@ -202,6 +232,27 @@ def kvec_decode_attention(handle: int, batch: int, q: int, k_cache: int, v_cache
     _check(load().kvec_decode_attention(handle, int(batch), q, k_cache, v_cache, lens, int(cap), out, stream))
 
 
+def kvec_rotate_append(handle: int, args: kvec_rotate_args, batch: int, cu_tokens: Optional[int] = None,
+                       cache: Optional[kvec_paged_cache] = None, stream: int = 0) -> None:
+    _check(load().kvec_rotate_append(handle, args, batch, cu_tokens, cache, stream))
+
+
+def kvec_paged_decode_bytes(handle: int, batch: int, max_len: int, with_weights: bool) -> int:
+    return int(load().kvec_paged_decode_bytes(handle, batch, max_len, 1 if with_weights else 0))
+
+
+def kvec_paged_decode(handle: int, batch: int, q: int, cache: kvec_paged_cache, max_len: int, window: int, sinks: int,
+                      out: int, scratch: int, scratch_bytes: int, stream: int = 0) -> None:
+    _check(load().kvec_paged_decode(handle, batch, q, cache, max_len, window, sinks, out, scratch, scratch_bytes,
+                                    stream))
+
+
+def kvec_paged_evict(handle: int, batch: int, cache: kvec_paged_cache, new_table: int, new_max_pages: int, max_len: int,
+                     budget: int, sinks: int, recent: int, new_lens: int, kept: int, stream: int = 0) -> None:
+    _check(load().kvec_paged_evict(handle, batch, cache, new_table, new_max_pages, max_len, budget, sinks, recent,
+                                   new_lens, kept, stream))
+
+
 def kvec_debug_scores(handle: int) -> kvec_debug_view:
     view = kvec_debug_view()
     _check(load().kvec_debug_scores(handle, ctypes.byref(view)))
@@ -254,6 +305,48 @@ class _DeviceArray:
                                          "version": 3, "strides": None}
 
 
+def _dtype_code(t, dtype) -> int:
+    if dtype is t.bfloat16:
+        return KVEC_BF16
+    if dtype is t.float16:
+        return KVEC_FP16
+    raise KvecError(KVEC_ERR_INVALID_ARG, f"dtype {dtype} is neither bfloat16 nor float16")
+
+
+def _want(ok: bool, message: str) -> None:
+    if not ok:
+        raise KvecError(KVEC_ERR_INVALID_ARG, message)
+
+
+class PagedCache:
+    """A paged cache (kvec_paged_cache): holds its tensors, computes nothing.
+
+    k_pages, v_pages bf16 or fp16 [num_pages][H_kv][page_size][d]; page_table int32 [batch][max_pages];
+    lens int32 [batch]; weights fp32 [num_pages][H_kv][page_size] or None.  All contiguous, on one device."""
+
+    def __init__(self, k_pages, v_pages, page_table, lens, weights=None):
+        import torch as t
+        self.dtype_code = _dtype_code(t, k_pages.dtype)
+        _want(k_pages.dim() == 4 and v_pages.shape == k_pages.shape and v_pages.dtype == k_pages.dtype,
+              "k_pages and v_pages must be [num_pages][H_kv][page_size][d], of one type")
+        _want(page_table.dim() == 2 and page_table.dtype == t.int32 and page_table.shape[1] >= 1,
+              "page_table must be int32 [batch][max_pages]")
+        _want(lens.dtype == t.int32 and tuple(lens.shape) == (page_table.shape[0],), "lens must be int32 [batch]")
+        _want(weights is None or (weights.dtype == t.float32 and weights.shape == k_pages.shape[:3]),
+              "weights must be fp32 [num_pages][H_kv][page_size]")
+        parts = [x for x in (k_pages, v_pages, page_table, lens, weights) if x is not None]
+        _want(all(x.is_contiguous() for x in parts), "a cache's tensors must be contiguous")
+        _want(all(x.device == k_pages.device for x in parts), "a cache's tensors must be on one device")
+        self.k_pages, self.v_pages, self.page_table, self.lens, self.weights = k_pages, v_pages, page_table, lens, weights
+        self.batch, self.max_pages = page_table.shape
+        self.page_size = k_pages.shape[2]
+        self.capacity = self.max_pages * self.page_size
+        self.dtype, self.device = k_pages.dtype, k_pages.device
+        self.c = kvec_paged_cache(self.dtype_code, self.page_size, k_pages.shape[0], self.max_pages,
+                                  k_pages.data_ptr(), v_pages.data_ptr(),
+                                  None if weights is None else weights.data_ptr(), page_table.data_ptr(), lens.data_ptr())
+
+
 class KvecSelector:
     """Owns a kvec handle; torch tensors in, torch tensors out.  Marshalling only.
 
@@ -264,7 +357,9 @@ class KvecSelector:
         import torch
         self._torch = torch
         self.params = params
+        self.handle = None
         self.handle = kvec_create(params)
+        self.device = torch.device("cuda", torch.cuda.current_device())
         self.state_bytes = kvec_state_bytes(params.max_seqlen)
 
     def close(self) -> None:
@@ -339,6 +434,136 @@ class KvecSelector:
         kvec_decode_attention(self.handle, batch, q.data_ptr(), k_cache.data_ptr(), v_cache.data_ptr(),
                               lens.data_ptr(), cap, out.data_ptr(), s.cuda_stream)
         return out
+
+    # ------------------------------------------------------------ decoding over pages
+
+    def _stream(self, stream, device):
+        """The stream of a call on tensors of `device`, which must be the handle's."""
+        _want(device == self.device, f"the tensors are on {device}, the handle on {self.device}")
+        return self._torch.cuda.current_stream(device) if stream is None else stream
+
+    def _empty(self, shape, dtype, stream):
+        """Memory that work on `stream` may use at once, from that stream's pool."""
+        t = self._torch
+        if stream == t.cuda.current_stream(self.device):
+            return t.empty(shape, dtype=dtype, device=self.device)
+        with t.cuda.stream(stream):
+            return t.empty(shape, dtype=dtype, device=self.device)
+
+    def _heads(self, x, heads, name, dtype, device):
+        """Checks token rows [T][heads][d] with contiguous heads; their stride in elements."""
+        d = self.params.head_dim
+        _want(x.dim() == 3 and x.shape[1] == heads and x.shape[2] == d and x.dtype == dtype and x.device == device,
+              f"{name} must be {dtype} [T][{heads}][{d}] on {device}")
+        st = x.stride()
+        _want(st[2] == 1 and st[1] == d, f"{name}'s heads must lie side by side")
+        return st[0] if x.shape[0] > 1 else heads * d
+
+    def _check_cache(self, cache):
+        _want(cache.k_pages.shape[1] == self.params.num_kv_heads and cache.k_pages.shape[3] == self.params.head_dim,
+              f"the cache's pages must have {self.params.num_kv_heads} KV heads of {self.params.head_dim}")
+
+    def rotate_append(self, q, k, v, positions, rot_table=None, cache=None, cu_tokens=None, q_norm=None, k_norm=None,
+                      eps: float = 1e-6, interleaved: bool = False, q_out=None, k_out=None, stream=None):
+        """Norms of new tokens' queries and keys, rotation, and the store into the cache (kvec_rotate_append).
+
+        q [T][H_q][d], k, v [T][H_kv][d], tokens any multiple of 8 elements apart; positions int32 [T];
+        rot_table fp32 [max_positions][rot_dim]; cu_tokens int32 [batch + 1] on the device (None: a token a sequence).
+        Without a cache k_out is made and (q_out, k_out) returned; with one q_out, or both where k_out is given."""
+        t, p = self._torch, self.params
+        T, dtype, dev = q.shape[0], q.dtype, q.device
+        a = kvec_rotate_args(dtype=_dtype_code(t, dtype), num_tokens=T, eps=eps, interleaved=1 if interleaved else 0)
+        a.q_stride = self._heads(q, p.num_q_heads, "q", dtype, dev)
+        a.k_stride = self._heads(k, p.num_kv_heads, "k", dtype, dev)
+        _want(k.shape[0] == T and positions.dtype == t.int32 and tuple(positions.shape) == (T,) and
+              positions.is_contiguous() and positions.device == dev, "k and int32 positions must be of q's tokens")
+        a.q, a.k, a.positions = q.data_ptr(), k.data_ptr(), positions.data_ptr()
+        if v is not None:
+            a.v_stride = self._heads(v, p.num_kv_heads, "v", dtype, dev)
+            _want(v.shape[0] == T, "v must be of q's tokens")
+            a.v = v.data_ptr()
+        if rot_table is not None:
+            _want(rot_table.dim() == 2 and rot_table.dtype == t.float32 and rot_table.is_contiguous() and
+                  rot_table.device == dev, "rot_table must be contiguous fp32 [max_positions][rot_dim]")
+            a.max_positions, a.rot_dim = rot_table.shape
+            a.rot_table = rot_table.data_ptr()
+        for name, w in (("q_norm", q_norm), ("k_norm", k_norm)):
+            if w is not None:
+                _want(w.dtype == dtype and tuple(w.shape) == (p.head_dim,) and w.is_contiguous() and w.device == dev,
+                      f"{name} must be {dtype} [{p.head_dim}]")
+                setattr(a, name, w.data_ptr())
+        batch = T
+        if cu_tokens is not None:
+            _want(cu_tokens.dtype == t.int32 and cu_tokens.dim() == 1 and cu_tokens.is_contiguous() and
+                  cu_tokens.device == dev, "cu_tokens must be int32 [batch + 1] on the device")
+            batch = cu_tokens.shape[0] - 1
+        if cache is not None:
+            self._check_cache(cache)
+            _want(cache.batch == batch and cache.device == dev, f"the cache has {cache.batch} sequences, the call {batch}")
+        for name, x, like in (("q_out", q_out, q), ("k_out", k_out, k)):
+            _want(x is None or (x.shape == like.shape and x.dtype == dtype and x.is_contiguous() and x.device == dev),
+                  f"{name} must be contiguous, of its input's shape and type")
+        want_k = cache is None or k_out is not None
+        stream = self._stream(stream, dev)
+        if q_out is None:
+            q_out = self._empty((T, p.num_q_heads, p.head_dim), dtype, stream)
+        if cache is None and k_out is None:
+            k_out = self._empty((T, p.num_kv_heads, p.head_dim), dtype, stream)
+        a.q_out, a.k_out = q_out.data_ptr(), None if k_out is None else k_out.data_ptr()
+        if T:
+            kvec_rotate_append(self.handle, a, batch, None if cu_tokens is None else cu_tokens.data_ptr(),
+                               None if cache is None else cache.c, stream.cuda_stream)
+        return (q_out, k_out) if want_k else q_out
+
+    def paged_decode(self, q, cache, max_len: Optional[int] = None, window: int = 0, sinks: int = 0, out=None,
+                     stream=None):
+        """One new token per sequence over a paged cache (kvec_paged_decode); adds to cache.weights where it has them.
+
+        q [batch][H_q][d] of the cache's type, contiguous; max_len: a bound on the lengths (the capacity)."""
+        t, p = self._torch, self.params
+        batch, dev = cache.batch, cache.device
+        self._check_cache(cache)
+        shape = (batch, p.num_q_heads, p.head_dim)
+        _want(tuple(q.shape) == shape and q.dtype == cache.dtype and q.is_contiguous() and q.device == dev,
+              f"q must be contiguous {cache.dtype} {list(shape)} on {dev}")
+        stream = self._stream(stream, dev)
+        if out is None:
+            out = self._empty(shape, q.dtype, stream)
+        else:
+            _want(tuple(out.shape) == shape and out.dtype == q.dtype and out.is_contiguous() and out.device == dev,
+                  "out must be as q")
+        max_len = cache.capacity if max_len is None else max_len
+        need = kvec_paged_decode_bytes(self.handle, batch, max_len, cache.weights is not None)
+        scratch = self._empty(max(need, 16), t.uint8, stream)
+        kvec_paged_decode(self.handle, batch, q.data_ptr(), cache.c, max_len, window, sinks, out.data_ptr(),
+                          scratch.data_ptr(), need, stream.cuda_stream)
+        return out
+
+    def paged_evict(self, cache, new_table, budget: int, sinks: int = 0, recent: int = 0, max_len: Optional[int] = None,
+                    new_lens=None, kept=None, stream=None):
+        """Eviction by accumulated weight to the pages of new_table (kvec_paged_evict).
+
+        new_table int32 [batch][pages], contiguous, of pages that page_table does not use.  Returns (new_lens int32
+        [batch], kept int32 [batch][H_kv][budget])."""
+        t, p = self._torch, self.params
+        batch, dev = cache.batch, cache.device
+        self._check_cache(cache)
+        _want(new_table.dim() == 2 and new_table.shape[0] == batch and new_table.dtype == t.int32 and
+              new_table.is_contiguous() and new_table.device == dev, f"new_table must be int32 [{batch}][pages] on {dev}")
+        _want(budget >= 1, f"budget {budget} < 1")
+        stream = self._stream(stream, dev)
+        if new_lens is None:
+            new_lens = self._empty(batch, t.int32, stream)
+        if kept is None:
+            kept = self._empty((batch, p.num_kv_heads, budget), t.int32, stream)
+        _want(new_lens.dtype == t.int32 and tuple(new_lens.shape) == (batch,) and new_lens.is_contiguous() and
+              new_lens.device == dev, "new_lens must be int32 [batch]")
+        _want(kept.dtype == t.int32 and tuple(kept.shape) == (batch, p.num_kv_heads, budget) and kept.is_contiguous() and
+              kept.device == dev, "kept must be int32 [batch][H_kv][budget]")
+        kvec_paged_evict(self.handle, batch, cache.c, new_table.data_ptr(), new_table.shape[1],
+                         cache.capacity if max_len is None else max_len, budget, sinks, recent, new_lens.data_ptr(),
+                         kept.data_ptr(), stream.cuda_stream)
+        return new_lens, kept
 
     def debug(self, device="cuda"):
         """Copies of the last layer's intermediates (see kvec_debug_view)."""
