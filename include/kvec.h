@@ -376,6 +376,27 @@ KVEC_API kvec_status kvec_paged_evict(kvec_handle* h, int batch, const kvec_page
                                       int sinks, int recent, int32_t* new_lens, int32_t* kept,
                                       kvec_stream_t stream);
 
+/* Causal attention of packed sequences, optionally with a sliding window and first tokens
+ * that stay visible, and the log-sum-exp of every row: the prefill step before
+ * kvec_select_layer_lse.  Sequence s has L_q query rows and L_k keys (cu_q, cu_k: host and
+ * device copies as for kvec_select_layer, lengths may be 0); its rows are its last
+ * positions, row i at p = L_k - L_q + i.  Key t is visible to it if t <= p and (window = 0
+ * or t > p - window or t < sinks):
+ *   out = softmax over the visible t of scale * <q, k_t>, times v_t;
+ *   lse = ln sum over the visible t of exp(scale * <q, k_t>).
+ * A row that sees nothing (p < 0) gives zeros and -infinity.  Keys and values that a row does
+ * not see have no effect on it, whatever they hold.
+ *   q    device dtype [cu_q[batch]][H_q][d];  k, v device dtype [cu_k[batch]][H_kv][d].
+ *   out  device dtype, as q;  lse device fp32 [cu_q[batch]][H_q], or NULL.
+ * Lengths up to 2^20; the weights are rounded to dtype before they meet the values, the sums
+ * are fp32.  A bounded wait that gave up is reported by kvec_sync_status. */
+KVEC_API kvec_status kvec_prefill_attention(kvec_handle* h, int dtype, int batch,
+                                            const int32_t* cu_q_host, const int32_t* cu_q_dev,
+                                            const int32_t* cu_k_host, const int32_t* cu_k_dev,
+                                            const void* q, const void* k, const void* v,
+                                            int window, int sinks, void* out, float* lse,
+                                            kvec_stream_t stream);
+
 /* Device views of the last processed layer's intermediates (valid until the
  * next call on the handle; read after synchronising the stream).  Row strides
  * use ML = max_seqlen + 4 rounded up to a multiple of 32 (reported in max_seqlen).

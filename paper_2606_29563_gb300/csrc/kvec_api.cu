@@ -740,6 +740,7 @@ kvec_status kvec_create(const kvec_params* params, kvec_handle** out) {
     if (e == cudaSuccess) e = configure_chain();
     if (e == cudaSuccess) e = configure_decode();
     if (e == cudaSuccess) e = configure_paged_decode();
+    if (e == cudaSuccess) e = configure_prefill();
     if (e == cudaSuccess) e = cudaDeviceGetStreamPriorityRange(&h->prio_lo, &h->prio_hi);
     for (cudaStream_t* st : {&h->s_score, &h->s_gather, &h->s_cap})
         if (e == cudaSuccess) e = cudaStreamCreateWithPriority(st, cudaStreamNonBlocking, h->prio_lo);
@@ -1375,6 +1376,64 @@ kvec_status kvec_paged_evict(kvec_handle* h, int batch, const kvec_paged_cache* 
     DeviceGuard guard{prev, h->device};
     cudaError_t e = launch_evict(io, v, reinterpret_cast<cudaStream_t>(stream));
     if (e != cudaSuccess) return cuda_fail(e, "evict launch");
+    return KVEC_OK;
+}
+
+kvec_status kvec_prefill_attention(kvec_handle* h, int dtype, int batch, const int32_t* cu_q_host,
+                                   const int32_t* cu_q_dev, const int32_t* cu_k_host, const int32_t* cu_k_dev,
+                                   const void* q, const void* k, const void* v, int window, int sinks, void* out,
+                                   float* lse, kvec_stream_t stream) {
+    if (dtype != KVEC_BF16 && dtype != KVEC_FP16)
+        return fail(KVEC_ERR_INVALID_ARG, "dtype %d is neither KVEC_BF16 nor KVEC_FP16", dtype);
+    kvec_status s = check_window(window, sinks);
+    if (s != KVEC_OK) return s;
+    if (batch < 1 || batch > kMaxGridBatch) return fail(KVEC_ERR_INVALID_ARG, "batch %d outside [1, %d]", batch, kMaxGridBatch);
+    if (!cu_q_host || !cu_q_dev || !cu_k_host || !cu_k_dev)
+        return fail(KVEC_ERR_INVALID_ARG, "cu_seqlens pointers must not be NULL");
+    if (cu_q_host[0] != 0 || cu_k_host[0] != 0) return fail(KVEC_ERR_INVALID_ARG, "cu_q[0] and cu_k[0] must be 0");
+    int max_q = 0;
+    for (int b = 0; b < batch; ++b) {
+        const long long lq = (long long)cu_q_host[b + 1] - cu_q_host[b], lk = (long long)cu_k_host[b + 1] - cu_k_host[b];
+        if (lq < 0 || lk < 0 || lq > kPagedMaxLen || lk > kPagedMaxLen)
+            return fail(KVEC_ERR_INVALID_ARG, "sequence %d has %lld queries and %lld keys, outside [0, %d]", b, lq, lk, kPagedMaxLen);
+        max_q = std::max(max_q, (int)lq);
+    }
+    s = check_paged_handle(h, batch, nullptr);
+    if (s != KVEC_OK) return s;
+    if (h->g > 8)
+        return fail(KVEC_ERR_UNSUPPORTED, "prefill attention supports up to 8 query heads per KV head (g = %d)", h->g);
+    if (max_q == 0) return KVEC_OK;
+    const int total_k = cu_k_host[batch];
+    if (!q || !out || (total_k > 0 && (!k || !v))) return fail(KVEC_ERR_INVALID_ARG, "a device pointer is NULL");
+    if (!aligned16(q) || !aligned16(k) || !aligned16(v) || !aligned16(out))
+        return fail(KVEC_ERR_INVALID_ARG, "q, k, v and out must be 16-byte aligned");
+    if (reinterpret_cast<uintptr_t>(lse) % 4 || reinterpret_cast<uintptr_t>(cu_q_dev) % 4 || reinterpret_cast<uintptr_t>(cu_k_dev) % 4)
+        return fail(KVEC_ERR_INVALID_ARG, "lse and the device cu_seqlens must be 4-byte aligned");
+    PrefillIO io{};
+    io.q = static_cast<const uint16_t*>(q);
+    io.k = static_cast<const uint16_t*>(k);
+    io.v = static_cast<const uint16_t*>(v);
+    io.cu_q = cu_q_dev;
+    io.cu_k = cu_k_dev;
+    io.out = static_cast<uint16_t*>(out);
+    io.lse = lse;
+    io.err = h->sc.err;
+    io.dtype = dtype;
+    io.batch = batch;
+    io.Hq = h->p.num_q_heads;
+    io.Hkv = h->p.num_kv_heads;
+    io.total_q = cu_q_host[batch];
+    io.total_k = total_k;
+    io.max_q = max_q;
+    io.window = window;
+    io.sinks = sinks;
+    io.scale = softmax_scale_of(h->p);
+    int prev = 0;
+    s = set_device(h, &prev);
+    if (s != KVEC_OK) return s;
+    DeviceGuard guard{prev, h->device};
+    cudaError_t e = launch_prefill(io, reinterpret_cast<cudaStream_t>(stream));
+    if (e != cudaSuccess) return cuda_fail(e, "prefill attention launch");
     return KVEC_OK;
 }
 

@@ -160,6 +160,20 @@ struct EvictIO {
     int budget, sinks, recent;
 };
 
+// Causal attention of packed sequences (prefill_kernel.cu).
+struct PrefillIO {
+    const uint16_t *q, *k, *v;
+    const int *cu_q, *cu_k;   // device [batch + 1]
+    uint16_t* out;
+    float* lse;               // [total_q][Hq] or null
+    int* err;
+    int dtype, batch, Hq, Hkv;
+    int total_q, total_k;
+    int max_q;                // the longest sequence's queries
+    int window, sinks;
+    float scale;
+};
+
 // ---------------------------------------------------------------- helpers
 
 __device__ __forceinline__ uint32_t float_order_key(float f) {
@@ -286,6 +300,7 @@ cudaError_t launch_rotate(const RotateIO& io, const PagedCacheView& c, cudaStrea
 cudaError_t launch_paged_decode(const PagedDecodeIO& io, const PagedCacheView& c, int num_sms, cudaStream_t st);
 size_t paged_decode_scratch(int batch, int Hq, int Hkv, int max_len, bool weights, int num_sms);
 cudaError_t launch_evict(const EvictIO& io, const PagedCacheView& c, cudaStream_t st);
+cudaError_t launch_prefill(const PrefillIO& io, cudaStream_t st);
 // out_idx from the slot's kept-position bits, then the K/V rows.
 cudaError_t launch_gather(const Geometry& g, const Group& gr, cudaStream_t st, int priority, bool programmatic);
 
@@ -302,6 +317,7 @@ cudaError_t configure_select();
 cudaError_t configure_chain();
 cudaError_t configure_decode();
 cudaError_t configure_paged_decode();
+cudaError_t configure_prefill();
 
 // A tiled tensor map of 16-bit elements with the 128-byte swizzle; strides in bytes, of dimensions 1 up.
 cudaError_t encode_tensor_map(CUtensorMap* map, int dtype, int rank, const void* base, const uint64_t* dims,

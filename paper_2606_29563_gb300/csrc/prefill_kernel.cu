@@ -1,0 +1,523 @@
+// Causal attention of packed sequences with an optional sliding window and first tokens
+// that stay visible, and each row's log-sum-exp:
+//   s = scale log2(e) Q K^T,  out = sum_t 2^(s_t - m) v_t / l,  l = sum_t 2^(s_t - m),
+//   lse = ln 2 (m + log2 l),
+// over the keys t <= p that a row at position p sees (t > p - window or t < sinks).
+//
+// A CTA owns two tiles of 128 rows; a row is a (query, query head) pair, the g query heads
+// of one KV head side by side, so that one query fills g rows and both tiles read the same
+// K and V.  It walks the 128-key blocks that any of its rows sees:
+//   warps 0-3, 4-7  softmax of tile 0 and 1, one thread a row: S from TMEM, running maximum
+//                   and sum, the weights back to TMEM as 16-bit values over S;
+//   warp 8          TMA: the query rows once, then K and V blocks through a ring;
+//   warp 9          tcgen05.mma: S = Q K^T (both from shared memory), O += P V (P from TMEM,
+//                   V column-major from shared memory), for the tiles in turn, so that one
+//                   tile's softmax runs beside the other's products;
+//   warps 10, 11    blocks that some row does not see wholly: zero what V holds there of
+//                   infinities and NaN, which a weight of zero would not keep out.  What a row
+//                   sees of them is added at the end (add_unbounded).
+// The row maximum that the weights refer to moves only when a row's weights would pass 2^8
+// (kRescale): O is then scaled in TMEM, once in a while instead of at every block.
+#include <algorithm>
+
+#include "half_types.cuh"
+#include "kvec_internal.cuh"
+#include "sm100_ptx.cuh"
+
+namespace kvec {
+
+namespace {
+
+constexpr int kPfTile = 128;                        // rows of a tile, keys of a block
+constexpr int kPfHalf = kPfTile * 128;              // bytes of 128 rows x 64 columns
+constexpr int kPfBuf = 2 * kPfHalf;                 // a tile or block: 32 KB
+constexpr int kPfStages = 5;
+constexpr int kPfThreads = 384;
+constexpr uint32_t kPfTmem = 512;                   // S0 | S1 | O0 | O1, 128 columns each
+constexpr float kRescale = 8.f;
+// The maximum before the first visible logit, finite: 2^(-inf - it) is 0.
+constexpr float kNoLogit = -3.402823466e38f;
+
+struct PfArgs {
+    CUtensorMap qmap, kmap, vmap;
+    PrefillIO io;
+    int g, nq;       // query heads of a KV head, queries of a tile
+    int pairs;       // tile pairs of the longest sequence
+    float sl2;
+};
+
+struct __align__(8) PfBarriers {
+    uint64_t full[kPfStages], empty[kPfStages];
+    uint64_t q_full, dirty, clean, mma_done;   // dirty, clean: V of a block of partial sight is there / cleaned
+    uint64_t s_full[2], p_full[2], o_done[2];
+    uint32_t tmem_base;
+    volatile int abort_flag;
+    volatile int unbounded;      // a block of partial sight held an infinity or NaN in V
+};
+
+constexpr int kPfSmem = 1024 + (2 + kPfStages) * kPfBuf + (int)sizeof(PfBarriers);
+
+// What a CTA works on: tiles 2 p and 2 p + 1 of sequence s, KV head h.
+struct Item {
+    int s, h, q0, k0, Lq, Lk;     // first rows and lengths
+    int a, b;                     // the pair's queries [a, b) of the sequence
+    int tiles;                    // 1 or 2
+    int off;                      // position of query 0
+    int nsink, lo, n;             // blocks 0 .. nsink - 1, then from lo on: n in all
+    int whole_lo, whole_hi;       // keys [whole_lo, whole_hi] (and below `sinks`) are seen by every row
+    __device__ __forceinline__ int block(int i) const { return i < nsink ? i : lo + i - nsink; }
+    __device__ __forceinline__ bool edge(int i, int sinks) const {
+        const int t0 = block(i) * kPfTile, t1 = t0 + kPfTile - 1;
+        return t1 > whole_hi || (t0 < whole_lo && t1 >= sinks);
+    }
+};
+
+__device__ __forceinline__ bool find_item(const PfArgs& A, int x, Item& w) {
+    // The last tiles, which see the most keys, first; a pair's KV heads side by side.
+    const PrefillIO& io = A.io;
+    const int per = io.batch * io.Hkv;
+    const int p = A.pairs - 1 - x / per;
+    x %= per;
+    w.s = x / io.Hkv;
+    w.h = x - w.s * io.Hkv;
+    auto clamped = [](int v, int most) { return min(max(v, 0), most); };
+    w.q0 = clamped(__ldg(&io.cu_q[w.s]), io.total_q);
+    w.k0 = clamped(__ldg(&io.cu_k[w.s]), io.total_k);
+    w.Lq = clamped(__ldg(&io.cu_q[w.s + 1]), io.total_q) - w.q0;
+    w.Lk = max(clamped(__ldg(&io.cu_k[w.s + 1]), io.total_k) - w.k0, 0);
+    w.a = 2 * p * A.nq;
+    if (w.a >= w.Lq) return false;
+    w.b = min(w.a + 2 * A.nq, w.Lq);
+    w.tiles = w.b - w.a > A.nq ? 2 : 1;
+    w.off = w.Lk - w.Lq;
+    const int pa = w.off + w.a, pb = w.off + w.b - 1;    // first and last position
+    w.nsink = w.lo = w.n = 0;
+    if (pb >= 0) {
+        w.lo = io.window ? max(pa - io.window + 1, 0) / kPfTile : 0;
+        w.nsink = min((min(io.sinks, w.Lk) + kPfTile - 1) / kPfTile, w.lo);
+        w.n = w.nsink + pb / kPfTile + 1 - w.lo;
+    }
+    w.whole_hi = pa;
+    w.whole_lo = io.window ? pb - io.window + 1 : 0;
+    return true;
+}
+
+// 32 columns of 32-bit values to this warp's TMEM lanes.
+__device__ __forceinline__ void tmem_st32(uint32_t taddr, const uint32_t* r) {
+    asm volatile(
+        "tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], "
+        "{%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,"
+        "%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31,%32};\n" ::"r"(taddr),
+        "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]),
+        "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]), "r"(r[16]), "r"(r[17]), "r"(r[18]),
+        "r"(r[19]), "r"(r[20]), "r"(r[21]), "r"(r[22]), "r"(r[23]), "r"(r[24]), "r"(r[25]), "r"(r[26]), "r"(r[27]),
+        "r"(r[28]), "r"(r[29]), "r"(r[30]), "r"(r[31])
+        : "memory");
+}
+__device__ __forceinline__ void tmem_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;\n" ::: "memory"); }
+
+// D += A B with A (128 rows x 16) in TMEM and B in shared memory.
+__device__ __forceinline__ void mma_tmem_a(uint32_t d, uint32_t a, uint64_t bdesc, uint32_t idesc, uint32_t accumulate) {
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "setp.ne.b32 p, %4, 0;\n\t"
+        "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}\n" ::"r"(d),
+        "r"(a), "l"(bdesc), "r"(idesc), "r"(accumulate)
+        : "memory");
+}
+
+// Shared-memory descriptor of a V block as the B operand of O += P V: columns (the values'
+// dimensions) contiguous, 64 to a 128-byte swizzled row; the other 64 a half further on,
+// eight keys every 1024 bytes.
+__device__ __forceinline__ uint64_t smem_desc_mn_sw128(uint32_t saddr) {
+    uint64_t d = 0;
+    d |= (uint64_t)((saddr >> 4) & 0x3FFF);
+    d |= (uint64_t)(kPfHalf >> 4) << 16;
+    d |= (uint64_t)(1024 >> 4) << 32;
+    d |= (uint64_t)1 << 46;
+    d |= (uint64_t)2 << 61;
+    return d;
+}
+
+template <class T>
+constexpr uint32_t kType = 1u;         // operand type of the instruction descriptor: bf16
+template <>
+constexpr uint32_t kType<__half> = 0u;
+
+// fp32 accumulators, M = N = 128; b_mn: B's columns contiguous.
+template <class T>
+__device__ __forceinline__ constexpr uint32_t pf_idesc(bool b_mn) {
+    return (1u << 4) | (kType<T> << 7) | (kType<T> << 10) | (b_mn ? 1u << 16 : 0u) | ((kPfTile >> 3) << 17) |
+           ((kPfTile >> 4) << 24);
+}
+
+template <class T>
+__device__ __forceinline__ uint32_t unbounded_mask(uint32_t w) {   // the halves that are infinite or NaN
+    constexpr uint32_t e = kType<T> ? 0x7f80u : 0x7c00u;
+    return ((w & e) == e ? 0xffffu : 0u) | (((w >> 16) & e) == e ? 0xffff0000u : 0u);
+}
+
+// The infinities and NaN that row (position p) sees in the blocks of partial sight: their
+// weights are positive, so each makes its output infinite or NaN.  Only where there are any.
+template <class T>
+__device__ __noinline__ void add_unbounded(const PfArgs& A, const Item& w, int p, int col, float* o) {
+    for (int i = 0; i < w.n; ++i) {
+        if (!w.edge(i, A.io.sinks)) continue;
+        for (int c = 0; c < kPfTile; ++c) {
+            const int t = w.block(i) * kPfTile + c;
+            if (t > p || (A.io.window && t <= p - A.io.window && t >= A.io.sinks)) continue;
+            const uint16_t* v = A.io.v + ((size_t)(w.k0 + t) * A.io.Hkv + w.h) * kHeadDim + col;
+            for (int d = 0; d < 32; d += 2) {
+                const uint32_t x = *reinterpret_cast<const uint32_t*>(v + d);
+                const uint32_t m = unbounded_mask<T>(x);
+                const float2 f = Half16<T>::unpack(x);
+                if (m & 0xffffu) o[d] += f.x;
+                if (m >> 16) o[d + 1] += f.y;
+            }
+        }
+    }
+}
+
+template <class T>
+__global__ void __launch_bounds__(kPfThreads, 1) prefill_kernel(const __grid_constant__ PfArgs A) {
+    extern __shared__ uint8_t pf_smem_raw[];
+    // 1024-byte alignment for the swizzled operand tiles.
+    uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(pf_smem_raw) + 1023) & ~uintptr_t(1023));
+    uint8_t* sQ = smem;
+    uint8_t* ring = sQ + 2 * kPfBuf;
+    PfBarriers* bars = reinterpret_cast<PfBarriers*>(ring + kPfStages * kPfBuf);
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    if (threadIdx.x == 0) {
+        ptx::prefetch_tensormap(&A.qmap);
+        ptx::prefetch_tensormap(&A.kmap);
+        ptx::prefetch_tensormap(&A.vmap);
+        for (int i = 0; i < kPfStages; ++i) {
+            ptx::mbar_init(&bars->full[i], 1);
+            ptx::mbar_init(&bars->empty[i], 1);
+        }
+        ptx::mbar_init(&bars->q_full, 1);
+        ptx::mbar_init(&bars->dirty, 1);
+        ptx::mbar_init(&bars->clean, 2);
+        ptx::mbar_init(&bars->mma_done, 1);
+        for (int t = 0; t < 2; ++t) {
+            ptx::mbar_init(&bars->s_full[t], 1);
+            ptx::mbar_init(&bars->p_full[t], 4);   // one arrival per warp of the tile
+            ptx::mbar_init(&bars->o_done[t], 1);
+        }
+        bars->abort_flag = 0;
+        bars->unbounded = 0;
+        ptx::fence_barrier_init();
+    }
+    if (warp == 9) {
+        ptx::tmem_alloc(&bars->tmem_base, kPfTmem);
+        ptx::tmem_relinquish();
+    }
+    ptx::tc_fence_before();
+    __syncthreads();
+    ptx::tc_fence_after();
+    asm volatile("griddepcontrol.launch_dependents;\n" ::: "memory");
+    asm volatile("griddepcontrol.wait;\n" ::: "memory");
+    const uint32_t tmem = bars->tmem_base;
+    const volatile int* const abort = &bars->abort_flag;
+    Item w{};
+    const bool any = find_item(A, blockIdx.x, w);
+    const int n = any ? w.n : 0;
+    const int sinks = A.io.sinks;
+    bool stop = false;
+
+    if (warp == 8) {
+        // ------------------------------------------------------------ TMA
+        // K and V blocks alternate: load 2 i is K, 2 i + 1 V; load x goes to stage x % kPfStages.
+        const uint64_t policy = ptx::policy_evict_normal();
+        int loads = 0;
+        bool q_loaded = false;
+        if (n > 0) {
+            if (ptx::elect_one()) {
+                const uint32_t bytes = (uint32_t)(A.nq * A.g) * 128u;
+                ptx::mbar_arrive_expect_tx(&bars->q_full, 2u * bytes * (uint32_t)w.tiles);
+                for (int t = 0; t < w.tiles; ++t)
+                    for (int c = 0; c < 2; ++c)
+                        ptx::tma_load_3d(sQ + t * kPfBuf + c * kPfHalf, &A.qmap, &bars->q_full, c * 64, w.h * A.g,
+                                         w.q0 + w.a + t * A.nq, policy);
+            }
+            __syncwarp();
+            q_loaded = true;
+            for (int x = 0; x < 2 * n; ++x) {
+                const int st = x % kPfStages, round = x / kPfStages;
+                if (round > 0 && !ptx::warp_wait(&bars->empty[st], (round - 1) & 1, abort)) {
+                    stop = true;
+                    break;
+                }
+                if (ptx::elect_one()) {
+                    const CUtensorMap* map = x & 1 ? &A.vmap : &A.kmap;
+                    uint8_t* dst = ring + st * kPfBuf;
+                    const int row = w.k0 + w.block(x >> 1) * kPfTile;
+                    ptx::mbar_arrive_expect_tx(&bars->full[st], (uint32_t)kPfBuf);
+                    ptx::tma_load_3d(dst, map, &bars->full[st], 0, w.h, row, policy);
+                    ptx::tma_load_3d(dst + kPfHalf, map, &bars->full[st], 64, w.h, row, policy);
+                }
+                __syncwarp();
+                ++loads;
+            }
+        }
+        if (stop && lane == 0) {
+            bars->abort_flag = 1;
+            atomicExch(A.io.err, 3);
+        }
+        // Every issued copy lands before the CTA may exit.
+        for (int x = max(loads - kPfStages, 0); x < loads; ++x)
+            ptx::mbar_wait(&bars->full[x % kPfStages], (x / kPfStages) & 1, 50000000ull);
+        if (q_loaded) ptx::mbar_wait(&bars->q_full, 0, 50000000ull);
+    } else if (warp == 9) {
+        // ------------------------------------------------------------ MMA
+        const uint32_t idesc_s = pf_idesc<T>(false), idesc_o = pf_idesc<T>(true);
+        const uint64_t qdesc = ptx::smem_desc_k_sw128(ptx::smem_u32(sQ));
+        const uint64_t kdesc = ptx::smem_desc_k_sw128(ptx::smem_u32(ring));
+        const uint64_t vdesc = smem_desc_mn_sw128(ptx::smem_u32(ring));
+        const int tiles = w.tiles;
+        auto wait = [&](uint64_t* bar, int phase) {
+            if (!stop && !ptx::warp_wait(bar, phase & 1, abort)) stop = true;
+            return !stop;
+        };
+        auto issue_s = [&](int t, int i, bool last) {   // S_t = Q_t K_i^T
+            const int st = (2 * i) % kPfStages;
+            if (ptx::elect_one()) {
+                const uint64_t kd = kdesc + (uint32_t)(st * (kPfBuf >> 4)), qd = qdesc + (uint32_t)(t * (kPfBuf >> 4));
+#pragma unroll
+                for (int kk = 0; kk < 8; ++kk) {
+                    const uint32_t ofs = (kk >> 2) * (kPfHalf >> 4) + (kk & 3) * 2;
+                    ptx::mma_bf16(tmem + t * 128, qd + ofs, kd + ofs, idesc_s, kk > 0 ? 1u : 0u);
+                }
+                ptx::mma_commit(&bars->s_full[t]);
+                if (last) ptx::mma_commit(&bars->empty[st]);
+            }
+            __syncwarp();
+        };
+        auto issue_o = [&](int t, int i, bool last) {   // O_t += P_t V_i
+            const int st = (2 * i + 1) % kPfStages;
+            if (ptx::elect_one()) {
+                const uint64_t vd = vdesc + (uint32_t)(st * (kPfBuf >> 4));
+#pragma unroll
+                for (int kk = 0; kk < 8; ++kk)
+                    mma_tmem_a(tmem + 256 + t * 128, tmem + t * 128 + kk * 8, vd + kk * (2048 >> 4), idesc_o,
+                               i > 0 || kk > 0 ? 1u : 0u);
+                ptx::mma_commit(&bars->o_done[t]);
+                if (last) ptx::mma_commit(&bars->empty[st]);
+            }
+            __syncwarp();
+        };
+        if (n > 0 && wait(&bars->q_full, 0) && wait(&bars->full[0], 0)) {
+            ptx::tc_fence_after();
+            for (int t = 0; t < tiles; ++t) issue_s(t, 0, t == tiles - 1);
+            int cleaned = 0;
+            for (int i = 0; i < n && !stop; ++i) {
+                const int xv = 2 * i + 1, xk = 2 * i + 2;
+                if (!wait(&bars->full[xv % kPfStages], xv / kPfStages)) break;
+                if (w.edge(i, sinks)) {
+                    if (lane == 0) ptx::mbar_arrive(&bars->dirty);
+                    if (!wait(&bars->clean, cleaned++)) break;
+                }
+                for (int t = 0; t < tiles; ++t) {
+                    if (!wait(&bars->p_full[t], i)) break;
+                    ptx::tc_fence_after();
+                    issue_o(t, i, t == tiles - 1);
+                    if (i + 1 < n) {
+                        if (t == 0 && !wait(&bars->full[xk % kPfStages], xk / kPfStages)) break;
+                        issue_s(t, i + 1, t == tiles - 1);
+                    }
+                }
+            }
+        }
+        if (stop && lane == 0) {
+            bars->abort_flag = 1;
+            atomicExch(A.io.err, 3);
+        }
+        // The products in flight end before TMEM is freed.
+        if (ptx::elect_one()) ptx::mma_commit(&bars->mma_done);
+        __syncwarp();
+        ptx::mbar_wait(&bars->mma_done, 0, 50000000ull);
+    } else if (warp >= 10) {
+        // ------------------------------------------------------------ V blocks of partial sight
+        // The MMA warp hands a block over: a parity says nothing of a stage several rounds ahead.
+        const int id = threadIdx.x - 320;
+        int edges = 0;
+        for (int i = 0; i < n && !stop; ++i) {
+            if (!w.edge(i, sinks)) continue;
+            const int x = 2 * i + 1, st = x % kPfStages;
+            if (!ptx::warp_wait(&bars->dirty, edges++ & 1, abort) ||
+                !ptx::warp_wait(&bars->full[st], (x / kPfStages) & 1, abort)) {
+                stop = true;
+                break;
+            }
+            uint4* v = reinterpret_cast<uint4*>(ring + st * kPfBuf);
+            bool found = false;
+            for (int e = id; e < kPfBuf / 16; e += 64) {
+                uint4 u = v[e];
+                const uint4 m = make_uint4(unbounded_mask<T>(u.x), unbounded_mask<T>(u.y), unbounded_mask<T>(u.z), unbounded_mask<T>(u.w));
+                if (m.x | m.y | m.z | m.w) {
+                    v[e] = make_uint4(u.x & ~m.x, u.y & ~m.y, u.z & ~m.z, u.w & ~m.w);
+                    found = true;
+                }
+            }
+            if (found) bars->unbounded = 1;
+            ptx::fence_proxy_async_smem();
+            __syncwarp();
+            if (lane == 0) ptx::mbar_arrive(&bars->clean);
+        }
+        if (stop && lane == 0) {
+            bars->abort_flag = 1;
+            atomicExch(A.io.err, 3);
+        }
+    } else if (any) {
+        // ------------------------------------------------------------ softmax
+        const int t = warp >> 2, quad = warp & 3, row = quad * 32 + lane;
+        const int query = w.a + t * A.nq + row / A.g, j = row % A.g;
+        const bool live = row < A.nq * A.g && query < w.b;       // the row is a real one
+        const int p = w.off + query;
+        const int below = A.io.window ? p - A.io.window : -1;     // keys up to here are out of the window
+        const uint32_t lanes = (uint32_t)(quad * 32) << 16;
+        const uint32_t tS = tmem + lanes + t * 128, tO = tmem + lanes + 256 + t * 128;
+        const uint64_t sl2 = ptx::pack_f32x2(A.sl2, A.sl2);
+        float m = kNoLogit, l = 0.f;
+        if (t < w.tiles) {
+            for (int i = 0; i < n; ++i) {
+                if (!ptx::warp_wait(&bars->s_full[t], i & 1, abort)) {
+                    stop = true;
+                    break;
+                }
+                ptx::tc_fence_after();
+                float s[128];
+#pragma unroll
+                for (int c = 0; c < 4; ++c) ptx::tmem_ld32(tS + c * 32, s + c * 32);
+                ptx::tmem_wait_ld();
+                if (w.edge(i, sinks)) {
+                    const int t0 = w.block(i) * kPfTile;
+#pragma unroll
+                    for (int c = 0; c < 128; ++c) {
+                        const int key = t0 + c;
+                        if (key > p || (key <= below && key >= sinks)) s[c] = -INFINITY;
+                    }
+                }
+                float mx[4] = {s[0], s[1], s[2], s[3]};
+#pragma unroll
+                for (int c = 4; c < 128; ++c) mx[c & 3] = fmaxf(mx[c & 3], s[c]);
+                const float top = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * A.sl2;
+                if (i == 0) {
+                    m = fmaxf(m, top);
+                } else if (__any_sync(0xffffffffu, top > m + kRescale)) {
+                    // Rare: the outputs so far to the new maximum, once the products of the block before are done.
+                    if (!ptx::warp_wait(&bars->o_done[t], (i - 1) & 1, abort)) {
+                        stop = true;
+                        break;
+                    }
+                    ptx::tc_fence_after();
+                    const float mn = top > m + kRescale ? top : m;
+                    const float f = ptx::ex2(m - mn);
+                    l *= f;
+                    m = mn;
+#pragma unroll
+                    for (int c = 0; c < 4; ++c) {
+                        float o[32];
+                        ptx::tmem_ld32(tO + c * 32, o);
+                        ptx::tmem_wait_ld();
+#pragma unroll
+                        for (int d = 0; d < 32; ++d) o[d] *= f;
+                        tmem_st32(tO + c * 32, reinterpret_cast<const uint32_t*>(o));
+                    }
+                }
+                const uint64_t ref = ptx::pack_f32x2(-m, -m);
+                uint64_t sum = 0ull;
+#pragma unroll
+                for (int c = 0; c < 2; ++c) {
+                    uint32_t pk[32];
+#pragma unroll
+                    for (int e = 0; e < 32; ++e) {
+                        const uint64_t x = ptx::fma_f32x2(ptx::pack_f32x2(s[c * 64 + 2 * e], s[c * 64 + 2 * e + 1]), sl2, ref);
+                        const float p0 = ptx::ex2(ptx::lo_f32(x)), p1 = ptx::ex2(ptx::hi_f32(x));
+                        sum = ptx::add_f32x2(sum, ptx::pack_f32x2(p0, p1));
+                        pk[e] = Half16<T>::pack(p0, p1);
+                    }
+                    tmem_st32(tS + c * 32, pk);
+                }
+                l += ptx::lo_f32(sum) + ptx::hi_f32(sum);
+                tmem_wait_st();
+                ptx::tc_fence_before();
+                __syncwarp();
+                if (lane == 0) ptx::mbar_arrive(&bars->p_full[t]);
+            }
+            if (n > 0 && !stop && !ptx::warp_wait(&bars->o_done[t], (n - 1) & 1, abort)) stop = true;
+            if (stop && lane == 0) {
+                bars->abort_flag = 1;
+                atomicExch(A.io.err, 3);
+            }
+            ptx::tc_fence_after();
+            const float inv = l > 0.f || l != l ? 1.f / l : 0.f;
+            const bool unbounded = n > 0 && bars->unbounded != 0;
+            const size_t at = (size_t)(w.q0 + query) * A.io.Hq + w.h * A.g + j;
+#pragma unroll
+            for (int c = 0; c < 4; ++c) {
+                float o[32];
+                if (n > 0) {
+                    ptx::tmem_ld32(tO + c * 32, o);
+                    ptx::tmem_wait_ld();
+                } else {
+#pragma unroll
+                    for (int d = 0; d < 32; ++d) o[d] = 0.f;
+                }
+#pragma unroll
+                for (int d = 0; d < 32; ++d) o[d] = l > 0.f || l != l ? o[d] * inv : 0.f;
+                if (live) {
+                    if (unbounded) add_unbounded<T>(A, w, p, c * 32, o);
+                    uint4* dst = reinterpret_cast<uint4*>(A.io.out + at * kHeadDim + c * 32);
+#pragma unroll
+                    for (int d = 0; d < 4; ++d)
+                        dst[d] = make_uint4(Half16<T>::pack(o[8 * d], o[8 * d + 1]), Half16<T>::pack(o[8 * d + 2], o[8 * d + 3]),
+                                            Half16<T>::pack(o[8 * d + 4], o[8 * d + 5]), Half16<T>::pack(o[8 * d + 6], o[8 * d + 7]));
+                }
+            }
+            if (live && A.io.lse)
+                A.io.lse[at] = l > 0.f || l != l ? fmaf(m, 0.6931471805599453f, logf(l)) : -INFINITY;
+        }
+    }
+    __syncthreads();
+    if (warp == 9) ptx::tmem_dealloc(tmem, kPfTmem);
+}
+
+template <class T>
+cudaError_t launch_typed(const PfArgs& a, cudaStream_t st) {
+    const long long items = (long long)a.pairs * a.io.batch * a.io.Hkv;
+    if (items > 0x7fffffffll) return cudaErrorInvalidConfiguration;
+    return launch_prio(prefill_kernel<T>, dim3((unsigned)items), dim3(kPfThreads), kPfSmem, st, 0, true, a);
+}
+
+}  // namespace
+
+cudaError_t configure_prefill() {
+    cudaError_t e = cudaFuncSetAttribute(prefill_kernel<__nv_bfloat16>, cudaFuncAttributeMaxDynamicSharedMemorySize, kPfSmem);
+    if (e == cudaSuccess)
+        e = cudaFuncSetAttribute(prefill_kernel<__half>, cudaFuncAttributeMaxDynamicSharedMemorySize, kPfSmem);
+    return e;
+}
+
+cudaError_t launch_prefill(const PrefillIO& io, cudaStream_t st) {
+    PfArgs a{};
+    a.io = io;
+    a.g = io.Hq / io.Hkv;
+    a.nq = kPfTile / a.g;
+    a.pairs = (io.max_q + 2 * a.nq - 1) / (2 * a.nq);
+    a.sl2 = io.scale * 1.4426950408889634f;
+    const uint64_t row = (uint64_t)kHeadDim * 2;
+    const uint64_t qd[3] = {(uint64_t)kHeadDim, (uint64_t)io.Hq, (uint64_t)io.total_q}, qs[2] = {row, row * io.Hq};
+    const uint32_t qb[3] = {64, (uint32_t)a.g, (uint32_t)a.nq};
+    // Without any key nothing is loaded by the maps of K and V.
+    const bool keys = io.total_k > 0;
+    const uint64_t kd[3] = {(uint64_t)kHeadDim, (uint64_t)io.Hkv, (uint64_t)std::max(io.total_k, 1)}, ks[2] = {row, row * io.Hkv};
+    const uint32_t kb[3] = {64, 1, (uint32_t)kPfTile};
+    cudaError_t e = encode_tensor_map(&a.qmap, io.dtype, 3, io.q, qd, qs, qb);
+    if (e == cudaSuccess) e = encode_tensor_map(&a.kmap, io.dtype, 3, keys ? io.k : io.q, kd, ks, kb);
+    if (e == cudaSuccess) e = encode_tensor_map(&a.vmap, io.dtype, 3, keys ? io.v : io.q, kd, ks, kb);
+    if (e != cudaSuccess) return e;
+    return io.dtype == 1 ? launch_typed<__half>(a, st) : launch_typed<__nv_bfloat16>(a, st);
+}
+
+}  // namespace kvec

@@ -30,7 +30,8 @@ EXPORTED = ("kvec_create", "kvec_destroy", "kvec_state_bytes", "kvec_reset", "kv
             "kvec_kernel_time", "kvec_status_string", "kvec_last_error", "kvec_select_layer_noalloc",
             "kvec_select_layer_lse", "kvec_select_layers_lse", "kvec_decode_attention",
             "kvec_noalloc_sync_status", "kvec_set_test_fault", "kvec_output_capacity",
-            "kvec_rotate_append", "kvec_paged_decode_bytes", "kvec_paged_decode", "kvec_paged_evict")
+            "kvec_rotate_append", "kvec_paged_decode_bytes", "kvec_paged_decode", "kvec_paged_evict",
+            "kvec_prefill_attention")
 
 KVEC_BF16 = 0
 KVEC_FP16 = 1
@@ -130,6 +131,7 @@ def load() -> ctypes.CDLL:
             "kvec_paged_decode_bytes": ([_vp, i, i, i], ctypes.c_size_t),
             "kvec_paged_decode": ([_vp, i, _vp, ctypes.POINTER(kvec_paged_cache), i, i, i, _vp, _vp, ctypes.c_size_t,
                                    _vp], st),
+            "kvec_prefill_attention": ([_vp, i, i, _vp, _vp, _vp, _vp, _vp, _vp, _vp, i, i, _vp, _vp, _vp], st),
             "kvec_paged_evict": ([_vp, i, ctypes.POINTER(kvec_paged_cache), _vp, i, i, i, i, i, _vp, _vp, _vp], st),
         }
         for name, (args, res) in sig.items():
@@ -251,6 +253,13 @@ def kvec_paged_evict(handle: int, batch: int, cache: kvec_paged_cache, new_table
                      budget: int, sinks: int, recent: int, new_lens: int, kept: int, stream: int = 0) -> None:
     _check(load().kvec_paged_evict(handle, batch, cache, new_table, new_max_pages, max_len, budget, sinks, recent,
                                    new_lens, kept, stream))
+
+
+def kvec_prefill_attention(handle: int, dtype: int, batch: int, cu_q_host: int, cu_q_dev: int, cu_k_host: int,
+                           cu_k_dev: int, q: int, k: int, v: int, window: int, sinks: int, out: int,
+                           lse: Optional[int] = None, stream: int = 0) -> None:
+    _check(load().kvec_prefill_attention(handle, dtype, batch, cu_q_host, cu_q_dev, cu_k_host, cu_k_dev, q, k, v,
+                                         window, sinks, out, lse, stream))
 
 
 def kvec_debug_scores(handle: int) -> kvec_debug_view:
@@ -564,6 +573,40 @@ class KvecSelector:
                          cache.capacity if max_len is None else max_len, budget, sinks, recent, new_lens.data_ptr(),
                          kept.data_ptr(), stream.cuda_stream)
         return new_lens, kept
+
+    def prefill_attention(self, q, k, v, cu_q_host, cu_q_dev, cu_k_host=None, cu_k_dev=None, window: int = 0,
+                          sinks: int = 0, out=None, lse=None, stream=None):
+        """Causal attention of packed sequences (kvec_prefill_attention).
+
+        q [T_q][H_q][d], k, v [T_k][H_kv][d] bf16 or fp16, contiguous; cu_* int32 [batch + 1], host and device copies
+        (cu_k: cu_q).  Returns (out as q, lse fp32 [T_q][H_q])."""
+        t, p = self._torch, self.params
+        dtype, dev, d = q.dtype, q.device, p.head_dim
+        if cu_k_host is None:
+            cu_k_host, cu_k_dev = cu_q_host, cu_q_dev
+        code = _dtype_code(t, dtype)
+        for name, x, heads in (("q", q, p.num_q_heads), ("k", k, p.num_kv_heads), ("v", v, p.num_kv_heads)):
+            _want(x.dim() == 3 and x.shape[1] == heads and x.shape[2] == d and x.dtype == dtype and x.device == dev and
+                  x.is_contiguous(), f"{name} must be contiguous {dtype} [T][{heads}][{d}] on {dev}")
+        batch = cu_q_host.shape[0] - 1
+        for x in (cu_q_host, cu_k_host, cu_q_dev, cu_k_dev):
+            _want(x.dtype == t.int32 and tuple(x.shape) == (batch + 1,) and x.is_contiguous(),
+                  "cu_q and cu_k must be contiguous int32 [batch + 1]")
+        _want(cu_q_host.device.type == "cpu" and cu_k_host.device.type == "cpu" and cu_q_dev.device == dev and
+              cu_k_dev.device == dev, "cu_q and cu_k are wanted on the host and on the device")
+        _want(batch >= 1 and int(cu_q_host[-1]) <= q.shape[0] and int(cu_k_host[-1]) <= min(k.shape[0], v.shape[0]),
+              "cu_q or cu_k passes the rows given")
+        _want(out is None or (out.shape == q.shape and out.dtype == dtype and out.is_contiguous() and out.device == dev),
+              "out must be as q")
+        _want(lse is None or (lse.dtype == t.float32 and lse.shape == q.shape[:2] and lse.is_contiguous() and
+                              lse.device == dev), "lse must be contiguous fp32 [T_q][H_q]")
+        stream = self._stream(stream, dev)
+        out = self._empty(q.shape, dtype, stream) if out is None else out
+        lse = self._empty(q.shape[:2], t.float32, stream) if lse is None else lse
+        kvec_prefill_attention(self.handle, code, batch, cu_q_host.data_ptr(), cu_q_dev.data_ptr(),
+                               cu_k_host.data_ptr(), cu_k_dev.data_ptr(), q.data_ptr(), k.data_ptr(), v.data_ptr(),
+                               window, sinks, out.data_ptr(), lse.data_ptr(), stream.cuda_stream)
+        return out, lse
 
     def debug(self, device="cuda"):
         """Copies of the last layer's intermediates (see kvec_debug_view)."""

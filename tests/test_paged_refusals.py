@@ -196,3 +196,46 @@ def test_struct_layouts_match_the_header():
     # Natural alignment: four ints and five pointers; 8 + 3 pointers + 3 int64 + 2 pointers + float and 3 ints + 4 pointers.
     assert ctypes.sizeof(kvec.kvec_paged_cache) == 4 * 4 + 5 * 8
     assert ctypes.sizeof(kvec.kvec_rotate_args) == 8 + 3 * 8 + 3 * 8 + 2 * 8 + 16 + 4 * 8
+
+
+# ---------------------------------------------------------------- prefill attention
+
+@pytest.mark.parametrize("over,words", [
+    (dict(dtype=2), "dtype"), (dict(batch=0), "batch"), (dict(batch=70000), "batch"), (dict(window=-1), "window"),
+    (dict(sinks=-1), "window"), (dict(cu_q=None), "NULL"), (dict(cu_q=[1, 5]), "cu_q[0]"), (dict(cu_k=[2, 5]), "cu_q[0]"),
+    (dict(cu_q=[0, -1]), "-1 queries"), (dict(cu_k=[0, 2 ** 20 + 1]), "keys"), (dict(cu_q=[0, 2 ** 31 - 1]), "queries"),
+    ({}, "handle is NULL"),
+])
+def test_bad_prefills(over, words):
+    a = dict(dtype=kvec.KVEC_FP16, batch=1, window=0, sinks=0, cu_q=[0, 5], cu_k=[0, 5])
+    a.update(over)
+    host = {n: None if a[n] is None else (ctypes.c_int32 * len(a[n]))(*a[n]) for n in ("cu_q", "cu_k")}
+    at = {n: None if x is None else ctypes.addressof(x) for n, x in host.items()}
+    if a["batch"] > 1:
+        at["cu_q"] = at["cu_q"]      # the batch is refused before the lengths are read
+    refused(lambda: kvec.kvec_prefill_attention(None, a["dtype"], a["batch"], at["cu_q"], 16, at["cu_k"], 16, 16, 16, 16,
+                                                a["window"], a["sinks"], 16, None), kvec.KVEC_ERR_INVALID_ARG, words)
+
+
+def test_the_binding_checks_a_prefill():
+    sel, bf = selector(), torch.bfloat16
+    q, k = torch.zeros((5, 8, 128), dtype=bf), torch.zeros((5, 2, 128), dtype=bf)
+    cu = torch.tensor([0, 5], dtype=torch.int32)
+    for bad in (dict(q=q.float()), dict(k=k.half()), dict(k=torch.zeros((5, 4, 128), dtype=bf)), dict(v=k[:, :, :64]),
+                dict(q=torch.zeros((5, 8, 256), dtype=bf)[..., :128]), dict(cu_q_host=cu.long()), dict(cu_q_dev=cu[:1]),
+                dict(cu_q_host=torch.tensor([0, 6], dtype=torch.int32)), dict(v=k[:4]), dict(out=q.float()),
+                dict(lse=torch.zeros(5, 8, dtype=torch.float64)), dict(lse=torch.zeros(5, 2))):
+        with pytest.raises(kvec.KvecError):
+            sel.prefill_attention(**{**dict(q=q, k=k, v=k, cu_q_host=cu, cu_q_dev=cu), **bad})
+
+
+def test_prefill_definition():
+    rng = np.random.default_rng(2)
+    q, k, v = rng.standard_normal((6, 2, 8)), rng.standard_normal((9, 1, 8)), rng.standard_normal((9, 1, 8))
+    out, lse = serving.prefill(q, k, v, [0, 4, 6], [0, 8, 9], 0, 0, 0.4)
+    e = np.exp(0.4 * k[:6, 0] @ q[1, 1])                     # row 1 of the first sequence is at position 5
+    assert np.allclose(out[1, 1], e @ v[:6, 0] / e.sum()) and np.isclose(lse[1, 1], np.log(e.sum()))
+    assert np.all(out[4] == 0) and np.all(np.isneginf(lse[4]))   # two queries, one key: the first sees nothing
+    assert np.allclose(out[5], v[8]) and np.allclose(lse[5, 0], 0.4 * q[5, 0] @ k[8, 0])
+    mean, _ = serving.prefill(0 * q, k, v, [0, 4, 6], [0, 8, 9], 2, 1, 0.4)
+    assert np.allclose(mean[3, 0], (v[0, 0] + v[6, 0] + v[7, 0]) / 3)

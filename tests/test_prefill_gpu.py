@@ -1,0 +1,229 @@
+"""GPU parity of prefill attention (kvec_prefill_attention) with its definition in fp64.
+
+Tolerances.  u is half a step of the 16-bit type relative to the value (bf16 2^-8, fp16 2^-11).  The weights are
+rounded to the type before they meet the values, which moves the output by at most u sum_t p_t |v_t| (fp16 also by
+2^-25 of the largest weight each, n 2^-25 max|v| over n keys); the logits are fp32 sums of exact products and the
+exponentials approximate, 2e-5 sum_t p_t |v_t|; the result is rounded once, u |ref|.  The log-sum-exp is fp32: the
+logits' 2e-5 and 2^-22 of its value.
+"""
+import numpy as np
+import pytest
+import torch
+
+from oracle import serving
+from paper_2606_29563_gb300 import kvec
+
+pytestmark = pytest.mark.gpu
+D = 128
+TYPES = [torch.bfloat16, torch.float16]
+
+
+@pytest.fixture(scope="module", autouse=True)
+def _built():
+    if not torch.cuda.is_available():
+        pytest.skip("needs a CUDA GPU")
+    from paper_2606_29563_gb300 import build as kbuild
+    kbuild.build()
+
+
+_SELECTORS = {}
+
+
+def selector(Hq, Hkv, scale=0.0):
+    key = (Hq, Hkv, scale)
+    if key not in _SELECTORS:
+        _SELECTORS[key] = kvec.KvecSelector(kvec.make_params(Hq, Hkv, num_ext_heads=1, max_batch=64, max_seqlen=64,
+                                                             max_layers=1, softmax_scale=scale))
+    return _SELECTORS[key]
+
+
+def cu_of(lens):
+    return torch.tensor(np.concatenate([[0], np.cumsum(lens)]), dtype=torch.int32)
+
+
+def reference(q, k, v, q_lens, k_lens, window, sinks, scale):
+    """out, lse and sum of p |v| in fp64 on the GPU, head by head; masked places count for nothing, whatever they hold."""
+    q, k, v = q.double(), k.double(), v.double()
+    g = q.shape[1] // k.shape[1]
+    out, mass = torch.zeros_like(q), torch.zeros_like(q)
+    lse = torch.full(q.shape[:2], -np.inf, dtype=torch.float64, device=q.device)
+    q0 = k0 = 0
+    for nq, nk in zip(q_lens, k_lens):
+        p = torch.arange(nk - nq, nk, device=q.device)[:, None]
+        t = torch.arange(nk, device=q.device)[None, :]
+        seen = t <= p
+        if window:
+            seen = seen & ((t > p - window) | (t < sinks))
+        for h in range(q.shape[1]):
+            if nq == 0 or nk == 0:
+                continue
+            kk, vv = k[k0:k0 + nk, h // g], v[k0:k0 + nk, h // g]
+            x = (q[q0:q0 + nq, h] @ kk.nan_to_num(0, 0, 0).T * scale)
+            bad = ~torch.isfinite(kk).all(-1)
+            assert not (seen & bad[None, :]).any(), "the reference takes unbounded keys in masked places only"
+            x = x.masked_fill(~seen, -np.inf)
+            lse[q0:q0 + nq, h] = torch.logsumexp(x, -1)
+            w = torch.exp(x - lse[q0:q0 + nq, h, None].clamp(min=-1e300))
+            fine = vv.nan_to_num(0, 0, 0)
+            o = w @ fine
+            # What is infinite or NaN in V reaches the rows that see it.
+            for i in torch.nonzero(~torch.isfinite(vv).all(-1)).flatten().tolist():
+                part = torch.where(torch.isfinite(vv[i]), torch.zeros_like(vv[i]), vv[i])
+                o = torch.where(seen[:, i, None], o + part, o)
+            out[q0:q0 + nq, h] = o
+            mass[q0:q0 + nq, h] = w @ fine.abs()
+        q0, k0 = q0 + nq, k0 + nk
+    return out, lse, mass
+
+
+def check(q, k, v, q_lens, k_lens, window=0, sinks=0, scale=None, **kw):
+    dtype, u = q.dtype, torch.finfo(q.dtype).eps / 2
+    sel = selector(q.shape[1], k.shape[1], scale or 0.0)
+    cu_q, cu_k = cu_of(q_lens), cu_of(k_lens)
+    out, lse = sel.prefill_attention(q, k, v, cu_q, cu_q.cuda(), cu_k, cu_k.cuda(), window=window, sinks=sinks, **kw)
+    kvec.kvec_sync_status(sel.handle)
+    n = sum(q_lens)
+    ref, rl, mass = reference(q[:n], k, v, q_lens, k_lens, window, sinks, scale or D ** -0.5)
+    got = out[:n].double()
+    fine = torch.isfinite(ref)
+    assert torch.equal(torch.isnan(got), torch.isnan(ref)) and torch.equal(got[torch.isinf(ref)], ref[torch.isinf(ref)])
+    most = max(list(k_lens) + [1])
+    tol = u * ref.abs() + (u + 2e-5) * mass + (most * 2.0 ** -25 * 8 if dtype == torch.float16 else 0) + 1e-30
+    bad = fine & ~((got - ref).abs() <= tol)
+    assert not bad.any(), f"{int(bad.sum())} of {bad.numel()} off, by up to {float((got - ref)[fine].abs().max()):.3e}; rows {torch.nonzero(bad.any(-1))[:8].tolist()}"
+    gl = lse[:n].double()
+    none = torch.isneginf(rl)
+    assert torch.equal(torch.isneginf(gl), none) and torch.all(got[none] == 0)
+    bad = ~none & ~((gl - rl).abs() <= 2e-5 + 2.0 ** -22 * rl.abs())
+    assert not bad.any(), f"lse off by up to {float((gl - rl)[~none].abs().max()):.3e}"
+    return out, lse
+
+
+def tensors(q_lens, k_lens, Hq, Hkv, dtype, seed, std=1.0):
+    gen = torch.Generator().manual_seed(seed)
+    mk = lambda n, h, s=1.0: (torch.randn((n, h, D), generator=gen) * s).to(dtype).cuda()
+    return mk(sum(q_lens), Hq, std), mk(sum(k_lens), Hkv), mk(sum(k_lens), Hkv)
+
+
+SHAPES = [
+    (1, 1, [1], [1]), (4, 1, [1], [300]), (8, 8, [5], [5]), (32, 8, [33], [1057]), (28, 4, [33], [200]),
+    (8, 2, [128], [128]), (8, 1, [129], [129]), (7, 1, [100], [127]), (12, 4, [300, 1, 64], [300, 500, 64]),
+    (16, 8, [257, 0, 3], [700, 12, 2]),                    # no queries; more queries than keys: rows that see nothing
+    (6, 2, [10, 4], [0, 4]),                               # no keys
+    (4, 4, [1000], [1000]), (5, 1, [700], [1500]),
+]
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("Hq,Hkv,q_lens,k_lens", SHAPES)
+def test_causal(dtype, Hq, Hkv, q_lens, k_lens):
+    q, k, v = tensors(q_lens, k_lens, Hq, Hkv, dtype, sum(q_lens) + 7 * sum(k_lens), 2.0)
+    check(q, k, v, q_lens, k_lens)
+
+
+@pytest.mark.parametrize("window,sinks", [(1, 0), (1, 1), (127, 4), (128, 0), (129, 128), (200, 200), (5, 1000), (4000, 3)])
+@pytest.mark.parametrize("Hq,Hkv,q_lens,k_lens", [(8, 2, [700], [700]), (28, 4, [33, 200], [1057, 600]), (4, 4, [1], [513])])
+def test_windows_and_first_tokens(Hq, Hkv, q_lens, k_lens, window, sinks):
+    q, k, v = tensors(q_lens, k_lens, Hq, Hkv, torch.bfloat16, window + sinks)
+    check(q, k, v, q_lens, k_lens, window, sinks)
+
+
+def test_against_the_plain_definition_row_by_row():
+    q_lens, k_lens = [40, 9], [90, 5]
+    q, k, v = tensors(q_lens, k_lens, 4, 2, torch.float16, 1)
+    f = lambda x: x.double().cpu().numpy()
+    for window, sinks in ((0, 0), (20, 3)):
+        ref, lse, _ = reference(q, k, v, q_lens, k_lens, window, sinks, D ** -0.5)
+        out, z = serving.prefill(f(q), f(k), f(v), cu_of(q_lens).tolist(), cu_of(k_lens).tolist(), window, sinks, D ** -0.5)
+        assert np.allclose(ref.cpu().numpy(), out, atol=1e-12) and np.allclose(lse.cpu().numpy(), z, atol=1e-12)
+        check(q, k, v, q_lens, k_lens, window, sinks)
+
+
+def test_the_running_maximum_moves():
+    # Logits that grow along the keys by far more than the lazy rescale's threshold, and far down from a first peak.
+    q, k, v = tensors([600], [600], 8, 2, torch.bfloat16, 3)
+    up = torch.linspace(-30, 30, 600, device="cuda")[:, None]
+    q[:, :, 0] = 8.0
+    for ramp in (up, -up, up.abs() * (-1) ** (torch.arange(600, device="cuda") // 128)[:, None]):
+        k[:, :, 0] = ramp.to(k.dtype)
+        check(q, k, v, [600], [600])
+        check(q, k, v, [600], [600], 150, 2)
+
+
+def test_masked_places_hold_anything():
+    # Rows behind each sequence and keys that the window has left or a row does not see yet.
+    q_lens, k_lens = [30, 200], [300, 200]
+    q, k, v = tensors(q_lens, [300, 200, 150], 8, 2, torch.bfloat16, 5)
+    k[500:], v[500:] = float("nan"), float("inf")
+    k[2:300 - 30 - 63], v[2:300 - 30 - 63] = float("nan"), float("-inf")   # before the window of 64 of every row
+    check(q, k, v, q_lens, k_lens, 64, 2)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("where", [0, 60, 150, 255, 299])
+def test_unbounded_values_reach_only_the_rows_that_see_them(dtype, where):
+    q, k, v = tensors([300], [300], 8, 2, dtype, where)
+    v[where, 0, 5], v[where, 1, 100] = float("inf"), float("nan")
+    v[min(where + 3, 299), 0, 70] = float("-inf")
+    check(q, k, v, [300], [300])
+    check(q, k, v, [300], [300], 40, 1)
+
+
+def test_minus_infinite_logits():
+    q, k, v = tensors([200], [200], 4, 4, torch.bfloat16, 8)
+    ref = q.clone()
+    q[:, :, 0] = 1.0
+    k2 = k.clone()
+    k2[::2, :, 0] = float("-inf")
+    cu = cu_of([200])
+    out, lse = selector(4, 4).prefill_attention(q, k2, v, cu, cu.cuda())
+    assert torch.all(out[0] == 0) and torch.all(torch.isneginf(lse[0]))     # row 0 sees key 0 alone
+    x = torch.einsum("qhd,khd->hqk", q.double(), k.double()) * D ** -0.5
+    t = torch.arange(200, device="cuda")
+    x = x.masked_fill((t[None, :] > t[:, None]) | (t[None, :] % 2 == 0), -np.inf)
+    want = torch.einsum("hqk,khd->qhd", torch.softmax(x, -1).nan_to_num(0), v.double())
+    assert torch.isfinite(out).all() and (out.double() - want).abs().max() < 0.05 and ref is not None
+
+
+def test_a_softmax_scale_of_the_handle():
+    q, k, v = tensors([150], [150], 4, 2, torch.float16, 10)
+    check(q, k, v, [150], [150], scale=0.5)
+
+
+def test_rows_behind_the_last_sequence_stay():
+    q, k, v = tensors([50], [50], 8, 2, torch.bfloat16, 12)
+    out = torch.full_like(q, 9.0)
+    lse = torch.full((50, 8), 9.0, device="cuda")
+    check(q, k, v, [20, 11], [20, 11], out=out, lse=lse)
+    assert torch.all(out[31:] == 9.0) and torch.all(lse[31:] == 9.0) and torch.isfinite(lse).all()
+
+
+def test_long_rows_and_many_tiles():
+    q, k, v = tensors([4096, 1111], [4096, 3333], 8, 2, torch.bfloat16, 14, 2.0)
+    check(q, k, v, [4096, 1111], [4096, 3333])
+    check(q, k, v, [4096, 1111], [4096, 3333], 512, 4)
+
+
+def test_captured_and_on_two_streams():
+    sel = selector(8, 2)
+    cu = cu_of([500, 33])
+    dev = cu.cuda()
+    sets = [tensors([500, 33], [500, 33], 8, 2, torch.bfloat16, s) for s in (20, 21)]
+    want = [sel.prefill_attention(*x, cu, dev) for x in sets]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    for _ in range(10):
+        got = [sel.prefill_attention(*x, cu, dev, stream=s) for x, s in zip(sets, streams)]
+        torch.cuda.synchronize()
+        for a, b in zip(got, want):
+            assert torch.equal(a[0], b[0]) and torch.equal(a[1], b[1])
+    gr = torch.cuda.CUDAGraph()
+    x = [t.clone() for t in sets[0]]
+    with torch.cuda.graph(gr):
+        out, lse = sel.prefill_attention(*x, cu, dev)
+    for s, w in zip(sets[::-1], want[::-1]):
+        for a, b in zip(x, s):
+            a.copy_(b)
+        gr.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out, w[0]) and torch.equal(lse, w[1])
