@@ -15,7 +15,7 @@
 //                   tile's softmax runs beside the other's products;
 //   warps 10, 11    blocks that some row does not see wholly: zero what V holds there of
 //                   infinities and NaN, which a weight of zero would not keep out.  What a row
-//                   sees of them is added at the end (add_unbounded).
+//                   sees of them is added at the end.
 // The row maximum that the weights refer to moves only when a row's weights would pass 2^8
 // (kRescale): O is then scaled in TMEM, once in a while instead of at every block.
 #include <algorithm>
@@ -34,6 +34,9 @@ constexpr int kPfBuf = 2 * kPfHalf;                 // a tile or block: 32 KB
 constexpr int kPfStages = 5;
 constexpr int kPfThreads = 384;
 constexpr uint32_t kPfTmem = 512;                   // S0 | S1 | O0 | O1, 128 columns each
+// Registers of a thread: at launch (the most that 384 threads may have), and after the split.
+constexpr int kPfRegs = 168, kPfSoftmaxRegs = 208, kPfOtherRegs = 88;
+static_assert(256 * kPfSoftmaxRegs + 128 * kPfOtherRegs <= kPfThreads * kPfRegs, "the split fits what the block was launched with");
 constexpr float kRescale = 8.f;
 // The maximum before the first visible logit, finite: 2^(-inf - it) is 0.
 constexpr float kNoLogit = -3.402823466e38f;
@@ -49,7 +52,7 @@ struct PfArgs {
 struct __align__(8) PfBarriers {
     uint64_t full[kPfStages], empty[kPfStages];
     uint64_t q_full, dirty, clean, mma_done;   // dirty, clean: V of a block of partial sight is there / cleaned
-    uint64_t s_full[2], p_full[2], o_done[2];
+    uint64_t s_full[2], p_half[2], p_full[2], o_done[2];   // p_half: the weights of the block's first 64 keys
     uint32_t tmem_base;
     volatile int abort_flag;
     volatile int unbounded;      // a block of partial sight held an infinity or NaN in V
@@ -100,6 +103,12 @@ __device__ __forceinline__ bool find_item(const PfArgs& A, int x, Item& w) {
     w.whole_hi = pa;
     w.whole_lo = io.window ? pb - io.window + 1 : 0;
     return true;
+}
+
+__device__ __forceinline__ float max3(float a, float b, float c) {
+    float r;
+    asm("max.f32 %0, %1, %2, %3;\n" : "=f"(r) : "f"(a), "f"(b), "f"(c));
+    return r;
 }
 
 // 32 columns of 32-bit values to this warp's TMEM lanes.
@@ -157,27 +166,6 @@ __device__ __forceinline__ uint32_t unbounded_mask(uint32_t w) {   // the halves
     return ((w & e) == e ? 0xffffu : 0u) | (((w >> 16) & e) == e ? 0xffff0000u : 0u);
 }
 
-// The infinities and NaN that row (position p) sees in the blocks of partial sight: their
-// weights are positive, so each makes its output infinite or NaN.  Only where there are any.
-template <class T>
-__device__ __noinline__ void add_unbounded(const PfArgs& A, const Item& w, int p, int col, float* o) {
-    for (int i = 0; i < w.n; ++i) {
-        if (!w.edge(i, A.io.sinks)) continue;
-        for (int c = 0; c < kPfTile; ++c) {
-            const int t = w.block(i) * kPfTile + c;
-            if (t > p || (A.io.window && t <= p - A.io.window && t >= A.io.sinks)) continue;
-            const uint16_t* v = A.io.v + ((size_t)(w.k0 + t) * A.io.Hkv + w.h) * kHeadDim + col;
-            for (int d = 0; d < 32; d += 2) {
-                const uint32_t x = *reinterpret_cast<const uint32_t*>(v + d);
-                const uint32_t m = unbounded_mask<T>(x);
-                const float2 f = Half16<T>::unpack(x);
-                if (m & 0xffffu) o[d] += f.x;
-                if (m >> 16) o[d + 1] += f.y;
-            }
-        }
-    }
-}
-
 template <class T>
 __global__ void __launch_bounds__(kPfThreads, 1) prefill_kernel(const __grid_constant__ PfArgs A) {
     extern __shared__ uint8_t pf_smem_raw[];
@@ -201,7 +189,8 @@ __global__ void __launch_bounds__(kPfThreads, 1) prefill_kernel(const __grid_con
         ptx::mbar_init(&bars->mma_done, 1);
         for (int t = 0; t < 2; ++t) {
             ptx::mbar_init(&bars->s_full[t], 1);
-            ptx::mbar_init(&bars->p_full[t], 4);   // one arrival per warp of the tile
+            ptx::mbar_init(&bars->p_half[t], 4);   // one arrival per warp of the tile
+            ptx::mbar_init(&bars->p_full[t], 4);
             ptx::mbar_init(&bars->o_done[t], 1);
         }
         bars->abort_flag = 0;
@@ -224,7 +213,9 @@ __global__ void __launch_bounds__(kPfThreads, 1) prefill_kernel(const __grid_con
     const int n = any ? w.n : 0;
     const int sinks = A.io.sinks;
     bool stop = false;
-
+    // A softmax thread holds a row of S: registers move to the two softmax warpgroups.
+    if (warp >= 8) {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;\n" ::"n"(kPfOtherRegs));
     if (warp == 8) {
         // ------------------------------------------------------------ TMA
         // K and V blocks alternate: load 2 i is K, 2 i + 1 V; load x goes to stage x % kPfStages.
@@ -293,16 +284,20 @@ __global__ void __launch_bounds__(kPfThreads, 1) prefill_kernel(const __grid_con
             }
             __syncwarp();
         };
-        auto issue_o = [&](int t, int i, bool last) {   // O_t += P_t V_i
+        auto issue_o = [&](int t, int i, int half, bool last) {   // O_t += P_t V_i, 64 keys of it
             const int st = (2 * i + 1) % kPfStages;
             if (ptx::elect_one()) {
                 const uint64_t vd = vdesc + (uint32_t)(st * (kPfBuf >> 4));
 #pragma unroll
-                for (int kk = 0; kk < 8; ++kk)
+                for (int k4 = 0; k4 < 4; ++k4) {
+                    const int kk = half * 4 + k4;
                     mma_tmem_a(tmem + 256 + t * 128, tmem + t * 128 + kk * 8, vd + kk * (2048 >> 4), idesc_o,
                                i > 0 || kk > 0 ? 1u : 0u);
-                ptx::mma_commit(&bars->o_done[t]);
-                if (last) ptx::mma_commit(&bars->empty[st]);
+                }
+                if (half) {
+                    ptx::mma_commit(&bars->o_done[t]);
+                    if (last) ptx::mma_commit(&bars->empty[st]);
+                }
             }
             __syncwarp();
         };
@@ -318,9 +313,12 @@ __global__ void __launch_bounds__(kPfThreads, 1) prefill_kernel(const __grid_con
                     if (!wait(&bars->clean, cleaned++)) break;
                 }
                 for (int t = 0; t < tiles; ++t) {
+                    if (!wait(&bars->p_half[t], i)) break;
+                    ptx::tc_fence_after();
+                    issue_o(t, i, 0, t == tiles - 1);
                     if (!wait(&bars->p_full[t], i)) break;
                     ptx::tc_fence_after();
-                    issue_o(t, i, t == tiles - 1);
+                    issue_o(t, i, 1, t == tiles - 1);
                     if (i + 1 < n) {
                         if (t == 0 && !wait(&bars->full[xk % kPfStages], xk / kPfStages)) break;
                         issue_s(t, i + 1, t == tiles - 1);
@@ -336,7 +334,7 @@ __global__ void __launch_bounds__(kPfThreads, 1) prefill_kernel(const __grid_con
         if (ptx::elect_one()) ptx::mma_commit(&bars->mma_done);
         __syncwarp();
         ptx::mbar_wait(&bars->mma_done, 0, 50000000ull);
-    } else if (warp >= 10) {
+    } else {
         // ------------------------------------------------------------ V blocks of partial sight
         // The MMA warp hands a block over: a parity says nothing of a stage several rounds ahead.
         const int id = threadIdx.x - 320;
@@ -368,7 +366,10 @@ __global__ void __launch_bounds__(kPfThreads, 1) prefill_kernel(const __grid_con
             bars->abort_flag = 1;
             atomicExch(A.io.err, 3);
         }
-    } else if (any) {
+    }
+    } else {
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;\n" ::"n"(kPfSoftmaxRegs));
+        if (any) {
         // ------------------------------------------------------------ softmax
         const int t = warp >> 2, quad = warp & 3, row = quad * 32 + lane;
         const int query = w.a + t * A.nq + row / A.g, j = row % A.g;
@@ -377,7 +378,8 @@ __global__ void __launch_bounds__(kPfThreads, 1) prefill_kernel(const __grid_con
         const int below = A.io.window ? p - A.io.window : -1;     // keys up to here are out of the window
         const uint32_t lanes = (uint32_t)(quad * 32) << 16;
         const uint32_t tS = tmem + lanes + t * 128, tO = tmem + lanes + 256 + t * 128;
-        const uint64_t sl2 = ptx::pack_f32x2(A.sl2, A.sl2);
+        const float sl2f = A.sl2;
+        const uint64_t sl2 = ptx::pack_f32x2(sl2f, sl2f);
         float m = kNoLogit, l = 0.f;
         if (t < w.tiles) {
             for (int i = 0; i < n; ++i) {
@@ -400,8 +402,10 @@ __global__ void __launch_bounds__(kPfThreads, 1) prefill_kernel(const __grid_con
                 }
                 float mx[4] = {s[0], s[1], s[2], s[3]};
 #pragma unroll
-                for (int c = 4; c < 128; ++c) mx[c & 3] = fmaxf(mx[c & 3], s[c]);
-                const float top = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * A.sl2;
+                for (int c = 4; c < 124; c += 2) mx[(c >> 1) & 3] = max3(mx[(c >> 1) & 3], s[c], s[c + 1]);
+#pragma unroll
+                for (int c = 0; c < 4; ++c) mx[c] = fmaxf(mx[c], s[124 + c]);
+                const float top = fmaxf(max3(mx[0], mx[1], mx[2]), mx[3]) * sl2f;
                 if (i == 0) {
                     m = fmaxf(m, top);
                 } else if (__any_sync(0xffffffffu, top > m + kRescale)) {
@@ -438,12 +442,12 @@ __global__ void __launch_bounds__(kPfThreads, 1) prefill_kernel(const __grid_con
                         pk[e] = Half16<T>::pack(p0, p1);
                     }
                     tmem_st32(tS + c * 32, pk);
+                    tmem_wait_st();
+                    ptx::tc_fence_before();
+                    __syncwarp();
+                    if (lane == 0) ptx::mbar_arrive(c == 0 ? &bars->p_half[t] : &bars->p_full[t]);
                 }
                 l += ptx::lo_f32(sum) + ptx::hi_f32(sum);
-                tmem_wait_st();
-                ptx::tc_fence_before();
-                __syncwarp();
-                if (lane == 0) ptx::mbar_arrive(&bars->p_full[t]);
             }
             if (n > 0 && !stop && !ptx::warp_wait(&bars->o_done[t], (n - 1) & 1, abort)) stop = true;
             if (stop && lane == 0) {
@@ -452,7 +456,6 @@ __global__ void __launch_bounds__(kPfThreads, 1) prefill_kernel(const __grid_con
             }
             ptx::tc_fence_after();
             const float inv = l > 0.f || l != l ? 1.f / l : 0.f;
-            const bool unbounded = n > 0 && bars->unbounded != 0;
             const size_t at = (size_t)(w.q0 + query) * A.io.Hq + w.h * A.g + j;
 #pragma unroll
             for (int c = 0; c < 4; ++c) {
@@ -467,7 +470,6 @@ __global__ void __launch_bounds__(kPfThreads, 1) prefill_kernel(const __grid_con
 #pragma unroll
                 for (int d = 0; d < 32; ++d) o[d] = l > 0.f || l != l ? o[d] * inv : 0.f;
                 if (live) {
-                    if (unbounded) add_unbounded<T>(A, w, p, c * 32, o);
                     uint4* dst = reinterpret_cast<uint4*>(A.io.out + at * kHeadDim + c * 32);
 #pragma unroll
                     for (int d = 0; d < 4; ++d)
@@ -475,8 +477,26 @@ __global__ void __launch_bounds__(kPfThreads, 1) prefill_kernel(const __grid_con
                                             Half16<T>::pack(o[8 * d + 4], o[8 * d + 5]), Half16<T>::pack(o[8 * d + 6], o[8 * d + 7]));
                 }
             }
+            if (live && n > 0 && bars->unbounded) {
+                // The infinities and NaN that the row sees in the blocks of partial sight: their
+                // weights are positive, so each makes its output infinite or NaN.
+                uint16_t* dst = A.io.out + at * kHeadDim;
+                for (int i = 0; i < n; ++i) {
+                    if (!w.edge(i, sinks)) continue;
+                    for (int c = 0; c < kPfTile; ++c) {
+                        const int key = w.block(i) * kPfTile + c;
+                        if (key > p || (key <= below && key >= sinks)) continue;
+                        const uint16_t* v = A.io.v + ((size_t)(w.k0 + key) * A.io.Hkv + w.h) * kHeadDim;
+#pragma unroll 1
+                        for (int d = 0; d < kHeadDim; ++d)
+                            if (unbounded_mask<T>(v[d]))
+                                dst[d] = (uint16_t)Half16<T>::pack(Half16<T>::unpack(dst[d]).x + Half16<T>::unpack(v[d]).x, 0.f);
+                    }
+                }
+            }
             if (live && A.io.lse)
                 A.io.lse[at] = l > 0.f || l != l ? fmaf(m, 0.6931471805599453f, logf(l)) : -INFINITY;
+        }
         }
     }
     __syncthreads();
