@@ -1432,7 +1432,7 @@ kvec_status kvec_prefill_attention(kvec_handle* h, int dtype, int batch, const i
     s = set_device(h, &prev);
     if (s != KVEC_OK) return s;
     DeviceGuard guard{prev, h->device};
-    cudaError_t e = launch_prefill(io, reinterpret_cast<cudaStream_t>(stream));
+    cudaError_t e = launch_prefill(io, h->num_sms, reinterpret_cast<cudaStream_t>(stream));
     if (e != cudaSuccess) return cuda_fail(e, "prefill attention launch");
     return KVEC_OK;
 }

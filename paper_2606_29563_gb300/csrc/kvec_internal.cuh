@@ -300,7 +300,7 @@ cudaError_t launch_rotate(const RotateIO& io, const PagedCacheView& c, cudaStrea
 cudaError_t launch_paged_decode(const PagedDecodeIO& io, const PagedCacheView& c, int num_sms, cudaStream_t st);
 size_t paged_decode_scratch(int batch, int Hq, int Hkv, int max_len, bool weights, int num_sms);
 cudaError_t launch_evict(const EvictIO& io, const PagedCacheView& c, cudaStream_t st);
-cudaError_t launch_prefill(const PrefillIO& io, cudaStream_t st);
+cudaError_t launch_prefill(const PrefillIO& io, int num_sms, cudaStream_t st);
 // out_idx from the slot's kept-position bits, then the K/V rows.
 cudaError_t launch_gather(const Geometry& g, const Group& gr, cudaStream_t st, int priority, bool programmatic);
 

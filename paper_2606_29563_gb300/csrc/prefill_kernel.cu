@@ -16,8 +16,10 @@
 //   warps 10, 11    blocks that some row does not see wholly: zero what V holds there of
 //                   infinities and NaN, which a weight of zero would not keep out.  What a row
 //                   sees of them is added at the end.
-// The row maximum that the weights refer to moves only when a row's weights would pass 2^8
-// (kRescale): O is then scaled in TMEM, once in a while instead of at every block.
+// A row's weights refer to a maximum m that need not be the largest: it is that of the row's
+// first 64 visible keys, and moves only when the sum of 64 weights passes 2^14 (kMostWeight),
+// so that no block waits for a maximum and O is scaled in TMEM once in a while.  Results do not
+// depend on m: 2^(s - m) keeps its relative precision, and so does l.
 #include <algorithm>
 
 #include "half_types.cuh"
@@ -37,7 +39,8 @@ constexpr uint32_t kPfTmem = 512;                   // S0 | S1 | O0 | O1, 128 co
 // Registers of a thread: at launch (the most that 384 threads may have), and after the split.
 constexpr int kPfRegs = 168, kPfSoftmaxRegs = 208, kPfOtherRegs = 88;
 static_assert(256 * kPfSoftmaxRegs + 128 * kPfOtherRegs <= kPfThreads * kPfRegs, "the split fits what the block was launched with");
-constexpr float kRescale = 8.f;
+// The largest sum of a row's 64 weights: below it, no maximum of them is formed.  fp16 holds them.
+constexpr float kMostWeight = 16384.f;
 // The maximum before the first visible logit, finite: 2^(-inf - it) is 0.
 constexpr float kNoLogit = -3.402823466e38f;
 
@@ -46,16 +49,18 @@ struct PfArgs {
     PrefillIO io;
     int g, nq;       // query heads of a KV head, queries of a tile
     int pairs;       // tile pairs of the longest sequence
+    int items;       // pairs * batch * Hkv
     float sl2;
 };
 
 struct __align__(8) PfBarriers {
     uint64_t full[kPfStages], empty[kPfStages];
-    uint64_t q_full, dirty, clean, mma_done;   // dirty, clean: V of a block of partial sight is there / cleaned
-    uint64_t s_full[2], p_half[2], p_full[2], o_done[2];   // p_half: the weights of the block's first 64 keys
+    uint64_t clean[kPfStages];   // the cleaning warps have passed the stage
+    uint64_t q_full, q_empty, mma_done;
+    uint64_t s_full[2], p_half[2], p_full[2], o_half[2], o_done[2];   // half: of the block's first 64 keys
     uint32_t tmem_base;
     volatile int abort_flag;
-    volatile int unbounded;      // a block of partial sight held an infinity or NaN in V
+    volatile int unbounded;      // a block of partial sight held an infinity or NaN in V (of any item so far)
 };
 
 constexpr int kPfSmem = 1024 + (2 + kPfStages) * kPfBuf + (int)sizeof(PfBarriers);
@@ -78,6 +83,7 @@ struct Item {
 __device__ __forceinline__ bool find_item(const PfArgs& A, int x, Item& w) {
     // The last tiles, which see the most keys, first; a pair's KV heads side by side.
     const PrefillIO& io = A.io;
+    if (x >= A.items) return false;
     const int per = io.batch * io.Hkv;
     const int p = A.pairs - 1 - x / per;
     x %= per;
@@ -166,6 +172,14 @@ __device__ __forceinline__ uint32_t unbounded_mask(uint32_t w) {   // the halves
     return ((w & e) == e ? 0xffffu : 0u) | (((w >> 16) & e) == e ? 0xffff0000u : 0u);
 }
 
+__device__ __forceinline__ int item_of(int turn) {
+    const int c = blockIdx.x, G = gridDim.x;
+    return turn * G + (turn & 1 ? G - 1 - c : c);
+}
+
+// Persistent: of every gridDim.x items a CTA takes one, in turns from the front and from the
+// back (items cost less and less, so that the shares are even), and no role waits for an item's end: the next one's K and V follow through the ring, its first S is formed
+// behind the last products of this one, while the softmax warps write their outputs.
 template <class T>
 __global__ void __launch_bounds__(kPfThreads, 1) prefill_kernel(const __grid_constant__ PfArgs A) {
     extern __shared__ uint8_t pf_smem_raw[];
@@ -181,16 +195,17 @@ __global__ void __launch_bounds__(kPfThreads, 1) prefill_kernel(const __grid_con
         ptx::prefetch_tensormap(&A.vmap);
         for (int i = 0; i < kPfStages; ++i) {
             ptx::mbar_init(&bars->full[i], 1);
-            ptx::mbar_init(&bars->empty[i], 1);
+            ptx::mbar_init(&bars->empty[i], 3);    // the products, and the two cleaning warps
+            ptx::mbar_init(&bars->clean[i], 2);
         }
         ptx::mbar_init(&bars->q_full, 1);
-        ptx::mbar_init(&bars->dirty, 1);
-        ptx::mbar_init(&bars->clean, 2);
+        ptx::mbar_init(&bars->q_empty, 1);
         ptx::mbar_init(&bars->mma_done, 1);
         for (int t = 0; t < 2; ++t) {
             ptx::mbar_init(&bars->s_full[t], 1);
             ptx::mbar_init(&bars->p_half[t], 4);   // one arrival per warp of the tile
             ptx::mbar_init(&bars->p_full[t], 4);
+            ptx::mbar_init(&bars->o_half[t], 1);
             ptx::mbar_init(&bars->o_done[t], 1);
         }
         bars->abort_flag = 0;
@@ -206,184 +221,228 @@ __global__ void __launch_bounds__(kPfThreads, 1) prefill_kernel(const __grid_con
     ptx::tc_fence_after();
     asm volatile("griddepcontrol.launch_dependents;\n" ::: "memory");
     asm volatile("griddepcontrol.wait;\n" ::: "memory");
-    const uint32_t tmem = bars->tmem_base;
+    const uint32_t tmem = (uint32_t)ptx::warp_uniform((int)bars->tmem_base);
     const volatile int* const abort = &bars->abort_flag;
-    Item w{};
-    const bool any = find_item(A, blockIdx.x, w);
-    const int n = any ? w.n : 0;
-    const int sinks = A.io.sinks;
+    const int sinks = A.io.sinks, turns = (A.items + gridDim.x - 1) / gridDim.x;
     bool stop = false;
-    // A softmax thread holds a row of S: registers move to the two softmax warpgroups.
-    if (warp >= 8) {
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;\n" ::"n"(kPfOtherRegs));
-    if (warp == 8) {
-        // ------------------------------------------------------------ TMA
-        // K and V blocks alternate: load 2 i is K, 2 i + 1 V; load x goes to stage x % kPfStages.
-        const uint64_t policy = ptx::policy_evict_normal();
-        int loads = 0;
-        bool q_loaded = false;
-        if (n > 0) {
-            if (ptx::elect_one()) {
-                const uint32_t bytes = (uint32_t)(A.nq * A.g) * 128u;
-                ptx::mbar_arrive_expect_tx(&bars->q_full, 2u * bytes * (uint32_t)w.tiles);
-                for (int t = 0; t < w.tiles; ++t)
-                    for (int c = 0; c < 2; ++c)
-                        ptx::tma_load_3d(sQ + t * kPfBuf + c * kPfHalf, &A.qmap, &bars->q_full, c * 64, w.h * A.g,
-                                         w.q0 + w.a + t * A.nq, policy);
-            }
-            __syncwarp();
-            q_loaded = true;
-            for (int x = 0; x < 2 * n; ++x) {
-                const int st = x % kPfStages, round = x / kPfStages;
-                if (round > 0 && !ptx::warp_wait(&bars->empty[st], (round - 1) & 1, abort)) {
-                    stop = true;
-                    break;
-                }
-                if (ptx::elect_one()) {
-                    const CUtensorMap* map = x & 1 ? &A.vmap : &A.kmap;
-                    uint8_t* dst = ring + st * kPfBuf;
-                    const int row = w.k0 + w.block(x >> 1) * kPfTile;
-                    ptx::mbar_arrive_expect_tx(&bars->full[st], (uint32_t)kPfBuf);
-                    ptx::tma_load_3d(dst, map, &bars->full[st], 0, w.h, row, policy);
-                    ptx::tma_load_3d(dst + kPfHalf, map, &bars->full[st], 64, w.h, row, policy);
-                }
-                __syncwarp();
-                ++loads;
-            }
-        }
+    auto give_up = [&]() {
         if (stop && lane == 0) {
             bars->abort_flag = 1;
             atomicExch(A.io.err, 3);
         }
-        // Every issued copy lands before the CTA may exit.
-        for (int x = max(loads - kPfStages, 0); x < loads; ++x)
-            ptx::mbar_wait(&bars->full[x % kPfStages], (x / kPfStages) & 1, 50000000ull);
-        if (q_loaded) ptx::mbar_wait(&bars->q_full, 0, 50000000ull);
-    } else if (warp == 9) {
-        // ------------------------------------------------------------ MMA
-        const uint32_t idesc_s = pf_idesc<T>(false), idesc_o = pf_idesc<T>(true);
-        const uint64_t qdesc = ptx::smem_desc_k_sw128(ptx::smem_u32(sQ));
-        const uint64_t kdesc = ptx::smem_desc_k_sw128(ptx::smem_u32(ring));
-        const uint64_t vdesc = smem_desc_mn_sw128(ptx::smem_u32(ring));
-        const int tiles = w.tiles;
-        auto wait = [&](uint64_t* bar, int phase) {
-            if (!stop && !ptx::warp_wait(bar, phase & 1, abort)) stop = true;
-            return !stop;
-        };
-        auto issue_s = [&](int t, int i, bool last) {   // S_t = Q_t K_i^T
-            const int st = (2 * i) % kPfStages;
-            if (ptx::elect_one()) {
-                const uint64_t kd = kdesc + (uint32_t)(st * (kPfBuf >> 4)), qd = qdesc + (uint32_t)(t * (kPfBuf >> 4));
-#pragma unroll
-                for (int kk = 0; kk < 8; ++kk) {
-                    const uint32_t ofs = (kk >> 2) * (kPfHalf >> 4) + (kk & 3) * 2;
-                    ptx::mma_bf16(tmem + t * 128, qd + ofs, kd + ofs, idesc_s, kk > 0 ? 1u : 0u);
+    };
+    // A softmax thread holds a row of S: registers move to the two softmax warpgroups.
+    if (warp >= 8) {
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;\n" ::"n"(kPfOtherRegs));
+        int x = 0;   // loads of K and V so far: load x goes to stage x % kPfStages
+        if (warp == 8) {
+            // -------------------------------------------------------- TMA
+            const uint64_t policy = ptx::policy_evict_normal();
+            int qloads = 0;
+            for (int turn = 0; turn < turns && !stop; ++turn) {
+                Item w{};
+                if (!find_item(A, item_of(turn), w) || w.n == 0) continue;
+                auto load_kv = [&](int y) {   // load y of the item: K and V blocks alternate
+                    const int st = x % kPfStages, round = x / kPfStages;
+                    if (round > 0 && !ptx::warp_wait(&bars->empty[st], (round - 1) & 1, abort)) {
+                        stop = true;
+                        return;
+                    }
+                    if (ptx::elect_one()) {
+                        const CUtensorMap* map = y & 1 ? &A.vmap : &A.kmap;
+                        uint8_t* dst = ring + st * kPfBuf;
+                        const int row = w.k0 + w.block(y >> 1) * kPfTile;
+                        ptx::mbar_arrive_expect_tx(&bars->full[st], (uint32_t)kPfBuf);
+                        ptx::tma_load_3d(dst, map, &bars->full[st], 0, w.h, row, policy);
+                        ptx::tma_load_3d(dst + kPfHalf, map, &bars->full[st], 64, w.h, row, policy);
+                    }
+                    __syncwarp();
+                    ++x;
+                };
+                load_kv(0);
+                // The queries' buffers are free once the item before has formed its last S.
+                if (!stop && qloads > 0 && !ptx::warp_wait(&bars->q_empty, (qloads - 1) & 1, abort)) stop = true;
+                if (stop) break;
+                if (ptx::elect_one()) {
+                    const uint32_t bytes = (uint32_t)(A.nq * A.g) * 128u;
+                    ptx::mbar_arrive_expect_tx(&bars->q_full, 2u * bytes * (uint32_t)w.tiles);
+                    for (int t = 0; t < w.tiles; ++t)
+                        for (int c = 0; c < 2; ++c)
+                            ptx::tma_load_3d(sQ + t * kPfBuf + c * kPfHalf, &A.qmap, &bars->q_full, c * 64, w.h * A.g,
+                                             w.q0 + w.a + t * A.nq, policy);
                 }
-                ptx::mma_commit(&bars->s_full[t]);
-                if (last) ptx::mma_commit(&bars->empty[st]);
+                __syncwarp();
+                ++qloads;
+                for (int y = 1; y < 2 * w.n && !stop; ++y) load_kv(y);
             }
-            __syncwarp();
-        };
-        auto issue_o = [&](int t, int i, int half, bool last) {   // O_t += P_t V_i, 64 keys of it
-            const int st = (2 * i + 1) % kPfStages;
-            if (ptx::elect_one()) {
-                const uint64_t vd = vdesc + (uint32_t)(st * (kPfBuf >> 4));
+            give_up();
+            // Every issued copy lands before the CTA may exit.
+            for (int y = max(x - kPfStages, 0); y < x; ++y)
+                ptx::mbar_wait(&bars->full[y % kPfStages], (y / kPfStages) & 1, 50000000ull);
+            if (qloads > 0) ptx::mbar_wait(&bars->q_full, (qloads - 1) & 1, 50000000ull);
+        } else if (warp == 9) {
+            // -------------------------------------------------------- MMA
+            const uint32_t idesc_s = pf_idesc<T>(false), idesc_o = pf_idesc<T>(true);
+            const uint64_t qdesc = ptx::smem_desc_k_sw128(ptx::smem_u32(sQ));
+            const uint64_t kdesc = ptx::smem_desc_k_sw128(ptx::smem_u32(ring));
+            const uint64_t vdesc = smem_desc_mn_sw128(ptx::smem_u32(ring));
+            auto wait = [&](uint64_t* bar, int phase) {
+                if (!stop && !ptx::warp_wait(bar, phase & 1, abort)) stop = true;
+                return !stop;
+            };
+            // Stages as values that the compiler knows to be the warp's, so that descriptors stay in uniform registers.
+            auto issue_s = [&](int t, int y, bool last) {   // S_t = Q_t K^T, K of load y
+                const int st = ptx::warp_uniform(y % kPfStages);
+                if (ptx::elect_one()) {
+                    const uint64_t kd = kdesc + (uint32_t)(st * (kPfBuf >> 4)), qd = qdesc + (uint32_t)(t * (kPfBuf >> 4));
 #pragma unroll
-                for (int k4 = 0; k4 < 4; ++k4) {
-                    const int kk = half * 4 + k4;
-                    mma_tmem_a(tmem + 256 + t * 128, tmem + t * 128 + kk * 8, vd + kk * (2048 >> 4), idesc_o,
-                               i > 0 || kk > 0 ? 1u : 0u);
-                }
-                if (half) {
-                    ptx::mma_commit(&bars->o_done[t]);
+                    for (int kk = 0; kk < 8; ++kk) {
+                        const uint32_t ofs = (kk >> 2) * (kPfHalf >> 4) + (kk & 3) * 2;
+                        ptx::mma_bf16(tmem + t * 128, qd + ofs, kd + ofs, idesc_s, kk > 0 ? 1u : 0u);
+                    }
+                    ptx::mma_commit(&bars->s_full[t]);
                     if (last) ptx::mma_commit(&bars->empty[st]);
                 }
-            }
-            __syncwarp();
-        };
-        if (n > 0 && wait(&bars->q_full, 0) && wait(&bars->full[0], 0)) {
-            ptx::tc_fence_after();
-            for (int t = 0; t < tiles; ++t) issue_s(t, 0, t == tiles - 1);
-            int cleaned = 0;
-            for (int i = 0; i < n && !stop; ++i) {
-                const int xv = 2 * i + 1, xk = 2 * i + 2;
-                if (!wait(&bars->full[xv % kPfStages], xv / kPfStages)) break;
-                if (w.edge(i, sinks)) {
-                    if (lane == 0) ptx::mbar_arrive(&bars->dirty);
-                    if (!wait(&bars->clean, cleaned++)) break;
+                __syncwarp();
+            };
+            auto issue_o = [&](int t, int y, bool add, int half, bool last) {   // O_t += P_t V, 64 keys of load y
+                const int st = ptx::warp_uniform(y % kPfStages);
+                if (ptx::elect_one()) {
+                    const uint64_t vd = vdesc + (uint32_t)(st * (kPfBuf >> 4));
+#pragma unroll
+                    for (int k4 = 0; k4 < 4; ++k4) {
+                        const int kk = half * 4 + k4;
+                        mma_tmem_a(tmem + 256 + t * 128, tmem + t * 128 + kk * 8, vd + kk * (2048 >> 4), idesc_o,
+                                   add || kk > 0 ? 1u : 0u);
+                    }
+                    ptx::mma_commit(half ? &bars->o_done[t] : &bars->o_half[t]);
+                    if (half && last) ptx::mma_commit(&bars->empty[st]);
                 }
-                for (int t = 0; t < tiles; ++t) {
-                    if (!wait(&bars->p_half[t], i)) break;
-                    ptx::tc_fence_after();
-                    issue_o(t, i, 0, t == tiles - 1);
-                    if (!wait(&bars->p_full[t], i)) break;
-                    ptx::tc_fence_after();
-                    issue_o(t, i, 1, t == tiles - 1);
-                    if (i + 1 < n) {
-                        if (t == 0 && !wait(&bars->full[xk % kPfStages], xk / kPfStages)) break;
-                        issue_s(t, i + 1, t == tiles - 1);
+                __syncwarp();
+            };
+            int qloads = 0, blocks[2] = {0, 0};   // blocks of each tile so far: the phase of its P
+            // S of an item's first block is issued between the last products of the item before.
+            Item w{};
+            int turn = 0;
+            auto next_item = [&]() {
+                while (turn < turns)
+                    if (find_item(A, item_of(turn++), w) && w.n > 0) return true;
+                return false;
+            };
+            bool more = next_item();
+            if (more && wait(&bars->full[0], 0) && wait(&bars->q_full, 0)) {
+                ptx::tc_fence_after();
+                for (int t = 0; t < w.tiles; ++t) issue_s(t, 0, t == w.tiles - 1);
+                ++qloads;
+                if (w.n == 1 && ptx::elect_one()) ptx::mma_commit(&bars->q_empty);
+                __syncwarp();
+            }
+            while (more && !stop) {
+                const Item cur = w;
+                for (int i = 0; i < cur.n && !stop; ++i) {
+                    const bool last_block = i + 1 == cur.n;
+                    if (last_block) more = next_item();
+                    const int xv = x + 1;
+                    x += 2;
+                    // The tiles that the next S is for: this item's, or the next one's.
+                    const int next_tiles = !last_block ? cur.tiles : more ? w.tiles : 0;
+                    if (!wait(&bars->full[xv % kPfStages], xv / kPfStages)) break;
+                    if (cur.edge(i, sinks) && !wait(&bars->clean[xv % kPfStages], xv / kPfStages)) break;
+#pragma unroll
+                    for (int t = 0; t < 2; ++t) {
+                        if (t < cur.tiles) {
+                            if (!wait(&bars->p_half[t], blocks[t])) break;
+                            ptx::tc_fence_after();
+                            issue_o(t, xv, i > 0, 0, t == cur.tiles - 1);
+                        }
+                        if (t == 0 && next_tiles > 0) {
+                            if (!wait(&bars->full[x % kPfStages], x / kPfStages)) break;
+                            if (last_block && !wait(&bars->q_full, qloads)) break;
+                        }
+                        if (t < cur.tiles) {
+                            if (!wait(&bars->p_full[t], blocks[t])) break;
+                            ptx::tc_fence_after();
+                            issue_o(t, xv, i > 0, 1, t == cur.tiles - 1);
+                            ++blocks[t];
+                        }
+                        if (t < next_tiles) {
+                            ptx::tc_fence_after();
+                            issue_s(t, x, t == next_tiles - 1);
+                        }
+                    }
+                    if (stop) break;
+                    if (last_block && more) ++qloads;
+                    // The item's queries have been read once its last S is done.
+                    const bool q_last = last_block ? more && w.n == 1 : i + 2 == cur.n;
+                    if (q_last) {
+                        if (ptx::elect_one()) ptx::mma_commit(&bars->q_empty);
+                        __syncwarp();
                     }
                 }
             }
-        }
-        if (stop && lane == 0) {
-            bars->abort_flag = 1;
-            atomicExch(A.io.err, 3);
-        }
-        // The products in flight end before TMEM is freed.
-        if (ptx::elect_one()) ptx::mma_commit(&bars->mma_done);
-        __syncwarp();
-        ptx::mbar_wait(&bars->mma_done, 0, 50000000ull);
-    } else {
-        // ------------------------------------------------------------ V blocks of partial sight
-        // The MMA warp hands a block over: a parity says nothing of a stage several rounds ahead.
-        const int id = threadIdx.x - 320;
-        int edges = 0;
-        for (int i = 0; i < n && !stop; ++i) {
-            if (!w.edge(i, sinks)) continue;
-            const int x = 2 * i + 1, st = x % kPfStages;
-            if (!ptx::warp_wait(&bars->dirty, edges++ & 1, abort) ||
-                !ptx::warp_wait(&bars->full[st], (x / kPfStages) & 1, abort)) {
-                stop = true;
-                break;
-            }
-            uint4* v = reinterpret_cast<uint4*>(ring + st * kPfBuf);
-            bool found = false;
-            for (int e = id; e < kPfBuf / 16; e += 64) {
-                uint4 u = v[e];
-                const uint4 m = make_uint4(unbounded_mask<T>(u.x), unbounded_mask<T>(u.y), unbounded_mask<T>(u.z), unbounded_mask<T>(u.w));
-                if (m.x | m.y | m.z | m.w) {
-                    v[e] = make_uint4(u.x & ~m.x, u.y & ~m.y, u.z & ~m.z, u.w & ~m.w);
-                    found = true;
+            give_up();
+            // The products in flight end before TMEM is freed.
+            if (ptx::elect_one()) ptx::mma_commit(&bars->mma_done);
+            __syncwarp();
+            ptx::mbar_wait(&bars->mma_done, 0, 50000000ull);
+        } else {
+            // -------------------------------------------------------- V blocks of partial sight
+            // Every load is passed in turn: a parity says nothing of a stage several rounds ahead.
+            for (int turn = 0; turn < turns && !stop; ++turn) {
+                Item w{};
+                if (!find_item(A, item_of(turn), w)) continue;
+                for (int y = 0; y < 2 * w.n; ++y, ++x) {
+                    const int st = x % kPfStages;
+                    if (!ptx::warp_wait(&bars->full[st], (x / kPfStages) & 1, abort)) {
+                        stop = true;
+                        break;
+                    }
+                    if ((y & 1) && w.edge(y >> 1, sinks)) {
+                        uint4* v = reinterpret_cast<uint4*>(ring + st * kPfBuf);
+                        bool found = false;
+#pragma unroll 8
+                        for (int e = threadIdx.x - 320; e < kPfBuf / 16; e += 64) {
+                            const uint4 u = v[e];
+                            const uint4 m = make_uint4(unbounded_mask<T>(u.x), unbounded_mask<T>(u.y), unbounded_mask<T>(u.z),
+                                                       unbounded_mask<T>(u.w));
+                            if (m.x | m.y | m.z | m.w) {
+                                v[e] = make_uint4(u.x & ~m.x, u.y & ~m.y, u.z & ~m.z, u.w & ~m.w);
+                                found = true;
+                            }
+                        }
+                        if (found) bars->unbounded = 1;
+                        ptx::fence_proxy_async_smem();
+                    }
+                    __syncwarp();
+                    if (lane == 0) {
+                        ptx::mbar_arrive(&bars->clean[st]);
+                        ptx::mbar_arrive(&bars->empty[st]);
+                    }
                 }
             }
-            if (found) bars->unbounded = 1;
-            ptx::fence_proxy_async_smem();
-            __syncwarp();
-            if (lane == 0) ptx::mbar_arrive(&bars->clean);
+            give_up();
         }
-        if (stop && lane == 0) {
-            bars->abort_flag = 1;
-            atomicExch(A.io.err, 3);
-        }
-    }
     } else {
         asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;\n" ::"n"(kPfSoftmaxRegs));
-        if (any) {
         // ------------------------------------------------------------ softmax
         const int t = warp >> 2, quad = warp & 3, row = quad * 32 + lane;
-        const int query = w.a + t * A.nq + row / A.g, j = row % A.g;
-        const bool live = row < A.nq * A.g && query < w.b;       // the row is a real one
-        const int p = w.off + query;
-        const int below = A.io.window ? p - A.io.window : -1;     // keys up to here are out of the window
+        const int row_q = row / A.g, j = row - row_q * A.g;
         const uint32_t lanes = (uint32_t)(quad * 32) << 16;
         const uint32_t tS = tmem + lanes + t * 128, tO = tmem + lanes + 256 + t * 128;
         const float sl2f = A.sl2;
         const uint64_t sl2 = ptx::pack_f32x2(sl2f, sl2f);
-        float m = kNoLogit, l = 0.f;
-        if (t < w.tiles) {
-            for (int i = 0; i < n; ++i) {
-                if (!ptx::warp_wait(&bars->s_full[t], i & 1, abort)) {
+        int blocks = 0;   // of this tile: the phase of its barriers
+        for (int turn = 0; turn < turns && !stop; ++turn) {
+            Item w{};
+            if (!find_item(A, item_of(turn), w) || t >= w.tiles) continue;
+            const int query = w.a + t * A.nq + row_q;
+            const bool live = row < A.nq * A.g && query < w.b;        // the row is a real one
+            const int p = w.off + query;
+            const int below = A.io.window ? p - A.io.window : -1;     // keys up to here are out of the window
+            const int n = w.n;
+            float m = kNoLogit, l = 0.f;
+            for (int i = 0; i < n; ++i, ++blocks) {
+                if (!ptx::warp_wait(&bars->s_full[t], blocks & 1, abort)) {
                     stop = true;
                     break;
                 }
@@ -400,62 +459,67 @@ __global__ void __launch_bounds__(kPfThreads, 1) prefill_kernel(const __grid_con
                         if (key > p || (key <= below && key >= sinks)) s[c] = -INFINITY;
                     }
                 }
-                float mx[4] = {s[0], s[1], s[2], s[3]};
-#pragma unroll
-                for (int c = 4; c < 124; c += 2) mx[(c >> 1) & 3] = max3(mx[(c >> 1) & 3], s[c], s[c + 1]);
-#pragma unroll
-                for (int c = 0; c < 4; ++c) mx[c] = fmaxf(mx[c], s[124 + c]);
-                const float top = fmaxf(max3(mx[0], mx[1], mx[2]), mx[3]) * sl2f;
-                if (i == 0) {
-                    m = fmaxf(m, top);
-                } else if (__any_sync(0xffffffffu, top > m + kRescale)) {
-                    // Rare: the outputs so far to the new maximum, once the products of the block before are done.
-                    if (!ptx::warp_wait(&bars->o_done[t], (i - 1) & 1, abort)) {
-                        stop = true;
-                        break;
-                    }
-                    ptx::tc_fence_after();
-                    const float mn = top > m + kRescale ? top : m;
-                    const float f = ptx::ex2(m - mn);
-                    l *= f;
-                    m = mn;
-#pragma unroll
-                    for (int c = 0; c < 4; ++c) {
-                        float o[32];
-                        ptx::tmem_ld32(tO + c * 32, o);
-                        ptx::tmem_wait_ld();
-#pragma unroll
-                        for (int d = 0; d < 32; ++d) o[d] *= f;
-                        tmem_st32(tO + c * 32, reinterpret_cast<const uint32_t*>(o));
-                    }
-                }
-                const uint64_t ref = ptx::pack_f32x2(-m, -m);
-                uint64_t sum = 0ull;
-#pragma unroll
-                for (int c = 0; c < 2; ++c) {
-                    uint32_t pk[32];
+                // The weights of 64 keys relative to m, as pairs of 16-bit values, and their sum.
+                uint32_t pk[32];
+                auto weights = [&](const float* x) {
+                    const uint64_t ref = ptx::pack_f32x2(-m, -m);
+                    uint64_t sum[4] = {0ull, 0ull, 0ull, 0ull};
 #pragma unroll
                     for (int e = 0; e < 32; ++e) {
-                        const uint64_t x = ptx::fma_f32x2(ptx::pack_f32x2(s[c * 64 + 2 * e], s[c * 64 + 2 * e + 1]), sl2, ref);
-                        const float p0 = ptx::ex2(ptx::lo_f32(x)), p1 = ptx::ex2(ptx::hi_f32(x));
-                        sum = ptx::add_f32x2(sum, ptx::pack_f32x2(p0, p1));
+                        const uint64_t y = ptx::fma_f32x2(ptx::pack_f32x2(x[2 * e], x[2 * e + 1]), sl2, ref);
+                        const float p0 = ptx::ex2(ptx::lo_f32(y)), p1 = ptx::ex2(ptx::hi_f32(y));
+                        sum[e & 3] = ptx::add_f32x2(sum[e & 3], ptx::pack_f32x2(p0, p1));
                         pk[e] = Half16<T>::pack(p0, p1);
                     }
+                    const uint64_t all = ptx::add_f32x2(ptx::add_f32x2(sum[0], sum[1]), ptx::add_f32x2(sum[2], sum[3]));
+                    return ptx::lo_f32(all) + ptx::hi_f32(all);
+                };
+#pragma unroll
+                for (int c = 0; c < 2; ++c) {
+                    float z = weights(s + c * 64);
+                    if (__any_sync(0xffffffffu, !(z < kMostWeight))) {
+                        // The row's first logits, or ones far above m (or NaN): m moves to the largest.
+                        float mx = m;
+#pragma unroll
+                        for (int e = 0; e < 64; e += 2) mx = max3(mx, s[c * 64 + e] * sl2f, s[c * 64 + e + 1] * sl2f);
+                        if (z < kMostWeight) mx = m;
+                        const float f = ptx::ex2(m - mx);
+                        l *= f;
+                        m = mx;
+                        if (i > 0 || c > 0) {
+                            // The outputs so far with it, once their products are done.
+                            if (!(c > 0 ? ptx::warp_wait(&bars->o_half[t], blocks & 1, abort)
+                                        : ptx::warp_wait(&bars->o_done[t], (blocks - 1) & 1, abort))) {
+                                stop = true;
+                                break;
+                            }
+                            ptx::tc_fence_after();
+#pragma unroll 1
+                            for (int d0 = 0; d0 < kHeadDim; d0 += 32) {
+                                float o[32];
+                                ptx::tmem_ld32(tO + d0, o);
+                                ptx::tmem_wait_ld();
+#pragma unroll
+                                for (int d = 0; d < 32; ++d) o[d] *= f;
+                                tmem_st32(tO + d0, reinterpret_cast<const uint32_t*>(o));
+                            }
+                        }
+                        z = weights(s + c * 64);
+                    }
+                    l += z;
                     tmem_st32(tS + c * 32, pk);
                     tmem_wait_st();
                     ptx::tc_fence_before();
                     __syncwarp();
                     if (lane == 0) ptx::mbar_arrive(c == 0 ? &bars->p_half[t] : &bars->p_full[t]);
                 }
-                l += ptx::lo_f32(sum) + ptx::hi_f32(sum);
+                if (stop) break;
             }
-            if (n > 0 && !stop && !ptx::warp_wait(&bars->o_done[t], (n - 1) & 1, abort)) stop = true;
-            if (stop && lane == 0) {
-                bars->abort_flag = 1;
-                atomicExch(A.io.err, 3);
-            }
+            if (n > 0 && !stop && !ptx::warp_wait(&bars->o_done[t], (blocks - 1) & 1, abort)) stop = true;
+            if (stop) break;
             ptx::tc_fence_after();
-            const float inv = l > 0.f || l != l ? 1.f / l : 0.f;
+            const bool some = l > 0.f || l != l;
+            const float inv = some ? 1.f / l : 0.f;
             const size_t at = (size_t)(w.q0 + query) * A.io.Hq + w.h * A.g + j;
 #pragma unroll
             for (int c = 0; c < 4; ++c) {
@@ -468,7 +532,7 @@ __global__ void __launch_bounds__(kPfThreads, 1) prefill_kernel(const __grid_con
                     for (int d = 0; d < 32; ++d) o[d] = 0.f;
                 }
 #pragma unroll
-                for (int d = 0; d < 32; ++d) o[d] = l > 0.f || l != l ? o[d] * inv : 0.f;
+                for (int d = 0; d < 32; ++d) o[d] = some ? o[d] * inv : 0.f;
                 if (live) {
                     uint4* dst = reinterpret_cast<uint4*>(A.io.out + at * kHeadDim + c * 32);
 #pragma unroll
@@ -477,6 +541,7 @@ __global__ void __launch_bounds__(kPfThreads, 1) prefill_kernel(const __grid_con
                                             Half16<T>::pack(o[8 * d + 4], o[8 * d + 5]), Half16<T>::pack(o[8 * d + 6], o[8 * d + 7]));
                 }
             }
+            ptx::tc_fence_before();   // O has been read before the next item's weights are handed over
             if (live && n > 0 && bars->unbounded) {
                 // The infinities and NaN that the row sees in the blocks of partial sight: their
                 // weights are positive, so each makes its output infinite or NaN.
@@ -494,20 +559,18 @@ __global__ void __launch_bounds__(kPfThreads, 1) prefill_kernel(const __grid_con
                     }
                 }
             }
-            if (live && A.io.lse)
-                A.io.lse[at] = l > 0.f || l != l ? fmaf(m, 0.6931471805599453f, logf(l)) : -INFINITY;
+            if (live && A.io.lse) A.io.lse[at] = some ? fmaf(m, 0.6931471805599453f, logf(l)) : -INFINITY;
+            __syncwarp();
         }
-        }
+        give_up();
     }
     __syncthreads();
     if (warp == 9) ptx::tmem_dealloc(tmem, kPfTmem);
 }
 
 template <class T>
-cudaError_t launch_typed(const PfArgs& a, cudaStream_t st) {
-    const long long items = (long long)a.pairs * a.io.batch * a.io.Hkv;
-    if (items > 0x7fffffffll) return cudaErrorInvalidConfiguration;
-    return launch_prio(prefill_kernel<T>, dim3((unsigned)items), dim3(kPfThreads), kPfSmem, st, 0, true, a);
+cudaError_t launch_typed(const PfArgs& a, int num_sms, cudaStream_t st) {
+    return launch_prio(prefill_kernel<T>, dim3((unsigned)std::min(a.items, num_sms)), dim3(kPfThreads), kPfSmem, st, 0, true, a);
 }
 
 }  // namespace
@@ -519,12 +582,15 @@ cudaError_t configure_prefill() {
     return e;
 }
 
-cudaError_t launch_prefill(const PrefillIO& io, cudaStream_t st) {
+cudaError_t launch_prefill(const PrefillIO& io, int num_sms, cudaStream_t st) {
     PfArgs a{};
     a.io = io;
     a.g = io.Hq / io.Hkv;
     a.nq = kPfTile / a.g;
     a.pairs = (io.max_q + 2 * a.nq - 1) / (2 * a.nq);
+    const long long items = (long long)a.pairs * io.batch * io.Hkv;
+    if (items > 0x3fffffffll) return cudaErrorInvalidConfiguration;
+    a.items = (int)items;
     a.sl2 = io.scale * 1.4426950408889634f;
     const uint64_t row = (uint64_t)kHeadDim * 2;
     const uint64_t qd[3] = {(uint64_t)kHeadDim, (uint64_t)io.Hq, (uint64_t)io.total_q}, qs[2] = {row, row * io.Hq};
@@ -537,7 +603,7 @@ cudaError_t launch_prefill(const PrefillIO& io, cudaStream_t st) {
     if (e == cudaSuccess) e = encode_tensor_map(&a.kmap, io.dtype, 3, keys ? io.k : io.q, kd, ks, kb);
     if (e == cudaSuccess) e = encode_tensor_map(&a.vmap, io.dtype, 3, keys ? io.v : io.q, kd, ks, kb);
     if (e != cudaSuccess) return e;
-    return io.dtype == 1 ? launch_typed<__half>(a, st) : launch_typed<__nv_bfloat16>(a, st);
+    return io.dtype == 1 ? launch_typed<__half>(a, num_sms, st) : launch_typed<__nv_bfloat16>(a, num_sms, st);
 }
 
 }  // namespace kvec
