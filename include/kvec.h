@@ -376,6 +376,12 @@ KVEC_API kvec_status kvec_paged_evict(kvec_handle* h, int batch, const kvec_page
                                       int sinks, int recent, int32_t* new_lens, int32_t* kept,
                                       kvec_stream_t stream);
 
+/* Bytes of scratch that kvec_prefill_attention needs for these lengths: 0 for most, more
+ * where there are so few query rows that the keys have to be divided over the device (and 0
+ * if an argument is invalid).  Host only. */
+KVEC_API size_t kvec_prefill_bytes(kvec_handle* h, int batch, const int32_t* cu_q_host, const int32_t* cu_k_host,
+                                   int window, int sinks);
+
 /* Causal attention of packed sequences, optionally with a sliding window and first tokens
  * that stay visible, and the log-sum-exp of every row: the prefill step before
  * kvec_select_layer_lse.  Sequence s has L_q query rows and L_k keys (cu_q, cu_k: host and
@@ -387,7 +393,9 @@ KVEC_API kvec_status kvec_paged_evict(kvec_handle* h, int batch, const kvec_page
  * A row that sees nothing (p < 0) gives zeros and -infinity.  Keys and values that a row does
  * not see have no effect on it, whatever they hold.
  *   q    device dtype [cu_q[batch]][H_q][d];  k, v device dtype [cu_k[batch]][H_kv][d].
- *   out  device dtype, as q;  lse device fp32 [cu_q[batch]][H_q], or NULL.
+ *   out  device dtype, as q, 32-byte aligned;  lse device fp32 [cu_q[batch]][H_q], or NULL.
+ *   scratch  device, kvec_prefill_bytes bytes, 32-byte aligned (NULL for none): written and
+ *            read within the call; calls that may overlap need one each.
  * Lengths up to 2^20; the weights are rounded to dtype before they meet the values, the sums
  * are fp32.  A bounded wait that gave up is reported by kvec_sync_status. */
 KVEC_API kvec_status kvec_prefill_attention(kvec_handle* h, int dtype, int batch,
@@ -395,7 +403,7 @@ KVEC_API kvec_status kvec_prefill_attention(kvec_handle* h, int dtype, int batch
                                             const int32_t* cu_k_host, const int32_t* cu_k_dev,
                                             const void* q, const void* k, const void* v,
                                             int window, int sinks, void* out, float* lse,
-                                            kvec_stream_t stream);
+                                            void* scratch, size_t scratch_bytes, kvec_stream_t stream);
 
 /* Device views of the last processed layer's intermediates (valid until the
  * next call on the handle; read after synchronising the stream).  Row strides

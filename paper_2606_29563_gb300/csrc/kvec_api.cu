@@ -1379,34 +1379,58 @@ kvec_status kvec_paged_evict(kvec_handle* h, int batch, const kvec_paged_cache* 
     return KVEC_OK;
 }
 
-kvec_status kvec_prefill_attention(kvec_handle* h, int dtype, int batch, const int32_t* cu_q_host,
-                                   const int32_t* cu_q_dev, const int32_t* cu_k_host, const int32_t* cu_k_dev,
-                                   const void* q, const void* k, const void* v, int window, int sinks, void* out,
-                                   float* lse, kvec_stream_t stream) {
-    if (dtype != KVEC_BF16 && dtype != KVEC_FP16)
-        return fail(KVEC_ERR_INVALID_ARG, "dtype %d is neither KVEC_BF16 nor KVEC_FP16", dtype);
+namespace {
+
+// The checks of a prefill call that need no handle, and its longest sequences.
+kvec_status check_prefill(int batch, const int32_t* cu_q, const int32_t* cu_k, int window, int sinks, int* max_q, int* max_k) {
     kvec_status s = check_window(window, sinks);
     if (s != KVEC_OK) return s;
     if (batch < 1 || batch > kMaxGridBatch) return fail(KVEC_ERR_INVALID_ARG, "batch %d outside [1, %d]", batch, kMaxGridBatch);
-    if (!cu_q_host || !cu_q_dev || !cu_k_host || !cu_k_dev)
-        return fail(KVEC_ERR_INVALID_ARG, "cu_seqlens pointers must not be NULL");
-    if (cu_q_host[0] != 0 || cu_k_host[0] != 0) return fail(KVEC_ERR_INVALID_ARG, "cu_q[0] and cu_k[0] must be 0");
-    int max_q = 0;
+    if (!cu_q || !cu_k) return fail(KVEC_ERR_INVALID_ARG, "cu_seqlens pointers must not be NULL");
+    if (cu_q[0] != 0 || cu_k[0] != 0) return fail(KVEC_ERR_INVALID_ARG, "cu_q[0] and cu_k[0] must be 0");
+    *max_q = *max_k = 0;
     for (int b = 0; b < batch; ++b) {
-        const long long lq = (long long)cu_q_host[b + 1] - cu_q_host[b], lk = (long long)cu_k_host[b + 1] - cu_k_host[b];
+        const long long lq = (long long)cu_q[b + 1] - cu_q[b], lk = (long long)cu_k[b + 1] - cu_k[b];
         if (lq < 0 || lk < 0 || lq > kPagedMaxLen || lk > kPagedMaxLen)
             return fail(KVEC_ERR_INVALID_ARG, "sequence %d has %lld queries and %lld keys, outside [0, %d]", b, lq, lk, kPagedMaxLen);
-        max_q = std::max(max_q, (int)lq);
+        *max_q = std::max(*max_q, (int)lq);
+        *max_k = std::max(*max_k, (int)lk);
     }
+    return KVEC_OK;
+}
+
+}  // namespace
+
+size_t kvec_prefill_bytes(kvec_handle* h, int batch, const int32_t* cu_q_host, const int32_t* cu_k_host, int window, int sinks) {
+    int max_q = 0, max_k = 0;
+    if (check_prefill(batch, cu_q_host, cu_k_host, window, sinks, &max_q, &max_k) != KVEC_OK || !h || h->g > 8) return 0;
+    return plan_prefill(batch, h->p.num_q_heads, h->p.num_kv_heads, max_q, max_k, window, sinks, h->num_sms).scratch;
+}
+
+kvec_status kvec_prefill_attention(kvec_handle* h, int dtype, int batch, const int32_t* cu_q_host,
+                                   const int32_t* cu_q_dev, const int32_t* cu_k_host, const int32_t* cu_k_dev,
+                                   const void* q, const void* k, const void* v, int window, int sinks, void* out,
+                                   float* lse, void* scratch, size_t scratch_bytes, kvec_stream_t stream) {
+    if (dtype != KVEC_BF16 && dtype != KVEC_FP16)
+        return fail(KVEC_ERR_INVALID_ARG, "dtype %d is neither KVEC_BF16 nor KVEC_FP16", dtype);
+    int max_q = 0, max_k = 0;
+    kvec_status s = check_prefill(batch, cu_q_host, cu_k_host, window, sinks, &max_q, &max_k);
+    if (s != KVEC_OK) return s;
+    if (!cu_q_dev || !cu_k_dev) return fail(KVEC_ERR_INVALID_ARG, "cu_seqlens pointers must not be NULL");
     s = check_paged_handle(h, batch, nullptr);
     if (s != KVEC_OK) return s;
     if (h->g > 8)
         return fail(KVEC_ERR_UNSUPPORTED, "prefill attention supports up to 8 query heads per KV head (g = %d)", h->g);
     if (max_q == 0) return KVEC_OK;
     const int total_k = cu_k_host[batch];
-    if (!q || !out || (total_k > 0 && (!k || !v))) return fail(KVEC_ERR_INVALID_ARG, "a device pointer is NULL");
-    if (!aligned16(q) || !aligned16(k) || !aligned16(v) || !aligned16(out))
-        return fail(KVEC_ERR_INVALID_ARG, "q, k, v and out must be 16-byte aligned");
+    const PrefillPlan plan = plan_prefill(batch, h->p.num_q_heads, h->p.num_kv_heads, max_q, max_k, window, sinks, h->num_sms);
+    if (!q || !out || (total_k > 0 && (!k || !v)) || (plan.scratch && !scratch))
+        return fail(KVEC_ERR_INVALID_ARG, "a device pointer is NULL");
+    if (scratch_bytes < plan.scratch)
+        return fail(KVEC_ERR_INVALID_ARG, "scratch of %zu bytes, %zu are needed", scratch_bytes, plan.scratch);
+    if (!aligned16(q) || !aligned16(k) || !aligned16(v) || reinterpret_cast<uintptr_t>(out) % 32 ||
+        reinterpret_cast<uintptr_t>(scratch) % 32)
+        return fail(KVEC_ERR_INVALID_ARG, "q, k and v must be 16-byte aligned, out and scratch 32-byte aligned");
     if (reinterpret_cast<uintptr_t>(lse) % 4 || reinterpret_cast<uintptr_t>(cu_q_dev) % 4 || reinterpret_cast<uintptr_t>(cu_k_dev) % 4)
         return fail(KVEC_ERR_INVALID_ARG, "lse and the device cu_seqlens must be 4-byte aligned");
     PrefillIO io{};
@@ -1424,7 +1448,7 @@ kvec_status kvec_prefill_attention(kvec_handle* h, int dtype, int batch, const i
     io.Hkv = h->p.num_kv_heads;
     io.total_q = cu_q_host[batch];
     io.total_k = total_k;
-    io.max_q = max_q;
+    io.scratch = scratch;
     io.window = window;
     io.sinks = sinks;
     io.scale = softmax_scale_of(h->p);
@@ -1432,7 +1456,7 @@ kvec_status kvec_prefill_attention(kvec_handle* h, int dtype, int batch, const i
     s = set_device(h, &prev);
     if (s != KVEC_OK) return s;
     DeviceGuard guard{prev, h->device};
-    cudaError_t e = launch_prefill(io, h->num_sms, reinterpret_cast<cudaStream_t>(stream));
+    cudaError_t e = launch_prefill(io, plan, h->num_sms, reinterpret_cast<cudaStream_t>(stream));
     if (e != cudaSuccess) return cuda_fail(e, "prefill attention launch");
     return KVEC_OK;
 }

@@ -169,9 +169,19 @@ struct PrefillIO {
     int* err;
     int dtype, batch, Hq, Hkv;
     int total_q, total_k;
-    int max_q;                // the longest sequence's queries
+    void* scratch;            // PrefillPlan::scratch bytes
     int window, sinks;
     float scale;
+};
+
+// How a prefill call is divided (from the host's lengths).
+struct PrefillPlan {
+    int batch, Hkv;
+    int nq;                   // queries of a 128-row tile
+    int pairs;                // tile pairs of the longest sequence
+    int max_blocks;           // most 128-key blocks that a pair sees
+    int parts;                // that a pair's blocks are divided into
+    size_t scratch;           // bytes, 0 for one part
 };
 
 // ---------------------------------------------------------------- helpers
@@ -300,7 +310,8 @@ cudaError_t launch_rotate(const RotateIO& io, const PagedCacheView& c, cudaStrea
 cudaError_t launch_paged_decode(const PagedDecodeIO& io, const PagedCacheView& c, int num_sms, cudaStream_t st);
 size_t paged_decode_scratch(int batch, int Hq, int Hkv, int max_len, bool weights, int num_sms);
 cudaError_t launch_evict(const EvictIO& io, const PagedCacheView& c, cudaStream_t st);
-cudaError_t launch_prefill(const PrefillIO& io, int num_sms, cudaStream_t st);
+PrefillPlan plan_prefill(int batch, int Hq, int Hkv, int max_q, int max_k, int window, int sinks, int num_sms);
+cudaError_t launch_prefill(const PrefillIO& io, const PrefillPlan& plan, int num_sms, cudaStream_t st);
 // out_idx from the slot's kept-position bits, then the K/V rows.
 cudaError_t launch_gather(const Geometry& g, const Group& gr, cudaStream_t st, int priority, bool programmatic);
 

@@ -37,19 +37,31 @@ constexpr int kPfStages = 5;
 constexpr int kPfThreads = 384;
 constexpr uint32_t kPfTmem = 512;                   // S0 | S1 | O0 | O1, 128 columns each
 // Registers of a thread: at launch (the most that 384 threads may have), and after the split.
-constexpr int kPfRegs = 168, kPfSoftmaxRegs = 208, kPfOtherRegs = 88;
+constexpr int kPfRegs = 168, kPfSoftmaxRegs = 200, kPfOtherRegs = 104;
 static_assert(256 * kPfSoftmaxRegs + 128 * kPfOtherRegs <= kPfThreads * kPfRegs, "the split fits what the block was launched with");
 // The largest sum of a row's 64 weights: below it, no maximum of them is formed.  fp16 holds them.
 constexpr float kMostWeight = 16384.f;
 // The maximum before the first visible logit, finite: 2^(-inf - it) is 0.
 constexpr float kNoLogit = -3.402823466e38f;
 
+// Division of 0 <= x < 2^30 by a d below 2^21 that the host knows: x ceil(2^52 / d) / 2^52 is
+// off by less than x d / 2^52 / d < 1 / d.
+struct Divisor {
+    unsigned long long m;
+    __host__ void set(int d) { m = ((1ull << 52) + d - 1) / d; }
+    __device__ __forceinline__ int divide(int x) const { return (int)__umul64hi((unsigned long long)x << 12, m); }
+};
+
 struct PfArgs {
     CUtensorMap qmap, kmap, vmap;
     PrefillIO io;
     int g, nq;       // query heads of a KV head, queries of a tile
     int pairs;       // tile pairs of the longest sequence
-    int items;       // pairs * batch * Hkv
+    int parts;       // of a pair's blocks, each an item (1: none are split)
+    int items;       // pairs * batch * Hkv * parts
+    float* part_o;   // [items][2][128][128] a part's sums P V, by row
+    float2* part_ml; // [items][2][128] (m, l) of the rows
+    Divisor by_per, by_heads;   // batch * Hkv, Hkv
     float sl2;
 };
 
@@ -71,23 +83,31 @@ struct Item {
     int a, b;                     // the pair's queries [a, b) of the sequence
     int tiles;                    // 1 or 2
     int off;                      // position of query 0
-    int nsink, lo, n;             // blocks 0 .. nsink - 1, then from lo on: n in all
+    int nsink, lo;                // the blocks seen: 0 .. nsink - 1, then from lo on
+    int i0, n;                    // of them this item's part: the n from the i0-th on
     int whole_lo, whole_hi;       // keys [whole_lo, whole_hi] (and below `sinks`) are seen by every row
-    __device__ __forceinline__ int block(int i) const { return i < nsink ? i : lo + i - nsink; }
+    __device__ __forceinline__ int block(int i) const { return i0 + i < nsink ? i0 + i : lo + i0 + i - nsink; }
     __device__ __forceinline__ bool edge(int i, int sinks) const {
         const int t0 = block(i) * kPfTile, t1 = t0 + kPfTile - 1;
         return t1 > whole_hi || (t0 < whole_lo && t1 >= sinks);
     }
 };
 
+template <bool PARTS>
 __device__ __forceinline__ bool find_item(const PfArgs& A, int x, Item& w) {
     // The last tiles, which see the most keys, first; a pair's KV heads side by side.
     const PrefillIO& io = A.io;
     if (x >= A.items) return false;
+    int part = 0;
+    if constexpr (PARTS) {
+        part = x % A.parts;
+        x /= A.parts;
+    }
     const int per = io.batch * io.Hkv;
-    const int p = A.pairs - 1 - x / per;
-    x %= per;
-    w.s = x / io.Hkv;
+    const int top = A.by_per.divide(x);
+    const int p = A.pairs - 1 - top;
+    x -= top * per;
+    w.s = A.by_heads.divide(x);
     w.h = x - w.s * io.Hkv;
     auto clamped = [](int v, int most) { return min(max(v, 0), most); };
     w.q0 = clamped(__ldg(&io.cu_q[w.s]), io.total_q);
@@ -100,15 +120,35 @@ __device__ __forceinline__ bool find_item(const PfArgs& A, int x, Item& w) {
     w.tiles = w.b - w.a > A.nq ? 2 : 1;
     w.off = w.Lk - w.Lq;
     const int pa = w.off + w.a, pb = w.off + w.b - 1;    // first and last position
-    w.nsink = w.lo = w.n = 0;
+    w.nsink = w.lo = w.i0 = w.n = 0;
     if (pb >= 0) {
         w.lo = io.window ? max(pa - io.window + 1, 0) / kPfTile : 0;
         w.nsink = min((min(io.sinks, w.Lk) + kPfTile - 1) / kPfTile, w.lo);
         w.n = w.nsink + pb / kPfTile + 1 - w.lo;
+        if constexpr (PARTS) {
+            const int all = w.n;
+            w.i0 = all * part / A.parts;
+            w.n = all * (part + 1) / A.parts - w.i0;
+        }
     }
     w.whole_hi = pa;
     w.whole_lo = io.window ? pb - io.window + 1 : 0;
     return true;
+}
+
+// ptx::warp_wait; a phase that is over, the usual case, costs one poll and one vote.
+__device__ __forceinline__ bool pf_wait(uint64_t* bar, uint32_t parity, const volatile int* abort) {
+    return __all_sync(0xffffffffu, ptx::mbar_try_wait(bar, parity)) || ptx::warp_wait(bar, parity, abort);
+}
+
+// The n lowest bits, n clamped to [0, 32].
+__device__ __forceinline__ uint32_t low_bits(int n) { return n <= 0 ? 0u : n >= 32 ? 0xffffffffu : (1u << n) - 1u; }
+
+// 32 bytes to a 32-byte aligned place.
+__device__ __forceinline__ void st_global_v8(void* p, const uint32_t* r) {
+    asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};\n" ::"l"(p), "r"(r[0]), "r"(r[1]), "r"(r[2]),
+                 "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7])
+                 : "memory");
 }
 
 __device__ __forceinline__ float max3(float a, float b, float c) {
@@ -180,7 +220,8 @@ __device__ __forceinline__ int item_of(int turn) {
 // Persistent: of every gridDim.x items a CTA takes one, in turns from the front and from the
 // back (items cost less and less, so that the shares are even), and no role waits for an item's end: the next one's K and V follow through the ring, its first S is formed
 // behind the last products of this one, while the softmax warps write their outputs.
-template <class T>
+// PARTS: a pair's blocks are divided into several items, which leave sums for prefill_join_kernel.
+template <class T, bool PARTS>
 __global__ void __launch_bounds__(kPfThreads, 1) prefill_kernel(const __grid_constant__ PfArgs A) {
     extern __shared__ uint8_t pf_smem_raw[];
     // 1024-byte alignment for the swizzled operand tiles.
@@ -241,10 +282,10 @@ __global__ void __launch_bounds__(kPfThreads, 1) prefill_kernel(const __grid_con
             int qloads = 0;
             for (int turn = 0; turn < turns && !stop; ++turn) {
                 Item w{};
-                if (!find_item(A, item_of(turn), w) || w.n == 0) continue;
+                if (!find_item<PARTS>(A, item_of(turn), w) || w.n == 0) continue;
                 auto load_kv = [&](int y) {   // load y of the item: K and V blocks alternate
                     const int st = x % kPfStages, round = x / kPfStages;
-                    if (round > 0 && !ptx::warp_wait(&bars->empty[st], (round - 1) & 1, abort)) {
+                    if (round > 0 && !pf_wait(&bars->empty[st], (round - 1) & 1, abort)) {
                         stop = true;
                         return;
                     }
@@ -261,7 +302,7 @@ __global__ void __launch_bounds__(kPfThreads, 1) prefill_kernel(const __grid_con
                 };
                 load_kv(0);
                 // The queries' buffers are free once the item before has formed its last S.
-                if (!stop && qloads > 0 && !ptx::warp_wait(&bars->q_empty, (qloads - 1) & 1, abort)) stop = true;
+                if (!stop && qloads > 0 && !pf_wait(&bars->q_empty, (qloads - 1) & 1, abort)) stop = true;
                 if (stop) break;
                 if (ptx::elect_one()) {
                     const uint32_t bytes = (uint32_t)(A.nq * A.g) * 128u;
@@ -287,7 +328,7 @@ __global__ void __launch_bounds__(kPfThreads, 1) prefill_kernel(const __grid_con
             const uint64_t kdesc = ptx::smem_desc_k_sw128(ptx::smem_u32(ring));
             const uint64_t vdesc = smem_desc_mn_sw128(ptx::smem_u32(ring));
             auto wait = [&](uint64_t* bar, int phase) {
-                if (!stop && !ptx::warp_wait(bar, phase & 1, abort)) stop = true;
+                if (!stop && !pf_wait(bar, phase & 1, abort)) stop = true;
                 return !stop;
             };
             // Stages as values that the compiler knows to be the warp's, so that descriptors stay in uniform registers.
@@ -326,7 +367,7 @@ __global__ void __launch_bounds__(kPfThreads, 1) prefill_kernel(const __grid_con
             int turn = 0;
             auto next_item = [&]() {
                 while (turn < turns)
-                    if (find_item(A, item_of(turn++), w) && w.n > 0) return true;
+                    if (find_item<PARTS>(A, item_of(turn++), w) && w.n > 0) return true;
                 return false;
             };
             bool more = next_item();
@@ -390,10 +431,10 @@ __global__ void __launch_bounds__(kPfThreads, 1) prefill_kernel(const __grid_con
             // Every load is passed in turn: a parity says nothing of a stage several rounds ahead.
             for (int turn = 0; turn < turns && !stop; ++turn) {
                 Item w{};
-                if (!find_item(A, item_of(turn), w)) continue;
+                if (!find_item<PARTS>(A, item_of(turn), w)) continue;
                 for (int y = 0; y < 2 * w.n; ++y, ++x) {
                     const int st = x % kPfStages;
-                    if (!ptx::warp_wait(&bars->full[st], (x / kPfStages) & 1, abort)) {
+                    if (!pf_wait(&bars->full[st], (x / kPfStages) & 1, abort)) {
                         stop = true;
                         break;
                     }
@@ -431,10 +472,27 @@ __global__ void __launch_bounds__(kPfThreads, 1) prefill_kernel(const __grid_con
         const uint32_t tS = tmem + lanes + t * 128, tO = tmem + lanes + 256 + t * 128;
         const float sl2f = A.sl2;
         const uint64_t sl2 = ptx::pack_f32x2(sl2f, sl2f);
+        // The infinities and NaN that a row sees in the blocks of partial sight: their weights
+        // are positive, so each makes its output infinite or NaN.
+        auto add_unbounded = [&](int p, int below, const Item& w, int n, auto add) {
+#pragma unroll 1
+            for (int i = 0; i < n; ++i) {
+                if (!w.edge(i, sinks)) continue;
+#pragma unroll 1
+                for (int c = 0; c < kPfTile; ++c) {
+                    const int key = w.block(i) * kPfTile + c;
+                    if (key > p || (key <= below && key >= sinks)) continue;
+                    const uint16_t* v = A.io.v + ((size_t)(w.k0 + key) * A.io.Hkv + w.h) * kHeadDim;
+#pragma unroll 1
+                    for (int d = 0; d < kHeadDim; ++d)
+                        if (unbounded_mask<T>(v[d])) add(d, Half16<T>::unpack(v[d]).x);
+                }
+            }
+        };
         int blocks = 0;   // of this tile: the phase of its barriers
         for (int turn = 0; turn < turns && !stop; ++turn) {
             Item w{};
-            if (!find_item(A, item_of(turn), w) || t >= w.tiles) continue;
+            if (!find_item<PARTS>(A, item_of(turn), w) || t >= w.tiles) continue;
             const int query = w.a + t * A.nq + row_q;
             const bool live = row < A.nq * A.g && query < w.b;        // the row is a real one
             const int p = w.off + query;
@@ -442,7 +500,7 @@ __global__ void __launch_bounds__(kPfThreads, 1) prefill_kernel(const __grid_con
             const int n = w.n;
             float m = kNoLogit, l = 0.f;
             for (int i = 0; i < n; ++i, ++blocks) {
-                if (!ptx::warp_wait(&bars->s_full[t], blocks & 1, abort)) {
+                if (!pf_wait(&bars->s_full[t], blocks & 1, abort)) {
                     stop = true;
                     break;
                 }
@@ -452,11 +510,15 @@ __global__ void __launch_bounds__(kPfThreads, 1) prefill_kernel(const __grid_con
                 for (int c = 0; c < 4; ++c) ptx::tmem_ld32(tS + c * 32, s + c * 32);
                 ptx::tmem_wait_ld();
                 if (w.edge(i, sinks)) {
+                    // Bit c of the words: the row sees key t0 + c.  (Comparisons for each column
+                    // became branches, 12,000 cycles a block.)
                     const int t0 = w.block(i) * kPfTile;
 #pragma unroll
-                    for (int c = 0; c < 128; ++c) {
-                        const int key = t0 + c;
-                        if (key > p || (key <= below && key >= sinks)) s[c] = -INFINITY;
+                    for (int g = 0; g < 4; ++g) {
+                        const int b0 = t0 + 32 * g;
+                        const uint32_t seen = low_bits(p + 1 - b0) & (~low_bits(below + 1 - b0) | low_bits(sinks - b0));
+#pragma unroll
+                        for (int c = 0; c < 32; ++c) s[32 * g + c] = (seen >> c) & 1u ? s[32 * g + c] : -INFINITY;
                     }
                 }
                 // The weights of 64 keys relative to m, as pairs of 16-bit values, and their sum.
@@ -488,8 +550,8 @@ __global__ void __launch_bounds__(kPfThreads, 1) prefill_kernel(const __grid_con
                         m = mx;
                         if (i > 0 || c > 0) {
                             // The outputs so far with it, once their products are done.
-                            if (!(c > 0 ? ptx::warp_wait(&bars->o_half[t], blocks & 1, abort)
-                                        : ptx::warp_wait(&bars->o_done[t], (blocks - 1) & 1, abort))) {
+                            if (!(c > 0 ? pf_wait(&bars->o_half[t], blocks & 1, abort)
+                                        : pf_wait(&bars->o_done[t], (blocks - 1) & 1, abort))) {
                                 stop = true;
                                 break;
                             }
@@ -515,12 +577,34 @@ __global__ void __launch_bounds__(kPfThreads, 1) prefill_kernel(const __grid_con
                 }
                 if (stop) break;
             }
-            if (n > 0 && !stop && !ptx::warp_wait(&bars->o_done[t], (blocks - 1) & 1, abort)) stop = true;
+            if (n > 0 && !stop && !pf_wait(&bars->o_done[t], (blocks - 1) & 1, abort)) stop = true;
             if (stop) break;
             ptx::tc_fence_after();
             const bool some = l > 0.f || l != l;
             const float inv = some ? 1.f / l : 0.f;
             const size_t at = (size_t)(w.q0 + query) * A.io.Hq + w.h * A.g + j;
+            if constexpr (PARTS) {
+                // Sums and maximum as they are, for prefill_join_kernel.
+                const size_t prow = ((size_t)item_of(turn) * 2 + t) * kPfTile + row;
+                float* dst = A.part_o + prow * kHeadDim;
+#pragma unroll 1
+                for (int c = 0; c < 4 && n > 0; ++c) {
+                    float o[32];
+                    ptx::tmem_ld32(tO + c * 32, o);
+                    ptx::tmem_wait_ld();
+                    if (live) {
+#pragma unroll
+                        for (int d = 0; d < 32; d += 8) st_global_v8(dst + c * 32 + d, reinterpret_cast<const uint32_t*>(o) + d);
+                    }
+                }
+                ptx::tc_fence_before();
+                if (live) {
+                    A.part_ml[prow] = make_float2(n > 0 ? m : kNoLogit, l);
+                    if (n > 0 && bars->unbounded) add_unbounded(p, below, w, n, [&](int d, float v) { dst[d] += v; });
+                }
+                __syncwarp();
+                continue;
+            }
 #pragma unroll
             for (int c = 0; c < 4; ++c) {
                 float o[32];
@@ -534,30 +618,19 @@ __global__ void __launch_bounds__(kPfThreads, 1) prefill_kernel(const __grid_con
 #pragma unroll
                 for (int d = 0; d < 32; ++d) o[d] = some ? o[d] * inv : 0.f;
                 if (live) {
-                    uint4* dst = reinterpret_cast<uint4*>(A.io.out + at * kHeadDim + c * 32);
+                    uint32_t u[16];
 #pragma unroll
-                    for (int d = 0; d < 4; ++d)
-                        dst[d] = make_uint4(Half16<T>::pack(o[8 * d], o[8 * d + 1]), Half16<T>::pack(o[8 * d + 2], o[8 * d + 3]),
-                                            Half16<T>::pack(o[8 * d + 4], o[8 * d + 5]), Half16<T>::pack(o[8 * d + 6], o[8 * d + 7]));
+                    for (int d = 0; d < 16; ++d) u[d] = Half16<T>::pack(o[2 * d], o[2 * d + 1]);
+                    st_global_v8(A.io.out + at * kHeadDim + c * 32, u);
+                    st_global_v8(A.io.out + at * kHeadDim + c * 32 + 16, u + 8);
                 }
             }
             ptx::tc_fence_before();   // O has been read before the next item's weights are handed over
             if (live && n > 0 && bars->unbounded) {
-                // The infinities and NaN that the row sees in the blocks of partial sight: their
-                // weights are positive, so each makes its output infinite or NaN.
                 uint16_t* dst = A.io.out + at * kHeadDim;
-                for (int i = 0; i < n; ++i) {
-                    if (!w.edge(i, sinks)) continue;
-                    for (int c = 0; c < kPfTile; ++c) {
-                        const int key = w.block(i) * kPfTile + c;
-                        if (key > p || (key <= below && key >= sinks)) continue;
-                        const uint16_t* v = A.io.v + ((size_t)(w.k0 + key) * A.io.Hkv + w.h) * kHeadDim;
-#pragma unroll 1
-                        for (int d = 0; d < kHeadDim; ++d)
-                            if (unbounded_mask<T>(v[d]))
-                                dst[d] = (uint16_t)Half16<T>::pack(Half16<T>::unpack(dst[d]).x + Half16<T>::unpack(v[d]).x, 0.f);
-                    }
-                }
+                add_unbounded(p, below, w, n, [&](int d, float v) {
+                    dst[d] = (uint16_t)Half16<T>::pack(Half16<T>::unpack(dst[d]).x + v, 0.f);
+                });
             }
             if (live && A.io.lse) A.io.lse[at] = some ? fmaf(m, 0.6931471805599453f, logf(l)) : -INFINITY;
             __syncwarp();
@@ -568,29 +641,100 @@ __global__ void __launch_bounds__(kPfThreads, 1) prefill_kernel(const __grid_con
     if (warp == 9) ptx::tmem_dealloc(tmem, kPfTmem);
 }
 
+// Rows whose blocks several items share: one warp a row, four dimensions a lane.
+constexpr int kPjWarps = 8;
+template <class T>
+__global__ void __launch_bounds__(32 * kPjWarps) prefill_join_kernel(const __grid_constant__ PfArgs A) {
+    asm volatile("griddepcontrol.launch_dependents;\n" ::: "memory");
+    asm volatile("griddepcontrol.wait;\n" ::: "memory");
+    const int lane = threadIdx.x & 31, r = blockIdx.y * kPjWarps + (threadIdx.x >> 5);   // row of the pair
+    const int first = blockIdx.x * A.parts, t = r / kPfTile, row = r % kPfTile;
+    Item w{};
+    const int query = row / A.g + t * A.nq;
+    const bool live = find_item<true>(A, first, w) && row < A.nq * A.g && w.a + query < w.b;
+    if (!live) return;
+    auto prow = [&](int i) { return ((size_t)(first + i) * 2 + t) * kPfTile + row; };
+    float M = kNoLogit, L = 0.f;
+    float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+    for (int i = 0; i < A.parts; ++i) M = fmaxf(M, A.part_ml[prow(i)].x);
+    for (int i = 0; i < A.parts; ++i) {
+        const float2 ml = A.part_ml[prow(i)];
+        if (ml.x == kNoLogit && ml.y == 0.f) continue;   // a part that sees nothing wrote no sums
+        const float f = ptx::ex2(ml.x - M);
+        const float4 v = reinterpret_cast<const float4*>(A.part_o + prow(i) * kHeadDim)[lane];
+        L = fmaf(f, ml.y, L);
+        o = make_float4(fmaf(f, v.x, o.x), fmaf(f, v.y, o.y), fmaf(f, v.z, o.z), fmaf(f, v.w, o.w));
+    }
+    const bool some = L > 0.f || L != L;
+    const float inv = some ? 1.f / L : 0.f;
+    const size_t at = (size_t)(w.q0 + w.a + query) * A.io.Hq + w.h * A.g + row % A.g;
+    reinterpret_cast<uint2*>(A.io.out + at * kHeadDim)[lane] =
+        some ? make_uint2(Half16<T>::pack(o.x * inv, o.y * inv), Half16<T>::pack(o.z * inv, o.w * inv)) : make_uint2(0u, 0u);
+    if (lane == 0 && A.io.lse) A.io.lse[at] = some ? fmaf(M, 0.6931471805599453f, logf(L)) : -INFINITY;
+}
+
 template <class T>
 cudaError_t launch_typed(const PfArgs& a, int num_sms, cudaStream_t st) {
-    return launch_prio(prefill_kernel<T>, dim3((unsigned)std::min(a.items, num_sms)), dim3(kPfThreads), kPfSmem, st, 0, true, a);
+    const dim3 grid((unsigned)std::min(a.items, num_sms));
+    if (a.parts == 1) return launch_prio(prefill_kernel<T, false>, grid, dim3(kPfThreads), kPfSmem, st, 0, true, a);
+    cudaError_t e = launch_prio(prefill_kernel<T, true>, grid, dim3(kPfThreads), kPfSmem, st, 0, true, a);
+    if (e != cudaSuccess) return e;
+    return launch_prio(prefill_join_kernel<T>, dim3((unsigned)(a.items / a.parts), 2 * kPfTile / kPjWarps), dim3(32 * kPjWarps),
+                       0, st, 0, true, a);
+}
+
+// Pairs of tiles over all sequences, and the parts that each pair's blocks are divided into: as
+// many as SMs would be idle otherwise, of two blocks and more.
+int split_parts(const PrefillPlan& p, int num_sms) {
+    const long long whole = (long long)p.pairs * p.batch * p.Hkv;
+    return (int)std::max<long long>(1, std::min<long long>(num_sms / std::max<long long>(whole, 1), p.max_blocks / 2));
 }
 
 }  // namespace
 
 cudaError_t configure_prefill() {
-    cudaError_t e = cudaFuncSetAttribute(prefill_kernel<__nv_bfloat16>, cudaFuncAttributeMaxDynamicSharedMemorySize, kPfSmem);
-    if (e == cudaSuccess)
-        e = cudaFuncSetAttribute(prefill_kernel<__half>, cudaFuncAttributeMaxDynamicSharedMemorySize, kPfSmem);
+    cudaError_t e = cudaSuccess;
+    auto one = [&](auto kernel) {
+        if (e == cudaSuccess) e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kPfSmem);
+    };
+    one(prefill_kernel<__nv_bfloat16, false>);
+    one(prefill_kernel<__nv_bfloat16, true>);
+    one(prefill_kernel<__half, false>);
+    one(prefill_kernel<__half, true>);
     return e;
 }
 
-cudaError_t launch_prefill(const PrefillIO& io, int num_sms, cudaStream_t st) {
+PrefillPlan plan_prefill(int batch, int Hq, int Hkv, int max_q, int max_k, int window, int sinks, int num_sms) {
+    PrefillPlan p{};
+    p.batch = batch;
+    p.Hkv = Hkv;
+    p.nq = kPfTile / (Hq / Hkv);
+    p.pairs = (max_q + 2 * p.nq - 1) / (2 * p.nq);
+    long long blocks = (max_k + kPfTile - 1) / kPfTile;
+    // A window's blocks, and those of the first tokens.
+    if (window)
+        blocks = std::min(blocks, ((long long)window + 2 * p.nq) / kPfTile + 2 + ((long long)std::min(sinks, max_k) + kPfTile - 1) / kPfTile);
+    p.max_blocks = (int)blocks;
+    p.parts = split_parts(p, num_sms);
+    const size_t items = (size_t)p.pairs * batch * Hkv * p.parts;
+    p.scratch = p.parts > 1 ? items * 2 * kPfTile * (kHeadDim * sizeof(float) + sizeof(float2)) : 0;
+    return p;
+}
+
+cudaError_t launch_prefill(const PrefillIO& io, const PrefillPlan& plan, int num_sms, cudaStream_t st) {
     PfArgs a{};
     a.io = io;
     a.g = io.Hq / io.Hkv;
-    a.nq = kPfTile / a.g;
-    a.pairs = (io.max_q + 2 * a.nq - 1) / (2 * a.nq);
-    const long long items = (long long)a.pairs * io.batch * io.Hkv;
+    a.nq = plan.nq;
+    a.pairs = plan.pairs;
+    a.parts = plan.parts;
+    const long long items = (long long)a.pairs * io.batch * io.Hkv * a.parts;
     if (items > 0x3fffffffll) return cudaErrorInvalidConfiguration;
     a.items = (int)items;
+    a.part_o = static_cast<float*>(io.scratch);
+    a.part_ml = reinterpret_cast<float2*>(a.part_o + (size_t)items * 2 * kPfTile * kHeadDim);
+    a.by_per.set(io.batch * io.Hkv);
+    a.by_heads.set(io.Hkv);
     a.sl2 = io.scale * 1.4426950408889634f;
     const uint64_t row = (uint64_t)kHeadDim * 2;
     const uint64_t qd[3] = {(uint64_t)kHeadDim, (uint64_t)io.Hq, (uint64_t)io.total_q}, qs[2] = {row, row * io.Hq};

@@ -31,7 +31,7 @@ EXPORTED = ("kvec_create", "kvec_destroy", "kvec_state_bytes", "kvec_reset", "kv
             "kvec_select_layer_lse", "kvec_select_layers_lse", "kvec_decode_attention",
             "kvec_noalloc_sync_status", "kvec_set_test_fault", "kvec_output_capacity",
             "kvec_rotate_append", "kvec_paged_decode_bytes", "kvec_paged_decode", "kvec_paged_evict",
-            "kvec_prefill_attention")
+            "kvec_prefill_bytes", "kvec_prefill_attention")
 
 KVEC_BF16 = 0
 KVEC_FP16 = 1
@@ -131,7 +131,9 @@ def load() -> ctypes.CDLL:
             "kvec_paged_decode_bytes": ([_vp, i, i, i], ctypes.c_size_t),
             "kvec_paged_decode": ([_vp, i, _vp, ctypes.POINTER(kvec_paged_cache), i, i, i, _vp, _vp, ctypes.c_size_t,
                                    _vp], st),
-            "kvec_prefill_attention": ([_vp, i, i, _vp, _vp, _vp, _vp, _vp, _vp, _vp, i, i, _vp, _vp, _vp], st),
+            "kvec_prefill_bytes": ([_vp, i, _vp, _vp, i, i], ctypes.c_size_t),
+            "kvec_prefill_attention": ([_vp, i, i, _vp, _vp, _vp, _vp, _vp, _vp, _vp, i, i, _vp, _vp, _vp,
+                                        ctypes.c_size_t, _vp], st),
             "kvec_paged_evict": ([_vp, i, ctypes.POINTER(kvec_paged_cache), _vp, i, i, i, i, i, _vp, _vp, _vp], st),
         }
         for name, (args, res) in sig.items():
@@ -257,9 +259,14 @@ def kvec_paged_evict(handle: int, batch: int, cache: kvec_paged_cache, new_table
 
 def kvec_prefill_attention(handle: int, dtype: int, batch: int, cu_q_host: int, cu_q_dev: int, cu_k_host: int,
                            cu_k_dev: int, q: int, k: int, v: int, window: int, sinks: int, out: int,
-                           lse: Optional[int] = None, stream: int = 0) -> None:
+                           lse: Optional[int] = None, scratch: Optional[int] = None, scratch_bytes: int = 0,
+                           stream: int = 0) -> None:
     _check(load().kvec_prefill_attention(handle, dtype, batch, cu_q_host, cu_q_dev, cu_k_host, cu_k_dev, q, k, v,
-                                         window, sinks, out, lse, stream))
+                                         window, sinks, out, lse, scratch, scratch_bytes, stream))
+
+
+def kvec_prefill_bytes(handle: int, batch: int, cu_q_host: int, cu_k_host: int, window: int = 0, sinks: int = 0) -> int:
+    return int(load().kvec_prefill_bytes(handle, batch, cu_q_host, cu_k_host, window, sinks))
 
 
 def kvec_debug_scores(handle: int) -> kvec_debug_view:
@@ -603,9 +610,12 @@ class KvecSelector:
         stream = self._stream(stream, dev)
         out = self._empty(q.shape, dtype, stream) if out is None else out
         lse = self._empty(q.shape[:2], t.float32, stream) if lse is None else lse
+        need = kvec_prefill_bytes(self.handle, batch, cu_q_host.data_ptr(), cu_k_host.data_ptr(), window, sinks)
+        scratch = self._empty(need, t.uint8, stream) if need else None
         kvec_prefill_attention(self.handle, code, batch, cu_q_host.data_ptr(), cu_q_dev.data_ptr(),
                                cu_k_host.data_ptr(), cu_k_dev.data_ptr(), q.data_ptr(), k.data_ptr(), v.data_ptr(),
-                               window, sinks, out.data_ptr(), lse.data_ptr(), stream.cuda_stream)
+                               window, sinks, out.data_ptr(), lse.data_ptr(),
+                               scratch.data_ptr() if need else None, need, stream.cuda_stream)
         return out, lse
 
     def debug(self, device="cuda"):

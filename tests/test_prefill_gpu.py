@@ -227,3 +227,23 @@ def test_captured_and_on_two_streams():
         gr.replay()
         torch.cuda.synchronize()
         assert torch.equal(out, w[0]) and torch.equal(lse, w[1])
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("Hq,Hkv,q_lens,k_lens,window,sinks", [
+    (28, 4, [1], [20000], 0, 0), (8, 1, [33, 2, 5], [5000, 300, 1], 0, 0), (32, 8, [64], [3001], 0, 0),
+    (4, 2, [100], [9000], 4096, 130), (8, 8, [7], [700], 0, 0), (16, 2, [20, 0], [1500, 800], 300, 4),
+])
+def test_few_rows_on_many_keys(dtype, Hq, Hkv, q_lens, k_lens, window, sinks):
+    # The keys of a row are divided over the device; parts of a short sequence see nothing.
+    sel = selector(Hq, Hkv)
+    cu_q, cu_k = cu_of(q_lens), cu_of(k_lens)
+    assert kvec.kvec_prefill_bytes(sel.handle, len(q_lens), cu_q.data_ptr(), cu_k.data_ptr(), window, sinks) > 0
+    q, k, v = tensors(q_lens, k_lens, Hq, Hkv, dtype, sum(k_lens), 2.0)
+    check(q, k, v, q_lens, k_lens, window, sinks)
+    # Logits that jump between the parts, and values without bounds in the blocks of partial sight.
+    k[:, :, 0] = torch.where(torch.arange(k.shape[0], device="cuda") % 1000 < 500, 20.0, -20.0)[:, None].to(dtype)
+    q[:, :, 0] = 5.0
+    check(q, k, v, q_lens, k_lens, window, sinks)
+    v[k_lens[0] - 1, 0, 3], v[k_lens[0] - min(k_lens[0], 2), 0, 77] = float("nan"), float("inf")
+    check(q, k, v, q_lens, k_lens, window, sinks)
