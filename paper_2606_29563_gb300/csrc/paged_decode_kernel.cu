@@ -106,34 +106,52 @@ struct Walker {
             }
         }
     }
-    // To block `at` of the whole list; `total` blocks are in it.
+    // To block `at` of the whole list, by a whole warp: a lane looks at a sequence.
     __device__ __forceinline__ void seek(const PdArgs& A, long long at) {
-        h = 0;
-        for (s = 0; s < A.io.batch; ++s) {
-            v.init(A, s);
-            const long long here = (long long)v.nb * A.io.Hkv;
-            if (at < here) {
-                h = (int)(at / v.nb);
-                i = (int)(at - (long long)h * v.nb);
+        const int lane = threadIdx.x & 31;
+        for (int s0 = 0; s0 < A.io.batch; s0 += 32) {
+            v.nb = 0;
+            if (s0 + lane < A.io.batch) v.init(A, s0 + lane);
+            const long long mine = (long long)v.nb * A.io.Hkv;
+            long long upto = mine;
+#pragma unroll
+            for (int o = 1; o < 32; o <<= 1) {
+                const long long y = __shfl_up_sync(0xffffffffu, upto, o);
+                if (lane >= o) upto += y;
+            }
+            const uint32_t past = __ballot_sync(0xffffffffu, at < upto);
+            if (past) {
+                const int l = __ffs(past) - 1;
+                at -= __shfl_sync(0xffffffffu, upto - mine, l);
+                s = s0 + l;
+                v.init(A, s);
+                h = (int)at / v.nb;      // at < nb * Hkv <= 2^21
+                i = (int)at - h * v.nb;
                 return;
             }
-            at -= here;
+            at -= __shfl_sync(0xffffffffu, upto, 31);
         }
-        i = 0;
+        s = A.io.batch;
+        h = i = 0;
+        v.nb = 0;
     }
 };
 
-// Blocks of the sequences before `upto`, over all KV heads: the whole warp.
-__device__ __forceinline__ long long blocks_before(const PdArgs& A, int upto) {
-    long long sum = 0;
-    for (int s = threadIdx.x & 31; s < upto; s += 32) {
+// Blocks of the sequences before `upto`, and of all, over all KV heads: the whole warp.
+__device__ __forceinline__ longlong2 blocks_before(const PdArgs& A, int upto) {
+    long long before = 0, all = 0;
+    for (int s = threadIdx.x & 31; s < A.io.batch; s += 32) {
         Visible v;
         v.init(A, s);
-        sum += v.nb;
+        all += v.nb;
+        if (s < upto) before += v.nb;
     }
 #pragma unroll
-    for (int o = 16; o; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
-    return sum * A.io.Hkv;
+    for (int o = 16; o; o >>= 1) {
+        all += __shfl_xor_sync(0xffffffffu, all, o);
+        before += __shfl_xor_sync(0xffffffffu, before, o);
+    }
+    return make_longlong2(before * A.io.Hkv, all * A.io.Hkv);
 }
 
 __device__ __forceinline__ long long share_start(long long total, int cta, int ctas) { return total * cta / ctas; }
@@ -207,7 +225,7 @@ __global__ void __launch_bounds__(kPdThreads, kPdCtasPerSm) paged_decode_kernel(
         cur.i = (int)((long long)cur.v.nb * rank / splits);
         count = (long long)cur.v.nb * (rank + 1) / splits - cur.i;
     } else {
-        const long long total = blocks_before(A, A.io.batch);
+        const long long total = blocks_before(A, 0).y;
         const long long at = share_start(total, blockIdx.x, A.ctas);
         count = share_start(total, blockIdx.x + 1, A.ctas) - at;
         cur.seek(A, at);
@@ -463,57 +481,89 @@ __global__ void __launch_bounds__(kPdThreads, kPdCtasPerSm) paged_decode_kernel(
 }
 
 // The pairs whose blocks several CTAs share.  Block x < g of (x, h, s): query head x; the
-// others add the weights, kJoinRows slots each.
+// others add the weights, kJoinRows slots each.  (A thread finds a share, so that the shares'
+// places, sums and outputs are each read at once: one thread in a loop over the 38 shares of
+// 131072 slots took 58 us.)
 template <class T>
 __global__ void __launch_bounds__(kHeadDim) paged_join_kernel(const __grid_constant__ PdArgs A) {
-    __shared__ float fm[kPdHeads], finv[kPdHeads];
+    extern __shared__ float2 share[];                 // (place as an int, factor) of the output block's shares
+    __shared__ float fm[kPdHeads], finv[kPdHeads], red[2][kHeadDim / 32];
     asm volatile("griddepcontrol.launch_dependents;\n" ::: "memory");
     asm volatile("griddepcontrol.wait;\n" ::: "memory");
-    const int h = blockIdx.y, s = blockIdx.z, tid = threadIdx.x, g = A.g;
+    const int h = blockIdx.y, s = blockIdx.z, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = A.g;
     Visible v;
     v.init(A, s);
     const int i0 = ((int)blockIdx.x - g) * (kJoinRows / kPdBlock);
     if ((int)blockIdx.x >= g && i0 >= v.nb) return;
-    const size_t out = ((size_t)s * A.io.Hq + (size_t)h * g) * kHeadDim + tid;
+    const size_t out = ((size_t)s * A.io.Hq + (size_t)h * g + blockIdx.x) * kHeadDim + tid;
     if (v.nb == 0) {
-        if ((int)blockIdx.x < g) reinterpret_cast<T*>(A.io.out)[out + (size_t)blockIdx.x * kHeadDim] = T(0.f);
+        if ((int)blockIdx.x < g) reinterpret_cast<T*>(A.io.out)[out] = T(0.f);
         return;
     }
-    const long long total = blocks_before(A, A.io.batch);
-    const long long p0 = blocks_before(A, s) + (long long)h * v.nb, p1 = p0 + v.nb;
+    const longlong2 list = blocks_before(A, s);
+    const long long total = list.y, p0 = list.x + (long long)h * v.nb, p1 = p0 + v.nb;
     const int c0 = (int)(((p0 + 1) * A.ctas - 1) / total), c1 = (int)((p1 * A.ctas - 1) / total);
     if (c0 == c1) return;   // finished by its CTA
-    // The share of CTA c: its first segment, unless the pair begins inside it.
-    auto slot_of = [&](int c) { return (size_t)c * 2 + (share_start(total, c, A.ctas) < p0 ? 1 : 0); };
-    auto empty = [&](int c) { return share_start(total, c, A.ctas) == share_start(total, c + 1, A.ctas); };
-    auto sums = [&](int j, float& M, float& L) {
-        M = kNoLogit;
-        L = 0.f;
-        for (int c = c0; c <= c1; ++c)
-            if (!empty(c)) M = fmaxf(M, A.part_ml[slot_of(c) * kPdHeads + j].x);
-        for (int c = c0; c <= c1; ++c) {
-            if (empty(c)) continue;
-            const float2 o = A.part_ml[slot_of(c) * kPdHeads + j];
-            L = fmaf(ptx::ex2(o.x - M), o.y, L);
-        }
+    // The place of CTA c's share, -1 if it has no blocks: its first segment's, unless the pair begins inside it.
+    auto place = [&](int c) {
+        const long long from = share_start(total, c, A.ctas);
+        return from == share_start(total, c + 1, A.ctas) ? -1 : c * 2 + (from < p0 ? 1 : 0);
     };
     if ((int)blockIdx.x < g) {
         const int j = blockIdx.x;
-        float M, L, O = 0.f;
-        sums(j, M, L);
-        for (int c = c0; c <= c1; ++c) {
-            if (empty(c)) continue;
-            const size_t slot = slot_of(c) * kPdHeads + j;
-            O = fmaf(ptx::ex2(A.part_ml[slot].x - M), A.part_o[slot * kHeadDim + tid], O);
+        float M = kNoLogit, L = 0.f;
+        for (int c = tid; c <= c1 - c0; c += kHeadDim) {
+            const int at = place(c0 + c);
+            const float2 ml = at < 0 ? make_float2(kNoLogit, 0.f) : A.part_ml[at * kPdHeads + j];
+            share[c] = make_float2(__int_as_float(at), ml.x);
+            M = fmaxf(M, ml.x);
         }
-        reinterpret_cast<T*>(A.io.out)[out + (size_t)j * kHeadDim] = T(L > 0.f || L != L ? O / L : 0.f);
+#pragma unroll
+        for (int o = 16; o; o >>= 1) M = fmaxf(M, __shfl_xor_sync(0xffffffffu, M, o));
+        if (lane == 0) red[0][warp] = M;
+        __syncthreads();
+        M = fmaxf(fmaxf(red[0][0], red[0][1]), fmaxf(red[0][2], red[0][3]));
+        for (int c = tid; c <= c1 - c0; c += kHeadDim) {
+            const int at = __float_as_int(share[c].x);
+            const float f = at < 0 ? 0.f : ptx::ex2(share[c].y - M);
+            share[c].y = f;
+            if (at >= 0) L = fmaf(f, A.part_ml[at * kPdHeads + j].y, L);
+        }
+#pragma unroll
+        for (int o = 16; o; o >>= 1) L += __shfl_xor_sync(0xffffffffu, L, o);
+        if (lane == 0) red[1][warp] = L;
+        __syncthreads();
+        L = (red[1][0] + red[1][1]) + (red[1][2] + red[1][3]);
+        float O = 0.f;
+#pragma unroll 8
+        for (int c = 0; c <= c1 - c0; ++c) {
+            const int at = __float_as_int(share[c].x);
+            if (at >= 0) O = fmaf(share[c].y, A.part_o[((size_t)at * kPdHeads + j) * kHeadDim + tid], O);
+        }
+        reinterpret_cast<T*>(A.io.out)[out] = T(L > 0.f || L != L ? O / L : 0.f);
         return;
     }
-    if (tid < g) {
-        float M, L;
-        sums(tid, M, L);
-        fm[tid] = M;
-        finv[tid] = L > 0.f || L != L ? 1.f / L : 0.f;
+    for (int j = warp; j < g; j += kHeadDim / 32) {   // a warp a query head, a lane a share
+        float M = kNoLogit, L = 0.f;
+        for (int c = c0 + lane; c <= c1; c += 32) {
+            const int at = place(c);
+            if (at < 0) continue;
+            const float2 ml = A.part_ml[at * kPdHeads + j];
+            const float m = fmaxf(M, ml.x);
+            L = fmaf(L, ptx::ex2(M - m), ml.y * ptx::ex2(ml.x - m));
+            M = m;
+        }
+#pragma unroll
+        for (int o = 16; o; o >>= 1) {
+            const float M2 = __shfl_xor_sync(0xffffffffu, M, o), L2 = __shfl_xor_sync(0xffffffffu, L, o);
+            const float m = fmaxf(M, M2);
+            L = fmaf(L, ptx::ex2(M - m), L2 * ptx::ex2(M2 - m));
+            M = m;
+        }
+        if (lane == 0) {
+            fm[j] = M;
+            finv[j] = L > 0.f || L != L ? 1.f / L : 0.f;
+        }
     }
     __syncthreads();
     add_weights<kHeadDim>(A, s, h, v, i0, min(v.nb, i0 + kJoinRows / kPdBlock), fm, finv);
@@ -549,7 +599,8 @@ cudaError_t launch_typed(const PdArgs& a, cudaStream_t st) {
     cudaError_t e = launch_prio(paged_decode_kernel<T, false>, dim3(a.ctas), dim3(kPdThreads), kPdSmem, st, 0, true, a);
     if (e != cudaSuccess) return e;
     const int rows = a.c.weights ? (a.nbmax * kPdBlock + kJoinRows - 1) / kJoinRows : 0;
-    return launch_prio(paged_join_kernel<T>, dim3(a.g + rows, a.io.Hkv, a.io.batch), dim3(kHeadDim), 0, st, 0, true, a);
+    return launch_prio(paged_join_kernel<T>, dim3(a.g + rows, a.io.Hkv, a.io.batch), dim3(kHeadDim),
+                       a.ctas * sizeof(float2), st, 0, true, a);
 }
 
 int visible_blocks(const PagedDecodeIO& io) {

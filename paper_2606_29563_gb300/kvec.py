@@ -358,6 +358,7 @@ class PagedCache:
         self.page_size = k_pages.shape[2]
         self.capacity = self.max_pages * self.page_size
         self.dtype, self.device = k_pages.dtype, k_pages.device
+        self.kv_heads, self.head_dim = k_pages.shape[1], k_pages.shape[3]
         self.c = kvec_paged_cache(self.dtype_code, self.page_size, k_pages.shape[0], self.max_pages,
                                   k_pages.data_ptr(), v_pages.data_ptr(),
                                   None if weights is None else weights.data_ptr(), page_table.data_ptr(), lens.data_ptr())
@@ -376,6 +377,7 @@ class KvecSelector:
         self.handle = None
         self.handle = kvec_create(params)
         self.device = torch.device("cuda", torch.cuda.current_device())
+        self._current = torch._C._cuda_getCurrentRawStream   # torch.cuda.current_stream makes an object, 2 us
         self.state_bytes = kvec_state_bytes(params.max_seqlen)
 
     def close(self) -> None:
@@ -452,32 +454,41 @@ class KvecSelector:
         return out
 
     # ------------------------------------------------------------ decoding over pages
-
-    def _stream(self, stream, device):
-        """The stream of a call on tensors of `device`, which must be the handle's."""
-        _want(device == self.device, f"the tensors are on {device}, the handle on {self.device}")
-        return self._torch.cuda.current_stream(device) if stream is None else stream
+    # A small call is bound by its host time: messages are formed only where a check fails.
 
     def _empty(self, shape, dtype, stream):
-        """Memory that work on `stream` may use at once, from that stream's pool."""
+        """Memory that work on `stream` (None: the current one) may use at once, from that stream's pool."""
         t = self._torch
-        if stream == t.cuda.current_stream(self.device):
+        if stream is None or stream.cuda_stream == self._current(self.device.index):
             return t.empty(shape, dtype=dtype, device=self.device)
         with t.cuda.stream(stream):
             return t.empty(shape, dtype=dtype, device=self.device)
 
-    def _heads(self, x, heads, name, dtype, device):
-        """Checks token rows [T][heads][d] with contiguous heads; their stride in elements."""
+    def _raw(self, stream):
+        return self._current(self.device.index) if stream is None else stream.cuda_stream
+
+    def _check(self, name, x, shape, dtype):
+        """A contiguous tensor of the handle's device."""
+        if x.shape != shape or x.dtype is not dtype or x.device != self.device or not x.is_contiguous():
+            raise KvecError(KVEC_ERR_INVALID_ARG, f"{name} must be contiguous {dtype} {list(shape)} on {self.device}, "
+                                                  f"not {x.dtype} {list(x.shape)} on {x.device}")
+
+    def _rows(self, name, x, T, heads, dtype):
+        """Token rows [T][heads][d], heads side by side; the elements from a token to the next."""
         d = self.params.head_dim
-        _want(x.dim() == 3 and x.shape[1] == heads and x.shape[2] == d and x.dtype == dtype and x.device == device,
-              f"{name} must be {dtype} [T][{heads}][{d}] on {device}")
+        if x.shape != (T, heads, d) or x.dtype is not dtype or x.device != self.device:
+            raise KvecError(KVEC_ERR_INVALID_ARG, f"{name} must be {dtype} {[T, heads, d]} on {self.device}, "
+                                                  f"not {x.dtype} {list(x.shape)} on {x.device}")
         st = x.stride()
-        _want(st[2] == 1 and st[1] == d, f"{name}'s heads must lie side by side")
-        return st[0] if x.shape[0] > 1 else heads * d
+        if T and (st[2] != 1 or (st[1] != d and heads > 1)):
+            raise KvecError(KVEC_ERR_INVALID_ARG, f"{name}'s heads must lie side by side")
+        return st[0] if T > 1 else heads * d
 
     def _check_cache(self, cache):
-        _want(cache.k_pages.shape[1] == self.params.num_kv_heads and cache.k_pages.shape[3] == self.params.head_dim,
-              f"the cache's pages must have {self.params.num_kv_heads} KV heads of {self.params.head_dim}")
+        p = self.params
+        if cache.kv_heads != p.num_kv_heads or cache.head_dim != p.head_dim or cache.device != self.device:
+            raise KvecError(KVEC_ERR_INVALID_ARG, f"the cache's pages must have {p.num_kv_heads} KV heads of "
+                                                  f"{p.head_dim}, on {self.device}")
 
     def rotate_append(self, q, k, v, positions, rot_table=None, cache=None, cu_tokens=None, q_norm=None, k_norm=None,
                       eps: float = 1e-6, interleaved: bool = False, q_out=None, k_out=None, stream=None):
@@ -487,48 +498,46 @@ class KvecSelector:
         rot_table fp32 [max_positions][rot_dim]; cu_tokens int32 [batch + 1] on the device (None: a token a sequence).
         Without a cache k_out is made and (q_out, k_out) returned; with one q_out, or both where k_out is given."""
         t, p = self._torch, self.params
-        T, dtype, dev = q.shape[0], q.dtype, q.device
-        a = kvec_rotate_args(dtype=_dtype_code(t, dtype), num_tokens=T, eps=eps, interleaved=1 if interleaved else 0)
-        a.q_stride = self._heads(q, p.num_q_heads, "q", dtype, dev)
-        a.k_stride = self._heads(k, p.num_kv_heads, "k", dtype, dev)
-        _want(k.shape[0] == T and positions.dtype == t.int32 and tuple(positions.shape) == (T,) and
-              positions.is_contiguous() and positions.device == dev, "k and int32 positions must be of q's tokens")
-        a.q, a.k, a.positions = q.data_ptr(), k.data_ptr(), positions.data_ptr()
-        if v is not None:
-            a.v_stride = self._heads(v, p.num_kv_heads, "v", dtype, dev)
-            _want(v.shape[0] == T, "v must be of q's tokens")
-            a.v = v.data_ptr()
+        T, dtype, Hq, Hkv, d = q.shape[0], q.dtype, p.num_q_heads, p.num_kv_heads, p.head_dim
+        code = _dtype_code(t, dtype)
+        q_stride = self._rows("q", q, T, Hq, dtype)
+        k_stride = self._rows("k", k, T, Hkv, dtype)
+        v_stride = 0 if v is None else self._rows("v", v, T, Hkv, dtype)
+        self._check("positions", positions, (T,), t.int32)
+        rot = most = 0
         if rot_table is not None:
-            _want(rot_table.dim() == 2 and rot_table.dtype == t.float32 and rot_table.is_contiguous() and
-                  rot_table.device == dev, "rot_table must be contiguous fp32 [max_positions][rot_dim]")
-            a.max_positions, a.rot_dim = rot_table.shape
-            a.rot_table = rot_table.data_ptr()
-        for name, w in (("q_norm", q_norm), ("k_norm", k_norm)):
-            if w is not None:
-                _want(w.dtype == dtype and tuple(w.shape) == (p.head_dim,) and w.is_contiguous() and w.device == dev,
-                      f"{name} must be {dtype} [{p.head_dim}]")
-                setattr(a, name, w.data_ptr())
+            _want(rot_table.dim() == 2, "rot_table must be [max_positions][rot_dim]")
+            most, rot = rot_table.shape
+            self._check("rot_table", rot_table, (most, rot), t.float32)
+        if q_norm is not None:
+            self._check("q_norm", q_norm, (d,), dtype)
+        if k_norm is not None:
+            self._check("k_norm", k_norm, (d,), dtype)
         batch = T
         if cu_tokens is not None:
-            _want(cu_tokens.dtype == t.int32 and cu_tokens.dim() == 1 and cu_tokens.is_contiguous() and
-                  cu_tokens.device == dev, "cu_tokens must be int32 [batch + 1] on the device")
             batch = cu_tokens.shape[0] - 1
+            self._check("cu_tokens", cu_tokens, (batch + 1,), t.int32)
         if cache is not None:
             self._check_cache(cache)
-            _want(cache.batch == batch and cache.device == dev, f"the cache has {cache.batch} sequences, the call {batch}")
-        for name, x, like in (("q_out", q_out, q), ("k_out", k_out, k)):
-            _want(x is None or (x.shape == like.shape and x.dtype == dtype and x.is_contiguous() and x.device == dev),
-                  f"{name} must be contiguous, of its input's shape and type")
+            if cache.batch != batch:
+                raise KvecError(KVEC_ERR_INVALID_ARG, f"the cache has {cache.batch} sequences, the call {batch}")
         want_k = cache is None or k_out is not None
-        stream = self._stream(stream, dev)
         if q_out is None:
-            q_out = self._empty((T, p.num_q_heads, p.head_dim), dtype, stream)
-        if cache is None and k_out is None:
-            k_out = self._empty((T, p.num_kv_heads, p.head_dim), dtype, stream)
-        a.q_out, a.k_out = q_out.data_ptr(), None if k_out is None else k_out.data_ptr()
+            q_out = self._empty((T, Hq, d), dtype, stream)
+        else:
+            self._check("q_out", q_out, (T, Hq, d), dtype)
+        if k_out is not None:
+            self._check("k_out", k_out, (T, Hkv, d), dtype)
+        elif cache is None:
+            k_out = self._empty((T, Hkv, d), dtype, stream)
         if T:
+            a = kvec_rotate_args(code, T, q.data_ptr(), k.data_ptr(), None if v is None else v.data_ptr(), q_stride,
+                                 k_stride, v_stride, None if q_norm is None else q_norm.data_ptr(),
+                                 None if k_norm is None else k_norm.data_ptr(), eps, rot, 1 if interleaved else 0, most,
+                                 None if rot_table is None else rot_table.data_ptr(), positions.data_ptr(),
+                                 q_out.data_ptr(), None if k_out is None else k_out.data_ptr())
             kvec_rotate_append(self.handle, a, batch, None if cu_tokens is None else cu_tokens.data_ptr(),
-                               None if cache is None else cache.c, stream.cuda_stream)
+                               None if cache is None else cache.c, self._raw(stream))
         return (q_out, k_out) if want_k else q_out
 
     def paged_decode(self, q, cache, max_len: Optional[int] = None, window: int = 0, sinks: int = 0, out=None,
@@ -536,23 +545,21 @@ class KvecSelector:
         """One new token per sequence over a paged cache (kvec_paged_decode); adds to cache.weights where it has them.
 
         q [batch][H_q][d] of the cache's type, contiguous; max_len: a bound on the lengths (the capacity)."""
-        t, p = self._torch, self.params
-        batch, dev = cache.batch, cache.device
-        self._check_cache(cache)
+        p = self.params
+        batch, dtype = cache.batch, cache.dtype
         shape = (batch, p.num_q_heads, p.head_dim)
-        _want(tuple(q.shape) == shape and q.dtype == cache.dtype and q.is_contiguous() and q.device == dev,
-              f"q must be contiguous {cache.dtype} {list(shape)} on {dev}")
-        stream = self._stream(stream, dev)
+        self._check_cache(cache)
+        self._check("q", q, shape, dtype)
         if out is None:
-            out = self._empty(shape, q.dtype, stream)
+            out = self._empty(shape, dtype, stream)
         else:
-            _want(tuple(out.shape) == shape and out.dtype == q.dtype and out.is_contiguous() and out.device == dev,
-                  "out must be as q")
-        max_len = cache.capacity if max_len is None else max_len
+            self._check("out", out, shape, dtype)
+        if max_len is None:
+            max_len = cache.capacity
         need = kvec_paged_decode_bytes(self.handle, batch, max_len, cache.weights is not None)
-        scratch = self._empty(max(need, 16), t.uint8, stream)
+        scratch = self._empty(max(need, 16), self._torch.uint8, stream)
         kvec_paged_decode(self.handle, batch, q.data_ptr(), cache.c, max_len, window, sinks, out.data_ptr(),
-                          scratch.data_ptr(), need, stream.cuda_stream)
+                          scratch.data_ptr(), need, self._raw(stream))
         return out
 
     def paged_evict(self, cache, new_table, budget: int, sinks: int = 0, recent: int = 0, max_len: Optional[int] = None,
@@ -562,23 +569,22 @@ class KvecSelector:
         new_table int32 [batch][pages], contiguous, of pages that page_table does not use.  Returns (new_lens int32
         [batch], kept int32 [batch][H_kv][budget])."""
         t, p = self._torch, self.params
-        batch, dev = cache.batch, cache.device
+        batch, Hkv = cache.batch, p.num_kv_heads
         self._check_cache(cache)
-        _want(new_table.dim() == 2 and new_table.shape[0] == batch and new_table.dtype == t.int32 and
-              new_table.is_contiguous() and new_table.device == dev, f"new_table must be int32 [{batch}][pages] on {dev}")
-        _want(budget >= 1, f"budget {budget} < 1")
-        stream = self._stream(stream, dev)
+        _want(new_table.dim() == 2, "new_table must be int32 [batch][pages]")
+        self._check("new_table", new_table, (batch, new_table.shape[1]), t.int32)
+        _want(1 <= budget <= 1 << 20, "budget must be in [1, 2^20]")
         if new_lens is None:
-            new_lens = self._empty(batch, t.int32, stream)
+            new_lens = self._empty((batch,), t.int32, stream)
+        else:
+            self._check("new_lens", new_lens, (batch,), t.int32)
         if kept is None:
-            kept = self._empty((batch, p.num_kv_heads, budget), t.int32, stream)
-        _want(new_lens.dtype == t.int32 and tuple(new_lens.shape) == (batch,) and new_lens.is_contiguous() and
-              new_lens.device == dev, "new_lens must be int32 [batch]")
-        _want(kept.dtype == t.int32 and tuple(kept.shape) == (batch, p.num_kv_heads, budget) and kept.is_contiguous() and
-              kept.device == dev, "kept must be int32 [batch][H_kv][budget]")
+            kept = self._empty((batch, Hkv, budget), t.int32, stream)
+        else:
+            self._check("kept", kept, (batch, Hkv, budget), t.int32)
         kvec_paged_evict(self.handle, batch, cache.c, new_table.data_ptr(), new_table.shape[1],
                          cache.capacity if max_len is None else max_len, budget, sinks, recent, new_lens.data_ptr(),
-                         kept.data_ptr(), stream.cuda_stream)
+                         kept.data_ptr(), self._raw(stream))
         return new_lens, kept
 
     def prefill_attention(self, q, k, v, cu_q_host, cu_q_dev, cu_k_host=None, cu_k_dev=None, window: int = 0,
@@ -588,34 +594,35 @@ class KvecSelector:
         q [T_q][H_q][d], k, v [T_k][H_kv][d] bf16 or fp16, contiguous; cu_* int32 [batch + 1], host and device copies
         (cu_k: cu_q).  Returns (out as q, lse fp32 [T_q][H_q])."""
         t, p = self._torch, self.params
-        dtype, dev, d = q.dtype, q.device, p.head_dim
+        dtype, Tq, Hq, Hkv, d = q.dtype, q.shape[0], p.num_q_heads, p.num_kv_heads, p.head_dim
+        code = _dtype_code(t, dtype)
         if cu_k_host is None:
             cu_k_host, cu_k_dev = cu_q_host, cu_q_dev
-        code = _dtype_code(t, dtype)
-        for name, x, heads in (("q", q, p.num_q_heads), ("k", k, p.num_kv_heads), ("v", v, p.num_kv_heads)):
-            _want(x.dim() == 3 and x.shape[1] == heads and x.shape[2] == d and x.dtype == dtype and x.device == dev and
-                  x.is_contiguous(), f"{name} must be contiguous {dtype} [T][{heads}][{d}] on {dev}")
-        batch = cu_q_host.shape[0] - 1
-        for x in (cu_q_host, cu_k_host, cu_q_dev, cu_k_dev):
-            _want(x.dtype == t.int32 and tuple(x.shape) == (batch + 1,) and x.is_contiguous(),
-                  "cu_q and cu_k must be contiguous int32 [batch + 1]")
-        _want(cu_q_host.device.type == "cpu" and cu_k_host.device.type == "cpu" and cu_q_dev.device == dev and
-              cu_k_dev.device == dev, "cu_q and cu_k are wanted on the host and on the device")
-        _want(batch >= 1 and int(cu_q_host[-1]) <= q.shape[0] and int(cu_k_host[-1]) <= min(k.shape[0], v.shape[0]),
-              "cu_q or cu_k passes the rows given")
-        _want(out is None or (out.shape == q.shape and out.dtype == dtype and out.is_contiguous() and out.device == dev),
-              "out must be as q")
-        _want(lse is None or (lse.dtype == t.float32 and lse.shape == q.shape[:2] and lse.is_contiguous() and
-                              lse.device == dev), "lse must be contiguous fp32 [T_q][H_q]")
-        stream = self._stream(stream, dev)
-        out = self._empty(q.shape, dtype, stream) if out is None else out
-        lse = self._empty(q.shape[:2], t.float32, stream) if lse is None else lse
-        need = kvec_prefill_bytes(self.handle, batch, cu_q_host.data_ptr(), cu_k_host.data_ptr(), window, sinks)
-        scratch = self._empty(need, t.uint8, stream) if need else None
-        kvec_prefill_attention(self.handle, code, batch, cu_q_host.data_ptr(), cu_q_dev.data_ptr(),
-                               cu_k_host.data_ptr(), cu_k_dev.data_ptr(), q.data_ptr(), k.data_ptr(), v.data_ptr(),
-                               window, sinks, out.data_ptr(), lse.data_ptr(),
-                               scratch.data_ptr() if need else None, need, stream.cuda_stream)
+        Tk, batch = k.shape[0], cu_q_host.shape[0] - 1
+        self._check("q", q, (Tq, Hq, d), dtype)
+        self._check("k", k, (Tk, Hkv, d), dtype)
+        self._check("v", v, (Tk, Hkv, d), dtype)
+        self._check("cu_q_dev", cu_q_dev, (batch + 1,), t.int32)
+        self._check("cu_k_dev", cu_k_dev, (batch + 1,), t.int32)
+        for x in (cu_q_host, cu_k_host):
+            _want(x.dtype is t.int32 and x.shape == (batch + 1,) and x.device.type == "cpu" and x.is_contiguous(),
+                  "cu_q_host and cu_k_host must be contiguous int32 [batch + 1] on the host")
+        _want(batch >= 1 and cu_q_host[-1].item() <= Tq and cu_k_host[-1].item() <= Tk,
+              "cu_q_host or cu_k_host passes the rows given")
+        if out is None:
+            out = self._empty((Tq, Hq, d), dtype, stream)
+        else:
+            self._check("out", out, (Tq, Hq, d), dtype)
+        if lse is None:
+            lse = self._empty((Tq, Hq), t.float32, stream)
+        else:
+            self._check("lse", lse, (Tq, Hq), t.float32)
+        cu_q, cu_k = cu_q_host.data_ptr(), cu_k_host.data_ptr()
+        need = kvec_prefill_bytes(self.handle, batch, cu_q, cu_k, window, sinks)
+        scratch = self._empty((need,), t.uint8, stream).data_ptr() if need else None
+        kvec_prefill_attention(self.handle, code, batch, cu_q, cu_q_dev.data_ptr(), cu_k, cu_k_dev.data_ptr(),
+                               q.data_ptr(), k.data_ptr(), v.data_ptr(), window, sinks, out.data_ptr(), lse.data_ptr(),
+                               scratch, need, self._raw(stream))
         return out, lse
 
     def debug(self, device="cuda"):
