@@ -106,55 +106,70 @@ struct Walker {
             }
         }
     }
-    // To block `at` of the whole list, by a whole warp: a lane looks at a sequence.
-    __device__ __forceinline__ void seek(const PdArgs& A, long long at) {
+};
+
+// The list of all blocks as a warp sees it: lane l holds the blocks of the sequences
+// l * per .. l * per + per - 1, over all KV heads.
+struct List {
+    int per;
+    long long before, mine, total;   // of the lanes before, of this lane, of all
+    __device__ __forceinline__ void init(const PdArgs& A) {
         const int lane = threadIdx.x & 31;
-        for (int s0 = 0; s0 < A.io.batch; s0 += 32) {
-            v.nb = 0;
-            if (s0 + lane < A.io.batch) v.init(A, s0 + lane);
-            const long long mine = (long long)v.nb * A.io.Hkv;
-            long long upto = mine;
-#pragma unroll
-            for (int o = 1; o < 32; o <<= 1) {
-                const long long y = __shfl_up_sync(0xffffffffu, upto, o);
-                if (lane >= o) upto += y;
-            }
-            const uint32_t past = __ballot_sync(0xffffffffu, at < upto);
-            if (past) {
-                const int l = __ffs(past) - 1;
-                at -= __shfl_sync(0xffffffffu, upto - mine, l);
-                s = s0 + l;
-                v.init(A, s);
-                h = (int)at / v.nb;      // at < nb * Hkv <= 2^21
-                i = (int)at - h * v.nb;
-                return;
-            }
-            at -= __shfl_sync(0xffffffffu, upto, 31);
+        per = (A.io.batch + 31) >> 5;
+        mine = 0;
+        for (int k = 0; k < per; ++k) {
+            const int s = lane * per + k;
+            if (s >= A.io.batch) break;
+            Visible v;
+            v.init(A, s);
+            mine += v.nb;
         }
-        s = A.io.batch;
-        h = i = 0;
-        v.nb = 0;
+        mine *= A.io.Hkv;
+        long long upto = mine;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const long long y = __shfl_up_sync(0xffffffffu, upto, o);
+            if (lane >= o) upto += y;
+        }
+        before = upto - mine;
+        total = __shfl_sync(0xffffffffu, upto, 31);
+    }
+    // The place of block `at`.
+    __device__ __forceinline__ void seek(const PdArgs& A, long long at, Walker& w) const {
+        const uint32_t past = __ballot_sync(0xffffffffu, at < before + mine);
+        w.s = A.io.batch;
+        w.h = w.i = 0;
+        w.v.nb = 0;
+        if (!past) return;
+        const int l = __ffs(past) - 1;
+        at -= __shfl_sync(0xffffffffu, before, l);
+        for (w.s = l * per;; ++w.s) {
+            w.v.init(A, w.s);
+            const long long here = (long long)w.v.nb * A.io.Hkv;
+            if (at < here) break;
+            at -= here;
+        }
+        w.h = (int)at / w.v.nb;          // at < nb * Hkv <= 2^21
+        w.i = (int)at - w.h * w.v.nb;
+    }
+    // Blocks of the sequences before s.
+    __device__ __forceinline__ long long blocks_before(const PdArgs& A, int s) const {
+        const int l = s / per;
+        long long b = __shfl_sync(0xffffffffu, before, l);
+        for (int k = l * per; k < s; ++k) {
+            Visible v;
+            v.init(A, k);
+            b += (long long)v.nb * A.io.Hkv;
+        }
+        return b;
     }
 };
 
-// Blocks of the sequences before `upto`, and of all, over all KV heads: the whole warp.
-__device__ __forceinline__ longlong2 blocks_before(const PdArgs& A, int upto) {
-    long long before = 0, all = 0;
-    for (int s = threadIdx.x & 31; s < A.io.batch; s += 32) {
-        Visible v;
-        v.init(A, s);
-        all += v.nb;
-        if (s < upto) before += v.nb;
-    }
-#pragma unroll
-    for (int o = 16; o; o >>= 1) {
-        all += __shfl_xor_sync(0xffffffffu, all, o);
-        before += __shfl_xor_sync(0xffffffffu, before, o);
-    }
-    return make_longlong2(before * A.io.Hkv, all * A.io.Hkv);
+// a / b, in 32 bits where they do.
+__device__ __forceinline__ long long quotient(long long a, long long b) {
+    return ((a | b) >> 32) == 0 ? (long long)((uint32_t)a / (uint32_t)b) : a / b;
 }
-
-__device__ __forceinline__ long long share_start(long long total, int cta, int ctas) { return total * cta / ctas; }
+__device__ __forceinline__ long long share_start(long long total, int cta, int ctas) { return quotient(total * cta, ctas); }
 
 __device__ __forceinline__ void ldmatrix_x4(uint32_t addr, uint32_t (&r)[4]) {
     asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0, %1, %2, %3}, [%4];\n"
@@ -169,21 +184,58 @@ __device__ __forceinline__ void ldmatrix_x4_trans(uint32_t addr, uint32_t (&r)[4
                  : "memory");
 }
 
-// Adds the attention weights of blocks [i0, i1) of pair (s, h) to the cache's, from the
-// pair's logits and its query heads' (maximum, 1 / sum).
+// The attention weights of four slots of a block: what is read for them, and their sum over
+// the query heads once these' (maximum, 1 / sum) are known.
+struct SlotWeights {
+    float4 x[kPdHeads], w;
+    int row;          // of the first, -1: none of them is visible or they are on no page
+    bool seen[4];
+    // Quarter e of the pair's blocks from block i0 on.
+    __device__ __forceinline__ void load(const PdArgs& A, int s, int h, const Visible& v, int i0, int e) {
+        const int i = i0 + (e >> 2), r = (e & 3) * 4, b = v.block(i);
+        row = block_row(A, s, h, b);
+        bool any = false;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) any |= seen[k] = v.sees(b * kPdBlock + r + k);
+        row = any && row >= 0 ? row + r : -1;
+        if (row < 0) return;
+        const float* lg = A.logits + (((size_t)s * A.io.Hkv + h) * A.nbmax + i) * (size_t)(A.g * kPdBlock) + r;
+#pragma unroll
+        for (int j = 0; j < kPdHeads; ++j)
+            if (j < A.g) x[j] = *reinterpret_cast<const float4*>(lg + j * kPdBlock);
+        w = *reinterpret_cast<const float4*>(A.c.weights + row);
+    }
+    __device__ __forceinline__ void store(const PdArgs& A, const float* mx, const float* inv) const {
+        if (row < 0) return;
+        float p[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int j = 0; j < kPdHeads; ++j) {
+            if (j >= A.g) break;
+            const float m = mx[j], f = inv[j];
+            p[0] = fmaf(ptx::ex2(x[j].x - m), f, p[0]);
+            p[1] = fmaf(ptx::ex2(x[j].y - m), f, p[1]);
+            p[2] = fmaf(ptx::ex2(x[j].z - m), f, p[2]);
+            p[3] = fmaf(ptx::ex2(x[j].w - m), f, p[3]);
+        }
+        *reinterpret_cast<float4*>(A.c.weights + row) =
+            make_float4(seen[0] ? w.x + p[0] : w.x, seen[1] ? w.y + p[1] : w.y, seen[2] ? w.z + p[2] : w.z,
+                        seen[3] ? w.w + p[3] : w.w);
+    }
+};
+
+// Adds the attention weights of blocks [i0, i1) of pair (s, h) to the cache's.  Two quarters
+// of a thread's are read at once: one after the other, the latencies of a long row added up.
 template <int NT>
 __device__ void add_weights(const PdArgs& A, int s, int h, const Visible& v, int i0, int i1, const float* mx,
                             const float* inv) {
-    const float* lg = A.logits + ((size_t)s * A.io.Hkv + h) * A.nbmax * (size_t)(A.g * kPdBlock);
-    for (int e = threadIdx.x; e < (i1 - i0) * kPdBlock; e += NT) {
-        const int i = i0 + e / kPdBlock, r = e % kPdBlock, b = v.block(i);
-        if (!v.sees(b * kPdBlock + r)) continue;
-        const int row = block_row(A, s, h, b);
-        if (row < 0) continue;
-        const float* x = lg + (size_t)i * (A.g * kPdBlock) + r;
-        float w = 0.f;
-        for (int j = 0; j < A.g; ++j) w = fmaf(ptx::ex2(x[j * kPdBlock] - mx[j]), inv[j], w);
-        A.c.weights[(size_t)row + r] += w;
+    const int n = (i1 - i0) * 4;
+    for (int e = threadIdx.x; e < n; e += 2 * NT) {
+        SlotWeights a, b;
+        b.row = -1;
+        a.load(A, s, h, v, i0, e);
+        if (e + NT < n) b.load(A, s, h, v, i0, e + NT);
+        a.store(A, mx, inv);
+        b.store(A, mx, inv);
     }
 }
 
@@ -199,7 +251,7 @@ __global__ void __launch_bounds__(kPdThreads, kPdCtasPerSm) paged_decode_kernel(
     __shared__ float* wacc[kPdWarps];                           // the warps' outputs, each in its free stage
     __shared__ float cm[kPdHeads], cl[kPdHeads], fm[kPdHeads], finv[kPdHeads];
     __shared__ __align__(16) float co[CL ? kPdHeads : 1][kHeadDim];
-    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    const int tid = threadIdx.x, lane = tid & 31, warp = ptx::warp_uniform(tid >> 5);
     const int Hq = A.io.Hq, Hkv = A.io.Hkv, g = A.g;
     if (tid == 0) {
         ptx::prefetch_tensormap(&A.kmap);
@@ -209,12 +261,14 @@ __global__ void __launch_bounds__(kPdThreads, kPdCtasPerSm) paged_decode_kernel(
         ptx::fence_barrier_init();
     }
     __syncthreads();
-    asm volatile("griddepcontrol.launch_dependents;\n" ::: "memory");
+    // The trigger follows the wait: what was complete before this grid may be read by the
+    // join kernel before its own wait.
     asm volatile("griddepcontrol.wait;\n" ::: "memory");
+    asm volatile("griddepcontrol.launch_dependents;\n" ::: "memory");
 
     // This CTA's blocks: `count` from (s, h, i) on.
     Walker cur;
-    long long count;
+    int count;   // a share of at most 65535 * 32 * 2^16 blocks
     int splits = 1, rank = 0;
     if constexpr (CL) {
         splits = (int)gridDim.x;
@@ -222,32 +276,45 @@ __global__ void __launch_bounds__(kPdThreads, kPdCtasPerSm) paged_decode_kernel(
         cur.s = blockIdx.z;
         cur.h = blockIdx.y;
         cur.v.init(A, cur.s);
-        cur.i = (int)((long long)cur.v.nb * rank / splits);
-        count = (long long)cur.v.nb * (rank + 1) / splits - cur.i;
+        cur.i = cur.v.nb * rank / splits;
+        count = cur.v.nb * (rank + 1) / splits - cur.i;
     } else {
-        const long long total = blocks_before(A, 0).y;
-        const long long at = share_start(total, blockIdx.x, A.ctas);
-        count = share_start(total, blockIdx.x + 1, A.ctas) - at;
-        cur.seek(A, at);
+        List list;
+        list.init(A);
+        const long long at = share_start(list.total, blockIdx.x, A.ctas);
+        count = (int)(share_start(list.total, blockIdx.x + 1, A.ctas) - at);
+        list.seek(A, at, cur);
     }
 
     uint8_t* ring = smem + warp * (kPdStages * kPdStage);
     const uint32_t ring32 = ptx::smem_u32(ring);
     // Loads: this warp's blocks are warp, warp + 4, ... of the CTA's; load number k goes to
     // stage k % kPdStages, and one stage is free while a block is worked on.
+    // The rows of the next two are fetched ahead: a page's number takes as long as its rows.
     Walker ld = cur;
-    long long ld_at = warp;
-    if (ld_at < count) ld.advance(A, warp);
+    int ld_at = warp, row_at = warp;      // the next load, the next row to fetch
+    if (row_at < count) ld.advance(A, warp);
+    auto next_row = [&]() {
+        if (row_at >= count) return -1;
+        const int row = block_row(A, ld.s, ld.h, ld.v.block(ld.i));
+        row_at += kPdWarps;
+        if (row_at < count) ld.advance(A, kPdWarps);
+        return row;
+    };
+    int rows[2];
+    rows[0] = next_row();
+    rows[1] = next_row();
     int ld_stage = 0;
     bool failed = false;      // a wait gave up: no further loads and waits, outputs are invalid
     auto load_next = [&]() {
         if (ld_at < count && !failed) {
-            const int row = block_row(A, ld.s, ld.h, ld.v.block(ld.i));
-            if (lane == 0) {
-                srow[warp][ld_stage] = row;
+            // Warp-uniform operands: else each TMA instruction moves its own to uniform registers.
+            const int row = ptx::warp_uniform(rows[0]), at = ptx::warp_uniform(ld_stage);
+            if (ptx::elect_one()) {
+                srow[warp][at] = row;
                 if (row >= 0) {
-                    uint8_t* dst = ring + ld_stage * kPdStage;
-                    uint64_t* bar = &full[warp][ld_stage];
+                    uint8_t* dst = ring + at * kPdStage;
+                    uint64_t* bar = &full[warp][at];
                     ptx::mbar_arrive_expect_tx(bar, kPdStage);
                     ptx::tma_load_2d(dst, &A.kmap, bar, 0, row);
                     ptx::tma_load_2d(dst + kPdTile, &A.kmap, bar, 64, row);
@@ -256,7 +323,8 @@ __global__ void __launch_bounds__(kPdThreads, kPdCtasPerSm) paged_decode_kernel(
                 }
             }
             ld_at += kPdWarps;
-            if (ld_at < count) ld.advance(A, kPdWarps);
+            rows[0] = rows[1];
+            rows[1] = next_row();
         }
         ld_stage = ld_stage + 1 == kPdStages ? 0 : ld_stage + 1;
     };
@@ -267,12 +335,12 @@ __global__ void __launch_bounds__(kPdThreads, kPdCtasPerSm) paged_decode_kernel(
     int st = 0;               // stage of this warp's next block
     uint32_t phases = 0u;     // bit i: parity of stage i's next completion
     bool first_segment = true;
-    long long done = 0;       // blocks of the CTA's that precede the current segment
+    int done = 0;             // blocks of the CTA's that precede the current segment
     while (CL || done < count) {
         // A segment: the CTA's blocks of one pair.
         const int s = cur.s, h = cur.h, i_begin = cur.i;
         const Visible v = cur.v;
-        const int len = (int)min(count - done, (long long)(v.nb - i_begin));
+        const int len = min(count - done, v.nb - i_begin);
         const bool whole = len == v.nb;
         // The group's query rows as the upper half of the tile's row operand: head lane / 4.
         uint32_t qa[8][2];
@@ -294,7 +362,7 @@ __global__ void __launch_bounds__(kPdThreads, kPdCtasPerSm) paged_decode_kernel(
             for (int c = 0; c < 4; ++c) acc[d][c] = 0.f;
         float m = kNoLogit, l = 0.f;   // head lane / 4; l of this lane's slots
         // The warp's first block of the segment: its blocks are warp mod kPdWarps of the CTA's.
-        const int skip = (int)((warp - done % kPdWarps + kPdWarps) % kPdWarps);
+        const int skip = (warp - done % kPdWarps + kPdWarps) % kPdWarps;
         for (int e = skip; e < len; e += kPdWarps) {
             const int i = i_begin + e, b = v.block(i);
             __syncwarp();
@@ -434,6 +502,10 @@ __global__ void __launch_bounds__(kPdThreads, kPdCtasPerSm) paged_decode_kernel(
         ptx::fence_proxy_async_smem();   // the outputs lay where the next load goes
         __syncthreads();
         if constexpr (CL) {
+            // A CTA of a cluster has 32 blocks at most, a quarter a thread, read while the cluster meets.
+            SlotWeights sw;
+            sw.row = -1;
+            if (A.c.weights && tid < len * 4) sw.load(A, s, h, v, i_begin, tid);
             if (splits > 1) {
                 cg::cluster_group cluster = cg::this_cluster();
                 cluster.sync();
@@ -463,14 +535,17 @@ __global__ void __launch_bounds__(kPdThreads, kPdCtasPerSm) paged_decode_kernel(
                     }
                     reinterpret_cast<T*>(A.io.out)[((size_t)s * Hq + (size_t)h * g + j) * kHeadDim + c] = T(O * finv[j]);
                 }
+                if (A.c.weights) sw.store(A, fm, finv);
                 cluster.sync();   // no CTA leaves while another still reads its shared memory
+            } else if (A.c.weights) {
+                sw.store(A, fm, finv);
             }
+            break;
         }
-        if (A.c.weights && (CL || whole)) {
+        if (A.c.weights && whole) {
             add_weights<kPdThreads>(A, s, h, v, i_begin, i_begin + len, fm, finv);
             __syncthreads();      // before the next segment's fm and finv
         }
-        if constexpr (CL) break;
         done += len;
         cur.advance(A, len);
         first_segment = false;
@@ -488,26 +563,30 @@ template <class T>
 __global__ void __launch_bounds__(kHeadDim) paged_join_kernel(const __grid_constant__ PdArgs A) {
     extern __shared__ float2 share[];                 // (place as an int, factor) of the output block's shares
     __shared__ float fm[kPdHeads], finv[kPdHeads], red[2][kHeadDim / 32];
-    asm volatile("griddepcontrol.launch_dependents;\n" ::: "memory");
-    asm volatile("griddepcontrol.wait;\n" ::: "memory");
     const int h = blockIdx.y, s = blockIdx.z, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = A.g;
     Visible v;
     v.init(A, s);
     const int i0 = ((int)blockIdx.x - g) * (kJoinRows / kPdBlock);
-    if ((int)blockIdx.x >= g && i0 >= v.nb) return;
     const size_t out = ((size_t)s * A.io.Hq + (size_t)h * g + blockIdx.x) * kHeadDim + tid;
+    // The lengths were complete before the kernel that this one waits for began.
+    List list;
+    list.init(A);
+    const long long total = list.total, p0 = list.blocks_before(A, s) + (long long)h * v.nb, p1 = p0 + v.nb;
+    const int c0 = v.nb ? (int)quotient((p0 + 1) * A.ctas - 1, total) : 0, c1 = v.nb ? (int)quotient(p1 * A.ctas - 1, total) : 0;
+    asm volatile("griddepcontrol.launch_dependents;\n" ::: "memory");
+    asm volatile("griddepcontrol.wait;\n" ::: "memory");
     if (v.nb == 0) {
         if ((int)blockIdx.x < g) reinterpret_cast<T*>(A.io.out)[out] = T(0.f);
         return;
     }
-    const longlong2 list = blocks_before(A, s);
-    const long long total = list.y, p0 = list.x + (long long)h * v.nb, p1 = p0 + v.nb;
-    const int c0 = (int)(((p0 + 1) * A.ctas - 1) / total), c1 = (int)((p1 * A.ctas - 1) / total);
-    if (c0 == c1) return;   // finished by its CTA
-    // The place of CTA c's share, -1 if it has no blocks: its first segment's, unless the pair begins inside it.
+    // Finished by its CTA, or a block of slots that the sequence does not have.
+    if (c0 == c1 || i0 >= v.nb) return;
+    // The place of CTA c's share, -1 if it has no blocks (there are fewer than CTAs): its first
+    // segment's, unless the pair begins inside it, as it may in c0's.
+    const int first = c0 * 2 + (share_start(total, c0, A.ctas) < p0 ? 1 : 0);
     auto place = [&](int c) {
-        const long long from = share_start(total, c, A.ctas);
-        return from == share_start(total, c + 1, A.ctas) ? -1 : c * 2 + (from < p0 ? 1 : 0);
+        if (c == c0) return first;
+        return total < A.ctas && share_start(total, c, A.ctas) == share_start(total, c + 1, A.ctas) ? -1 : c * 2;
     };
     if ((int)blockIdx.x < g) {
         const int j = blockIdx.x;
@@ -535,10 +614,23 @@ __global__ void __launch_bounds__(kHeadDim) paged_join_kernel(const __grid_const
         __syncthreads();
         L = (red[1][0] + red[1][1]) + (red[1][2] + red[1][3]);
         float O = 0.f;
-#pragma unroll 8
-        for (int c = 0; c <= c1 - c0; ++c) {
-            const int at = __float_as_int(share[c].x);
-            if (at >= 0) O = fmaf(share[c].y, A.part_o[((size_t)at * kPdHeads + j) * kHeadDim + tid], O);
+        const float* part = A.part_o + (size_t)j * kHeadDim + tid;
+        constexpr size_t kPlace = (size_t)kPdHeads * kHeadDim;
+        if (total >= A.ctas) {   // no share is empty: eight reads at once, with no branch between them
+            int c = 0;
+            for (; c + 8 <= c1 - c0 + 1; c += 8) {
+                float o[8];
+#pragma unroll
+                for (int k = 0; k < 8; ++k) o[k] = part[__float_as_int(share[c + k].x) * kPlace];
+#pragma unroll
+                for (int k = 0; k < 8; ++k) O = fmaf(share[c + k].y, o[k], O);
+            }
+            for (; c <= c1 - c0; ++c) O = fmaf(share[c].y, part[__float_as_int(share[c].x) * kPlace], O);
+        } else {
+            for (int c = 0; c <= c1 - c0; ++c) {
+                const int at = __float_as_int(share[c].x);
+                if (at >= 0) O = fmaf(share[c].y, part[at * kPlace], O);
+            }
         }
         reinterpret_cast<T*>(A.io.out)[out] = T(L > 0.f || L != L ? O / L : 0.f);
         return;
