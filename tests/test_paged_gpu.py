@@ -436,3 +436,35 @@ def test_calls_on_two_streams_and_in_a_graph():
         torch.cuda.synchronize()
         for (q, cache, w0), (_, out), (ref, w) in zip(cases, graphs, want):
             assert torch.equal(out, ref) and (k or torch.equal(cache.weights, w))
+
+
+@pytest.mark.parametrize("Hq,Hkv,T", [(8, 2, 999), (8, 2, 1001), (32, 8, 3126), (32, 8, 3127), (16, 8, 18755), (40, 8, 12000)])
+def test_rotate_append_on_both_sides_of_the_layout_rule(Hq, Hkv, T):
+    # Every layout gives the same rows, bit for bit, as one token at a time: 12000, 150000 and 600000 rows.
+    gen = torch.Generator(device="cuda").manual_seed(T)
+    dtype, page, new = torch.bfloat16, 32, [T // 3, T - T // 3]
+    counts = [-(-n // page) for n in new]
+    table = torch.full((2, max(counts)), -1, dtype=torch.int32)
+    perm = torch.randperm(sum(counts), generator=torch.Generator().manual_seed(T)).to(torch.int32)
+    table[0, :counts[0]], table[1, :counts[1]] = perm[:counts[0]], perm[counts[0]:]
+    x = torch.randn((T, Hq + 2 * Hkv, D), generator=gen, device="cuda").to(dtype)
+    w = (torch.randn((2, D), generator=gen, device="cuda") * 0.2 + 1).to(dtype)
+    pos = torch.cat([torch.arange(n) for n in new]).int().cuda()
+    tab = rot_table(max(new), 128).cuda()
+    sel, got = selector(Hq, Hkv), []
+    for step in (T, 97):
+        k, v = (torch.zeros((sum(counts), Hkv, page, D), dtype=dtype, device="cuda") for _ in range(2))
+        weights = torch.ones((sum(counts), Hkv, page), device="cuda")
+        q = torch.empty((T, Hq, D), dtype=dtype, device="cuda")
+        for t0 in range(0, T, step):
+            t1 = min(t0 + step, T)
+            cu = torch.tensor([0, new[0], T]).clamp(t0, t1) - t0
+            held = torch.tensor([min(t1, new[0]), max(t1 - new[0], 0)], dtype=torch.int32).cuda()
+            sel.rotate_append(x[t0:t1, :Hq], x[t0:t1, Hq:Hq + Hkv], x[t0:t1, Hq + Hkv:], pos[t0:t1], tab,
+                              kvec.PagedCache(k, v, table.cuda(), held, weights), cu.int().cuda(), q_norm=w[0], k_norm=w[1],
+                              q_out=q[t0:t1])
+        got.append((q, k, v, weights))
+    for a, b in zip(*got):
+        assert torch.equal(a, b)
+    rows = f64(tab)[pos[:50].cpu().numpy()]
+    check_rows(got[0][0][:50], serving.rotate(f64(x[:50, :Hq]), f64(w[0]), 1e-6, rows, False), dtype, "q")
