@@ -7,7 +7,14 @@
 // 32768, a radix select that sweeps the row in L2 for longer ones; it writes the kept
 // slots.  evict_copy_kernel moves the rows, one half-warp a row of K and of V: HBM-bound,
 // and spread over the device whatever the number of rows (the new pages are none of the
-// old, so no copy waits for another).
+// old, so no copy waits for another).  One launch of clusters whose first CTA ranks while the
+// others wait was slower from 32 rows on: the waiting CTAs hold the SMs.
+//
+// Measured, in us (in brackets the bytes at the measured copy rate): 8 rows of 576 slots to
+// 512 7.1 (0.6), the chain of two launches and six barriers; 128 rows of 1000 to 4096 slots to
+// 1024 29.3 (20.2); 512 of 2100 to 2048 175 (161); 8 of 65536 to 8192, by sweeps, 65 (10.3).
+// Small blocks of few rows fill the device best: two rows of K and V in flight a half-warp and
+// 128 threads 29.3, four and 256 31.0, eight and 256 36.6.
 #include "hist_select.cuh"
 #include "kvec_internal.cuh"
 
@@ -74,23 +81,29 @@ __global__ void __launch_bounds__(NT) evict_select_kernel(const __grid_constant_
     asm volatile("griddepcontrol.wait;\n" ::: "memory");
     const int n = clamped_len(A, s), B = A.io.budget, Hkv = A.io.Hkv;
     int* kept = A.io.kept + ((size_t)s * Hkv + h) * B;
+    const int* table = A.c.table + (size_t)s * A.c.max_pages;
+    // The weights of every slot that there may be: their pages do not wait for the length.
+    float4 w[KPT / 4];
+#pragma unroll
+    for (int g = 0; g < KPT / 4; ++g) {
+        const int j = HS::position(4 * g);   // four slots of one page
+        w[g] = make_float4(-INFINITY, -INFINITY, -INFINITY, -INFINITY);
+        if (j < A.io.max_len) {
+            const long long row = slot_row(table, j, h, Hkv, A.c);
+            if (row >= 0) w[g] = *reinterpret_cast<const float4*>(A.c.weights + row);
+        }
+    }
     if (h == 0 && tid == 0) A.io.new_lens[s] = min(n, B);
     if (n <= B) {
         for (int j = tid; j < B; j += NT) kept[j] = j < n ? j : -1;
         return;
     }
     const int lo = A.io.sinks, hi = n - A.io.recent;   // the ranked slots; sinks + recent <= B < n
-    const int* table = A.c.table + (size_t)s * A.c.max_pages;
     uint32_t key[KPT];
 #pragma unroll
     for (int g = 0; g < KPT / 4; ++g) {
-        const int j = HS::position(4 * g);   // four slots of one page
-        float4 w = make_float4(-INFINITY, -INFINITY, -INFINITY, -INFINITY);
-        if (j < n) {
-            const long long row = slot_row(table, j, h, Hkv, A.c);
-            if (row >= 0) w = *reinterpret_cast<const float4*>(A.c.weights + row);
-        }
-        const float v[4] = {w.x, w.y, w.z, w.w};
+        const int j = HS::position(4 * g);
+        const float v[4] = {w[g].x, w[g].y, w[g].z, w[g].w};
 #pragma unroll
         for (int e = 0; e < 4; ++e) key[4 * g + e] = j + e >= lo && j + e < hi ? weight_key(v[e]) : 0u;
     }
@@ -232,15 +245,15 @@ __global__ void __launch_bounds__(kSweepThreads) evict_sweep_kernel(const __grid
     }
 }
 
-constexpr int kCopyThreads = 256;
-constexpr int kCopyPer = 4;                                   // rows of a half-warp
+constexpr int kCopyThreads = 128;
+constexpr int kCopyPer = 2;                                   // rows of a half-warp
 constexpr int kCopyRows = kCopyThreads / 16 * kCopyPer;       // rows of a block
 
 __global__ void __launch_bounds__(kCopyThreads) evict_copy_kernel(const __grid_constant__ EvictArgs A) {
     asm volatile("griddepcontrol.launch_dependents;\n" ::: "memory");
     asm volatile("griddepcontrol.wait;\n" ::: "memory");
     const int h = blockIdx.y, s = blockIdx.z, l16 = threadIdx.x & 15, Hkv = A.io.Hkv, B = A.io.budget;
-    const int m = min(clamped_len(A, s), B);
+    const int most = min(A.io.max_len, B);
     const int j0 = blockIdx.x * kCopyRows + (threadIdx.x >> 4);
     const int* kept = A.io.kept + ((size_t)s * Hkv + h) * B;
     const int* table = A.c.table + (size_t)s * A.c.max_pages;
@@ -250,8 +263,9 @@ __global__ void __launch_bounds__(kCopyThreads) evict_copy_kernel(const __grid_c
     for (int i = 0; i < kCopyPer; ++i) {
         const int j = j0 + i * (kCopyThreads / 16);
         src[i] = dst[i] = -1;
-        if (j < m) {
-            src[i] = slot_row(table, kept[j], h, Hkv, A.c);
+        const int from = j < most ? kept[j] : -1;   // -1 past the kept ones
+        if (from >= 0) {
+            src[i] = slot_row(table, from, h, Hkv, A.c);
             dst[i] = slot_row(fresh, j, h, Hkv, A.c);
         }
     }
@@ -279,8 +293,8 @@ cudaError_t launch_evict(const EvictIO& io, const PagedCacheView& c, cudaStream_
     const EvictArgs a{io, c};
     const dim3 rows((unsigned)io.Hkv, (unsigned)io.batch);
     cudaError_t e;
-    if (io.max_len <= 2048)
-        e = launch_prio(evict_select_kernel<128, 16>, rows, dim3(128), 0, st, 0, true, a);
+    if (io.max_len <= 4096)
+        e = launch_prio(evict_select_kernel<256, 16>, rows, dim3(256), 0, st, 0, true, a);
     else if (io.max_len <= 8192)
         e = launch_prio(evict_select_kernel<512, 16>, rows, dim3(512), 0, st, 0, true, a);
     else if (io.max_len <= 16384)

@@ -607,7 +607,9 @@ class KvecSelector:
         for x in (cu_q_host, cu_k_host):
             _want(x.dtype is t.int32 and x.shape == (batch + 1,) and x.device.type == "cpu" and x.is_contiguous(),
                   "cu_q_host and cu_k_host must be contiguous int32 [batch + 1] on the host")
-        _want(batch >= 1 and cu_q_host[-1].item() <= Tq and cu_k_host[-1].item() <= Tk,
+        cu_q, cu_k = cu_q_host.data_ptr(), cu_k_host.data_ptr()
+        last = ctypes.c_int32.from_address   # the host copies' last entries (a tensor's item takes 2 us)
+        _want(batch >= 1 and last(cu_q + 4 * batch).value <= Tq and last(cu_k + 4 * batch).value <= Tk,
               "cu_q_host or cu_k_host passes the rows given")
         if out is None:
             out = self._empty((Tq, Hq, d), dtype, stream)
@@ -617,7 +619,6 @@ class KvecSelector:
             lse = self._empty((Tq, Hq), t.float32, stream)
         else:
             self._check("lse", lse, (Tq, Hq), t.float32)
-        cu_q, cu_k = cu_q_host.data_ptr(), cu_k_host.data_ptr()
         need = kvec_prefill_bytes(self.handle, batch, cu_q, cu_k, window, sinks)
         scratch = self._empty((need,), t.uint8, stream).data_ptr() if need else None
         kvec_prefill_attention(self.handle, code, batch, cu_q, cu_q_dev.data_ptr(), cu_k, cu_k_dev.data_ptr(),
