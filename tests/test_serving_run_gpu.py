@@ -1,0 +1,165 @@
+"""The operators of a serving loop run together, as they would be used: a ragged prompt through rotation, prefill
+attention and the eviction that takes its log-sum-exp, the kept rows into pages, then decoding steps with
+rotation, store, attention and eviction by accumulated weight, on eager calls and from a captured graph.
+
+Every step is compared with its definition in fp64 on the state that the GPU has (keys as stored, weights as
+accumulated), with the tolerances of the operators' own tests.
+"""
+import numpy as np
+import pytest
+import torch
+
+from oracle import serving
+from paper_2606_29563_gb300 import kvec
+import test_paged_gpu as paged
+import test_prefill_gpu as prefill
+
+pytestmark = pytest.mark.gpu
+D, HQ, HKV, PAGE = 128, 16, 4, 32
+
+
+@pytest.fixture(scope="module", autouse=True)
+def _built():
+    if not torch.cuda.is_available():
+        pytest.skip("needs a CUDA GPU")
+    from paper_2606_29563_gb300 import build as kbuild
+    kbuild.build()
+
+
+def selector():
+    return kvec.KvecSelector(kvec.make_params(HQ, HKV, num_ext_heads=1, max_batch=4, max_seqlen=1024, max_layers=4))
+
+
+def test_prompt_eviction_and_decoding():
+    dtype, lens, budget, w = torch.bfloat16, [700, 333, 90], 128, 32
+    gen = torch.Generator().manual_seed(77)
+    sel = selector()
+    T, cu = sum(lens), prefill.cu_of(lens)
+    cu_host, cu_dev = cu.pin_memory(), cu.cuda()
+    tab = paged.rot_table(900, D).cuda()
+    norms = [(torch.randn(D, generator=gen) * 0.2 + 1).to(dtype).cuda() for _ in range(2)]
+    qkv = torch.randn((T, HQ + 2 * HKV, D), generator=gen).to(dtype).cuda()
+    pos = torch.cat([torch.arange(n) for n in lens]).int()
+    v = qkv[:, HQ + HKV:].contiguous()
+    q, k = sel.rotate_append(qkv[:, :HQ], qkv[:, HQ:HQ + HKV], None, pos.cuda(), tab, cu_tokens=cu_dev, q_norm=norms[0], k_norm=norms[1])
+    rows = paged.f64(tab)[pos.numpy()]
+    paged.check_rows(q, serving.rotate(paged.f64(qkv[:, :HQ]), paged.f64(norms[0]), 1e-6, rows, False), dtype, "q")
+    paged.check_rows(k, serving.rotate(paged.f64(qkv[:, HQ:HQ + HKV]), paged.f64(norms[1]), 1e-6, rows, False), dtype, "k")
+    out, lse = sel.prefill_attention(q, k, v, cu_host, cu_dev)
+    ref, rl, mass = prefill.reference(q, k, v, lens, lens, 0, 0, D ** -0.5)
+    u = 2.0 ** -8
+    assert torch.all((out.double() - ref).abs() <= u * ref.abs() + (u + 2e-5) * mass)
+    assert torch.all((lse.double() - rl).abs() <= 2e-5 + 2.0 ** -22 * rl.abs())
+
+    # The eviction with the prefill's log-sum-exp scores as the one that forms it itself.
+    ends = np.cumsum(lens)
+    q_obs = torch.stack([q[e - w:e] for e in ends])
+    lse_obs = torch.stack([lse[e - w:e] for e in ends])
+    got = []
+    for given in (None, lse_obs):
+        state = sel.new_state(3)
+        idx, kk, vv = sel.select_layer(cu_host, cu_dev, q_obs, k, v, state, budget, lse=given)
+        kvec.kvec_sync_status(sel.handle)
+        got.append((idx.cpu().numpy(), kk, vv, sel.debug()["P_O"].cpu().numpy()))
+    for s, n in enumerate(lens):
+        if n > budget:
+            a, b = got[0][3][s, :, :n - w], got[1][3][s, :, :n - w]
+            assert np.abs(a - b).max() <= 2e-3 * (np.abs(a) + a.mean()).max()
+    idx, kept_k, kept_v = got[1][:3]
+    held = [min(n, budget) for n in lens]
+    for s, n in enumerate(lens):
+        base = ends[s] - n
+        for h in range(HKV):
+            j = torch.from_numpy(idx[s, h, :held[s]]).long().cuda()
+            assert torch.equal(kept_k[s, h, :held[s]], k[base + j, h]) and torch.equal(kept_v[s, h, :held[s]], v[base + j, h])
+
+    # Pages for the kept rows and 40 decoded tokens, and as many for the cache after each eviction.
+    per = -(-(budget + 40) // PAGE)
+    pool = torch.randperm(6 * per, generator=gen).to(torch.int32)
+    tables = [pool[:3 * per].view(3, per).contiguous().cuda(), pool[3 * per:].view(3, per).contiguous().cuda()]
+    pages = [torch.full((6 * per, HKV, PAGE, D), float("nan"), dtype=dtype, device="cuda") for _ in range(2)]
+    weights = torch.zeros((6 * per, HKV, PAGE), device="cuda")
+    for s in range(3):
+        for j in range(held[s]):
+            at = int(tables[0][s, j // PAGE])
+            pages[0][at, :, j % PAGE], pages[1][at, :, j % PAGE] = kept_k[s, :, j], kept_v[s, :, j]
+    seq = torch.tensor(held, dtype=torch.int32).cuda()
+    positions = torch.tensor(lens, dtype=torch.int32).cuda()
+    one = torch.ones(3, dtype=torch.int32).cuda()
+    cache = kvec.PagedCache(pages[0], pages[1], tables[0], seq, weights)
+    static = torch.zeros((3, HQ + 2 * HKV, D), dtype=dtype, device="cuda")
+
+    def step():
+        seq.add_(one)
+        qq = sel.rotate_append(static[:, :HQ], static[:, HQ:HQ + HKV], static[:, HQ + HKV:], positions, tab, cache,
+                               q_norm=norms[0], k_norm=norms[1])
+        positions.add_(one)
+        return qq, sel.paged_decode(qq, cache, window=0)
+
+    graph, which = None, 0
+    for i in range(36):
+        static.copy_(torch.randn(static.shape, generator=gen).to(dtype))
+        before = weights.cpu().double().numpy()
+        if i in (5, 21):
+            graph = torch.cuda.CUDAGraph()
+            torch.cuda.synchronize()
+            with torch.cuda.graph(graph):
+                qq, out = step()
+        if graph is None:
+            qq, out = step()
+        else:
+            graph.replay()
+        torch.cuda.synchronize()
+        n = seq.tolist()
+        rows = paged.f64(tab)[positions.cpu().numpy() - 1]
+        paged.check_rows(qq, serving.rotate(paged.f64(static[:, :HQ]), paged.f64(norms[0]), 1e-6, rows, False), dtype, "q")
+        new_k = serving.rotate(paged.f64(static[:, HQ:HQ + HKV]), paged.f64(norms[1]), 1e-6, rows, False)
+        kp, vp = paged.f64(pages[0]), paged.f64(pages[1])
+        for s in range(3):
+            at = serving.place(tables[which][s].tolist(), n[s] - 1, PAGE, 6 * per)
+            paged.check_rows(torch.from_numpy(kp[at[0], :, at[1]]), new_k[s], dtype, "stored key")
+            assert np.array_equal(vp[at[0], :, at[1]], paged.f64(static[s, HQ + HKV:]))
+            before[at[0], :, at[1]] = 0.0
+        grown = before.copy()
+        ref = serving.paged_decode(paged.f64(qq), kp, vp, grown, tables[which].cpu().numpy(), n, per * PAGE, 0, 0, D ** -0.5)
+        assert np.all(np.abs(paged.f64(out) - ref) <= u * np.abs(ref) + (u * u + 2e-5) * 8.0)
+        got_w = weights.cpu().double().numpy()
+        assert np.all(np.abs(got_w - grown) <= 2e-5 * (grown - before) + 2.0 ** -24 * np.abs(grown) + 1e-9)
+        if i % 16 == 15:   # back to the budget, into the other pages
+            kp, vp, wp = paged.f64(pages[0]), paged.f64(pages[1]), got_w.copy()
+            rl, rk = serving.evict(kp, vp, wp, tables[which].cpu().numpy(), n, tables[1 - which].cpu().numpy(), per * PAGE, budget, 4, 16)
+            nl, kept = sel.paged_evict(cache, tables[1 - which], budget, sinks=4, recent=16)
+            torch.cuda.synchronize()
+            assert np.array_equal(nl.cpu().numpy(), rl) and np.array_equal(kept.cpu().numpy(), rk)
+            assert np.array_equal(paged.f64(pages[0]), kp, equal_nan=True) and np.array_equal(weights.cpu().double().numpy(), wp)
+            which = 1 - which
+            seq.copy_(nl)
+            cache = kvec.PagedCache(pages[0], pages[1], tables[which], seq, weights)
+            graph = None
+    sel.close()
+
+
+def test_streaming_with_first_slots_and_a_window():
+    # Chunks of a prompt under a window with four first tokens in sight, then steps over the pages that
+    # hold the last of them: the same rows by both attentions.
+    dtype, n, window, sinks = torch.float16, 300, 100, 4
+    gen = torch.Generator().manual_seed(5)
+    sel = selector()
+    q, k, v = (torch.randn((n, h, D), generator=gen).to(dtype).cuda() for h in (HQ, HKV, HKV))
+    cu = prefill.cu_of([n])
+    whole, _ = sel.prefill_attention(q, k, v, cu, cu.cuda(), window=window, sinks=sinks)
+    for a, b in ((0, 129), (129, 131), (131, 300)):
+        cq, ck = prefill.cu_of([b - a]), prefill.cu_of([b])
+        part, _ = sel.prefill_attention(q[a:b], k[:b], v[:b], cq, cq.cuda(), ck, ck.cuda(), window=window, sinks=sinks)
+        # The same blocks in the same order, but other tiles: each within its tolerance of the same value.
+        assert torch.all((part - whole[a:b]).abs().float() <= 3 * 2.0 ** -11 * whole[a:b].abs().float() + 2e-3)
+    per = -(-n // 64)
+    pages = [torch.zeros((per, HKV, 64, D), dtype=dtype, device="cuda") for _ in range(2)]
+    for x, p in ((k, pages[0]), (v, pages[1])):
+        p.copy_(torch.nn.functional.pad(x, (0, 0, 0, 0, 0, per * 64 - n)).view(per, 64, HKV, D).transpose(1, 2))
+    table = torch.arange(per, dtype=torch.int32)[None].cuda()
+    for m in (300, 150, 101, 100, 5, 1):
+        cache = kvec.PagedCache(pages[0], pages[1], table, torch.tensor([m], dtype=torch.int32).cuda())
+        row = sel.paged_decode(q[m - 1:m].contiguous(), cache, window=window, sinks=sinks)
+        assert torch.all((row - whole[m - 1:m]).abs().float() <= 3 * 2.0 ** -11 * whole[m - 1:m].abs().float() + 2e-3)
+    sel.close()
