@@ -315,7 +315,8 @@ typedef struct {
  * its lens already counts them, and token t of cu_tokens[s] <= t < cu_tokens[s + 1] goes to
  * slot lens[s] - (cu_tokens[s + 1] - t).  The slot's accumulated weight becomes 0.
  * cu_tokens is device int32 [batch + 1], ascending from 0 (NULL: token t is sequence t's
- * only new one, batch = T); tokens from cu_tokens[batch] on are padding.  A slot below 0 or past the
+ * only new one, batch = T; without a cache every token counts and batch is not looked at);
+ * tokens from cu_tokens[batch] on are padding.  A slot below 0 or past the
  * sequence's capacity is not stored.  v may be NULL without a cache.
  * No two tokens may share a slot.  0 <= T; T = 0 does nothing. */
 typedef struct {
@@ -448,7 +449,8 @@ KVEC_API kvec_status kvec_kernel_time(kvec_handle* h, int kernel, double* total_
  * and that call's outputs are invalid.  fault = 2 makes one epilogue warp of
  * every score CTA report that its wait for work gave up, at once, and one of every
  * general window kernel's CTA that its wait for a buffer did (at its third unit); the
- * rest is the same.  fault = 3 makes kvec_create treat every allocation but the one
+ * rest is the same.  fault = 4 makes kvec_prefill_attention signal none of its logits and
+ * kvec_paged_decode leave out one warp's copies: their waits give up after about 0.2 s.  fault = 3 makes kvec_create treat every allocation but the one
  * of the shortest rings as failed.  fault = 0 (the default) switches it off.  Process-wide; while it is set,
  * multi-layer calls are neither captured into nor replayed from the handle's
  * graph cache. */

@@ -1213,6 +1213,9 @@ kvec_status check_window(int window, int sinks) {
     return KVEC_OK;
 }
 
+// Of sequences of up to kPagedMaxLen slots a longer window hides none and more first slots are all.
+int within_length(int n) { return std::min(n, kPagedMaxLen); }
+
 float softmax_scale_of(const kvec_params& p) {
     return p.softmax_scale > 0.f ? p.softmax_scale : (float)(1.0 / sqrt((double)p.head_dim));
 }
@@ -1241,10 +1244,14 @@ kvec_status kvec_rotate_append(kvec_handle* h, const kvec_rotate_args* a, int ba
         return fail(KVEC_ERR_INVALID_ARG, "a rotation needs rot_table and max_positions >= 1");
     if (!stride_ok(a->q_stride) || !stride_ok(a->k_stride) || !stride_ok(a->v_stride))
         return fail(KVEC_ERR_INVALID_ARG, "strides must be non-negative multiples of 8 elements");
-    kvec_status s = check_paged_handle(h, batch, cache ? &v : nullptr);
+    // Without a cache and cu_tokens there are no sequences to speak of.
+    const bool sequences = cache || cu_tokens;
+    kvec_status s = sequences ? check_paged_handle(h, batch, cache ? &v : nullptr)
+                    : h       ? KVEC_OK
+                              : fail(KVEC_ERR_INVALID_ARG, "handle is NULL");
     if (s != KVEC_OK) return s;
     if (a->num_tokens == 0) return KVEC_OK;
-    if (!cu_tokens && a->num_tokens != batch)
+    if (cache && !cu_tokens && a->num_tokens != batch)
         return fail(KVEC_ERR_INVALID_ARG, "without cu_tokens every sequence has one token: num_tokens %d, batch %d",
                     a->num_tokens, batch);
     if (!a->q || !a->k || !a->positions || !a->q_out || (cache && !a->v) || (!cache && !a->k_out))
@@ -1276,7 +1283,7 @@ kvec_status kvec_rotate_append(kvec_handle* h, const kvec_rotate_args* a, int ba
     io.eps = a->eps;
     io.dtype = a->dtype;
     io.num_tokens = a->num_tokens;
-    io.batch = batch;
+    io.batch = sequences ? batch : a->num_tokens;
     io.Hq = p.num_q_heads;
     io.Hkv = p.num_kv_heads;
     io.rot_dim = a->rot_dim;
@@ -1324,8 +1331,8 @@ kvec_status kvec_paged_decode(kvec_handle* h, int batch, const void* q, const kv
     io.Hq = h->p.num_q_heads;
     io.Hkv = h->p.num_kv_heads;
     io.max_len = max_len;
-    io.window = window;
-    io.sinks = sinks;
+    io.window = within_length(window);
+    io.sinks = within_length(sinks);
     io.scale = softmax_scale_of(h->p);
     int prev = 0;
     s = set_device(h, &prev);
@@ -1404,7 +1411,8 @@ kvec_status check_prefill(int batch, const int32_t* cu_q, const int32_t* cu_k, i
 size_t kvec_prefill_bytes(kvec_handle* h, int batch, const int32_t* cu_q_host, const int32_t* cu_k_host, int window, int sinks) {
     int max_q = 0, max_k = 0;
     if (check_prefill(batch, cu_q_host, cu_k_host, window, sinks, &max_q, &max_k) != KVEC_OK || !h || h->g > 8) return 0;
-    return plan_prefill(batch, h->p.num_q_heads, h->p.num_kv_heads, max_q, max_k, window, sinks, h->num_sms).scratch;
+    return plan_prefill(batch, h->p.num_q_heads, h->p.num_kv_heads, max_q, max_k, within_length(window), within_length(sinks),
+                        h->num_sms).scratch;
 }
 
 kvec_status kvec_prefill_attention(kvec_handle* h, int dtype, int batch, const int32_t* cu_q_host,
@@ -1423,7 +1431,8 @@ kvec_status kvec_prefill_attention(kvec_handle* h, int dtype, int batch, const i
         return fail(KVEC_ERR_UNSUPPORTED, "prefill attention supports up to 8 query heads per KV head (g = %d)", h->g);
     if (max_q == 0) return KVEC_OK;
     const int total_k = cu_k_host[batch];
-    const PrefillPlan plan = plan_prefill(batch, h->p.num_q_heads, h->p.num_kv_heads, max_q, max_k, window, sinks, h->num_sms);
+    const PrefillPlan plan = plan_prefill(batch, h->p.num_q_heads, h->p.num_kv_heads, max_q, max_k, within_length(window),
+                                          within_length(sinks), h->num_sms);
     if (!q || !out || (total_k > 0 && (!k || !v)) || (plan.scratch && !scratch))
         return fail(KVEC_ERR_INVALID_ARG, "a device pointer is NULL");
     if (scratch_bytes < plan.scratch)
@@ -1449,8 +1458,8 @@ kvec_status kvec_prefill_attention(kvec_handle* h, int dtype, int batch, const i
     io.total_q = cu_q_host[batch];
     io.total_k = total_k;
     io.scratch = scratch;
-    io.window = window;
-    io.sinks = sinks;
+    io.window = within_length(window);
+    io.sinks = within_length(sinks);
     io.scale = softmax_scale_of(h->p);
     int prev = 0;
     s = set_device(h, &prev);
@@ -1495,7 +1504,7 @@ kvec_status kvec_sync_status(kvec_handle* h) {
     return KVEC_OK;
 }
 
-void kvec_set_test_fault(int fault) { g_test_fault.store(fault >= 1 && fault <= 3 ? fault : 0, std::memory_order_relaxed); }
+void kvec_set_test_fault(int fault) { g_test_fault.store(fault >= 1 && fault <= 4 ? fault : 0, std::memory_order_relaxed); }
 
 kvec_status kvec_set_profiling(kvec_handle* h, int enable) {
     if (!h) return fail(KVEC_ERR_INVALID_ARG, "handle is NULL");

@@ -60,6 +60,7 @@ struct PdArgs {
     int nbmax;                // most visible blocks of a pair
     int g;
     float sl2;                // scale * log2(e)
+    int fault;                // test of the error path (kvec_set_test_fault): warp 0 of CTA 0 loads nothing
 };
 
 // A sequence's visible slots and the blocks that hold them: blocks 0 .. first - 1, then
@@ -312,7 +313,7 @@ __global__ void __launch_bounds__(kPdThreads, kPdCtasPerSm) paged_decode_kernel(
             const int row = ptx::warp_uniform(rows[0]), at = ptx::warp_uniform(ld_stage);
             if (ptx::elect_one()) {
                 srow[warp][at] = row;
-                if (row >= 0) {
+                if (row >= 0 && !(A.fault && warp == 0 && blockIdx.x == 0)) {
                     uint8_t* dst = ring + at * kPdStage;
                     uint64_t* bar = &full[warp][at];
                     ptx::mbar_arrive_expect_tx(bar, kPdStage);
@@ -736,6 +737,7 @@ cudaError_t launch_paged_decode(const PagedDecodeIO& io, const PagedCacheView& c
     a.io = io;
     a.g = io.Hq / io.Hkv;
     a.sl2 = io.scale * 1.4426950408889634f;
+    a.fault = test_fault() == 4 ? 1 : 0;
     a.ctas = share_ctas(num_sms);
     a.nbmax = visible_blocks(io);
     const size_t slots = (size_t)a.ctas * 2 * kPdHeads;

@@ -63,6 +63,7 @@ struct PfArgs {
     float2* part_ml; // [items][2][128] (m, l) of the rows
     Divisor by_per, by_heads;   // batch * Hkv, Hkv
     float sl2;
+    int fault;       // test of the error path (kvec_set_test_fault): no S is signalled
 };
 
 struct __align__(8) PfBarriers {
@@ -341,7 +342,7 @@ __global__ void __launch_bounds__(kPfThreads, 1) prefill_kernel(const __grid_con
                         const uint32_t ofs = (kk >> 2) * (kPfHalf >> 4) + (kk & 3) * 2;
                         ptx::mma_bf16(tmem + t * 128, qd + ofs, kd + ofs, idesc_s, kk > 0 ? 1u : 0u);
                     }
-                    ptx::mma_commit(&bars->s_full[t]);
+                    if (!A.fault) ptx::mma_commit(&bars->s_full[t]);   // (withheld for a test of the waits)
                     if (last) ptx::mma_commit(&bars->empty[st]);
                 }
                 __syncwarp();
@@ -539,12 +540,12 @@ __global__ void __launch_bounds__(kPfThreads, 1) prefill_kernel(const __grid_con
 #pragma unroll
                 for (int c = 0; c < 2; ++c) {
                     float z = weights(s + c * 64);
-                    if (__any_sync(0xffffffffu, !(z < kMostWeight))) {
+                    if (__any_sync(0xffffffffu, live && !(z < kMostWeight))) {
                         // The row's first logits, or ones far above m (or NaN): m moves to the largest.
                         float mx = m;
 #pragma unroll
                         for (int e = 0; e < 64; e += 2) mx = max3(mx, s[c * 64 + e] * sl2f, s[c * 64 + e + 1] * sl2f);
-                        if (z < kMostWeight) mx = m;
+                        if (z < kMostWeight || !live) mx = m;
                         const float f = ptx::ex2(m - mx);
                         l *= f;
                         m = mx;
@@ -736,6 +737,7 @@ cudaError_t launch_prefill(const PrefillIO& io, const PrefillPlan& plan, int num
     a.by_per.set(io.batch * io.Hkv);
     a.by_heads.set(io.Hkv);
     a.sl2 = io.scale * 1.4426950408889634f;
+    a.fault = test_fault() == 4 ? 1 : 0;
     const uint64_t row = (uint64_t)kHeadDim * 2;
     const uint64_t qd[3] = {(uint64_t)kHeadDim, (uint64_t)io.Hq, (uint64_t)io.total_q}, qs[2] = {row, row * io.Hq};
     const uint32_t qb[3] = {64, (uint32_t)a.g, (uint32_t)a.nq};

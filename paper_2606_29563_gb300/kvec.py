@@ -227,7 +227,7 @@ def kvec_output_capacity(params: kvec_params, budget: int) -> int:
 def kvec_set_test_fault(fault: int) -> None:
     """Test hook of the error path (1: window kernels give up on a withheld accumulator;
     2: a warp of the score and general window kernels gives up on a wait; 3: kvec_create's larger
-    allocations fail; 0: off)."""
+    allocations fail; 4: prefill attention and paged decode wait for what does not come; 0: off)."""
     load().kvec_set_test_fault(int(fault))
 
 

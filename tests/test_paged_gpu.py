@@ -468,3 +468,23 @@ def test_rotate_append_on_both_sides_of_the_layout_rule(Hq, Hkv, T):
         assert torch.equal(a, b)
     rows = f64(tab)[pos[:50].cpu().numpy()]
     check_rows(got[0][0][:50], serving.rotate(f64(x[:50, :Hq]), f64(w[0]), 1e-6, rows, False), dtype, "q")
+
+
+def test_windows_and_first_slots_of_any_size():
+    gen = torch.Generator().manual_seed(6)
+    cache, _ = make_cache([77, 3000], 2, 16, torch.bfloat16, gen, weights=False)
+    q = torch.randn((2, 4, D), generator=gen).to(torch.bfloat16).cuda()
+    sel, most = selector(4, 2), 2 ** 31 - 1
+    whole = sel.paged_decode(q, cache)
+    for window, sinks in ((most, 0), (most, most), (1, most), (2 ** 20, 5)):
+        assert torch.equal(sel.paged_decode(q, cache, window=window, sinks=sinks), whole)
+
+
+def test_rotation_without_sequences_takes_any_number_of_tokens():
+    gen = torch.Generator().manual_seed(8)
+    q, k = (torch.randn((1000, h, D), generator=gen).to(torch.float16).cuda() for h in (4, 2))
+    pos, tab = torch.arange(1000, dtype=torch.int32).cuda(), rot_table(1000, 128).cuda()
+    got = selector(4, 2).rotate_append(q, k, None, pos, tab)
+    cu = torch.tensor([0, 1000], dtype=torch.int32).cuda()
+    want = selector(4, 2).rotate_append(q, k, None, pos, tab, cu_tokens=cu)
+    assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])

@@ -247,3 +247,27 @@ def test_few_rows_on_many_keys(dtype, Hq, Hkv, q_lens, k_lens, window, sinks):
     check(q, k, v, q_lens, k_lens, window, sinks)
     v[k_lens[0] - 1, 0, 3], v[k_lens[0] - min(k_lens[0], 2), 0, 77] = float("nan"), float("inf")
     check(q, k, v, q_lens, k_lens, window, sinks)
+
+
+def test_windows_and_first_tokens_of_any_size():
+    q, k, v = tensors([90], [700], 8, 2, torch.bfloat16, 40)
+    cq, ck = cu_of([90]), cu_of([700])
+    run = lambda w, s: selector(8, 2).prefill_attention(q, k, v, cq, cq.cuda(), ck, ck.cuda(), window=w, sinks=s)
+    whole, most = run(0, 0), 2 ** 31 - 1
+    for window, sinks in ((most, 0), (most, most), (2 ** 20, 7)):
+        got = run(window, sinks)
+        assert torch.equal(got[0], whole[0]) and torch.equal(got[1], whole[1])
+    got = run(1, most)   # every key by the first tokens' rule: other blocks are looked at, the same rows come out
+    assert (got[1] - whole[1]).abs().max() <= 4e-5 and torch.all((got[0] - whole[0]).abs().float() <= 0.02)
+
+
+def test_rows_that_fill_no_tile_do_not_matter():
+    # Seven heads leave two of a tile's 128 rows unused; what shared memory holds there is not the call's.
+    q, k, v = tensors([200], [600], 7, 1, torch.bfloat16, 41)
+    big = [torch.full((400, 8, D), float("nan"), dtype=torch.bfloat16, device="cuda") for _ in range(3)]
+    cu8, cu = cu_of([400]), cu_of([200])
+    ck = cu_of([600])
+    want = selector(7, 1).prefill_attention(q, k, v, cu, cu.cuda(), ck, ck.cuda())
+    selector(8, 8).prefill_attention(*big, cu8, cu8.cuda())      # leaves NaN in shared memory
+    got = selector(7, 1).prefill_attention(q, k, v, cu, cu.cuda(), ck, ck.cuda())
+    assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])

@@ -163,3 +163,113 @@ def test_streaming_with_first_slots_and_a_window():
         row = sel.paged_decode(q[m - 1:m].contiguous(), cache, window=window, sinks=sinks)
         assert torch.all((row - whole[m - 1:m]).abs().float() <= 3 * 2.0 ** -11 * whole[m - 1:m].abs().float() + 2e-3)
     sel.close()
+
+
+# Kernels are programmatic dependents of what precedes them on the stream; in a caller's captured graph that
+# may be a copy, a fill or another stream's kernel, whose results they must still see.
+@pytest.mark.parametrize("before", ["copy", "fill", "other stream"])
+@pytest.mark.parametrize("call", ["rotate", "decode", "long decode", "evict", "prefill", "divided prefill"])
+def test_captured_calls_see_the_work_before_them(before, call):
+    gen = torch.Generator(device="cuda").manual_seed(3)
+    rand = lambda shape, dt=torch.bfloat16: torch.randn(shape, generator=gen, device="cuda").to(dt)
+    sel = selector()
+    n = {"decode": 300, "long decode": 20000, "evict": 4000}.get(call, 900)
+    per = -(-n // 64)
+    pool = (2 * per, HKV, 64, D)
+    table = torch.arange(per, dtype=torch.int32)[None].cuda()
+    lens, lens_src = torch.zeros(1, dtype=torch.int32).cuda(), torch.tensor([n], dtype=torch.int32).cuda()
+    outs = []
+    if call in ("decode", "long decode", "evict"):
+        a, b, w = torch.zeros(pool, dtype=torch.bfloat16, device="cuda"), rand(pool), torch.zeros(pool[:3], device="cuda")
+        srcs = [rand(pool), rand(pool[:3], torch.float32).abs()]
+        fills = [a, w]
+        cache = kvec.PagedCache(a, b, table, lens, w)
+        q = rand((1, HQ, D))
+        if call == "evict":
+            fresh = (table + per).contiguous()
+            run = lambda: (*sel.paged_evict(cache, fresh, 1000, sinks=2, recent=9), a, b, w)
+        else:
+            run = lambda: (sel.paged_decode(q, cache), w)
+    else:
+        few = call == "divided prefill"
+        rows = 20 if few else n
+        a, k, v = torch.zeros((rows, HQ, D), dtype=torch.bfloat16, device="cuda"), rand((n, HKV, D)), rand((n, HKV, D))
+        srcs, fills = [rand((rows, HQ, D))], [a]
+        cq, ck = prefill.cu_of([rows]), prefill.cu_of([n])
+        dq, dk = cq.cuda(), ck.cuda()
+        pos, tab = torch.arange(n, dtype=torch.int32).cuda(), paged.rot_table(n, D).cuda()
+        cache = kvec.PagedCache(rand(pool), rand(pool), table, lens)
+        if call == "rotate":
+            run = lambda: (sel.rotate_append(a, k, v, pos, tab, cache, dq), cache.k_pages[:per - 1], cache.v_pages[:per - 1])
+        else:
+            run = lambda: sel.prefill_attention(a, k, v, cq, dq, ck, dk)
+    side, main = torch.cuda.Stream(), torch.cuda.Stream()
+
+    def work():
+        if before == "copy":
+            for f, s in zip(fills, srcs):
+                f.copy_(s)
+            lens.copy_(lens_src)
+        elif before == "fill":
+            for f, s in zip(fills, srcs):
+                f.copy_(s)
+            lens.copy_(lens_src)
+            fills[0].zero_()
+        else:
+            side.wait_stream(torch.cuda.current_stream())
+            with torch.cuda.stream(side):
+                for f, s in zip(fills, srcs):
+                    torch.add(s, 1.0, out=f)
+                torch.add(lens_src, 0, out=lens)
+            torch.cuda.current_stream().wait_stream(side)
+        return run()
+
+    with torch.cuda.stream(main):
+        work()
+        torch.cuda.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=main):
+            got = work()
+        for _ in range(3):
+            for s in srcs:
+                s.copy_(torch.randn(s.shape, generator=gen, device="cuda").abs().to(s.dtype))
+            want = [x.clone() for x in work()]
+            torch.cuda.synchronize()
+            for f in fills:
+                f.fill_(0.5)
+            lens.fill_(n // 2)
+            graph.replay()
+            torch.cuda.synchronize()
+            for x, y in zip(want, got):
+                assert torch.equal(x, y)
+    sel.close()
+
+
+@pytest.mark.parametrize("call", ["decode", "long decode", "prefill", "divided prefill"])
+def test_a_wait_that_runs_out_is_reported_and_the_handle_recovers(call):
+    gen = torch.Generator().manual_seed(4)
+    sel = selector()
+    if "decode" in call:
+        lens = [100 if call == "decode" else 20000]
+        cache, _ = paged.make_cache(lens, HKV, 64, torch.bfloat16, gen, weights=False)
+        q = torch.randn((1, HQ, D), generator=gen).to(torch.bfloat16).cuda()
+        run = lambda: sel.paged_decode(q, cache)
+    else:
+        rows = 700 if call == "prefill" else 5
+        q, k, v = prefill.tensors([rows], [700], HQ, HKV, torch.bfloat16, 6)
+        cq, ck = prefill.cu_of([rows]), prefill.cu_of([700])
+        run = lambda: sel.prefill_attention(q, k, v, cq, cq.cuda(), ck, ck.cuda())[0]
+    want = run().clone()
+    kvec.kvec_sync_status(sel.handle)
+    try:
+        kvec.kvec_set_test_fault(4)
+        run()
+        with pytest.raises(kvec.KvecError) as e:
+            kvec.kvec_sync_status(sel.handle)
+        assert e.value.status == kvec.KVEC_ERR_DEVICE_TIMEOUT
+    finally:
+        kvec.kvec_set_test_fault(0)
+    kvec.kvec_sync_status(sel.handle)
+    assert torch.equal(run(), want)
+    kvec.kvec_sync_status(sel.handle)
+    sel.close()
