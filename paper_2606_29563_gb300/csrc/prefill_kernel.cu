@@ -7,8 +7,8 @@
 // A CTA owns two tiles of 128 rows; a row is a (query, query head) pair, the g query heads
 // of one KV head side by side, so that one query fills g rows and both tiles read the same
 // K and V.  It walks the 128-key blocks that any of its rows sees:
-//   warps 0-3, 4-7  softmax of tile 0 and 1, one thread a row: S from TMEM, running maximum
-//                   and sum, the weights back to TMEM as 16-bit values over S;
+//   warps 0-3, 4-7  softmax of tile 0 and 1, one thread a row: S from TMEM, running sum, the
+//                   weights back to TMEM as 16-bit values over S; at the end the outputs;
 //   warp 8          TMA: the query rows once, then K and V blocks through a ring;
 //   warp 9          tcgen05.mma: S = Q K^T (both from shared memory), O += P V (P from TMEM,
 //                   V column-major from shared memory), for the tiles in turn, so that one
@@ -16,10 +16,25 @@
 //   warps 10, 11    blocks that some row does not see wholly: zero what V holds there of
 //                   infinities and NaN, which a weight of zero would not keep out.  What a row
 //                   sees of them is added at the end.
-// A row's weights refer to a maximum m that need not be the largest: it is that of the row's
-// first 64 visible keys, and moves only when the sum of 64 weights passes 2^14 (kMostWeight),
-// so that no block waits for a maximum and O is scaled in TMEM once in a while.  Results do not
-// depend on m: 2^(s - m) keeps its relative precision, and so does l.
+// A row's weights refer to a maximum m that need not be the largest: it is that of the first
+// block in which the row sees a key, and moves only when the weights of a block sum up to 2^14
+// (kMostWeight), so that no block waits for a maximum and O is scaled in TMEM once in a while.
+// Results do not depend on m: 2^(s - m) keeps its relative precision, and so does l.
+//
+// Bound by the products' chain: a block of both tiles takes 2048 cycles of the tensor pipe (32
+// products of 64 cycles, which is what they take when nothing waits) and about 3000 in all,
+// since a tile's softmax (S read 60, exponentials 2 x 370, weights written and handed over 250
+// cycles) and the waits of the MMA warp outlast the other tile's 1024.  Measured, 32 query and 8
+// KV heads, bf16: 32768 tokens 5.5 ms, 1594 TFLOP/s (85 % of the measured cuBLAS burst); 8192
+// tokens 376 us, 1460 TFLOP/s; 16384 tokens with a window of 2048 and 4 first tokens 440 us,
+// 1174 TFLOP/s of visible pairs (18 blocks an item for 16 of keys seen, and about 6 us an item
+// before its first and after its last products).  What that took, 8192 tokens in us: S in
+// registers without spills 451, items one behind the other in persistent CTAs 445, no maximum
+// pass 421, waits of one poll 406, 32-byte stores 398, stages stepped 390, whole blocks of
+// weights handed over at once 378.  Slower: an issuer warp for each tile (466: products of two
+// tiles that take turns delay both), outputs by a warpgroup of their own (396: 64 registers
+// for the others spill), halves of blocks left out where no row sees them (425: the branches
+// stand between the products).
 #include <algorithm>
 
 #include "half_types.cuh"
@@ -37,9 +52,9 @@ constexpr int kPfStages = 5;
 constexpr int kPfThreads = 384;
 constexpr uint32_t kPfTmem = 512;                   // S0 | S1 | O0 | O1, 128 columns each
 // Registers of a thread: at launch (the most that 384 threads may have), and after the split.
-constexpr int kPfRegs = 168, kPfSoftmaxRegs = 200, kPfOtherRegs = 104;
+constexpr int kPfRegs = 168, kPfSoftmaxRegs = 192, kPfOtherRegs = 120;
 static_assert(256 * kPfSoftmaxRegs + 128 * kPfOtherRegs <= kPfThreads * kPfRegs, "the split fits what the block was launched with");
-// The largest sum of a row's 64 weights: below it, no maximum of them is formed.  fp16 holds them.
+// A row's weights of a block that sum up to less are taken as they are; fp16 holds them.
 constexpr float kMostWeight = 16384.f;
 // The maximum before the first visible logit, finite: 2^(-inf - it) is 0.
 constexpr float kNoLogit = -3.402823466e38f;
@@ -63,14 +78,14 @@ struct PfArgs {
     float2* part_ml; // [items][2][128] (m, l) of the rows
     Divisor by_per, by_heads;   // batch * Hkv, Hkv
     float sl2;
-    int fault;       // test of the error path (kvec_set_test_fault): no S is signalled
+    int fault;       // test of the error path (kvec_set_test_fault): no S is ever complete
 };
 
 struct __align__(8) PfBarriers {
     uint64_t full[kPfStages], empty[kPfStages];
     uint64_t clean[kPfStages];   // the cleaning warps have passed the stage
     uint64_t q_full, q_empty, mma_done;
-    uint64_t s_full[2], p_half[2], p_full[2], o_half[2], o_done[2];   // half: of the block's first 64 keys
+    uint64_t s_full[2], p_full[2], o_done[2];
     uint32_t tmem_base;
     volatile int abort_flag;
     volatile int unbounded;      // a block of partial sight held an infinity or NaN in V (of any item so far)
@@ -86,12 +101,9 @@ struct Item {
     int off;                      // position of query 0
     int nsink, lo;                // the blocks seen: 0 .. nsink - 1, then from lo on
     int i0, n;                    // of them this item's part: the n from the i0-th on
-    int whole_lo, whole_hi;       // keys [whole_lo, whole_hi] (and below `sinks`) are seen by every row
+    int whole_lo, whole_hi;       // the blocks from the whole_lo-th to before the whole_hi-th are seen by every row
     __device__ __forceinline__ int block(int i) const { return i0 + i < nsink ? i0 + i : lo + i0 + i - nsink; }
-    __device__ __forceinline__ bool edge(int i, int sinks) const {
-        const int t0 = block(i) * kPfTile, t1 = t0 + kPfTile - 1;
-        return t1 > whole_hi || (t0 < whole_lo && t1 >= sinks);
-    }
+    __device__ __forceinline__ bool edge(int i) const { return i < whole_lo || i >= whole_hi; }
 };
 
 template <bool PARTS>
@@ -132,8 +144,11 @@ __device__ __forceinline__ bool find_item(const PfArgs& A, int x, Item& w) {
             w.n = all * (part + 1) / A.parts - w.i0;
         }
     }
-    w.whole_hi = pa;
-    w.whole_lo = io.window ? pb - io.window + 1 : 0;
+    // Keys [pb - window + 1, pa] are seen by every row.
+    const int first = io.window ? max(pb - io.window + 1, 0) : 0;
+    w.whole_lo = max((first + kPfTile - 1) / kPfTile, w.lo) - w.lo + w.nsink - w.i0;
+    w.whole_hi = ((pa + 1) >> 7) - w.lo + w.nsink - w.i0;
+    static_assert(kPfTile == 128, "the shift");
     return true;
 }
 
@@ -219,8 +234,9 @@ __device__ __forceinline__ int item_of(int turn) {
 }
 
 // Persistent: of every gridDim.x items a CTA takes one, in turns from the front and from the
-// back (items cost less and less, so that the shares are even), and no role waits for an item's end: the next one's K and V follow through the ring, its first S is formed
-// behind the last products of this one, while the softmax warps write their outputs.
+// back (items cost less and less, so that the shares are even), and no role waits for an
+// item's end: the next one's K and V follow through the ring, its first S is formed behind the
+// last products of this one, while the softmax warps write their outputs.
 // PARTS: a pair's blocks are divided into several items, which leave sums for prefill_join_kernel.
 template <class T, bool PARTS>
 __global__ void __launch_bounds__(kPfThreads, 1) prefill_kernel(const __grid_constant__ PfArgs A) {
@@ -244,10 +260,8 @@ __global__ void __launch_bounds__(kPfThreads, 1) prefill_kernel(const __grid_con
         ptx::mbar_init(&bars->q_empty, 1);
         ptx::mbar_init(&bars->mma_done, 1);
         for (int t = 0; t < 2; ++t) {
-            ptx::mbar_init(&bars->s_full[t], 1);
-            ptx::mbar_init(&bars->p_half[t], 4);   // one arrival per warp of the tile
-            ptx::mbar_init(&bars->p_full[t], 4);
-            ptx::mbar_init(&bars->o_half[t], 1);
+            ptx::mbar_init(&bars->s_full[t], A.fault ? 2 : 1);   // 2, for a test of the waits: never complete
+            ptx::mbar_init(&bars->p_full[t], 4);   // one arrival per warp of the tile
             ptx::mbar_init(&bars->o_done[t], 1);
         }
         bars->abort_flag = 0;
@@ -332,35 +346,38 @@ __global__ void __launch_bounds__(kPfThreads, 1) prefill_kernel(const __grid_con
                 if (!stop && !pf_wait(bar, phase & 1, abort)) stop = true;
                 return !stop;
             };
-            // Stages as values that the compiler knows to be the warp's, so that descriptors stay in uniform registers.
-            auto issue_s = [&](int t, int y, bool last) {   // S_t = Q_t K^T, K of load y
-                const int st = ptx::warp_uniform(y % kPfStages);
-                if (ptx::elect_one()) {
-                    const uint64_t kd = kdesc + (uint32_t)(st * (kPfBuf >> 4)), qd = qdesc + (uint32_t)(t * (kPfBuf >> 4));
-#pragma unroll
-                    for (int kk = 0; kk < 8; ++kk) {
-                        const uint32_t ofs = (kk >> 2) * (kPfHalf >> 4) + (kk & 3) * 2;
-                        ptx::mma_bf16(tmem + t * 128, qd + ofs, kd + ofs, idesc_s, kk > 0 ? 1u : 0u);
+            // The stage of a load and its parity, stepped: what stands between two products in this warp
+            // counts, as few products queue up.
+            struct Place {
+                int st = 0, parity = 0;
+                __device__ __forceinline__ void step() {
+                    if (++st == kPfStages) {
+                        st = 0;
+                        parity ^= 1;
                     }
-                    if (!A.fault) ptx::mma_commit(&bars->s_full[t]);   // (withheld for a test of the waits)
-                    if (last) ptx::mma_commit(&bars->empty[st]);
                 }
-                __syncwarp();
             };
-            auto issue_o = [&](int t, int y, bool add, int half, bool last) {   // O_t += P_t V, 64 keys of load y
-                const int st = ptx::warp_uniform(y % kPfStages);
-                if (ptx::elect_one()) {
-                    const uint64_t vd = vdesc + (uint32_t)(st * (kPfBuf >> 4));
+            Place pk, pv;   // of the next K and V
+            pv.step();
+            // Stages as values that the compiler knows to be the warp's, so that descriptors stay in uniform registers.
+            auto products_s = [&](int t, int st, bool last) {   // S_t = Q_t K^T, K in stage st; one thread
+                const uint64_t kd = kdesc + (uint32_t)(st * (kPfBuf >> 4)), qd = qdesc + (uint32_t)(t * (kPfBuf >> 4));
 #pragma unroll
-                    for (int k4 = 0; k4 < 4; ++k4) {
-                        const int kk = half * 4 + k4;
-                        mma_tmem_a(tmem + 256 + t * 128, tmem + t * 128 + kk * 8, vd + kk * (2048 >> 4), idesc_o,
-                                   add || kk > 0 ? 1u : 0u);
-                    }
-                    ptx::mma_commit(half ? &bars->o_done[t] : &bars->o_half[t]);
-                    if (half && last) ptx::mma_commit(&bars->empty[st]);
+                for (int kk = 0; kk < 8; ++kk) {
+                    const uint32_t ofs = (kk >> 2) * (kPfHalf >> 4) + (kk & 3) * 2;
+                    ptx::mma_bf16(tmem + t * 128, qd + ofs, kd + ofs, idesc_s, kk > 0 ? 1u : 0u);
                 }
-                __syncwarp();
+                ptx::mma_commit(&bars->s_full[t]);
+                if (last) ptx::mma_commit(&bars->empty[st]);
+            };
+            auto products_o = [&](int t, int st, bool add, bool last) {   // O_t += P_t V, V in stage st
+                const uint64_t vd = vdesc + (uint32_t)(st * (kPfBuf >> 4));
+#pragma unroll
+                for (int kk = 0; kk < 8; ++kk)
+                    mma_tmem_a(tmem + 256 + t * 128, tmem + t * 128 + kk * 8, vd + kk * (2048 >> 4), idesc_o,
+                               add || kk > 0 ? 1u : 0u);
+                ptx::mma_commit(&bars->o_done[t]);
+                if (last) ptx::mma_commit(&bars->empty[st]);
             };
             int qloads = 0, blocks[2] = {0, 0};   // blocks of each tile so far: the phase of its P
             // S of an item's first block is issued between the last products of the item before.
@@ -374,7 +391,9 @@ __global__ void __launch_bounds__(kPfThreads, 1) prefill_kernel(const __grid_con
             bool more = next_item();
             if (more && wait(&bars->full[0], 0) && wait(&bars->q_full, 0)) {
                 ptx::tc_fence_after();
-                for (int t = 0; t < w.tiles; ++t) issue_s(t, 0, t == w.tiles - 1);
+                if (ptx::elect_one())
+                    for (int t = 0; t < w.tiles; ++t) products_s(t, 0, t == w.tiles - 1);
+                __syncwarp();
                 ++qloads;
                 if (w.n == 1 && ptx::elect_one()) ptx::mma_commit(&bars->q_empty);
                 __syncwarp();
@@ -384,35 +403,32 @@ __global__ void __launch_bounds__(kPfThreads, 1) prefill_kernel(const __grid_con
                 for (int i = 0; i < cur.n && !stop; ++i) {
                     const bool last_block = i + 1 == cur.n;
                     if (last_block) more = next_item();
-                    const int xv = x + 1;
-                    x += 2;
+                    pk.step();
+                    pk.step();   // the next K
                     // The tiles that the next S is for: this item's, or the next one's.
                     const int next_tiles = !last_block ? cur.tiles : more ? w.tiles : 0;
-                    if (!wait(&bars->full[xv % kPfStages], xv / kPfStages)) break;
-                    if (cur.edge(i, sinks) && !wait(&bars->clean[xv % kPfStages], xv / kPfStages)) break;
+                    if (!wait(&bars->full[pv.st], pv.parity)) break;
+                    if (cur.edge(i) && !wait(&bars->clean[pv.st], pv.parity)) break;
+                    const int sv = ptx::warp_uniform(pv.st), sk = ptx::warp_uniform(pk.st);
 #pragma unroll
                     for (int t = 0; t < 2; ++t) {
-                        if (t < cur.tiles) {
-                            if (!wait(&bars->p_half[t], blocks[t])) break;
-                            ptx::tc_fence_after();
-                            issue_o(t, xv, i > 0, 0, t == cur.tiles - 1);
-                        }
+                        const bool here = t < cur.tiles, next = t < next_tiles;
                         if (t == 0 && next_tiles > 0) {
-                            if (!wait(&bars->full[x % kPfStages], x / kPfStages)) break;
+                            if (!wait(&bars->full[pk.st], pk.parity)) break;
                             if (last_block && !wait(&bars->q_full, qloads)) break;
                         }
-                        if (t < cur.tiles) {
-                            if (!wait(&bars->p_full[t], blocks[t])) break;
-                            ptx::tc_fence_after();
-                            issue_o(t, xv, i > 0, 1, t == cur.tiles - 1);
-                            ++blocks[t];
+                        if (here && !wait(&bars->p_full[t], blocks[t])) break;
+                        ptx::tc_fence_after();
+                        if (ptx::elect_one()) {
+                            if (here) products_o(t, sv, i > 0, t == cur.tiles - 1);
+                            if (next) products_s(t, sk, t == next_tiles - 1);
                         }
-                        if (t < next_tiles) {
-                            ptx::tc_fence_after();
-                            issue_s(t, x, t == next_tiles - 1);
-                        }
+                        __syncwarp();
+                        if (here) ++blocks[t];
                     }
                     if (stop) break;
+                    pv.step();
+                    pv.step();
                     if (last_block && more) ++qloads;
                     // The item's queries have been read once its last S is done.
                     const bool q_last = last_block ? more && w.n == 1 : i + 2 == cur.n;
@@ -439,7 +455,7 @@ __global__ void __launch_bounds__(kPfThreads, 1) prefill_kernel(const __grid_con
                         stop = true;
                         break;
                     }
-                    if ((y & 1) && w.edge(y >> 1, sinks)) {
+                    if ((y & 1) && w.edge(y >> 1)) {
                         uint4* v = reinterpret_cast<uint4*>(ring + st * kPfBuf);
                         bool found = false;
 #pragma unroll 8
@@ -478,7 +494,7 @@ __global__ void __launch_bounds__(kPfThreads, 1) prefill_kernel(const __grid_con
         auto add_unbounded = [&](int p, int below, const Item& w, int n, auto add) {
 #pragma unroll 1
             for (int i = 0; i < n; ++i) {
-                if (!w.edge(i, sinks)) continue;
+                if (!w.edge(i)) continue;
 #pragma unroll 1
                 for (int c = 0; c < kPfTile; ++c) {
                     const int key = w.block(i) * kPfTile + c;
@@ -510,7 +526,7 @@ __global__ void __launch_bounds__(kPfThreads, 1) prefill_kernel(const __grid_con
 #pragma unroll
                 for (int c = 0; c < 4; ++c) ptx::tmem_ld32(tS + c * 32, s + c * 32);
                 ptx::tmem_wait_ld();
-                if (w.edge(i, sinks)) {
+                if (w.edge(i)) {
                     // Bit c of the words: the row sees key t0 + c.  (Comparisons for each column
                     // became branches, 12,000 cycles a block.)
                     const int t0 = w.block(i) * kPfTile;
@@ -522,61 +538,62 @@ __global__ void __launch_bounds__(kPfThreads, 1) prefill_kernel(const __grid_con
                         for (int c = 0; c < 32; ++c) s[32 * g + c] = (seen >> c) & 1u ? s[32 * g + c] : -INFINITY;
                     }
                 }
-                // The weights of 64 keys relative to m, as pairs of 16-bit values, and their sum.
-                uint32_t pk[32];
-                auto weights = [&](const float* x) {
+                // The weights of 64 keys relative to m, as pairs of 16-bit values over S, and their sum.
+                auto weights = [&](int c) {
                     const uint64_t ref = ptx::pack_f32x2(-m, -m);
                     uint64_t sum[4] = {0ull, 0ull, 0ull, 0ull};
+                    uint32_t pk[32];
 #pragma unroll
                     for (int e = 0; e < 32; ++e) {
-                        const uint64_t y = ptx::fma_f32x2(ptx::pack_f32x2(x[2 * e], x[2 * e + 1]), sl2, ref);
+                        const uint64_t y = ptx::fma_f32x2(ptx::pack_f32x2(s[c * 64 + 2 * e], s[c * 64 + 2 * e + 1]), sl2, ref);
                         const float p0 = ptx::ex2(ptx::lo_f32(y)), p1 = ptx::ex2(ptx::hi_f32(y));
                         sum[e & 3] = ptx::add_f32x2(sum[e & 3], ptx::pack_f32x2(p0, p1));
                         pk[e] = Half16<T>::pack(p0, p1);
                     }
+                    tmem_st32(tS + c * 32, pk);
                     const uint64_t all = ptx::add_f32x2(ptx::add_f32x2(sum[0], sum[1]), ptx::add_f32x2(sum[2], sum[3]));
                     return ptx::lo_f32(all) + ptx::hi_f32(all);
                 };
+                if (i == 0) {   // the row's first maximum
 #pragma unroll
-                for (int c = 0; c < 2; ++c) {
-                    float z = weights(s + c * 64);
-                    if (__any_sync(0xffffffffu, live && !(z < kMostWeight))) {
-                        // The row's first logits, or ones far above m (or NaN): m moves to the largest.
-                        float mx = m;
-#pragma unroll
-                        for (int e = 0; e < 64; e += 2) mx = max3(mx, s[c * 64 + e] * sl2f, s[c * 64 + e + 1] * sl2f);
-                        if (z < kMostWeight || !live) mx = m;
-                        const float f = ptx::ex2(m - mx);
-                        l *= f;
-                        m = mx;
-                        if (i > 0 || c > 0) {
-                            // The outputs so far with it, once their products are done.
-                            if (!(c > 0 ? pf_wait(&bars->o_half[t], blocks & 1, abort)
-                                        : pf_wait(&bars->o_done[t], (blocks - 1) & 1, abort))) {
-                                stop = true;
-                                break;
-                            }
-                            ptx::tc_fence_after();
-#pragma unroll 1
-                            for (int d0 = 0; d0 < kHeadDim; d0 += 32) {
-                                float o[32];
-                                ptx::tmem_ld32(tO + d0, o);
-                                ptx::tmem_wait_ld();
-#pragma unroll
-                                for (int d = 0; d < 32; ++d) o[d] *= f;
-                                tmem_st32(tO + d0, reinterpret_cast<const uint32_t*>(o));
-                            }
-                        }
-                        z = weights(s + c * 64);
-                    }
-                    l += z;
-                    tmem_st32(tS + c * 32, pk);
-                    tmem_wait_st();
-                    ptx::tc_fence_before();
-                    __syncwarp();
-                    if (lane == 0) ptx::mbar_arrive(c == 0 ? &bars->p_half[t] : &bars->p_full[t]);
+                    for (int e = 0; e < 128; e += 2) m = max3(m, s[e] * sl2f, s[e + 1] * sl2f);
                 }
-                if (stop) break;
+                float z = weights(0);
+                z += weights(1);
+                if (__any_sync(0xffffffffu, live && !(z < kMostWeight))) {
+                    // The row's first logits, ones far above m, or NaN: m moves to the largest.
+                    float mx = m;
+#pragma unroll
+                    for (int e = 0; e < 128; e += 2) mx = max3(mx, s[e] * sl2f, s[e + 1] * sl2f);
+                    if (z < kMostWeight || !live) mx = m;
+                    const float f = ptx::ex2(m - mx);
+                    l *= f;
+                    m = mx;
+                    if (i > 0) {
+                        // The outputs so far with it, once the products of the block before are done.
+                        if (!pf_wait(&bars->o_done[t], (blocks - 1) & 1, abort)) {
+                            stop = true;
+                            break;
+                        }
+                        ptx::tc_fence_after();
+#pragma unroll 1
+                        for (int d0 = 0; d0 < kHeadDim; d0 += 32) {
+                            float o[32];
+                            ptx::tmem_ld32(tO + d0, o);
+                            ptx::tmem_wait_ld();
+#pragma unroll
+                            for (int d = 0; d < 32; ++d) o[d] *= f;
+                            tmem_st32(tO + d0, reinterpret_cast<const uint32_t*>(o));
+                        }
+                    }
+                    z = weights(0);
+                    z += weights(1);
+                }
+                l += z;
+                tmem_wait_st();
+                ptx::tc_fence_before();
+                __syncwarp();
+                if (lane == 0) ptx::mbar_arrive(&bars->p_full[t]);
             }
             if (n > 0 && !stop && !pf_wait(&bars->o_done[t], (blocks - 1) & 1, abort)) stop = true;
             if (stop) break;
