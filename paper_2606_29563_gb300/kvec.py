@@ -378,6 +378,8 @@ class KvecSelector:
         self.handle = kvec_create(params)
         self.device = torch.device("cuda", torch.cuda.current_device())
         self._current = torch._C._cuda_getCurrentRawStream   # torch.cuda.current_stream makes an object, 2 us
+        self._lib = load()
+        self._decode_bytes = {}      # kvec_paged_decode_bytes by its sizes
         self.state_bytes = kvec_state_bytes(params.max_seqlen)
 
     def close(self) -> None:
@@ -536,8 +538,10 @@ class KvecSelector:
                                  None if k_norm is None else k_norm.data_ptr(), eps, rot, 1 if interleaved else 0, most,
                                  None if rot_table is None else rot_table.data_ptr(), positions.data_ptr(),
                                  q_out.data_ptr(), None if k_out is None else k_out.data_ptr())
-            kvec_rotate_append(self.handle, a, batch, None if cu_tokens is None else cu_tokens.data_ptr(),
-                               None if cache is None else cache.c, self._raw(stream))
+            st = self._lib.kvec_rotate_append(self.handle, a, batch, None if cu_tokens is None else cu_tokens.data_ptr(),
+                                              None if cache is None else cache.c, self._raw(stream))
+            if st:
+                _check(st)
         return (q_out, k_out) if want_k else q_out
 
     def paged_decode(self, q, cache, max_len: Optional[int] = None, window: int = 0, sinks: int = 0, out=None,
@@ -556,10 +560,15 @@ class KvecSelector:
             self._check("out", out, shape, dtype)
         if max_len is None:
             max_len = cache.capacity
-        need = kvec_paged_decode_bytes(self.handle, batch, max_len, cache.weights is not None)
+        sizes = (batch, max_len, cache.weights is not None)
+        need = self._decode_bytes.get(sizes)
+        if need is None:
+            need = self._decode_bytes[sizes] = kvec_paged_decode_bytes(self.handle, *sizes)
         scratch = self._empty(max(need, 16), self._torch.uint8, stream)
-        kvec_paged_decode(self.handle, batch, q.data_ptr(), cache.c, max_len, window, sinks, out.data_ptr(),
-                          scratch.data_ptr(), need, self._raw(stream))
+        st = self._lib.kvec_paged_decode(self.handle, batch, q.data_ptr(), cache.c, max_len, window, sinks, out.data_ptr(),
+                                         scratch.data_ptr(), need, self._raw(stream))
+        if st:
+            _check(st)
         return out
 
     def paged_evict(self, cache, new_table, budget: int, sinks: int = 0, recent: int = 0, max_len: Optional[int] = None,
@@ -582,9 +591,11 @@ class KvecSelector:
             kept = self._empty((batch, Hkv, budget), t.int32, stream)
         else:
             self._check("kept", kept, (batch, Hkv, budget), t.int32)
-        kvec_paged_evict(self.handle, batch, cache.c, new_table.data_ptr(), new_table.shape[1],
-                         cache.capacity if max_len is None else max_len, budget, sinks, recent, new_lens.data_ptr(),
-                         kept.data_ptr(), self._raw(stream))
+        st = self._lib.kvec_paged_evict(self.handle, batch, cache.c, new_table.data_ptr(), new_table.shape[1],
+                                        cache.capacity if max_len is None else max_len, budget, sinks, recent,
+                                        new_lens.data_ptr(), kept.data_ptr(), self._raw(stream))
+        if st:
+            _check(st)
         return new_lens, kept
 
     def prefill_attention(self, q, k, v, cu_q_host, cu_q_dev, cu_k_host=None, cu_k_dev=None, window: int = 0,
@@ -619,11 +630,13 @@ class KvecSelector:
             lse = self._empty((Tq, Hq), t.float32, stream)
         else:
             self._check("lse", lse, (Tq, Hq), t.float32)
-        need = kvec_prefill_bytes(self.handle, batch, cu_q, cu_k, window, sinks)
-        scratch = self._empty((need,), t.uint8, stream).data_ptr() if need else None
-        kvec_prefill_attention(self.handle, code, batch, cu_q, cu_q_dev.data_ptr(), cu_k, cu_k_dev.data_ptr(),
-                               q.data_ptr(), k.data_ptr(), v.data_ptr(), window, sinks, out.data_ptr(), lse.data_ptr(),
-                               scratch, need, self._raw(stream))
+        need = self._lib.kvec_prefill_bytes(self.handle, batch, cu_q, cu_k, window, sinks)
+        scratch = self._empty(need, t.uint8, stream) if need else None
+        st = self._lib.kvec_prefill_attention(self.handle, code, batch, cu_q, cu_q_dev.data_ptr(), cu_k, cu_k_dev.data_ptr(),
+                                              q.data_ptr(), k.data_ptr(), v.data_ptr(), window, sinks, out.data_ptr(),
+                                              lse.data_ptr(), scratch.data_ptr() if need else None, need, self._raw(stream))
+        if st:
+            _check(st)
         return out, lse
 
     def debug(self, device="cuda"):

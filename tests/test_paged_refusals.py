@@ -102,6 +102,7 @@ def selector(Hq=8, Hkv=2):
     """The binding's own checks need no handle."""
     s = kvec.KvecSelector.__new__(kvec.KvecSelector)
     s._torch, s.params, s.handle, s.device = torch, kvec.make_params(Hq, Hkv), None, torch.device("cpu")
+    s._lib, s._decode_bytes = kvec.load(), {}
     return s
 
 
