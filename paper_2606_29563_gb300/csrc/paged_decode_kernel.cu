@@ -18,8 +18,14 @@
 // need a row's final sums: the logits wait for them in scratch (4 bytes a query head and
 // slot beside 512 of keys and values).
 //
-// With few pairs of few slots the CTAs of a pair form a cluster, and meet over distributed
-// shared memory in one launch.
+// With few pairs the CTAs of a pair form a cluster, and with short ones each has a CTA; these
+// meet over distributed shared memory in one launch.
+//
+// HBM-bound when there is much to read: 131072 slots of 8 heads (537 MB) in 84 us, 6.4 TB/s, 94 %
+// of the measured copy rate; 64 rows of 1024 to 2048 slots of 4 heads and 7 query heads each (203 MB
+// with the weights) in 60 us, of which the reading takes 31: before it lie the lengths, the
+// list, the pages' numbers and the first copies (4 us), behind it the merges, the join and the
+// weights, each a chain of loads.  512 slots 6.2 us, the same chain once.
 #include "half_types.cuh"
 #include "kvec_internal.cuh"
 #include "sm100_ptx.cuh"
@@ -59,6 +65,7 @@ struct PdArgs {
     int ctas;                 // that share the list of blocks
     int nbmax;                // most visible blocks of a pair
     int g;
+    int join_heads;           // query heads of a block of the join
     float sl2;                // scale * log2(e)
     int fault;                // test of the error path (kvec_set_test_fault): warp 0 of CTA 0 loads nothing
 };
@@ -556,8 +563,8 @@ __global__ void __launch_bounds__(kPdThreads, kPdCtasPerSm) paged_decode_kernel(
         for (int i = 0; i < kPdStages; ++i) ptx::mbar_wait(&full[warp][i], (phases >> i) & 1u, 20000000ull);
 }
 
-// The pairs whose blocks several CTAs share.  Block x < g of (x, h, s): query head x; the
-// others add the weights, kJoinRows slots each.  (A thread finds a share, so that the shares'
+// The pairs whose blocks several CTAs share.  The first blocks x of (x, h, s) join the outputs of
+// join_heads query heads each; the others add the weights, kJoinRows slots each.  (A thread finds a share, so that the shares'
 // places, sums and outputs are each read at once: one thread in a loop over the 38 shares of
 // 131072 slots took 58 us.)
 template <class T>
@@ -567,8 +574,11 @@ __global__ void __launch_bounds__(kHeadDim) paged_join_kernel(const __grid_const
     const int h = blockIdx.y, s = blockIdx.z, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = A.g;
     Visible v;
     v.init(A, s);
-    const int i0 = ((int)blockIdx.x - g) * (kJoinRows / kPdBlock);
-    const size_t out = ((size_t)s * A.io.Hq + (size_t)h * g + blockIdx.x) * kHeadDim + tid;
+    const int joins = (g + A.join_heads - 1) / A.join_heads;
+    const bool weights = (int)blockIdx.x >= joins;
+    const int i0 = ((int)blockIdx.x - joins) * (kJoinRows / kPdBlock);
+    const int j0 = (int)blockIdx.x * A.join_heads, j1 = min(j0 + A.join_heads, g);
+    T* const out = reinterpret_cast<T*>(A.io.out) + ((size_t)s * A.io.Hq + (size_t)h * g) * kHeadDim + tid;
     // The lengths were complete before the kernel that this one waits for began.
     List list;
     list.init(A);
@@ -577,7 +587,8 @@ __global__ void __launch_bounds__(kHeadDim) paged_join_kernel(const __grid_const
     asm volatile("griddepcontrol.launch_dependents;\n" ::: "memory");
     asm volatile("griddepcontrol.wait;\n" ::: "memory");
     if (v.nb == 0) {
-        if ((int)blockIdx.x < g) reinterpret_cast<T*>(A.io.out)[out] = T(0.f);
+        if (!weights)
+            for (int j = j0; j < j1; ++j) out[j * kHeadDim] = T(0.f);
         return;
     }
     // Finished by its CTA, or a block of slots that the sequence does not have.
@@ -589,8 +600,7 @@ __global__ void __launch_bounds__(kHeadDim) paged_join_kernel(const __grid_const
         if (c == c0) return first;
         return total < A.ctas && share_start(total, c, A.ctas) == share_start(total, c + 1, A.ctas) ? -1 : c * 2;
     };
-    if ((int)blockIdx.x < g) {
-        const int j = blockIdx.x;
+    for (int j = j0; !weights && j < j1; ++j) {
         float M = kNoLogit, L = 0.f;
         for (int c = tid; c <= c1 - c0; c += kHeadDim) {
             const int at = place(c0 + c);
@@ -633,9 +643,10 @@ __global__ void __launch_bounds__(kHeadDim) paged_join_kernel(const __grid_const
                 if (at >= 0) O = fmaf(share[c].y, part[at * kPlace], O);
             }
         }
-        reinterpret_cast<T*>(A.io.out)[out] = T(L > 0.f || L != L ? O / L : 0.f);
-        return;
+        out[j * kHeadDim] = T(L > 0.f || L != L ? O / L : 0.f);
+        __syncthreads();   // the shares and sums are read before the next head's
     }
+    if (!weights) return;
     for (int j = warp; j < g; j += kHeadDim / 32) {   // a warp a query head, a lane a share
         float M = kNoLogit, L = 0.f;
         for (int c = c0 + lane; c <= c1; c += 32) {
@@ -668,11 +679,16 @@ int share_ctas(int num_sms) { return kPdCtasPerSm * num_sms; }
 
 template <class T>
 cudaError_t launch_typed(const PdArgs& a, cudaStream_t st) {
-    // CTAs of a pair: the largest cluster that fits the device's resident CTAs in one wave.
+    // CTAs of a pair: the largest cluster that fits the device's resident CTAs in one wave, with
+    // two blocks a warp and more; taken where that leaves a CTA 32 blocks and less (a quarter of
+    // one a thread for the weights), else the list of all blocks.  Measured with weights, 8 KV
+    // heads, in us by cluster and by list: one row of 4096 slots 13.3, of 8192 (list) 15.4; 512
+    // rows of 100 to 300 slots (a CTA each) 117 and 262, the list's CTAs ending a pair every 19
+    // blocks; 40 of 1000 slots (two CTAs each, more than a wave) 47.7 and 43.5, 256 of 1500 365 and 303.
     const int pairs = a.io.batch * a.io.Hkv;
     int splits = 1;
     while (splits < kPdMaxCluster && (long long)pairs * splits * 2 <= a.ctas && a.nbmax >= kPdWarps * 2 * splits) splits *= 2;
-    if (pairs <= a.ctas && a.nbmax <= 8 * kPdWarps * splits) {
+    if (a.nbmax <= 8 * kPdWarps * splits) {
         cudaLaunchConfig_t cfg = {};
         cfg.gridDim = dim3(splits, a.io.Hkv, a.io.batch);
         cfg.blockDim = dim3(kPdThreads);
@@ -692,7 +708,8 @@ cudaError_t launch_typed(const PdArgs& a, cudaStream_t st) {
     cudaError_t e = launch_prio(paged_decode_kernel<T, false>, dim3(a.ctas), dim3(kPdThreads), kPdSmem, st, 0, true, a);
     if (e != cudaSuccess) return e;
     const int rows = a.c.weights ? (a.nbmax * kPdBlock + kJoinRows - 1) / kJoinRows : 0;
-    return launch_prio(paged_join_kernel<T>, dim3(a.g + rows, a.io.Hkv, a.io.batch), dim3(kHeadDim),
+    const int joins = (a.g + a.join_heads - 1) / a.join_heads;
+    return launch_prio(paged_join_kernel<T>, dim3(joins + rows, a.io.Hkv, a.io.batch), dim3(kHeadDim),
                        a.ctas * sizeof(float2), st, 0, true, a);
 }
 
@@ -736,6 +753,9 @@ cudaError_t launch_paged_decode(const PagedDecodeIO& io, const PagedCacheView& c
     a.c = c;
     a.io = io;
     a.g = io.Hq / io.Hkv;
+    // A block a query head where pairs are few, one for all of a pair's where they are many: 256
+    // pairs of 7 heads with weights 59.7 us a head, 63.4 all; 320 of 4 43.6 and 42.7, 2048 of 4 303 and 287.
+    a.join_heads = io.batch * io.Hkv > 2 * num_sms ? a.g : 1;
     a.sl2 = io.scale * 1.4426950408889634f;
     a.fault = test_fault() == 4 ? 1 : 0;
     a.ctas = share_ctas(num_sms);

@@ -199,7 +199,7 @@ def check_decode(sel, q, cache, lens, max_len=None, window=0, sinks=0, scale=Non
     kvec.kvec_sync_status(sel.handle)
     got = f64(out)
     vmax = 8.0   # of the normal values here (a draw above it has odds of 1e-15)
-    assert np.abs(vp[np.isfinite(vp)]).max() < vmax
+    assert np.abs(vp[np.isfinite(vp)]).max(initial=0.0) < vmax
     n = max(1, min(max_len, max(lens)))
     tol = u * np.abs(ref) + (u * u + (n * 2.0 ** -25 if dtype == torch.float16 else 0.0) + 2e-5) * vmax
     bad = ~(np.abs(got - ref) <= tol)
@@ -488,3 +488,26 @@ def test_rotation_without_sequences_takes_any_number_of_tokens():
     cu = torch.tensor([0, 1000], dtype=torch.int32).cuda()
     want = selector(4, 2).rotate_append(q, k, None, pos, tab, cu_tokens=cu)
     assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+
+
+@pytest.mark.parametrize("batch,scale,Hq,Hkv", [(290, 2, 8, 4), (70, 9, 28, 4), (300, 3, 32, 8)])
+def test_many_sequences_on_the_list_path(batch, scale, Hq, Hkv):
+    # Rows past 512 slots share the list of all blocks; empty ones lie between them and at its ends.
+    gen = torch.Generator().manual_seed(batch * scale)
+    lens = [scale * (0, 1, 15, 16, 17, 63, 64, 65, 128, 130, 255, 257, 31, 7, 300, 48)[(5 * b + b // 16) % 16] for b in range(batch)]
+    cache, _ = make_cache(lens, Hkv, 32, torch.bfloat16, gen)
+    assert cache.capacity > 512
+    q = torch.randn((batch, Hq, D), generator=gen).to(torch.bfloat16).cuda()
+    check_decode(selector(Hq, Hkv), q, cache, lens)
+
+
+@pytest.mark.parametrize("lens", [[5, 0, 17], [0, 0, 0], [1], [0, 300], [40, 33, 2, 0, 0, 1, 99]])
+@pytest.mark.parametrize("weights", [False, True])
+def test_a_bound_far_above_the_lengths(lens, weights):
+    # The work is divided by max_len: most CTAs have no block, and pairs are shared with empty shares between.
+    gen = torch.Generator().manual_seed(len(lens) + sum(lens))
+    cache, _ = make_cache(lens, 2, 64, torch.float16, gen, max_pages=16384 // 64, weights=weights)
+    q = torch.randn((len(lens), 14, D), generator=gen).to(torch.float16).cuda()
+    out = check_decode(selector(14, 2), q, cache, lens)
+    for s, n in enumerate(lens):
+        assert n or torch.all(out[s] == 0)
