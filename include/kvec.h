@@ -24,7 +24,7 @@
  *     for the calling thread.  No C++ exception crosses this boundary.
  *   - A handle is used from one host thread at a time, and its selection calls
  *     share one workspace: calls on different streams must not overlap.
- *   - bf16 tensors are raw IEEE bfloat16 (2 bytes per element).
+ *   - bf16 tensors are raw IEEE bfloat16 (2 bytes per element), fp16 ones IEEE half.
  */
 #ifndef KVEC_H
 #define KVEC_H
