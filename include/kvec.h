@@ -310,7 +310,8 @@ typedef struct {
  *             their sines.  rot_dim is a multiple of 16 up to d (0: no rotation; the table
  *             may then be NULL and positions below 2^31 - 1 are valid).
  *   q_out     device dtype [T][H_q][d]; may be q itself where q_stride = H_q * d.
- *   k_out     device dtype [T][H_kv][d] (may be k in the same way), or NULL.
+ *   k_out     device dtype [T][H_kv][d] (may be k in the same way), or NULL.  Outputs and
+ *             pages overlap the inputs in no other way.
  * With a cache (NULL: none; k_out is then needed) sequence s's tokens take its last slots:
  * its lens already counts them, and token t of cu_tokens[s] <= t < cu_tokens[s + 1] goes to
  * slot lens[s] - (cu_tokens[s + 1] - t).  The slot's accumulated weight becomes 0.

@@ -23,7 +23,7 @@
 //
 // HBM-bound when there is much to read: 131072 slots of 8 heads (537 MB) in 84 us, 6.4 TB/s, 94 %
 // of the measured copy rate; 64 rows of 1024 to 2048 slots of 4 heads and 7 query heads each (203 MB
-// with the weights) in 60 us, of which the reading takes 31: before it lie the lengths, the
+// with the weights) in 54 us, of which the reading takes 31: before it lie the lengths, the
 // list, the pages' numbers and the first copies (4 us), behind it the merges, the join and the
 // weights, each a chain of loads.  512 slots 6.2 us, the same chain once.
 #include "half_types.cuh"
@@ -231,19 +231,19 @@ struct SlotWeights {
     }
 };
 
-// Adds the attention weights of blocks [i0, i1) of pair (s, h) to the cache's.  Two quarters
-// of a thread's are read at once: one after the other, the latencies of a long row added up.
+// Adds the attention weights of blocks [i0, i1) of pair (s, h) to the cache's.  One quarter of
+// a thread's at a time: two at once take 36 registers more in the decode kernel, which spills
+// then, and 40 in the join, of which fewer blocks are resident (64 rows of 1024 to 2048 slots
+// 59.6 us, 54.3 with one; a thread a slot 78).
 template <int NT>
 __device__ void add_weights(const PdArgs& A, int s, int h, const Visible& v, int i0, int i1, const float* mx,
                             const float* inv) {
     const int n = (i1 - i0) * 4;
-    for (int e = threadIdx.x; e < n; e += 2 * NT) {
-        SlotWeights a, b;
-        b.row = -1;
+#pragma unroll 1
+    for (int e = threadIdx.x; e < n; e += NT) {
+        SlotWeights a;
         a.load(A, s, h, v, i0, e);
-        if (e + NT < n) b.load(A, s, h, v, i0, e + NT);
         a.store(A, mx, inv);
-        b.store(A, mx, inv);
     }
 }
 
@@ -382,7 +382,7 @@ __global__ void __launch_bounds__(kPdThreads, kPdCtasPerSm) paged_decode_kernel(
                     failed = true;
                     if (lane == 0) atomicExch(A.io.err, 3);
                 }
-                phases ^= 1u << st;
+                if (!failed) phases ^= 1u << st;   // the parities stay those of copies in flight
 #pragma unroll
                 for (int t = 0; t < 2; ++t)
 #pragma unroll
@@ -682,9 +682,9 @@ cudaError_t launch_typed(const PdArgs& a, cudaStream_t st) {
     // CTAs of a pair: the largest cluster that fits the device's resident CTAs in one wave, with
     // two blocks a warp and more; taken where that leaves a CTA 32 blocks and less (a quarter of
     // one a thread for the weights), else the list of all blocks.  Measured with weights, 8 KV
-    // heads, in us by cluster and by list: one row of 4096 slots 13.3, of 8192 (list) 15.4; 512
+    // heads, in us by cluster and by list: one row of 4096 slots 13.3, of 8192 (list) 16.3; 512
     // rows of 100 to 300 slots (a CTA each) 117 and 262, the list's CTAs ending a pair every 19
-    // blocks; 40 of 1000 slots (two CTAs each, more than a wave) 47.7 and 43.5, 256 of 1500 365 and 303.
+    // blocks; 40 of 1000 slots (two CTAs each, more than a wave) 47.7 and 43.5, 256 of 1500 365 and 279.
     const int pairs = a.io.batch * a.io.Hkv;
     int splits = 1;
     while (splits < kPdMaxCluster && (long long)pairs * splits * 2 <= a.ctas && a.nbmax >= kPdWarps * 2 * splits) splits *= 2;

@@ -538,7 +538,7 @@ __global__ void __launch_bounds__(kPfThreads, 1) prefill_kernel(const __grid_con
                         for (int c = 0; c < 32; ++c) s[32 * g + c] = (seen >> c) & 1u ? s[32 * g + c] : -INFINITY;
                     }
                 }
-                // The weights of 64 keys relative to m, as pairs of 16-bit values over S, and their sum.
+                // The weights of half the keys relative to m, as pairs of 16-bit values over S, and their sum.
                 auto weights = [&](int c) {
                     const uint64_t ref = ptx::pack_f32x2(-m, -m);
                     uint64_t sum[4] = {0ull, 0ull, 0ull, 0ull};
@@ -562,6 +562,7 @@ __global__ void __launch_bounds__(kPfThreads, 1) prefill_kernel(const __grid_con
                 z += weights(1);
                 if (__any_sync(0xffffffffu, live && !(z < kMostWeight))) {
                     // The row's first logits, ones far above m, or NaN: m moves to the largest.
+                    tmem_wait_st();   // these weights are written again
                     float mx = m;
 #pragma unroll
                     for (int e = 0; e < 128; e += 2) mx = max3(mx, s[e] * sl2f, s[e + 1] * sl2f);

@@ -338,7 +338,8 @@ class PagedCache:
     """A paged cache (kvec_paged_cache): holds its tensors, computes nothing.
 
     k_pages, v_pages bf16 or fp16 [num_pages][H_kv][page_size][d]; page_table int32 [batch][max_pages];
-    lens int32 [batch]; weights fp32 [num_pages][H_kv][page_size] or None.  All contiguous, on one device."""
+    lens int32 [batch]; weights fp32 [num_pages][H_kv][page_size] or None.  All contiguous, on one device.  Their
+    contents may change between calls; other tensors need another PagedCache."""
 
     def __init__(self, k_pages, v_pages, page_table, lens, weights=None):
         import torch as t
@@ -457,6 +458,8 @@ class KvecSelector:
 
     # ------------------------------------------------------------ decoding over pages
     # A small call is bound by its host time: messages are formed only where a check fails.
+    # stream: the call's (None: the current one); what it reads must be ready there, and what is made
+    # for it comes from that stream's memory.
 
     def _empty(self, shape, dtype, stream):
         """Memory that work on `stream` (None: the current one) may use at once, from that stream's pool."""
