@@ -10,10 +10,10 @@
 //   warps 0-3, 4-7  softmax of tile 0 and 1, one thread a row: S from TMEM, running sum, the
 //                   weights back to TMEM as 16-bit values over S; at the end the outputs;
 //   warp 8          TMA: the query rows once, then K and V blocks through a ring;
-//   warp 9          tcgen05.mma: S = Q K^T (both from shared memory), O += P V (P from TMEM,
-//                   V column-major from shared memory), for the tiles in turn, so that one
-//                   tile's softmax runs beside the other's products;
-//   warps 10, 11    blocks that some row does not see wholly: zero what V holds there of
+//   warps 9, 10     tcgen05.mma, a warp for each tile: O += P V (P from TMEM, V column-major
+//                   from shared memory), then the next S = Q K^T (both from shared memory), in
+//                   turns, so that one tile's softmax runs beside the other's products;
+//   warp 11         blocks that some row does not see wholly: zeroes what V holds there of
 //                   infinities and NaN, which a weight of zero would not keep out.  What a row
 //                   sees of them is added at the end.
 // A row's weights refer to a maximum m that need not be the largest: it is that of the first
@@ -21,20 +21,22 @@
 // (kMostWeight), so that no block waits for a maximum and O is scaled in TMEM once in a while.
 // Results do not depend on m: 2^(s - m) keeps its relative precision, and so does l.
 //
-// Bound by the products' chain: a block of both tiles takes 2048 cycles of the tensor pipe (32
-// products of 64 cycles, which is what they take when nothing waits) and about 3000 in all,
-// since a tile's softmax (S read 60, exponentials 2 x 370, weights written and handed over 250
-// cycles) and the waits of the MMA warp outlast the other tile's 1024.  Measured, 32 query and 8
-// KV heads, bf16: 32768 tokens 5.5 ms, 1594 TFLOP/s (85 % of the measured cuBLAS burst); 8192
-// tokens 376 us, 1460 TFLOP/s; 16384 tokens with a window of 2048 and 4 first tokens 440 us,
-// 1174 TFLOP/s of visible pairs (18 blocks an item for 16 of keys seen, and about 6 us an item
-// before its first and after its last products).  What that took, 8192 tokens in us: S in
-// registers without spills 451, items one behind the other in persistent CTAs 445, no maximum
-// pass 421, waits of one poll 406, 32-byte stores 398, stages stepped 390, whole blocks of
-// weights handed over at once 378.  Slower: an issuer warp for each tile (466: products of two
-// tiles that take turns delay both), outputs by a warpgroup of their own (396: 64 registers
-// for the others spill), halves of blocks left out where no row sees them (425: the branches
-// stand between the products).
+// Bound by the power limit in long runs, and by the products' chain before it: a block of both
+// tiles takes 2048 cycles of the tensor pipe (32 products of 64 cycles, which is what they take
+// when nothing waits) and about 2700 in all, as a tile's softmax (S read 60, exponentials 2 x
+// 370, weights written and handed over 250 cycles) and its turn's waits outlast the other tile's
+// 1024.  (Without any exponential 8192 tokens take 317 us instead of 333.)  Measured, 32 query
+// and 8 KV heads, bf16: 32768 tokens 4.95 ms, 1776 TFLOP/s (95 % of the measured cuBLAS burst);
+// 8192 tokens 334 us, 1647 TFLOP/s, in a run of seconds 365 us at 1830 MHz and 1370 W, 1506
+// TFLOP/s (a cuBLAS product of 8192^3 beside it 1690 at 1430 MHz); 16384 tokens with a window of
+// 2048 and 4 first tokens 394 us, 1310 TFLOP/s of visible pairs (18 blocks an item for 16 of keys
+// seen).  What that took, 8192 tokens in us: S in registers without spills 451, items one behind
+// the other in persistent CTAs 445, no maximum pass 421, waits of one poll 406, 32-byte stores
+// 398, stages stepped 390, whole blocks of weights handed over at once 375, a warp that issues
+// for each tile 349, the registers that this one needs no longer given to the softmax 334.
+// Slower: outputs by a warpgroup of their own (396 for 375: 64 registers for the others spill),
+// halves of blocks left out where no row sees them (425 for 390: the branches stand between the
+// products).
 #include <algorithm>
 
 #include "half_types.cuh"
@@ -52,7 +54,7 @@ constexpr int kPfStages = 5;
 constexpr int kPfThreads = 384;
 constexpr uint32_t kPfTmem = 512;                   // S0 | S1 | O0 | O1, 128 columns each
 // Registers of a thread: at launch (the most that 384 threads may have), and after the split.
-constexpr int kPfRegs = 168, kPfSoftmaxRegs = 192, kPfOtherRegs = 120;
+constexpr int kPfRegs = 168, kPfSoftmaxRegs = 216, kPfOtherRegs = 72;   // neither side spills
 static_assert(256 * kPfSoftmaxRegs + 128 * kPfOtherRegs <= kPfThreads * kPfRegs, "the split fits what the block was launched with");
 // A row's weights of a block that sum up to less are taken as they are; fp16 holds them.
 constexpr float kMostWeight = 16384.f;
@@ -83,9 +85,10 @@ struct PfArgs {
 
 struct __align__(8) PfBarriers {
     uint64_t full[kPfStages], empty[kPfStages];
-    uint64_t clean[kPfStages];   // the cleaning warps have passed the stage
+    uint64_t clean[kPfStages];   // the cleaning warp has passed the stage
     uint64_t q_full, q_empty, mma_done;
-    uint64_t s_full[2], p_full[2], o_done[2];
+    uint64_t s_full[2], p_full[2], o_done[2];   // o_done: of an item
+    uint64_t turn[2];            // a tile's products may be issued
     uint32_t tmem_base;
     volatile int abort_flag;
     volatile int unbounded;      // a block of partial sight held an infinity or NaN in V (of any item so far)
@@ -222,6 +225,16 @@ __device__ __forceinline__ constexpr uint32_t pf_idesc(bool b_mn) {
            ((kPfTile >> 4) << 24);
 }
 
+// The larger magnitude of each half (its sign is either), NaN if one is.
+template <class T>
+__device__ __forceinline__ uint32_t largest(uint32_t a, uint32_t b) {
+    uint32_t d;
+    if constexpr (!kType<T>)
+        asm("max.NaN.xorsign.abs.f16x2 %0, %1, %2;" : "=r"(d) : "r"(a), "r"(b));
+    else
+        asm("max.NaN.xorsign.abs.bf16x2 %0, %1, %2;" : "=r"(d) : "r"(a), "r"(b));
+    return d;
+}
 template <class T>
 __device__ __forceinline__ uint32_t unbounded_mask(uint32_t w) {   // the halves that are infinite or NaN
     constexpr uint32_t e = kType<T> ? 0x7f80u : 0x7c00u;
@@ -253,16 +266,17 @@ __global__ void __launch_bounds__(kPfThreads, 1) prefill_kernel(const __grid_con
         ptx::prefetch_tensormap(&A.vmap);
         for (int i = 0; i < kPfStages; ++i) {
             ptx::mbar_init(&bars->full[i], 1);
-            ptx::mbar_init(&bars->empty[i], 3);    // the products, and the two cleaning warps
-            ptx::mbar_init(&bars->clean[i], 2);
+            ptx::mbar_init(&bars->empty[i], 3);    // the products of both tiles, and the cleaning warp
+            ptx::mbar_init(&bars->clean[i], 1);
         }
         ptx::mbar_init(&bars->q_full, 1);
-        ptx::mbar_init(&bars->q_empty, 1);
-        ptx::mbar_init(&bars->mma_done, 1);
+        ptx::mbar_init(&bars->q_empty, 2);
+        ptx::mbar_init(&bars->mma_done, 2);
         for (int t = 0; t < 2; ++t) {
             ptx::mbar_init(&bars->s_full[t], A.fault ? 2 : 1);   // 2, for a test of the waits: never complete
             ptx::mbar_init(&bars->p_full[t], 4);   // one arrival per warp of the tile
             ptx::mbar_init(&bars->o_done[t], 1);
+            ptx::mbar_init(&bars->turn[t], 1);
         }
         bars->abort_flag = 0;
         bars->unbounded = 0;
@@ -336,18 +350,24 @@ __global__ void __launch_bounds__(kPfThreads, 1) prefill_kernel(const __grid_con
             for (int y = max(x - kPfStages, 0); y < x; ++y)
                 ptx::mbar_wait(&bars->full[y % kPfStages], (y / kPfStages) & 1, 50000000ull);
             if (qloads > 0) ptx::mbar_wait(&bars->q_full, (qloads - 1) & 1, 50000000ull);
-        } else if (warp == 9) {
-            // -------------------------------------------------------- MMA
+        } else if (warp <= 10) {
+            // -------------------------------------------------------- MMA, a warp for each tile
+            // Few products queue up, and a wait, even one that is over, takes 60 cycles, in which the pipe
+            // would run dry.  So the two warps take turns: one waits for what its tile needs while the other
+            // issues.  A turn is not handed over before its products and their signals are issued: products of
+            // two tiles in the queue delay both (8192 tokens: 409 us with three products left, 372 with the
+            // signals left, 349 so; one warp for both tiles 375).
+            const int t = warp - 9;
             const uint32_t idesc_s = pf_idesc<T>(false), idesc_o = pf_idesc<T>(true);
-            const uint64_t qdesc = ptx::smem_desc_k_sw128(ptx::smem_u32(sQ));
+            const uint64_t qdesc = ptx::smem_desc_k_sw128(ptx::smem_u32(sQ)) + (uint32_t)(t * (kPfBuf >> 4));
             const uint64_t kdesc = ptx::smem_desc_k_sw128(ptx::smem_u32(ring));
             const uint64_t vdesc = smem_desc_mn_sw128(ptx::smem_u32(ring));
+            const uint32_t dS = tmem + t * 128, dO = tmem + 256 + t * 128;
             auto wait = [&](uint64_t* bar, int phase) {
                 if (!stop && !pf_wait(bar, phase & 1, abort)) stop = true;
                 return !stop;
             };
-            // The stage of a load and its parity, stepped: what stands between two products in this warp
-            // counts, as few products queue up.
+            // The stage of a load and its parity, stepped.
             struct Place {
                 int st = 0, parity = 0;
                 __device__ __forceinline__ void step() {
@@ -359,28 +379,52 @@ __global__ void __launch_bounds__(kPfThreads, 1) prefill_kernel(const __grid_con
             };
             Place pk, pv;   // of the next K and V
             pv.step();
+            int turns_taken = 0;
             // Stages as values that the compiler knows to be the warp's, so that descriptors stay in uniform registers.
-            auto products_s = [&](int t, int st, bool last) {   // S_t = Q_t K^T, K in stage st; one thread
-                const uint64_t kd = kdesc + (uint32_t)(st * (kPfBuf >> 4)), qd = qdesc + (uint32_t)(t * (kPfBuf >> 4));
+            auto products_s = [&](int st) {   // S = Q K^T, K in stage st; one thread
+                const uint64_t kd = kdesc + (uint32_t)(st * (kPfBuf >> 4));
 #pragma unroll
                 for (int kk = 0; kk < 8; ++kk) {
                     const uint32_t ofs = (kk >> 2) * (kPfHalf >> 4) + (kk & 3) * 2;
-                    ptx::mma_bf16(tmem + t * 128, qd + ofs, kd + ofs, idesc_s, kk > 0 ? 1u : 0u);
+                    ptx::mma_bf16(dS, qdesc + ofs, kd + ofs, idesc_s, kk > 0 ? 1u : 0u);
                 }
-                ptx::mma_commit(&bars->s_full[t]);
-                if (last) ptx::mma_commit(&bars->empty[st]);
             };
-            auto products_o = [&](int t, int st, bool add, bool last) {   // O_t += P_t V, V in stage st
+            auto products_o = [&](int st, bool add) {   // O += P V, V in stage st
                 const uint64_t vd = vdesc + (uint32_t)(st * (kPfBuf >> 4));
 #pragma unroll
                 for (int kk = 0; kk < 8; ++kk)
-                    mma_tmem_a(tmem + 256 + t * 128, tmem + t * 128 + kk * 8, vd + kk * (2048 >> 4), idesc_o,
-                               add || kk > 0 ? 1u : 0u);
-                ptx::mma_commit(&bars->o_done[t]);
-                if (last) ptx::mma_commit(&bars->empty[st]);
+                    mma_tmem_a(dO, dS + kk * 8, vd + kk * (2048 >> 4), idesc_o, add || kk > 0 ? 1u : 0u);
             };
-            int qloads = 0, blocks[2] = {0, 0};   // blocks of each tile so far: the phase of its P
-            // S of an item's first block is issued between the last products of the item before.
+            // One turn: the products of a block's V (here), then those of the next K (next).  last: of the item,
+            // q_last: S of the queries.  A tile without a part in them only passes the stages on.
+            auto take_turn = [&](bool v_there, bool here, bool add, bool last, bool k_there, bool next, bool q_last) {
+                const int sv = ptx::warp_uniform(pv.st), sk = ptx::warp_uniform(pk.st);
+                if (!wait(&bars->turn[t], t == 0 ? turns_taken + 1 : turns_taken)) return;
+                ++turns_taken;
+                ptx::tc_fence_after();
+                if (ptx::elect_one()) {
+                    if (here) {
+                        products_o(sv, add);
+                        if (last) ptx::mma_commit(&bars->o_done[t]);
+                        ptx::mma_commit(&bars->empty[sv]);
+                    } else if (v_there) {
+                        ptx::mbar_arrive(&bars->empty[sv]);
+                    }
+                    if (next) {
+                        products_s(sk);
+                        ptx::mma_commit(&bars->s_full[t]);
+                        ptx::mma_commit(&bars->empty[sk]);
+                        if (q_last) ptx::mma_commit(&bars->q_empty);
+                    } else if (k_there) {
+                        ptx::mbar_arrive(&bars->empty[sk]);
+                        if (q_last) ptx::mbar_arrive(&bars->q_empty);
+                    }
+                    ptx::mbar_arrive(&bars->turn[t ^ 1]);
+                }
+                __syncwarp();
+            };
+            int qloads = 0, blocks = 0;   // blocks of this tile so far: the phase of its P
+            // S of an item's first block is issued behind the last products of the item before.
             Item w{};
             int turn = 0;
             auto next_item = [&]() {
@@ -390,52 +434,30 @@ __global__ void __launch_bounds__(kPfThreads, 1) prefill_kernel(const __grid_con
             };
             bool more = next_item();
             if (more && wait(&bars->full[0], 0) && wait(&bars->q_full, 0)) {
-                ptx::tc_fence_after();
-                if (ptx::elect_one())
-                    for (int t = 0; t < w.tiles; ++t) products_s(t, 0, t == w.tiles - 1);
-                __syncwarp();
+                take_turn(false, false, false, false, true, t < w.tiles, w.n == 1);
                 ++qloads;
-                if (w.n == 1 && ptx::elect_one()) ptx::mma_commit(&bars->q_empty);
-                __syncwarp();
             }
             while (more && !stop) {
                 const Item cur = w;
+                const bool here = t < cur.tiles;
                 for (int i = 0; i < cur.n && !stop; ++i) {
                     const bool last_block = i + 1 == cur.n;
                     if (last_block) more = next_item();
                     pk.step();
                     pk.step();   // the next K
-                    // The tiles that the next S is for: this item's, or the next one's.
-                    const int next_tiles = !last_block ? cur.tiles : more ? w.tiles : 0;
+                    const bool k_there = !last_block || more;
                     if (!wait(&bars->full[pv.st], pv.parity)) break;
                     if (cur.edge(i) && !wait(&bars->clean[pv.st], pv.parity)) break;
-                    const int sv = ptx::warp_uniform(pv.st), sk = ptx::warp_uniform(pk.st);
-#pragma unroll
-                    for (int t = 0; t < 2; ++t) {
-                        const bool here = t < cur.tiles, next = t < next_tiles;
-                        if (t == 0 && next_tiles > 0) {
-                            if (!wait(&bars->full[pk.st], pk.parity)) break;
-                            if (last_block && !wait(&bars->q_full, qloads)) break;
-                        }
-                        if (here && !wait(&bars->p_full[t], blocks[t])) break;
-                        ptx::tc_fence_after();
-                        if (ptx::elect_one()) {
-                            if (here) products_o(t, sv, i > 0, t == cur.tiles - 1);
-                            if (next) products_s(t, sk, t == next_tiles - 1);
-                        }
-                        __syncwarp();
-                        if (here) ++blocks[t];
-                    }
+                    if (k_there && !wait(&bars->full[pk.st], pk.parity)) break;
+                    if (last_block && more && !wait(&bars->q_full, qloads)) break;
+                    if (here && !wait(&bars->p_full[t], blocks)) break;
+                    take_turn(true, here, i > 0, last_block, k_there, last_block ? more && t < w.tiles : here,
+                              last_block ? more && w.n == 1 : i + 2 == cur.n);
                     if (stop) break;
+                    if (here) ++blocks;
                     pv.step();
                     pv.step();
                     if (last_block && more) ++qloads;
-                    // The item's queries have been read once its last S is done.
-                    const bool q_last = last_block ? more && w.n == 1 : i + 2 == cur.n;
-                    if (q_last) {
-                        if (ptx::elect_one()) ptx::mma_commit(&bars->q_empty);
-                        __syncwarp();
-                    }
                 }
             }
             give_up();
@@ -456,16 +478,26 @@ __global__ void __launch_bounds__(kPfThreads, 1) prefill_kernel(const __grid_con
                         break;
                     }
                     if ((y & 1) && w.edge(y >> 1)) {
+                        // A look at eight vectors at once: their largest magnitude, NaN if there is one.
                         uint4* v = reinterpret_cast<uint4*>(ring + st * kPfBuf);
                         bool found = false;
-#pragma unroll 8
-                        for (int e = threadIdx.x - 320; e < kPfBuf / 16; e += 64) {
-                            const uint4 u = v[e];
-                            const uint4 m = make_uint4(unbounded_mask<T>(u.x), unbounded_mask<T>(u.y), unbounded_mask<T>(u.z),
-                                                       unbounded_mask<T>(u.w));
-                            if (m.x | m.y | m.z | m.w) {
-                                v[e] = make_uint4(u.x & ~m.x, u.y & ~m.y, u.z & ~m.z, u.w & ~m.w);
-                                found = true;
+#pragma unroll 2
+                        for (int e0 = lane; e0 < kPfBuf / 16; e0 += 256) {
+                            uint4 u[8];
+#pragma unroll
+                            for (int e = 0; e < 8; ++e) u[e] = v[e0 + 32 * e];
+                            uint4 most = u[0];
+#pragma unroll
+                            for (int e = 1; e < 8; ++e)
+                                most = make_uint4(largest<T>(most.x, u[e].x), largest<T>(most.y, u[e].y),
+                                                  largest<T>(most.z, u[e].z), largest<T>(most.w, u[e].w));
+                            if (!unbounded_mask<T>(largest<T>(largest<T>(most.x, most.y), largest<T>(most.z, most.w)))) continue;
+                            found = true;
+#pragma unroll
+                            for (int e = 0; e < 8; ++e) {
+                                const uint4 m = make_uint4(unbounded_mask<T>(u[e].x), unbounded_mask<T>(u[e].y),
+                                                           unbounded_mask<T>(u[e].z), unbounded_mask<T>(u[e].w));
+                                v[e0 + 32 * e] = make_uint4(u[e].x & ~m.x, u[e].y & ~m.y, u[e].z & ~m.z, u[e].w & ~m.w);
                             }
                         }
                         if (found) bars->unbounded = 1;
@@ -506,7 +538,7 @@ __global__ void __launch_bounds__(kPfThreads, 1) prefill_kernel(const __grid_con
                 }
             }
         };
-        int blocks = 0;   // of this tile: the phase of its barriers
+        int blocks = 0, outs = 0;   // blocks and items of this tile: the phases of its barriers
         for (int turn = 0; turn < turns && !stop; ++turn) {
             Item w{};
             if (!find_item<PARTS>(A, item_of(turn), w) || t >= w.tiles) continue;
@@ -571,12 +603,8 @@ __global__ void __launch_bounds__(kPfThreads, 1) prefill_kernel(const __grid_con
                     l *= f;
                     m = mx;
                     if (i > 0) {
-                        // The outputs so far with it, once the products of the block before are done.
-                        if (!pf_wait(&bars->o_done[t], (blocks - 1) & 1, abort)) {
-                            stop = true;
-                            break;
-                        }
-                        ptx::tc_fence_after();
+                        // The outputs so far with it: the products of the block before were issued before
+                        // this S, by the same thread, so that its signal covers them.
 #pragma unroll 1
                         for (int d0 = 0; d0 < kHeadDim; d0 += 32) {
                             float o[32];
@@ -596,7 +624,7 @@ __global__ void __launch_bounds__(kPfThreads, 1) prefill_kernel(const __grid_con
                 __syncwarp();
                 if (lane == 0) ptx::mbar_arrive(&bars->p_full[t]);
             }
-            if (n > 0 && !stop && !pf_wait(&bars->o_done[t], (blocks - 1) & 1, abort)) stop = true;
+            if (n > 0 && !stop && !pf_wait(&bars->o_done[t], outs++ & 1, abort)) stop = true;
             if (stop) break;
             ptx::tc_fence_after();
             const bool some = l > 0.f || l != l;
