@@ -1431,8 +1431,10 @@ kvec_status kvec_prefill_attention(kvec_handle* h, int dtype, int batch, const i
         return fail(KVEC_ERR_UNSUPPORTED, "prefill attention supports up to 8 query heads per KV head (g = %d)", h->g);
     if (max_q == 0) return KVEC_OK;
     const int total_k = cu_k_host[batch];
-    const PrefillPlan plan = plan_prefill(batch, h->p.num_q_heads, h->p.num_kv_heads, max_q, max_k, within_length(window),
-                                          within_length(sinks), h->num_sms);
+    PrefillPlan plan = plan_prefill(batch, h->p.num_q_heads, h->p.num_kv_heads, max_q, max_k, within_length(window),
+                                    within_length(sinks), h->num_sms);
+    for (int b = 0; b < batch; ++b)
+        plan.used_pairs += ((long long)cu_q_host[b + 1] - cu_q_host[b] + 2 * plan.nq - 1) / (2 * plan.nq);
     if (!q || !out || (total_k > 0 && (!k || !v)) || (plan.scratch && !scratch))
         return fail(KVEC_ERR_INVALID_ARG, "a device pointer is NULL");
     if (scratch_bytes < plan.scratch)

@@ -179,6 +179,7 @@ struct PrefillPlan {
     int batch, Hkv;
     int nq;                   // queries of a 128-row tile
     int pairs;                // tile pairs of the longest sequence
+    long long used_pairs;     // of all sequences
     int max_blocks;           // most 128-key blocks that a pair sees
     int parts;                // that a pair's blocks are divided into
     size_t scratch;           // bytes, 0 for one part

@@ -9,7 +9,8 @@
 // K and V.  It walks the 128-key blocks that any of its rows sees:
 //   warps 0-3, 4-7  softmax of tile 0 and 1, one thread a row: S from TMEM, running sum, the
 //                   weights back to TMEM as 16-bit values over S; at the end the outputs;
-//   warp 8          TMA: the query rows once, then K and V blocks through a ring;
+//   warp 8          TMA: the query rows once, then K and V blocks through a ring; finds the items of
+//                   sequences of different lengths;
 //   warps 9, 10     tcgen05.mma, a warp for each tile: O += P V (P from TMEM, V column-major
 //                   from shared memory), then the next S = Q K^T (both from shared memory), in
 //                   turns, so that one tile's softmax runs beside the other's products;
@@ -26,18 +27,20 @@
 // when nothing waits) and about 2700 in all, as a tile's softmax (S read 60, exponentials 2 x
 // 370, weights written and handed over 250 cycles) and its turn's waits outlast the other tile's
 // 1024.  (Without any exponential 8192 tokens take 317 us instead of 333.)  Measured, 32 query
-// and 8 KV heads, bf16: 32768 tokens 4.95 ms, 1776 TFLOP/s (95 % of the measured cuBLAS burst);
-// 8192 tokens 334 us, 1647 TFLOP/s, in a run of seconds 365 us at 1830 MHz and 1370 W, 1506
+// and 8 KV heads, bf16: 32768 tokens 4.87 ms, 1806 TFLOP/s (96 % of the measured cuBLAS burst);
+// 8192 tokens 331 us, 1660 TFLOP/s, in a run of seconds 365 us at 1830 MHz and 1370 W, 1506
 // TFLOP/s (a cuBLAS product of 8192^3 beside it 1690 at 1430 MHz); 16384 tokens with a window of
-// 2048 and 4 first tokens 394 us, 1310 TFLOP/s of visible pairs (18 blocks an item for 16 of keys
-// seen).  What that took, 8192 tokens in us: S in registers without spills 451, items one behind
+// 2048 and 4 first tokens 393 us, 1314 TFLOP/s of visible pairs (18 blocks an item for 16 of keys
+// seen); 8192 and 5001 tokens together 466 us, 1620 TFLOP/s.  What that took, 8192 tokens in us: S in registers without spills 451, items one behind
 // the other in persistent CTAs 445, no maximum pass 421, waits of one poll 406, 32-byte stores
 // 398, stages stepped 390, whole blocks of weights handed over at once 375, a warp that issues
-// for each tile 349, the registers that this one needs no longer given to the softmax 334.
+// for each tile 349, the registers that this one needs no longer given to the softmax 334, the
+// next item looked up before its turn 330.
 // Slower: outputs by a warpgroup of their own (396 for 375: 64 registers for the others spill),
 // halves of blocks left out where no row sees them (425 for 390: the branches stand between the
 // products).
 #include <algorithm>
+#include <type_traits>
 
 #include "half_types.cuh"
 #include "kvec_internal.cuh"
@@ -51,10 +54,11 @@ constexpr int kPfTile = 128;                        // rows of a tile, keys of a
 constexpr int kPfHalf = kPfTile * 128;              // bytes of 128 rows x 64 columns
 constexpr int kPfBuf = 2 * kPfHalf;                 // a tile or block: 32 KB
 constexpr int kPfStages = 5;
+constexpr int kPfItems = 4;                         // items handed out and not yet taken by every warp
 constexpr int kPfThreads = 384;
 constexpr uint32_t kPfTmem = 512;                   // S0 | S1 | O0 | O1, 128 columns each
 // Registers of a thread: at launch (the most that 384 threads may have), and after the split.
-constexpr int kPfRegs = 168, kPfSoftmaxRegs = 216, kPfOtherRegs = 72;   // neither side spills
+constexpr int kPfRegs = 168, kPfSoftmaxRegs = 216, kPfOtherRegs = 72;   // neither side spills in its loops over blocks
 static_assert(256 * kPfSoftmaxRegs + 128 * kPfOtherRegs <= kPfThreads * kPfRegs, "the split fits what the block was launched with");
 // A row's weights of a block that sum up to less are taken as they are; fp16 holds them.
 constexpr float kMostWeight = 16384.f;
@@ -75,7 +79,7 @@ struct PfArgs {
     int g, nq;       // query heads of a KV head, queries of a tile
     int pairs;       // tile pairs of the longest sequence
     int parts;       // of a pair's blocks, each an item (1: none are split)
-    int items;       // pairs * batch * Hkv * parts
+    int items;       // pairs * batch * Hkv * parts: places for items, of which a short sequence leaves some unused
     float* part_o;   // [items][2][128][128] a part's sums P V, by row
     float2* part_ml; // [items][2][128] (m, l) of the rows
     Divisor by_per, by_heads;   // batch * Hkv, Hkv
@@ -83,12 +87,28 @@ struct PfArgs {
     int fault;       // test of the error path (kvec_set_test_fault): no S is ever complete
 };
 
-struct __align__(8) PfBarriers {
+// What a CTA works on: tiles 2 p and 2 p + 1 of sequence s, KV head h.
+struct alignas(16) Item {
+    int h, q0, k0;                // first rows of the sequence
+    int a, b;                     // the pair's queries [a, b) of the sequence
+    int tiles;                    // 1 or 2
+    int off;                      // position of query 0
+    int nsink, lo;                // the blocks seen: 0 .. nsink - 1, then from lo on
+    int i0, n;                    // of them this item's part: the n from the i0-th on (-1: the work is done)
+    int place;                    // among A.items
+    int whole_lo, whole_hi;       // the blocks from the whole_lo-th to before the whole_hi-th are seen by every row
+    __device__ __forceinline__ int block(int i) const { return i0 + i < nsink ? i0 + i : lo + i0 + i - nsink; }
+    __device__ __forceinline__ bool edge(int i) const { return i < whole_lo || i >= whole_hi; }
+};
+
+struct PfBarriers {
     uint64_t full[kPfStages], empty[kPfStages];
     uint64_t clean[kPfStages];   // the cleaning warp has passed the stage
     uint64_t q_full, q_empty, mma_done;
     uint64_t s_full[2], p_full[2], o_done[2];   // o_done: of an item
     uint64_t turn[2];            // a tile's products may be issued
+    uint64_t item_full[kPfItems], item_empty[kPfItems];
+    Item items[kPfItems];        // handed from the TMA warp to the others
     uint32_t tmem_base;
     volatile int abort_flag;
     volatile int unbounded;      // a block of partial sight held an infinity or NaN in V (of any item so far)
@@ -96,50 +116,37 @@ struct __align__(8) PfBarriers {
 
 constexpr int kPfSmem = 1024 + (2 + kPfStages) * kPfBuf + (int)sizeof(PfBarriers);
 
-// What a CTA works on: tiles 2 p and 2 p + 1 of sequence s, KV head h.
-struct Item {
-    int s, h, q0, k0, Lq, Lk;     // first rows and lengths
-    int a, b;                     // the pair's queries [a, b) of the sequence
-    int tiles;                    // 1 or 2
-    int off;                      // position of query 0
-    int nsink, lo;                // the blocks seen: 0 .. nsink - 1, then from lo on
-    int i0, n;                    // of them this item's part: the n from the i0-th on
-    int whole_lo, whole_hi;       // the blocks from the whole_lo-th to before the whole_hi-th are seen by every row
-    __device__ __forceinline__ int block(int i) const { return i0 + i < nsink ? i0 + i : lo + i0 + i - nsink; }
-    __device__ __forceinline__ bool edge(int i) const { return i < whole_lo || i >= whole_hi; }
+// Where a sequence's queries and keys begin, and how many there are.
+struct Rows {
+    int q0, Lq, k0, Lk;
+    __device__ __forceinline__ Rows(const PfArgs& A, int s) : q0(0), Lq(0), k0(0), Lk(0) {
+        if (s >= A.io.batch) return;
+        auto clamped = [](int v, int most) { return min(max(v, 0), most); };
+        q0 = clamped(__ldg(&A.io.cu_q[s]), A.io.total_q);
+        k0 = clamped(__ldg(&A.io.cu_k[s]), A.io.total_k);
+        Lq = max(clamped(__ldg(&A.io.cu_q[s + 1]), A.io.total_q) - q0, 0);
+        Lk = max(clamped(__ldg(&A.io.cu_k[s + 1]), A.io.total_k) - k0, 0);
+    }
 };
 
+// Part `part` of what KV head h of pair p of sequence s sees; false: the sequence has no such pair.
 template <bool PARTS>
-__device__ __forceinline__ bool find_item(const PfArgs& A, int x, Item& w) {
-    // The last tiles, which see the most keys, first; a pair's KV heads side by side.
+__device__ __forceinline__ bool make_item(const PfArgs& A, int p, int s, const Rows& r, int h, int part, Item& w) {
     const PrefillIO& io = A.io;
-    if (x >= A.items) return false;
-    int part = 0;
-    if constexpr (PARTS) {
-        part = x % A.parts;
-        x /= A.parts;
-    }
-    const int per = io.batch * io.Hkv;
-    const int top = A.by_per.divide(x);
-    const int p = A.pairs - 1 - top;
-    x -= top * per;
-    w.s = A.by_heads.divide(x);
-    w.h = x - w.s * io.Hkv;
-    auto clamped = [](int v, int most) { return min(max(v, 0), most); };
-    w.q0 = clamped(__ldg(&io.cu_q[w.s]), io.total_q);
-    w.k0 = clamped(__ldg(&io.cu_k[w.s]), io.total_k);
-    w.Lq = clamped(__ldg(&io.cu_q[w.s + 1]), io.total_q) - w.q0;
-    w.Lk = max(clamped(__ldg(&io.cu_k[w.s + 1]), io.total_k) - w.k0, 0);
+    w.h = h;
+    w.place = (((A.pairs - 1 - p) * io.batch + s) * io.Hkv + h) * A.parts + part;
+    w.q0 = r.q0;
+    w.k0 = r.k0;
     w.a = 2 * p * A.nq;
-    if (w.a >= w.Lq) return false;
-    w.b = min(w.a + 2 * A.nq, w.Lq);
+    if (w.a >= r.Lq) return false;
+    w.b = min(w.a + 2 * A.nq, r.Lq);
     w.tiles = w.b - w.a > A.nq ? 2 : 1;
-    w.off = w.Lk - w.Lq;
+    w.off = r.Lk - r.Lq;
     const int pa = w.off + w.a, pb = w.off + w.b - 1;    // first and last position
     w.nsink = w.lo = w.i0 = w.n = 0;
     if (pb >= 0) {
         w.lo = io.window ? max(pa - io.window + 1, 0) / kPfTile : 0;
-        w.nsink = min((min(io.sinks, w.Lk) + kPfTile - 1) / kPfTile, w.lo);
+        w.nsink = min((min(io.sinks, r.Lk) + kPfTile - 1) / kPfTile, w.lo);
         w.n = w.nsink + pb / kPfTile + 1 - w.lo;
         if constexpr (PARTS) {
             const int all = w.n;
@@ -155,6 +162,29 @@ __device__ __forceinline__ bool find_item(const PfArgs& A, int x, Item& w) {
     return true;
 }
 
+// The item of a place; false: there is none.
+template <bool PARTS>
+__device__ __forceinline__ bool item_at(const PfArgs& A, int x, Item& w) {
+    if (x >= A.items) return false;
+    int part = 0;
+    if constexpr (PARTS) {
+        part = x % A.parts;
+        x /= A.parts;
+    }
+    const int per = A.io.batch * A.io.Hkv;
+    const int top = A.by_per.divide(x);
+    x -= top * per;
+    const int s = A.by_heads.divide(x);
+    return make_item<PARTS>(A, A.pairs - 1 - top, s, Rows(A, s), x - s * A.io.Hkv, part, w);
+}
+
+// Of every gridDim.x items (or places for them) a CTA takes one, in turns from the front and
+// from the back: they cost less and less, so that the shares are even.
+__device__ __forceinline__ int item_of(int turn) {
+    const int c = blockIdx.x, G = gridDim.x;
+    return turn * G + (turn & 1 ? G - 1 - c : c);
+}
+
 // ptx::warp_wait; a phase that is over, the usual case, costs one poll and one vote.
 __device__ __forceinline__ bool pf_wait(uint64_t* bar, uint32_t parity, const volatile int* abort) {
     return __all_sync(0xffffffffu, ptx::mbar_try_wait(bar, parity)) || ptx::warp_wait(bar, parity, abort);
@@ -162,6 +192,66 @@ __device__ __forceinline__ bool pf_wait(uint64_t* bar, uint32_t parity, const vo
 
 // The n lowest bits, n clamped to [0, 32].
 __device__ __forceinline__ uint32_t low_bits(int n) { return n <= 0 ? 0u : n >= 32 ? 0xffffffffu : (1u << n) - 1u; }
+
+// The items in order: the last pairs, which see the most keys, first, then by sequence and head,
+// without the pairs that shorter sequences lack.  One warp walks them: pairs lo <= p < hi are
+// there in the same `count` sequences, those with hi pairs and more, and make up a run of items
+// from the base-th on.  A lane keeps one of the first 32 sequences.
+struct Finder {
+    const PfArgs& A;
+    const int lane;
+    const Rows mine;
+    int hi, lo, count = 0, base = 0;
+    __device__ __forceinline__ Finder(const PfArgs& args, int l)
+        : A(args), lane(l), mine(args, l), hi(args.pairs), lo(args.pairs) {}
+    __device__ __forceinline__ int pairs_of(int s) const {
+        const int Lq = s < 32 ? mine.Lq : Rows(A, s).Lq;
+        return min((int)(((unsigned)Lq + 2u * A.nq - 1u) / (2u * A.nq)), A.pairs);
+    }
+    // The x-th item, x larger than in the calls before.
+    __device__ __forceinline__ bool find(int x, Item& w) {
+        const int each = A.io.Hkv;   // items of a pair
+        while (x - base >= (hi - lo) * count * each) {
+            if (lo == 0) return false;
+            base += (hi - lo) * count * each;
+            hi = lo;
+            count = 0;
+            int below = 0;
+#pragma unroll 1
+            for (int s = lane; s - lane < A.io.batch; s += 32) {
+                const int p = pairs_of(s);
+                count += __popc(__ballot_sync(0xffffffffu, p >= hi));
+                below = max(below, p < hi ? p : 0);
+            }
+            lo = __reduce_max_sync(0xffffffffu, below);
+        }
+        int k = (x - base) / each;
+        const int h = x - base - k * each;
+        const int level = k / count;
+        k -= level * count;   // the k-th of the sequences
+#pragma unroll 1
+        for (int s = lane; s - lane < A.io.batch; s += 32) {
+            const uint32_t there = __ballot_sync(0xffffffffu, pairs_of(s) >= hi);
+            const uint32_t it = __ballot_sync(0xffffffffu, (there >> lane & 1u) && __popc(there & low_bits(lane)) == k);
+            if (it) {
+                const int from = __ffs(it) - 1;
+                Rows r = mine;
+                if (s >= 32) r = Rows(A, s - lane + from);
+                r.q0 = __shfl_sync(0xffffffffu, r.q0, from);
+                r.Lq = __shfl_sync(0xffffffffu, r.Lq, from);
+                r.k0 = __shfl_sync(0xffffffffu, r.k0, from);
+                r.Lk = __shfl_sync(0xffffffffu, r.Lk, from);
+                return make_item<false>(A, hi - 1 - level, s - lane + from, r, h, 0, w);
+            }
+            k -= __popc(there);
+        }
+        return false;   // never: `count` sequences are there
+    }
+};
+
+struct NoFinder {
+    __device__ __forceinline__ NoFinder(const PfArgs&, int) {}
+};
 
 // 32 bytes to a 32-byte aligned place.
 __device__ __forceinline__ void st_global_v8(void* p, const uint32_t* r) {
@@ -241,18 +331,15 @@ __device__ __forceinline__ uint32_t unbounded_mask(uint32_t w) {   // the halves
     return ((w & e) == e ? 0xffffu : 0u) | (((w >> 16) & e) == e ? 0xffff0000u : 0u);
 }
 
-__device__ __forceinline__ int item_of(int turn) {
-    const int c = blockIdx.x, G = gridDim.x;
-    return turn * G + (turn & 1 ? G - 1 - c : c);
-}
-
-// Persistent: of every gridDim.x items a CTA takes one, in turns from the front and from the
-// back (items cost less and less, so that the shares are even), and no role waits for an
-// item's end: the next one's K and V follow through the ring, its first S is formed behind the
-// last products of this one, while the softmax warps write their outputs.
+// Persistent: no role waits for an item's end: the next one's K and V follow through the ring,
+// its first S is formed behind the last products of this one, while the softmax warps write
+// their outputs.
 // PARTS: a pair's blocks are divided into several items, which leave sums for prefill_join_kernel.
-template <class T, bool PARTS>
+// RAGGED: the CTAs share out the items, which the TMA warp finds and hands to the others, instead
+// of the places for them, of which shorter sequences leave many unused.
+template <class T, bool PARTS, bool RAGGED>
 __global__ void __launch_bounds__(kPfThreads, 1) prefill_kernel(const __grid_constant__ PfArgs A) {
+    static_assert(!(PARTS && RAGGED), "items that are parts have a place each");
     extern __shared__ uint8_t pf_smem_raw[];
     // 1024-byte alignment for the swizzled operand tiles.
     uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(pf_smem_raw) + 1023) & ~uintptr_t(1023));
@@ -278,6 +365,10 @@ __global__ void __launch_bounds__(kPfThreads, 1) prefill_kernel(const __grid_con
             ptx::mbar_init(&bars->o_done[t], 1);
             ptx::mbar_init(&bars->turn[t], 1);
         }
+        for (int i = 0; i < kPfItems; ++i) {
+            ptx::mbar_init(&bars->item_full[i], 1);
+            ptx::mbar_init(&bars->item_empty[i], kPfThreads / 32 - 1);   // every warp but the one that hands out
+        }
         bars->abort_flag = 0;
         bars->unbounded = 0;
         ptx::fence_barrier_init();
@@ -293,13 +384,33 @@ __global__ void __launch_bounds__(kPfThreads, 1) prefill_kernel(const __grid_con
     asm volatile("griddepcontrol.wait;\n" ::: "memory");
     const uint32_t tmem = (uint32_t)ptx::warp_uniform((int)bars->tmem_base);
     const volatile int* const abort = &bars->abort_flag;
-    const int sinks = A.io.sinks, turns = (A.items + gridDim.x - 1) / gridDim.x;
+    const int sinks = A.io.sinks;
     bool stop = false;
     auto give_up = [&]() {
         if (stop && lane == 0) {
             bars->abort_flag = 1;
             atomicExch(A.io.err, 3);
         }
+    };
+    // The next item, the same for every warp; false: none is left.
+    int taken = 0;
+    const int turns = (A.items + gridDim.x - 1) / gridDim.x;
+    auto take_item = [&](Item& w) {
+        if constexpr (!RAGGED) {
+            while (taken < turns)
+                if (item_at<PARTS>(A, item_of(taken++), w)) return true;
+            return false;
+        }
+        const int slot = taken % kPfItems;
+        if (stop || !pf_wait(&bars->item_full[slot], (taken / kPfItems) & 1, abort)) {
+            stop = true;
+            return false;
+        }
+        w = bars->items[slot];
+        __syncwarp();
+        if (lane == 0) ptx::mbar_arrive(&bars->item_empty[slot]);
+        ++taken;
+        return w.n >= 0;
     };
     // A softmax thread holds a row of S: registers move to the two softmax warpgroups.
     if (warp >= 8) {
@@ -309,9 +420,33 @@ __global__ void __launch_bounds__(kPfThreads, 1) prefill_kernel(const __grid_con
             // -------------------------------------------------------- TMA
             const uint64_t policy = ptx::policy_evict_normal();
             int qloads = 0;
-            for (int turn = 0; turn < turns && !stop; ++turn) {
+            // The CTA's item of a turn, handed out while the one before is loaded.
+            auto hand_out = [&, finder = std::conditional_t<RAGGED, Finder, NoFinder>(A, lane)](int turn) mutable {
+                if constexpr (RAGGED) {
+                    const int slot = turn % kPfItems;
+                    Item w{};
+                    if (!finder.find(item_of(turn), w)) w.n = -1;
+                    if (turn >= kPfItems && !pf_wait(&bars->item_empty[slot], (turn / kPfItems - 1) & 1, abort)) stop = true;
+                    if (!stop && lane == 0) {
+                        bars->items[slot] = w;
+                        ptx::mbar_arrive(&bars->item_full[slot]);
+                    }
+                    __syncwarp();
+                }
+            };
+            hand_out(0);
+            for (int turn = 0; !stop; ++turn) {
                 Item w{};
-                if (!find_item<PARTS>(A, item_of(turn), w) || w.n == 0) continue;
+                if constexpr (RAGGED) {
+                    w = bars->items[turn % kPfItems];
+                    if (w.n < 0) break;
+                } else if (!take_item(w)) {
+                    break;
+                }
+                if (w.n == 0) {
+                    hand_out(turn + 1);
+                    continue;
+                }
                 auto load_kv = [&](int y) {   // load y of the item: K and V blocks alternate
                     const int st = x % kPfStages, round = x / kPfStages;
                     if (round > 0 && !pf_wait(&bars->empty[st], (round - 1) & 1, abort)) {
@@ -343,7 +478,9 @@ __global__ void __launch_bounds__(kPfThreads, 1) prefill_kernel(const __grid_con
                 }
                 __syncwarp();
                 ++qloads;
-                for (int y = 1; y < 2 * w.n && !stop; ++y) load_kv(y);
+                load_kv(1);
+                if (!stop) hand_out(turn + 1);
+                for (int y = 2; y < 2 * w.n && !stop; ++y) load_kv(y);
             }
             give_up();
             // Every issued copy lands before the CTA may exit.
@@ -395,69 +532,86 @@ __global__ void __launch_bounds__(kPfThreads, 1) prefill_kernel(const __grid_con
                 for (int kk = 0; kk < 8; ++kk)
                     mma_tmem_a(dO, dS + kk * 8, vd + kk * (2048 >> 4), idesc_o, add || kk > 0 ? 1u : 0u);
             };
-            // One turn: the products of a block's V (here), then those of the next K (next).  last: of the item,
-            // q_last: S of the queries.  A tile without a part in them only passes the stages on.
-            auto take_turn = [&](bool v_there, bool here, bool add, bool last, bool k_there, bool next, bool q_last) {
-                const int sv = ptx::warp_uniform(pv.st), sk = ptx::warp_uniform(pk.st);
-                if (!wait(&bars->turn[t], t == 0 ? turns_taken + 1 : turns_taken)) return;
+            // A turn begins once the other tile's is over.
+            auto begin_turn = [&]() {
+                if (!wait(&bars->turn[t], t == 0 ? turns_taken + 1 : turns_taken)) return false;
                 ++turns_taken;
                 ptx::tc_fence_after();
+                return true;
+            };
+            // The products of a block's V; a tile without rows only passes the stage on.  last: of the item.
+            auto issue_o = [&](bool here, bool add, bool last) {
+                const int st = ptx::warp_uniform(pv.st);
                 if (ptx::elect_one()) {
                     if (here) {
-                        products_o(sv, add);
+                        products_o(st, add);
                         if (last) ptx::mma_commit(&bars->o_done[t]);
-                        ptx::mma_commit(&bars->empty[sv]);
-                    } else if (v_there) {
-                        ptx::mbar_arrive(&bars->empty[sv]);
+                        ptx::mma_commit(&bars->empty[st]);
+                    } else {
+                        ptx::mbar_arrive(&bars->empty[st]);
                     }
-                    if (next) {
-                        products_s(sk);
-                        ptx::mma_commit(&bars->s_full[t]);
-                        ptx::mma_commit(&bars->empty[sk]);
-                        if (q_last) ptx::mma_commit(&bars->q_empty);
-                    } else if (k_there) {
-                        ptx::mbar_arrive(&bars->empty[sk]);
-                        if (q_last) ptx::mbar_arrive(&bars->q_empty);
-                    }
-                    ptx::mbar_arrive(&bars->turn[t ^ 1]);
                 }
+                __syncwarp();
+                pv.step();
+                pv.step();
+            };
+            // Those of a K.  last: with the item's queries.
+            auto issue_s = [&](bool here, bool last) {
+                const int st = ptx::warp_uniform(pk.st);
+                if (ptx::elect_one()) {
+                    if (here) {
+                        products_s(st);
+                        ptx::mma_commit(&bars->s_full[t]);
+                        ptx::mma_commit(&bars->empty[st]);
+                        if (last) ptx::mma_commit(&bars->q_empty);
+                    } else {
+                        ptx::mbar_arrive(&bars->empty[st]);
+                        if (last) ptx::mbar_arrive(&bars->q_empty);
+                    }
+                }
+                __syncwarp();
+                pk.step();
+                pk.step();
+            };
+            auto end_turn = [&]() {
+                if (ptx::elect_one()) ptx::mbar_arrive(&bars->turn[t ^ 1]);
                 __syncwarp();
             };
             int qloads = 0, blocks = 0;   // blocks of this tile so far: the phase of its P
-            // S of an item's first block is issued behind the last products of the item before.
-            Item w{};
-            int turn = 0;
+            Item w{}, next{};
             auto next_item = [&]() {
-                while (turn < turns)
-                    if (find_item<PARTS>(A, item_of(turn++), w) && w.n > 0) return true;
+                while (take_item(next))
+                    if (next.n > 0) return true;
                 return false;
             };
-            bool more = next_item();
-            if (more && wait(&bars->full[0], 0) && wait(&bars->q_full, 0)) {
-                take_turn(false, false, false, false, true, t < w.tiles, w.n == 1);
-                ++qloads;
+            // The item's first S, behind the last products of the one before.
+            auto wait_q = [&]() { return wait(&bars->full[pk.st], pk.parity) && wait(&bars->q_full, qloads++); };
+            auto first_s = [&]() { issue_s(t < next.tiles, next.n == 1); };
+            bool more = next_item() && wait_q();
+            if (more && begin_turn()) {
+                first_s();
+                end_turn();
             }
             while (more && !stop) {
-                const Item cur = w;
-                const bool here = t < cur.tiles;
-                for (int i = 0; i < cur.n && !stop; ++i) {
-                    const bool last_block = i + 1 == cur.n;
-                    if (last_block) more = next_item();
-                    pk.step();
-                    pk.step();   // the next K
-                    const bool k_there = !last_block || more;
-                    if (!wait(&bars->full[pv.st], pv.parity)) break;
-                    if (cur.edge(i) && !wait(&bars->clean[pv.st], pv.parity)) break;
-                    if (k_there && !wait(&bars->full[pk.st], pk.parity)) break;
-                    if (last_block && more && !wait(&bars->q_full, qloads)) break;
-                    if (here && !wait(&bars->p_full[t], blocks)) break;
-                    take_turn(true, here, i > 0, last_block, k_there, last_block ? more && t < w.tiles : here,
-                              last_block ? more && w.n == 1 : i + 2 == cur.n);
-                    if (stop) break;
-                    if (here) ++blocks;
-                    pv.step();
-                    pv.step();
-                    if (last_block && more) ++qloads;
+                w = next;
+                const bool here = t < w.tiles;
+                const int n = w.n;
+                for (int i = 0; i < n; ++i) {
+                    const bool last = i + 1 == n;
+                    if (last) more = next_item();
+                    if (stop || !wait(&bars->full[pv.st], pv.parity)) break;
+                    if (w.edge(i) && !wait(&bars->clean[pv.st], pv.parity)) break;
+                    if (!last && !wait(&bars->full[pk.st], pk.parity)) break;
+                    if (last && more && !wait_q()) break;
+                    if (here && !wait(&bars->p_full[t], blocks++)) break;
+                    if (!begin_turn()) break;
+                    issue_o(here, i > 0, last);
+                    if (!last) {
+                        issue_s(here, i + 2 == n);
+                    } else if (more) {
+                        first_s();
+                    }
+                    end_turn();
                 }
             }
             give_up();
@@ -468,9 +622,8 @@ __global__ void __launch_bounds__(kPfThreads, 1) prefill_kernel(const __grid_con
         } else {
             // -------------------------------------------------------- V blocks of partial sight
             // Every load is passed in turn: a parity says nothing of a stage several rounds ahead.
-            for (int turn = 0; turn < turns && !stop; ++turn) {
-                Item w{};
-                if (!find_item<PARTS>(A, item_of(turn), w)) continue;
+            Item w{};
+            while (!stop && take_item(w)) {
                 for (int y = 0; y < 2 * w.n; ++y, ++x) {
                     const int st = x % kPfStages;
                     if (!pf_wait(&bars->full[st], (x / kPfStages) & 1, abort)) {
@@ -539,9 +692,9 @@ __global__ void __launch_bounds__(kPfThreads, 1) prefill_kernel(const __grid_con
             }
         };
         int blocks = 0, outs = 0;   // blocks and items of this tile: the phases of its barriers
-        for (int turn = 0; turn < turns && !stop; ++turn) {
-            Item w{};
-            if (!find_item<PARTS>(A, item_of(turn), w) || t >= w.tiles) continue;
+        Item w{};
+        while (!stop && take_item(w)) {
+            if (t >= w.tiles) continue;
             const int query = w.a + t * A.nq + row_q;
             const bool live = row < A.nq * A.g && query < w.b;        // the row is a real one
             const int p = w.off + query;
@@ -632,7 +785,7 @@ __global__ void __launch_bounds__(kPfThreads, 1) prefill_kernel(const __grid_con
             const size_t at = (size_t)(w.q0 + query) * A.io.Hq + w.h * A.g + j;
             if constexpr (PARTS) {
                 // Sums and maximum as they are, for prefill_join_kernel.
-                const size_t prow = ((size_t)item_of(turn) * 2 + t) * kPfTile + row;
+                const size_t prow = ((size_t)w.place * 2 + t) * kPfTile + row;
                 float* dst = A.part_o + prow * kHeadDim;
 #pragma unroll 1
                 for (int c = 0; c < 4 && n > 0; ++c) {
@@ -698,7 +851,8 @@ __global__ void __launch_bounds__(32 * kPjWarps) prefill_join_kernel(const __gri
     const int first = blockIdx.x * A.parts, t = r / kPfTile, row = r % kPfTile;
     Item w{};
     const int query = row / A.g + t * A.nq;
-    const bool live = find_item<true>(A, first, w) && row < A.nq * A.g && w.a + query < w.b;
+    const int top = A.by_per.divide(blockIdx.x), sh = blockIdx.x - top * A.io.batch * A.io.Hkv, seq = A.by_heads.divide(sh);
+    const bool live = make_item<true>(A, A.pairs - 1 - top, seq, Rows(A, seq), sh - seq * A.io.Hkv, 0, w) && row < A.nq * A.g && w.a + query < w.b;
     if (!live) return;
     auto prow = [&](int i) { return ((size_t)(first + i) * 2 + t) * kPfTile + row; };
     float M = kNoLogit, L = 0.f;
@@ -721,10 +875,18 @@ __global__ void __launch_bounds__(32 * kPjWarps) prefill_join_kernel(const __gri
 }
 
 template <class T>
-cudaError_t launch_typed(const PfArgs& a, int num_sms, cudaStream_t st) {
+cudaError_t launch_typed(const PfArgs& a, long long used_pairs, int num_sms, cudaStream_t st) {
     const dim3 grid((unsigned)std::min(a.items, num_sms));
-    if (a.parts == 1) return launch_prio(prefill_kernel<T, false>, grid, dim3(kPfThreads), kPfSmem, st, 0, true, a);
-    cudaError_t e = launch_prio(prefill_kernel<T, true>, grid, dim3(kPfThreads), kPfSmem, st, 0, true, a);
+    // Places that shorter sequences leave unused make the shares uneven, unless the turns are many, while an
+    // item that is handed over costs half a microsecond more.  Shared out by place and by item, us: 8192 and 5001 tokens 503 and 465 (14
+    // turns), one of 8192 and four of 100 391 and 333 (34), 24 of 100 to 1000 133 and 116 (20); but 32 of 1000
+    // 289 and 308 (nothing unused), 32 of 1 to 4000 1064 and 1080 (106 turns).
+    const bool ragged = (long long)a.pairs * a.io.batch * 15 > used_pairs * 16 && a.items <= 64 * num_sms;
+    if (a.parts == 1)
+        return ragged
+                   ? launch_prio(prefill_kernel<T, false, true>, grid, dim3(kPfThreads), kPfSmem, st, 0, true, a)
+                   : launch_prio(prefill_kernel<T, false, false>, grid, dim3(kPfThreads), kPfSmem, st, 0, true, a);
+    cudaError_t e = launch_prio(prefill_kernel<T, true, false>, grid, dim3(kPfThreads), kPfSmem, st, 0, true, a);
     if (e != cudaSuccess) return e;
     return launch_prio(prefill_join_kernel<T>, dim3((unsigned)(a.items / a.parts), 2 * kPfTile / kPjWarps), dim3(32 * kPjWarps),
                        0, st, 0, true, a);
@@ -744,10 +906,12 @@ cudaError_t configure_prefill() {
     auto one = [&](auto kernel) {
         if (e == cudaSuccess) e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kPfSmem);
     };
-    one(prefill_kernel<__nv_bfloat16, false>);
-    one(prefill_kernel<__nv_bfloat16, true>);
-    one(prefill_kernel<__half, false>);
-    one(prefill_kernel<__half, true>);
+    one(prefill_kernel<__nv_bfloat16, false, false>);
+    one(prefill_kernel<__nv_bfloat16, false, true>);
+    one(prefill_kernel<__nv_bfloat16, true, false>);
+    one(prefill_kernel<__half, false, false>);
+    one(prefill_kernel<__half, false, true>);
+    one(prefill_kernel<__half, true, false>);
     return e;
 }
 
@@ -795,7 +959,7 @@ cudaError_t launch_prefill(const PrefillIO& io, const PrefillPlan& plan, int num
     if (e == cudaSuccess) e = encode_tensor_map(&a.kmap, io.dtype, 3, keys ? io.k : io.q, kd, ks, kb);
     if (e == cudaSuccess) e = encode_tensor_map(&a.vmap, io.dtype, 3, keys ? io.v : io.q, kd, ks, kb);
     if (e != cudaSuccess) return e;
-    return io.dtype == 1 ? launch_typed<__half>(a, num_sms, st) : launch_typed<__nv_bfloat16>(a, num_sms, st);
+    return io.dtype == 1 ? launch_typed<__half>(a, plan.used_pairs, num_sms, st) : launch_typed<__nv_bfloat16>(a, plan.used_pairs, num_sms, st);
 }
 
 }  // namespace kvec

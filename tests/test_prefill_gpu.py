@@ -271,3 +271,66 @@ def test_rows_that_fill_no_tile_do_not_matter():
     selector(8, 8).prefill_attention(*big, cu8, cu8.cuda())      # leaves NaN in shared memory
     got = selector(7, 1).prefill_attention(q, k, v, cu, cu.cuda(), ck, ck.cuda())
     assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+
+
+# Sequences of very different lengths: of the places for the longest one's tiles most are unused.
+RAGGED = [
+    [1500] + [60] * 3, [1, 0, 700, 0, 0, 130, 2000], [100] * 40 + [1300], [0] * 35 + [900, 5] + [0] * 20,
+    list(range(0, 640, 10)),                              # 64 lengths, each with its own number of tiles
+]
+
+
+@pytest.mark.parametrize("lens", RAGGED)
+@pytest.mark.parametrize("Hq,Hkv,window,sinks", [(8, 8, 0, 0), (32, 8, 0, 0), (28, 4, 100, 3)])
+def test_sequences_of_very_different_lengths(lens, Hq, Hkv, window, sinks):
+    q, k, v = tensors(lens, lens, Hq, Hkv, torch.bfloat16, sum(lens), 2.0)
+    check(q, k, v, lens, lens, window, sinks)
+    keys = [n + 37 * (i % 3) for i, n in enumerate(lens)]
+    q, k, v = tensors(lens, keys, Hq, Hkv, torch.float16, sum(lens) + 1, 2.0)
+    check(q, k, v, lens, keys, window, sinks)
+
+
+def test_lengths_on_the_device_below_those_announced():
+    # A captured call is replayed with shorter sequences: what the device says counts, rows behind it stay.
+    lens, then = [900, 300, 1200, 40], [700, 0, 260, 39]
+    q, k, v = tensors(lens, lens, 32, 8, torch.bfloat16, 77)
+    sel, cu = selector(32, 8), cu_of(lens)
+    dev = cu.cuda()
+    out, lse = torch.empty_like(q), torch.empty(q.shape[:2], device="cuda")
+    run = lambda: sel.prefill_attention(q, k, v, cu, dev, cu, dev, out=out, lse=lse)
+    run()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        run()
+    dev.copy_(cu_of(then))
+    out.fill_(7.0)
+    graph.replay()
+    kvec.kvec_sync_status(sel.handle)
+    n = sum(then)
+    ref, rl, mass = reference(q[:n], k[:n], v[:n], then, then, 0, 0, D ** -0.5)
+    u = torch.finfo(torch.bfloat16).eps / 2
+    assert torch.all((out[:n].double() - ref).abs() <= u * ref.abs() + (u + 2e-5) * mass)
+    assert torch.all((lse[:n].double() - rl).abs() <= 2e-5 + 2.0 ** -22 * rl.abs())
+    assert torch.all(out[n:] == 7.0)
+
+
+def test_a_wait_that_runs_out_among_sequences_of_different_lengths():
+    lens = [2000, 100, 300, 50]
+    q, k, v = tensors(lens, lens, 32, 8, torch.bfloat16, 78)
+    sel = kvec.KvecSelector(kvec.make_params(32, 8, num_ext_heads=1, max_batch=64, max_seqlen=64, max_layers=1))
+    cu = cu_of(lens)
+    run = lambda: sel.prefill_attention(q, k, v, cu, cu.cuda())[0]
+    want = run().clone()
+    kvec.kvec_sync_status(sel.handle)
+    try:
+        kvec.kvec_set_test_fault(4)
+        run()
+        with pytest.raises(kvec.KvecError) as e:
+            kvec.kvec_sync_status(sel.handle)
+        assert e.value.status == kvec.KVEC_ERR_DEVICE_TIMEOUT
+    finally:
+        kvec.kvec_set_test_fault(0)
+    kvec.kvec_sync_status(sel.handle)
+    assert torch.equal(run(), want)
+    sel.close()
