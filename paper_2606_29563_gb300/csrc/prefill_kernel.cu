@@ -31,7 +31,8 @@
 // 8192 tokens 331 us, 1660 TFLOP/s, in a run of seconds 365 us at 1830 MHz and 1370 W, 1506
 // TFLOP/s (a cuBLAS product of 8192^3 beside it 1690 at 1430 MHz); 16384 tokens with a window of
 // 2048 and 4 first tokens 393 us, 1314 TFLOP/s of visible pairs (18 blocks an item for 16 of keys
-// seen); 8192 and 5001 tokens together 466 us, 1620 TFLOP/s.  What that took, 8192 tokens in us: S in registers without spills 451, items one behind
+// seen); 8192 and 5001 tokens together 466 us, 1620 TFLOP/s.  What that took, 8192 tokens in
+// us: S in registers without spills 451, items one behind
 // the other in persistent CTAs 445, no maximum pass 421, waits of one poll 406, 32-byte stores
 // 398, stages stepped 390, whole blocks of weights handed over at once 375, a warp that issues
 // for each tile 349, the registers that this one needs no longer given to the softmax 334, the
