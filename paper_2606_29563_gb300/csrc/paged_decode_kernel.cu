@@ -23,9 +23,9 @@
 //
 // HBM-bound when there is much to read: 131072 slots of 8 heads (537 MB) in 84 us, 6.4 TB/s, 94 %
 // of the measured copy rate; 64 rows of 1024 to 2048 slots of 4 heads and 7 query heads each (203 MB
-// with the weights) in 54 us, of which the reading takes 31: before it lie the lengths, the
-// list, the pages' numbers and the first copies (4 us), behind it the merges, the join and the
-// weights, each a chain of loads.  512 slots 6.2 us, the same chain once.
+// with the weights) in 48 us, of which the reading takes 31: before it lie the lengths, the
+// list, the pages' numbers and the first copies (4 us), behind it the merge, the weights (7 us, each
+// round a chain of loads) and an empty join.  512 slots 6.2 us, the same chain once.
 #include "half_types.cuh"
 #include "kvec_internal.cuh"
 #include "sm100_ptx.cuh"
@@ -50,7 +50,9 @@ constexpr int kPdSmem = kPdWarps * kPdStages * kPdStage + 1024;
 constexpr int kPdCtasPerSm = 2;
 constexpr int kPdMaxCluster = 8;
 constexpr int kPdHeads = 8;                  // most query heads of a KV head
-constexpr int kJoinRows = 1024;              // slots of a join block's weights
+constexpr int kPairCost = 12;                // what beginning and ending a pair takes, in blocks
+constexpr int kJoinThreads = 128;
+constexpr int kJoinRows = 8 * kJoinThreads;  // slots of a join block's weights, two times four a thread
 // The maximum before the first logit: the lowest finite value, so that a logit of minus
 // infinity gets the weight 2^-inf = 0 there too, and not 2^(-inf + inf).
 constexpr float kNoLogit = -3.402823466e38f;
@@ -63,9 +65,9 @@ struct PdArgs {
     float* part_o;            // [2 * ctas][8][128] shares of split pairs, unnormalised
     float2* part_ml;          // [2 * ctas][8] their maxima and sums
     int ctas;                 // that share the list of blocks
+    int pairs;                // batch * Hkv where a CTA each may do, else 0
     int nbmax;                // most visible blocks of a pair
     int g;
-    int join_heads;           // query heads of a block of the join
     float sl2;                // scale * log2(e)
     int fault;                // test of the error path (kvec_set_test_fault): warp 0 of CTA 0 loads nothing
 };
@@ -116,58 +118,85 @@ struct Walker {
     }
 };
 
-// The list of all blocks as a warp sees it: lane l holds the blocks of the sequences
-// l * per .. l * per + per - 1, over all KV heads.
+// The list of all blocks as a warp sees it: lane l holds those of the sequences l * per .. l *
+// per + per - 1, over all KV heads.  Ahead of a pair's blocks stand kPairCost places without one,
+// so that a share of many short pairs does not take longer than others (32 rows of 100 to 4000
+// slots 75 us without, 68 with 4, 60 with 8, 56 with 12 and 16, 58 with 28).
 struct List {
-    int per;
-    long long before, mine, total;   // of the lanes before, of this lane, of all
+    int per, longest;                // most blocks of a pair
+    int pairs_before, pairs;         // with blocks: of the lanes before, of all
+    long long before, mine, total;   // places: of the lanes before, of this lane, of all
+    __device__ __forceinline__ static int places(const Visible& v) { return v.nb ? v.nb + kPairCost : 0; }
     __device__ __forceinline__ void init(const PdArgs& A) {
         const int lane = threadIdx.x & 31;
         per = (A.io.batch + 31) >> 5;
         mine = 0;
+        int most = 0, own = 0;
         for (int k = 0; k < per; ++k) {
             const int s = lane * per + k;
             if (s >= A.io.batch) break;
             Visible v;
             v.init(A, s);
-            mine += v.nb;
+            mine += places(v);
+            own += v.nb ? A.io.Hkv : 0;
+            most = max(most, v.nb);
         }
+        longest = __reduce_max_sync(0xffffffffu, most);
         mine *= A.io.Hkv;
         long long upto = mine;
+        int upto_pairs = own;
 #pragma unroll
         for (int o = 1; o < 32; o <<= 1) {
             const long long y = __shfl_up_sync(0xffffffffu, upto, o);
-            if (lane >= o) upto += y;
+            const int z = __shfl_up_sync(0xffffffffu, upto_pairs, o);
+            if (lane >= o) {
+                upto += y;
+                upto_pairs += z;
+            }
         }
         before = upto - mine;
+        pairs_before = upto_pairs - own;
         total = __shfl_sync(0xffffffffu, upto, 31);
+        pairs = __shfl_sync(0xffffffffu, upto_pairs, 31);
     }
-    // The place of block `at`.
-    __device__ __forceinline__ void seek(const PdArgs& A, long long at, Walker& w) const {
+    // Whether each pair is a CTA's.  That saves the join, but the longest pair must not hold up the others: a
+    // block takes a CTA alone 0.25 us, all places together take 0.0013 us each, and the join and the shares'
+    // ends about 5 us.  Measured, by pair and by share: 64 rows of 1024 to 2048 slots 48 and 54, 64 of
+    // 200 to 3200 65 and 54, 30 of 100 to 3100 58 and 44, one of 8000 beside 31 of 500 129 and 28.
+    __device__ __forceinline__ bool whole_pairs(const PdArgs& A) const {
+        return A.pairs && (long long)longest * 190 <= total + 20 * 190;
+    }
+    // The first block from place `at` on; returns how many are before it.
+    __device__ __forceinline__ long long seek(const PdArgs& A, long long at, Walker& w) const {
         const uint32_t past = __ballot_sync(0xffffffffu, at < before + mine);
         w.s = A.io.batch;
         w.h = w.i = 0;
         w.v.nb = 0;
-        if (!past) return;
+        if (!past) return total - (long long)pairs * kPairCost;
         const int l = __ffs(past) - 1;
+        const long long whole = at;
         at -= __shfl_sync(0xffffffffu, before, l);
+        int p = __shfl_sync(0xffffffffu, pairs_before, l);
         for (w.s = l * per;; ++w.s) {
             w.v.init(A, w.s);
-            const long long here = (long long)w.v.nb * A.io.Hkv;
+            const long long here = (long long)places(w.v) * A.io.Hkv;
             if (at < here) break;
             at -= here;
+            p += here ? A.io.Hkv : 0;
         }
-        w.h = (int)at / w.v.nb;          // at < nb * Hkv <= 2^21
-        w.i = (int)at - w.h * w.v.nb;
+        w.h = (int)at / places(w.v);          // at < 2^22
+        const int i = (int)at - w.h * places(w.v);
+        w.i = max(i - kPairCost, 0);
+        return whole - (long long)(p + w.h) * kPairCost - min(i, kPairCost);
     }
-    // Blocks of the sequences before s.
-    __device__ __forceinline__ long long blocks_before(const PdArgs& A, int s) const {
+    // Places of the sequences before s.
+    __device__ __forceinline__ long long places_before(const PdArgs& A, int s) const {
         const int l = s / per;
         long long b = __shfl_sync(0xffffffffu, before, l);
         for (int k = l * per; k < s; ++k) {
             Visible v;
             v.init(A, k);
-            b += (long long)v.nb * A.io.Hkv;
+            b += (long long)places(v) * A.io.Hkv;
         }
         return b;
     }
@@ -289,9 +318,17 @@ __global__ void __launch_bounds__(kPdThreads, kPdCtasPerSm) paged_decode_kernel(
     } else {
         List list;
         list.init(A);
-        const long long at = share_start(list.total, blockIdx.x, A.ctas);
-        count = (int)(share_start(list.total, blockIdx.x + 1, A.ctas) - at);
-        list.seek(A, at, cur);
+        if (list.whole_pairs(A)) {
+            cur.s = blockIdx.x / Hkv;
+            cur.h = blockIdx.x - cur.s * Hkv;
+            cur.i = cur.v.nb = 0;
+            if ((int)blockIdx.x < A.pairs) cur.v.init(A, cur.s);
+            count = cur.v.nb;
+        } else {
+            const long long first = list.seek(A, share_start(list.total, blockIdx.x, A.ctas), cur);
+            Walker end;
+            count = (int)(list.seek(A, share_start(list.total, blockIdx.x + 1, A.ctas), end) - first);
+        }
     }
 
     uint8_t* ring = smem + warp * (kPdStages * kPdStage);
@@ -563,96 +600,50 @@ __global__ void __launch_bounds__(kPdThreads, kPdCtasPerSm) paged_decode_kernel(
         for (int i = 0; i < kPdStages; ++i) ptx::mbar_wait(&full[warp][i], (phases >> i) & 1u, 20000000ull);
 }
 
-// The pairs whose blocks several CTAs share.  The first blocks x of (x, h, s) join the outputs of
-// join_heads query heads each; the others add the weights, kJoinRows slots each.  (A thread finds a share, so that the shares'
-// places, sums and outputs are each read at once: one thread in a loop over the 38 shares of
-// 131072 slots took 58 us.)
+// The pairs whose blocks several CTAs share.  Block x = 0 of (x, h, s) joins the outputs, a warp a query head, the
+// others add the weights, kJoinRows slots each.  (A lane finds a share's place and sums, and eight shares' outputs are
+// read at once: one thread in a loop over the 38 shares of 131072 slots took 58 us.  Six blocks resident on an
+// SM: eight spill, 64 rows take the same but a window of 4096 in 16 caches 55.5 us instead of 53.6.)
 template <class T>
-__global__ void __launch_bounds__(kHeadDim) paged_join_kernel(const __grid_constant__ PdArgs A) {
-    extern __shared__ float2 share[];                 // (place as an int, factor) of the output block's shares
-    __shared__ float fm[kPdHeads], finv[kPdHeads], red[2][kHeadDim / 32];
-    const int h = blockIdx.y, s = blockIdx.z, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = A.g;
+__global__ void __launch_bounds__(kJoinThreads, 6) paged_join_kernel(const __grid_constant__ PdArgs A) {
+    extern __shared__ float2 share[];                 // [shares][kPdHeads] (place as an int, maximum)
+    __shared__ float fm[kPdHeads], finv[kPdHeads];
+    const int h = blockIdx.y, s = blockIdx.z, lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = A.g;
     Visible v;
     v.init(A, s);
-    const int joins = (g + A.join_heads - 1) / A.join_heads;
-    const bool weights = (int)blockIdx.x >= joins;
-    const int i0 = ((int)blockIdx.x - joins) * (kJoinRows / kPdBlock);
-    const int j0 = (int)blockIdx.x * A.join_heads, j1 = min(j0 + A.join_heads, g);
-    T* const out = reinterpret_cast<T*>(A.io.out) + ((size_t)s * A.io.Hq + (size_t)h * g) * kHeadDim + tid;
+    const bool weights = blockIdx.x > 0;
+    const int i0 = ((int)blockIdx.x - 1) * (kJoinRows / kPdBlock);
     // The lengths were complete before the kernel that this one waits for began.
     List list;
     list.init(A);
-    const long long total = list.total, p0 = list.blocks_before(A, s) + (long long)h * v.nb, p1 = p0 + v.nb;
-    const int c0 = v.nb ? (int)quotient((p0 + 1) * A.ctas - 1, total) : 0, c1 = v.nb ? (int)quotient(p1 * A.ctas - 1, total) : 0;
+    // Nothing to join: finished by its CTA, or a block of slots that the sequence does not have.
+    bool done = list.whole_pairs(A) || i0 >= v.nb;
+    const long long total = list.total;
+    long long p0 = 0;
+    int c0 = 0, c1 = 0;
+    if (!done) {
+        p0 = list.places_before(A, s) + (long long)h * List::places(v);
+        c0 = (int)quotient((p0 + kPairCost + 1) * A.ctas - 1, total);
+        c1 = (int)quotient((p0 + kPairCost + v.nb) * A.ctas - 1, total);
+        done = c0 == c1;
+    }
     asm volatile("griddepcontrol.launch_dependents;\n" ::: "memory");
     asm volatile("griddepcontrol.wait;\n" ::: "memory");
-    if (v.nb == 0) {
-        if (!weights)
-            for (int j = j0; j < j1; ++j) out[j * kHeadDim] = T(0.f);
-        return;
-    }
-    // Finished by its CTA, or a block of slots that the sequence does not have.
-    if (c0 == c1 || i0 >= v.nb) return;
-    // The place of CTA c's share, -1 if it has no blocks (there are fewer than CTAs): its first
-    // segment's, unless the pair begins inside it, as it may in c0's.
-    const int first = c0 * 2 + (share_start(total, c0, A.ctas) < p0 ? 1 : 0);
-    auto place = [&](int c) {
-        if (c == c0) return first;
-        return total < A.ctas && share_start(total, c, A.ctas) == share_start(total, c + 1, A.ctas) ? -1 : c * 2;
-    };
-    for (int j = j0; !weights && j < j1; ++j) {
+    T* const out = reinterpret_cast<T*>(A.io.out) + ((size_t)s * A.io.Hq + (size_t)h * g) * kHeadDim + lane * 4;
+    if (v.nb == 0 && !weights)
+        for (int j = warp; j < g; j += kJoinThreads / 32) *reinterpret_cast<uint2*>(out + j * kHeadDim) = make_uint2(0u, 0u);
+    if (done) return;
+    for (int j = warp; j < g; j += kJoinThreads / 32) {   // a lane a share
         float M = kNoLogit, L = 0.f;
-        for (int c = tid; c <= c1 - c0; c += kHeadDim) {
-            const int at = place(c0 + c);
+        for (int c = lane; c <= c1 - c0; c += 32) {
+            // A CTA's first segment, unless the pair begins inside its share, as it may in c0's; none if the CTA has
+            // no blocks (there are fewer than CTAs).
+            const int cta = c0 + c;
+            int at = cta * 2;
+            if (c == 0) at += share_start(total, c0, A.ctas) < p0 ? 1 : 0;
+            else if (total < A.ctas && share_start(total, cta, A.ctas) == share_start(total, cta + 1, A.ctas)) at = -1;
             const float2 ml = at < 0 ? make_float2(kNoLogit, 0.f) : A.part_ml[at * kPdHeads + j];
-            share[c] = make_float2(__int_as_float(at), ml.x);
-            M = fmaxf(M, ml.x);
-        }
-#pragma unroll
-        for (int o = 16; o; o >>= 1) M = fmaxf(M, __shfl_xor_sync(0xffffffffu, M, o));
-        if (lane == 0) red[0][warp] = M;
-        __syncthreads();
-        M = fmaxf(fmaxf(red[0][0], red[0][1]), fmaxf(red[0][2], red[0][3]));
-        for (int c = tid; c <= c1 - c0; c += kHeadDim) {
-            const int at = __float_as_int(share[c].x);
-            const float f = at < 0 ? 0.f : ptx::ex2(share[c].y - M);
-            share[c].y = f;
-            if (at >= 0) L = fmaf(f, A.part_ml[at * kPdHeads + j].y, L);
-        }
-#pragma unroll
-        for (int o = 16; o; o >>= 1) L += __shfl_xor_sync(0xffffffffu, L, o);
-        if (lane == 0) red[1][warp] = L;
-        __syncthreads();
-        L = (red[1][0] + red[1][1]) + (red[1][2] + red[1][3]);
-        float O = 0.f;
-        const float* part = A.part_o + (size_t)j * kHeadDim + tid;
-        constexpr size_t kPlace = (size_t)kPdHeads * kHeadDim;
-        if (total >= A.ctas) {   // no share is empty: eight reads at once, with no branch between them
-            int c = 0;
-            for (; c + 8 <= c1 - c0 + 1; c += 8) {
-                float o[8];
-#pragma unroll
-                for (int k = 0; k < 8; ++k) o[k] = part[__float_as_int(share[c + k].x) * kPlace];
-#pragma unroll
-                for (int k = 0; k < 8; ++k) O = fmaf(share[c + k].y, o[k], O);
-            }
-            for (; c <= c1 - c0; ++c) O = fmaf(share[c].y, part[__float_as_int(share[c].x) * kPlace], O);
-        } else {
-            for (int c = 0; c <= c1 - c0; ++c) {
-                const int at = __float_as_int(share[c].x);
-                if (at >= 0) O = fmaf(share[c].y, part[at * kPlace], O);
-            }
-        }
-        out[j * kHeadDim] = T(L > 0.f || L != L ? O / L : 0.f);
-        __syncthreads();   // the shares and sums are read before the next head's
-    }
-    if (!weights) return;
-    for (int j = warp; j < g; j += kHeadDim / 32) {   // a warp a query head, a lane a share
-        float M = kNoLogit, L = 0.f;
-        for (int c = c0 + lane; c <= c1; c += 32) {
-            const int at = place(c);
-            if (at < 0) continue;
-            const float2 ml = A.part_ml[at * kPdHeads + j];
+            share[c * kPdHeads + j] = make_float2(__int_as_float(at), ml.x);
             const float m = fmaxf(M, ml.x);
             L = fmaf(L, ptx::ex2(M - m), ml.y * ptx::ex2(ml.x - m));
             M = m;
@@ -664,13 +655,39 @@ __global__ void __launch_bounds__(kHeadDim) paged_join_kernel(const __grid_const
             L = fmaf(L, ptx::ex2(M - m), L2 * ptx::ex2(M2 - m));
             M = m;
         }
+        // (The two halves of a pair of lanes sum in different orders: lane 0's is taken.)
+        L = __shfl_sync(0xffffffffu, L, 0);
+        const bool some = L > 0.f || L != L;
         if (lane == 0) {
             fm[j] = M;
-            finv[j] = L > 0.f || L != L ? 1.f / L : 0.f;
+            finv[j] = some ? 1.f / L : 0.f;
+        }
+        __syncwarp();
+        if (!weights) {
+            float4 O = make_float4(0.f, 0.f, 0.f, 0.f);
+            const float* part = A.part_o + (size_t)j * kHeadDim + lane * 4;
+            for (int c = 0; c <= c1 - c0; c += 8) {
+                float4 o[8];
+                float f[8];
+#pragma unroll
+                for (int k = 0; k < 8; ++k) {
+                    const float2 sh = c + k <= c1 - c0 ? share[(c + k) * kPdHeads + j] : make_float2(__int_as_float(-1), kNoLogit);
+                    const int at = __float_as_int(sh.x);
+                    o[k] = at < 0 ? make_float4(0.f, 0.f, 0.f, 0.f)
+                                  : *reinterpret_cast<const float4*>(part + (size_t)at * (kPdHeads * kHeadDim));
+                    f[k] = ptx::ex2(sh.y - M);
+                }
+#pragma unroll
+                for (int k = 0; k < 8; ++k)
+                    O = make_float4(fmaf(f[k], o[k].x, O.x), fmaf(f[k], o[k].y, O.y), fmaf(f[k], o[k].z, O.z), fmaf(f[k], o[k].w, O.w));
+            }
+            *reinterpret_cast<uint2*>(out + j * kHeadDim) = some ? make_uint2(Half16<T>::pack(O.x / L, O.y / L), Half16<T>::pack(O.z / L, O.w / L))
+                                                  : make_uint2(0u, 0u);
         }
     }
+    if (!weights) return;
     __syncthreads();
-    add_weights<kHeadDim>(A, s, h, v, i0, min(v.nb, i0 + kJoinRows / kPdBlock), fm, finv);
+    add_weights<kJoinThreads>(A, s, h, v, i0, min(v.nb, i0 + kJoinRows / kPdBlock), fm, finv);
 }
 
 size_t round16(size_t x) { return (x + 15) & ~size_t(15); }
@@ -683,8 +700,8 @@ cudaError_t launch_typed(const PdArgs& a, cudaStream_t st) {
     // two blocks a warp and more; taken where that leaves a CTA 32 blocks and less (a quarter of
     // one a thread for the weights), else the list of all blocks.  Measured with weights, 8 KV
     // heads, in us by cluster and by list: one row of 4096 slots 13.3, of 8192 (list) 16.3; 512
-    // rows of 100 to 300 slots (a CTA each) 117 and 262, the list's CTAs ending a pair every 19
-    // blocks; 40 of 1000 slots (two CTAs each, more than a wave) 47.7 and 43.5, 256 of 1500 365 and 279.
+    // rows of 100 to 300 slots (a CTA each) 110 and 147; 40 of 1000 slots (two CTAs each, more than a
+    // wave) 47.7 and 39.5, 256 of 1500 365 and 272.
     const int pairs = a.io.batch * a.io.Hkv;
     int splits = 1;
     while (splits < kPdMaxCluster && (long long)pairs * splits * 2 <= a.ctas && a.nbmax >= kPdWarps * 2 * splits) splits *= 2;
@@ -708,9 +725,8 @@ cudaError_t launch_typed(const PdArgs& a, cudaStream_t st) {
     cudaError_t e = launch_prio(paged_decode_kernel<T, false>, dim3(a.ctas), dim3(kPdThreads), kPdSmem, st, 0, true, a);
     if (e != cudaSuccess) return e;
     const int rows = a.c.weights ? (a.nbmax * kPdBlock + kJoinRows - 1) / kJoinRows : 0;
-    const int joins = (a.g + a.join_heads - 1) / a.join_heads;
-    return launch_prio(paged_join_kernel<T>, dim3(joins + rows, a.io.Hkv, a.io.batch), dim3(kHeadDim),
-                       a.ctas * sizeof(float2), st, 0, true, a);
+    return launch_prio(paged_join_kernel<T>, dim3(1 + rows, a.io.Hkv, a.io.batch), dim3(kJoinThreads),
+                       a.ctas * kPdHeads * sizeof(float2), st, 0, true, a);
 }
 
 int visible_blocks(const PagedDecodeIO& io) {
@@ -753,12 +769,11 @@ cudaError_t launch_paged_decode(const PagedDecodeIO& io, const PagedCacheView& c
     a.c = c;
     a.io = io;
     a.g = io.Hq / io.Hkv;
-    // A block a query head where pairs are few, one for all of a pair's where they are many: 256
-    // pairs of 7 heads with weights 59.7 us a head, 63.4 all; 320 of 4 43.6 and 42.7, 2048 of 4 303 and 287.
-    a.join_heads = io.batch * io.Hkv > 2 * num_sms ? a.g : 1;
     a.sl2 = io.scale * 1.4426950408889634f;
     a.fault = test_fault() == 4 ? 1 : 0;
     a.ctas = share_ctas(num_sms);
+    const long long pairs = (long long)io.batch * io.Hkv;
+    a.pairs = pairs <= a.ctas && pairs * 4 >= a.ctas * 3ll ? (int)pairs : 0;
     a.nbmax = visible_blocks(io);
     const size_t slots = (size_t)a.ctas * 2 * kPdHeads;
     char* p = static_cast<char*>(io.scratch);

@@ -511,3 +511,46 @@ def test_a_bound_far_above_the_lengths(lens, weights):
     out = check_decode(selector(14, 2), q, cache, lens)
     for s, n in enumerate(lens):
         assert n or torch.all(out[s] == 0)
+
+
+def lengths_of(kind, batch):
+    if kind == "alike":                                   # a CTA each
+        return [600 + (37 * b) % 100 for b in range(batch - 2)] + [0, 555]
+    if kind == "one long":                                # the list of all blocks
+        return [5000] + [30 + b for b in range(batch - 1)]
+    return [(b * 389) % 1500 if b % 3 else b % 20 for b in range(batch)]
+
+
+@pytest.mark.parametrize("kind", ["alike", "one long", "mixed"])
+@pytest.mark.parametrize("Hq,Hkv,batch,window,sinks", [(8, 4, 60, 0, 0), (28, 4, 70, 0, 0), (16, 8, 30, 530, 20)])
+def test_pairs_about_as_many_as_ctas(kind, Hq, Hkv, batch, window, sinks):
+    gen = torch.Generator().manual_seed(batch + window)
+    lens = lengths_of(kind, batch)
+    cache, _ = make_cache(lens, Hkv, 64, torch.bfloat16, gen)
+    q = torch.randn((batch, Hq, D), generator=gen).to(torch.bfloat16).cuda()
+    check_decode(selector(Hq, Hkv), q, cache, lens, window=window, sinks=sinks)
+
+
+def test_a_captured_call_takes_lengths_of_every_kind():
+    # The way the work is divided follows the lengths on the device.
+    gen = torch.Generator().manual_seed(50)
+    batch, Hq, Hkv = 60, 8, 4
+    kinds = [lengths_of(k, batch) for k in ("alike", "one long", "mixed")]
+    cache, _ = make_cache([max(x) for x in zip(*kinds)], Hkv, 64, torch.bfloat16, gen)
+    q = torch.randn((batch, Hq, D), generator=gen).to(torch.bfloat16).cuda()
+    sel, first = selector(Hq, Hkv), cache.weights.clone()
+    out = torch.empty_like(q)
+    sel.paged_decode(q, cache, 5000, out=out)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        sel.paged_decode(q, cache, 5000, out=out)
+    for lens in kinds[1:] + kinds[:2]:
+        cache.lens.copy_(torch.tensor(lens, dtype=torch.int32))
+        cache.weights.copy_(first)
+        graph.replay()
+        kvec.kvec_sync_status(sel.handle)
+        got, weights = out.clone(), cache.weights.clone()
+        cache.weights.copy_(first)
+        want = check_decode(sel, q, cache, lens, max_len=5000)
+        assert torch.equal(got, want) and torch.equal(weights, cache.weights)
