@@ -616,8 +616,8 @@ __global__ void __launch_bounds__(kJoinThreads, 6) paged_join_kernel(const __gri
     // The lengths were complete before the kernel that this one waits for began.
     List list;
     list.init(A);
-    // Nothing to join: finished by its CTA, or a block of slots that the sequence does not have.
-    bool done = list.whole_pairs(A) || i0 >= v.nb;
+    // Nothing to join: nothing is seen, finished by its CTA, or a block of slots that the sequence does not have.
+    bool done = v.nb == 0 || list.whole_pairs(A) || i0 >= v.nb;
     const long long total = list.total;
     long long p0 = 0;
     int c0 = 0, c1 = 0;
