@@ -554,3 +554,15 @@ def test_a_captured_call_takes_lengths_of_every_kind():
         cache.weights.copy_(first)
         want = check_decode(sel, q, cache, lens, max_len=5000)
         assert torch.equal(got, want) and torch.equal(weights, cache.weights)
+
+
+def test_rotate_of_rows_that_overlap():
+    # Tokens 8 elements apart, as documented: the outputs made for them are packed all the same.
+    gen = torch.Generator().manual_seed(60)
+    base = torch.randn(2000, generator=gen).to(torch.bfloat16).cuda()
+    q, k = torch.as_strided(base, (6, 4, D), (8, D, 1)), torch.as_strided(base, (6, 2, D), (16, D, 1))
+    pos, tab = torch.arange(6, dtype=torch.int32).cuda(), rot_table(16, D).cuda()
+    got = selector(4, 2).rotate_append(q, k, None, pos, tab)
+    want = selector(4, 2).rotate_append(q.contiguous(), k.contiguous(), None, pos, tab)
+    assert all(x.is_contiguous() for x in got)
+    assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
