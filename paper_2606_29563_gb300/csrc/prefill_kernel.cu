@@ -27,19 +27,20 @@
 // when nothing waits) and about 2700 in all, as a tile's softmax (S read 60, exponentials 2 x
 // 370, weights written and handed over 250 cycles) and its turn's waits outlast the other tile's
 // 1024.  (Without any exponential 8192 tokens take 317 us instead of 333.)  Measured, 32 query
-// and 8 KV heads, bf16: 32768 tokens 4.87 ms, 1806 TFLOP/s (96 % of the measured cuBLAS burst);
-// 8192 tokens 331 us, 1660 TFLOP/s, in a run of seconds 365 us at 1830 MHz and 1370 W, 1506
+// and 8 KV heads, bf16: 32768 tokens 4.8 ms, 1830 TFLOP/s (97 % of the measured cuBLAS burst);
+// 8192 tokens 328 us, 1676 TFLOP/s, in a run of seconds 365 us at 1830 MHz and 1370 W, 1506
 // TFLOP/s (a cuBLAS product of 8192^3 beside it 1690 at 1430 MHz); 16384 tokens with a window of
-// 2048 and 4 first tokens 393 us, 1314 TFLOP/s of visible pairs (18 blocks an item for 16 of keys
-// seen); 8192 and 5001 tokens together 466 us, 1620 TFLOP/s.  What that took, 8192 tokens in
-// us: S in registers without spills 451, items one behind
-// the other in persistent CTAs 445, no maximum pass 421, waits of one poll 406, 32-byte stores
-// 398, stages stepped 390, whole blocks of weights handed over at once 375, a warp that issues
-// for each tile 349, the registers that this one needs no longer given to the softmax 334, the
-// next item looked up before its turn 330.
+// 2048 and 4 first tokens 391 us, 1320 TFLOP/s of visible pairs (18 blocks an item for 16 of keys
+// seen); 8192 and 5001 tokens together 467 us, 1617 TFLOP/s.  What that took, 8192 tokens in us:
+// S in registers without spills 451, items one behind the other in persistent CTAs 445, no
+// maximum pass 421, waits of one poll 406, 32-byte stores 398, stages stepped 390, whole blocks
+// of weights handed over at once 375, a warp that issues for each tile 349, the registers that
+// this one needs no longer given to the softmax 334, the next item looked up before its turn 331,
+// no branch between most turns' products 328.
 // Slower: outputs by a warpgroup of their own (396 for 375: 64 registers for the others spill),
 // halves of blocks left out where no row sees them (425 for 390: the branches stand between the
-// products).
+// products), products of 16 keys for a block of few first tokens (348 for 331, and in turns of
+// their own no gain: 394 for 391 with the window).
 #include <algorithm>
 #include <type_traits>
 
@@ -605,6 +606,25 @@ __global__ void __launch_bounds__(kPfThreads, 1) prefill_kernel(const __grid_con
                     if (!last && !wait(&bars->full[pk.st], pk.parity)) break;
                     if (last && more && !wait_q()) break;
                     if (here && !wait(&bars->p_full[t], blocks++)) break;
+                    if (here && !last) {   // most turns: nothing stands between the products
+                        const int sv = ptx::warp_uniform(pv.st), sk = ptx::warp_uniform(pk.st);
+                        if (!begin_turn()) break;
+                        if (ptx::elect_one()) {
+                            products_o(sv, i > 0);
+                            ptx::mma_commit(&bars->empty[sv]);
+                            products_s(sk);
+                            ptx::mma_commit(&bars->s_full[t]);
+                            ptx::mma_commit(&bars->empty[sk]);
+                            if (i + 2 == n) ptx::mma_commit(&bars->q_empty);
+                            ptx::mbar_arrive(&bars->turn[t ^ 1]);
+                        }
+                        __syncwarp();
+                        pv.step();
+                        pv.step();
+                        pk.step();
+                        pk.step();
+                        continue;
+                    }
                     if (!begin_turn()) break;
                     issue_o(here, i > 0, last);
                     if (!last) {
