@@ -581,30 +581,43 @@ __global__ void __launch_bounds__(kPfThreads, 1) prefill_kernel(const __grid_con
             };
             int qloads = 0, blocks = 0;   // blocks of this tile so far: the phase of its P
             Item w{}, next{};
+            // One item further and no more where they are handed out: those behind one that sees nothing come once
+            // the softmax warps have passed it, for which they may need the products that are still to be issued.
             auto next_item = [&]() {
-                while (take_item(next))
-                    if (next.n > 0) return true;
-                return false;
+                do {
+                    if (!take_item(next)) return false;
+                } while (!RAGGED && next.n == 0);
+                return true;
             };
-            // The item's first S, behind the last products of the one before.
+            auto sees = [&]() { return !RAGGED || next.n > 0; };
             auto wait_q = [&]() { return wait(&bars->full[pk.st], pk.parity) && wait(&bars->q_full, qloads++); };
             auto first_s = [&]() { issue_s(t < next.tiles, next.n == 1); };
-            bool more = next_item() && wait_q();
-            if (more && begin_turn()) {
+            // The first S of the next item that sees a key, in a turn of its own.
+            auto start = [&]() {
+                do {
+                    if (!next_item()) return false;
+                } while (!sees());
+                if (!wait_q() || !begin_turn()) return false;
                 first_s();
                 end_turn();
-            }
+                return true;
+            };
+            bool more = start();
             while (more && !stop) {
                 w = next;
+                bool joined = false;   // the next item's first S goes behind this one's last products
                 const bool here = t < w.tiles;
                 const int n = w.n;
                 for (int i = 0; i < n; ++i) {
                     const bool last = i + 1 == n;
-                    if (last) more = next_item();
+                    if (last) {
+                        more = next_item();
+                        joined = more && sees();
+                    }
                     if (stop || !wait(&bars->full[pv.st], pv.parity)) break;
                     if (w.edge(i) && !wait(&bars->clean[pv.st], pv.parity)) break;
                     if (!last && !wait(&bars->full[pk.st], pk.parity)) break;
-                    if (last && more && !wait_q()) break;
+                    if (last && joined && !wait_q()) break;
                     if (here && !wait(&bars->p_full[t], blocks++)) break;
                     if (here && !last) {   // most turns: nothing stands between the products
                         const int sv = ptx::warp_uniform(pv.st), sk = ptx::warp_uniform(pk.st);
@@ -629,11 +642,12 @@ __global__ void __launch_bounds__(kPfThreads, 1) prefill_kernel(const __grid_con
                     issue_o(here, i > 0, last);
                     if (!last) {
                         issue_s(here, i + 2 == n);
-                    } else if (more) {
+                    } else if (joined) {
                         first_s();
                     }
                     end_turn();
                 }
+                if (RAGGED && more && !joined) more = !stop && start();
             }
             give_up();
             // The products in flight end before TMEM is freed.

@@ -334,3 +334,43 @@ def test_a_wait_that_runs_out_among_sequences_of_different_lengths():
     kvec.kvec_sync_status(sel.handle)
     assert torch.equal(run(), want)
     sel.close()
+
+
+# Sequences with far more queries than keys: most tiles hold rows before the first key and see nothing, and a CTA meets
+# runs of such tiles (of six in the first, of four in the last) between or behind those that do.
+MOSTLY_UNSEEING = [
+    (32, 8, [8192, 1], [64, 1]), (32, 8, [5000, 3000, 700], [300, 10, 700]), (28, 4, [300, 9000, 20], [300, 100, 20]),
+    (32, 8, [6000, 500, 40], [0, 500, 90]), (16, 8, [9000, 4000, 100], [500, 0, 100]),
+]
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("Hq,Hkv,q_lens,k_lens", MOSTLY_UNSEEING)
+def test_far_more_queries_than_keys(dtype, Hq, Hkv, q_lens, k_lens):
+    q, k, v = tensors(q_lens, k_lens, Hq, Hkv, dtype, sum(q_lens), 2.0)
+    check(q, k, v, q_lens, k_lens)
+    check(q, k, v, q_lens, k_lens, 50, 2)
+
+
+def test_a_captured_call_meets_far_fewer_keys():
+    # The lengths of the keys on the device fall behind those announced, and most rows see nothing any more.
+    lens, keys = [4096, 300, 1500], [100, 300, 20]
+    q, k, v = tensors(lens, lens, 32, 8, torch.bfloat16, 79)
+    sel, cu = selector(32, 8), cu_of(lens)
+    dq, dk = cu.cuda(), cu.cuda()
+    out, lse = torch.empty_like(q), torch.empty(q.shape[:2], device="cuda")
+    run = lambda: sel.prefill_attention(q, k, v, cu, dq, cu, dk, out=out, lse=lse)
+    run()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        run()
+    dk.copy_(cu_of(keys))
+    graph.replay()
+    kvec.kvec_sync_status(sel.handle)
+    ref, rl, mass = reference(q, k, v, lens, keys, 0, 0, D ** -0.5)
+    u = torch.finfo(torch.bfloat16).eps / 2
+    assert torch.all((out.double() - ref).abs() <= u * ref.abs() + (u + 2e-5) * mass)
+    none = torch.isneginf(rl)
+    assert torch.equal(torch.isneginf(lse), none) and torch.all(out[none] == 0)
+    assert torch.all((lse.double() - rl)[~none].abs() <= 2e-5 + 2.0 ** -22 * rl[~none].abs())
