@@ -347,7 +347,9 @@ KVEC_API size_t kvec_paged_decode_bytes(kvec_handle* h, int batch, int max_len, 
  * [0, min(max_len, capacity)], slot j < n is visible if window = 0, or j >= n - window, or
  * j < sinks (the first slots that stay visible beside a sliding window):
  *   out[s][hq] = sum_j p_j v_j,  p_j = softmax over the visible j of scale * <q[s][hq], k_j>;
- * no visible slot (or every logit minus infinity): a zero row.  With cache.weights every
+ * no visible slot (or every logit minus infinity): a zero row.  An infinity or NaN in a value
+ * that is visible reaches the outputs as the sum defines it (an infinity whose weight is at most
+ * 2^-25 of the largest may give NaN).  With cache.weights every
  * visible slot's weight grows by the p_j of the group's query heads:
  *   weights[slot j of head h] += sum over hq of h's group of p_j,
  * which is what kvec_paged_evict ranks by.
@@ -393,7 +395,8 @@ KVEC_API size_t kvec_prefill_bytes(kvec_handle* h, int batch, const int32_t* cu_
  *   out = softmax over the visible t of scale * <q, k_t>, times v_t;
  *   lse = ln sum over the visible t of exp(scale * <q, k_t>).
  * A row that sees nothing (p < 0) gives zeros and -infinity.  Keys and values that a row does
- * not see have no effect on it, whatever they hold.
+ * not see have no effect on it, whatever they hold; infinities and NaN in values that it sees
+ * reach it as for kvec_paged_decode.
  *   q    device dtype [cu_q[batch]][H_q][d];  k, v device dtype [cu_k[batch]][H_kv][d].
  *   out  device dtype, as q, 32-byte aligned;  lse device fp32 [cu_q[batch]][H_q], or NULL.
  *   scratch  device, kvec_prefill_bytes bytes, 32-byte aligned (NULL for none): written and

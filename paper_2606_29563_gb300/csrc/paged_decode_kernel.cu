@@ -221,6 +221,10 @@ __device__ __forceinline__ void ldmatrix_x4_trans(uint32_t addr, uint32_t (&r)[4
                  : "memory");
 }
 
+// The products with the weights' roundings and with what these left.  Against an infinite value the rest, which is
+// zero or has either sign, would make NaN of what the roundings give alone.
+__device__ __forceinline__ float with_rest(float hi, float lo) { return fabsf(hi) < INFINITY ? hi + lo : hi; }
+
 // The attention weights of four slots of a block: what is read for them, and their sum over
 // the query heads once these' (maximum, 1 / sum) are known.
 struct SlotWeights {
@@ -510,7 +514,7 @@ __global__ void __launch_bounds__(kPdThreads, kPdCtasPerSm) paged_decode_kernel(
 #pragma unroll
             for (int d = 0; d < 16; ++d)
                 *reinterpret_cast<float2*>(mine + j * kHeadDim + d * 8 + 2 * (lane & 3)) =
-                    make_float2(acc[d][0] + acc[d][2], acc[d][1] + acc[d][3]);
+                    make_float2(with_rest(acc[d][0], acc[d][2]), with_rest(acc[d][1], acc[d][3]));
         }
         __syncthreads();
         for (int e = tid; e < g * kHeadDim; e += kPdThreads) {

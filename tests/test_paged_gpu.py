@@ -566,3 +566,32 @@ def test_rotate_of_rows_that_overlap():
     want = selector(4, 2).rotate_append(q.contiguous(), k.contiguous(), None, pos, tab)
     assert all(x.is_contiguous() for x in got)
     assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("lens,window,sinks", [([40], 0, 0), ([500, 33], 0, 0), ([6000, 77], 0, 0), ([900, 2100], 64, 3)])
+def test_unbounded_values_in_sight(dtype, lens, window, sinks):
+    # What is infinite or NaN in V and seen gives sum p v as it is defined: an infinity stays one, two of different
+    # signs and NaN give NaN.  (q and k of normal values: each weight is above 2^-25 of the largest.)
+    gen = torch.Generator().manual_seed(sum(lens) + window)
+    cache, _ = make_cache(lens, 2, 16, dtype, gen)
+    q = torch.randn((len(lens), 8, D), generator=gen).to(dtype).cuda()
+    for s, n in enumerate(lens):
+        last, before, first = n - 1, n - 20, 0 if window == 0 or sinks else n - 2
+        for slot, col, value in ((last, 3, "inf"), (before, 9, "-inf"), (first, 70, "nan"), (last, 127, "inf"), (before, 127, "-inf")):
+            cache.v_pages[int(cache.page_table[s, slot // 16]), 1, slot % 16, col] = float(value)
+    w0 = f64(cache.weights)
+    w = w0.copy()
+    with np.errstate(invalid="ignore"):
+        ref = serving.paged_decode(f64(q), f64(cache.k_pages), f64(cache.v_pages), w, cache.page_table.cpu().numpy(), lens,
+                                   cache.capacity, window, sinks, 1 / np.sqrt(D))
+    sel, u = selector(8, 2), half_step(dtype)
+    got = f64(sel.paged_decode(q, cache, window=window, sinks=sinks))
+    kvec.kvec_sync_status(sel.handle)
+    assert np.array_equal(np.isnan(got), np.isnan(ref)) and np.array_equal(got[np.isinf(ref)], ref[np.isinf(ref)])
+    assert np.isinf(ref).sum() == len(lens) * 4 * 2 and np.isnan(ref).sum() == len(lens) * 4 * 2
+    fine = np.isfinite(ref)
+    n = max(lens)
+    tol = u * np.abs(ref[fine]) + (u * u + (n * 2.0 ** -25 if dtype == torch.float16 else 0.0) + 2e-5) * 8.0
+    assert np.all(np.abs(got[fine] - ref[fine]) <= tol)
+    assert np.all(np.abs(f64(cache.weights) - w) <= 2e-5 * (w - w0) + 2.0 ** -24 * np.abs(w) + 1e-9)
