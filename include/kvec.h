@@ -338,8 +338,12 @@ KVEC_API kvec_status kvec_rotate_append(kvec_handle* h, const kvec_rotate_args* 
                                         kvec_stream_t stream);
 
 /* Bytes of scratch that kvec_paged_decode needs for these sizes (0 if they are invalid).
- * with_weights: the cache keeps accumulated weights.  Host only; needs the handle for
- * the device's size. */
+ * with_weights: the cache keeps accumulated weights, for which the logits of every slot that
+ * may be in sight wait in scratch, 4 batch H_q bytes a slot.  kvec_paged_decode_bytes is the
+ * same with window = 0, and enough for any window.  Host only; they need the handle for the
+ * device's size. */
+KVEC_API size_t kvec_paged_decode_window_bytes(kvec_handle* h, int batch, int max_len, int window, int sinks,
+                                               int with_weights);
 KVEC_API size_t kvec_paged_decode_bytes(kvec_handle* h, int batch, int max_len, int with_weights);
 
 /* Attention of one new token per sequence over the paged cache.  The token's own key is
@@ -355,7 +359,7 @@ KVEC_API size_t kvec_paged_decode_bytes(kvec_handle* h, int batch, int max_len, 
  * which is what kvec_paged_evict ranks by.
  *   q        device cache.dtype [batch][H_q][d]; out the same shape and type.
  *   max_len  host bound on the lengths; the work is divided over the device by it.
- *   scratch  device, kvec_paged_decode_bytes bytes, 16-byte aligned: written and read
+ *   scratch  device, kvec_paged_decode_window_bytes bytes, 16-byte aligned: written and read
  *            within the call; calls that may overlap need one each.
  * No two sequences may share a page when weights are kept (their additions would race).
  * 1 <= batch <= max_batch, H_q/H_kv <= 8. */

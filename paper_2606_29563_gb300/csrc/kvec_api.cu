@@ -1298,9 +1298,14 @@ kvec_status kvec_rotate_append(kvec_handle* h, const kvec_rotate_args* a, int ba
     return KVEC_OK;
 }
 
+size_t kvec_paged_decode_window_bytes(kvec_handle* h, int batch, int max_len, int window, int sinks, int with_weights) {
+    if (!h || batch < 1 || batch > h->p.max_batch || max_len < 1 || max_len > kPagedMaxLen || window < 0 || sinks < 0) return 0;
+    return paged_decode_scratch(batch, h->p.num_q_heads, max_len, within_length(window), within_length(sinks),
+                                with_weights != 0, h->num_sms);
+}
+
 size_t kvec_paged_decode_bytes(kvec_handle* h, int batch, int max_len, int with_weights) {
-    if (!h || batch < 1 || batch > h->p.max_batch || max_len < 1 || max_len > kPagedMaxLen) return 0;
-    return paged_decode_scratch(batch, h->p.num_q_heads, h->p.num_kv_heads, max_len, with_weights != 0, h->num_sms);
+    return kvec_paged_decode_window_bytes(h, batch, max_len, 0, 0, with_weights);
 }
 
 kvec_status kvec_paged_decode(kvec_handle* h, int batch, const void* q, const kvec_paged_cache* cache, int max_len,
@@ -1319,7 +1324,7 @@ kvec_status kvec_paged_decode(kvec_handle* h, int batch, const void* q, const kv
     if (!q || !out || !scratch) return fail(KVEC_ERR_INVALID_ARG, "a device pointer is NULL");
     if (!aligned16(q) || !aligned16(out) || !aligned16(scratch))
         return fail(KVEC_ERR_INVALID_ARG, "q, out and scratch must be 16-byte aligned");
-    const size_t need = kvec_paged_decode_bytes(h, batch, max_len, v.weights != nullptr);
+    const size_t need = kvec_paged_decode_window_bytes(h, batch, max_len, window, sinks, v.weights != nullptr);
     if (scratch_bytes < need)
         return fail(KVEC_ERR_INVALID_ARG, "scratch of %zu bytes, %zu are needed", scratch_bytes, need);
     PagedDecodeIO io{};

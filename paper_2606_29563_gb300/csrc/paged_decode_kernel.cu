@@ -733,20 +733,21 @@ cudaError_t launch_typed(const PdArgs& a, cudaStream_t st) {
                        a.ctas * kPdHeads * sizeof(float2), st, 0, true, a);
 }
 
-int visible_blocks(const PagedDecodeIO& io) {
-    const int all = (io.max_len + kPdBlock - 1) / kPdBlock;
-    if (!io.window) return all;
+// Most blocks that a sequence of up to max_len slots has in sight.
+int visible_blocks(int max_len, int window, int sinks) {
+    const int all = (max_len + kPdBlock - 1) / kPdBlock;
+    if (!window) return all;
     // A window ends and begins inside a block.
-    const long long some = (long long)io.window / kPdBlock + 2 + (std::min(io.sinks, io.max_len) + kPdBlock - 1) / kPdBlock;
+    const long long some = (long long)window / kPdBlock + 2 + (std::min(sinks, max_len) + kPdBlock - 1) / kPdBlock;
     return (int)std::min<long long>(all, some);
 }
 
 }  // namespace
 
-size_t paged_decode_scratch(int batch, int Hq, int Hkv, int max_len, bool weights, int num_sms) {
+size_t paged_decode_scratch(int batch, int Hq, int max_len, int window, int sinks, bool weights, int num_sms) {
     const size_t slots = (size_t)share_ctas(num_sms) * 2 * kPdHeads;
     size_t b = round16(slots * kHeadDim * sizeof(float)) + round16(slots * sizeof(float2));
-    if (weights) b += (size_t)batch * Hq * ((max_len + kPdBlock - 1) / kPdBlock) * kPdBlock * sizeof(float);
+    if (weights) b += (size_t)batch * Hq * visible_blocks(max_len, window, sinks) * kPdBlock * sizeof(float);
     return b;
 }
 
@@ -778,7 +779,7 @@ cudaError_t launch_paged_decode(const PagedDecodeIO& io, const PagedCacheView& c
     a.ctas = share_ctas(num_sms);
     const long long pairs = (long long)io.batch * io.Hkv;
     a.pairs = pairs <= a.ctas && pairs * 4 >= a.ctas * 3ll ? (int)pairs : 0;
-    a.nbmax = visible_blocks(io);
+    a.nbmax = visible_blocks(io.max_len, io.window, io.sinks);
     const size_t slots = (size_t)a.ctas * 2 * kPdHeads;
     char* p = static_cast<char*>(io.scratch);
     a.part_o = reinterpret_cast<float*>(p);

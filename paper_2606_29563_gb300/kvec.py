@@ -30,8 +30,8 @@ EXPORTED = ("kvec_create", "kvec_destroy", "kvec_state_bytes", "kvec_reset", "kv
             "kvec_kernel_time", "kvec_status_string", "kvec_last_error", "kvec_select_layer_noalloc",
             "kvec_select_layer_lse", "kvec_select_layers_lse", "kvec_decode_attention",
             "kvec_noalloc_sync_status", "kvec_set_test_fault", "kvec_output_capacity",
-            "kvec_rotate_append", "kvec_paged_decode_bytes", "kvec_paged_decode", "kvec_paged_evict",
-            "kvec_prefill_bytes", "kvec_prefill_attention")
+            "kvec_rotate_append", "kvec_paged_decode_bytes", "kvec_paged_decode_window_bytes", "kvec_paged_decode",
+            "kvec_paged_evict", "kvec_prefill_bytes", "kvec_prefill_attention")
 
 KVEC_BF16 = 0
 KVEC_FP16 = 1
@@ -129,6 +129,7 @@ def load() -> ctypes.CDLL:
             "kvec_rotate_append": ([_vp, ctypes.POINTER(kvec_rotate_args), i, _vp, ctypes.POINTER(kvec_paged_cache),
                                     _vp], st),
             "kvec_paged_decode_bytes": ([_vp, i, i, i], ctypes.c_size_t),
+            "kvec_paged_decode_window_bytes": ([_vp, i, i, i, i, i], ctypes.c_size_t),
             "kvec_paged_decode": ([_vp, i, _vp, ctypes.POINTER(kvec_paged_cache), i, i, i, _vp, _vp, ctypes.c_size_t,
                                    _vp], st),
             "kvec_prefill_bytes": ([_vp, i, _vp, _vp, i, i], ctypes.c_size_t),
@@ -243,6 +244,10 @@ def kvec_rotate_append(handle: int, args: kvec_rotate_args, batch: int, cu_token
 
 def kvec_paged_decode_bytes(handle: int, batch: int, max_len: int, with_weights: bool) -> int:
     return int(load().kvec_paged_decode_bytes(handle, batch, max_len, 1 if with_weights else 0))
+
+
+def kvec_paged_decode_window_bytes(handle: int, batch: int, max_len: int, window: int, sinks: int, with_weights: bool) -> int:
+    return int(load().kvec_paged_decode_window_bytes(handle, batch, max_len, window, sinks, 1 if with_weights else 0))
 
 
 def kvec_paged_decode(handle: int, batch: int, q: int, cache: kvec_paged_cache, max_len: int, window: int, sinks: int,
@@ -380,7 +385,7 @@ class KvecSelector:
         self.device = torch.device("cuda", torch.cuda.current_device())
         self._current = torch._C._cuda_getCurrentRawStream   # torch.cuda.current_stream makes an object, 2 us
         self._lib = load()
-        self._decode_bytes = {}      # kvec_paged_decode_bytes by its sizes
+        self._decode_bytes = {}      # kvec_paged_decode_window_bytes by its sizes
         self.state_bytes = kvec_state_bytes(params.max_seqlen)
 
     def close(self) -> None:
@@ -551,7 +556,9 @@ class KvecSelector:
                      stream=None):
         """One new token per sequence over a paged cache (kvec_paged_decode); adds to cache.weights where it has them.
 
-        q [batch][H_q][d] of the cache's type, contiguous; max_len: a bound on the lengths (the capacity)."""
+        q [batch][H_q][d] of the cache's type, contiguous; max_len: a bound on the lengths (the capacity).  Scratch
+        (kvec_paged_decode_window_bytes) and, with weights, part of the time go by max_len or the window: give the least
+        bound that is known."""
         p = self.params
         batch, dtype = cache.batch, cache.dtype
         shape = (batch, p.num_q_heads, p.head_dim)
@@ -563,10 +570,10 @@ class KvecSelector:
             self._check("out", out, shape, dtype)
         if max_len is None:
             max_len = cache.capacity
-        sizes = (batch, max_len, cache.weights is not None)
+        sizes = (batch, max_len, window, sinks, cache.weights is not None)
         need = self._decode_bytes.get(sizes)
         if need is None:
-            need = self._decode_bytes[sizes] = kvec_paged_decode_bytes(self.handle, *sizes)
+            need = self._decode_bytes[sizes] = kvec_paged_decode_window_bytes(self.handle, *sizes)
         scratch = self._empty(max(need, 16), self._torch.uint8, stream)
         st = self._lib.kvec_paged_decode(self.handle, batch, q.data_ptr(), cache.c, max_len, window, sinks, out.data_ptr(),
                                          scratch.data_ptr(), need, self._raw(stream))

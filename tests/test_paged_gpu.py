@@ -595,3 +595,50 @@ def test_unbounded_values_in_sight(dtype, lens, window, sinks):
     tol = u * np.abs(ref[fine]) + (u * u + (n * 2.0 ** -25 if dtype == torch.float16 else 0.0) + 2e-5) * 8.0
     assert np.all(np.abs(got[fine] - ref[fine]) <= tol)
     assert np.all(np.abs(f64(cache.weights) - w) <= 2e-5 * (w - w0) + 2.0 ** -24 * np.abs(w) + 1e-9)
+
+
+def test_scratch_goes_by_what_is_in_sight():
+    # With a window no more than its slots wait in scratch, and the call stays within the bytes that it asks for.
+    gen = torch.Generator().manual_seed(70)
+    lens, window, sinks = [900, 40, 3000], 100, 20
+    cache, _ = make_cache(lens, 2, 64, torch.bfloat16, gen, max_pages=131072 // 64)
+    q = torch.randn((3, 16, D), generator=gen).to(torch.bfloat16).cuda()
+    sel, first = selector(16, 2), cache.weights.clone()
+    whole = kvec.kvec_paged_decode_bytes(sel.handle, 3, 131072, True)
+    need = kvec.kvec_paged_decode_window_bytes(sel.handle, 3, 131072, window, sinks, True)
+    fixed = kvec.kvec_paged_decode_window_bytes(sel.handle, 3, 131072, window, sinks, False)
+    assert fixed == kvec.kvec_paged_decode_bytes(sel.handle, 3, 131072, False)
+    assert whole - fixed == 3 * 16 * 131072 * 4 and need - fixed == 3 * 16 * (100 // 16 + 2 + 2) * 16 * 4
+    assert kvec.kvec_paged_decode_window_bytes(sel.handle, 3, 131072, 0, 7, True) == whole
+    assert kvec.kvec_paged_decode_window_bytes(sel.handle, 3, 131072, -1, 0, True) == 0
+    assert kvec.kvec_paged_decode_window_bytes(sel.handle, 3, 131072, 9, -1, True) == 0
+    out = torch.empty_like(q)
+
+    def run(scratch, size):
+        cache.weights.copy_(first)
+        kvec.kvec_paged_decode(sel.handle, 3, q.data_ptr(), cache.c, 131072, window, sinks, out.data_ptr(), scratch.data_ptr(),
+                               size, torch.cuda.current_stream().cuda_stream)
+        kvec.kvec_sync_status(sel.handle)
+        return out.clone(), cache.weights.clone()
+
+    large = run(torch.empty(whole, dtype=torch.uint8, device="cuda"), whole)
+    room = torch.full((need + 4096,), 0xA5, dtype=torch.uint8, device="cuda")
+    small = run(room, need)
+    assert torch.equal(small[0], large[0]) and torch.equal(small[1], large[1]) and torch.all(room[need:] == 0xA5)
+    with pytest.raises(kvec.KvecError):
+        run(room, need - 1)
+    cache.weights.copy_(first)
+    check_decode(sel, q, cache, lens, max_len=131072, window=window, sinks=sinks)
+
+
+def test_a_windowed_call_takes_little_memory():
+    # 64 caches with room for 131072 slots each: the logits of all of them would take 1.07 GB.
+    gen = torch.Generator().manual_seed(71)
+    cache, _ = make_cache([50] * 64, 8, 64, torch.bfloat16, gen, max_pages=131072 // 64)
+    q = torch.randn((64, 32, D), generator=gen).to(torch.bfloat16).cuda()
+    sel = selector(32, 8)
+    torch.cuda.synchronize()
+    held = torch.cuda.memory_allocated()
+    torch.cuda.reset_peak_memory_stats()
+    sel.paged_decode(q, cache, window=512, sinks=4)
+    assert torch.cuda.max_memory_allocated() - held < 10 << 20   # 64 * 32 * (512 + 3 * 16) * 4 = 4.6 MB, and 2.6 MB
