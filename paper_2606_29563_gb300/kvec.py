@@ -573,6 +573,8 @@ class KvecSelector:
         sizes = (batch, max_len, window, sinks, cache.weights is not None)
         need = self._decode_bytes.get(sizes)
         if need is None:
+            if len(self._decode_bytes) >= 256:   # a loop's bounds may grow with every step
+                self._decode_bytes.clear()
             need = self._decode_bytes[sizes] = kvec_paged_decode_window_bytes(self.handle, *sizes)
         scratch = self._empty(max(need, 16), self._torch.uint8, stream)
         st = self._lib.kvec_paged_decode(self.handle, batch, q.data_ptr(), cache.c, max_len, window, sinks, out.data_ptr(),

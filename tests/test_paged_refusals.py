@@ -238,3 +238,14 @@ def test_prefill_definition():
     assert np.allclose(out[5], v[8]) and np.allclose(lse[5, 0], 0.4 * q[5, 0] @ k[8, 0])
     mean, _ = serving.prefill(0 * q, k, v, [0, 4, 6], [0, 8, 9], 2, 1, 0.4)
     assert np.allclose(mean[3, 0], (v[0, 0] + v[6, 0] + v[7, 0]) / 3)
+
+
+def test_the_binding_remembers_few_sizes():
+    # A loop that passes the longest length of each step meets a new bound every time.
+    sel = selector()
+    sel._current = lambda index: 0
+    c = kvec.PagedCache(**{**tensors(), "page_table": torch.zeros((2, 2000), dtype=torch.int32)})
+    q = torch.zeros((2, 8, 128), dtype=torch.bfloat16)
+    for n in range(1, 3000):
+        refused(lambda: sel.paged_decode(q, c, max_len=n), kvec.KVEC_ERR_INVALID_ARG, "handle is NULL")
+    assert 1 <= len(sel._decode_bytes) <= 256
