@@ -570,6 +570,8 @@ class KvecSelector:
             self._check("out", out, shape, dtype)
         if max_len is None:
             max_len = cache.capacity
+        if (max_len | window | sinks) >> 31:   # ctypes would pass their lower 32 bits
+            raise KvecError(KVEC_ERR_INVALID_ARG, "max_len, window and sinks must be in [0, 2^31)")
         sizes = (batch, max_len, window, sinks, cache.weights is not None)
         need = self._decode_bytes.get(sizes)
         if need is None:
@@ -595,6 +597,10 @@ class KvecSelector:
         _want(new_table.dim() == 2, "new_table must be int32 [batch][pages]")
         self._check("new_table", new_table, (batch, new_table.shape[1]), t.int32)
         _want(1 <= budget <= 1 << 20, "budget must be in [1, 2^20]")
+        if max_len is None:
+            max_len = cache.capacity
+        if (max_len | sinks | recent) >> 31:
+            raise KvecError(KVEC_ERR_INVALID_ARG, "max_len, sinks and recent must be in [0, 2^31)")
         if new_lens is None:
             new_lens = self._empty((batch,), t.int32, stream)
         else:
@@ -604,7 +610,7 @@ class KvecSelector:
         else:
             self._check("kept", kept, (batch, Hkv, budget), t.int32)
         st = self._lib.kvec_paged_evict(self.handle, batch, cache.c, new_table.data_ptr(), new_table.shape[1],
-                                        cache.capacity if max_len is None else max_len, budget, sinks, recent,
+                                        max_len, budget, sinks, recent,
                                         new_lens.data_ptr(), kept.data_ptr(), self._raw(stream))
         if st:
             _check(st)
@@ -630,6 +636,8 @@ class KvecSelector:
         for x in (cu_q_host, cu_k_host):
             _want(x.dtype is t.int32 and x.shape == (batch + 1,) and x.device.type == "cpu" and x.is_contiguous(),
                   "cu_q_host and cu_k_host must be contiguous int32 [batch + 1] on the host")
+        if (window | sinks) >> 31:
+            raise KvecError(KVEC_ERR_INVALID_ARG, "window and sinks must be in [0, 2^31)")
         cu_q, cu_k = cu_q_host.data_ptr(), cu_k_host.data_ptr()
         last = ctypes.c_int32.from_address   # the host copies' last entries (a tensor's item takes 2 us)
         _want(batch >= 1 and last(cu_q + 4 * batch).value <= Tq and last(cu_k + 4 * batch).value <= Tk,

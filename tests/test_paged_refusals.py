@@ -249,3 +249,20 @@ def test_the_binding_remembers_few_sizes():
     for n in range(1, 3000):
         refused(lambda: sel.paged_decode(q, c, max_len=n), kvec.KVEC_ERR_INVALID_ARG, "handle is NULL")
     assert 1 <= len(sel._decode_bytes) <= 256
+
+
+@pytest.mark.parametrize("far", [2 ** 31, 2 ** 32, 2 ** 32 + 16, 2 ** 40])
+def test_the_binding_refuses_sizes_past_32_bits(far):
+    # Their lower 32 bits would count: 2^32 as no window, 2^32 + 16 as 16.
+    sel, c = selector(), kvec.PagedCache(**tensors())
+    sel._current = lambda index: 0
+    bf, cu = torch.bfloat16, torch.tensor([0, 2], dtype=torch.int32)
+    q, k, table = torch.zeros((2, 8, 128), dtype=bf), torch.zeros((2, 2, 128), dtype=bf), torch.zeros((2, 3), dtype=torch.int32)
+    for bad in ("max_len", "window", "sinks"):
+        refused(lambda: sel.paged_decode(q, c, **{bad: far}), kvec.KVEC_ERR_INVALID_ARG, "2^31")
+    for bad in ("max_len", "sinks", "recent"):
+        refused(lambda: sel.paged_evict(c, table, 16, **{bad: far}), kvec.KVEC_ERR_INVALID_ARG, "2^31")
+    for bad in ("window", "sinks"):
+        refused(lambda: sel.prefill_attention(q, k, k, cu, cu, **{bad: far}), kvec.KVEC_ERR_INVALID_ARG, "2^31")
+    # The largest that is taken reaches the library.
+    refused(lambda: sel.paged_decode(q, c, window=2 ** 31 - 1, sinks=2 ** 31 - 1), kvec.KVEC_ERR_INVALID_ARG, "handle is NULL")
