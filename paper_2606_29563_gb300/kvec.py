@@ -464,7 +464,8 @@ class KvecSelector:
     # ------------------------------------------------------------ decoding over pages
     # A small call is bound by its host time: messages are formed only where a check fails.
     # stream: the call's (None: the current one); what it reads must be ready there, and what is made
-    # for it comes from that stream's memory.
+    # for it comes from that stream's memory.  What is given to a call on another stream than the current one may be
+    # let go at once: its memory is not used again before that stream's work so far is done.
 
     def _empty(self, shape, dtype, stream):
         """Memory that work on `stream` (None: the current one) may use at once, from that stream's pool."""
@@ -476,6 +477,16 @@ class KvecSelector:
 
     def _raw(self, stream):
         return self._current(self.device.index) if stream is None else stream.cuda_stream
+
+    def _used(self, stream, cache, *tensors):
+        """After a call on `stream`: tells the allocator of its tensors, which came from other streams' memory."""
+        if stream.cuda_stream == self._current(self.device.index):
+            return
+        if cache is not None:
+            tensors += (cache.k_pages, cache.v_pages, cache.page_table, cache.lens, cache.weights)
+        for x in tensors:
+            if x is not None:
+                x.record_stream(stream)
 
     def _check(self, name, x, shape, dtype):
         """A contiguous tensor of the handle's device."""
@@ -550,6 +561,8 @@ class KvecSelector:
                                               None if cache is None else cache.c, self._raw(stream))
             if st:
                 _check(st)
+            if stream is not None:
+                self._used(stream, cache, q, k, v, positions, rot_table, cu_tokens, q_norm, k_norm, q_out, k_out)
         return (q_out, k_out) if want_k else q_out
 
     def paged_decode(self, q, cache, max_len: Optional[int] = None, window: int = 0, sinks: int = 0, out=None,
@@ -583,6 +596,8 @@ class KvecSelector:
                                          scratch.data_ptr(), need, self._raw(stream))
         if st:
             _check(st)
+        if stream is not None:
+            self._used(stream, cache, q, out)
         return out
 
     def paged_evict(self, cache, new_table, budget: int, sinks: int = 0, recent: int = 0, max_len: Optional[int] = None,
@@ -614,6 +629,8 @@ class KvecSelector:
                                         new_lens.data_ptr(), kept.data_ptr(), self._raw(stream))
         if st:
             _check(st)
+        if stream is not None:
+            self._used(stream, cache, new_table, new_lens, kept)
         return new_lens, kept
 
     def prefill_attention(self, q, k, v, cu_q_host, cu_q_dev, cu_k_host=None, cu_k_dev=None, window: int = 0,
@@ -657,6 +674,8 @@ class KvecSelector:
                                               lse.data_ptr(), scratch.data_ptr() if need else None, need, self._raw(stream))
         if st:
             _check(st)
+        if stream is not None:
+            self._used(stream, None, q, k, v, cu_q_dev, cu_k_dev, out, lse)
         return out, lse
 
     def debug(self, device="cuda"):

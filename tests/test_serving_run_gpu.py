@@ -274,3 +274,45 @@ def test_a_wait_that_runs_out_is_reported_and_the_handle_recovers(call):
     assert torch.equal(run(), want)
     kvec.kvec_sync_status(sel.handle)
     sel.close()
+
+
+@pytest.mark.parametrize("call", ["rotate", "decode", "evict", "prefill"])
+def test_inputs_of_a_call_on_another_stream_may_be_let_go(call):
+    # The call waits behind a long one on its stream; its inputs are let go at once, and the next tensors of their sizes
+    # are written on the current stream meanwhile.
+    gen = torch.Generator(device="cuda").manual_seed(9)
+    rand = lambda *shape: torch.randn(shape, generator=gen, device="cuda").to(torch.bfloat16)
+    sel, n = selector(), 700
+    per = -(-n // 64)
+    pool = (2 * per, HKV, 64, D)
+    fixed = [rand(*pool), rand(*pool), torch.arange(per, dtype=torch.int32, device="cuda")[None], torch.tensor([n], dtype=torch.int32).cuda(),
+             torch.rand(pool[:3], generator=gen, device="cuda")]
+    if call == "rotate":
+        given = [rand(n, HQ, D), rand(n, HKV, D), rand(n, HKV, D), torch.arange(n, dtype=torch.int32).cuda(),
+                 paged.rot_table(n, D).cuda(), torch.tensor([0, n], dtype=torch.int32).cuda(), rand(D), rand(D)]
+        run = lambda c, x, **kw: (*sel.rotate_append(*x[:5], c, x[5], q_norm=x[6], k_norm=x[7], k_out=torch.empty_like(x[1]), **kw),
+                                  c.k_pages, c.v_pages)
+    elif call == "decode":
+        given = [rand(1, HQ, D)]
+        run = lambda c, x, **kw: (sel.paged_decode(x[0], c, **kw), c.weights)
+    elif call == "evict":
+        given = [torch.arange(per, 2 * per, dtype=torch.int32, device="cuda")[None].clone()]
+        run = lambda c, x, **kw: (*sel.paged_evict(c, x[0], 300, sinks=2, recent=9, **kw), c.k_pages, c.v_pages, c.weights)
+    else:
+        cu = prefill.cu_of([n])
+        given = [rand(n, HQ, D), rand(n, HKV, D), rand(n, HKV, D), cu.cuda()]
+        run = lambda c, x, **kw: sel.prefill_attention(*x[:3], cu, x[3], **kw)
+    fresh = lambda: (kvec.PagedCache(*[x.clone() for x in fixed]), [x.clone() for x in given])
+    want = [x.clone() for x in run(*fresh())]
+    side = torch.cuda.Stream()
+    run(*fresh(), stream=side)                          # the side stream's first allocations
+    cache, x = fresh()
+    torch.cuda.synchronize()
+    with torch.cuda.stream(side):
+        torch.cuda._sleep(100_000_000)
+    got = run(cache, x, stream=side)
+    del cache, x
+    junk = [torch.full_like(t, 77) for t in given + fixed for _ in range(12)]
+    kvec.kvec_sync_status(sel.handle)
+    assert len(got) == len(want) and all(torch.equal(a, b) for a, b in zip(got, want)) and junk
+    sel.close()
