@@ -374,3 +374,44 @@ def test_a_captured_call_meets_far_fewer_keys():
     none = torch.isneginf(rl)
     assert torch.equal(torch.isneginf(lse), none) and torch.all(out[none] == 0)
     assert torch.all((lse.double() - rl)[~none].abs() <= 2e-5 + 2.0 ** -22 * rl[~none].abs())
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("q_lens,k_lens", [([200], [200]), ([20], [3000]), ([700, 20, 40], [700, 300, 40])])
+@pytest.mark.parametrize("hit", ["every other", "the first blocks", "all but one"])
+def test_minus_infinite_logits_count_for_nothing(dtype, q_lens, k_lens, hit):
+    # One tile after another, divided keys, and sequences of different lengths; every row by the tolerances above.
+    q, k, v = tensors(q_lens, k_lens, 4, 4, dtype, sum(k_lens) + 1)
+    q[:, :, 0] = 1.0
+    out_of = torch.zeros(sum(k_lens), dtype=torch.bool, device="cuda")
+    at = 0
+    for n in k_lens:
+        here = out_of[at:at + n]
+        if hit == "every other":
+            here[::2] = True
+        elif hit == "the first blocks":
+            here[:n - n // 3] = True
+        else:
+            here[:] = True
+            here[n // 2] = False
+        at += n
+    k2 = torch.where(out_of[:, None, None] & (torch.arange(D, device="cuda") == 0), torch.full_like(k, -np.inf), k)
+    sel, cq, ck = selector(4, 4), cu_of(q_lens), cu_of(k_lens)
+    out, lse = sel.prefill_attention(q, k2, v, cq, cq.cuda(), ck, ck.cuda())
+    kvec.kvec_sync_status(sel.handle)
+    u, q0, k0 = torch.finfo(dtype).eps / 2, 0, 0
+    for nq, nk in zip(q_lens, k_lens):
+        a, b, c = q[q0:q0 + nq].double(), k[k0:k0 + nk].double(), v[k0:k0 + nk].double()
+        x = torch.einsum("qhd,khd->hqk", a, b) * D ** -0.5
+        t, p = torch.arange(nk, device="cuda"), torch.arange(nk - nq, nk, device="cuda")
+        x = x.masked_fill((t[None, :] > p[:, None]) | out_of[k0:k0 + nk][None, :], -np.inf)
+        z = torch.logsumexp(x, -1)
+        w = torch.exp(x - z.clamp(min=-1e300)[..., None])
+        ref, mass = torch.einsum("hqk,khd->qhd", w, c), torch.einsum("hqk,khd->qhd", w, c.abs())
+        got, gl, z = out[q0:q0 + nq].double(), lse[q0:q0 + nq].double(), z.T
+        tol = u * ref.abs() + (u + 2e-5) * mass + (nk * 2.0 ** -25 * 8 if dtype == torch.float16 else 0)
+        assert torch.all((got - ref).abs() <= tol)
+        none = torch.isneginf(z)
+        assert torch.equal(torch.isneginf(gl), none) and torch.all(got[none] == 0)
+        assert torch.all((gl - z)[~none].abs() <= 2e-5 + 2.0 ** -22 * z[~none].abs())
+        q0, k0 = q0 + nq, k0 + nk
