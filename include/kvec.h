@@ -358,7 +358,8 @@ KVEC_API size_t kvec_paged_decode_bytes(kvec_handle* h, int batch, int max_len, 
  *   weights[slot j of head h] += sum over hq of h's group of p_j,
  * which is what kvec_paged_evict ranks by.
  *   q        device cache.dtype [batch][H_q][d]; out the same shape and type.
- *   max_len  host bound on the lengths; the work is divided over the device by it.
+ *   max_len  host bound on the lengths.  Scratch and, with weights, the call's time grow with
+ *            it (or with the window, where that is shorter): give the least bound that is known.
  *   scratch  device, kvec_paged_decode_window_bytes bytes, 16-byte aligned: written and read
  *            within the call; calls that may overlap need one each.
  * No two sequences may share a page when weights are kept (their additions would race).
@@ -378,7 +379,10 @@ KVEC_API kvec_status kvec_paged_decode(kvec_handle* h, int batch, const void* q,
  *             page_table and none twice (the copies of a page that is would race).
  *   new_lens  device int32 [batch]: m.
  *   kept      device int32 [batch][H_kv][budget]: the kept slots, ascending; -1 past m.
- * A slot on no page ranks as NaN does; kept, its row is left as the new page has it. */
+ * A slot on no page ranks as NaN does; kept, its row is left as the new page has it.
+ * The weights are what kvec_paged_decode added since kvec_rotate_append set them to 0: a
+ * prompt's own attention is not among them, and before the first eviction its slots rank
+ * by the decoded tokens alone unless the caller has written weights for them. */
 KVEC_API kvec_status kvec_paged_evict(kvec_handle* h, int batch, const kvec_paged_cache* cache,
                                       const int32_t* new_table, int new_max_pages, int max_len, int budget,
                                       int sinks, int recent, int32_t* new_lens, int32_t* kept,
@@ -405,8 +409,9 @@ KVEC_API size_t kvec_prefill_bytes(kvec_handle* h, int batch, const int32_t* cu_
  *   out  device dtype, as q, 32-byte aligned;  lse device fp32 [cu_q[batch]][H_q], or NULL.
  *   scratch  device, kvec_prefill_bytes bytes, 32-byte aligned (NULL for none): written and
  *            read within the call; calls that may overlap need one each.
- * Lengths up to 2^20; the weights are rounded to dtype before they meet the values, the sums
- * are fp32.  A bounded wait that gave up is reported by kvec_sync_status. */
+ * Lengths up to 2^20; the weights are rounded to dtype before they meet the values (half a step
+ * of it beside the output's own rounding), the sums are fp32.  A bounded wait that gave up is
+ * reported by kvec_sync_status. */
 KVEC_API kvec_status kvec_prefill_attention(kvec_handle* h, int dtype, int batch,
                                             const int32_t* cu_q_host, const int32_t* cu_q_dev,
                                             const int32_t* cu_k_host, const int32_t* cu_k_dev,

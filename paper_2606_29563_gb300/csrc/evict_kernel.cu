@@ -12,7 +12,9 @@
 //
 // Measured, in us (in brackets the bytes at the measured copy rate): 8 rows of 576 slots to
 // 512 7.1 (0.6), the chain of two launches and six barriers; 128 rows of 1000 to 4096 slots to
-// 1024 29.3 (20.2); 512 of 2100 to 2048 175 (161); 8 of 65536 to 8192, by sweeps, 65 (10.3).
+// 1024 29.3 (20.2); 512 of 2100 to 2048 175 (161); 8 of 32768 to 8192 27 (10.2), of 65536, by
+// sweeps, 65 to 74 (10.3), of 131072 130 (10.6).  The kernel goes by the bound on the lengths: 8 rows of
+// 576 slots take 7.4 under their own, 13.5 under one of 32768 and 8.5 under one of 131072 (by sweeps).
 // Small blocks of few rows fill the device best: two rows of K and V in flight a half-warp and
 // 128 threads 29.3, four and 256 31.0, eight and 256 36.6.
 #include "hist_select.cuh"

@@ -21,11 +21,12 @@
 // With few pairs the CTAs of a pair form a cluster, and with short ones each has a CTA; these
 // meet over distributed shared memory in one launch.
 //
-// HBM-bound when there is much to read: 131072 slots of 8 heads (537 MB) in 84 us, 6.4 TB/s, 94 %
+// HBM-bound when there is much to read: 131072 slots of 8 heads (537 MB) in 86 us, 6.3 TB/s, 92 %
 // of the measured copy rate; 64 rows of 1024 to 2048 slots of 4 heads and 7 query heads each (203 MB
 // with the weights) in 48 us, of which the reading takes 31: before it lie the lengths, the
 // list, the pages' numbers and the first copies (4 us), behind it the merge, the weights (7 us, each
-// round a chain of loads) and an empty join.  512 slots 6.2 us, the same chain once.
+// round a chain of loads) and an empty join.  512 slots 6.2 us, the same chain once.  The join's grid goes
+// by the bound on the lengths: the 64 rows take 51 us under one of 8192, 57 of 32768 and 82 of 131072.
 #include "half_types.cuh"
 #include "kvec_internal.cuh"
 #include "sm100_ptx.cuh"

@@ -21,17 +21,21 @@
 // block in which the row sees a key, and moves only when the weights of a block sum up to 2^14
 // (kMostWeight), so that no block waits for a maximum and O is scaled in TMEM once in a while.
 // Results do not depend on m: 2^(s - m) keeps its relative precision, and so does l.
+// The weights meet V rounded to its type, as the tensor cores take both operands of one type; their
+// sum l is that of the unrounded ones.  That adds half a step of the type to the output's own
+// rounding (error against 64 bits 2.2e-3 of the output for 1.6e-3 in bf16, 2.6e-4 for 2.1e-4 in
+// fp16); a second product with what the rounding left would take half as much tensor time again.
 //
 // Bound by the power limit in long runs, and by the products' chain before it: a block of both
 // tiles takes 2048 cycles of the tensor pipe (32 products of 64 cycles, which is what they take
 // when nothing waits) and about 2700 in all, as a tile's softmax (S read 60, exponentials 2 x
 // 370, weights written and handed over 250 cycles) and its turn's waits outlast the other tile's
 // 1024.  (Without any exponential 8192 tokens take 317 us instead of 333.)  Measured, 32 query
-// and 8 KV heads, bf16: 32768 tokens 4.8 ms, 1830 TFLOP/s (97 % of the measured cuBLAS burst);
-// 8192 tokens 328 us, 1676 TFLOP/s, in a run of seconds 365 us at 1830 MHz and 1370 W, 1506
-// TFLOP/s (a cuBLAS product of 8192^3 beside it 1690 at 1430 MHz); 16384 tokens with a window of
-// 2048 and 4 first tokens 391 us, 1320 TFLOP/s of visible pairs (18 blocks an item for 16 of keys
-// seen); 8192 and 5001 tokens together 467 us, 1617 TFLOP/s.  What that took, 8192 tokens in us:
+// and 8 KV heads, bf16, in CUDA graphs of a few calls: 32768 tokens 5.15 ms, 1709 TFLOP/s;
+// 8192 tokens 330 us, 1667 TFLOP/s (89 % of the measured cuBLAS burst), in a run of seconds 365 us
+// at 1830 MHz and 1370 W, 1506 TFLOP/s (a cuBLAS product of 8192^3 beside it 1690 at 1430 MHz); 16384
+// tokens with a window of 2048 and 4 first tokens 389 us, 1327 TFLOP/s of visible pairs (18 blocks an item
+// for 16 of keys seen); 8192 and 5001 tokens together 464 us, 1627 TFLOP/s.  What that took, 8192 tokens in us:
 // S in registers without spills 451, items one behind the other in persistent CTAs 445, no
 // maximum pass 421, waits of one poll 406, 32-byte stores 398, stages stepped 390, whole blocks
 // of weights handed over at once 375, a warp that issues for each tile 349, the registers that
@@ -60,7 +64,8 @@ constexpr int kPfItems = 4;                         // items handed out and not 
 constexpr int kPfThreads = 384;
 constexpr uint32_t kPfTmem = 512;                   // S0 | S1 | O0 | O1, 128 columns each
 // Registers of a thread: at launch (the most that 384 threads may have), and after the split.
-constexpr int kPfRegs = 168, kPfSoftmaxRegs = 216, kPfOtherRegs = 72;   // neither side spills in its loops over blocks
+// The compiler spills one or two words, and eight in the variant of ragged lengths (-Xptxas -v).
+constexpr int kPfRegs = 168, kPfSoftmaxRegs = 216, kPfOtherRegs = 72;
 static_assert(256 * kPfSoftmaxRegs + 128 * kPfOtherRegs <= kPfThreads * kPfRegs, "the split fits what the block was launched with");
 // A row's weights of a block that sum up to less are taken as they are; fp16 holds them.
 constexpr float kMostWeight = 16384.f;

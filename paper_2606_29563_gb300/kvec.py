@@ -604,6 +604,8 @@ class KvecSelector:
                     new_lens=None, kept=None, stream=None):
         """Eviction by accumulated weight to the pages of new_table (kvec_paged_evict).
 
+        cache.weights hold what paged_decode added since rotate_append set a slot's to 0; a prompt's slots count with
+        its own attention only where the caller has written it there.
         new_table int32 [batch][pages], contiguous, of pages that page_table does not use.  Returns (new_lens int32
         [batch], kept int32 [batch][H_kv][budget])."""
         t, p = self._torch, self.params
