@@ -465,7 +465,8 @@ class KvecSelector:
     # A small call is bound by its host time: messages are formed only where a check fails.
     # stream: the call's (None: the current one); what it reads must be ready there, and what is made
     # for it comes from that stream's memory.  What is given to a call on another stream than the current one may be
-    # let go at once: its memory is not used again before that stream's work so far is done.
+    # let go at once: its memory is not used again before that stream's work so far is done.  (A stream that torch did
+    # not make has to live until they are let go.)
 
     def _empty(self, shape, dtype, stream):
         """Memory that work on `stream` (None: the current one) may use at once, from that stream's pool."""
