@@ -388,6 +388,54 @@ KVEC_API kvec_status kvec_paged_evict(kvec_handle* h, int batch, const kvec_page
                                       int sinks, int recent, int32_t* new_lens, int32_t* kept,
                                       kvec_stream_t stream);
 
+/* ------------------------------------------------------------------ a cache of 8 bits
+ *
+ * Keys and values as e4m3 numbers (4 exponent and 3 mantissa bits, up to 448) with an fp32
+ * factor for each row: row r of a page stands for scale[r] * (its d numbers).  That is 132
+ * bytes a row instead of 256.  The cache is a kvec_paged_cache whose k_pages and v_pages
+ * hold bytes, [num_pages][H_kv][page_size][d]; its dtype stays that of q, of the outputs
+ * and of rows that are read back.  The functions below are those above with this in place
+ * of the rows of 16 bits, and what is said there holds here. */
+typedef struct {
+    float *k_scales, *v_scales;   /* device fp32 [num_pages][H_kv][page_size], 16-byte aligned */
+} kvec_paged_scales;
+
+/* kvec_rotate_append into such a cache (which is needed here).  A key or value row y, in
+ * fp32 as it comes from the norm and the rotation, is stored as
+ *   scale = max(max |y| / 448, 2^-126),  numbers = y / scale rounded to nearest even,
+ * so that a number is off by 1/16 of itself or 2^-10 scale at most.  A row that holds an
+ * infinity or NaN gets such a scale, and reads as NaN.  q_out and k_out are dtype as ever. */
+KVEC_API kvec_status kvec_rotate_append_quant(kvec_handle* h, const kvec_rotate_args* args, int batch,
+                                              const int32_t* cu_tokens, const kvec_paged_cache* cache,
+                                              const kvec_paged_scales* scales, kvec_stream_t stream);
+
+/* kvec_paged_decode over such a cache, with the same scratch: keys and values count as the
+ * exact products of numbers and scales.  (Queries of bf16 enter with 2^-39 of their row's
+ * largest magnitude, weights with 2^-22 of themselves.)  A scale may be any fp32 number. */
+KVEC_API kvec_status kvec_paged_decode_quant(kvec_handle* h, int batch, const void* q, const kvec_paged_cache* cache,
+                                             const kvec_paged_scales* scales, int max_len, int window, int sinks,
+                                             void* out, void* scratch, size_t scratch_bytes, kvec_stream_t stream);
+
+/* kvec_paged_evict of such a cache: numbers and scales move as they are. */
+KVEC_API kvec_status kvec_paged_evict_quant(kvec_handle* h, int batch, const kvec_paged_cache* cache,
+                                            const kvec_paged_scales* scales, const int32_t* new_table,
+                                            int new_max_pages, int max_len, int budget, int sinks, int recent,
+                                            int32_t* new_lens, int32_t* kept, kvec_stream_t stream);
+
+/* Slots of a paged cache as packed rows of dtype, [num_rows][H_kv][d], as
+ * kvec_prefill_attention takes keys and values: what a prompt's next chunk attends to.  Row
+ * t of cu_rows[s] <= t < cu_rows[s + 1] is slot first[s] + t - cu_rows[s] of sequence s.
+ *   scales   of a cache of 8 bits, whose rows are rounded once to dtype; NULL: the cache's
+ *            rows are of 16 bits and are copied.
+ *   first    device int32 [batch]; NULL: 0 for every sequence.
+ *   cu_rows  device int32 [batch + 1], ascending from 0.
+ *   k_out, v_out  device, 16-byte aligned, none of the cache's memory.
+ * A row whose slot lies outside [0, min(lens[s], capacity)) or on no page is zeros; rows from
+ * cu_rows[batch] on are left as they are.  num_rows = 0 does nothing.  1 <= batch <= max_batch. */
+KVEC_API kvec_status kvec_paged_read(kvec_handle* h, int batch, const kvec_paged_cache* cache,
+                                     const kvec_paged_scales* scales, const int32_t* first, const int32_t* cu_rows,
+                                     int num_rows, void* k_out, void* v_out, kvec_stream_t stream);
+
 /* Bytes of scratch that kvec_prefill_attention needs for these lengths: 0 for most, more
  * where there are so few query rows that the keys have to be divided over the device (and 0
  * if an argument is invalid).  Host only. */

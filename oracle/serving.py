@@ -50,6 +50,34 @@ def append(k_pages, v_pages, weights, table, lens, cu, positions, max_positions,
                 weights[at[0], :, at[1]] = 0.0
 
 
+def e4m3(x):
+    """x rounded to the nearest e4m3 number, ties to even: steps of 2^(e - 3) from 2^e on, of 2^-9 below 2^-6; 448 at most."""
+    x = np.asarray(x, dtype=np.float64)
+    with np.errstate(divide="ignore", invalid="ignore"):
+        e = np.clip(np.floor(np.log2(np.abs(x))), -6, None)
+    e = np.where(np.isfinite(e), e, -6)
+    step = 2.0 ** (e - 3)
+    return np.clip(np.round(x / step) * step, -448.0, 448.0)
+
+
+def scale_of(y):
+    """The factor of rows y [...][d] of a cache of 8 bits, before its own rounding."""
+    return np.maximum(np.abs(y).max(axis=-1) / 448.0, 2.0 ** -126)
+
+
+def paged_read(k_pages, v_pages, table, lens, first, cu, num_rows, fill):
+    """Packed rows (k, v) [num_rows][H_kv][d] of pages that hold the values themselves; `fill` behind the last sequence."""
+    num_pages, Hkv, page_size, d = k_pages.shape
+    k, v = (np.full((num_rows, Hkv, d), float(fill)) for _ in range(2))
+    for s in range(len(lens)):
+        for t in range(int(cu[s]), min(int(cu[s + 1]), num_rows)):
+            slot = int(first[s]) + t - int(cu[s])
+            at = place(table[s], slot, page_size, num_pages) if slot < int(lens[s]) else None
+            k[t] = 0.0 if at is None else k_pages[at[0], :, at[1]]
+            v[t] = 0.0 if at is None else v_pages[at[0], :, at[1]]
+    return k, v
+
+
 def softmax(x):
     """Rows of x; (weights, ln of the sum).  A row of minus infinities has no weights."""
     m = np.max(x, axis=-1, keepdims=True, initial=-np.inf)

@@ -247,10 +247,12 @@ __global__ void __launch_bounds__(kSweepThreads) evict_sweep_kernel(const __grid
     }
 }
 
+// E8: rows of 128 bytes and a scale each; the lower eight lanes of a half-warp move K's, the upper V's.
 constexpr int kCopyThreads = 128;
 constexpr int kCopyPer = 2;                                   // rows of a half-warp
 constexpr int kCopyRows = kCopyThreads / 16 * kCopyPer;       // rows of a block
 
+template <bool E8>
 __global__ void __launch_bounds__(kCopyThreads) evict_copy_kernel(const __grid_constant__ EvictArgs A) {
     asm volatile("griddepcontrol.launch_dependents;\n" ::: "memory");
     asm volatile("griddepcontrol.wait;\n" ::: "memory");
@@ -273,19 +275,36 @@ __global__ void __launch_bounds__(kCopyThreads) evict_copy_kernel(const __grid_c
     }
     uint4 k[kCopyPer], v[kCopyPer];
     float w[kCopyPer];
+    if constexpr (E8) {
+        uint8_t* const rows = reinterpret_cast<uint8_t*>(l16 < 8 ? A.c.k : A.c.v) + (l16 & 7) * 16;
+        float* const one = l16 == 0 ? A.c.weights : l16 == 1 ? A.c.k_scales : A.c.v_scales;
 #pragma unroll
-    for (int i = 0; i < kCopyPer; ++i) {
-        if (src[i] < 0 || dst[i] < 0) continue;
-        k[i] = reinterpret_cast<const uint4*>(A.c.k + src[i] * kHeadDim)[l16];
-        v[i] = reinterpret_cast<const uint4*>(A.c.v + src[i] * kHeadDim)[l16];
-        if (l16 == 0) w[i] = A.c.weights[src[i]];
-    }
+        for (int i = 0; i < kCopyPer; ++i) {
+            if (src[i] < 0 || dst[i] < 0) continue;
+            k[i] = *reinterpret_cast<const uint4*>(rows + src[i] * kHeadDim);
+            if (l16 < 3) w[i] = one[src[i]];
+        }
 #pragma unroll
-    for (int i = 0; i < kCopyPer; ++i) {
-        if (src[i] < 0 || dst[i] < 0) continue;
-        reinterpret_cast<uint4*>(A.c.k + dst[i] * kHeadDim)[l16] = k[i];
-        reinterpret_cast<uint4*>(A.c.v + dst[i] * kHeadDim)[l16] = v[i];
-        if (l16 == 0) A.c.weights[dst[i]] = w[i];
+        for (int i = 0; i < kCopyPer; ++i) {
+            if (src[i] < 0 || dst[i] < 0) continue;
+            *reinterpret_cast<uint4*>(rows + dst[i] * kHeadDim) = k[i];
+            if (l16 < 3) one[dst[i]] = w[i];
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < kCopyPer; ++i) {
+            if (src[i] < 0 || dst[i] < 0) continue;
+            k[i] = reinterpret_cast<const uint4*>(A.c.k + src[i] * kHeadDim)[l16];
+            v[i] = reinterpret_cast<const uint4*>(A.c.v + src[i] * kHeadDim)[l16];
+            if (l16 == 0) w[i] = A.c.weights[src[i]];
+        }
+#pragma unroll
+        for (int i = 0; i < kCopyPer; ++i) {
+            if (src[i] < 0 || dst[i] < 0) continue;
+            reinterpret_cast<uint4*>(A.c.k + dst[i] * kHeadDim)[l16] = k[i];
+            reinterpret_cast<uint4*>(A.c.v + dst[i] * kHeadDim)[l16] = v[i];
+            if (l16 == 0) A.c.weights[dst[i]] = w[i];
+        }
     }
 }
 
@@ -308,7 +327,8 @@ cudaError_t launch_evict(const EvictIO& io, const PagedCacheView& c, cudaStream_
     if (e != cudaSuccess) return e;
     const int most = io.budget < io.max_len ? io.budget : io.max_len;
     const dim3 grid((unsigned)((most + kCopyRows - 1) / kCopyRows), (unsigned)io.Hkv, (unsigned)io.batch);
-    return launch_prio(evict_copy_kernel, grid, dim3(kCopyThreads), 0, st, 0, true, a);
+    return c.k_scales ? launch_prio(evict_copy_kernel<true>, grid, dim3(kCopyThreads), 0, st, 0, true, a)
+                      : launch_prio(evict_copy_kernel<false>, grid, dim3(kCopyThreads), 0, st, 0, true, a);
 }
 
 }  // namespace kvec

@@ -1,4 +1,4 @@
-// The two 16-bit types of keys, values and queries, as one template parameter.
+// The two 16-bit types of keys, values and queries, as one template parameter, and e4m3 numbers.
 #pragma once
 
 #include <cuda_bf16.h>
@@ -51,5 +51,24 @@ struct Half16<__half> {
             : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
     }
 };
+
+// Two e4m3 numbers, the lower byte `lo`; round to nearest even, the largest is 448, NaN stays one.
+__device__ __forceinline__ uint32_t pack_e4m3(float lo, float hi) {
+    uint16_t r;
+    asm("cvt.rn.satfinite.e4m3x2.f32 %0, %2, %1;\n" : "=h"(r) : "f"(lo), "f"(hi));
+    return r;
+}
+// The two in the lower half of w as fp16, which holds every one of them.
+__device__ __forceinline__ uint32_t e4m3_to_half2(uint32_t w) {
+    uint32_t r;
+    asm("{\n\t.reg .b16 l, h;\n\tmov.b32 {l, h}, %1;\n\tcvt.rn.f16x2.e4m3x2 %0, l;\n\t}\n" : "=r"(r) : "r"(w));
+    return r;
+}
+// Those in the upper half.
+__device__ __forceinline__ uint32_t e4m3_to_half2_upper(uint32_t w) {
+    uint32_t r;
+    asm("{\n\t.reg .b16 l, h;\n\tmov.b32 {l, h}, %1;\n\tcvt.rn.f16x2.e4m3x2 %0, h;\n\t}\n" : "=r"(r) : "r"(w));
+    return r;
+}
 
 }  // namespace kvec

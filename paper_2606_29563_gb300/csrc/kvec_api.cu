@@ -1197,6 +1197,18 @@ kvec_status view_cache(const kvec_paged_cache* c, PagedCacheView* v) {
     return KVEC_OK;
 }
 
+// The same with scales: a cache of 8 bits.
+kvec_status view_quant_cache(const kvec_paged_cache* c, const kvec_paged_scales* scales, PagedCacheView* v) {
+    kvec_status s = view_cache(c, v);
+    if (s != KVEC_OK) return s;
+    if (!scales || !scales->k_scales || !scales->v_scales) return fail(KVEC_ERR_INVALID_ARG, "a cache of 8 bits needs k_scales and v_scales");
+    if (!aligned16(scales->k_scales) || !aligned16(scales->v_scales))
+        return fail(KVEC_ERR_INVALID_ARG, "k_scales and v_scales must be 16-byte aligned");
+    v->k_scales = scales->k_scales;
+    v->v_scales = scales->v_scales;
+    return KVEC_OK;
+}
+
 // What a call over pages asks of its handle.
 kvec_status check_paged_handle(kvec_handle* h, int batch, const PagedCacheView* v) {
     if (!h) return fail(KVEC_ERR_INVALID_ARG, "handle is NULL");
@@ -1222,15 +1234,10 @@ float softmax_scale_of(const kvec_params& p) {
 
 bool stride_ok(int64_t s) { return s >= 0 && s % 8 == 0 && s < ((int64_t)1 << 40); }
 
-}  // namespace
-
-kvec_status kvec_rotate_append(kvec_handle* h, const kvec_rotate_args* a, int batch, const int32_t* cu_tokens,
-                               const kvec_paged_cache* cache, kvec_stream_t stream) {
-    if (!a) return fail(KVEC_ERR_INVALID_ARG, "args is NULL");
-    PagedCacheView v{};
+// v: of the cache, looked over.
+kvec_status rotate_append(kvec_handle* h, const kvec_rotate_args* a, int batch, const int32_t* cu_tokens,
+                          const kvec_paged_cache* cache, const PagedCacheView& v, kvec_stream_t stream) {
     if (cache) {
-        kvec_status s = view_cache(cache, &v);
-        if (s != KVEC_OK) return s;
         if (cache->dtype != a->dtype) return fail(KVEC_ERR_INVALID_ARG, "the cache's dtype differs from the inputs'");
     }
     if (a->dtype != KVEC_BF16 && a->dtype != KVEC_FP16)
@@ -1298,6 +1305,28 @@ kvec_status kvec_rotate_append(kvec_handle* h, const kvec_rotate_args* a, int ba
     return KVEC_OK;
 }
 
+}  // namespace
+
+kvec_status kvec_rotate_append(kvec_handle* h, const kvec_rotate_args* a, int batch, const int32_t* cu_tokens,
+                               const kvec_paged_cache* cache, kvec_stream_t stream) {
+    if (!a) return fail(KVEC_ERR_INVALID_ARG, "args is NULL");
+    PagedCacheView v{};
+    if (cache) {
+        kvec_status s = view_cache(cache, &v);
+        if (s != KVEC_OK) return s;
+    }
+    return rotate_append(h, a, batch, cu_tokens, cache, v, stream);
+}
+
+kvec_status kvec_rotate_append_quant(kvec_handle* h, const kvec_rotate_args* a, int batch, const int32_t* cu_tokens,
+                                     const kvec_paged_cache* cache, const kvec_paged_scales* scales,
+                                     kvec_stream_t stream) {
+    if (!a) return fail(KVEC_ERR_INVALID_ARG, "args is NULL");
+    PagedCacheView v{};
+    kvec_status s = view_quant_cache(cache, scales, &v);
+    return s != KVEC_OK ? s : rotate_append(h, a, batch, cu_tokens, cache, v, stream);
+}
+
 size_t kvec_paged_decode_window_bytes(kvec_handle* h, int batch, int max_len, int window, int sinks, int with_weights) {
     if (!h || batch < 1 || batch > h->p.max_batch || max_len < 1 || max_len > kPagedMaxLen || window < 0 || sinks < 0) return 0;
     return paged_decode_scratch(batch, h->p.num_q_heads, max_len, within_length(window), within_length(sinks),
@@ -1308,12 +1337,11 @@ size_t kvec_paged_decode_bytes(kvec_handle* h, int batch, int max_len, int with_
     return kvec_paged_decode_window_bytes(h, batch, max_len, 0, 0, with_weights);
 }
 
-kvec_status kvec_paged_decode(kvec_handle* h, int batch, const void* q, const kvec_paged_cache* cache, int max_len,
-                              int window, int sinks, void* out, void* scratch, size_t scratch_bytes,
-                              kvec_stream_t stream) {
-    PagedCacheView v{};
-    kvec_status s = view_cache(cache, &v);
-    if (s == KVEC_OK) s = check_window(window, sinks);
+namespace {
+
+kvec_status paged_decode(kvec_handle* h, int batch, const void* q, const PagedCacheView& v, int max_len, int window, int sinks,
+                         void* out, void* scratch, size_t scratch_bytes, kvec_stream_t stream) {
+    kvec_status s = check_window(window, sinks);
     if (s != KVEC_OK) return s;
     if (max_len < 1 || max_len > v.capacity)
         return fail(KVEC_ERR_INVALID_ARG, "max_len %d outside [1, max_pages * page_size = %d]", max_len, v.capacity);
@@ -1348,12 +1376,29 @@ kvec_status kvec_paged_decode(kvec_handle* h, int batch, const void* q, const kv
     return KVEC_OK;
 }
 
-kvec_status kvec_paged_evict(kvec_handle* h, int batch, const kvec_paged_cache* cache, const int32_t* new_table,
-                             int new_max_pages, int max_len, int budget, int sinks, int recent, int32_t* new_lens,
-                             int32_t* kept, kvec_stream_t stream) {
+}  // namespace
+
+kvec_status kvec_paged_decode(kvec_handle* h, int batch, const void* q, const kvec_paged_cache* cache, int max_len,
+                              int window, int sinks, void* out, void* scratch, size_t scratch_bytes,
+                              kvec_stream_t stream) {
     PagedCacheView v{};
     kvec_status s = view_cache(cache, &v);
-    if (s != KVEC_OK) return s;
+    return s != KVEC_OK ? s : paged_decode(h, batch, q, v, max_len, window, sinks, out, scratch, scratch_bytes, stream);
+}
+
+kvec_status kvec_paged_decode_quant(kvec_handle* h, int batch, const void* q, const kvec_paged_cache* cache,
+                                    const kvec_paged_scales* scales, int max_len, int window, int sinks, void* out,
+                                    void* scratch, size_t scratch_bytes, kvec_stream_t stream) {
+    PagedCacheView v{};
+    kvec_status s = view_quant_cache(cache, scales, &v);
+    return s != KVEC_OK ? s : paged_decode(h, batch, q, v, max_len, window, sinks, out, scratch, scratch_bytes, stream);
+}
+
+namespace {
+
+kvec_status paged_evict(kvec_handle* h, int batch, const PagedCacheView& v, const int32_t* new_table, int new_max_pages,
+                        int max_len, int budget, int sinks, int recent, int32_t* new_lens, int32_t* kept,
+                        kvec_stream_t stream) {
     if (!v.weights) return fail(KVEC_ERR_INVALID_ARG, "the cache keeps no weights to rank by");
     if (max_len < 1 || max_len > v.capacity)
         return fail(KVEC_ERR_INVALID_ARG, "max_len %d outside [1, max_pages * page_size = %d]", max_len, v.capacity);
@@ -1363,7 +1408,7 @@ kvec_status kvec_paged_evict(kvec_handle* h, int batch, const kvec_paged_cache* 
     if (new_max_pages < 1 || ((long long)new_max_pages << v.log_page) < std::min(budget, max_len))
         return fail(KVEC_ERR_INVALID_ARG, "new_table's %d pages of a sequence hold fewer than min(budget, max_len) slots",
                     new_max_pages);
-    s = check_paged_handle(h, batch, &v);
+    kvec_status s = check_paged_handle(h, batch, &v);
     if (s != KVEC_OK) return s;
     if (!new_table || !new_lens || !kept) return fail(KVEC_ERR_INVALID_ARG, "a device pointer is NULL");
     if (new_table == v.table || new_lens == v.lens)
@@ -1388,6 +1433,56 @@ kvec_status kvec_paged_evict(kvec_handle* h, int batch, const kvec_paged_cache* 
     DeviceGuard guard{prev, h->device};
     cudaError_t e = launch_evict(io, v, reinterpret_cast<cudaStream_t>(stream));
     if (e != cudaSuccess) return cuda_fail(e, "evict launch");
+    return KVEC_OK;
+}
+
+}  // namespace
+
+kvec_status kvec_paged_evict(kvec_handle* h, int batch, const kvec_paged_cache* cache, const int32_t* new_table,
+                             int new_max_pages, int max_len, int budget, int sinks, int recent, int32_t* new_lens,
+                             int32_t* kept, kvec_stream_t stream) {
+    PagedCacheView v{};
+    kvec_status s = view_cache(cache, &v);
+    return s != KVEC_OK ? s : paged_evict(h, batch, v, new_table, new_max_pages, max_len, budget, sinks, recent, new_lens, kept, stream);
+}
+
+kvec_status kvec_paged_evict_quant(kvec_handle* h, int batch, const kvec_paged_cache* cache,
+                                   const kvec_paged_scales* scales, const int32_t* new_table, int new_max_pages,
+                                   int max_len, int budget, int sinks, int recent, int32_t* new_lens, int32_t* kept,
+                                   kvec_stream_t stream) {
+    PagedCacheView v{};
+    kvec_status s = view_quant_cache(cache, scales, &v);
+    return s != KVEC_OK ? s : paged_evict(h, batch, v, new_table, new_max_pages, max_len, budget, sinks, recent, new_lens, kept, stream);
+}
+
+kvec_status kvec_paged_read(kvec_handle* h, int batch, const kvec_paged_cache* cache, const kvec_paged_scales* scales,
+                            const int32_t* first, const int32_t* cu_rows, int num_rows, void* k_out, void* v_out,
+                            kvec_stream_t stream) {
+    PagedCacheView v{};
+    kvec_status s = scales ? view_quant_cache(cache, scales, &v) : view_cache(cache, &v);
+    if (s != KVEC_OK) return s;
+    if (num_rows < 0) return fail(KVEC_ERR_INVALID_ARG, "num_rows %d < 0", num_rows);
+    s = check_paged_handle(h, batch, &v);
+    if (s != KVEC_OK) return s;
+    if (num_rows == 0) return KVEC_OK;
+    if (!cu_rows || !k_out || !v_out) return fail(KVEC_ERR_INVALID_ARG, "a device pointer is NULL");
+    if (!aligned16(k_out) || !aligned16(v_out)) return fail(KVEC_ERR_INVALID_ARG, "k_out and v_out must be 16-byte aligned");
+    if (reinterpret_cast<uintptr_t>(first) % 4 || reinterpret_cast<uintptr_t>(cu_rows) % 4)
+        return fail(KVEC_ERR_INVALID_ARG, "first and cu_rows must be 4-byte aligned");
+    ReadIO io{};
+    io.first = first;
+    io.cu = cu_rows;
+    io.k_out = static_cast<uint16_t*>(k_out);
+    io.v_out = static_cast<uint16_t*>(v_out);
+    io.batch = batch;
+    io.num_rows = num_rows;
+    io.Hkv = h->p.num_kv_heads;
+    int prev = 0;
+    s = set_device(h, &prev);
+    if (s != KVEC_OK) return s;
+    DeviceGuard guard{prev, h->device};
+    cudaError_t e = launch_read(io, v, reinterpret_cast<cudaStream_t>(stream));
+    if (e != cudaSuccess) return cuda_fail(e, "paged read launch");
     return KVEC_OK;
 }
 

@@ -115,7 +115,7 @@ struct DecodeIO {
 // A paged cache as its kernels see it (kvec_paged_cache): rows of kHeadDim values, row
 // (page * Hkv + h) << log_page | slot within the page.
 struct PagedCacheView {
-    uint16_t* k;              // null: no cache
+    uint16_t* k;              // null: no cache; e4m3 numbers of a byte where there are scales
     uint16_t* v;
     float* weights;           // null: none kept
     const int* table;         // [batch][max_pages]
@@ -123,6 +123,15 @@ struct PagedCacheView {
     int dtype;                // kvec_dtype
     int log_page, num_pages, max_pages;
     int capacity;             // max_pages << log_page
+    float *k_scales, *v_scales;   // a factor for each row; null: rows of 16 bits
+};
+
+// A cache's slots as packed 16-bit rows (read_kernel.cu).
+struct ReadIO {
+    const int* first;         // [batch] or null
+    const int* cu;            // [batch + 1]
+    uint16_t *k_out, *v_out;  // [num_rows][Hkv][d]
+    int batch, num_rows, Hkv;
 };
 
 // New tokens' norms, rotation and store (rotate_kernel.cu).
@@ -310,6 +319,7 @@ cudaError_t launch_decode(const DecodeIO& io, int num_sms, cudaStream_t st);
 cudaError_t launch_rotate(const RotateIO& io, const PagedCacheView& c, cudaStream_t st);
 cudaError_t launch_paged_decode(const PagedDecodeIO& io, const PagedCacheView& c, int num_sms, cudaStream_t st);
 size_t paged_decode_scratch(int batch, int Hq, int max_len, int window, int sinks, bool weights, int num_sms);
+cudaError_t launch_read(const ReadIO& io, const PagedCacheView& c, cudaStream_t st);
 cudaError_t launch_evict(const EvictIO& io, const PagedCacheView& c, cudaStream_t st);
 PrefillPlan plan_prefill(int batch, int Hq, int Hkv, int max_q, int max_k, int window, int sinks, int num_sms);
 cudaError_t launch_prefill(const PrefillIO& io, const PrefillPlan& plan, int num_sms, cudaStream_t st);

@@ -34,6 +34,7 @@
 #include <cooperative_groups.h>
 
 #include <algorithm>
+#include <type_traits>
 
 namespace kvec {
 
@@ -43,11 +44,17 @@ namespace cg = cooperative_groups;
 
 constexpr int kPdWarps = 4;
 constexpr int kPdThreads = 32 * kPdWarps;
-constexpr int kPdStages = 3;                 // blocks in a warp's ring
 constexpr int kPdBlock = 16;                 // slots of a block
 constexpr int kPdTile = kPdBlock * 128;      // bytes of 16 rows x 64 columns
-constexpr int kPdStage = 4 * kPdTile;        // K columns 0-63, 64-127, V the same
-constexpr int kPdSmem = kPdWarps * kPdStages * kPdStage + 1024;
+// A block in a warp's ring: K columns 0-63, 64-127 and V the same, or with 8 bits a tile of 16 whole rows each; and
+// how many of them are there.
+template <bool E8>
+constexpr int kPdStage = (E8 ? 2 : 4) * kPdTile;
+template <bool E8>
+constexpr int kPdStages = E8 ? 6 : 3;
+constexpr int kPdRing = kPdStages<false> * kPdStage<false>;
+static_assert(kPdRing == kPdStages<true> * kPdStage<true>, "either format fills the same shared memory");
+constexpr int kPdSmem = kPdWarps * kPdRing + 1024;
 constexpr int kPdCtasPerSm = 2;
 constexpr int kPdMaxCluster = 8;
 constexpr int kPdHeads = 8;                  // most query heads of a KV head
@@ -59,7 +66,7 @@ constexpr int kJoinRows = 8 * kJoinThreads;  // slots of a join block's weights,
 constexpr float kNoLogit = -3.402823466e38f;
 
 struct PdArgs {
-    CUtensorMap kmap, vmap;   // [rows][128], boxes of 16 x 64
+    CUtensorMap kmap, vmap;   // [rows][128], boxes of 16 x 64 (of 16 rows of 128 bytes)
     PagedCacheView c;
     PagedDecodeIO io;
     float* logits;            // [pair][nbmax][g][16]
@@ -222,6 +229,13 @@ __device__ __forceinline__ void ldmatrix_x4_trans(uint32_t addr, uint32_t (&r)[4
                  : "memory");
 }
 
+// The power of two that brings a magnitude to [2^14, 2^15), within the range of normal numbers on both sides, and its
+// inverse.  fp16 products lose nothing near their largest factor then, and 2^-39 of it at most.
+__device__ __forceinline__ float to_fp16_range(float a) {
+    return __uint_as_float((uint32_t)min(268 - (int)(__float_as_uint(a) >> 23), 253) << 23);
+}
+__device__ __forceinline__ float inverse_power(float p) { return __uint_as_float((254u << 23) - __float_as_uint(p)); }
+
 // The products with the weights' roundings and with what these left.  Against an infinite value the rest, which is
 // zero or has either sign, would make NaN of what the roundings give alone.
 __device__ __forceinline__ float with_rest(float hi, float lo) { return fabsf(hi) < INFINITY ? hi + lo : hi; }
@@ -282,13 +296,19 @@ __device__ void add_weights(const PdArgs& A, int s, int h, const Visible& v, int
 }
 
 // CL: a cluster of CTAs per pair (grid splits x Hkv x batch) instead of a share of the list.
-template <class T, bool CL>
+// E8: rows of e4m3 numbers with a scale each.  They become fp16, which holds them all, on their way from shared memory
+// to the tiles: the scale of a key multiplies its logit, that of a value its weight.  For that the
+// queries (in bf16) and the values' scales are brought to fp16's range by powers of two, a row's and the warp's so far.
+template <class T, bool CL, bool E8>
 __global__ void __launch_bounds__(kPdThreads, kPdCtasPerSm) paged_decode_kernel(const __grid_constant__ PdArgs A) {
+    constexpr int kStage = kPdStage<E8>, kStages = kPdStages<E8>;
+    using Operand = std::conditional_t<E8, __half, T>;          // the tiles' type
     extern __shared__ uint8_t pd_smem_raw[];
     // 1024-byte alignment for the swizzled tiles.
     uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(pd_smem_raw) + 1023) & ~uintptr_t(1023));
-    __shared__ __align__(8) uint64_t full[kPdWarps][kPdStages];
-    __shared__ int srow[kPdWarps][kPdStages];                   // first row of the staged block, -1: none
+    __shared__ __align__(8) uint64_t full[kPdWarps][kStages];
+    __shared__ int srow[kPdWarps][kStages];                    // first row of the staged block, -1: none
+    __shared__ __align__(16) float scales[kPdWarps][E8 ? kStages : 1][2][kPdBlock];   // of the staged block's K and V
     __shared__ float wm[kPdWarps][kPdHeads], wl[kPdWarps][kPdHeads];
     __shared__ float* wacc[kPdWarps];                           // the warps' outputs, each in its free stage
     __shared__ float cm[kPdHeads], cl[kPdHeads], fm[kPdHeads], finv[kPdHeads];
@@ -299,7 +319,7 @@ __global__ void __launch_bounds__(kPdThreads, kPdCtasPerSm) paged_decode_kernel(
         ptx::prefetch_tensormap(&A.kmap);
         ptx::prefetch_tensormap(&A.vmap);
         for (int w = 0; w < kPdWarps; ++w)
-            for (int i = 0; i < kPdStages; ++i) ptx::mbar_init(&full[w][i], 1);
+            for (int i = 0; i < kStages; ++i) ptx::mbar_init(&full[w][i], 1);
         ptx::fence_barrier_init();
     }
     __syncthreads();
@@ -336,10 +356,10 @@ __global__ void __launch_bounds__(kPdThreads, kPdCtasPerSm) paged_decode_kernel(
         }
     }
 
-    uint8_t* ring = smem + warp * (kPdStages * kPdStage);
+    uint8_t* ring = smem + warp * kPdRing;
     const uint32_t ring32 = ptx::smem_u32(ring);
     // Loads: this warp's blocks are warp, warp + 4, ... of the CTA's; load number k goes to
-    // stage k % kPdStages, and one stage is free while a block is worked on.
+    // stage k % kStages, and one stage is free while a block is worked on.
     // The rows of the next two are fetched ahead: a page's number takes as long as its rows.
     Walker ld = cur;
     int ld_at = warp, row_at = warp;      // the next load, the next row to fetch
@@ -363,23 +383,29 @@ __global__ void __launch_bounds__(kPdThreads, kPdCtasPerSm) paged_decode_kernel(
             if (ptx::elect_one()) {
                 srow[warp][at] = row;
                 if (row >= 0 && !(A.fault && warp == 0 && blockIdx.x == 0)) {
-                    uint8_t* dst = ring + at * kPdStage;
+                    uint8_t* dst = ring + at * kStage;
                     uint64_t* bar = &full[warp][at];
-                    ptx::mbar_arrive_expect_tx(bar, kPdStage);
+                    ptx::mbar_arrive_expect_tx(bar, kStage + (E8 ? 2 * kPdBlock * 4 : 0));
                     ptx::tma_load_2d(dst, &A.kmap, bar, 0, row);
-                    ptx::tma_load_2d(dst + kPdTile, &A.kmap, bar, 64, row);
-                    ptx::tma_load_2d(dst + 2 * kPdTile, &A.vmap, bar, 0, row);
-                    ptx::tma_load_2d(dst + 3 * kPdTile, &A.vmap, bar, 64, row);
+                    if constexpr (E8) {
+                        ptx::tma_load_2d(dst + kPdTile, &A.vmap, bar, 0, row);
+                        ptx::bulk_load(scales[warp][at][0], A.c.k_scales + row, kPdBlock * 4, bar);
+                        ptx::bulk_load(scales[warp][at][1], A.c.v_scales + row, kPdBlock * 4, bar);
+                    } else {
+                        ptx::tma_load_2d(dst + kPdTile, &A.kmap, bar, 64, row);
+                        ptx::tma_load_2d(dst + 2 * kPdTile, &A.vmap, bar, 0, row);
+                        ptx::tma_load_2d(dst + 3 * kPdTile, &A.vmap, bar, 64, row);
+                    }
                 }
             }
             ld_at += kPdWarps;
             rows[0] = rows[1];
             rows[1] = next_row();
         }
-        ld_stage = ld_stage + 1 == kPdStages ? 0 : ld_stage + 1;
+        ld_stage = ld_stage + 1 == kStages ? 0 : ld_stage + 1;
     };
 #pragma unroll
-    for (int i = 0; i < kPdStages - 1; ++i) load_next();
+    for (int i = 0; i < kStages - 1; ++i) load_next();
     __syncwarp();
 
     int st = 0;               // stage of this warp's next block
@@ -394,7 +420,37 @@ __global__ void __launch_bounds__(kPdThreads, kPdCtasPerSm) paged_decode_kernel(
         const bool whole = len == v.nb;
         // The group's query rows as the upper half of the tile's row operand: head lane / 4.
         uint32_t qa[8][2];
-        {
+        float sl2 = A.sl2;             // with E8 also what the row was divided by
+        if constexpr (E8) {
+            // Columns 16 kk + 4 (lane % 4) on, in the order in which a key's bytes lie in a lane's word.
+            const int j = lane >> 2;
+            const uint2* qr =
+                reinterpret_cast<const uint2*>(A.io.q + ((size_t)s * Hq + (size_t)h * g + (j < g ? j : 0)) * kHeadDim) + (lane & 3);
+#pragma unroll
+            for (int kk = 0; kk < 8; ++kk) {
+                const uint2 w = j < g ? __ldg(qr + 4 * kk) : make_uint2(0u, 0u);
+                qa[kk][0] = w.x;
+                qa[kk][1] = w.y;
+            }
+            if constexpr (!std::is_same_v<T, __half>) {
+                float top = 0.f;       // of the finite ones
+#pragma unroll
+                for (int kk = 0; kk < 16; ++kk) {
+                    const float2 f = Half16<T>::unpack(qa[kk >> 1][kk & 1]);
+                    top = fabsf(f.x) < INFINITY ? fmaxf(top, fabsf(f.x)) : top;
+                    top = fabsf(f.y) < INFINITY ? fmaxf(top, fabsf(f.y)) : top;
+                }
+                top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
+                top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
+                const float up = to_fp16_range(top);
+                sl2 *= inverse_power(up);
+#pragma unroll
+                for (int kk = 0; kk < 16; ++kk) {
+                    const float2 f = Half16<T>::unpack(qa[kk >> 1][kk & 1]);
+                    qa[kk >> 1][kk & 1] = Half16<__half>::pack(f.x * up, f.y * up);
+                }
+            }
+        } else {
             const int j = lane >> 2;
             const uint32_t* qr =
                 reinterpret_cast<const uint32_t*>(A.io.q + ((size_t)s * Hq + (size_t)h * g + (j < g ? j : 0)) * kHeadDim) +
@@ -411,13 +467,14 @@ __global__ void __launch_bounds__(kPdThreads, kPdCtasPerSm) paged_decode_kernel(
 #pragma unroll
             for (int c = 0; c < 4; ++c) acc[d][c] = 0.f;
         float m = kNoLogit, l = 0.f;   // head lane / 4; l of this lane's slots
+        float up = to_fp16_range(0.f); // E8: acc is this times the sums
         // The warp's first block of the segment: its blocks are warp mod kPdWarps of the CTA's.
         const int skip = (warp - done % kPdWarps + kPdWarps) % kPdWarps;
         for (int e = skip; e < len; e += kPdWarps) {
             const int i = i_begin + e, b = v.block(i);
             __syncwarp();
             const int row = srow[warp][st];
-            const uint32_t src = ring32 + st * kPdStage;
+            const uint32_t src = ring32 + st * kStage;
             float x[2][4];
             if (row >= 0) {
                 if (!failed && !__all_sync(0xffffffffu, ptx::mbar_wait(&full[warp][st], (phases >> st) & 1u))) {
@@ -431,24 +488,51 @@ __global__ void __launch_bounds__(kPdThreads, kPdCtasPerSm) paged_decode_kernel(
                     for (int c = 0; c < 4; ++c) x[t][c] = 0.f;
                 // Logits: key row (lane & 7) + 8 (lane / 16), columns 16 kk + 8 (lane / 8 % 2).
                 const int kr = (lane & 7) + ((lane >> 4) << 3);
+                if constexpr (E8) {
+                    // Bytes 16 c + 4 (lane % 4) on of key row lane / 4 (+ 8): the lower two meet the tile's lower columns.
 #pragma unroll
-                for (int kk = 0; kk < 8; ++kk) {
-                    uint32_t kb[4];
-                    const int chunk = (2 * kk + ((lane >> 3) & 1)) & 7;
-                    ldmatrix_x4(src + (kk >> 2) * kPdTile + kr * 128 + ((chunk ^ (kr & 7)) << 4), kb);
-                    Half16<T>::mma(x[0], qa[kk][0], 0u, qa[kk][1], 0u, kb[0], kb[1]);
-                    Half16<T>::mma(x[1], qa[kk][0], 0u, qa[kk][1], 0u, kb[2], kb[3]);
+                    for (int kk = 0; kk < 4; ++kk) {
+                        uint32_t kb[4];
+                        const int chunk = 2 * kk + ((lane >> 3) & 1);
+                        ldmatrix_x4(src + kr * 128 + ((chunk ^ (kr & 7)) << 4), kb);
+#pragma unroll
+                        for (int c = 0; c < 2; ++c)
+#pragma unroll
+                            for (int t = 0; t < 2; ++t)
+                                Half16<Operand>::mma(x[t], qa[2 * kk + c][0], 0u, qa[2 * kk + c][1], 0u, e4m3_to_half2(kb[2 * t + c]),
+                                               e4m3_to_half2_upper(kb[2 * t + c]));
+                    }
+                } else {
+#pragma unroll
+                    for (int kk = 0; kk < 8; ++kk) {
+                        uint32_t kb[4];
+                        const int chunk = (2 * kk + ((lane >> 3) & 1)) & 7;
+                        ldmatrix_x4(src + (kk >> 2) * kPdTile + kr * 128 + ((chunk ^ (kr & 7)) << 4), kb);
+                        Half16<Operand>::mma(x[0], qa[kk][0], 0u, qa[kk][1], 0u, kb[0], kb[1]);
+                        Half16<Operand>::mma(x[1], qa[kk][0], 0u, qa[kk][1], 0u, kb[2], kb[3]);
+                    }
                 }
             }
             // This lane's slots: 8 t + 2 (lane % 4) + c.
             const bool all = row >= 0 && v.whole(b);
+            float vs[2][2];           // E8: the values' scales, 0 where no one sees them
 #pragma unroll
-            for (int t = 0; t < 2; ++t)
+            for (int t = 0; t < 2; ++t) {
+                float2 ks2 = make_float2(1.f, 1.f), vs2 = ks2;
+                if constexpr (E8) {
+                    if (row >= 0) {
+                        ks2 = *reinterpret_cast<const float2*>(&scales[warp][st][0][8 * t + 2 * (lane & 3)]);
+                        vs2 = *reinterpret_cast<const float2*>(&scales[warp][st][1][8 * t + 2 * (lane & 3)]);
+                    }
+                }
 #pragma unroll
                 for (int c = 0; c < 2; ++c) {
                     const int slot = b * kPdBlock + 8 * t + 2 * (lane & 3) + c;
-                    x[t][c] = all || (row >= 0 && v.sees(slot)) ? x[t][c] * A.sl2 : -INFINITY;
+                    const bool seen = all || (row >= 0 && v.sees(slot));
+                    x[t][c] = seen ? x[t][c] * (E8 ? sl2 * (c ? ks2.y : ks2.x) : sl2) : -INFINITY;
+                    vs[t][c] = seen ? (c ? vs2.y : vs2.x) : 0.f;
                 }
+            }
             if (A.c.weights && (lane >> 2) < g) {
                 float* lg = A.logits + (((size_t)s * Hkv + h) * A.nbmax + i) * (size_t)(g * kPdBlock) +
                             (lane >> 2) * kPdBlock + 2 * (lane & 3);
@@ -459,8 +543,8 @@ __global__ void __launch_bounds__(kPdThreads, kPdCtasPerSm) paged_decode_kernel(
                 if (!all) {
                     // Values that no one sees may be anything: zeros meet the weights of zero.
                     for (int r = 0; r < kPdBlock; ++r)
-                        if (!v.sees(b * kPdBlock + r) && lane < 16)
-                            ptx::st_shared_v4(src + (2 + (lane >> 3)) * kPdTile + r * 128 + ((lane & 7) << 4), 0u, 0u, 0u, 0u);
+                        if (!v.sees(b * kPdBlock + r) && lane < (E8 ? 8 : 16))
+                            ptx::st_shared_v4(src + (E8 ? 1 : 2 + (lane >> 3)) * kPdTile + r * 128 + ((lane & 7) << 4), 0u, 0u, 0u, 0u);
                     ptx::fence_proxy_async_smem();   // before the stage's next TMA load
                     __syncwarp();
                 }
@@ -468,6 +552,26 @@ __global__ void __launch_bounds__(kPdThreads, kPdCtasPerSm) paged_decode_kernel(
                 t = fmaxf(t, __shfl_xor_sync(0xffffffffu, t, 1));
                 t = fmaxf(t, __shfl_xor_sync(0xffffffffu, t, 2));
                 const float mn = fmaxf(m, t);
+                if constexpr (E8) {
+                    // The block's largest finite scale, the same for every lane, may lower the power of two.
+                    float top = 0.f;
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) {
+                        const float a = fabsf(vs[k >> 1][k & 1]);
+                        top = a < INFINITY ? fmaxf(top, a) : top;
+                    }
+                    top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
+                    top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
+                    const float to = to_fp16_range(top);
+                    if (to < up) {
+                        const float down = to * inverse_power(up);
+                        up = to;
+#pragma unroll
+                        for (int d = 0; d < 16; ++d)
+#pragma unroll
+                            for (int c = 0; c < 4; ++c) acc[d][c] *= down;
+                    }
+                }
                 if (__any_sync(0xffffffffu, mn != m)) {
                     const float corr = ptx::ex2(m - mn);   // 0 from kNoLogit on
                     l *= corr;
@@ -480,31 +584,52 @@ __global__ void __launch_bounds__(kPdThreads, kPdCtasPerSm) paged_decode_kernel(
                 uint32_t hi[2], lo[2];
 #pragma unroll
                 for (int t2 = 0; t2 < 2; ++t2) {
-                    const float p0 = ptx::ex2(x[t2][0] - m), p1 = ptx::ex2(x[t2][1] - m);
+                    float p0 = ptx::ex2(x[t2][0] - m), p1 = ptx::ex2(x[t2][1] - m);
                     l += p0 + p1;
-                    hi[t2] = Half16<T>::pack(p0, p1);
-                    const float2 r = Half16<T>::unpack(hi[t2]);
-                    lo[t2] = Half16<T>::pack(p0 - r.x, p1 - r.y);
+                    if constexpr (E8) {
+                        p0 *= vs[t2][0] * up;
+                        p1 *= vs[t2][1] * up;
+                    }
+                    hi[t2] = Half16<Operand>::pack(p0, p1);
+                    const float2 r = Half16<Operand>::unpack(hi[t2]);
+                    lo[t2] = Half16<Operand>::pack(p0 - r.x, p1 - r.y);
                 }
                 // Values: row (lane & 7) + 8 (lane / 8 % 2), columns 16 dd + 8 (lane / 16).
                 const int vr = (lane & 7) + (((lane >> 3) & 1) << 3);
+                if constexpr (E8) {
+                    // A word holds two slots' columns 2 n and 2 n + 1: a tile of the even columns, one of the odd.
 #pragma unroll
-                for (int dd = 0; dd < 8; ++dd) {
-                    uint32_t vb[4];
-                    const int chunk = (2 * dd + (lane >> 4)) & 7;
-                    ldmatrix_x4_trans(src + (2 + (dd >> 2)) * kPdTile + vr * 128 + ((chunk ^ (vr & 7)) << 4), vb);
-                    Half16<T>::mma(acc[2 * dd], hi[0], lo[0], hi[1], lo[1], vb[0], vb[1]);
-                    Half16<T>::mma(acc[2 * dd + 1], hi[0], lo[0], hi[1], lo[1], vb[2], vb[3]);
+                    for (int dd = 0; dd < 4; ++dd) {
+                        uint32_t vb[4];
+                        const int chunk = 2 * dd + (lane >> 4);
+                        ldmatrix_x4_trans(src + kPdTile + vr * 128 + ((chunk ^ (vr & 7)) << 4), vb);
+#pragma unroll
+                        for (int c = 0; c < 2; ++c) {
+                            const uint32_t a = __byte_perm(vb[2 * c], 0u, 0x3120), b8 = __byte_perm(vb[2 * c + 1], 0u, 0x3120);
+                            Half16<Operand>::mma(acc[4 * dd + 2 * c], hi[0], lo[0], hi[1], lo[1], e4m3_to_half2(a), e4m3_to_half2(b8));
+                            Half16<Operand>::mma(acc[4 * dd + 2 * c + 1], hi[0], lo[0], hi[1], lo[1], e4m3_to_half2_upper(a),
+                                           e4m3_to_half2_upper(b8));
+                        }
+                    }
+                } else {
+#pragma unroll
+                    for (int dd = 0; dd < 8; ++dd) {
+                        uint32_t vb[4];
+                        const int chunk = (2 * dd + (lane >> 4)) & 7;
+                        ldmatrix_x4_trans(src + (2 + (dd >> 2)) * kPdTile + vr * 128 + ((chunk ^ (vr & 7)) << 4), vb);
+                        Half16<Operand>::mma(acc[2 * dd], hi[0], lo[0], hi[1], lo[1], vb[0], vb[1]);
+                        Half16<Operand>::mma(acc[2 * dd + 1], hi[0], lo[0], hi[1], lo[1], vb[2], vb[3]);
+                    }
                 }
             }
             __syncwarp();   // every lane is done with the stage's tiles and row
-            st = st + 1 == kPdStages ? 0 : st + 1;
+            st = st + 1 == kStages ? 0 : st + 1;
             load_next();    // into the stage that the step before freed; this step's is free now
         }
         // The warp's (maximum, sum, outputs), in its free stage: the one before st.
         l += __shfl_xor_sync(0xffffffffu, l, 1);
         l += __shfl_xor_sync(0xffffffffu, l, 2);
-        float* mine = reinterpret_cast<float*>(ring + (st == 0 ? kPdStages - 1 : st - 1) * kPdStage);
+        float* mine = reinterpret_cast<float*>(ring + (st == 0 ? kStages - 1 : st - 1) * kStage);
         {
             const int j = lane >> 2;
             if ((lane & 3) == 0) {
@@ -512,10 +637,19 @@ __global__ void __launch_bounds__(kPdThreads, kPdCtasPerSm) paged_decode_kernel(
                 wl[warp][j] = l;
             }
             if (lane == 0) wacc[warp] = mine;
+            if constexpr (E8) {
+                const float down = inverse_power(up);
 #pragma unroll
-            for (int d = 0; d < 16; ++d)
-                *reinterpret_cast<float2*>(mine + j * kHeadDim + d * 8 + 2 * (lane & 3)) =
-                    make_float2(with_rest(acc[d][0], acc[d][2]), with_rest(acc[d][1], acc[d][3]));
+                for (int d = 0; d < 16; d += 2)
+                    *reinterpret_cast<float4*>(mine + j * kHeadDim + d * 8 + 4 * (lane & 3)) =
+                        make_float4(with_rest(acc[d][0], acc[d][2]) * down, with_rest(acc[d + 1][0], acc[d + 1][2]) * down,
+                                    with_rest(acc[d][1], acc[d][3]) * down, with_rest(acc[d + 1][1], acc[d + 1][3]) * down);
+            } else {
+#pragma unroll
+                for (int d = 0; d < 16; ++d)
+                    *reinterpret_cast<float2*>(mine + j * kHeadDim + d * 8 + 2 * (lane & 3)) =
+                        make_float2(with_rest(acc[d][0], acc[d][2]), with_rest(acc[d][1], acc[d][3]));
+            }
         }
         __syncthreads();
         for (int e = tid; e < g * kHeadDim; e += kPdThreads) {
@@ -602,7 +736,7 @@ __global__ void __launch_bounds__(kPdThreads, kPdCtasPerSm) paged_decode_kernel(
     }
     // Copies in flight land before the CTA may exit (a stage without one runs into the limit).
     if (failed)
-        for (int i = 0; i < kPdStages; ++i) ptx::mbar_wait(&full[warp][i], (phases >> i) & 1u, 20000000ull);
+        for (int i = 0; i < kStages; ++i) ptx::mbar_wait(&full[warp][i], (phases >> i) & 1u, 20000000ull);
 }
 
 // The pairs whose blocks several CTAs share.  Block x = 0 of (x, h, s) joins the outputs, a warp a query head, the
@@ -699,7 +833,7 @@ size_t round16(size_t x) { return (x + 15) & ~size_t(15); }
 
 int share_ctas(int num_sms) { return kPdCtasPerSm * num_sms; }
 
-template <class T>
+template <class T, bool E8>
 cudaError_t launch_typed(const PdArgs& a, cudaStream_t st) {
     // CTAs of a pair: the largest cluster that fits the device's resident CTAs in one wave, with
     // two blocks a warp and more; taken where that leaves a CTA 32 blocks and less (a quarter of
@@ -725,9 +859,9 @@ cudaError_t launch_typed(const PdArgs& a, cudaStream_t st) {
         attr[1].val.programmaticStreamSerializationAllowed = 1;
         cfg.attrs = attr;
         cfg.numAttrs = 2;
-        return cudaLaunchKernelEx(&cfg, paged_decode_kernel<T, true>, a);
+        return cudaLaunchKernelEx(&cfg, paged_decode_kernel<T, true, E8>, a);
     }
-    cudaError_t e = launch_prio(paged_decode_kernel<T, false>, dim3(a.ctas), dim3(kPdThreads), kPdSmem, st, 0, true, a);
+    cudaError_t e = launch_prio(paged_decode_kernel<T, false, E8>, dim3(a.ctas), dim3(kPdThreads), kPdSmem, st, 0, true, a);
     if (e != cudaSuccess) return e;
     const int rows = a.c.weights ? (a.nbmax * kPdBlock + kJoinRows - 1) / kJoinRows : 0;
     return launch_prio(paged_join_kernel<T>, dim3(1 + rows, a.io.Hkv, a.io.batch), dim3(kJoinThreads),
@@ -757,17 +891,23 @@ cudaError_t configure_paged_decode() {
     auto one = [&](auto kernel) {
         if (e == cudaSuccess) e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kPdSmem);
     };
-    one(paged_decode_kernel<__nv_bfloat16, true>);
-    one(paged_decode_kernel<__nv_bfloat16, false>);
-    one(paged_decode_kernel<__half, true>);
-    one(paged_decode_kernel<__half, false>);
+    one(paged_decode_kernel<__nv_bfloat16, true, false>);
+    one(paged_decode_kernel<__nv_bfloat16, false, false>);
+    one(paged_decode_kernel<__half, true, false>);
+    one(paged_decode_kernel<__half, false, false>);
+    one(paged_decode_kernel<__nv_bfloat16, true, true>);
+    one(paged_decode_kernel<__nv_bfloat16, false, true>);
+    one(paged_decode_kernel<__half, true, true>);
+    one(paged_decode_kernel<__half, false, true>);
     return e;
 }
 
 cudaError_t launch_paged_decode(const PagedDecodeIO& io, const PagedCacheView& c, int num_sms, cudaStream_t st) {
     PdArgs a{};
-    const uint64_t dims[2] = {(uint64_t)kHeadDim, ((uint64_t)c.num_pages * io.Hkv) << c.log_page};
-    const uint64_t strides[1] = {(uint64_t)kHeadDim * 2};
+    // Rows of 8 bits as 64 elements of 16: the copies only move them.
+    const bool e8 = c.k_scales != nullptr;
+    const uint64_t dims[2] = {(uint64_t)(e8 ? kHeadDim / 2 : kHeadDim), ((uint64_t)c.num_pages * io.Hkv) << c.log_page};
+    const uint64_t strides[1] = {dims[0] * 2};
     const uint32_t box[2] = {64, (uint32_t)kPdBlock};
     cudaError_t e = encode_tensor_map(&a.kmap, c.dtype, 2, c.k, dims, strides, box);
     if (e == cudaSuccess) e = encode_tensor_map(&a.vmap, c.dtype, 2, c.v, dims, strides, box);
@@ -788,7 +928,8 @@ cudaError_t launch_paged_decode(const PagedDecodeIO& io, const PagedCacheView& c
     a.part_ml = reinterpret_cast<float2*>(p);
     p += round16(slots * sizeof(float2));
     a.logits = reinterpret_cast<float*>(p);
-    return c.dtype == 1 ? launch_typed<__half>(a, st) : launch_typed<__nv_bfloat16>(a, st);
+    if (e8) return c.dtype == 1 ? launch_typed<__half, true>(a, st) : launch_typed<__nv_bfloat16, true>(a, st);
+    return c.dtype == 1 ? launch_typed<__half, false>(a, st) : launch_typed<__nv_bfloat16, false>(a, st);
 }
 
 }  // namespace kvec

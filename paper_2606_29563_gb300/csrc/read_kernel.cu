@@ -1,0 +1,111 @@
+// A cache's slots as packed rows of 16 bits, [row][KV head][d], as prefill_attention takes keys and values: the
+// cache behind a prompt's next chunk.  Numbers of 8 bits times their row's scale, in fp32, rounded once.
+//
+// A block takes a few tokens, whose places (sequence, page) a thread each finds first; then a half-warp moves a
+// (token, head)'s rows of K and of V, eight values a lane, several in flight.
+#include "half_types.cuh"
+#include "kvec_internal.cuh"
+
+namespace kvec {
+
+namespace {
+
+constexpr int kReadThreads = 128;
+constexpr int kReadTokens = 8;      // of a block
+constexpr int kReadPer = 4;         // (token, head)s of a half-warp in flight
+
+struct ReadArgs {
+    ReadIO io;
+    PagedCacheView c;
+};
+
+// Row of KV head 0 that output row t comes from; -1: none, its values are zeros; -2: behind the last sequence.
+__device__ __forceinline__ long long source_row(const ReadArgs& A, int t) {
+    const ReadIO& io = A.io;
+    int lo = 0, hi = io.batch;   // the last sequence that starts at or before t
+    while (lo < hi) {
+        const int mid = (lo + hi + 1) >> 1;
+        if (__ldg(&io.cu[mid]) <= t) lo = mid; else hi = mid - 1;
+    }
+    if (lo >= io.batch) return -2;
+    const long long slot = (io.first ? (long long)__ldg(&io.first[lo]) : 0) + t - __ldg(&io.cu[lo]);
+    if (slot < 0 || slot >= A.c.capacity || slot >= __ldg(&A.c.lens[lo])) return -1;
+    const int page = __ldg(&A.c.table[(size_t)lo * A.c.max_pages + (slot >> A.c.log_page)]);
+    if (page < 0 || page >= A.c.num_pages) return -1;
+    return ((long long)page * io.Hkv << A.c.log_page) + (slot & ((1 << A.c.log_page) - 1));
+}
+
+// Eight e4m3 numbers times a factor, rounded to T.
+template <class T>
+__device__ __forceinline__ uint4 widened(const uint2& w, float s) {
+    uint32_t r[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const uint32_t u = i < 2 ? w.x : w.y;
+        const float2 f = Half16<__half>::unpack(i & 1 ? e4m3_to_half2_upper(u) : e4m3_to_half2(u));
+        r[i] = Half16<T>::pack(f.x * s, f.y * s);
+    }
+    return make_uint4(r[0], r[1], r[2], r[3]);
+}
+
+template <class T, bool E8>
+__global__ void __launch_bounds__(kReadThreads) read_kernel(const __grid_constant__ ReadArgs A) {
+    __shared__ long long from[kReadTokens];
+    asm volatile("griddepcontrol.launch_dependents;\n" ::: "memory");
+    asm volatile("griddepcontrol.wait;\n" ::: "memory");
+    const int t0 = blockIdx.x * kReadTokens, nt = min(kReadTokens, A.io.num_rows - t0), Hkv = A.io.Hkv;
+    if (threadIdx.x < nt) from[threadIdx.x] = source_row(A, t0 + threadIdx.x);
+    __syncthreads();
+    const int l16 = threadIdx.x & 15, items = nt * Hkv;
+    constexpr int kHalves = kReadThreads / 16;
+    for (int e0 = threadIdx.x >> 4; e0 < items; e0 += kHalves * kReadPer) {
+        long long src[kReadPer];
+        uint4 k[kReadPer], v[kReadPer];
+        uint2 k8[kReadPer], v8[kReadPer];
+        float ks[kReadPer], vs[kReadPer];
+#pragma unroll
+        for (int i = 0; i < kReadPer; ++i) {
+            const int e = e0 + i * kHalves, t = e / Hkv;
+            src[i] = -2;
+            k[i] = v[i] = make_uint4(0u, 0u, 0u, 0u);
+            k8[i] = v8[i] = make_uint2(0u, 0u);
+            ks[i] = vs[i] = 0.f;
+            if (e >= items) continue;
+            src[i] = from[t];
+            if (src[i] < 0) continue;
+            const size_t row = (size_t)src[i] + ((size_t)(e - t * Hkv) << A.c.log_page);
+            if constexpr (E8) {
+                k8[i] = __ldg(reinterpret_cast<const uint2*>(reinterpret_cast<const uint8_t*>(A.c.k) + row * kHeadDim) + l16);
+                v8[i] = __ldg(reinterpret_cast<const uint2*>(reinterpret_cast<const uint8_t*>(A.c.v) + row * kHeadDim) + l16);
+                ks[i] = __ldg(&A.c.k_scales[row]);
+                vs[i] = __ldg(&A.c.v_scales[row]);
+            } else {
+                k[i] = __ldg(reinterpret_cast<const uint4*>(A.c.k + row * kHeadDim) + l16);
+                v[i] = __ldg(reinterpret_cast<const uint4*>(A.c.v + row * kHeadDim) + l16);
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < kReadPer; ++i) {
+            if (src[i] == -2) continue;
+            const size_t to = ((size_t)t0 * Hkv + e0 + i * kHalves) * kHeadDim;
+            if constexpr (E8) {
+                k[i] = widened<T>(k8[i], ks[i]);
+                v[i] = widened<T>(v8[i], vs[i]);
+            }
+            reinterpret_cast<uint4*>(A.io.k_out + to)[l16] = k[i];
+            reinterpret_cast<uint4*>(A.io.v_out + to)[l16] = v[i];
+        }
+    }
+}
+
+}  // namespace
+
+cudaError_t launch_read(const ReadIO& io, const PagedCacheView& c, cudaStream_t st) {
+    const ReadArgs a{io, c};
+    const dim3 grid((unsigned)((io.num_rows + kReadTokens - 1) / kReadTokens));
+    auto launch = [&](auto kernel) { return launch_prio(kernel, grid, dim3(kReadThreads), 0, st, 0, true, a); };
+    if (!c.k_scales) return launch(read_kernel<__nv_bfloat16, false>);   // copies: any type of 16 bits
+    return c.dtype == 1 ? launch(read_kernel<__half, true>) : launch(read_kernel<__nv_bfloat16, true>);
+}
+
+}  // namespace kvec

@@ -82,8 +82,30 @@ __device__ __forceinline__ Place place_of(const RotateArgs& A, int t) {
     return p;
 }
 
-// NR: rows of a token that a half-warp takes, NT: tokens of a block.  IL: interleaved pairs.
-template <class T, int NR, int NT, bool IL>
+// A cache of 8 bits: the row's largest magnitude fills e4m3's range, s = max(max|y| / 448, 2^-126), and y / s is
+// rounded; both divisions are exact to the last bit, as a quotient beside the middle of two e4m3 numbers must fall to
+// its own side.  Magnitudes are compared as integers, by which NaN is the largest: a row that holds one, or an
+// infinity, gets a scale of NaN or infinity and is NaN when it is read.
+constexpr float kMostE4m3 = 448.f, kLeastScale = 1.1754943508222875e-38f;
+
+// Eight values of a row, by the sixteen lanes of a half-warp; the row's scale.
+__device__ __forceinline__ float quantise_row(const float (&y)[8], uint2* out) {
+    uint32_t top = 0u;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) top = max(top, __float_as_uint(y[e]) & 0x7fffffffu);
+#pragma unroll
+    for (int o = 8; o; o >>= 1) top = max(top, __shfl_xor_sync(0xffffffffu, top, o));
+    float s = __fdiv_rn(__uint_as_float(top), kMostE4m3);
+    s = s < kLeastScale ? kLeastScale : s;
+    float z[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) z[e] = __fdiv_rn(y[e], s);
+    *out = make_uint2(pack_e4m3(z[0], z[1]) | pack_e4m3(z[2], z[3]) << 16, pack_e4m3(z[4], z[5]) | pack_e4m3(z[6], z[7]) << 16);
+    return s;
+}
+
+// NR: rows of a token that a half-warp takes, NT: tokens of a block.  IL: interleaved pairs.  E8: the cache holds 8 bits.
+template <class T, int NR, int NT, bool IL, bool E8>
 __global__ void __launch_bounds__(32 * kRotWarps, 8) rotate_kernel(const __grid_constant__ RotateArgs A) {
     __shared__ Place places[NT];
     const int lane = threadIdx.x & 31, l16 = lane & 15;
@@ -140,9 +162,9 @@ __global__ void __launch_bounds__(32 * kRotWarps, 8) rotate_kernel(const __grid_
             const int u = u0 + i * kRotRows;
             const bool isq = u < Hq, isk = !isq && u < Hq + Hkv;
             uint4 out = x[i];   // a value row is copied as it is
+            float y[8];
             // The half-warps of a warp share the shuffles: both stay, whatever they store.
             if (__any_sync(0xffffffffu, isq || isk)) {
-                float y[8];
                 unpack8<T>(x[i], y);
                 const uint16_t* norm = isq ? io.q_norm : isk ? io.k_norm : nullptr;
                 if (io.q_norm || io.k_norm) {
@@ -179,6 +201,14 @@ __global__ void __launch_bounds__(32 * kRotWarps, 8) rotate_kernel(const __grid_
                     out = make_uint4(Half16<T>::pack(y[0], y[1]), Half16<T>::pack(y[2], y[3]), Half16<T>::pack(y[4], y[5]),
                                      Half16<T>::pack(y[6], y[7]));
             }
+            uint2 bytes;
+            float scale;
+            if constexpr (E8) {
+                if (__any_sync(0xffffffffu, !isq && u < heads)) {
+                    if (!isq && !isk) unpack8<T>(x[i], y);
+                    scale = quantise_row(y, &bytes);
+                }
+            }
             if (u >= heads) continue;
             if (isq) {
                 reinterpret_cast<uint4*>(io.q_out + ((size_t)t * Hq + u) * kHeadDim)[l16] = out;
@@ -188,7 +218,12 @@ __global__ void __launch_bounds__(32 * kRotWarps, 8) rotate_kernel(const __grid_
             if (isk && io.k_out) reinterpret_cast<uint4*>(io.k_out + ((size_t)t * Hkv + h) * kHeadDim)[l16] = out;
             if (at.row < 0) continue;
             const size_t row = (size_t)at.row + ((size_t)h << A.c.log_page);
-            reinterpret_cast<uint4*>((isk ? A.c.k : A.c.v) + row * kHeadDim)[l16] = out;
+            if constexpr (E8) {
+                reinterpret_cast<uint2*>(reinterpret_cast<uint8_t*>(isk ? A.c.k : A.c.v) + row * kHeadDim)[l16] = bytes;
+                if (l16 == 0) (isk ? A.c.k_scales : A.c.v_scales)[row] = scale;
+            } else {
+                reinterpret_cast<uint4*>((isk ? A.c.k : A.c.v) + row * kHeadDim)[l16] = out;
+            }
             if (isk && A.c.weights && l16 == 0) A.c.weights[row] = 0.f;
         }
     }
@@ -197,8 +232,10 @@ __global__ void __launch_bounds__(32 * kRotWarps, 8) rotate_kernel(const __grid_
 template <class T, int NR, int NT>
 cudaError_t launch_rows(const RotateArgs& a, cudaStream_t st) {
     const dim3 grid((unsigned)((a.io.num_tokens + NT - 1) / NT), (unsigned)((a.heads + kRotRows * NR - 1) / (kRotRows * NR)));
-    if (a.io.interleaved) return launch_prio(rotate_kernel<T, NR, NT, true>, grid, dim3(32 * kRotWarps), 0, st, 0, true, a);
-    return launch_prio(rotate_kernel<T, NR, NT, false>, grid, dim3(32 * kRotWarps), 0, st, 0, true, a);
+    auto launch = [&](auto kernel) { return launch_prio(kernel, grid, dim3(32 * kRotWarps), 0, st, 0, true, a); };
+    if (a.c.k_scales)
+        return a.io.interleaved ? launch(rotate_kernel<T, NR, NT, true, true>) : launch(rotate_kernel<T, NR, NT, false, true>);
+    return a.io.interleaved ? launch(rotate_kernel<T, NR, NT, true, false>) : launch(rotate_kernel<T, NR, NT, false, false>);
 }
 
 template <class T>

@@ -31,7 +31,8 @@ EXPORTED = ("kvec_create", "kvec_destroy", "kvec_state_bytes", "kvec_reset", "kv
             "kvec_select_layer_lse", "kvec_select_layers_lse", "kvec_decode_attention",
             "kvec_noalloc_sync_status", "kvec_set_test_fault", "kvec_output_capacity",
             "kvec_rotate_append", "kvec_paged_decode_bytes", "kvec_paged_decode_window_bytes", "kvec_paged_decode",
-            "kvec_paged_evict", "kvec_prefill_bytes", "kvec_prefill_attention")
+            "kvec_paged_evict", "kvec_prefill_bytes", "kvec_prefill_attention", "kvec_rotate_append_quant",
+            "kvec_paged_decode_quant", "kvec_paged_evict_quant", "kvec_paged_read")
 
 KVEC_BF16 = 0
 KVEC_FP16 = 1
@@ -74,6 +75,10 @@ class kvec_paged_cache(ctypes.Structure):
         ("k_pages", ctypes.c_void_p), ("v_pages", ctypes.c_void_p), ("weights", ctypes.c_void_p),
         ("page_table", ctypes.c_void_p), ("lens", ctypes.c_void_p),
     ]
+
+
+class kvec_paged_scales(ctypes.Structure):
+    _fields_ = [("k_scales", ctypes.c_void_p), ("v_scales", ctypes.c_void_p)]
 
 
 class kvec_rotate_args(ctypes.Structure):
@@ -136,6 +141,14 @@ def load() -> ctypes.CDLL:
             "kvec_prefill_attention": ([_vp, i, i, _vp, _vp, _vp, _vp, _vp, _vp, _vp, i, i, _vp, _vp, _vp,
                                         ctypes.c_size_t, _vp], st),
             "kvec_paged_evict": ([_vp, i, ctypes.POINTER(kvec_paged_cache), _vp, i, i, i, i, i, _vp, _vp, _vp], st),
+            "kvec_rotate_append_quant": ([_vp, ctypes.POINTER(kvec_rotate_args), i, _vp, ctypes.POINTER(kvec_paged_cache),
+                                          ctypes.POINTER(kvec_paged_scales), _vp], st),
+            "kvec_paged_decode_quant": ([_vp, i, _vp, ctypes.POINTER(kvec_paged_cache), ctypes.POINTER(kvec_paged_scales),
+                                         i, i, i, _vp, _vp, ctypes.c_size_t, _vp], st),
+            "kvec_paged_evict_quant": ([_vp, i, ctypes.POINTER(kvec_paged_cache), ctypes.POINTER(kvec_paged_scales), _vp,
+                                        i, i, i, i, i, _vp, _vp, _vp], st),
+            "kvec_paged_read": ([_vp, i, ctypes.POINTER(kvec_paged_cache), ctypes.POINTER(kvec_paged_scales), _vp, _vp, i,
+                                 _vp, _vp, _vp], st),
         }
         for name, (args, res) in sig.items():
             fn = getattr(lib, name)
@@ -262,6 +275,30 @@ def kvec_paged_evict(handle: int, batch: int, cache: kvec_paged_cache, new_table
                                    new_lens, kept, stream))
 
 
+def kvec_rotate_append_quant(handle: int, args: kvec_rotate_args, batch: int, cu_tokens: Optional[int],
+                             cache: kvec_paged_cache, scales: kvec_paged_scales, stream: int = 0) -> None:
+    _check(load().kvec_rotate_append_quant(handle, args, batch, cu_tokens, cache, scales, stream))
+
+
+def kvec_paged_decode_quant(handle: int, batch: int, q: int, cache: kvec_paged_cache, scales: kvec_paged_scales,
+                            max_len: int, window: int, sinks: int, out: int, scratch: int, scratch_bytes: int,
+                            stream: int = 0) -> None:
+    _check(load().kvec_paged_decode_quant(handle, batch, q, cache, scales, max_len, window, sinks, out, scratch,
+                                          scratch_bytes, stream))
+
+
+def kvec_paged_evict_quant(handle: int, batch: int, cache: kvec_paged_cache, scales: kvec_paged_scales, new_table: int,
+                           new_max_pages: int, max_len: int, budget: int, sinks: int, recent: int, new_lens: int,
+                           kept: int, stream: int = 0) -> None:
+    _check(load().kvec_paged_evict_quant(handle, batch, cache, scales, new_table, new_max_pages, max_len, budget, sinks,
+                                         recent, new_lens, kept, stream))
+
+
+def kvec_paged_read(handle: int, batch: int, cache: kvec_paged_cache, scales: Optional[kvec_paged_scales],
+                    first: Optional[int], cu_rows: int, num_rows: int, k_out: int, v_out: int, stream: int = 0) -> None:
+    _check(load().kvec_paged_read(handle, batch, cache, scales, first, cu_rows, num_rows, k_out, v_out, stream))
+
+
 def kvec_prefill_attention(handle: int, dtype: int, batch: int, cu_q_host: int, cu_q_dev: int, cu_k_host: int,
                            cu_k_dev: int, q: int, k: int, v: int, window: int, sinks: int, out: int,
                            lse: Optional[int] = None, scratch: Optional[int] = None, scratch_bytes: int = 0,
@@ -344,30 +381,44 @@ class PagedCache:
 
     k_pages, v_pages bf16 or fp16 [num_pages][H_kv][page_size][d]; page_table int32 [batch][max_pages];
     lens int32 [batch]; weights fp32 [num_pages][H_kv][page_size] or None.  All contiguous, on one device.  Their
-    contents may change between calls; other tensors need another PagedCache."""
+    contents may change between calls; other tensors need another PagedCache.
 
-    def __init__(self, k_pages, v_pages, page_table, lens, weights=None):
+    A cache of 8 bits has float8_e4m3fn pages, k_scales and v_scales fp32 [num_pages][H_kv][page_size] and dtype, the
+    type of the queries that go with it and of rows that are read back; the same methods take it."""
+
+    def __init__(self, k_pages, v_pages, page_table, lens, weights=None, k_scales=None, v_scales=None, dtype=None):
         import torch as t
-        self.dtype_code = _dtype_code(t, k_pages.dtype)
+        self.eight = k_pages.dtype is t.float8_e4m3fn
+        if self.eight:
+            _want(dtype is not None and k_scales is not None and v_scales is not None,
+                  "a cache of 8 bits needs k_scales, v_scales and dtype")
+        else:
+            _want(k_scales is None and v_scales is None, "k_scales and v_scales go with float8_e4m3fn pages")
+            _want(dtype is None or dtype is k_pages.dtype, "dtype is the pages' where these are of 16 bits")
+            dtype = k_pages.dtype
+        self.dtype_code = _dtype_code(t, dtype)
         _want(k_pages.dim() == 4 and v_pages.shape == k_pages.shape and v_pages.dtype == k_pages.dtype,
               "k_pages and v_pages must be [num_pages][H_kv][page_size][d], of one type")
         _want(page_table.dim() == 2 and page_table.dtype == t.int32 and page_table.shape[1] >= 1,
               "page_table must be int32 [batch][max_pages]")
         _want(lens.dtype == t.int32 and tuple(lens.shape) == (page_table.shape[0],), "lens must be int32 [batch]")
-        _want(weights is None or (weights.dtype == t.float32 and weights.shape == k_pages.shape[:3]),
-              "weights must be fp32 [num_pages][H_kv][page_size]")
-        parts = [x for x in (k_pages, v_pages, page_table, lens, weights) if x is not None]
+        for name, x in (("weights", weights), ("k_scales", k_scales), ("v_scales", v_scales)):
+            _want(x is None or (x.dtype == t.float32 and x.shape == k_pages.shape[:3]),
+                  f"{name} must be fp32 [num_pages][H_kv][page_size]")
+        parts = [x for x in (k_pages, v_pages, page_table, lens, weights, k_scales, v_scales) if x is not None]
         _want(all(x.is_contiguous() for x in parts), "a cache's tensors must be contiguous")
         _want(all(x.device == k_pages.device for x in parts), "a cache's tensors must be on one device")
         self.k_pages, self.v_pages, self.page_table, self.lens, self.weights = k_pages, v_pages, page_table, lens, weights
+        self.k_scales, self.v_scales = k_scales, v_scales
         self.batch, self.max_pages = page_table.shape
         self.page_size = k_pages.shape[2]
         self.capacity = self.max_pages * self.page_size
-        self.dtype, self.device = k_pages.dtype, k_pages.device
+        self.dtype, self.device = dtype, k_pages.device
         self.kv_heads, self.head_dim = k_pages.shape[1], k_pages.shape[3]
         self.c = kvec_paged_cache(self.dtype_code, self.page_size, k_pages.shape[0], self.max_pages,
                                   k_pages.data_ptr(), v_pages.data_ptr(),
                                   None if weights is None else weights.data_ptr(), page_table.data_ptr(), lens.data_ptr())
+        self.scales = kvec_paged_scales(k_scales.data_ptr(), v_scales.data_ptr()) if self.eight else None
 
 
 class KvecSelector:
@@ -484,7 +535,8 @@ class KvecSelector:
         if stream.cuda_stream == self._current(self.device.index):
             return
         if cache is not None:
-            tensors += (cache.k_pages, cache.v_pages, cache.page_table, cache.lens, cache.weights)
+            tensors += (cache.k_pages, cache.v_pages, cache.page_table, cache.lens, cache.weights, cache.k_scales,
+                        cache.v_scales)
         for x in tensors:
             if x is not None:
                 x.record_stream(stream)
@@ -514,7 +566,8 @@ class KvecSelector:
 
     def rotate_append(self, q, k, v, positions, rot_table=None, cache=None, cu_tokens=None, q_norm=None, k_norm=None,
                       eps: float = 1e-6, interleaved: bool = False, q_out=None, k_out=None, stream=None):
-        """Norms of new tokens' queries and keys, rotation, and the store into the cache (kvec_rotate_append).
+        """Norms of new tokens' queries and keys, rotation, and the store into the cache (kvec_rotate_append, or
+        kvec_rotate_append_quant for one of 8 bits).
 
         q [T][H_q][d], k, v [T][H_kv][d], tokens any multiple of 8 elements apart; positions int32 [T];
         rot_table fp32 [max_positions][rot_dim]; cu_tokens int32 [batch + 1] on the device (None: a token a sequence).
@@ -558,8 +611,12 @@ class KvecSelector:
                                  None if k_norm is None else k_norm.data_ptr(), eps, rot, 1 if interleaved else 0, most,
                                  None if rot_table is None else rot_table.data_ptr(), positions.data_ptr(),
                                  q_out.data_ptr(), None if k_out is None else k_out.data_ptr())
-            st = self._lib.kvec_rotate_append(self.handle, a, batch, None if cu_tokens is None else cu_tokens.data_ptr(),
-                                              None if cache is None else cache.c, self._raw(stream))
+            cu = None if cu_tokens is None else cu_tokens.data_ptr()
+            if cache is not None and cache.eight:
+                st = self._lib.kvec_rotate_append_quant(self.handle, a, batch, cu, cache.c, cache.scales, self._raw(stream))
+            else:
+                st = self._lib.kvec_rotate_append(self.handle, a, batch, cu, None if cache is None else cache.c,
+                                                  self._raw(stream))
             if st:
                 _check(st)
             if stream is not None:
@@ -568,7 +625,8 @@ class KvecSelector:
 
     def paged_decode(self, q, cache, max_len: Optional[int] = None, window: int = 0, sinks: int = 0, out=None,
                      stream=None):
-        """One new token per sequence over a paged cache (kvec_paged_decode); adds to cache.weights where it has them.
+        """One new token per sequence over a paged cache (kvec_paged_decode, or kvec_paged_decode_quant over one of 8 bits);
+        adds to cache.weights where it has them.
 
         q [batch][H_q][d] of the cache's type, contiguous; max_len: a bound on the lengths (the capacity).  Scratch
         (kvec_paged_decode_window_bytes) and, with weights, part of the time go by max_len or the window: give the least
@@ -593,8 +651,12 @@ class KvecSelector:
                 self._decode_bytes.clear()
             need = self._decode_bytes[sizes] = kvec_paged_decode_window_bytes(self.handle, *sizes)
         scratch = self._empty(max(need, 16), self._torch.uint8, stream)
-        st = self._lib.kvec_paged_decode(self.handle, batch, q.data_ptr(), cache.c, max_len, window, sinks, out.data_ptr(),
-                                         scratch.data_ptr(), need, self._raw(stream))
+        if cache.eight:
+            st = self._lib.kvec_paged_decode_quant(self.handle, batch, q.data_ptr(), cache.c, cache.scales, max_len, window,
+                                                   sinks, out.data_ptr(), scratch.data_ptr(), need, self._raw(stream))
+        else:
+            st = self._lib.kvec_paged_decode(self.handle, batch, q.data_ptr(), cache.c, max_len, window, sinks,
+                                             out.data_ptr(), scratch.data_ptr(), need, self._raw(stream))
         if st:
             _check(st)
         if stream is not None:
@@ -603,7 +665,7 @@ class KvecSelector:
 
     def paged_evict(self, cache, new_table, budget: int, sinks: int = 0, recent: int = 0, max_len: Optional[int] = None,
                     new_lens=None, kept=None, stream=None):
-        """Eviction by accumulated weight to the pages of new_table (kvec_paged_evict).
+        """Eviction by accumulated weight to the pages of new_table (kvec_paged_evict, or kvec_paged_evict_quant).
 
         cache.weights hold what paged_decode added since rotate_append set a slot's to 0; a prompt's slots count with
         its own attention only where the caller has written it there.
@@ -627,14 +689,45 @@ class KvecSelector:
             kept = self._empty((batch, Hkv, budget), t.int32, stream)
         else:
             self._check("kept", kept, (batch, Hkv, budget), t.int32)
-        st = self._lib.kvec_paged_evict(self.handle, batch, cache.c, new_table.data_ptr(), new_table.shape[1],
-                                        max_len, budget, sinks, recent,
-                                        new_lens.data_ptr(), kept.data_ptr(), self._raw(stream))
+        tail = (new_table.data_ptr(), new_table.shape[1], max_len, budget, sinks, recent, new_lens.data_ptr(),
+                kept.data_ptr(), self._raw(stream))
+        if cache.eight:
+            st = self._lib.kvec_paged_evict_quant(self.handle, batch, cache.c, cache.scales, *tail)
+        else:
+            st = self._lib.kvec_paged_evict(self.handle, batch, cache.c, *tail)
         if st:
             _check(st)
         if stream is not None:
             self._used(stream, cache, new_table, new_lens, kept)
         return new_lens, kept
+
+    def paged_read(self, cache, cu_rows, num_rows: int, first=None, k_out=None, v_out=None, stream=None):
+        """A paged cache's slots as packed rows of its dtype, as prefill_attention takes keys and values (kvec_paged_read).
+
+        cu_rows int32 [batch + 1] on the device, num_rows its last entry, which the host knows; first int32 [batch] (None:
+        0): the slots that the sequences' rows begin with.  Returns (k, v) [num_rows][H_kv][d]."""
+        t, p = self._torch, self.params
+        batch, shape = cache.batch, (num_rows, p.num_kv_heads, p.head_dim)
+        self._check_cache(cache)
+        _want(0 <= num_rows < 1 << 31, "num_rows must be in [0, 2^31)")
+        self._check("cu_rows", cu_rows, (batch + 1,), t.int32)
+        if first is not None:
+            self._check("first", first, (batch,), t.int32)
+        if k_out is None:
+            k_out = self._empty(shape, cache.dtype, stream)
+        else:
+            self._check("k_out", k_out, shape, cache.dtype)
+        if v_out is None:
+            v_out = self._empty(shape, cache.dtype, stream)
+        else:
+            self._check("v_out", v_out, shape, cache.dtype)
+        st = self._lib.kvec_paged_read(self.handle, batch, cache.c, cache.scales, None if first is None else first.data_ptr(),
+                                       cu_rows.data_ptr(), num_rows, k_out.data_ptr(), v_out.data_ptr(), self._raw(stream))
+        if st:
+            _check(st)
+        if stream is not None:
+            self._used(stream, cache, cu_rows, first, k_out, v_out)
+        return k_out, v_out
 
     def prefill_attention(self, q, k, v, cu_q_host, cu_q_dev, cu_k_host=None, cu_k_dev=None, window: int = 0,
                           sinks: int = 0, out=None, lse=None, stream=None):
