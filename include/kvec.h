@@ -388,6 +388,40 @@ KVEC_API kvec_status kvec_paged_evict(kvec_handle* h, int batch, const kvec_page
                                       int sinks, int recent, int32_t* new_lens, int32_t* kept,
                                       kvec_stream_t stream);
 
+/* A prefix that groups of consecutive sequences share: sequences cu_seqs[r] <= s <
+ * cu_seqs[r + 1] see the lens[r] slots of row r of page_table before their own.  The pages
+ * are of the same pool as the sequences' own and are only read; a table entry outside
+ * [0, num_pages) is no page, as there. */
+typedef struct {
+    int num_groups;              /* 1 to 65535; a group may be empty and a prefix too */
+    int max_pages;               /* entries of a page_table row, max_pages * page_size <= 2^20 */
+    const int32_t* page_table;   /* device [num_groups][max_pages] */
+    const int32_t* lens;         /* device [num_groups]: clamped to [0, max_prefix] */
+    const int32_t* cu_seqs;      /* device [num_groups + 1], ascending from 0 to at most batch;
+                                    sequences from the last on have no prefix */
+} kvec_shared_prefix;
+
+/* Attention of one new token per sequence where groups of sequences share a prefix: as
+ * kvec_paged_decode over the group's prefix followed by the sequence's own slots (cache's
+ * page_table and lens, which count the new token),
+ *   out[s][hq] = sum_j p_j v_j,  p_j = softmax over prefix and own slots of scale * <q[s][hq], k_j>,
+ * but a prefix's keys and values are read for all queries of its group at once.  Keys are
+ * rotated by their positions before they are stored, so own slots continue after the prefix.
+ * With cache.weights the own slots' weights grow by their p_j, as there; a prefix's do not
+ * (its sequences would not agree on what to evict).  The rows of 16 bits only; no window.
+ * The weights of a prefix's slots are rounded to dtype before they meet the values, as in
+ * kvec_prefill_attention, those of own slots as in kvec_paged_decode.
+ *   q, out     device cache.dtype [batch][H_q][d], 16-byte aligned.
+ *   max_len    host bound on the own lengths, max_prefix one on the prefixes'.
+ *   scratch    device, kvec_shared_decode_bytes bytes, 256-byte aligned: written and read
+ *              within the call; calls that may overlap need one each.
+ * A bounded wait that gave up is reported by kvec_sync_status.  1 <= batch <= max_batch,
+ * H_q/H_kv <= 8. */
+KVEC_API size_t kvec_shared_decode_bytes(kvec_handle* h, int batch, int max_len, int with_weights);
+KVEC_API kvec_status kvec_shared_decode(kvec_handle* h, int batch, const void* q, const kvec_paged_cache* cache,
+                                        const kvec_shared_prefix* prefix, int max_len, int max_prefix, void* out,
+                                        void* scratch, size_t scratch_bytes, kvec_stream_t stream);
+
 /* ------------------------------------------------------------------ a cache of 8 bits
  *
  * Keys and values as e4m3 numbers (4 exponent and 3 mantissa bits, up to 448) with an fp32
@@ -510,7 +544,7 @@ KVEC_API kvec_status kvec_kernel_time(kvec_handle* h, int kernel, double* total_
  * and that call's outputs are invalid.  fault = 2 makes one epilogue warp of
  * every score CTA report that its wait for work gave up, at once, and one of every
  * general window kernel's CTA that its wait for a buffer did (at its third unit); the
- * rest is the same.  fault = 4 makes kvec_prefill_attention signal none of its logits and
+ * rest is the same.  fault = 4 makes kvec_prefill_attention (and kvec_shared_decode) signal none of its logits and
  * kvec_paged_decode leave out one warp's copies: their waits give up after about 0.2 s.  fault = 3 makes kvec_create treat every allocation but the one
  * of the shortest rings as failed.  fault = 0 (the default) switches it off.  Process-wide; while it is set,
  * multi-layer calls are neither captured into nor replayed from the handle's

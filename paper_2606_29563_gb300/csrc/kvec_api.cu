@@ -1488,6 +1488,96 @@ kvec_status kvec_paged_read(kvec_handle* h, int batch, const kvec_paged_cache* c
 
 namespace {
 
+// Parts of a shared decode's scratch, each from a multiple of 256 bytes on.
+struct SharedScratch {
+    size_t out, ml, prefix, total;   // behind paged_decode's
+    SharedScratch(const kvec_handle* h, int batch, int max_len, bool weights) {
+        const size_t rows = (size_t)batch * h->p.num_q_heads;
+        out = round_up(paged_decode_scratch(batch, h->p.num_q_heads, max_len, 0, 0, weights, h->num_sms), 256);
+        ml = out + rows * h->p.head_dim * sizeof(float);
+        prefix = round_up(ml + rows * sizeof(float2), 256);
+        total = prefix + prefix_scratch(batch, h->p.num_q_heads, h->num_sms);
+    }
+};
+
+}  // namespace
+
+size_t kvec_shared_decode_bytes(kvec_handle* h, int batch, int max_len, int with_weights) {
+    if (!h || batch < 1 || batch > h->p.max_batch || max_len < 1 || max_len > kPagedMaxLen) return 0;
+    return SharedScratch(h, batch, max_len, with_weights != 0).total;
+}
+
+kvec_status kvec_shared_decode(kvec_handle* h, int batch, const void* q, const kvec_paged_cache* cache,
+                               const kvec_shared_prefix* prefix, int max_len, int max_prefix, void* out, void* scratch,
+                               size_t scratch_bytes, kvec_stream_t stream) {
+    PagedCacheView v{};
+    kvec_status s = view_cache(cache, &v);
+    if (s != KVEC_OK) return s;
+    if (!prefix) return fail(KVEC_ERR_INVALID_ARG, "prefix is NULL");
+    if (max_len < 1 || max_len > v.capacity)
+        return fail(KVEC_ERR_INVALID_ARG, "max_len %d outside [1, max_pages * page_size = %d]", max_len, v.capacity);
+    if (prefix->num_groups < 1 || prefix->num_groups > kMaxGridBatch)
+        return fail(KVEC_ERR_INVALID_ARG, "num_groups %d outside [1, %d]", prefix->num_groups, kMaxGridBatch);
+    if (prefix->max_pages < 1 || ((long long)prefix->max_pages << v.log_page) > kPagedMaxLen)
+        return fail(KVEC_ERR_INVALID_ARG, "need 1 <= max_pages * page_size <= %d of a prefix", kPagedMaxLen);
+    if (max_prefix < 1 || max_prefix > prefix->max_pages << v.log_page)
+        return fail(KVEC_ERR_INVALID_ARG, "max_prefix %d outside [1, max_pages * page_size = %d]", max_prefix,
+                    prefix->max_pages << v.log_page);
+    if (!prefix->page_table || !prefix->lens || !prefix->cu_seqs) return fail(KVEC_ERR_INVALID_ARG, "a device pointer of the prefix is NULL");
+    for (const int32_t* p : {prefix->page_table, prefix->lens, prefix->cu_seqs})
+        if (reinterpret_cast<uintptr_t>(p) % 4) return fail(KVEC_ERR_INVALID_ARG, "the prefix's page_table, lens and cu_seqs must be 4-byte aligned");
+    s = check_paged_handle(h, batch, &v);
+    if (s != KVEC_OK) return s;
+    if (h->g > 8)
+        return fail(KVEC_ERR_UNSUPPORTED, "decode attention supports up to 8 query heads per KV head (g = %d)", h->g);
+    if (!q || !out || !scratch) return fail(KVEC_ERR_INVALID_ARG, "a device pointer is NULL");
+    if (!aligned16(q) || !aligned16(out) || reinterpret_cast<uintptr_t>(scratch) % 256)
+        return fail(KVEC_ERR_INVALID_ARG, "q and out must be 16-byte and scratch 256-byte aligned");
+    const SharedScratch part(h, batch, max_len, v.weights != nullptr);
+    if (scratch_bytes < part.total)
+        return fail(KVEC_ERR_INVALID_ARG, "scratch of %zu bytes, %zu are needed", scratch_bytes, part.total);
+    char* const base = static_cast<char*>(scratch);
+    PrefixIO px{};
+    px.q = static_cast<const uint16_t*>(q);
+    px.c = v;
+    px.table = prefix->page_table;
+    px.lens = prefix->lens;
+    px.cu = prefix->cu_seqs;
+    px.groups = prefix->num_groups;
+    px.max_pages = prefix->max_pages;
+    px.max_prefix = max_prefix;
+    px.batch = batch;
+    px.Hq = h->p.num_q_heads;
+    px.Hkv = h->p.num_kv_heads;
+    px.scale = softmax_scale_of(h->p);
+    px.err = h->sc.err;
+    px.scratch = base + part.prefix;
+    px.out = reinterpret_cast<float*>(base + part.out);
+    px.ml = reinterpret_cast<float2*>(base + part.ml);
+    PagedDecodeIO io{};
+    io.q = px.q;
+    io.out = static_cast<uint16_t*>(out);
+    io.scratch = scratch;
+    io.err = px.err;
+    io.batch = batch;
+    io.Hq = px.Hq;
+    io.Hkv = px.Hkv;
+    io.max_len = max_len;
+    io.scale = px.scale;
+    io.pre_o = px.out;
+    io.pre_ml = px.ml;
+    int prev = 0;
+    s = set_device(h, &prev);
+    if (s != KVEC_OK) return s;
+    DeviceGuard guard{prev, h->device};
+    cudaError_t e = launch_prefix(px, h->num_sms, reinterpret_cast<cudaStream_t>(stream));
+    if (e == cudaSuccess) e = launch_paged_decode(io, v, h->num_sms, reinterpret_cast<cudaStream_t>(stream));
+    if (e != cudaSuccess) return cuda_fail(e, "shared decode launch");
+    return KVEC_OK;
+}
+
+namespace {
+
 // The checks of a prefill call that need no handle, and its longest sequences.
 kvec_status check_prefill(int batch, const int32_t* cu_q, const int32_t* cu_k, int window, int sinks, int* max_q, int* max_k) {
     kvec_status s = check_window(window, sinks);

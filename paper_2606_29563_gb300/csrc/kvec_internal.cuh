@@ -157,6 +157,8 @@ struct PagedDecodeIO {
     int max_len;              // bound on the lengths, within the cache's capacity
     int window, sinks;
     float scale;
+    const float* pre_o;       // [batch][Hq][d] sums of what is seen before the sequence's own slots (launch_prefix),
+    const float2* pre_ml;     // [batch][Hq] their maxima and sums of weights; null: nothing
 };
 
 // Eviction by accumulated weight (evict_kernel.cu).
@@ -181,6 +183,25 @@ struct PrefillIO {
     void* scratch;            // PrefillPlan::scratch bytes
     int window, sinks;
     float scale;
+};
+
+// What groups of sequences share: attention of all their queries over a prefix in pages, as sums that the attention
+// over the sequences' own slots takes in (prefill_kernel.cu, paged_decode_kernel.cu).
+struct PrefixIO {
+    const uint16_t* q;        // [batch][Hq][d]
+    PagedCacheView c;         // the pool; its table and lengths are the sequences' own
+    const int* table;         // [groups][max_pages]
+    const int* lens;          // [groups]
+    const int* cu;            // [groups + 1]: the groups' sequences
+    int groups, max_pages;
+    int max_prefix;           // bound on the lengths, within a row of the table
+    int batch, Hq, Hkv;
+    float scale;
+    int* err;
+    void* scratch;            // prefix_scratch bytes
+    float* out;               // [batch][Hq][d] sums, relative to
+    float2* ml;               // [batch][Hq] (maximum, sum)
+    int rows;                 // of the pages
 };
 
 // How a prefill call is divided (from the host's lengths).
@@ -322,6 +343,9 @@ size_t paged_decode_scratch(int batch, int Hq, int max_len, int window, int sink
 cudaError_t launch_read(const ReadIO& io, const PagedCacheView& c, cudaStream_t st);
 cudaError_t launch_evict(const EvictIO& io, const PagedCacheView& c, cudaStream_t st);
 PrefillPlan plan_prefill(int batch, int Hq, int Hkv, int max_q, int max_k, int window, int sinks, int num_sms);
+size_t prefix_scratch(int batch, int Hq, int num_sms);
+// A programmatic dependent may read before its wait what was complete before the call.
+cudaError_t launch_prefix(const PrefixIO& px, int num_sms, cudaStream_t st);
 cudaError_t launch_prefill(const PrefillIO& io, const PrefillPlan& plan, int num_sms, cudaStream_t st);
 // out_idx from the slot's kept-position bits, then the K/V rows.
 cudaError_t launch_gather(const Geometry& g, const Group& gr, cudaStream_t st, int priority, bool programmatic);

@@ -210,6 +210,17 @@ struct List {
     }
 };
 
+// What comes before a sequence's own slots, for query row `at`: its maximum and sum of weights joined to (M, L).
+// Returns the factors of the sums so far and of those before.
+__device__ __forceinline__ float2 join_before(const PdArgs& A, size_t at, float& M, float& L) {
+    const float2 b = __ldcg(A.io.pre_ml + at);
+    const float m = fmaxf(M, b.x);
+    const float2 f = make_float2(ptx::ex2(M - m), ptx::ex2(b.x - m));
+    L = fmaf(f.y, b.y, L * f.x);
+    M = m;
+    return f;
+}
+
 // a / b, in 32 bits where they do.
 __device__ __forceinline__ long long quotient(long long a, long long b) {
     return ((a | b) >> 32) == 0 ? (long long)((uint32_t)a / (uint32_t)b) : a / b;
@@ -299,7 +310,9 @@ __device__ void add_weights(const PdArgs& A, int s, int h, const Visible& v, int
 // E8: rows of e4m3 numbers with a scale each.  They become fp16, which holds them all, on their way from shared memory
 // to the tiles: the scale of a key multiplies its logit, that of a value its weight.  For that the
 // queries (in bf16) and the values' scales are brought to fp16's range by powers of two, a row's and the warp's so far.
-template <class T, bool CL, bool E8>
+// PRE: sums of what comes before the sequence's own slots are merged at the end (launch_prefix); the kernels that leave
+// them may still run until then.
+template <class T, bool CL, bool E8, bool PRE>
 __global__ void __launch_bounds__(kPdThreads, kPdCtasPerSm) paged_decode_kernel(const __grid_constant__ PdArgs A) {
     constexpr int kStage = kPdStage<E8>, kStages = kPdStages<E8>;
     using Operand = std::conditional_t<E8, __half, T>;          // the tiles' type
@@ -324,8 +337,8 @@ __global__ void __launch_bounds__(kPdThreads, kPdCtasPerSm) paged_decode_kernel(
     }
     __syncthreads();
     // The trigger follows the wait: what was complete before this grid may be read by the
-    // join kernel before its own wait.
-    asm volatile("griddepcontrol.wait;\n" ::: "memory");
+    // join kernel before its own wait.  (With PRE it was before the call's first kernel let others start.)
+    if constexpr (!PRE) asm volatile("griddepcontrol.wait;\n" ::: "memory");
     asm volatile("griddepcontrol.launch_dependents;\n" ::: "memory");
 
     // This CTA's blocks: `count` from (s, h, i) on.
@@ -652,6 +665,7 @@ __global__ void __launch_bounds__(kPdThreads, kPdCtasPerSm) paged_decode_kernel(
             }
         }
         __syncthreads();
+        if constexpr (PRE) asm volatile("griddepcontrol.wait;\n" ::: "memory");
         for (int e = tid; e < g * kHeadDim; e += kPdThreads) {
             const int j = e / kHeadDim, c = e % kHeadDim;
             float M = kNoLogit;
@@ -671,6 +685,11 @@ __global__ void __launch_bounds__(kPdThreads, kPdCtasPerSm) paged_decode_kernel(
                     cl[j] = L;
                 }
             } else if (CL || whole) {
+                if constexpr (PRE) {
+                    const size_t at = (size_t)s * Hq + (size_t)h * g + j;
+                    const float2 f = join_before(A, at, M, L);
+                    O = fmaf(f.y, __ldcg(A.io.pre_o + at * kHeadDim + c), O * f.x);
+                }
                 const float o = L > 0.f || L != L ? O / L : 0.f;
                 reinterpret_cast<T*>(A.io.out)[((size_t)s * Hq + (size_t)h * g + j) * kHeadDim + c] = T(o);
                 if (c == 0) {
@@ -704,6 +723,7 @@ __global__ void __launch_bounds__(kPdThreads, kPdCtasPerSm) paged_decode_kernel(
 #pragma unroll
                     for (int r = 0; r < kPdMaxCluster; ++r)
                         if (r < splits) L = fmaf(ptx::ex2(mc[r] - M), *cluster.map_shared_rank(&cl[tid], r), L);
+                    if constexpr (PRE) join_before(A, (size_t)s * Hq + (size_t)h * g + tid, M, L);
                     fm[tid] = M;
                     finv[tid] = L > 0.f || L != L ? 1.f / L : 0.f;
                 }
@@ -711,6 +731,10 @@ __global__ void __launch_bounds__(kPdThreads, kPdCtasPerSm) paged_decode_kernel(
                 for (int e = tid; rank + (e / kHeadDim) * splits < g; e += kPdThreads) {
                     const int j = rank + (e / kHeadDim) * splits, c = e % kHeadDim;
                     float O = 0.f;
+                    if constexpr (PRE) {
+                        const size_t at = (size_t)s * Hq + (size_t)h * g + j;
+                        O = ptx::ex2(__ldcg(A.io.pre_ml + at).x - fm[j]) * __ldcg(A.io.pre_o + at * kHeadDim + c);
+                    }
 #pragma unroll
                     for (int r = 0; r < kPdMaxCluster; ++r) {
                         if (r >= splits) break;
@@ -734,6 +758,8 @@ __global__ void __launch_bounds__(kPdThreads, kPdCtasPerSm) paged_decode_kernel(
         cur.advance(A, len);
         first_segment = false;
     }
+    // (A CTA without a block has not waited.)
+    if constexpr (PRE) asm volatile("griddepcontrol.wait;\n" ::: "memory");
     // Copies in flight land before the CTA may exit (a stage without one runs into the limit).
     if (failed)
         for (int i = 0; i < kStages; ++i) ptx::mbar_wait(&full[warp][i], (phases >> i) & 1u, 20000000ull);
@@ -743,7 +769,7 @@ __global__ void __launch_bounds__(kPdThreads, kPdCtasPerSm) paged_decode_kernel(
 // others add the weights, kJoinRows slots each.  (A lane finds a share's place and sums, and eight shares' outputs are
 // read at once: one thread in a loop over the 38 shares of 131072 slots took 58 us.  Six blocks resident on an
 // SM: eight spill, 64 rows take the same but a window of 4096 in 16 caches 55.5 us instead of 53.6.)
-template <class T>
+template <class T, bool PRE>
 __global__ void __launch_bounds__(kJoinThreads, 6) paged_join_kernel(const __grid_constant__ PdArgs A) {
     extern __shared__ float2 share[];                 // [shares][kPdHeads] (place as an int, maximum)
     __shared__ float fm[kPdHeads], finv[kPdHeads];
@@ -769,8 +795,17 @@ __global__ void __launch_bounds__(kJoinThreads, 6) paged_join_kernel(const __gri
     asm volatile("griddepcontrol.launch_dependents;\n" ::: "memory");
     asm volatile("griddepcontrol.wait;\n" ::: "memory");
     T* const out = reinterpret_cast<T*>(A.io.out) + ((size_t)s * A.io.Hq + (size_t)h * g) * kHeadDim + lane * 4;
+    const size_t first = (size_t)s * A.io.Hq + (size_t)h * g;   // query row
     if (v.nb == 0 && !weights)
-        for (int j = warp; j < g; j += kJoinThreads / 32) *reinterpret_cast<uint2*>(out + j * kHeadDim) = make_uint2(0u, 0u);
+        for (int j = warp; j < g; j += kJoinThreads / 32) {
+            uint2 o = make_uint2(0u, 0u);
+            if constexpr (PRE) {
+                const float L = __ldcg(A.io.pre_ml + first + j).y;
+                const float4 b = __ldcg(reinterpret_cast<const float4*>(A.io.pre_o + (first + j) * kHeadDim) + lane);
+                if (L > 0.f || L != L) o = make_uint2(Half16<T>::pack(b.x / L, b.y / L), Half16<T>::pack(b.z / L, b.w / L));
+            }
+            *reinterpret_cast<uint2*>(out + j * kHeadDim) = o;
+        }
     if (done) return;
     for (int j = warp; j < g; j += kJoinThreads / 32) {   // a lane a share
         float M = kNoLogit, L = 0.f;
@@ -796,6 +831,8 @@ __global__ void __launch_bounds__(kJoinThreads, 6) paged_join_kernel(const __gri
         }
         // (The two halves of a pair of lanes sum in different orders: lane 0's is taken.)
         L = __shfl_sync(0xffffffffu, L, 0);
+        float2 f2 = make_float2(1.f, 0.f);
+        if constexpr (PRE) f2 = join_before(A, first + j, M, L);
         const bool some = L > 0.f || L != L;
         if (lane == 0) {
             fm[j] = M;
@@ -804,6 +841,10 @@ __global__ void __launch_bounds__(kJoinThreads, 6) paged_join_kernel(const __gri
         __syncwarp();
         if (!weights) {
             float4 O = make_float4(0.f, 0.f, 0.f, 0.f);
+            if constexpr (PRE) {
+                const float4 b = __ldcg(reinterpret_cast<const float4*>(A.io.pre_o + (first + j) * kHeadDim) + lane);
+                O = make_float4(b.x * f2.y, b.y * f2.y, b.z * f2.y, b.w * f2.y);
+            }
             const float* part = A.part_o + (size_t)j * kHeadDim + lane * 4;
             for (int c = 0; c <= c1 - c0; c += 8) {
                 float4 o[8];
@@ -833,7 +874,7 @@ size_t round16(size_t x) { return (x + 15) & ~size_t(15); }
 
 int share_ctas(int num_sms) { return kPdCtasPerSm * num_sms; }
 
-template <class T, bool E8>
+template <class T, bool E8, bool PRE>
 cudaError_t launch_typed(const PdArgs& a, cudaStream_t st) {
     // CTAs of a pair: the largest cluster that fits the device's resident CTAs in one wave, with
     // two blocks a warp and more; taken where that leaves a CTA 32 blocks and less (a quarter of
@@ -859,12 +900,12 @@ cudaError_t launch_typed(const PdArgs& a, cudaStream_t st) {
         attr[1].val.programmaticStreamSerializationAllowed = 1;
         cfg.attrs = attr;
         cfg.numAttrs = 2;
-        return cudaLaunchKernelEx(&cfg, paged_decode_kernel<T, true, E8>, a);
+        return cudaLaunchKernelEx(&cfg, paged_decode_kernel<T, true, E8, PRE>, a);
     }
-    cudaError_t e = launch_prio(paged_decode_kernel<T, false, E8>, dim3(a.ctas), dim3(kPdThreads), kPdSmem, st, 0, true, a);
+    cudaError_t e = launch_prio(paged_decode_kernel<T, false, E8, PRE>, dim3(a.ctas), dim3(kPdThreads), kPdSmem, st, 0, true, a);
     if (e != cudaSuccess) return e;
     const int rows = a.c.weights ? (a.nbmax * kPdBlock + kJoinRows - 1) / kJoinRows : 0;
-    return launch_prio(paged_join_kernel<T>, dim3(1 + rows, a.io.Hkv, a.io.batch), dim3(kJoinThreads),
+    return launch_prio(paged_join_kernel<T, PRE>, dim3(1 + rows, a.io.Hkv, a.io.batch), dim3(kJoinThreads),
                        a.ctas * kPdHeads * sizeof(float2), st, 0, true, a);
 }
 
@@ -891,14 +932,17 @@ cudaError_t configure_paged_decode() {
     auto one = [&](auto kernel) {
         if (e == cudaSuccess) e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kPdSmem);
     };
-    one(paged_decode_kernel<__nv_bfloat16, true, false>);
-    one(paged_decode_kernel<__nv_bfloat16, false, false>);
-    one(paged_decode_kernel<__half, true, false>);
-    one(paged_decode_kernel<__half, false, false>);
-    one(paged_decode_kernel<__nv_bfloat16, true, true>);
-    one(paged_decode_kernel<__nv_bfloat16, false, true>);
-    one(paged_decode_kernel<__half, true, true>);
-    one(paged_decode_kernel<__half, false, true>);
+    auto both = [&](auto type) {
+        using T = decltype(type);
+        one(paged_decode_kernel<T, true, false, false>);
+        one(paged_decode_kernel<T, false, false, false>);
+        one(paged_decode_kernel<T, true, true, false>);
+        one(paged_decode_kernel<T, false, true, false>);
+        one(paged_decode_kernel<T, true, false, true>);
+        one(paged_decode_kernel<T, false, false, true>);
+    };
+    both(__nv_bfloat16{});
+    both(__half{});
     return e;
 }
 
@@ -928,8 +972,11 @@ cudaError_t launch_paged_decode(const PagedDecodeIO& io, const PagedCacheView& c
     a.part_ml = reinterpret_cast<float2*>(p);
     p += round16(slots * sizeof(float2));
     a.logits = reinterpret_cast<float*>(p);
-    if (e8) return c.dtype == 1 ? launch_typed<__half, true>(a, st) : launch_typed<__nv_bfloat16, true>(a, st);
-    return c.dtype == 1 ? launch_typed<__half, false>(a, st) : launch_typed<__nv_bfloat16, false>(a, st);
+    auto launch = [&](auto type) {
+        using T = decltype(type);
+        return e8 ? launch_typed<T, true, false>(a, st) : io.pre_o ? launch_typed<T, false, true>(a, st) : launch_typed<T, false, false>(a, st);
+    };
+    return c.dtype == 1 ? launch(__half{}) : launch(__nv_bfloat16{});
 }
 
 }  // namespace kvec

@@ -45,6 +45,11 @@
 // halves of blocks left out where no row sees them (425 for 390: the branches stand between the
 // products), products of 16 keys for a block of few first tokens (348 for 331, and in turns of
 // their own no gain: 394 for 391 with the window).
+//
+// The same products without the causal order serve shared_decode (PAGED): the queries of the sequences
+// that share a prefix are the rows, each of which sees all of it, and K and V blocks come from the
+// prefix's pages.  The blocks of all (group, KV head, pair of tiles) form one list, as the lengths
+// are on the device; every CTA takes an even share and leaves sums for prefix_join_kernel.
 #include <algorithm>
 #include <type_traits>
 
@@ -92,6 +97,8 @@ struct PfArgs {
     Divisor by_per, by_heads;   // batch * Hkv, Hkv
     float sl2;
     int fault;       // test of the error path (kvec_set_test_fault): no S is ever complete
+    PrefixIO px;     // PAGED: instead of io's keys and sequences
+    int page_log;    // PAGED: keys of a copy, the smaller of a page and a block (log2)
 };
 
 // What a CTA works on: tiles 2 p and 2 p + 1 of sequence s, KV head h.
@@ -195,6 +202,137 @@ __device__ __forceinline__ int item_of(int turn) {
 // ptx::warp_wait; a phase that is over, the usual case, costs one poll and one vote.
 __device__ __forceinline__ bool pf_wait(uint64_t* bar, uint32_t parity, const volatile int* abort) {
     return __all_sync(0xffffffffu, ptx::mbar_try_wait(bar, parity)) || ptx::warp_wait(bar, parity, abort);
+}
+
+// PAGED.  What group r of sequences shares: its sequences [q0, q0 + n), the keys of its prefix and their blocks.
+struct Group {
+    int q0, n, len, nb, pairs;
+    __device__ __forceinline__ Group(const PfArgs& A, int r) : q0(0), n(0), len(0), nb(0), pairs(0) {
+        if (r >= A.px.groups) return;
+        const int batch = A.io.total_q;
+        q0 = min(max(__ldg(&A.px.cu[r]), 0), batch);
+        n = max(min(max(__ldg(&A.px.cu[r + 1]), 0), batch) - q0, 0);
+        len = min(max(__ldg(&A.px.lens[r]), 0), A.px.max_prefix);
+        nb = (len + kPfTile - 1) / kPfTile;
+        pairs = (n + 2 * A.nq - 1) / (2 * A.nq);
+    }
+    // Places of an item in the list of all blocks: ahead of its blocks stand some for what beginning and ending it takes.
+    static constexpr int kCost = 1;
+    __device__ __forceinline__ int places() const { return nb && pairs ? nb + kCost : 0; }
+    // Row of the sums of the first query of an item's pair, without 2 kPfTile for each CTA before the one that leaves them.
+    __device__ __forceinline__ int first_row(const PfArgs& A, int h, int pair) const {
+        return q0 * A.io.Hq + (h * n + pair * 2 * A.nq) * A.g;
+    }
+};
+
+// The list as a warp sees it: lane l holds the groups l * per .. l * per + per - 1, over all heads and pairs.
+struct GroupList {
+    int per;
+    long long before, mine, total;   // places: of the lanes before, of this lane, of all
+    __device__ __forceinline__ GroupList(const PfArgs& A) : per((A.px.groups + 31) >> 5), before(0), mine(0), total(0) {
+        const int lane = threadIdx.x & 31;
+        for (int k = 0; k < per; ++k) {
+            const Group gr(A, lane * per + k);
+            mine += (long long)gr.places() * gr.pairs * A.io.Hkv;
+        }
+        long long upto = mine;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const long long y = __shfl_up_sync(0xffffffffu, upto, o);
+            if (lane >= o) upto += y;
+        }
+        before = upto - mine;
+        total = __shfl_sync(0xffffffffu, upto, 31);
+    }
+    // The group of place `at` < total, which becomes the place within the group.
+    __device__ __forceinline__ int group_at(const PfArgs& A, long long& at) const {
+        const int l = __ffs(__ballot_sync(0xffffffffu, at < before + mine)) - 1;
+        at -= __shfl_sync(0xffffffffu, before, l);
+        for (int r = l * per;; ++r) {
+            const Group gr(A, r);
+            const long long here = (long long)gr.places() * gr.pairs * A.io.Hkv;
+            if (at < here) return r;
+            at -= here;
+        }
+    }
+    __device__ __forceinline__ long long places_before(const PfArgs& A, int r) const {
+        const int l = r / per;
+        long long b = __shfl_sync(0xffffffffu, before, l);
+        for (int k = l * per; k < r; ++k) {
+            const Group gr(A, k);
+            b += (long long)gr.places() * gr.pairs * A.io.Hkv;
+        }
+        return b;
+    }
+};
+__device__ __forceinline__ long long group_share(long long total, int cta, int ctas) { return total * cta / ctas; }
+
+// The items of this CTA's share, in order.
+struct GroupWalk {
+    const PfArgs& A;
+    Group gr;
+    int r = 0, item = 0, i = 0;   // the next place: the i-th of an item
+    long long left = 0;
+    __device__ __forceinline__ GroupWalk(const PfArgs& args) : A(args), gr(args, args.px.groups) {
+        const GroupList list(A);
+        long long at = group_share(list.total, blockIdx.x, gridDim.x);
+        left = group_share(list.total, blockIdx.x + 1, gridDim.x) - at;
+        if (left == 0) return;
+        r = list.group_at(A, at);
+        gr = Group(A, r);
+        item = (int)(at / gr.places());
+        i = (int)(at - (long long)item * gr.places());
+    }
+    __device__ __forceinline__ bool next(Item& w) {
+        while (left > 0 && r < A.px.groups) {
+            const int take = (int)min((long long)(gr.places() - i), left);
+            const int b0 = max(i - Group::kCost, 0), b1 = max(i + take - Group::kCost, 0);
+            const int pair = item % gr.pairs;
+            w.h = item / gr.pairs;
+            w.q0 = gr.q0;
+            w.k0 = r;                   // whose pages
+            w.a = pair * 2 * A.nq;
+            w.b = min(w.a + 2 * A.nq, gr.n);
+            w.tiles = w.b - w.a > A.nq ? 2 : 1;
+            w.off = gr.len - 1;         // the last key, which every row sees
+            w.nsink = w.lo = 0;
+            w.i0 = b0;
+            w.n = b1 - b0;
+            w.place = gr.first_row(A, w.h, pair) + 2 * kPfTile * (int)blockIdx.x;
+            w.whole_lo = -b0;
+            w.whole_hi = gr.len / kPfTile - b0;
+            left -= take;
+            i += take;
+            if (i == gr.places()) {
+                i = 0;
+                if (++item == gr.pairs * A.io.Hkv) {
+                    item = 0;
+                    do gr = Group(A, ++r);
+                    while (gr.places() == 0 && r < A.px.groups);
+                }
+            }
+            if (w.n > 0) return true;
+        }
+        return false;
+    }
+};
+struct NoWalk {
+    __device__ __forceinline__ NoWalk(const PfArgs&) {}
+};
+
+// PAGED.  First row of KV head h from key `key` of group r's prefix on, in the pages seen as rows; -1 past it or on no page.
+__device__ __forceinline__ int prefix_row(const PfArgs& A, int r, int h, int key, int last) {
+    const PagedCacheView& c = A.px.c;
+    const int at = key >> c.log_page;
+    if (key > last || at >= A.px.max_pages) return -1;
+    const int page = __ldg(&A.px.table[(size_t)r * A.px.max_pages + at]);
+    if (page < 0 || page >= c.num_pages) return -1;
+    return (int)((((unsigned)page * (unsigned)A.io.Hkv + (unsigned)h) << c.log_page) + (unsigned)(key & ((1 << c.log_page) - 1)));
+}
+// Bit c: key + c is on a page (key a multiple of 32).
+__device__ __forceinline__ uint32_t on_pages(const PfArgs& A, int r, int key, int last) {
+    const uint32_t low = prefix_row(A, r, 0, key, last) >= 0 ? 0xffffu : 0u;
+    return low | (prefix_row(A, r, 0, key + 16, last) >= 0 ? 0xffff0000u : 0u);
 }
 
 // The n lowest bits, n clamped to [0, 32].
@@ -344,9 +482,11 @@ __device__ __forceinline__ uint32_t unbounded_mask(uint32_t w) {   // the halves
 // PARTS: a pair's blocks are divided into several items, which leave sums for prefill_join_kernel.
 // RAGGED: the CTAs share out the items, which the TMA warp finds and hands to the others, instead
 // of the places for them, of which shorter sequences leave many unused.
-template <class T, bool PARTS, bool RAGGED>
+// PAGED: a group's prefix instead of sequences (see the top); PARTS too.
+template <class T, bool PARTS, bool RAGGED, bool PAGED>
 __global__ void __launch_bounds__(kPfThreads, 1) prefill_kernel(const __grid_constant__ PfArgs A) {
     static_assert(!(PARTS && RAGGED), "items that are parts have a place each");
+    static_assert(PARTS || !PAGED, "shares of a prefix are parts");
     extern __shared__ uint8_t pf_smem_raw[];
     // 1024-byte alignment for the swizzled operand tiles.
     uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(pf_smem_raw) + 1023) & ~uintptr_t(1023));
@@ -387,8 +527,10 @@ __global__ void __launch_bounds__(kPfThreads, 1) prefill_kernel(const __grid_con
     ptx::tc_fence_before();
     __syncthreads();
     ptx::tc_fence_after();
-    asm volatile("griddepcontrol.launch_dependents;\n" ::: "memory");
+    // PAGED: the kernels behind this one read the call's inputs before they wait: the trigger comes when these are complete.
+    if constexpr (!PAGED) asm volatile("griddepcontrol.launch_dependents;\n" ::: "memory");
     asm volatile("griddepcontrol.wait;\n" ::: "memory");
+    if constexpr (PAGED) asm volatile("griddepcontrol.launch_dependents;\n" ::: "memory");
     const uint32_t tmem = (uint32_t)ptx::warp_uniform((int)bars->tmem_base);
     const volatile int* const abort = &bars->abort_flag;
     const int sinks = A.io.sinks;
@@ -402,7 +544,9 @@ __global__ void __launch_bounds__(kPfThreads, 1) prefill_kernel(const __grid_con
     // The next item, the same for every warp; false: none is left.
     int taken = 0;
     const int turns = (A.items + gridDim.x - 1) / gridDim.x;
+    std::conditional_t<PAGED, GroupWalk, NoWalk> walk(A);
     auto take_item = [&](Item& w) {
+        if constexpr (PAGED) return walk.next(w);
         if constexpr (!RAGGED) {
             while (taken < turns)
                 if (item_at<PARTS>(A, item_of(taken++), w)) return true;
@@ -454,13 +598,32 @@ __global__ void __launch_bounds__(kPfThreads, 1) prefill_kernel(const __grid_con
                     hand_out(turn + 1);
                     continue;
                 }
+                // PAGED: lane l finds where the l / 2-th piece of a block lies, a block ahead, and copies half its columns.
+                int piece = 0;
+                auto find_piece = [&](int i) {
+                    if constexpr (PAGED) {
+                        const int key = w.block(i) * kPfTile + ((lane >> 1) << A.page_log);
+                        piece = (lane >> 1) << A.page_log < kPfTile ? prefix_row(A, w.k0, w.h, key, w.off) : -1;
+                    }
+                };
+                find_piece(0);
                 auto load_kv = [&](int y) {   // load y of the item: K and V blocks alternate
                     const int st = x % kPfStages, round = x / kPfStages;
                     if (round > 0 && !pf_wait(&bars->empty[st], (round - 1) & 1, abort)) {
                         stop = true;
                         return;
                     }
-                    if (ptx::elect_one()) {
+                    if constexpr (PAGED) {
+                        if (lane == 0) ptx::mbar_arrive_expect_tx(&bars->full[st], (uint32_t)kPfBuf);
+                        __syncwarp();
+                        const int rows = 1 << A.page_log, at = (lane >> 1) * rows;
+                        // Rows behind the last of all are filled with zeros: what lies past the prefix or on no page.
+                        if (at < kPfTile)
+                            ptx::tma_load_2d(ring + st * kPfBuf + (lane & 1) * kPfHalf + at * 128, y & 1 ? &A.vmap : &A.kmap,
+                                             &bars->full[st], (lane & 1) * 64, piece < 0 ? A.px.rows : piece);
+                        __syncwarp();
+                        if ((y & 1) && (y >> 1) + 1 < w.n) find_piece((y >> 1) + 1);
+                    } else if (ptx::elect_one()) {
                         const CUtensorMap* map = y & 1 ? &A.vmap : &A.kmap;
                         uint8_t* dst = ring + st * kPfBuf;
                         const int row = w.k0 + w.block(y >> 1) * kPfTile;
@@ -724,7 +887,14 @@ __global__ void __launch_bounds__(kPfThreads, 1) prefill_kernel(const __grid_con
                 for (int c = 0; c < kPfTile; ++c) {
                     const int key = w.block(i) * kPfTile + c;
                     if (key > p || (key <= below && key >= sinks)) continue;
-                    const uint16_t* v = A.io.v + ((size_t)(w.k0 + key) * A.io.Hkv + w.h) * kHeadDim;
+                    const uint16_t* v;
+                    if constexpr (PAGED) {
+                        const int row = prefix_row(A, w.k0, w.h, key, p);
+                        if (row < 0) continue;
+                        v = A.px.c.v + (size_t)row * kHeadDim;
+                    } else {
+                        v = A.io.v + ((size_t)(w.k0 + key) * A.io.Hkv + w.h) * kHeadDim;
+                    }
 #pragma unroll 1
                     for (int d = 0; d < kHeadDim; ++d)
                         if (unbounded_mask<T>(v[d])) add(d, Half16<T>::unpack(v[d]).x);
@@ -737,9 +907,17 @@ __global__ void __launch_bounds__(kPfThreads, 1) prefill_kernel(const __grid_con
             if (t >= w.tiles) continue;
             const int query = w.a + t * A.nq + row_q;
             const bool live = row < A.nq * A.g && query < w.b;        // the row is a real one
-            const int p = w.off + query;
+            const int p = PAGED ? w.off : w.off + query;
             const int below = A.io.window ? p - A.io.window : -1;     // keys up to here are out of the window
             const int n = w.n;
+            // PAGED: whether some page is missing in the share (each block's are looked up then).
+            bool holes = false;
+            if constexpr (PAGED) {
+                const int pages = (min(n * kPfTile, p + 1 - w.i0 * kPfTile) + (1 << A.page_log) - 1) >> A.page_log;
+                for (int k = lane; k < pages; k += 32)
+                    holes |= prefix_row(A, w.k0, 0, w.i0 * kPfTile + (k << A.page_log), p) < 0;
+                holes = __any_sync(0xffffffffu, holes);
+            }
             float m = kNoLogit, l = 0.f;
             for (int i = 0; i < n; ++i, ++blocks) {
                 if (!pf_wait(&bars->s_full[t], blocks & 1, abort)) {
@@ -751,14 +929,17 @@ __global__ void __launch_bounds__(kPfThreads, 1) prefill_kernel(const __grid_con
 #pragma unroll
                 for (int c = 0; c < 4; ++c) ptx::tmem_ld32(tS + c * 32, s + c * 32);
                 ptx::tmem_wait_ld();
-                if (w.edge(i)) {
+                if (w.edge(i) || (PAGED && holes)) {
                     // Bit c of the words: the row sees key t0 + c.  (Comparisons for each column
                     // became branches, 12,000 cycles a block.)
                     const int t0 = w.block(i) * kPfTile;
 #pragma unroll
                     for (int g = 0; g < 4; ++g) {
                         const int b0 = t0 + 32 * g;
-                        const uint32_t seen = low_bits(p + 1 - b0) & (~low_bits(below + 1 - b0) | low_bits(sinks - b0));
+                        uint32_t seen = low_bits(p + 1 - b0) & (~low_bits(below + 1 - b0) | low_bits(sinks - b0));
+                        if constexpr (PAGED) {
+                            if (holes) seen &= on_pages(A, w.k0, b0, p);
+                        }
 #pragma unroll
                         for (int c = 0; c < 32; ++c) s[32 * g + c] = (seen >> c) & 1u ? s[32 * g + c] : -INFINITY;
                     }
@@ -825,7 +1006,7 @@ __global__ void __launch_bounds__(kPfThreads, 1) prefill_kernel(const __grid_con
             const size_t at = (size_t)(w.q0 + query) * A.io.Hq + w.h * A.g + j;
             if constexpr (PARTS) {
                 // Sums and maximum as they are, for prefill_join_kernel.
-                const size_t prow = ((size_t)w.place * 2 + t) * kPfTile + row;
+                const size_t prow = PAGED ? (size_t)w.place + t * A.nq * A.g + row : ((size_t)w.place * 2 + t) * kPfTile + row;
                 float* dst = A.part_o + prow * kHeadDim;
 #pragma unroll 1
                 for (int c = 0; c < 4 && n > 0; ++c) {
@@ -914,6 +1095,61 @@ __global__ void __launch_bounds__(32 * kPjWarps) prefill_join_kernel(const __gri
     if (lane == 0 && A.io.lse) A.io.lse[at] = some ? fmaf(M, 0.6931471805599453f, logf(L)) : -INFINITY;
 }
 
+// What the shares of a prefix sum up to for each row: a warp a (sequence, query head), four dimensions a lane.  The
+// maxima and sums of up to 32 shares are read by a lane each.
+constexpr int kXjWarps = 4;
+__global__ void __launch_bounds__(32 * kXjWarps) prefix_join_kernel(const __grid_constant__ PfArgs A, int ctas) {
+    asm volatile("griddepcontrol.launch_dependents;\n" ::: "memory");
+    const int lane = threadIdx.x & 31, row = blockIdx.x * kXjWarps + (threadIdx.x >> 5);
+    const int s = row / A.io.Hq, hq = row - s * A.io.Hq, h = hq / A.g;
+    // The lengths were complete before the kernel that this one waits for began.
+    int lo = 0, hi = A.px.groups;   // the last group that begins at or before s
+    while (lo < hi) {
+        const int mid = (lo + hi + 1) >> 1;
+        if (__ldg(&A.px.cu[mid]) <= s) lo = mid; else hi = mid - 1;
+    }
+    const Group gr(A, lo);
+    const bool some = s < A.io.total_q && gr.places() > 0 && s >= gr.q0 && s < gr.q0 + gr.n;   // behind the last group there is none
+    int c0 = 0, c1 = -1, base = 0;
+    const GroupList list(A);
+    if (some) {
+        const int seat = s - gr.q0, pair = seat / (2 * A.nq);
+        const long long at = list.places_before(A, lo) + (long long)(h * gr.pairs + pair) * gr.places() + Group::kCost;
+        c0 = (int)(((at + 1) * ctas - 1) / list.total);
+        c1 = (int)(((at + gr.nb) * ctas - 1) / list.total);
+        base = gr.first_row(A, h, pair) + (seat - pair * 2 * A.nq) * A.g + hq - h * A.g;
+    }
+    asm volatile("griddepcontrol.wait;\n" ::: "memory");
+    if (s >= A.io.total_q) return;
+    float M = kNoLogit, L = 0.f;
+    float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+    for (int c = c0; c <= c1; c += 32) {
+        const int cta = c + lane;
+        // A CTA of an empty share (there are more CTAs than blocks) leaves nothing.
+        const bool here = cta <= c1 && group_share(list.total, cta, ctas) < group_share(list.total, cta + 1, ctas);
+        const float2 ml = here ? A.part_ml[base + 2 * kPfTile * cta] : make_float2(kNoLogit, 0.f);
+        float m = ml.x;
+#pragma unroll
+        for (int d = 16; d; d >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, d));
+        m = fmaxf(m, M);
+        const float f = ptx::ex2(M - m);
+        L *= f;
+        o = make_float4(o.x * f, o.y * f, o.z * f, o.w * f);
+        M = m;
+        const float w = here ? ptx::ex2(ml.x - m) : 0.f;
+        const int n = min(32, c1 - c + 1);
+        for (int k = 0; k < n; ++k) {
+            if (!__shfl_sync(0xffffffffu, here ? 1 : 0, k)) continue;
+            const float wk = __shfl_sync(0xffffffffu, w, k);
+            const float4 v = reinterpret_cast<const float4*>(A.part_o + (size_t)(base + 2 * kPfTile * (c + k)) * kHeadDim)[lane];
+            L = fmaf(wk, __shfl_sync(0xffffffffu, ml.y, k), L);
+            o = make_float4(fmaf(wk, v.x, o.x), fmaf(wk, v.y, o.y), fmaf(wk, v.z, o.z), fmaf(wk, v.w, o.w));
+        }
+    }
+    reinterpret_cast<float4*>(A.px.out + (size_t)row * kHeadDim)[lane] = o;
+    if (lane == 0) A.px.ml[row] = make_float2(M, L);
+}
+
 template <class T>
 cudaError_t launch_typed(const PfArgs& a, long long used_pairs, int num_sms, cudaStream_t st) {
     const dim3 grid((unsigned)std::min(a.items, num_sms));
@@ -924,9 +1160,9 @@ cudaError_t launch_typed(const PfArgs& a, long long used_pairs, int num_sms, cud
     const bool ragged = (long long)a.pairs * a.io.batch * 15 > used_pairs * 16 && a.items <= 64 * num_sms;
     if (a.parts == 1)
         return ragged
-                   ? launch_prio(prefill_kernel<T, false, true>, grid, dim3(kPfThreads), kPfSmem, st, 0, true, a)
-                   : launch_prio(prefill_kernel<T, false, false>, grid, dim3(kPfThreads), kPfSmem, st, 0, true, a);
-    cudaError_t e = launch_prio(prefill_kernel<T, true, false>, grid, dim3(kPfThreads), kPfSmem, st, 0, true, a);
+                   ? launch_prio(prefill_kernel<T, false, true, false>, grid, dim3(kPfThreads), kPfSmem, st, 0, true, a)
+                   : launch_prio(prefill_kernel<T, false, false, false>, grid, dim3(kPfThreads), kPfSmem, st, 0, true, a);
+    cudaError_t e = launch_prio(prefill_kernel<T, true, false, false>, grid, dim3(kPfThreads), kPfSmem, st, 0, true, a);
     if (e != cudaSuccess) return e;
     return launch_prio(prefill_join_kernel<T>, dim3((unsigned)(a.items / a.parts), 2 * kPfTile / kPjWarps), dim3(32 * kPjWarps),
                        0, st, 0, true, a);
@@ -946,12 +1182,14 @@ cudaError_t configure_prefill() {
     auto one = [&](auto kernel) {
         if (e == cudaSuccess) e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kPfSmem);
     };
-    one(prefill_kernel<__nv_bfloat16, false, false>);
-    one(prefill_kernel<__nv_bfloat16, false, true>);
-    one(prefill_kernel<__nv_bfloat16, true, false>);
-    one(prefill_kernel<__half, false, false>);
-    one(prefill_kernel<__half, false, true>);
-    one(prefill_kernel<__half, true, false>);
+    one(prefill_kernel<__nv_bfloat16, false, false, false>);
+    one(prefill_kernel<__nv_bfloat16, false, true, false>);
+    one(prefill_kernel<__nv_bfloat16, true, false, false>);
+    one(prefill_kernel<__half, false, false, false>);
+    one(prefill_kernel<__half, false, true, false>);
+    one(prefill_kernel<__half, true, false, false>);
+    one(prefill_kernel<__nv_bfloat16, true, false, true>);
+    one(prefill_kernel<__half, true, false, true>);
     return e;
 }
 
@@ -1000,6 +1238,47 @@ cudaError_t launch_prefill(const PrefillIO& io, const PrefillPlan& plan, int num
     if (e == cudaSuccess) e = encode_tensor_map(&a.vmap, io.dtype, 3, keys ? io.v : io.q, kd, ks, kb);
     if (e != cudaSuccess) return e;
     return io.dtype == 1 ? launch_typed<__half>(a, plan.used_pairs, num_sms, st) : launch_typed<__nv_bfloat16>(a, plan.used_pairs, num_sms, st);
+}
+
+// Sums of the shares: a row for every query row, and a pair of tiles more for every CTA, as the items of a list may
+// each end in one and go on in the next.
+size_t prefix_scratch(int batch, int Hq, int num_sms) {
+    return ((size_t)batch * Hq + (size_t)2 * kPfTile * num_sms) * (kHeadDim * sizeof(float) + sizeof(float2));
+}
+
+cudaError_t launch_prefix(const PrefixIO& px, int num_sms, cudaStream_t st) {
+    PfArgs a{};
+    a.px = px;
+    a.io.Hq = px.Hq;
+    a.io.Hkv = px.Hkv;
+    a.io.total_q = px.batch;
+    a.io.err = px.err;
+    a.g = px.Hq / px.Hkv;
+    a.nq = kPfTile / a.g;
+    a.parts = 1;
+    a.page_log = std::min(px.c.log_page, 7);
+    static_assert(kPfTile == 1 << 7, "a block's keys");
+    a.px.rows = (int)(((long long)px.c.num_pages * px.Hkv) << px.c.log_page);
+    const size_t rows = (size_t)px.batch * px.Hq + (size_t)2 * kPfTile * num_sms;
+    a.part_o = static_cast<float*>(px.scratch);
+    a.part_ml = reinterpret_cast<float2*>(a.part_o + rows * kHeadDim);
+    a.sl2 = px.scale * 1.4426950408889634f;
+    a.fault = test_fault() == 4 ? 1 : 0;
+    const uint64_t row = (uint64_t)kHeadDim * 2;
+    const uint64_t qd[3] = {(uint64_t)kHeadDim, (uint64_t)px.Hq, (uint64_t)px.batch}, qs[2] = {row, row * px.Hq};
+    const uint32_t qb[3] = {64, (uint32_t)a.g, (uint32_t)a.nq};
+    const uint64_t kd[2] = {(uint64_t)kHeadDim, (uint64_t)a.px.rows}, ks[1] = {row};
+    const uint32_t kb[2] = {64, 1u << a.page_log};
+    cudaError_t e = encode_tensor_map(&a.qmap, px.c.dtype, 3, px.q, qd, qs, qb);
+    if (e == cudaSuccess) e = encode_tensor_map(&a.kmap, px.c.dtype, 2, px.c.k, kd, ks, kb);
+    if (e == cudaSuccess) e = encode_tensor_map(&a.vmap, px.c.dtype, 2, px.c.v, kd, ks, kb);
+    if (e != cudaSuccess) return e;
+    e = px.c.dtype == 1
+            ? launch_prio(prefill_kernel<__half, true, false, true>, dim3(num_sms), dim3(kPfThreads), kPfSmem, st, 0, true, a)
+            : launch_prio(prefill_kernel<__nv_bfloat16, true, false, true>, dim3(num_sms), dim3(kPfThreads), kPfSmem, st, 0, true, a);
+    if (e != cudaSuccess) return e;
+    const dim3 grid((unsigned)(((long long)px.batch * px.Hq + kXjWarps - 1) / kXjWarps));
+    return launch_prio(prefix_join_kernel, grid, dim3(32 * kXjWarps), 0, st, 0, true, a, num_sms);
 }
 
 }  // namespace kvec

@@ -32,7 +32,8 @@ EXPORTED = ("kvec_create", "kvec_destroy", "kvec_state_bytes", "kvec_reset", "kv
             "kvec_noalloc_sync_status", "kvec_set_test_fault", "kvec_output_capacity",
             "kvec_rotate_append", "kvec_paged_decode_bytes", "kvec_paged_decode_window_bytes", "kvec_paged_decode",
             "kvec_paged_evict", "kvec_prefill_bytes", "kvec_prefill_attention", "kvec_rotate_append_quant",
-            "kvec_paged_decode_quant", "kvec_paged_evict_quant", "kvec_paged_read")
+            "kvec_paged_decode_quant", "kvec_paged_evict_quant", "kvec_paged_read", "kvec_shared_decode_bytes",
+            "kvec_shared_decode")
 
 KVEC_BF16 = 0
 KVEC_FP16 = 1
@@ -79,6 +80,13 @@ class kvec_paged_cache(ctypes.Structure):
 
 class kvec_paged_scales(ctypes.Structure):
     _fields_ = [("k_scales", ctypes.c_void_p), ("v_scales", ctypes.c_void_p)]
+
+
+class kvec_shared_prefix(ctypes.Structure):
+    _fields_ = [
+        ("num_groups", ctypes.c_int), ("max_pages", ctypes.c_int),
+        ("page_table", ctypes.c_void_p), ("lens", ctypes.c_void_p), ("cu_seqs", ctypes.c_void_p),
+    ]
 
 
 class kvec_rotate_args(ctypes.Structure):
@@ -147,6 +155,9 @@ def load() -> ctypes.CDLL:
                                          i, i, i, _vp, _vp, ctypes.c_size_t, _vp], st),
             "kvec_paged_evict_quant": ([_vp, i, ctypes.POINTER(kvec_paged_cache), ctypes.POINTER(kvec_paged_scales), _vp,
                                         i, i, i, i, i, _vp, _vp, _vp], st),
+            "kvec_shared_decode_bytes": ([_vp, i, i, i], ctypes.c_size_t),
+            "kvec_shared_decode": ([_vp, i, _vp, ctypes.POINTER(kvec_paged_cache), ctypes.POINTER(kvec_shared_prefix), i, i,
+                                    _vp, _vp, ctypes.c_size_t, _vp], st),
             "kvec_paged_read": ([_vp, i, ctypes.POINTER(kvec_paged_cache), ctypes.POINTER(kvec_paged_scales), _vp, _vp, i,
                                  _vp, _vp, _vp], st),
         }
@@ -273,6 +284,16 @@ def kvec_paged_evict(handle: int, batch: int, cache: kvec_paged_cache, new_table
                      budget: int, sinks: int, recent: int, new_lens: int, kept: int, stream: int = 0) -> None:
     _check(load().kvec_paged_evict(handle, batch, cache, new_table, new_max_pages, max_len, budget, sinks, recent,
                                    new_lens, kept, stream))
+
+
+def kvec_shared_decode_bytes(handle: int, batch: int, max_len: int, with_weights: bool) -> int:
+    return int(load().kvec_shared_decode_bytes(handle, batch, max_len, 1 if with_weights else 0))
+
+
+def kvec_shared_decode(handle: int, batch: int, q: int, cache: kvec_paged_cache, prefix: kvec_shared_prefix, max_len: int,
+                       max_prefix: int, out: int, scratch: int, scratch_bytes: int, stream: int = 0) -> None:
+    _check(load().kvec_shared_decode(handle, batch, q, cache, prefix, max_len, max_prefix, out, scratch, scratch_bytes,
+                                     stream))
 
 
 def kvec_rotate_append_quant(handle: int, args: kvec_rotate_args, batch: int, cu_tokens: Optional[int],
@@ -421,6 +442,27 @@ class PagedCache:
         self.scales = kvec_paged_scales(k_scales.data_ptr(), v_scales.data_ptr()) if self.eight else None
 
 
+class SharedPrefix:
+    """Prefixes that groups of consecutive sequences share (kvec_shared_prefix): holds its tensors, computes nothing.
+
+    page_table int32 [num_groups][max_pages] of pages of the cache's pool; lens int32 [num_groups]; cu_seqs int32
+    [num_groups + 1]: group r's sequences are cu_seqs[r] .. cu_seqs[r + 1] - 1.  All contiguous, on the cache's device."""
+
+    def __init__(self, page_table, lens, cu_seqs):
+        import torch as t
+        _want(page_table.dim() == 2 and page_table.dtype == t.int32 and page_table.shape[1] >= 1,
+              "page_table must be int32 [num_groups][max_pages]")
+        groups = page_table.shape[0]
+        _want(lens.dtype == t.int32 and tuple(lens.shape) == (groups,), "lens must be int32 [num_groups]")
+        _want(cu_seqs.dtype == t.int32 and tuple(cu_seqs.shape) == (groups + 1,), "cu_seqs must be int32 [num_groups + 1]")
+        parts = (page_table, lens, cu_seqs)
+        _want(all(x.is_contiguous() for x in parts), "a prefix's tensors must be contiguous")
+        _want(all(x.device == lens.device for x in parts), "a prefix's tensors must be on one device")
+        self.page_table, self.lens, self.cu_seqs = parts
+        self.max_pages, self.device = page_table.shape[1], lens.device
+        self.c = kvec_shared_prefix(groups, self.max_pages, page_table.data_ptr(), lens.data_ptr(), cu_seqs.data_ptr())
+
+
 class KvecSelector:
     """Owns a kvec handle; torch tensors in, torch tensors out.  Marshalling only.
 
@@ -436,7 +478,7 @@ class KvecSelector:
         self.device = torch.device("cuda", torch.cuda.current_device())
         self._current = torch._C._cuda_getCurrentRawStream   # torch.cuda.current_stream makes an object, 2 us
         self._lib = load()
-        self._decode_bytes = {}      # kvec_paged_decode_window_bytes by its sizes
+        self._decode_bytes = {}      # kvec_paged_decode_window_bytes and kvec_shared_decode_bytes by their sizes
         self.state_bytes = kvec_state_bytes(params.max_seqlen)
 
     def close(self) -> None:
@@ -623,6 +665,15 @@ class KvecSelector:
                 self._used(stream, cache, q, k, v, positions, rot_table, cu_tokens, q_norm, k_norm, q_out, k_out)
         return (q_out, k_out) if want_k else q_out
 
+    def _scratch_bytes(self, of, *sizes):
+        # (Calls of different kinds have a different number of sizes.)
+        need = self._decode_bytes.get(sizes)
+        if need is None:
+            if len(self._decode_bytes) >= 256:   # a loop's bounds may grow with every step
+                self._decode_bytes.clear()
+            need = self._decode_bytes[sizes] = of(self.handle, *sizes)
+        return need
+
     def paged_decode(self, q, cache, max_len: Optional[int] = None, window: int = 0, sinks: int = 0, out=None,
                      stream=None):
         """One new token per sequence over a paged cache (kvec_paged_decode, or kvec_paged_decode_quant over one of 8 bits);
@@ -644,12 +695,7 @@ class KvecSelector:
             max_len = cache.capacity
         if (max_len | window | sinks) >> 31:   # ctypes would pass their lower 32 bits
             raise KvecError(KVEC_ERR_INVALID_ARG, "max_len, window and sinks must be in [0, 2^31)")
-        sizes = (batch, max_len, window, sinks, cache.weights is not None)
-        need = self._decode_bytes.get(sizes)
-        if need is None:
-            if len(self._decode_bytes) >= 256:   # a loop's bounds may grow with every step
-                self._decode_bytes.clear()
-            need = self._decode_bytes[sizes] = kvec_paged_decode_window_bytes(self.handle, *sizes)
+        need = self._scratch_bytes(kvec_paged_decode_window_bytes, batch, max_len, window, sinks, cache.weights is not None)
         scratch = self._empty(max(need, 16), self._torch.uint8, stream)
         if cache.eight:
             st = self._lib.kvec_paged_decode_quant(self.handle, batch, q.data_ptr(), cache.c, cache.scales, max_len, window,
@@ -661,6 +707,42 @@ class KvecSelector:
             _check(st)
         if stream is not None:
             self._used(stream, cache, q, out)
+        return out
+
+    def shared_decode(self, q, cache, prefix, max_len: Optional[int] = None, max_prefix: Optional[int] = None, out=None,
+                      stream=None):
+        """One new token per sequence where groups of sequences share a prefix (kvec_shared_decode); adds to cache.weights,
+        where it has them, for the sequences' own slots.
+
+        q [batch][H_q][d] of the cache's type (16 bits), contiguous; cache: the sequences' own slots, prefix a
+        SharedPrefix of pages of the same pool.  max_len bounds the own lengths, max_prefix those of the prefixes (the
+        capacities): give the least bounds that are known."""
+        p = self.params
+        batch, dtype = cache.batch, cache.dtype
+        shape = (batch, p.num_q_heads, p.head_dim)
+        self._check_cache(cache)
+        if cache.eight:
+            raise KvecError(KVEC_ERR_UNSUPPORTED, "shared_decode takes caches of 16 bits")
+        _want(prefix.device == self.device, "the prefix must be on the handle's device")
+        self._check("q", q, shape, dtype)
+        if out is None:
+            out = self._empty(shape, dtype, stream)
+        else:
+            self._check("out", out, shape, dtype)
+        if max_len is None:
+            max_len = cache.capacity
+        if max_prefix is None:
+            max_prefix = prefix.max_pages * cache.page_size
+        if (max_len | max_prefix) >> 31:
+            raise KvecError(KVEC_ERR_INVALID_ARG, "max_len and max_prefix must be in [0, 2^31)")
+        need = self._scratch_bytes(kvec_shared_decode_bytes, batch, max_len, cache.weights is not None)
+        scratch = self._empty(max(need, 16), self._torch.uint8, stream)
+        st = self._lib.kvec_shared_decode(self.handle, batch, q.data_ptr(), cache.c, prefix.c, max_len, max_prefix,
+                                          out.data_ptr(), scratch.data_ptr(), need, self._raw(stream))
+        if st:
+            _check(st)
+        if stream is not None:
+            self._used(stream, cache, q, out, prefix.page_table, prefix.lens, prefix.cu_seqs)
         return out
 
     def paged_evict(self, cache, new_table, budget: int, sinks: int = 0, recent: int = 0, max_len: Optional[int] = None,
