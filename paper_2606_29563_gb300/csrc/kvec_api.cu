@@ -1330,7 +1330,13 @@ kvec_status kvec_rotate_append_quant(kvec_handle* h, const kvec_rotate_args* a, 
 size_t kvec_paged_decode_window_bytes(kvec_handle* h, int batch, int max_len, int window, int sinks, int with_weights) {
     if (!h || batch < 1 || batch > h->p.max_batch || max_len < 1 || max_len > kPagedMaxLen || window < 0 || sinks < 0) return 0;
     return paged_decode_scratch(batch, h->p.num_q_heads, max_len, within_length(window), within_length(sinks),
-                                with_weights != 0, h->num_sms);
+                                with_weights != 0, false, h->num_sms);
+}
+
+size_t kvec_paged_decode_quant_bytes(kvec_handle* h, int batch, int max_len, int window, int sinks, int with_weights) {
+    if (!h || batch < 1 || batch > h->p.max_batch || max_len < 1 || max_len > kPagedMaxLen || window < 0 || sinks < 0) return 0;
+    return paged_decode_scratch(batch, h->p.num_q_heads, max_len, within_length(window), within_length(sinks),
+                                with_weights != 0, true, h->num_sms);
 }
 
 size_t kvec_paged_decode_bytes(kvec_handle* h, int batch, int max_len, int with_weights) {
@@ -1352,7 +1358,7 @@ kvec_status paged_decode(kvec_handle* h, int batch, const void* q, const PagedCa
     if (!q || !out || !scratch) return fail(KVEC_ERR_INVALID_ARG, "a device pointer is NULL");
     if (!aligned16(q) || !aligned16(out) || !aligned16(scratch))
         return fail(KVEC_ERR_INVALID_ARG, "q, out and scratch must be 16-byte aligned");
-    const size_t need = kvec_paged_decode_window_bytes(h, batch, max_len, window, sinks, v.weights != nullptr);
+    const size_t need = (v.k_scales ? kvec_paged_decode_quant_bytes : kvec_paged_decode_window_bytes)(h, batch, max_len, window, sinks, v.weights != nullptr);
     if (scratch_bytes < need)
         return fail(KVEC_ERR_INVALID_ARG, "scratch of %zu bytes, %zu are needed", scratch_bytes, need);
     PagedDecodeIO io{};
@@ -1493,7 +1499,7 @@ struct SharedScratch {
     size_t out, ml, prefix, total;   // behind paged_decode's
     SharedScratch(const kvec_handle* h, int batch, int max_len, bool weights) {
         const size_t rows = (size_t)batch * h->p.num_q_heads;
-        out = round_up(paged_decode_scratch(batch, h->p.num_q_heads, max_len, 0, 0, weights, h->num_sms), 256);
+        out = round_up(paged_decode_scratch(batch, h->p.num_q_heads, max_len, 0, 0, weights, false, h->num_sms), 256);
         ml = out + rows * h->p.head_dim * sizeof(float);
         prefix = round_up(ml + rows * sizeof(float2), 256);
         total = prefix + prefix_scratch(batch, h->p.num_q_heads, h->num_sms);

@@ -339,7 +339,7 @@ cudaError_t launch_ada(const Geometry& g, const LayerIO& io, const Scratch& sc, 
 cudaError_t launch_decode(const DecodeIO& io, int num_sms, cudaStream_t st);
 cudaError_t launch_rotate(const RotateIO& io, const PagedCacheView& c, cudaStream_t st);
 cudaError_t launch_paged_decode(const PagedDecodeIO& io, const PagedCacheView& c, int num_sms, cudaStream_t st);
-size_t paged_decode_scratch(int batch, int Hq, int max_len, int window, int sinks, bool weights, int num_sms);
+size_t paged_decode_scratch(int batch, int Hq, int max_len, int window, int sinks, bool weights, bool e8, int num_sms);
 cudaError_t launch_read(const ReadIO& io, const PagedCacheView& c, cudaStream_t st);
 cudaError_t launch_evict(const EvictIO& io, const PagedCacheView& c, cudaStream_t st);
 PrefillPlan plan_prefill(int batch, int Hq, int Hkv, int max_q, int max_k, int window, int sinks, int num_sms);

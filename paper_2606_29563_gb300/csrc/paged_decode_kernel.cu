@@ -44,17 +44,14 @@ namespace cg = cooperative_groups;
 
 constexpr int kPdWarps = 4;
 constexpr int kPdThreads = 32 * kPdWarps;
-constexpr int kPdBlock = 16;                 // slots of a block
-constexpr int kPdTile = kPdBlock * 128;      // bytes of 16 rows x 64 columns
-// A block in a warp's ring: K columns 0-63, 64-127 and V the same, or with 8 bits a tile of 16 whole rows each; and
-// how many of them are there.
+constexpr int kPdStages = 3;                 // blocks in a warp's ring
+constexpr int kPdHalf = 16;                  // slots that are surely of one page
+// Slots of a block: with 8 bits two halves of 16, each with a page of its own.
 template <bool E8>
-constexpr int kPdStage = (E8 ? 2 : 4) * kPdTile;
-template <bool E8>
-constexpr int kPdStages = E8 ? 6 : 3;
-constexpr int kPdRing = kPdStages<false> * kPdStage<false>;
-static_assert(kPdRing == kPdStages<true> * kPdStage<true>, "either format fills the same shared memory");
-constexpr int kPdSmem = kPdWarps * kPdRing + 1024;
+constexpr int kPdBlock = E8 ? 32 : 16;
+constexpr int kPdTile = 16 * 128;            // bytes of 16 rows x 64 columns, or of 16 whole rows of 8 bits
+constexpr int kPdStage = 4 * kPdTile;        // K columns 0-63, 64-127, V the same; 8 bits: 32 rows of K, of V
+constexpr int kPdSmem = kPdWarps * kPdStages * kPdStage + 1024;
 constexpr int kPdCtasPerSm = 2;
 constexpr int kPdMaxCluster = 8;
 constexpr int kPdHeads = 8;                  // most query heads of a KV head
@@ -66,22 +63,24 @@ constexpr int kJoinRows = 8 * kJoinThreads;  // slots of a join block's weights,
 constexpr float kNoLogit = -3.402823466e38f;
 
 struct PdArgs {
-    CUtensorMap kmap, vmap;   // [rows][128], boxes of 16 x 64 (of 16 rows of 128 bytes)
+    CUtensorMap kmap, vmap;   // [rows][128], boxes of 16 x 64; 8 bits: of 16 or 32 rows of 128 bytes
     PagedCacheView c;
     PagedDecodeIO io;
-    float* logits;            // [pair][nbmax][g][16]
+    float* logits;            // [pair][nbmax][g][slots of a block]
     float* part_o;            // [2 * ctas][8][128] shares of split pairs, unnormalised
     float2* part_ml;          // [2 * ctas][8] their maxima and sums
     int ctas;                 // that share the list of blocks
     int pairs;                // batch * Hkv where a CTA each may do, else 0
     int nbmax;                // most visible blocks of a pair
     int g;
+    int box;                  // 8 bits: rows of a copy, 32 where pages have that many
     float sl2;                // scale * log2(e)
     int fault;                // test of the error path (kvec_set_test_fault): warp 0 of CTA 0 loads nothing
 };
 
 // A sequence's visible slots and the blocks that hold them: blocks 0 .. first - 1, then
 // from block `from` on.
+template <int B>
 struct Visible {
     int n, lo, sinks;     // slots [0, min(sinks, n)) and [lo, n)
     int first, from, nb;
@@ -89,31 +88,43 @@ struct Visible {
         n = min(max(__ldg(&A.c.lens[s]), 0), A.io.max_len);
         lo = A.io.window ? max(n - A.io.window, 0) : 0;
         sinks = min(A.io.sinks, lo);
-        first = (sinks + kPdBlock - 1) / kPdBlock;
-        from = lo / kPdBlock;
+        first = (sinks + B - 1) / B;
+        from = lo / B;
         if (first >= from) first = from = 0;
-        nb = first + (n + kPdBlock - 1) / kPdBlock - from;
+        nb = first + (n + B - 1) / B - from;
     }
     __device__ __forceinline__ int block(int i) const { return i < first ? i : from + i - first; }
     __device__ __forceinline__ bool sees(int slot) const { return slot < n && (slot >= lo || slot < sinks); }
     __device__ __forceinline__ bool whole(int b) const {
-        return (b + 1) * kPdBlock <= n && (b * kPdBlock >= lo || (b + 1) * kPdBlock <= sinks);
+        return (b + 1) * B <= n && (b * B >= lo || (b + 1) * B <= sinks);
     }
 };
 
-// Row of block b's first slot for KV head h; -1 on no page.
-__device__ __forceinline__ int block_row(const PdArgs& A, int s, int h, int b) {
-    const int slot = b * kPdBlock;
+// Row of a slot for KV head h; -1 on no page.
+__device__ __forceinline__ int slot_row(const PdArgs& A, int s, int h, int slot) {
     const int page = __ldg(&A.c.table[(size_t)s * A.c.max_pages + (slot >> A.c.log_page)]);
     if (page < 0 || page >= A.c.num_pages) return -1;
     return (int)((((unsigned)page * (unsigned)A.io.Hkv + (unsigned)h) << A.c.log_page) +
                  (unsigned)(slot & ((1 << A.c.log_page) - 1)));
 }
+// Rows of block b's first slot and, of two halves, of the second's (-1: it lies behind the table, or in the bound's last
+// block behind that).
+template <int B>
+__device__ __forceinline__ int2 block_rows(const PdArgs& A, int s, int h, int b) {
+    int2 r = make_int2(slot_row(A, s, h, b * B), -1);
+    if constexpr (B > kPdHalf) {
+        const int slot = b * B + kPdHalf;
+        if (A.box == B) r.y = r.x < 0 ? -1 : r.x + kPdHalf;
+        else if (slot < A.io.max_len) r.y = slot_row(A, s, h, slot);
+    }
+    return r;
+}
 
 // A place in the list of blocks: block i of pair (s, h).
+template <int B>
 struct Walker {
     int s, h, i;
-    Visible v;
+    Visible<B> v;
     __device__ __forceinline__ void advance(const PdArgs& A, int by) {
         i += by;
         while (i >= v.nb && s < A.io.batch) {
@@ -130,11 +141,12 @@ struct Walker {
 // per + per - 1, over all KV heads.  Ahead of a pair's blocks stand kPairCost places without one,
 // so that a share of many short pairs does not take longer than others (32 rows of 100 to 4000
 // slots 75 us without, 68 with 4, 60 with 8, 56 with 12 and 16, 58 with 28).
+template <int B>
 struct List {
     int per, longest;                // most blocks of a pair
     int pairs_before, pairs;         // with blocks: of the lanes before, of all
     long long before, mine, total;   // places: of the lanes before, of this lane, of all
-    __device__ __forceinline__ static int places(const Visible& v) { return v.nb ? v.nb + kPairCost : 0; }
+    __device__ __forceinline__ static int places(const Visible<B>& v) { return v.nb ? v.nb + kPairCost : 0; }
     __device__ __forceinline__ void init(const PdArgs& A) {
         const int lane = threadIdx.x & 31;
         per = (A.io.batch + 31) >> 5;
@@ -143,7 +155,7 @@ struct List {
         for (int k = 0; k < per; ++k) {
             const int s = lane * per + k;
             if (s >= A.io.batch) break;
-            Visible v;
+            Visible<B> v;
             v.init(A, s);
             mine += places(v);
             own += v.nb ? A.io.Hkv : 0;
@@ -175,7 +187,7 @@ struct List {
         return A.pairs && (long long)longest * 190 <= total + 20 * 190;
     }
     // The first block from place `at` on; returns how many are before it.
-    __device__ __forceinline__ long long seek(const PdArgs& A, long long at, Walker& w) const {
+    __device__ __forceinline__ long long seek(const PdArgs& A, long long at, Walker<B>& w) const {
         const uint32_t past = __ballot_sync(0xffffffffu, at < before + mine);
         w.s = A.io.batch;
         w.h = w.i = 0;
@@ -202,7 +214,7 @@ struct List {
         const int l = s / per;
         long long b = __shfl_sync(0xffffffffu, before, l);
         for (int k = l * per; k < s; ++k) {
-            Visible v;
+            Visible<B> v;
             v.init(A, k);
             b += (long long)places(v) * A.io.Hkv;
         }
@@ -240,12 +252,23 @@ __device__ __forceinline__ void ldmatrix_x4_trans(uint32_t addr, uint32_t (&r)[4
                  : "memory");
 }
 
-// The power of two that brings a magnitude to [2^14, 2^15), within the range of normal numbers on both sides, and its
-// inverse.  fp16 products lose nothing near their largest factor then, and 2^-39 of it at most.
-__device__ __forceinline__ float to_fp16_range(float a) {
-    return __uint_as_float((uint32_t)min(268 - (int)(__float_as_uint(a) >> 23), 253) << 23);
+// The power of two that brings a magnitude to [2^E, 2^(E + 1)), within the range of normal numbers on both sides, and its
+// inverse.  In fp16's range (E = 14) products lose nothing near their largest factor then, and 2^-39 of it at most.
+template <int E>
+__device__ __forceinline__ float to_range(float a) {
+    return __uint_as_float((uint32_t)min(254 + E - (int)(__float_as_uint(a) >> 23), 253) << 23);
 }
 __device__ __forceinline__ float inverse_power(float p) { return __uint_as_float((254u << 23) - __float_as_uint(p)); }
+
+// d += A B, A 16 x 32 by rows, B 32 x 8 by columns, e4m3 with fp32 sums.
+__device__ __forceinline__ void mma_e4m3(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0,
+                                         uint32_t b1) {
+    asm volatile(
+        "mma.sync.aligned.m16n8k32.row.col.f32.e4m3.e4m3.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, "
+        "{%0, %1, %2, %3};\n"
+        : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+        : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
 
 // The products with the weights' roundings and with what these left.  Against an infinite value the rest, which is
 // zero or has either sign, would make NaN of what the roundings give alone.
@@ -253,23 +276,23 @@ __device__ __forceinline__ float with_rest(float hi, float lo) { return fabsf(hi
 
 // The attention weights of four slots of a block: what is read for them, and their sum over
 // the query heads once these' (maximum, 1 / sum) are known.
+template <int B>
 struct SlotWeights {
     float4 x[kPdHeads], w;
     int row;          // of the first, -1: none of them is visible or they are on no page
     bool seen[4];
-    // Quarter e of the pair's blocks from block i0 on.
-    __device__ __forceinline__ void load(const PdArgs& A, int s, int h, const Visible& v, int i0, int e) {
-        const int i = i0 + (e >> 2), r = (e & 3) * 4, b = v.block(i);
-        row = block_row(A, s, h, b);
+    // The e-th four slots of the pair's blocks from block i0 on.
+    __device__ __forceinline__ void load(const PdArgs& A, int s, int h, const Visible<B>& v, int i0, int e) {
+        const int i = i0 + e / (B / 4), r = e % (B / 4) * 4, slot = v.block(i) * B + r;
         bool any = false;
 #pragma unroll
-        for (int k = 0; k < 4; ++k) any |= seen[k] = v.sees(b * kPdBlock + r + k);
-        row = any && row >= 0 ? row + r : -1;
+        for (int k = 0; k < 4; ++k) any |= seen[k] = v.sees(slot + k);
+        row = any ? slot_row(A, s, h, slot) : -1;
         if (row < 0) return;
-        const float* lg = A.logits + (((size_t)s * A.io.Hkv + h) * A.nbmax + i) * (size_t)(A.g * kPdBlock) + r;
+        const float* lg = A.logits + (((size_t)s * A.io.Hkv + h) * A.nbmax + i) * (size_t)(A.g * B) + r;
 #pragma unroll
         for (int j = 0; j < kPdHeads; ++j)
-            if (j < A.g) x[j] = *reinterpret_cast<const float4*>(lg + j * kPdBlock);
+            if (j < A.g) x[j] = *reinterpret_cast<const float4*>(lg + j * B);
         w = *reinterpret_cast<const float4*>(A.c.weights + row);
     }
     __device__ __forceinline__ void store(const PdArgs& A, const float* mx, const float* inv) const {
@@ -294,34 +317,36 @@ struct SlotWeights {
 // a thread's at a time: two at once take 36 registers more in the decode kernel, which spills
 // then, and 40 in the join, of which fewer blocks are resident (64 rows of 1024 to 2048 slots
 // 59.6 us, 54.3 with one; a thread a slot 78).
-template <int NT>
-__device__ void add_weights(const PdArgs& A, int s, int h, const Visible& v, int i0, int i1, const float* mx,
+template <int NT, int B>
+__device__ void add_weights(const PdArgs& A, int s, int h, const Visible<B>& v, int i0, int i1, const float* mx,
                             const float* inv) {
-    const int n = (i1 - i0) * 4;
+    const int n = (i1 - i0) * (B / 4);
 #pragma unroll 1
     for (int e = threadIdx.x; e < n; e += NT) {
-        SlotWeights a;
+        SlotWeights<B> a;
         a.load(A, s, h, v, i0, e);
         a.store(A, mx, inv);
     }
 }
 
 // CL: a cluster of CTAs per pair (grid splits x Hkv x batch) instead of a share of the list.
-// E8: rows of e4m3 numbers with a scale each.  They become fp16, which holds them all, on their way from shared memory
-// to the tiles: the scale of a key multiplies its logit, that of a value its weight.  For that the
-// queries (in bf16) and the values' scales are brought to fp16's range by powers of two, a row's and the warp's so far.
+// E8: rows of e4m3 numbers with a scale each, which multiplies a key's logit and a value's weight.  The logits are tiles
+// of e4m3 (m16n8k32): a query row, brought to their range by a power of two, is the sum of two numbers (bf16, its 8 bits)
+// or three (fp16), so that keys go to the tiles as they are.  Values become fp16, which holds them all, on
+// their way; the weights with their scales are brought to its range by a power of two, the warp's so far.
 // PRE: sums of what comes before the sequence's own slots are merged at the end (launch_prefix); the kernels that leave
 // them may still run until then.
 template <class T, bool CL, bool E8, bool PRE>
 __global__ void __launch_bounds__(kPdThreads, kPdCtasPerSm) paged_decode_kernel(const __grid_constant__ PdArgs A) {
-    constexpr int kStage = kPdStage<E8>, kStages = kPdStages<E8>;
+    constexpr int B = kPdBlock<E8>;
+    constexpr bool kThird = E8 && std::is_same_v<T, __half>;    // a query is the sum of three e4m3 numbers
     using Operand = std::conditional_t<E8, __half, T>;          // the tiles' type
     extern __shared__ uint8_t pd_smem_raw[];
     // 1024-byte alignment for the swizzled tiles.
     uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(pd_smem_raw) + 1023) & ~uintptr_t(1023));
-    __shared__ __align__(8) uint64_t full[kPdWarps][kStages];
-    __shared__ int srow[kPdWarps][kStages];                    // first row of the staged block, -1: none
-    __shared__ __align__(16) float scales[kPdWarps][E8 ? kStages : 1][2][kPdBlock];   // of the staged block's K and V
+    __shared__ __align__(8) uint64_t full[kPdWarps][kPdStages];
+    __shared__ int2 srow[kPdWarps][kPdStages];                  // first rows of the staged block's halves, -1: none
+    __shared__ __align__(16) float scales[kPdWarps][E8 ? kPdStages : 1][2][B];   // of the staged block's K and V
     __shared__ float wm[kPdWarps][kPdHeads], wl[kPdWarps][kPdHeads];
     __shared__ float* wacc[kPdWarps];                           // the warps' outputs, each in its free stage
     __shared__ float cm[kPdHeads], cl[kPdHeads], fm[kPdHeads], finv[kPdHeads];
@@ -332,7 +357,7 @@ __global__ void __launch_bounds__(kPdThreads, kPdCtasPerSm) paged_decode_kernel(
         ptx::prefetch_tensormap(&A.kmap);
         ptx::prefetch_tensormap(&A.vmap);
         for (int w = 0; w < kPdWarps; ++w)
-            for (int i = 0; i < kStages; ++i) ptx::mbar_init(&full[w][i], 1);
+            for (int i = 0; i < kPdStages; ++i) ptx::mbar_init(&full[w][i], 1);
         ptx::fence_barrier_init();
     }
     __syncthreads();
@@ -342,7 +367,7 @@ __global__ void __launch_bounds__(kPdThreads, kPdCtasPerSm) paged_decode_kernel(
     asm volatile("griddepcontrol.launch_dependents;\n" ::: "memory");
 
     // This CTA's blocks: `count` from (s, h, i) on.
-    Walker cur;
+    Walker<B> cur;
     int count;   // a share of at most 65535 * 32 * 2^16 blocks
     int splits = 1, rank = 0;
     if constexpr (CL) {
@@ -354,7 +379,7 @@ __global__ void __launch_bounds__(kPdThreads, kPdCtasPerSm) paged_decode_kernel(
         cur.i = cur.v.nb * rank / splits;
         count = cur.v.nb * (rank + 1) / splits - cur.i;
     } else {
-        List list;
+        List<B> list;
         list.init(A);
         if (list.whole_pairs(A)) {
             cur.s = blockIdx.x / Hkv;
@@ -364,27 +389,27 @@ __global__ void __launch_bounds__(kPdThreads, kPdCtasPerSm) paged_decode_kernel(
             count = cur.v.nb;
         } else {
             const long long first = list.seek(A, share_start(list.total, blockIdx.x, A.ctas), cur);
-            Walker end;
+            Walker<B> end;
             count = (int)(list.seek(A, share_start(list.total, blockIdx.x + 1, A.ctas), end) - first);
         }
     }
 
-    uint8_t* ring = smem + warp * kPdRing;
+    uint8_t* ring = smem + warp * (kPdStages * kPdStage);
     const uint32_t ring32 = ptx::smem_u32(ring);
     // Loads: this warp's blocks are warp, warp + 4, ... of the CTA's; load number k goes to
-    // stage k % kStages, and one stage is free while a block is worked on.
+    // stage k % kPdStages, and one stage is free while a block is worked on.
     // The rows of the next two are fetched ahead: a page's number takes as long as its rows.
-    Walker ld = cur;
+    Walker<B> ld = cur;
     int ld_at = warp, row_at = warp;      // the next load, the next row to fetch
     if (row_at < count) ld.advance(A, warp);
     auto next_row = [&]() {
-        if (row_at >= count) return -1;
-        const int row = block_row(A, ld.s, ld.h, ld.v.block(ld.i));
+        if (row_at >= count) return make_int2(-1, -1);
+        const int2 row = block_rows<B>(A, ld.s, ld.h, ld.v.block(ld.i));
         row_at += kPdWarps;
         if (row_at < count) ld.advance(A, kPdWarps);
         return row;
     };
-    int rows[2];
+    int2 rows[2];
     rows[0] = next_row();
     rows[1] = next_row();
     int ld_stage = 0;
@@ -392,19 +417,27 @@ __global__ void __launch_bounds__(kPdThreads, kPdCtasPerSm) paged_decode_kernel(
     auto load_next = [&]() {
         if (ld_at < count && !failed) {
             // Warp-uniform operands: else each TMA instruction moves its own to uniform registers.
-            const int row = ptx::warp_uniform(rows[0]), at = ptx::warp_uniform(ld_stage);
+            const int row = ptx::warp_uniform(rows[0].x), upper = E8 ? ptx::warp_uniform(rows[0].y) : -1,
+                      at = ptx::warp_uniform(ld_stage);
             if (ptx::elect_one()) {
-                srow[warp][at] = row;
-                if (row >= 0 && !(A.fault && warp == 0 && blockIdx.x == 0)) {
-                    uint8_t* dst = ring + at * kStage;
+                srow[warp][at] = make_int2(row, upper);
+                if ((row >= 0 || upper >= 0) && !(A.fault && warp == 0 && blockIdx.x == 0)) {
+                    uint8_t* dst = ring + at * kPdStage;
                     uint64_t* bar = &full[warp][at];
-                    ptx::mbar_arrive_expect_tx(bar, kStage + (E8 ? 2 * kPdBlock * 4 : 0));
-                    ptx::tma_load_2d(dst, &A.kmap, bar, 0, row);
                     if constexpr (E8) {
-                        ptx::tma_load_2d(dst + kPdTile, &A.vmap, bar, 0, row);
-                        ptx::bulk_load(scales[warp][at][0], A.c.k_scales + row, kPdBlock * 4, bar);
-                        ptx::bulk_load(scales[warp][at][1], A.c.v_scales + row, kPdBlock * 4, bar);
+                        constexpr uint32_t kHalfBytes = 2 * (kPdTile + kPdHalf * 4);
+                        auto load = [&](int r, int from) {   // rows from r on, behind `from` slots of the block
+                            ptx::tma_load_2d(dst + from * 128, &A.kmap, bar, 0, r);
+                            ptx::tma_load_2d(dst + 2 * kPdTile + from * 128, &A.vmap, bar, 0, r);
+                            ptx::bulk_load(&scales[warp][at][0][from], A.c.k_scales + r, A.box * 4, bar);
+                            ptx::bulk_load(&scales[warp][at][1][from], A.c.v_scales + r, A.box * 4, bar);
+                        };
+                        ptx::mbar_arrive_expect_tx(bar, row >= 0 && upper >= 0 ? 2 * kHalfBytes : kHalfBytes);
+                        if (row >= 0) load(row, 0);
+                        if (upper >= 0 && A.box == kPdHalf) load(upper, kPdHalf);
                     } else {
+                        ptx::mbar_arrive_expect_tx(bar, kPdStage);
+                        ptx::tma_load_2d(dst, &A.kmap, bar, 0, row);
                         ptx::tma_load_2d(dst + kPdTile, &A.kmap, bar, 64, row);
                         ptx::tma_load_2d(dst + 2 * kPdTile, &A.vmap, bar, 0, row);
                         ptx::tma_load_2d(dst + 3 * kPdTile, &A.vmap, bar, 64, row);
@@ -415,10 +448,10 @@ __global__ void __launch_bounds__(kPdThreads, kPdCtasPerSm) paged_decode_kernel(
             rows[0] = rows[1];
             rows[1] = next_row();
         }
-        ld_stage = ld_stage + 1 == kStages ? 0 : ld_stage + 1;
+        ld_stage = ld_stage + 1 == kPdStages ? 0 : ld_stage + 1;
     };
 #pragma unroll
-    for (int i = 0; i < kStages - 1; ++i) load_next();
+    for (int i = 0; i < kPdStages - 1; ++i) load_next();
     __syncwarp();
 
     int st = 0;               // stage of this warp's next block
@@ -428,40 +461,47 @@ __global__ void __launch_bounds__(kPdThreads, kPdCtasPerSm) paged_decode_kernel(
     while (CL || done < count) {
         // A segment: the CTA's blocks of one pair.
         const int s = cur.s, h = cur.h, i_begin = cur.i;
-        const Visible v = cur.v;
+        const Visible<B> v = cur.v;
         const int len = min(count - done, v.nb - i_begin);
         const bool whole = len == v.nb;
         // The group's query rows as the upper half of the tile's row operand: head lane / 4.
-        uint32_t qa[8][2];
-        float sl2 = A.sl2;             // with E8 also what the row was divided by
+        uint32_t qa[8][2];             // E8: the lower half of it holds what the first numbers left
+        uint32_t q3[kThird ? 8 : 1];   // ... and what these left
+        float sl2 = A.sl2;             // E8: also what the row was divided by; NaN for one that holds NaN or infinities
         if constexpr (E8) {
-            // Columns 16 kk + 4 (lane % 4) on, in the order in which a key's bytes lie in a lane's word.
+            // Columns 16 kk + 4 (lane % 4) and three more.
             const int j = lane >> 2;
             const uint2* qr =
                 reinterpret_cast<const uint2*>(A.io.q + ((size_t)s * Hq + (size_t)h * g + (j < g ? j : 0)) * kHeadDim) + (lane & 3);
+            uint2 w[8];
+            uint32_t top = 0u;         // magnitudes compare as integers, NaN the largest
 #pragma unroll
             for (int kk = 0; kk < 8; ++kk) {
-                const uint2 w = j < g ? __ldg(qr + 4 * kk) : make_uint2(0u, 0u);
-                qa[kk][0] = w.x;
-                qa[kk][1] = w.y;
+                w[kk] = j < g ? __ldg(qr + 4 * kk) : make_uint2(0u, 0u);
+                const float2 a = Half16<T>::unpack(w[kk].x), b = Half16<T>::unpack(w[kk].y);
+                top = max(max(top, __float_as_uint(fabsf(a.x))), __float_as_uint(fabsf(a.y)));
+                top = max(max(top, __float_as_uint(fabsf(b.x))), __float_as_uint(fabsf(b.y)));
             }
-            if constexpr (!std::is_same_v<T, __half>) {
-                float top = 0.f;       // of the finite ones
+            top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
+            top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
+            const float up = to_range<7>(__uint_as_float(top));
+            sl2 = __uint_as_float(top) < INFINITY ? sl2 * inverse_power(up) : __uint_as_float(0x7fc00000u);
 #pragma unroll
-                for (int kk = 0; kk < 16; ++kk) {
-                    const float2 f = Half16<T>::unpack(qa[kk >> 1][kk & 1]);
-                    top = fabsf(f.x) < INFINITY ? fmaxf(top, fabsf(f.x)) : top;
-                    top = fabsf(f.y) < INFINITY ? fmaxf(top, fabsf(f.y)) : top;
-                }
-                top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
-                top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
-                const float up = to_fp16_range(top);
-                sl2 *= inverse_power(up);
-#pragma unroll
-                for (int kk = 0; kk < 16; ++kk) {
-                    const float2 f = Half16<T>::unpack(qa[kk >> 1][kk & 1]);
-                    qa[kk >> 1][kk & 1] = Half16<__half>::pack(f.x * up, f.y * up);
-                }
+            for (int kk = 0; kk < 8; ++kk) {
+                const float2 a = Half16<T>::unpack(w[kk].x), b = Half16<T>::unpack(w[kk].y);
+                float f[4] = {a.x * up, a.y * up, b.x * up, b.y * up};
+                auto part = [&]() {    // the nearest numbers; f becomes sixteen times what they leave
+                    const uint32_t n = pack_e4m3(f[0], f[1]) | pack_e4m3(f[2], f[3]) << 16;
+                    const float2 x = Half16<__half>::unpack(e4m3_to_half2(n)), y = Half16<__half>::unpack(e4m3_to_half2_upper(n));
+                    f[0] = (f[0] - x.x) * 16.f;
+                    f[1] = (f[1] - x.y) * 16.f;
+                    f[2] = (f[2] - y.x) * 16.f;
+                    f[3] = (f[3] - y.y) * 16.f;
+                    return n;
+                };
+                qa[kk][0] = part();
+                qa[kk][1] = part();
+                if constexpr (kThird) q3[kk] = part();
             }
         } else {
             const int j = lane >> 2;
@@ -474,21 +514,25 @@ __global__ void __launch_bounds__(kPdThreads, kPdCtasPerSm) paged_decode_kernel(
                 qa[kk][1] = j < g ? __ldg(qr + 8 * kk + 4) : 0u;
             }
         }
-        float acc[16][4];
+        // Head lane / 4, hi and lo.  E8: a column a head (2 (lane % 4) and the next), a row a dimension: the weights are
+        // the column operand, as which their tile needs no second half, and hi and lo meet in one sum.
+        constexpr int kAcc = E8 ? 8 : 16;
+        float acc[kAcc][4];
 #pragma unroll
-        for (int d = 0; d < 16; ++d)
+        for (int d = 0; d < kAcc; ++d)
 #pragma unroll
             for (int c = 0; c < 4; ++c) acc[d][c] = 0.f;
         float m = kNoLogit, l = 0.f;   // head lane / 4; l of this lane's slots
-        float up = to_fp16_range(0.f); // E8: acc is this times the sums
+        float up = to_range<14>(0.f);  // E8: acc is this times the sums
         // The warp's first block of the segment: its blocks are warp mod kPdWarps of the CTA's.
         const int skip = (warp - done % kPdWarps + kPdWarps) % kPdWarps;
         for (int e = skip; e < len; e += kPdWarps) {
             const int i = i_begin + e, b = v.block(i);
             __syncwarp();
-            const int row = srow[warp][st];
-            const uint32_t src = ring32 + st * kStage;
-            float x[2][4];
+            const int2 rows_at = srow[warp][st];
+            const int row = max(rows_at.x, rows_at.y);   // -1: nothing is there
+            const uint32_t src = ring32 + st * kPdStage;
+            float x[B / 8][4];
             if (row >= 0) {
                 if (!failed && !__all_sync(0xffffffffu, ptx::mbar_wait(&full[warp][st], (phases >> st) & 1u))) {
                     failed = true;
@@ -496,26 +540,35 @@ __global__ void __launch_bounds__(kPdThreads, kPdCtasPerSm) paged_decode_kernel(
                 }
                 if (!failed) phases ^= 1u << st;   // the parities stay those of copies in flight
 #pragma unroll
-                for (int t = 0; t < 2; ++t)
+                for (int t = 0; t < B / 8; ++t)
 #pragma unroll
                     for (int c = 0; c < 4; ++c) x[t][c] = 0.f;
-                // Logits: key row (lane & 7) + 8 (lane / 16), columns 16 kk + 8 (lane / 8 % 2).
-                const int kr = (lane & 7) + ((lane >> 4) << 3);
                 if constexpr (E8) {
-                    // Bytes 16 c + 4 (lane % 4) on of key row lane / 4 (+ 8): the lower two meet the tile's lower columns.
+                    // Eight keys at a time: chunks 4 cc + lane / 8 of row lane % 8, two of them a product.
+                    const int kr = lane & 7;
 #pragma unroll
-                    for (int kk = 0; kk < 4; ++kk) {
-                        uint32_t kb[4];
-                        const int chunk = 2 * kk + ((lane >> 3) & 1);
-                        ldmatrix_x4(src + kr * 128 + ((chunk ^ (kr & 7)) << 4), kb);
+                    for (int t = 0; t < B / 8; ++t) {
+                        float y[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-                        for (int c = 0; c < 2; ++c)
+                        for (int cc = 0; cc < 2; ++cc) {
+                            uint32_t kb[4];
+                            ldmatrix_x4(src + (8 * t + kr) * 128 + (((4 * cc + (lane >> 3)) ^ kr) << 4), kb);
 #pragma unroll
-                            for (int t = 0; t < 2; ++t)
-                                Half16<Operand>::mma(x[t], qa[2 * kk + c][0], 0u, qa[2 * kk + c][1], 0u, e4m3_to_half2(kb[2 * t + c]),
-                                               e4m3_to_half2_upper(kb[2 * t + c]));
+                            for (int c = 0; c < 2; ++c) {
+                                const int kk = 4 * cc + 2 * c;
+                                mma_e4m3(x[t], qa[kk][0], qa[kk][1], qa[kk + 1][0], qa[kk + 1][1], kb[2 * c], kb[2 * c + 1]);
+                                if constexpr (kThird) mma_e4m3(y, q3[kk], 0u, q3[kk + 1], 0u, kb[2 * c], kb[2 * c + 1]);
+                            }
+                        }
+#pragma unroll
+                        for (int c = 0; c < 2; ++c) {
+                            x[t][c] = fmaf(x[t][2 + c], 1.f / 16.f, x[t][c]);
+                            if constexpr (kThird) x[t][c] = fmaf(y[c], 1.f / 256.f, x[t][c]);
+                        }
                     }
                 } else {
+                    // Logits: key row (lane & 7) + 8 (lane / 16), columns 16 kk + 8 (lane / 8 % 2).
+                    const int kr = (lane & 7) + ((lane >> 4) << 3);
 #pragma unroll
                     for (int kk = 0; kk < 8; ++kk) {
                         uint32_t kb[4];
@@ -527,60 +580,82 @@ __global__ void __launch_bounds__(kPdThreads, kPdCtasPerSm) paged_decode_kernel(
                 }
             }
             // This lane's slots: 8 t + 2 (lane % 4) + c.
-            const bool all = row >= 0 && v.whole(b);
-            float vs[2][2];           // E8: the values' scales, 0 where no one sees them
+            const bool here[2] = {rows_at.x >= 0, rows_at.y >= 0};       // by halves
+            const bool all = here[0] && (!E8 || here[1]) && v.whole(b);
+            float vs[E8 ? B / 8 : 1][2];   // the values' scales, 0 where no one sees them
+            if constexpr (E8) {
 #pragma unroll
-            for (int t = 0; t < 2; ++t) {
-                float2 ks2 = make_float2(1.f, 1.f), vs2 = ks2;
-                if constexpr (E8) {
-                    if (row >= 0) {
-                        ks2 = *reinterpret_cast<const float2*>(&scales[warp][st][0][8 * t + 2 * (lane & 3)]);
-                        vs2 = *reinterpret_cast<const float2*>(&scales[warp][st][1][8 * t + 2 * (lane & 3)]);
-                    }
+                for (int t = 0; t < B / 8; ++t) {
+                    const float2 ks2 = *reinterpret_cast<const float2*>(&scales[warp][st][0][8 * t + 2 * (lane & 3)]);
+                    const float2 vs2 = *reinterpret_cast<const float2*>(&scales[warp][st][1][8 * t + 2 * (lane & 3)]);
+                    x[t][0] *= sl2 * ks2.x;
+                    x[t][1] *= sl2 * ks2.y;
+                    vs[t][0] = vs2.x;
+                    vs[t][1] = vs2.y;
                 }
+                if (!all) {   // most blocks are seen wholly
 #pragma unroll
-                for (int c = 0; c < 2; ++c) {
-                    const int slot = b * kPdBlock + 8 * t + 2 * (lane & 3) + c;
-                    const bool seen = all || (row >= 0 && v.sees(slot));
-                    x[t][c] = seen ? x[t][c] * (E8 ? sl2 * (c ? ks2.y : ks2.x) : sl2) : -INFINITY;
-                    vs[t][c] = seen ? (c ? vs2.y : vs2.x) : 0.f;
+                    for (int t = 0; t < B / 8; ++t)
+#pragma unroll
+                        for (int c = 0; c < 2; ++c) {
+                            const bool seen = here[t / 2] && v.sees(b * B + 8 * t + 2 * (lane & 3) + c);
+                            x[t][c] = seen ? x[t][c] : -INFINITY;
+                            vs[t][c] = seen ? vs[t][c] : 0.f;
+                        }
                 }
+            } else {
+#pragma unroll
+                for (int t = 0; t < B / 8; ++t)
+#pragma unroll
+                    for (int c = 0; c < 2; ++c)
+                        x[t][c] = all || (here[0] && v.sees(b * B + 8 * t + 2 * (lane & 3) + c)) ? x[t][c] * sl2 : -INFINITY;
             }
             if (A.c.weights && (lane >> 2) < g) {
-                float* lg = A.logits + (((size_t)s * Hkv + h) * A.nbmax + i) * (size_t)(g * kPdBlock) +
-                            (lane >> 2) * kPdBlock + 2 * (lane & 3);
-                *reinterpret_cast<float2*>(lg) = make_float2(x[0][0], x[0][1]);
-                *reinterpret_cast<float2*>(lg + 8) = make_float2(x[1][0], x[1][1]);
+                float* lg = A.logits + (((size_t)s * Hkv + h) * A.nbmax + i) * (size_t)(g * B) + (lane >> 2) * B + 2 * (lane & 3);
+#pragma unroll
+                for (int t = 0; t < B / 8; ++t) *reinterpret_cast<float2*>(lg + 8 * t) = make_float2(x[t][0], x[t][1]);
             }
             if (row >= 0) {
                 if (!all) {
                     // Values that no one sees may be anything: zeros meet the weights of zero.
-                    for (int r = 0; r < kPdBlock; ++r)
-                        if (!v.sees(b * kPdBlock + r) && lane < (E8 ? 8 : 16))
-                            ptx::st_shared_v4(src + (E8 ? 1 : 2 + (lane >> 3)) * kPdTile + r * 128 + ((lane & 7) << 4), 0u, 0u, 0u, 0u);
+                    for (int r = 0; r < B; ++r)
+                        if (!(here[r / kPdHalf] && v.sees(b * B + r)) && lane < (E8 ? 8 : 16))
+                            ptx::st_shared_v4(src + (2 + (E8 ? 0 : lane >> 3)) * kPdTile + r * 128 + ((lane & 7) << 4), 0u, 0u, 0u, 0u);
                     ptx::fence_proxy_async_smem();   // before the stage's next TMA load
                     __syncwarp();
                 }
-                float t = fmaxf(fmaxf(x[0][0], x[0][1]), fmaxf(x[1][0], x[1][1]));
+                float t = fmaxf(x[0][0], x[0][1]);
+#pragma unroll
+                for (int k = 1; k < B / 8; ++k) t = fmaxf(t, fmaxf(x[k][0], x[k][1]));
                 t = fmaxf(t, __shfl_xor_sync(0xffffffffu, t, 1));
                 t = fmaxf(t, __shfl_xor_sync(0xffffffffu, t, 2));
                 const float mn = fmaxf(m, t);
+                bool unbounded = false;   // E8: a scale is infinite or NaN
                 if constexpr (E8) {
-                    // The block's largest finite scale, the same for every lane, may lower the power of two.
-                    float top = 0.f;
+                    // The block's largest scale, the same for every lane, may lower the power of two.  (Magnitudes compare
+                    // as integers, infinities and NaN as the largest.)
+                    uint32_t top = 0u;
 #pragma unroll
-                    for (int k = 0; k < 4; ++k) {
-                        const float a = fabsf(vs[k >> 1][k & 1]);
-                        top = a < INFINITY ? fmaxf(top, a) : top;
+                    for (int k = 0; k < B / 4; ++k) top = max(top, __float_as_uint(fabsf(vs[k >> 1][k & 1])));
+                    top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
+                    top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
+                    unbounded = top >= 0x7f800000u;
+                    if (unbounded) {   // the largest finite one
+                        top = 0u;
+#pragma unroll
+                        for (int k = 0; k < B / 4; ++k) {
+                            const uint32_t a = __float_as_uint(fabsf(vs[k >> 1][k & 1]));
+                            top = a < 0x7f800000u ? max(top, a) : top;
+                        }
+                        top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
+                        top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
                     }
-                    top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
-                    top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
-                    const float to = to_fp16_range(top);
+                    const float to = to_range<14>(__uint_as_float(top));
                     if (to < up) {
                         const float down = to * inverse_power(up);
                         up = to;
 #pragma unroll
-                        for (int d = 0; d < 16; ++d)
+                        for (int d = 0; d < kAcc; ++d)
 #pragma unroll
                             for (int c = 0; c < 4; ++c) acc[d][c] *= down;
                     }
@@ -589,14 +664,17 @@ __global__ void __launch_bounds__(kPdThreads, kPdCtasPerSm) paged_decode_kernel(
                     const float corr = ptx::ex2(m - mn);   // 0 from kNoLogit on
                     l *= corr;
                     m = mn;
+                    // (E8: those of the lane's columns)
+                    const float c0 = E8 ? __shfl_sync(0xffffffffu, corr, (lane & 3) * 8) : corr;
+                    const float c1 = E8 ? __shfl_sync(0xffffffffu, corr, (lane & 3) * 8 + 4) : corr;
 #pragma unroll
-                    for (int d = 0; d < 16; ++d)
+                    for (int d = 0; d < kAcc; ++d)
 #pragma unroll
-                        for (int c = 0; c < 4; ++c) acc[d][c] *= corr;
+                        for (int c = 0; c < 4; ++c) acc[d][c] *= c & 1 ? c1 : c0;
                 }
-                uint32_t hi[2], lo[2];
+                uint32_t hi[B / 8], lo[B / 8];
 #pragma unroll
-                for (int t2 = 0; t2 < 2; ++t2) {
+                for (int t2 = 0; t2 < B / 8; ++t2) {
                     float p0 = ptx::ex2(x[t2][0] - m), p1 = ptx::ex2(x[t2][1] - m);
                     l += p0 + p1;
                     if constexpr (E8) {
@@ -606,24 +684,29 @@ __global__ void __launch_bounds__(kPdThreads, kPdCtasPerSm) paged_decode_kernel(
                     hi[t2] = Half16<Operand>::pack(p0, p1);
                     const float2 r = Half16<Operand>::unpack(hi[t2]);
                     lo[t2] = Half16<Operand>::pack(p0 - r.x, p1 - r.y);
+                    if (E8 && unbounded)   // an infinite weight leaves no rest, where infinity less infinity gave NaN
+                        lo[t2] &= (fabsf(r.x) < INFINITY ? 0xffffu : 0u) | (fabsf(r.y) < INFINITY ? 0xffff0000u : 0u);
                 }
                 // Values: row (lane & 7) + 8 (lane / 8 % 2), columns 16 dd + 8 (lane / 16).
                 const int vr = (lane & 7) + (((lane >> 3) & 1) << 3);
                 if constexpr (E8) {
-                    // A word holds two slots' columns 2 n and 2 n + 1: a tile of the even columns, one of the odd.
+                    // A word holds two slots' columns 2 n and 2 n + 1, n = lane / 4: rows n and n + 8 of a chunk's tile.
 #pragma unroll
-                    for (int dd = 0; dd < 4; ++dd) {
-                        uint32_t vb[4];
-                        const int chunk = 2 * dd + (lane >> 4);
-                        ldmatrix_x4_trans(src + kPdTile + vr * 128 + ((chunk ^ (vr & 7)) << 4), vb);
+                    for (int dd = 0; dd < 4; ++dd)
 #pragma unroll
-                        for (int c = 0; c < 2; ++c) {
-                            const uint32_t a = __byte_perm(vb[2 * c], 0u, 0x3120), b8 = __byte_perm(vb[2 * c + 1], 0u, 0x3120);
-                            Half16<Operand>::mma(acc[4 * dd + 2 * c], hi[0], lo[0], hi[1], lo[1], e4m3_to_half2(a), e4m3_to_half2(b8));
-                            Half16<Operand>::mma(acc[4 * dd + 2 * c + 1], hi[0], lo[0], hi[1], lo[1], e4m3_to_half2_upper(a),
-                                           e4m3_to_half2_upper(b8));
+                        for (int half = 0; half < 2; ++half) {
+                            uint32_t vb[4];
+                            const int chunk = 2 * dd + (lane >> 4);
+                            ldmatrix_x4_trans(src + (2 + half) * kPdTile + vr * 128 + ((chunk ^ (vr & 7)) << 4), vb);
+#pragma unroll
+                            for (int c = 0; c < 2; ++c) {
+                                uint32_t a[4];
+#pragma unroll
+                                for (int e = 0; e < 4; ++e) a[e] = e4m3_to_half2(__byte_perm(vb[2 * c + (e >> 1)], 0u, e & 1 ? 0x4431 : 0x4420));
+                                Half16<Operand>::mma(acc[2 * dd + c], a[0], a[1], a[2], a[3], hi[2 * half], hi[2 * half + 1]);
+                                Half16<Operand>::mma(acc[2 * dd + c], a[0], a[1], a[2], a[3], lo[2 * half], lo[2 * half + 1]);
+                            }
                         }
-                    }
                 } else {
 #pragma unroll
                     for (int dd = 0; dd < 8; ++dd) {
@@ -636,13 +719,13 @@ __global__ void __launch_bounds__(kPdThreads, kPdCtasPerSm) paged_decode_kernel(
                 }
             }
             __syncwarp();   // every lane is done with the stage's tiles and row
-            st = st + 1 == kStages ? 0 : st + 1;
+            st = st + 1 == kPdStages ? 0 : st + 1;
             load_next();    // into the stage that the step before freed; this step's is free now
         }
         // The warp's (maximum, sum, outputs), in its free stage: the one before st.
         l += __shfl_xor_sync(0xffffffffu, l, 1);
         l += __shfl_xor_sync(0xffffffffu, l, 2);
-        float* mine = reinterpret_cast<float*>(ring + (st == 0 ? kStages - 1 : st - 1) * kStage);
+        float* mine = reinterpret_cast<float*>(ring + (st == 0 ? kPdStages - 1 : st - 1) * kPdStage);
         {
             const int j = lane >> 2;
             if ((lane & 3) == 0) {
@@ -653,10 +736,11 @@ __global__ void __launch_bounds__(kPdThreads, kPdCtasPerSm) paged_decode_kernel(
             if constexpr (E8) {
                 const float down = inverse_power(up);
 #pragma unroll
-                for (int d = 0; d < 16; d += 2)
-                    *reinterpret_cast<float4*>(mine + j * kHeadDim + d * 8 + 4 * (lane & 3)) =
-                        make_float4(with_rest(acc[d][0], acc[d][2]) * down, with_rest(acc[d + 1][0], acc[d + 1][2]) * down,
-                                    with_rest(acc[d][1], acc[d][3]) * down, with_rest(acc[d + 1][1], acc[d + 1][3]) * down);
+                for (int d = 0; d < kAcc; ++d) {
+                    float* const to = mine + (lane & 3) * 2 * kHeadDim + d * 16 + 2 * j;   // j = lane / 4
+                    *reinterpret_cast<float2*>(to) = make_float2(acc[d][0] * down, acc[d][2] * down);
+                    *reinterpret_cast<float2*>(to + kHeadDim) = make_float2(acc[d][1] * down, acc[d][3] * down);
+                }
             } else {
 #pragma unroll
                 for (int d = 0; d < 16; ++d)
@@ -705,10 +789,10 @@ __global__ void __launch_bounds__(kPdThreads, kPdCtasPerSm) paged_decode_kernel(
         ptx::fence_proxy_async_smem();   // the outputs lay where the next load goes
         __syncthreads();
         if constexpr (CL) {
-            // A CTA of a cluster has 32 blocks at most, a quarter a thread, read while the cluster meets.
-            SlotWeights sw;
+            // A CTA of a cluster has 512 slots at most, four a thread, read while the cluster meets.
+            SlotWeights<B> sw;
             sw.row = -1;
-            if (A.c.weights && tid < len * 4) sw.load(A, s, h, v, i_begin, tid);
+            if (A.c.weights && tid < len * (B / 4)) sw.load(A, s, h, v, i_begin, tid);
             if (splits > 1) {
                 cg::cluster_group cluster = cg::this_cluster();
                 cluster.sync();
@@ -751,7 +835,7 @@ __global__ void __launch_bounds__(kPdThreads, kPdCtasPerSm) paged_decode_kernel(
             break;
         }
         if (A.c.weights && whole) {
-            add_weights<kPdThreads>(A, s, h, v, i_begin, i_begin + len, fm, finv);
+            add_weights<kPdThreads, B>(A, s, h, v, i_begin, i_begin + len, fm, finv);
             __syncthreads();      // before the next segment's fm and finv
         }
         done += len;
@@ -762,24 +846,24 @@ __global__ void __launch_bounds__(kPdThreads, kPdCtasPerSm) paged_decode_kernel(
     if constexpr (PRE) asm volatile("griddepcontrol.wait;\n" ::: "memory");
     // Copies in flight land before the CTA may exit (a stage without one runs into the limit).
     if (failed)
-        for (int i = 0; i < kStages; ++i) ptx::mbar_wait(&full[warp][i], (phases >> i) & 1u, 20000000ull);
+        for (int i = 0; i < kPdStages; ++i) ptx::mbar_wait(&full[warp][i], (phases >> i) & 1u, 20000000ull);
 }
 
 // The pairs whose blocks several CTAs share.  Block x = 0 of (x, h, s) joins the outputs, a warp a query head, the
 // others add the weights, kJoinRows slots each.  (A lane finds a share's place and sums, and eight shares' outputs are
 // read at once: one thread in a loop over the 38 shares of 131072 slots took 58 us.  Six blocks resident on an
 // SM: eight spill, 64 rows take the same but a window of 4096 in 16 caches 55.5 us instead of 53.6.)
-template <class T, bool PRE>
+template <class T, int B, bool PRE>
 __global__ void __launch_bounds__(kJoinThreads, 6) paged_join_kernel(const __grid_constant__ PdArgs A) {
     extern __shared__ float2 share[];                 // [shares][kPdHeads] (place as an int, maximum)
     __shared__ float fm[kPdHeads], finv[kPdHeads];
     const int h = blockIdx.y, s = blockIdx.z, lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = A.g;
-    Visible v;
+    Visible<B> v;
     v.init(A, s);
     const bool weights = blockIdx.x > 0;
-    const int i0 = ((int)blockIdx.x - 1) * (kJoinRows / kPdBlock);
+    const int i0 = ((int)blockIdx.x - 1) * (kJoinRows / B);
     // The lengths were complete before the kernel that this one waits for began.
-    List list;
+    List<B> list;
     list.init(A);
     // Nothing to join: nothing is seen, finished by its CTA, or a block of slots that the sequence does not have.
     bool done = v.nb == 0 || list.whole_pairs(A) || i0 >= v.nb;
@@ -787,7 +871,7 @@ __global__ void __launch_bounds__(kJoinThreads, 6) paged_join_kernel(const __gri
     long long p0 = 0;
     int c0 = 0, c1 = 0;
     if (!done) {
-        p0 = list.places_before(A, s) + (long long)h * List::places(v);
+        p0 = list.places_before(A, s) + (long long)h * List<B>::places(v);
         c0 = (int)quotient((p0 + kPairCost + 1) * A.ctas - 1, total);
         c1 = (int)quotient((p0 + kPairCost + v.nb) * A.ctas - 1, total);
         done = c0 == c1;
@@ -867,7 +951,7 @@ __global__ void __launch_bounds__(kJoinThreads, 6) paged_join_kernel(const __gri
     }
     if (!weights) return;
     __syncthreads();
-    add_weights<kJoinThreads>(A, s, h, v, i0, min(v.nb, i0 + kJoinRows / kPdBlock), fm, finv);
+    add_weights<kJoinThreads, B>(A, s, h, v, i0, min(v.nb, i0 + kJoinRows / B), fm, finv);
 }
 
 size_t round16(size_t x) { return (x + 15) & ~size_t(15); }
@@ -876,6 +960,7 @@ int share_ctas(int num_sms) { return kPdCtasPerSm * num_sms; }
 
 template <class T, bool E8, bool PRE>
 cudaError_t launch_typed(const PdArgs& a, cudaStream_t st) {
+    constexpr int B = kPdBlock<E8>;
     // CTAs of a pair: the largest cluster that fits the device's resident CTAs in one wave, with
     // two blocks a warp and more; taken where that leaves a CTA 32 blocks and less (a quarter of
     // one a thread for the weights), else the list of all blocks.  Measured with weights, 8 KV
@@ -885,7 +970,7 @@ cudaError_t launch_typed(const PdArgs& a, cudaStream_t st) {
     const int pairs = a.io.batch * a.io.Hkv;
     int splits = 1;
     while (splits < kPdMaxCluster && (long long)pairs * splits * 2 <= a.ctas && a.nbmax >= kPdWarps * 2 * splits) splits *= 2;
-    if (a.nbmax <= 8 * kPdWarps * splits) {
+    if (a.nbmax * (B / 4) <= kPdThreads * splits) {
         cudaLaunchConfig_t cfg = {};
         cfg.gridDim = dim3(splits, a.io.Hkv, a.io.batch);
         cfg.blockDim = dim3(kPdThreads);
@@ -904,26 +989,27 @@ cudaError_t launch_typed(const PdArgs& a, cudaStream_t st) {
     }
     cudaError_t e = launch_prio(paged_decode_kernel<T, false, E8, PRE>, dim3(a.ctas), dim3(kPdThreads), kPdSmem, st, 0, true, a);
     if (e != cudaSuccess) return e;
-    const int rows = a.c.weights ? (a.nbmax * kPdBlock + kJoinRows - 1) / kJoinRows : 0;
-    return launch_prio(paged_join_kernel<T, PRE>, dim3(1 + rows, a.io.Hkv, a.io.batch), dim3(kJoinThreads),
+    const int rows = a.c.weights ? (a.nbmax * B + kJoinRows - 1) / kJoinRows : 0;
+    return launch_prio(paged_join_kernel<T, B, PRE>, dim3(1 + rows, a.io.Hkv, a.io.batch), dim3(kJoinThreads),
                        a.ctas * kPdHeads * sizeof(float2), st, 0, true, a);
 }
 
-// Most blocks that a sequence of up to max_len slots has in sight.
-int visible_blocks(int max_len, int window, int sinks) {
-    const int all = (max_len + kPdBlock - 1) / kPdBlock;
+// Most blocks of B slots that a sequence of up to max_len slots has in sight.
+int visible_blocks(int B, int max_len, int window, int sinks) {
+    const int all = (max_len + B - 1) / B;
     if (!window) return all;
     // A window ends and begins inside a block.
-    const long long some = (long long)window / kPdBlock + 2 + (std::min(sinks, max_len) + kPdBlock - 1) / kPdBlock;
+    const long long some = (long long)window / B + 2 + (std::min(sinks, max_len) + B - 1) / B;
     return (int)std::min<long long>(all, some);
 }
 
 }  // namespace
 
-size_t paged_decode_scratch(int batch, int Hq, int max_len, int window, int sinks, bool weights, int num_sms) {
+size_t paged_decode_scratch(int batch, int Hq, int max_len, int window, int sinks, bool weights, bool e8, int num_sms) {
+    const int B = e8 ? kPdBlock<true> : kPdBlock<false>;
     const size_t slots = (size_t)share_ctas(num_sms) * 2 * kPdHeads;
     size_t b = round16(slots * kHeadDim * sizeof(float)) + round16(slots * sizeof(float2));
-    if (weights) b += (size_t)batch * Hq * visible_blocks(max_len, window, sinks) * kPdBlock * sizeof(float);
+    if (weights) b += (size_t)batch * Hq * visible_blocks(B, max_len, window, sinks) * B * sizeof(float);
     return b;
 }
 
@@ -952,7 +1038,8 @@ cudaError_t launch_paged_decode(const PagedDecodeIO& io, const PagedCacheView& c
     const bool e8 = c.k_scales != nullptr;
     const uint64_t dims[2] = {(uint64_t)(e8 ? kHeadDim / 2 : kHeadDim), ((uint64_t)c.num_pages * io.Hkv) << c.log_page};
     const uint64_t strides[1] = {dims[0] * 2};
-    const uint32_t box[2] = {64, (uint32_t)kPdBlock};
+    a.box = e8 && c.log_page >= 5 ? kPdBlock<true> : kPdHalf;
+    const uint32_t box[2] = {64, (uint32_t)a.box};
     cudaError_t e = encode_tensor_map(&a.kmap, c.dtype, 2, c.k, dims, strides, box);
     if (e == cudaSuccess) e = encode_tensor_map(&a.vmap, c.dtype, 2, c.v, dims, strides, box);
     if (e != cudaSuccess) return e;
@@ -964,7 +1051,7 @@ cudaError_t launch_paged_decode(const PagedDecodeIO& io, const PagedCacheView& c
     a.ctas = share_ctas(num_sms);
     const long long pairs = (long long)io.batch * io.Hkv;
     a.pairs = pairs <= a.ctas && pairs * 4 >= a.ctas * 3ll ? (int)pairs : 0;
-    a.nbmax = visible_blocks(io.max_len, io.window, io.sinks);
+    a.nbmax = visible_blocks(e8 ? kPdBlock<true> : kPdBlock<false>, io.max_len, io.window, io.sinks);
     const size_t slots = (size_t)a.ctas * 2 * kPdHeads;
     char* p = static_cast<char*>(io.scratch);
     a.part_o = reinterpret_cast<float*>(p);

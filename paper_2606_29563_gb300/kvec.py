@@ -33,7 +33,7 @@ EXPORTED = ("kvec_create", "kvec_destroy", "kvec_state_bytes", "kvec_reset", "kv
             "kvec_rotate_append", "kvec_paged_decode_bytes", "kvec_paged_decode_window_bytes", "kvec_paged_decode",
             "kvec_paged_evict", "kvec_prefill_bytes", "kvec_prefill_attention", "kvec_rotate_append_quant",
             "kvec_paged_decode_quant", "kvec_paged_evict_quant", "kvec_paged_read", "kvec_shared_decode_bytes",
-            "kvec_shared_decode")
+            "kvec_shared_decode", "kvec_paged_decode_quant_bytes")
 
 KVEC_BF16 = 0
 KVEC_FP16 = 1
@@ -155,6 +155,7 @@ def load() -> ctypes.CDLL:
                                          i, i, i, _vp, _vp, ctypes.c_size_t, _vp], st),
             "kvec_paged_evict_quant": ([_vp, i, ctypes.POINTER(kvec_paged_cache), ctypes.POINTER(kvec_paged_scales), _vp,
                                         i, i, i, i, i, _vp, _vp, _vp], st),
+            "kvec_paged_decode_quant_bytes": ([_vp, i, i, i, i, i], ctypes.c_size_t),
             "kvec_shared_decode_bytes": ([_vp, i, i, i], ctypes.c_size_t),
             "kvec_shared_decode": ([_vp, i, _vp, ctypes.POINTER(kvec_paged_cache), ctypes.POINTER(kvec_shared_prefix), i, i,
                                     _vp, _vp, ctypes.c_size_t, _vp], st),
@@ -284,6 +285,10 @@ def kvec_paged_evict(handle: int, batch: int, cache: kvec_paged_cache, new_table
                      budget: int, sinks: int, recent: int, new_lens: int, kept: int, stream: int = 0) -> None:
     _check(load().kvec_paged_evict(handle, batch, cache, new_table, new_max_pages, max_len, budget, sinks, recent,
                                    new_lens, kept, stream))
+
+
+def kvec_paged_decode_quant_bytes(handle: int, batch: int, max_len: int, window: int, sinks: int, with_weights: bool) -> int:
+    return int(load().kvec_paged_decode_quant_bytes(handle, batch, max_len, window, sinks, 1 if with_weights else 0))
 
 
 def kvec_shared_decode_bytes(handle: int, batch: int, max_len: int, with_weights: bool) -> int:
@@ -478,7 +483,7 @@ class KvecSelector:
         self.device = torch.device("cuda", torch.cuda.current_device())
         self._current = torch._C._cuda_getCurrentRawStream   # torch.cuda.current_stream makes an object, 2 us
         self._lib = load()
-        self._decode_bytes = {}      # kvec_paged_decode_window_bytes and kvec_shared_decode_bytes by their sizes
+        self._decode_bytes = {}      # the bytes of scratch by function and sizes
         self.state_bytes = kvec_state_bytes(params.max_seqlen)
 
     def close(self) -> None:
@@ -666,12 +671,11 @@ class KvecSelector:
         return (q_out, k_out) if want_k else q_out
 
     def _scratch_bytes(self, of, *sizes):
-        # (Calls of different kinds have a different number of sizes.)
-        need = self._decode_bytes.get(sizes)
+        need = self._decode_bytes.get((of, sizes))
         if need is None:
             if len(self._decode_bytes) >= 256:   # a loop's bounds may grow with every step
                 self._decode_bytes.clear()
-            need = self._decode_bytes[sizes] = of(self.handle, *sizes)
+            need = self._decode_bytes[of, sizes] = of(self.handle, *sizes)
         return need
 
     def paged_decode(self, q, cache, max_len: Optional[int] = None, window: int = 0, sinks: int = 0, out=None,
@@ -695,7 +699,8 @@ class KvecSelector:
             max_len = cache.capacity
         if (max_len | window | sinks) >> 31:   # ctypes would pass their lower 32 bits
             raise KvecError(KVEC_ERR_INVALID_ARG, "max_len, window and sinks must be in [0, 2^31)")
-        need = self._scratch_bytes(kvec_paged_decode_window_bytes, batch, max_len, window, sinks, cache.weights is not None)
+        need = self._scratch_bytes(kvec_paged_decode_quant_bytes if cache.eight else kvec_paged_decode_window_bytes, batch,
+                                   max_len, window, sinks, cache.weights is not None)
         scratch = self._empty(max(need, 16), self._torch.uint8, stream)
         if cache.eight:
             st = self._lib.kvec_paged_decode_quant(self.handle, batch, q.data_ptr(), cache.c, cache.scales, max_len, window,
