@@ -14,6 +14,8 @@
 // one token a block 556 us).  One token 2.3 us, the launch.  Between: 1600 tokens 9.9 us for 5.9 of bytes, 3200
 // 20.0 (11.8), 6400 32.9 (23.7), 12800 59 (47), as a block's chain of look-ups (sequence, position, length,
 // page) and its table row come before each one or two tokens' rows.
+//
+// A cache of 8 bits has a kernel of its own (below), with eight lanes a row.
 #include "half_types.cuh"
 #include "kvec_internal.cuh"
 
@@ -82,30 +84,8 @@ __device__ __forceinline__ Place place_of(const RotateArgs& A, int t) {
     return p;
 }
 
-// A cache of 8 bits: the row's largest magnitude fills e4m3's range, s = max(max|y| / 448, 2^-126), and y / s is
-// rounded; both divisions are exact to the last bit, as a quotient beside the middle of two e4m3 numbers must fall to
-// its own side.  Magnitudes are compared as integers, by which NaN is the largest: a row that holds one, or an
-// infinity, gets a scale of NaN or infinity and is NaN when it is read.
-constexpr float kMostE4m3 = 448.f, kLeastScale = 1.1754943508222875e-38f;
-
-// Eight values of a row, by the sixteen lanes of a half-warp; the row's scale.
-__device__ __forceinline__ float quantise_row(const float (&y)[8], uint2* out) {
-    uint32_t top = 0u;
-#pragma unroll
-    for (int e = 0; e < 8; ++e) top = max(top, __float_as_uint(y[e]) & 0x7fffffffu);
-#pragma unroll
-    for (int o = 8; o; o >>= 1) top = max(top, __shfl_xor_sync(0xffffffffu, top, o));
-    float s = __fdiv_rn(__uint_as_float(top), kMostE4m3);
-    s = s < kLeastScale ? kLeastScale : s;
-    float z[8];
-#pragma unroll
-    for (int e = 0; e < 8; ++e) z[e] = __fdiv_rn(y[e], s);
-    *out = make_uint2(pack_e4m3(z[0], z[1]) | pack_e4m3(z[2], z[3]) << 16, pack_e4m3(z[4], z[5]) | pack_e4m3(z[6], z[7]) << 16);
-    return s;
-}
-
-// NR: rows of a token that a half-warp takes, NT: tokens of a block.  IL: interleaved pairs.  E8: the cache holds 8 bits.
-template <class T, int NR, int NT, bool IL, bool E8>
+// NR: rows of a token that a half-warp takes, NT: tokens of a block.  IL: interleaved pairs.
+template <class T, int NR, int NT, bool IL>
 __global__ void __launch_bounds__(32 * kRotWarps, 8) rotate_kernel(const __grid_constant__ RotateArgs A) {
     __shared__ Place places[NT];
     const int lane = threadIdx.x & 31, l16 = lane & 15;
@@ -162,9 +142,9 @@ __global__ void __launch_bounds__(32 * kRotWarps, 8) rotate_kernel(const __grid_
             const int u = u0 + i * kRotRows;
             const bool isq = u < Hq, isk = !isq && u < Hq + Hkv;
             uint4 out = x[i];   // a value row is copied as it is
-            float y[8];
             // The half-warps of a warp share the shuffles: both stay, whatever they store.
             if (__any_sync(0xffffffffu, isq || isk)) {
+                float y[8];
                 unpack8<T>(x[i], y);
                 const uint16_t* norm = isq ? io.q_norm : isk ? io.k_norm : nullptr;
                 if (io.q_norm || io.k_norm) {
@@ -201,14 +181,6 @@ __global__ void __launch_bounds__(32 * kRotWarps, 8) rotate_kernel(const __grid_
                     out = make_uint4(Half16<T>::pack(y[0], y[1]), Half16<T>::pack(y[2], y[3]), Half16<T>::pack(y[4], y[5]),
                                      Half16<T>::pack(y[6], y[7]));
             }
-            uint2 bytes;
-            float scale;
-            if constexpr (E8) {
-                if (__any_sync(0xffffffffu, !isq && u < heads)) {
-                    if (!isq && !isk) unpack8<T>(x[i], y);
-                    scale = quantise_row(y, &bytes);
-                }
-            }
             if (u >= heads) continue;
             if (isq) {
                 reinterpret_cast<uint4*>(io.q_out + ((size_t)t * Hq + u) * kHeadDim)[l16] = out;
@@ -218,24 +190,201 @@ __global__ void __launch_bounds__(32 * kRotWarps, 8) rotate_kernel(const __grid_
             if (isk && io.k_out) reinterpret_cast<uint4*>(io.k_out + ((size_t)t * Hkv + h) * kHeadDim)[l16] = out;
             if (at.row < 0) continue;
             const size_t row = (size_t)at.row + ((size_t)h << A.c.log_page);
-            if constexpr (E8) {
-                reinterpret_cast<uint2*>(reinterpret_cast<uint8_t*>(isk ? A.c.k : A.c.v) + row * kHeadDim)[l16] = bytes;
-                if (l16 == 0) (isk ? A.c.k_scales : A.c.v_scales)[row] = scale;
-            } else {
-                reinterpret_cast<uint4*>((isk ? A.c.k : A.c.v) + row * kHeadDim)[l16] = out;
-            }
+            reinterpret_cast<uint4*>((isk ? A.c.k : A.c.v) + row * kHeadDim)[l16] = out;
             if (isk && A.c.weights && l16 == 0) A.c.weights[row] = 0.f;
         }
     }
 }
 
+// ------------------------------------------------------------------ a cache of 8 bits
+//
+// A row y of keys or values fills e4m3's range with its largest magnitude: s = max(max|y| / 448, 2^-126), and y / s is
+// rounded.  Eight lanes own a row, sixteen values (two granules of 16 bytes) a lane: half as many instructions for
+// addresses, sums and scales as with sixteen lanes, which matter here: that kernel was bound by its instructions
+// (82676 tokens 447 us, 407 with a product by 1 / s instead of quotients, 80 % of the issue slots taken).  The
+// granules are such that a pair of the rotation lies in one lane, of either layout, without shuffles.
+// The norm's factor r is common to a row: numbers are y' (448 / max|y'|) of y' = y / r, and the scale is r max|y'| / 448.
+// The products are off by 2^-22 of a quotient at most, which moves a number only where that lies as near to the middle
+// of two.
+constexpr float kMostE4m3 = 448.f, kLeastScale = 1.1754943508222875e-38f;
+constexpr int kQuantRows = 32 * kRotWarps / 8;      // rows of a block at a time
+
+// The larger magnitude, NaN if one is.
+__device__ __forceinline__ float max_abs(float a, float b) {
+    float r;
+    asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(fabsf(a)), "f"(fabsf(b)));
+    return r;
+}
+
+// Rows r y of 8-bit numbers: y becomes the numbers before their rounding; the scale is returned.  top: max|y|.
+__device__ __forceinline__ float scale_row(float (&y)[16], float top, float r) {
+    float s = top * r * (1.f / kMostE4m3);
+    // (A magnitude, or a product, near the ends of the range is divided step by step; NaN and infinities are too.)
+    if (top > 1e-18f && top < 1e18f && s > 1e-30f && s < 1e30f) {
+        const float f = kMostE4m3 / top;
+#pragma unroll
+        for (int e = 0; e < 16; ++e) y[e] *= f;
+        return s;
+    }
+    float z = 0.f;
+#pragma unroll
+    for (int e = 0; e < 16; ++e) {
+        y[e] *= r;
+        z = max_abs(z, y[e]);
+    }
+#pragma unroll
+    for (int o = 4; o; o >>= 1) z = max_abs(z, __shfl_xor_sync(0xffu << (threadIdx.x & 24), z, o));
+    s = z / kMostE4m3;
+    s = s < kLeastScale ? kLeastScale : s;
+#pragma unroll
+    for (int e = 0; e < 16; ++e) y[e] /= s;
+    return s;
+}
+
+template <class T, int NR, int NT, bool IL>
+__global__ void __launch_bounds__(32 * kRotWarps, 6) rotate_quant_kernel(const __grid_constant__ RotateArgs A) {
+    __shared__ Place places[NT];
+    __shared__ __align__(16) float weight[2][kHeadDim];   // the norms' of queries and keys
+    const int lane = threadIdx.x & 31, l8 = lane & 7;
+    const int t0 = blockIdx.x * NT, u0 = blockIdx.y * (kQuantRows * NR) + (threadIdx.x >> 3);
+    asm volatile("griddepcontrol.launch_dependents;\n" ::: "memory");
+    asm volatile("griddepcontrol.wait;\n" ::: "memory");
+    const RotateIO& io = A.io;
+    const int Hq = io.Hq, Hkv = io.Hkv, heads = A.heads;
+    const int rot = io.rot_dim, half = rot >> 1;
+    // This lane's granules of eight values: one of the first half of the rotated values and its partners, or two
+    // neighbours behind them.
+    const bool turn = l8 * 16 < rot;
+    const int ga = turn ? l8 : (rot >> 3) + 2 * (l8 - (rot >> 4)), gb = turn ? l8 + (rot >> 4) : ga + 1;
+    const int nt = min(NT, io.num_tokens - t0);
+    if (threadIdx.x < nt) places[threadIdx.x] = place_of(A, t0 + threadIdx.x);
+    static_assert(32 * kRotWarps == kHeadDim, "a thread a weight");
+    auto norm_weight = [&](const uint16_t* w) { return w ? Half16<T>::unpack(__ldg(w + threadIdx.x)).x : 1.f; };
+    weight[0][threadIdx.x] = norm_weight(io.q_norm);
+    weight[1][threadIdx.x] = norm_weight(io.k_norm);
+    __syncthreads();
+#pragma unroll 1
+    for (int k = 0; k < nt; ++k) {
+        const int t = t0 + k;
+        // Plain loads: an output may lie over its input, each row read before it is written.
+        uint4 xa[NR], xb[NR];
+#pragma unroll
+        for (int i = 0; i < NR; ++i) {
+            const int u = u0 + i * kQuantRows;
+            xa[i] = xb[i] = make_uint4(0u, 0u, 0u, 0u);
+            if (u >= heads) continue;
+            const uint16_t* row = u < Hq         ? io.q + (size_t)t * io.q_stride + (size_t)u * kHeadDim
+                                  : u < Hq + Hkv ? io.k + (size_t)t * io.k_stride + (size_t)(u - Hq) * kHeadDim
+                                                 : io.v + (size_t)t * io.v_stride + (size_t)(u - Hq - Hkv) * kHeadDim;
+            xa[i] = reinterpret_cast<const uint4*>(row)[ga];
+            xb[i] = reinterpret_cast<const uint4*>(row)[gb];
+        }
+        const Place at = places[k];
+        if (at.pos < 0) continue;
+        float c[8], s[8];
+        if (turn) {
+            const float* tab = io.rot_table + (size_t)at.pos * rot;
+            if constexpr (IL) {   // pairs 4 g .. 4 g + 3 of each granule
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
+                    const float4 a = __ldg(reinterpret_cast<const float4*>(tab) + (e ? gb : ga));
+                    const float4 b = __ldg(reinterpret_cast<const float4*>(tab + half) + (e ? gb : ga));
+                    c[4 * e] = a.x; c[4 * e + 1] = a.y; c[4 * e + 2] = a.z; c[4 * e + 3] = a.w;
+                    s[4 * e] = b.x; s[4 * e + 1] = b.y; s[4 * e + 2] = b.z; s[4 * e + 3] = b.w;
+                }
+            } else {
+                load8(tab + ga * 8, c);
+                load8(tab + half + ga * 8, s);
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < NR; ++i) {
+            const int u = u0 + i * kQuantRows;
+            if (u >= heads) continue;   // with its row's eight lanes
+            const uint32_t row_lanes = 0xffu << (lane & 24);
+            const bool isq = u < Hq, isk = !isq && u < Hq + Hkv;
+            float y[16];
+            {
+                float a[8], b[8];
+                unpack8<T>(xa[i], a);
+                unpack8<T>(xb[i], b);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    y[e] = a[e];
+                    y[8 + e] = b[e];
+                }
+            }
+            float r = 1.f;
+            if (isq ? io.q_norm != nullptr : isk && io.k_norm) {
+                float sq = 0.f;
+#pragma unroll
+                for (int e = 0; e < 16; ++e) sq = fmaf(y[e], y[e], sq);
+#pragma unroll
+                for (int o = 4; o; o >>= 1) sq += __shfl_xor_sync(row_lanes, sq, o);
+                r = rsqrtf(fmaf(sq, 1.f / kHeadDim, io.eps));
+                const float4* all = reinterpret_cast<const float4*>(weight[isq ? 0 : 1]);
+#pragma unroll
+                for (int e = 0; e < 16; e += 4) {
+                    const float4 v = all[(e < 8 ? ga : gb) * 2 + (e >> 2 & 1)];
+                    y[e] *= v.x;
+                    y[e + 1] *= v.y;
+                    y[e + 2] *= v.z;
+                    y[e + 3] *= v.w;
+                }
+            }
+            if (turn && (isq || isk)) {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    const int first = IL ? 2 * e : e, second = IL ? 2 * e + 1 : 8 + e;
+                    const float a = y[first], b = y[second];
+                    y[first] = a * c[e] - b * s[e];
+                    y[second] = b * c[e] + a * s[e];
+                }
+            }
+            if (isq || (isk && io.k_out)) {
+                uint16_t* const to = isq ? io.q_out + ((size_t)t * Hq + u) * kHeadDim : io.k_out + ((size_t)t * Hkv + u - Hq) * kHeadDim;
+                auto packed = [&](const float* v) {
+                    return make_uint4(Half16<T>::pack(v[0] * r, v[1] * r), Half16<T>::pack(v[2] * r, v[3] * r),
+                                      Half16<T>::pack(v[4] * r, v[5] * r), Half16<T>::pack(v[6] * r, v[7] * r));
+                };
+                reinterpret_cast<uint4*>(to)[ga] = packed(y);
+                reinterpret_cast<uint4*>(to)[gb] = packed(y + 8);
+            }
+            if (isq) continue;
+            float top = 0.f;
+#pragma unroll
+            for (int e = 0; e < 16; ++e) top = max_abs(top, y[e]);
+#pragma unroll
+            for (int o = 4; o; o >>= 1) top = max_abs(top, __shfl_xor_sync(row_lanes, top, o));
+            if (at.row < 0) continue;
+            const float scale = scale_row(y, top, r);
+            const size_t row = (size_t)at.row + ((size_t)(isk ? u - Hq : u - Hq - Hkv) << A.c.log_page);
+            uint2* const to = reinterpret_cast<uint2*>(reinterpret_cast<uint8_t*>(isk ? A.c.k : A.c.v) + row * kHeadDim);
+            auto packed = [&](const float* v) {
+                return make_uint2(pack_e4m3(v[0], v[1]) | pack_e4m3(v[2], v[3]) << 16, pack_e4m3(v[4], v[5]) | pack_e4m3(v[6], v[7]) << 16);
+            };
+            to[ga] = packed(y);
+            to[gb] = packed(y + 8);
+            if (l8 == 0) {
+                (isk ? A.c.k_scales : A.c.v_scales)[row] = scale;
+                if (isk && A.c.weights) A.c.weights[row] = 0.f;
+            }
+        }
+    }
+}
+
+template <class T, int NR, int NT>
+cudaError_t launch_quant_rows(const RotateArgs& a, cudaStream_t st) {
+    const dim3 grid((unsigned)((a.io.num_tokens + NT - 1) / NT), (unsigned)((a.heads + kQuantRows * NR - 1) / (kQuantRows * NR)));
+    if (a.io.interleaved) return launch_prio(rotate_quant_kernel<T, NR, NT, true>, grid, dim3(32 * kRotWarps), 0, st, 0, true, a);
+    return launch_prio(rotate_quant_kernel<T, NR, NT, false>, grid, dim3(32 * kRotWarps), 0, st, 0, true, a);
+}
+
 template <class T, int NR, int NT>
 cudaError_t launch_rows(const RotateArgs& a, cudaStream_t st) {
     const dim3 grid((unsigned)((a.io.num_tokens + NT - 1) / NT), (unsigned)((a.heads + kRotRows * NR - 1) / (kRotRows * NR)));
-    auto launch = [&](auto kernel) { return launch_prio(kernel, grid, dim3(32 * kRotWarps), 0, st, 0, true, a); };
-    if (a.c.k_scales)
-        return a.io.interleaved ? launch(rotate_kernel<T, NR, NT, true, true>) : launch(rotate_kernel<T, NR, NT, false, true>);
-    return a.io.interleaved ? launch(rotate_kernel<T, NR, NT, true, false>) : launch(rotate_kernel<T, NR, NT, false, false>);
+    if (a.io.interleaved) return launch_prio(rotate_kernel<T, NR, NT, true>, grid, dim3(32 * kRotWarps), 0, st, 0, true, a);
+    return launch_prio(rotate_kernel<T, NR, NT, false>, grid, dim3(32 * kRotWarps), 0, st, 0, true, a);
 }
 
 template <class T>
@@ -246,6 +395,11 @@ cudaError_t launch_typed(const RotateArgs& a, cudaStream_t st) {
     // (six rows, two tokens 11.7), 3200 17.4 (17.2), 6400 37.5 (32.5; four tokens 36.0); 12800
     // tokens two 59.1, four 58.9; 82676 346 and 333.
     const long long rows = (long long)a.io.num_tokens * a.heads;
+    if (a.c.k_scales) {
+        if (rows <= 12000) return launch_quant_rows<T, 1, 1>(a, st);
+        if (rows <= 150000) return launch_quant_rows<T, 3, 1>(a, st);
+        return launch_quant_rows<T, 3, 4>(a, st);
+    }
     if (rows <= 12000) return launch_rows<T, 1, 1>(a, st);
     if (rows <= 150000) return launch_rows<T, 3, 1>(a, st);
     if (rows <= 600000) return launch_rows<T, 6, 2>(a, st);
