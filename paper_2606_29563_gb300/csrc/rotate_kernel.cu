@@ -396,8 +396,12 @@ cudaError_t launch_typed(const RotateArgs& a, cudaStream_t st) {
     // tokens two 59.1, four 58.9; 82676 346 and 333.
     const long long rows = (long long)a.io.num_tokens * a.heads;
     if (a.c.k_scales) {
-        if (rows <= 12000) return launch_quant_rows<T, 1, 1>(a, st);
-        if (rows <= 150000) return launch_quant_rows<T, 3, 1>(a, st);
+        // By the rows, as below; 48 heads, in us: 200 tokens a row each 3.6 (three rows 4.6), 400 both 5.0, 800 7.3 and
+        // 5.4 (of two tokens 8.1); 1600 10.8 and 10.3, 3200 19.4 and 18.1 (of four tokens 17.1); 12800 65.0, 59.9 and
+        // 58.9; 82676 390, 349 and 330.  (Two rows 408, six 418: the registers of more than three leave fewer warps.)
+        if (rows <= 16000) return launch_quant_rows<T, 1, 1>(a, st);
+        if (rows <= 60000) return launch_quant_rows<T, 3, 1>(a, st);
+        if (rows <= 120000) return launch_quant_rows<T, 3, 2>(a, st);
         return launch_quant_rows<T, 3, 4>(a, st);
     }
     if (rows <= 12000) return launch_rows<T, 1, 1>(a, st);
