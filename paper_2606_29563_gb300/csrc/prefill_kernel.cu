@@ -1137,13 +1137,23 @@ __global__ void __launch_bounds__(32 * kXjWarps) prefix_join_kernel(const __grid
         o = make_float4(o.x * f, o.y * f, o.z * f, o.w * f);
         M = m;
         const float w = here ? ptx::ex2(ml.x - m) : 0.f;
+        // Eight shares' sums are read at once.
         const int n = min(32, c1 - c + 1);
-        for (int k = 0; k < n; ++k) {
-            if (!__shfl_sync(0xffffffffu, here ? 1 : 0, k)) continue;
-            const float wk = __shfl_sync(0xffffffffu, w, k);
-            const float4 v = reinterpret_cast<const float4*>(A.part_o + (size_t)(base + 2 * kPfTile * (c + k)) * kHeadDim)[lane];
-            L = fmaf(wk, __shfl_sync(0xffffffffu, ml.y, k), L);
-            o = make_float4(fmaf(wk, v.x, o.x), fmaf(wk, v.y, o.y), fmaf(wk, v.z, o.z), fmaf(wk, v.w, o.w));
+        const uint32_t there = __ballot_sync(0xffffffffu, here);
+        for (int k0 = 0; k0 < n; k0 += 8) {
+            float4 v[8];
+            float wk[8];
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+                const bool one = (there >> (k0 + k)) & 1u;   // k0 + k < 32
+                v[k] = one ? reinterpret_cast<const float4*>(A.part_o + (size_t)(base + 2 * kPfTile * (c + k0 + k)) * kHeadDim)[lane]
+                           : make_float4(0.f, 0.f, 0.f, 0.f);
+                wk[k] = __shfl_sync(0xffffffffu, w, k0 + k);
+                L = fmaf(wk[k], __shfl_sync(0xffffffffu, ml.y, k0 + k), L);
+            }
+#pragma unroll
+            for (int k = 0; k < 8; ++k)
+                o = make_float4(fmaf(wk[k], v[k].x, o.x), fmaf(wk[k], v[k].y, o.y), fmaf(wk[k], v[k].z, o.z), fmaf(wk[k], v[k].w, o.w));
         }
     }
     reinterpret_cast<float4*>(A.px.out + (size_t)row * kHeadDim)[lane] = o;
