@@ -1492,25 +1492,9 @@ kvec_status kvec_paged_read(kvec_handle* h, int batch, const kvec_paged_cache* c
     return KVEC_OK;
 }
 
-namespace {
-
-// Parts of a shared decode's scratch, each from a multiple of 256 bytes on.
-struct SharedScratch {
-    size_t out, ml, prefix, total;   // behind paged_decode's
-    SharedScratch(const kvec_handle* h, int batch, int max_len, bool weights) {
-        const size_t rows = (size_t)batch * h->p.num_q_heads;
-        out = round_up(paged_decode_scratch(batch, h->p.num_q_heads, max_len, 0, 0, weights, false, h->num_sms), 256);
-        ml = out + rows * h->p.head_dim * sizeof(float);
-        prefix = round_up(ml + rows * sizeof(float2), 256);
-        total = prefix + prefix_scratch(batch, h->p.num_q_heads, h->num_sms);
-    }
-};
-
-}  // namespace
-
 size_t kvec_shared_decode_bytes(kvec_handle* h, int batch, int max_len, int with_weights) {
     if (!h || batch < 1 || batch > h->p.max_batch || max_len < 1 || max_len > kPagedMaxLen) return 0;
-    return SharedScratch(h, batch, max_len, with_weights != 0).total;
+    return shared_decode_scratch(batch, h->p.num_q_heads, max_len, with_weights != 0, h->num_sms);
 }
 
 kvec_status kvec_shared_decode(kvec_handle* h, int batch, const void* q, const kvec_paged_cache* cache,
@@ -1539,45 +1523,33 @@ kvec_status kvec_shared_decode(kvec_handle* h, int batch, const void* q, const k
     if (!q || !out || !scratch) return fail(KVEC_ERR_INVALID_ARG, "a device pointer is NULL");
     if (!aligned16(q) || !aligned16(out) || reinterpret_cast<uintptr_t>(scratch) % 256)
         return fail(KVEC_ERR_INVALID_ARG, "q and out must be 16-byte and scratch 256-byte aligned");
-    const SharedScratch part(h, batch, max_len, v.weights != nullptr);
-    if (scratch_bytes < part.total)
-        return fail(KVEC_ERR_INVALID_ARG, "scratch of %zu bytes, %zu are needed", scratch_bytes, part.total);
-    char* const base = static_cast<char*>(scratch);
+    const size_t need = kvec_shared_decode_bytes(h, batch, max_len, v.weights != nullptr);
+    if (scratch_bytes < need)
+        return fail(KVEC_ERR_INVALID_ARG, "scratch of %zu bytes, %zu are needed", scratch_bytes, need);
+    const kvec_params& p = h->p;
     PrefixIO px{};
+    px.geom = {prefix->lens, prefix->cu_seqs, prefix->num_groups, max_prefix, batch, p.num_q_heads, p.num_kv_heads, h->g, 128 / h->g};
     px.q = static_cast<const uint16_t*>(q);
     px.c = v;
     px.table = prefix->page_table;
-    px.lens = prefix->lens;
-    px.cu = prefix->cu_seqs;
-    px.groups = prefix->num_groups;
     px.max_pages = prefix->max_pages;
-    px.max_prefix = max_prefix;
-    px.batch = batch;
-    px.Hq = h->p.num_q_heads;
-    px.Hkv = h->p.num_kv_heads;
-    px.scale = softmax_scale_of(h->p);
+    px.scale = softmax_scale_of(p);
     px.err = h->sc.err;
-    px.scratch = base + part.prefix;
-    px.out = reinterpret_cast<float*>(base + part.out);
-    px.ml = reinterpret_cast<float2*>(base + part.ml);
     PagedDecodeIO io{};
     io.q = px.q;
     io.out = static_cast<uint16_t*>(out);
     io.scratch = scratch;
     io.err = px.err;
     io.batch = batch;
-    io.Hq = px.Hq;
-    io.Hkv = px.Hkv;
+    io.Hq = p.num_q_heads;
+    io.Hkv = p.num_kv_heads;
     io.max_len = max_len;
     io.scale = px.scale;
-    io.pre_o = px.out;
-    io.pre_ml = px.ml;
     int prev = 0;
     s = set_device(h, &prev);
     if (s != KVEC_OK) return s;
     DeviceGuard guard{prev, h->device};
-    cudaError_t e = launch_prefix(px, h->num_sms, reinterpret_cast<cudaStream_t>(stream));
-    if (e == cudaSuccess) e = launch_paged_decode(io, v, h->num_sms, reinterpret_cast<cudaStream_t>(stream));
+    cudaError_t e = launch_shared_decode(io, v, px, h->num_sms, reinterpret_cast<cudaStream_t>(stream));
     if (e != cudaSuccess) return cuda_fail(e, "shared decode launch");
     return KVEC_OK;
 }

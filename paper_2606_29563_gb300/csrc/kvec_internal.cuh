@@ -157,8 +157,6 @@ struct PagedDecodeIO {
     int max_len;              // bound on the lengths, within the cache's capacity
     int window, sinks;
     float scale;
-    const float* pre_o;       // [batch][Hq][d] sums of what is seen before the sequence's own slots (launch_prefix),
-    const float2* pre_ml;     // [batch][Hq] their maxima and sums of weights; null: nothing
 };
 
 // Eviction by accumulated weight (evict_kernel.cu).
@@ -185,22 +183,26 @@ struct PrefillIO {
     float scale;
 };
 
-// What groups of sequences share: attention of all their queries over a prefix in pages, as sums that the attention
-// over the sequences' own slots takes in (prefill_kernel.cu, paged_decode_kernel.cu).
+// Groups of sequences that share a prefix.
+struct PrefixGeom {
+    const int *lens, *cu;     // [groups], [groups + 1]
+    int groups;
+    int max_prefix;           // bound on the lengths
+    int batch, Hq, Hkv;
+    int g, nq;                // query heads of a KV head, queries of a 128-row tile
+};
+
+// Attention of all queries of each group over its prefix in pages, as sums (prefill_kernel.cu).
 struct PrefixIO {
+    PrefixGeom geom;
     const uint16_t* q;        // [batch][Hq][d]
     PagedCacheView c;         // the pool; its table and lengths are the sequences' own
     const int* table;         // [groups][max_pages]
-    const int* lens;          // [groups]
-    const int* cu;            // [groups + 1]: the groups' sequences
-    int groups, max_pages;
-    int max_prefix;           // bound on the lengths, within a row of the table
-    int batch, Hq, Hkv;
+    int max_pages;
     float scale;
     int* err;
-    void* scratch;            // prefix_scratch bytes
-    float* out;               // [batch][Hq][d] sums, relative to
-    float2* ml;               // [batch][Hq] (maximum, sum)
+    float* part_o;            // [batch * Hq + 256 * SMs][d], by rows as PrefixGroup::first_row says
+    float2* part_ml;          // maxima and sums of weights
     int rows;                 // of the pages
 };
 
@@ -339,12 +341,15 @@ cudaError_t launch_ada(const Geometry& g, const LayerIO& io, const Scratch& sc, 
 cudaError_t launch_decode(const DecodeIO& io, int num_sms, cudaStream_t st);
 cudaError_t launch_rotate(const RotateIO& io, const PagedCacheView& c, cudaStream_t st);
 cudaError_t launch_paged_decode(const PagedDecodeIO& io, const PagedCacheView& c, int num_sms, cudaStream_t st);
+size_t shared_decode_scratch(int batch, int Hq, int max_len, bool weights, int num_sms);
+// px: but for the places of its sums.
+cudaError_t launch_shared_decode(const PagedDecodeIO& io, const PagedCacheView& c, const PrefixIO& px, int num_sms, cudaStream_t st);
 size_t paged_decode_scratch(int batch, int Hq, int max_len, int window, int sinks, bool weights, bool e8, int num_sms);
 cudaError_t launch_read(const ReadIO& io, const PagedCacheView& c, cudaStream_t st);
 cudaError_t launch_evict(const EvictIO& io, const PagedCacheView& c, cudaStream_t st);
 PrefillPlan plan_prefill(int batch, int Hq, int Hkv, int max_q, int max_k, int window, int sinks, int num_sms);
-size_t prefix_scratch(int batch, int Hq, int num_sms);
-// A programmatic dependent may read before its wait what was complete before the call.
+// A programmatic dependent of a kernel that let it start once all before that was complete, and does not wait for it
+// but at its end.
 cudaError_t launch_prefix(const PrefixIO& px, int num_sms, cudaStream_t st);
 cudaError_t launch_prefill(const PrefillIO& io, const PrefillPlan& plan, int num_sms, cudaStream_t st);
 // out_idx from the slot's kept-position bits, then the K/V rows.

@@ -29,6 +29,7 @@
 // by the bound on the lengths: the 64 rows take 51 us under one of 8192, 57 of 32768 and 82 of 131072.
 #include "half_types.cuh"
 #include "kvec_internal.cuh"
+#include "prefix_list.cuh"
 #include "sm100_ptx.cuh"
 
 #include <cooperative_groups.h>
@@ -69,6 +70,8 @@ struct PdArgs {
     float* logits;            // [pair][nbmax][g][slots of a block]
     float* part_o;            // [2 * ctas][8][128] shares of split pairs, unnormalised
     float2* part_ml;          // [2 * ctas][8] their maxima and sums
+    float* own_o;             // shared_decode: [pair][g][128] sums of whole pairs, in the rows behind part_o's, and
+    float2* own_ml;           // [pair][g] behind part_ml's; then come the prefixes'
     int ctas;                 // that share the list of blocks
     int pairs;                // batch * Hkv where a CTA each may do, else 0
     int nbmax;                // most visible blocks of a pair
@@ -222,17 +225,6 @@ struct List {
     }
 };
 
-// What comes before a sequence's own slots, for query row `at`: its maximum and sum of weights joined to (M, L).
-// Returns the factors of the sums so far and of those before.
-__device__ __forceinline__ float2 join_before(const PdArgs& A, size_t at, float& M, float& L) {
-    const float2 b = __ldcg(A.io.pre_ml + at);
-    const float m = fmaxf(M, b.x);
-    const float2 f = make_float2(ptx::ex2(M - m), ptx::ex2(b.x - m));
-    L = fmaf(f.y, b.y, L * f.x);
-    M = m;
-    return f;
-}
-
 // a / b, in 32 bits where they do.
 __device__ __forceinline__ long long quotient(long long a, long long b) {
     return ((a | b) >> 32) == 0 ? (long long)((uint32_t)a / (uint32_t)b) : a / b;
@@ -334,9 +326,8 @@ __device__ void add_weights(const PdArgs& A, int s, int h, const Visible<B>& v, 
 // of e4m3 (m16n8k32): a query row, brought to their range by a power of two, is the sum of two numbers (bf16, its 8 bits)
 // or three (fp16), so that keys go to the tiles as they are.  Values become fp16, which holds them all, on
 // their way; the weights with their scales are brought to its range by a power of two, the warp's so far.
-// PRE: sums of what comes before the sequence's own slots are merged at the end (launch_prefix); the kernels that leave
-// them may still run until then.
-template <class T, bool CL, bool E8, bool PRE>
+// OPEN: pairs' sums stay sums (own_o, own_ml), for shared_join_kernel, which adds the weights too.
+template <class T, bool CL, bool E8, bool OPEN>
 __global__ void __launch_bounds__(kPdThreads, kPdCtasPerSm) paged_decode_kernel(const __grid_constant__ PdArgs A) {
     constexpr int B = kPdBlock<E8>;
     constexpr bool kThird = E8 && std::is_same_v<T, __half>;    // a query is the sum of three e4m3 numbers
@@ -362,8 +353,8 @@ __global__ void __launch_bounds__(kPdThreads, kPdCtasPerSm) paged_decode_kernel(
     }
     __syncthreads();
     // The trigger follows the wait: what was complete before this grid may be read by the
-    // join kernel before its own wait.  (With PRE it was before the call's first kernel let others start.)
-    if constexpr (!PRE) asm volatile("griddepcontrol.wait;\n" ::: "memory");
+    // join kernel before its own wait.
+    asm volatile("griddepcontrol.wait;\n" ::: "memory");
     asm volatile("griddepcontrol.launch_dependents;\n" ::: "memory");
 
     // This CTA's blocks: `count` from (s, h, i) on.
@@ -749,7 +740,6 @@ __global__ void __launch_bounds__(kPdThreads, kPdCtasPerSm) paged_decode_kernel(
             }
         }
         __syncthreads();
-        if constexpr (PRE) asm volatile("griddepcontrol.wait;\n" ::: "memory");
         for (int e = tid; e < g * kHeadDim; e += kPdThreads) {
             const int j = e / kHeadDim, c = e % kHeadDim;
             float M = kNoLogit;
@@ -769,16 +759,17 @@ __global__ void __launch_bounds__(kPdThreads, kPdCtasPerSm) paged_decode_kernel(
                     cl[j] = L;
                 }
             } else if (CL || whole) {
-                if constexpr (PRE) {
-                    const size_t at = (size_t)s * Hq + (size_t)h * g + j;
-                    const float2 f = join_before(A, at, M, L);
-                    O = fmaf(f.y, __ldcg(A.io.pre_o + at * kHeadDim + c), O * f.x);
-                }
-                const float o = L > 0.f || L != L ? O / L : 0.f;
-                reinterpret_cast<T*>(A.io.out)[((size_t)s * Hq + (size_t)h * g + j) * kHeadDim + c] = T(o);
-                if (c == 0) {
-                    fm[j] = M;
-                    finv[j] = L > 0.f || L != L ? 1.f / L : 0.f;
+                const size_t at = (size_t)s * Hq + (size_t)h * g + j;
+                if constexpr (OPEN) {
+                    A.own_o[at * kHeadDim + c] = O;
+                    if (c == 0) A.own_ml[at] = make_float2(M, L);
+                } else {
+                    const float o = L > 0.f || L != L ? O / L : 0.f;
+                    reinterpret_cast<T*>(A.io.out)[at * kHeadDim + c] = T(o);
+                    if (c == 0) {
+                        fm[j] = M;
+                        finv[j] = L > 0.f || L != L ? 1.f / L : 0.f;
+                    }
                 }
             } else {
                 const size_t slot = (size_t)blockIdx.x * 2 + (first_segment ? 0 : 1);
@@ -792,7 +783,7 @@ __global__ void __launch_bounds__(kPdThreads, kPdCtasPerSm) paged_decode_kernel(
             // A CTA of a cluster has 512 slots at most, four a thread, read while the cluster meets.
             SlotWeights<B> sw;
             sw.row = -1;
-            if (A.c.weights && tid < len * (B / 4)) sw.load(A, s, h, v, i_begin, tid);
+            if (!OPEN && A.c.weights && tid < len * (B / 4)) sw.load(A, s, h, v, i_begin, tid);
             if (splits > 1) {
                 cg::cluster_group cluster = cg::this_cluster();
                 cluster.sync();
@@ -807,7 +798,7 @@ __global__ void __launch_bounds__(kPdThreads, kPdCtasPerSm) paged_decode_kernel(
 #pragma unroll
                     for (int r = 0; r < kPdMaxCluster; ++r)
                         if (r < splits) L = fmaf(ptx::ex2(mc[r] - M), *cluster.map_shared_rank(&cl[tid], r), L);
-                    if constexpr (PRE) join_before(A, (size_t)s * Hq + (size_t)h * g + tid, M, L);
+                    if (OPEN && rank == 0) A.own_ml[(size_t)s * Hq + (size_t)h * g + tid] = make_float2(M, L);
                     fm[tid] = M;
                     finv[tid] = L > 0.f || L != L ? 1.f / L : 0.f;
                 }
@@ -815,26 +806,24 @@ __global__ void __launch_bounds__(kPdThreads, kPdCtasPerSm) paged_decode_kernel(
                 for (int e = tid; rank + (e / kHeadDim) * splits < g; e += kPdThreads) {
                     const int j = rank + (e / kHeadDim) * splits, c = e % kHeadDim;
                     float O = 0.f;
-                    if constexpr (PRE) {
-                        const size_t at = (size_t)s * Hq + (size_t)h * g + j;
-                        O = ptx::ex2(__ldcg(A.io.pre_ml + at).x - fm[j]) * __ldcg(A.io.pre_o + at * kHeadDim + c);
-                    }
 #pragma unroll
                     for (int r = 0; r < kPdMaxCluster; ++r) {
                         if (r >= splits) break;
                         O = fmaf(ptx::ex2(*cluster.map_shared_rank(&cm[j], r) - fm[j]),
                                  *cluster.map_shared_rank(&co[CL ? j : 0][c], r), O);
                     }
-                    reinterpret_cast<T*>(A.io.out)[((size_t)s * Hq + (size_t)h * g + j) * kHeadDim + c] = T(O * finv[j]);
+                    const size_t at = (size_t)s * Hq + (size_t)h * g + j;
+                    if constexpr (OPEN) A.own_o[at * kHeadDim + c] = O;
+                    else reinterpret_cast<T*>(A.io.out)[at * kHeadDim + c] = T(O * finv[j]);
                 }
-                if (A.c.weights) sw.store(A, fm, finv);
+                if (!OPEN && A.c.weights) sw.store(A, fm, finv);
                 cluster.sync();   // no CTA leaves while another still reads its shared memory
-            } else if (A.c.weights) {
+            } else if (!OPEN && A.c.weights) {
                 sw.store(A, fm, finv);
             }
             break;
         }
-        if (A.c.weights && whole) {
+        if (!OPEN && A.c.weights && whole) {
             add_weights<kPdThreads, B>(A, s, h, v, i_begin, i_begin + len, fm, finv);
             __syncthreads();      // before the next segment's fm and finv
         }
@@ -842,8 +831,6 @@ __global__ void __launch_bounds__(kPdThreads, kPdCtasPerSm) paged_decode_kernel(
         cur.advance(A, len);
         first_segment = false;
     }
-    // (A CTA without a block has not waited.)
-    if constexpr (PRE) asm volatile("griddepcontrol.wait;\n" ::: "memory");
     // Copies in flight land before the CTA may exit (a stage without one runs into the limit).
     if (failed)
         for (int i = 0; i < kPdStages; ++i) ptx::mbar_wait(&full[warp][i], (phases >> i) & 1u, 20000000ull);
@@ -853,7 +840,7 @@ __global__ void __launch_bounds__(kPdThreads, kPdCtasPerSm) paged_decode_kernel(
 // others add the weights, kJoinRows slots each.  (A lane finds a share's place and sums, and eight shares' outputs are
 // read at once: one thread in a loop over the 38 shares of 131072 slots took 58 us.  Six blocks resident on an
 // SM: eight spill, 64 rows take the same but a window of 4096 in 16 caches 55.5 us instead of 53.6.)
-template <class T, int B, bool PRE>
+template <class T, int B>
 __global__ void __launch_bounds__(kJoinThreads, 6) paged_join_kernel(const __grid_constant__ PdArgs A) {
     extern __shared__ float2 share[];                 // [shares][kPdHeads] (place as an int, maximum)
     __shared__ float fm[kPdHeads], finv[kPdHeads];
@@ -879,17 +866,8 @@ __global__ void __launch_bounds__(kJoinThreads, 6) paged_join_kernel(const __gri
     asm volatile("griddepcontrol.launch_dependents;\n" ::: "memory");
     asm volatile("griddepcontrol.wait;\n" ::: "memory");
     T* const out = reinterpret_cast<T*>(A.io.out) + ((size_t)s * A.io.Hq + (size_t)h * g) * kHeadDim + lane * 4;
-    const size_t first = (size_t)s * A.io.Hq + (size_t)h * g;   // query row
     if (v.nb == 0 && !weights)
-        for (int j = warp; j < g; j += kJoinThreads / 32) {
-            uint2 o = make_uint2(0u, 0u);
-            if constexpr (PRE) {
-                const float L = __ldcg(A.io.pre_ml + first + j).y;
-                const float4 b = __ldcg(reinterpret_cast<const float4*>(A.io.pre_o + (first + j) * kHeadDim) + lane);
-                if (L > 0.f || L != L) o = make_uint2(Half16<T>::pack(b.x / L, b.y / L), Half16<T>::pack(b.z / L, b.w / L));
-            }
-            *reinterpret_cast<uint2*>(out + j * kHeadDim) = o;
-        }
+        for (int j = warp; j < g; j += kJoinThreads / 32) *reinterpret_cast<uint2*>(out + j * kHeadDim) = make_uint2(0u, 0u);
     if (done) return;
     for (int j = warp; j < g; j += kJoinThreads / 32) {   // a lane a share
         float M = kNoLogit, L = 0.f;
@@ -915,8 +893,6 @@ __global__ void __launch_bounds__(kJoinThreads, 6) paged_join_kernel(const __gri
         }
         // (The two halves of a pair of lanes sum in different orders: lane 0's is taken.)
         L = __shfl_sync(0xffffffffu, L, 0);
-        float2 f2 = make_float2(1.f, 0.f);
-        if constexpr (PRE) f2 = join_before(A, first + j, M, L);
         const bool some = L > 0.f || L != L;
         if (lane == 0) {
             fm[j] = M;
@@ -925,10 +901,6 @@ __global__ void __launch_bounds__(kJoinThreads, 6) paged_join_kernel(const __gri
         __syncwarp();
         if (!weights) {
             float4 O = make_float4(0.f, 0.f, 0.f, 0.f);
-            if constexpr (PRE) {
-                const float4 b = __ldcg(reinterpret_cast<const float4*>(A.io.pre_o + (first + j) * kHeadDim) + lane);
-                O = make_float4(b.x * f2.y, b.y * f2.y, b.z * f2.y, b.w * f2.y);
-            }
             const float* part = A.part_o + (size_t)j * kHeadDim + lane * 4;
             for (int c = 0; c <= c1 - c0; c += 8) {
                 float4 o[8];
@@ -954,12 +926,109 @@ __global__ void __launch_bounds__(kJoinThreads, 6) paged_join_kernel(const __gri
     add_weights<kJoinThreads, B>(A, s, h, v, i0, min(v.nb, i0 + kJoinRows / B), fm, finv);
 }
 
+// shared_decode: what the shares of a group's prefix and those of the sequence's own slots sum up to.  Block x = 0 of
+// (x, h, s) writes the outputs, a warp a query head, the others add the weights, kJoinRows slots each.  Sums lie as rows of
+// 128 values behind one another: the CTAs' shares of pairs, whole pairs, the prefixes' shares.  A lane reads a share's
+// maximum and sum, and eight shares' rows are read at once.
+// one_each: every pair's own sums are whole (a cluster each); else as the list of blocks says.
+template <class T>
+__global__ void __launch_bounds__(kJoinThreads, 6) shared_join_kernel(const __grid_constant__ PdArgs A, const __grid_constant__ PrefixGeom G,
+                                                                      int prefix_ctas, bool one_each) {
+    constexpr int B = kPdBlock<false>;
+    __shared__ float fm[kPdHeads], finv[kPdHeads];
+    const int h = blockIdx.y, s = blockIdx.z, lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = A.g;
+    // The lengths were complete before the call.
+    Visible<B> v;
+    v.init(A, s);
+    const bool weights = blockIdx.x > 0;
+    const int i0 = ((int)blockIdx.x - 1) * (kJoinRows / B);
+    int own = v.nb ? 1 : 0, c0 = 0;   // the pair's own shares, of CTAs c0 on
+    long long total = 0, p0 = 0;
+    bool whole = true;
+    if (!one_each && v.nb) {
+        List<B> list;
+        list.init(A);
+        whole = list.whole_pairs(A);
+        total = list.total;
+        if (!whole) {
+            p0 = list.places_before(A, s) + (long long)h * List<B>::places(v);
+            c0 = (int)quotient((p0 + kPairCost + 1) * A.ctas - 1, total);
+            own = (int)quotient((p0 + kPairCost + v.nb) * A.ctas - 1, total) - c0 + 1;
+            whole = own == 1;
+        }
+    }
+    const PrefixParts parts(G, s, h, prefix_ctas);
+    const int n = own + parts.c1 - parts.c0 + 1;
+    const int own_rows = A.ctas * 2 * kPdHeads, prefix_rows = own_rows + A.io.batch * A.io.Hq;
+    asm volatile("griddepcontrol.launch_dependents;\n" ::: "memory");
+    asm volatile("griddepcontrol.wait;\n" ::: "memory");
+    if (weights && i0 >= v.nb) return;
+    for (int j = warp; j < g; j += kJoinThreads / 32) {
+        float M = kNoLogit, L = 0.f;
+        float4 O = make_float4(0.f, 0.f, 0.f, 0.f);
+        for (int k0 = 0; k0 < n; k0 += 32) {
+            const int k = k0 + lane;
+            int row = -1;
+            if (k < own) {
+                const int cta = c0 + k;
+                if (whole) row = own_rows + s * A.io.Hq + h * g + j;
+                else if (k == 0) row = (cta * 2 + (share_start(total, c0, A.ctas) < p0 ? 1 : 0)) * kPdHeads + j;
+                else if (total >= A.ctas || share_start(total, cta, A.ctas) < share_start(total, cta + 1, A.ctas)) row = cta * 2 * kPdHeads + j;
+            } else if (k < n) {
+                row = parts.row(parts.c0 + k - own, prefix_ctas);
+                if (row >= 0) row += prefix_rows + j;
+            }
+            const float2 ml = row < 0 ? make_float2(kNoLogit, 0.f) : A.part_ml[row];
+            float m = ml.x;
+#pragma unroll
+            for (int o = 16; o; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
+            m = fmaxf(m, M);
+            const float f = ptx::ex2(M - m), w = row < 0 ? 0.f : ptx::ex2(ml.x - m);
+            float l = w * ml.y;
+#pragma unroll
+            for (int o = 16; o; o >>= 1) l += __shfl_xor_sync(0xffffffffu, l, o);
+            L = fmaf(L, f, l);
+            M = m;
+            if (weights) continue;
+            O = make_float4(O.x * f, O.y * f, O.z * f, O.w * f);
+            for (int e0 = 0; e0 < min(32, n - k0); e0 += 8) {
+                float4 o[8];
+                float wk[8];
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    const int from = __shfl_sync(0xffffffffu, row, e0 + e);
+                    wk[e] = __shfl_sync(0xffffffffu, w, e0 + e);
+                    o[e] = from < 0 ? make_float4(0.f, 0.f, 0.f, 0.f)
+                                    : reinterpret_cast<const float4*>(A.part_o + (size_t)from * kHeadDim)[lane];
+                }
+#pragma unroll
+                for (int e = 0; e < 8; ++e)
+                    O = make_float4(fmaf(wk[e], o[e].x, O.x), fmaf(wk[e], o[e].y, O.y), fmaf(wk[e], o[e].z, O.z), fmaf(wk[e], o[e].w, O.w));
+            }
+        }
+        // (The lanes sum in different orders: lane 0's sum is taken.)
+        L = __shfl_sync(0xffffffffu, L, 0);
+        const bool some = L > 0.f || L != L;
+        if (lane == 0) {
+            fm[j] = M;
+            finv[j] = some ? 1.f / L : 0.f;
+        }
+        if (!weights)
+            reinterpret_cast<uint2*>(reinterpret_cast<T*>(A.io.out) + ((size_t)s * A.io.Hq + (size_t)h * g + j) * kHeadDim)[lane] =
+                some ? make_uint2(Half16<T>::pack(O.x / L, O.y / L), Half16<T>::pack(O.z / L, O.w / L)) : make_uint2(0u, 0u);
+    }
+    if (!weights) return;
+    __syncthreads();
+    add_weights<kJoinThreads, B>(A, s, h, v, i0, min(v.nb, i0 + kJoinRows / B), fm, finv);
+}
+
 size_t round16(size_t x) { return (x + 15) & ~size_t(15); }
 
 int share_ctas(int num_sms) { return kPdCtasPerSm * num_sms; }
 
-template <class T, bool E8, bool PRE>
-cudaError_t launch_typed(const PdArgs& a, cudaStream_t st) {
+// one_each: set to whether each pair is finished by a cluster.
+template <class T, bool E8, bool OPEN>
+cudaError_t launch_pairs(const PdArgs& a, cudaStream_t st, bool* one_each) {
     constexpr int B = kPdBlock<E8>;
     // CTAs of a pair: the largest cluster that fits the device's resident CTAs in one wave, with
     // two blocks a warp and more; taken where that leaves a CTA 32 blocks and less (a quarter of
@@ -970,7 +1039,8 @@ cudaError_t launch_typed(const PdArgs& a, cudaStream_t st) {
     const int pairs = a.io.batch * a.io.Hkv;
     int splits = 1;
     while (splits < kPdMaxCluster && (long long)pairs * splits * 2 <= a.ctas && a.nbmax >= kPdWarps * 2 * splits) splits *= 2;
-    if (a.nbmax * (B / 4) <= kPdThreads * splits) {
+    *one_each = a.nbmax * (B / 4) <= kPdThreads * splits;
+    if (*one_each) {
         cudaLaunchConfig_t cfg = {};
         cfg.gridDim = dim3(splits, a.io.Hkv, a.io.batch);
         cfg.blockDim = dim3(kPdThreads);
@@ -985,13 +1055,32 @@ cudaError_t launch_typed(const PdArgs& a, cudaStream_t st) {
         attr[1].val.programmaticStreamSerializationAllowed = 1;
         cfg.attrs = attr;
         cfg.numAttrs = 2;
-        return cudaLaunchKernelEx(&cfg, paged_decode_kernel<T, true, E8, PRE>, a);
+        return cudaLaunchKernelEx(&cfg, paged_decode_kernel<T, true, E8, OPEN>, a);
     }
-    cudaError_t e = launch_prio(paged_decode_kernel<T, false, E8, PRE>, dim3(a.ctas), dim3(kPdThreads), kPdSmem, st, 0, true, a);
-    if (e != cudaSuccess) return e;
-    const int rows = a.c.weights ? (a.nbmax * B + kJoinRows - 1) / kJoinRows : 0;
-    return launch_prio(paged_join_kernel<T, B, PRE>, dim3(1 + rows, a.io.Hkv, a.io.batch), dim3(kJoinThreads),
+    return launch_prio(paged_decode_kernel<T, false, E8, OPEN>, dim3(a.ctas), dim3(kPdThreads), kPdSmem, st, 0, true, a);
+}
+
+// Blocks of a join that add the weights of a pair.
+int weight_blocks(const PdArgs& a, int B) { return a.c.weights ? (a.nbmax * B + kJoinRows - 1) / kJoinRows : 0; }
+
+template <class T, bool E8>
+cudaError_t launch_typed(const PdArgs& a, cudaStream_t st) {
+    constexpr int B = kPdBlock<E8>;
+    bool one_each = false;
+    const cudaError_t e = launch_pairs<T, E8, false>(a, st, &one_each);
+    if (e != cudaSuccess || one_each) return e;
+    return launch_prio(paged_join_kernel<T, B>, dim3(1 + weight_blocks(a, B), a.io.Hkv, a.io.batch), dim3(kJoinThreads),
                        a.ctas * kPdHeads * sizeof(float2), st, 0, true, a);
+}
+
+template <class T>
+cudaError_t launch_shared_typed(const PdArgs& a, const PrefixIO& px, int num_sms, cudaStream_t st) {
+    bool one_each = false;
+    cudaError_t e = launch_pairs<T, false, true>(a, st, &one_each);
+    if (e == cudaSuccess) e = launch_prefix(px, num_sms, st);
+    if (e != cudaSuccess) return e;
+    return launch_prio(shared_join_kernel<T>, dim3(1 + weight_blocks(a, kPdBlock<false>), a.io.Hkv, a.io.batch), dim3(kJoinThreads), 0,
+                       st, 0, true, a, px.geom, num_sms, one_each);
 }
 
 // Most blocks of B slots that a sequence of up to max_len slots has in sight.
@@ -1010,6 +1099,14 @@ size_t paged_decode_scratch(int batch, int Hq, int max_len, int window, int sink
     const size_t slots = (size_t)share_ctas(num_sms) * 2 * kPdHeads;
     size_t b = round16(slots * kHeadDim * sizeof(float)) + round16(slots * sizeof(float2));
     if (weights) b += (size_t)batch * Hq * visible_blocks(B, max_len, window, sinks) * B * sizeof(float);
+    return b;
+}
+
+// Rows of sums: the CTAs' shares, whole pairs, and the prefixes'.
+size_t shared_decode_scratch(int batch, int Hq, int max_len, bool weights, int num_sms) {
+    const size_t rows = (size_t)share_ctas(num_sms) * 2 * kPdHeads + (size_t)batch * Hq * 2 + (size_t)2 * kPrefixTile * num_sms;
+    size_t b = rows * kHeadDim * sizeof(float) + round16(rows * sizeof(float2));
+    if (weights) b += (size_t)batch * Hq * visible_blocks(kPdBlock<false>, max_len, 0, 0) * kPdBlock<false> * sizeof(float);
     return b;
 }
 
@@ -1032,8 +1129,10 @@ cudaError_t configure_paged_decode() {
     return e;
 }
 
-cudaError_t launch_paged_decode(const PagedDecodeIO& io, const PagedCacheView& c, int num_sms, cudaStream_t st) {
-    PdArgs a{};
+namespace {
+
+// Everything but the places in scratch.
+cudaError_t fill_args(PdArgs& a, const PagedDecodeIO& io, const PagedCacheView& c, int num_sms) {
     // Rows of 8 bits as 64 elements of 16: the copies only move them.
     const bool e8 = c.k_scales != nullptr;
     const uint64_t dims[2] = {(uint64_t)(e8 ? kHeadDim / 2 : kHeadDim), ((uint64_t)c.num_pages * io.Hkv) << c.log_page};
@@ -1042,7 +1141,6 @@ cudaError_t launch_paged_decode(const PagedDecodeIO& io, const PagedCacheView& c
     const uint32_t box[2] = {64, (uint32_t)a.box};
     cudaError_t e = encode_tensor_map(&a.kmap, c.dtype, 2, c.k, dims, strides, box);
     if (e == cudaSuccess) e = encode_tensor_map(&a.vmap, c.dtype, 2, c.v, dims, strides, box);
-    if (e != cudaSuccess) return e;
     a.c = c;
     a.io = io;
     a.g = io.Hq / io.Hkv;
@@ -1052,6 +1150,15 @@ cudaError_t launch_paged_decode(const PagedDecodeIO& io, const PagedCacheView& c
     const long long pairs = (long long)io.batch * io.Hkv;
     a.pairs = pairs <= a.ctas && pairs * 4 >= a.ctas * 3ll ? (int)pairs : 0;
     a.nbmax = visible_blocks(e8 ? kPdBlock<true> : kPdBlock<false>, io.max_len, io.window, io.sinks);
+    return e;
+}
+
+}  // namespace
+
+cudaError_t launch_paged_decode(const PagedDecodeIO& io, const PagedCacheView& c, int num_sms, cudaStream_t st) {
+    PdArgs a{};
+    const cudaError_t e = fill_args(a, io, c, num_sms);
+    if (e != cudaSuccess) return e;
     const size_t slots = (size_t)a.ctas * 2 * kPdHeads;
     char* p = static_cast<char*>(io.scratch);
     a.part_o = reinterpret_cast<float*>(p);
@@ -1061,9 +1168,26 @@ cudaError_t launch_paged_decode(const PagedDecodeIO& io, const PagedCacheView& c
     a.logits = reinterpret_cast<float*>(p);
     auto launch = [&](auto type) {
         using T = decltype(type);
-        return e8 ? launch_typed<T, true, false>(a, st) : io.pre_o ? launch_typed<T, false, true>(a, st) : launch_typed<T, false, false>(a, st);
+        return c.k_scales ? launch_typed<T, true>(a, st) : launch_typed<T, false>(a, st);
     };
     return c.dtype == 1 ? launch(__half{}) : launch(__nv_bfloat16{});
+}
+
+cudaError_t launch_shared_decode(const PagedDecodeIO& io, const PagedCacheView& c, const PrefixIO& prefix, int num_sms, cudaStream_t st) {
+    PdArgs a{};
+    const cudaError_t e = fill_args(a, io, c, num_sms);
+    if (e != cudaSuccess) return e;
+    const size_t shares = (size_t)a.ctas * 2 * kPdHeads, pairs = (size_t)io.batch * io.Hq;
+    const size_t rows = shares + 2 * pairs + (size_t)2 * kPrefixTile * num_sms;
+    a.part_o = static_cast<float*>(io.scratch);
+    a.part_ml = reinterpret_cast<float2*>(a.part_o + rows * kHeadDim);
+    a.own_o = a.part_o + shares * kHeadDim;
+    a.own_ml = a.part_ml + shares;
+    a.logits = reinterpret_cast<float*>(reinterpret_cast<char*>(a.part_ml) + round16(rows * sizeof(float2)));
+    PrefixIO px = prefix;
+    px.part_o = a.own_o + pairs * kHeadDim;
+    px.part_ml = a.own_ml + pairs;
+    return c.dtype == 1 ? launch_shared_typed<__half>(a, px, num_sms, st) : launch_shared_typed<__nv_bfloat16>(a, px, num_sms, st);
 }
 
 }  // namespace kvec

@@ -49,12 +49,13 @@
 // The same products without the causal order serve shared_decode (PAGED): the queries of the sequences
 // that share a prefix are the rows, each of which sees all of it, and K and V blocks come from the
 // prefix's pages.  The blocks of all (group, KV head, pair of tiles) form one list, as the lengths
-// are on the device; every CTA takes an even share and leaves sums for prefix_join_kernel.
+// are on the device; every CTA takes an even share and leaves sums for shared_join_kernel.
 #include <algorithm>
 #include <type_traits>
 
 #include "half_types.cuh"
 #include "kvec_internal.cuh"
+#include "prefix_list.cuh"
 #include "sm100_ptx.cuh"
 
 namespace kvec {
@@ -65,6 +66,7 @@ constexpr int kPfTile = 128;                        // rows of a tile, keys of a
 constexpr int kPfHalf = kPfTile * 128;              // bytes of 128 rows x 64 columns
 constexpr int kPfBuf = 2 * kPfHalf;                 // a tile or block: 32 KB
 constexpr int kPfStages = 5;
+constexpr int kPfAhead = 4;                         // PAGED: blocks that are fetched into L2 before they are loaded
 constexpr int kPfItems = 4;                         // items handed out and not yet taken by every warp
 constexpr int kPfThreads = 384;
 constexpr uint32_t kPfTmem = 512;                   // S0 | S1 | O0 | O1, 128 columns each
@@ -204,89 +206,26 @@ __device__ __forceinline__ bool pf_wait(uint64_t* bar, uint32_t parity, const vo
     return __all_sync(0xffffffffu, ptx::mbar_try_wait(bar, parity)) || ptx::warp_wait(bar, parity, abort);
 }
 
-// PAGED.  What group r of sequences shares: its sequences [q0, q0 + n), the keys of its prefix and their blocks.
-struct Group {
-    int q0, n, len, nb, pairs;
-    __device__ __forceinline__ Group(const PfArgs& A, int r) : q0(0), n(0), len(0), nb(0), pairs(0) {
-        if (r >= A.px.groups) return;
-        const int batch = A.io.total_q;
-        q0 = min(max(__ldg(&A.px.cu[r]), 0), batch);
-        n = max(min(max(__ldg(&A.px.cu[r + 1]), 0), batch) - q0, 0);
-        len = min(max(__ldg(&A.px.lens[r]), 0), A.px.max_prefix);
-        nb = (len + kPfTile - 1) / kPfTile;
-        pairs = (n + 2 * A.nq - 1) / (2 * A.nq);
-    }
-    // Places of an item in the list of all blocks: ahead of its blocks stand some for what beginning and ending it takes.
-    static constexpr int kCost = 1;
-    __device__ __forceinline__ int places() const { return nb && pairs ? nb + kCost : 0; }
-    // Row of the sums of the first query of an item's pair, without 2 kPfTile for each CTA before the one that leaves them.
-    __device__ __forceinline__ int first_row(const PfArgs& A, int h, int pair) const {
-        return q0 * A.io.Hq + (h * n + pair * 2 * A.nq) * A.g;
-    }
-};
-
-// The list as a warp sees it: lane l holds the groups l * per .. l * per + per - 1, over all heads and pairs.
-struct GroupList {
-    int per;
-    long long before, mine, total;   // places: of the lanes before, of this lane, of all
-    __device__ __forceinline__ GroupList(const PfArgs& A) : per((A.px.groups + 31) >> 5), before(0), mine(0), total(0) {
-        const int lane = threadIdx.x & 31;
-        for (int k = 0; k < per; ++k) {
-            const Group gr(A, lane * per + k);
-            mine += (long long)gr.places() * gr.pairs * A.io.Hkv;
-        }
-        long long upto = mine;
-#pragma unroll
-        for (int o = 1; o < 32; o <<= 1) {
-            const long long y = __shfl_up_sync(0xffffffffu, upto, o);
-            if (lane >= o) upto += y;
-        }
-        before = upto - mine;
-        total = __shfl_sync(0xffffffffu, upto, 31);
-    }
-    // The group of place `at` < total, which becomes the place within the group.
-    __device__ __forceinline__ int group_at(const PfArgs& A, long long& at) const {
-        const int l = __ffs(__ballot_sync(0xffffffffu, at < before + mine)) - 1;
-        at -= __shfl_sync(0xffffffffu, before, l);
-        for (int r = l * per;; ++r) {
-            const Group gr(A, r);
-            const long long here = (long long)gr.places() * gr.pairs * A.io.Hkv;
-            if (at < here) return r;
-            at -= here;
-        }
-    }
-    __device__ __forceinline__ long long places_before(const PfArgs& A, int r) const {
-        const int l = r / per;
-        long long b = __shfl_sync(0xffffffffu, before, l);
-        for (int k = l * per; k < r; ++k) {
-            const Group gr(A, k);
-            b += (long long)gr.places() * gr.pairs * A.io.Hkv;
-        }
-        return b;
-    }
-};
-__device__ __forceinline__ long long group_share(long long total, int cta, int ctas) { return total * cta / ctas; }
-
 // The items of this CTA's share, in order.
 struct GroupWalk {
     const PfArgs& A;
-    Group gr;
+    PrefixGroup gr;
     int r = 0, item = 0, i = 0;   // the next place: the i-th of an item
     long long left = 0;
-    __device__ __forceinline__ GroupWalk(const PfArgs& args) : A(args), gr(args, args.px.groups) {
-        const GroupList list(A);
+    __device__ __forceinline__ GroupWalk(const PfArgs& args) : A(args), gr(args.px.geom, args.px.geom.groups) {
+        const GroupList list(A.px.geom);
         long long at = group_share(list.total, blockIdx.x, gridDim.x);
         left = group_share(list.total, blockIdx.x + 1, gridDim.x) - at;
         if (left == 0) return;
-        r = list.group_at(A, at);
-        gr = Group(A, r);
+        r = list.group_at(A.px.geom, at);
+        gr = PrefixGroup(A.px.geom, r);
         item = (int)(at / gr.places());
         i = (int)(at - (long long)item * gr.places());
     }
     __device__ __forceinline__ bool next(Item& w) {
-        while (left > 0 && r < A.px.groups) {
+        while (left > 0 && r < A.px.geom.groups) {
             const int take = (int)min((long long)(gr.places() - i), left);
-            const int b0 = max(i - Group::kCost, 0), b1 = max(i + take - Group::kCost, 0);
+            const int b0 = max(i - PrefixGroup::kCost, 0), b1 = max(i + take - PrefixGroup::kCost, 0);
             const int pair = item % gr.pairs;
             w.h = item / gr.pairs;
             w.q0 = gr.q0;
@@ -298,7 +237,7 @@ struct GroupWalk {
             w.nsink = w.lo = 0;
             w.i0 = b0;
             w.n = b1 - b0;
-            w.place = gr.first_row(A, w.h, pair) + 2 * kPfTile * (int)blockIdx.x;
+            w.place = gr.first_row(A.px.geom, w.h, pair) + 2 * kPfTile * (int)blockIdx.x;
             w.whole_lo = -b0;
             w.whole_hi = gr.len / kPfTile - b0;
             left -= take;
@@ -307,8 +246,8 @@ struct GroupWalk {
                 i = 0;
                 if (++item == gr.pairs * A.io.Hkv) {
                     item = 0;
-                    do gr = Group(A, ++r);
-                    while (gr.places() == 0 && r < A.px.groups);
+                    do gr = PrefixGroup(A.px.geom, ++r);
+                    while (gr.places() == 0 && r < A.px.geom.groups);
                 }
             }
             if (w.n > 0) return true;
@@ -527,10 +466,9 @@ __global__ void __launch_bounds__(kPfThreads, 1) prefill_kernel(const __grid_con
     ptx::tc_fence_before();
     __syncthreads();
     ptx::tc_fence_after();
-    // PAGED: the kernels behind this one read the call's inputs before they wait: the trigger comes when these are complete.
-    if constexpr (!PAGED) asm volatile("griddepcontrol.launch_dependents;\n" ::: "memory");
-    asm volatile("griddepcontrol.wait;\n" ::: "memory");
-    if constexpr (PAGED) asm volatile("griddepcontrol.launch_dependents;\n" ::: "memory");
+    // PAGED: nothing of the kernel before this one is needed, which let others start when all before it was complete.
+    asm volatile("griddepcontrol.launch_dependents;\n" ::: "memory");
+    if constexpr (!PAGED) asm volatile("griddepcontrol.wait;\n" ::: "memory");
     const uint32_t tmem = (uint32_t)ptx::warp_uniform((int)bars->tmem_base);
     const volatile int* const abort = &bars->abort_flag;
     const int sinks = A.io.sinks;
@@ -606,6 +544,17 @@ __global__ void __launch_bounds__(kPfThreads, 1) prefill_kernel(const __grid_con
                         piece = (lane >> 1) << A.page_log < kPfTile ? prefix_row(A, w.k0, w.h, key, w.off) : -1;
                     }
                 };
+                // Into L2 ahead of the ring, which holds too little to cover the memory's latency.
+                auto fetch = [&](int i) {
+                    if constexpr (PAGED) {
+                        const int at = (lane >> 1) << A.page_log;
+                        if (i >= w.n || at >= kPfTile) return;
+                        const int row = prefix_row(A, w.k0, w.h, w.block(i) * kPfTile + at, w.off);
+                        if (row < 0) return;
+                        ptx::tma_prefetch_2d(&A.kmap, (lane & 1) * 64, row);
+                        ptx::tma_prefetch_2d(&A.vmap, (lane & 1) * 64, row);
+                    }
+                };
                 find_piece(0);
                 auto load_kv = [&](int y) {   // load y of the item: K and V blocks alternate
                     const int st = x % kPfStages, round = x / kPfStages;
@@ -622,7 +571,11 @@ __global__ void __launch_bounds__(kPfThreads, 1) prefill_kernel(const __grid_con
                             ptx::tma_load_2d(ring + st * kPfBuf + (lane & 1) * kPfHalf + at * 128, y & 1 ? &A.vmap : &A.kmap,
                                              &bars->full[st], (lane & 1) * 64, piece < 0 ? A.px.rows : piece);
                         __syncwarp();
-                        if ((y & 1) && (y >> 1) + 1 < w.n) find_piece((y >> 1) + 1);
+                        if (y & 1) {
+                            fetch((y >> 1) + kPfAhead);
+                            __syncwarp();
+                            if ((y >> 1) + 1 < w.n) find_piece((y >> 1) + 1);
+                        }
                     } else if (ptx::elect_one()) {
                         const CUtensorMap* map = y & 1 ? &A.vmap : &A.kmap;
                         uint8_t* dst = ring + st * kPfBuf;
@@ -648,6 +601,10 @@ __global__ void __launch_bounds__(kPfThreads, 1) prefill_kernel(const __grid_con
                 }
                 __syncwarp();
                 ++qloads;
+                if constexpr (PAGED) {
+                    for (int i = 2; i < kPfAhead; ++i) fetch(i);
+                    __syncwarp();
+                }
                 load_kv(1);
                 if (!stop) hand_out(turn + 1);
                 for (int y = 2; y < 2 * w.n && !stop; ++y) load_kv(y);
@@ -1058,6 +1015,8 @@ __global__ void __launch_bounds__(kPfThreads, 1) prefill_kernel(const __grid_con
         }
         give_up();
     }
+    // Complete only behind the kernel before: the next one waits for this grid alone.
+    if constexpr (PAGED) asm volatile("griddepcontrol.wait;\n" ::: "memory");
     __syncthreads();
     if (warp == 9) ptx::tmem_dealloc(tmem, kPfTmem);
 }
@@ -1093,71 +1052,6 @@ __global__ void __launch_bounds__(32 * kPjWarps) prefill_join_kernel(const __gri
     reinterpret_cast<uint2*>(A.io.out + at * kHeadDim)[lane] =
         some ? make_uint2(Half16<T>::pack(o.x * inv, o.y * inv), Half16<T>::pack(o.z * inv, o.w * inv)) : make_uint2(0u, 0u);
     if (lane == 0 && A.io.lse) A.io.lse[at] = some ? fmaf(M, 0.6931471805599453f, logf(L)) : -INFINITY;
-}
-
-// What the shares of a prefix sum up to for each row: a warp a (sequence, query head), four dimensions a lane.  The
-// maxima and sums of up to 32 shares are read by a lane each.
-constexpr int kXjWarps = 4;
-__global__ void __launch_bounds__(32 * kXjWarps) prefix_join_kernel(const __grid_constant__ PfArgs A, int ctas) {
-    asm volatile("griddepcontrol.launch_dependents;\n" ::: "memory");
-    const int lane = threadIdx.x & 31, row = blockIdx.x * kXjWarps + (threadIdx.x >> 5);
-    const int s = row / A.io.Hq, hq = row - s * A.io.Hq, h = hq / A.g;
-    // The lengths were complete before the kernel that this one waits for began.
-    int lo = 0, hi = A.px.groups;   // the last group that begins at or before s
-    while (lo < hi) {
-        const int mid = (lo + hi + 1) >> 1;
-        if (__ldg(&A.px.cu[mid]) <= s) lo = mid; else hi = mid - 1;
-    }
-    const Group gr(A, lo);
-    const bool some = s < A.io.total_q && gr.places() > 0 && s >= gr.q0 && s < gr.q0 + gr.n;   // behind the last group there is none
-    int c0 = 0, c1 = -1, base = 0;
-    const GroupList list(A);
-    if (some) {
-        const int seat = s - gr.q0, pair = seat / (2 * A.nq);
-        const long long at = list.places_before(A, lo) + (long long)(h * gr.pairs + pair) * gr.places() + Group::kCost;
-        c0 = (int)(((at + 1) * ctas - 1) / list.total);
-        c1 = (int)(((at + gr.nb) * ctas - 1) / list.total);
-        base = gr.first_row(A, h, pair) + (seat - pair * 2 * A.nq) * A.g + hq - h * A.g;
-    }
-    asm volatile("griddepcontrol.wait;\n" ::: "memory");
-    if (s >= A.io.total_q) return;
-    float M = kNoLogit, L = 0.f;
-    float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
-    for (int c = c0; c <= c1; c += 32) {
-        const int cta = c + lane;
-        // A CTA of an empty share (there are more CTAs than blocks) leaves nothing.
-        const bool here = cta <= c1 && group_share(list.total, cta, ctas) < group_share(list.total, cta + 1, ctas);
-        const float2 ml = here ? A.part_ml[base + 2 * kPfTile * cta] : make_float2(kNoLogit, 0.f);
-        float m = ml.x;
-#pragma unroll
-        for (int d = 16; d; d >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, d));
-        m = fmaxf(m, M);
-        const float f = ptx::ex2(M - m);
-        L *= f;
-        o = make_float4(o.x * f, o.y * f, o.z * f, o.w * f);
-        M = m;
-        const float w = here ? ptx::ex2(ml.x - m) : 0.f;
-        // Eight shares' sums are read at once.
-        const int n = min(32, c1 - c + 1);
-        const uint32_t there = __ballot_sync(0xffffffffu, here);
-        for (int k0 = 0; k0 < n; k0 += 8) {
-            float4 v[8];
-            float wk[8];
-#pragma unroll
-            for (int k = 0; k < 8; ++k) {
-                const bool one = (there >> (k0 + k)) & 1u;   // k0 + k < 32
-                v[k] = one ? reinterpret_cast<const float4*>(A.part_o + (size_t)(base + 2 * kPfTile * (c + k0 + k)) * kHeadDim)[lane]
-                           : make_float4(0.f, 0.f, 0.f, 0.f);
-                wk[k] = __shfl_sync(0xffffffffu, w, k0 + k);
-                L = fmaf(wk[k], __shfl_sync(0xffffffffu, ml.y, k0 + k), L);
-            }
-#pragma unroll
-            for (int k = 0; k < 8; ++k)
-                o = make_float4(fmaf(wk[k], v[k].x, o.x), fmaf(wk[k], v[k].y, o.y), fmaf(wk[k], v[k].z, o.z), fmaf(wk[k], v[k].w, o.w));
-        }
-    }
-    reinterpret_cast<float4*>(A.px.out + (size_t)row * kHeadDim)[lane] = o;
-    if (lane == 0) A.px.ml[row] = make_float2(M, L);
 }
 
 template <class T>
@@ -1250,32 +1144,26 @@ cudaError_t launch_prefill(const PrefillIO& io, const PrefillPlan& plan, int num
     return io.dtype == 1 ? launch_typed<__half>(a, plan.used_pairs, num_sms, st) : launch_typed<__nv_bfloat16>(a, plan.used_pairs, num_sms, st);
 }
 
-// Sums of the shares: a row for every query row, and a pair of tiles more for every CTA, as the items of a list may
-// each end in one and go on in the next.
-size_t prefix_scratch(int batch, int Hq, int num_sms) {
-    return ((size_t)batch * Hq + (size_t)2 * kPfTile * num_sms) * (kHeadDim * sizeof(float) + sizeof(float2));
-}
-
 cudaError_t launch_prefix(const PrefixIO& px, int num_sms, cudaStream_t st) {
     PfArgs a{};
+    const PrefixGeom& geom = px.geom;
     a.px = px;
-    a.io.Hq = px.Hq;
-    a.io.Hkv = px.Hkv;
-    a.io.total_q = px.batch;
+    a.io.Hq = geom.Hq;
+    a.io.Hkv = geom.Hkv;
+    a.io.total_q = geom.batch;
     a.io.err = px.err;
-    a.g = px.Hq / px.Hkv;
-    a.nq = kPfTile / a.g;
+    a.g = geom.g;
+    a.nq = geom.nq;
     a.parts = 1;
     a.page_log = std::min(px.c.log_page, 7);
-    static_assert(kPfTile == 1 << 7, "a block's keys");
-    a.px.rows = (int)(((long long)px.c.num_pages * px.Hkv) << px.c.log_page);
-    const size_t rows = (size_t)px.batch * px.Hq + (size_t)2 * kPfTile * num_sms;
-    a.part_o = static_cast<float*>(px.scratch);
-    a.part_ml = reinterpret_cast<float2*>(a.part_o + rows * kHeadDim);
+    static_assert(kPfTile == kPrefixTile && kPfTile == 1 << 7, "a block's keys");
+    a.px.rows = (int)(((long long)px.c.num_pages * geom.Hkv) << px.c.log_page);
+    a.part_o = px.part_o;
+    a.part_ml = px.part_ml;
     a.sl2 = px.scale * 1.4426950408889634f;
     a.fault = test_fault() == 4 ? 1 : 0;
     const uint64_t row = (uint64_t)kHeadDim * 2;
-    const uint64_t qd[3] = {(uint64_t)kHeadDim, (uint64_t)px.Hq, (uint64_t)px.batch}, qs[2] = {row, row * px.Hq};
+    const uint64_t qd[3] = {(uint64_t)kHeadDim, (uint64_t)geom.Hq, (uint64_t)geom.batch}, qs[2] = {row, row * geom.Hq};
     const uint32_t qb[3] = {64, (uint32_t)a.g, (uint32_t)a.nq};
     const uint64_t kd[2] = {(uint64_t)kHeadDim, (uint64_t)a.px.rows}, ks[1] = {row};
     const uint32_t kb[2] = {64, 1u << a.page_log};
@@ -1283,12 +1171,9 @@ cudaError_t launch_prefix(const PrefixIO& px, int num_sms, cudaStream_t st) {
     if (e == cudaSuccess) e = encode_tensor_map(&a.kmap, px.c.dtype, 2, px.c.k, kd, ks, kb);
     if (e == cudaSuccess) e = encode_tensor_map(&a.vmap, px.c.dtype, 2, px.c.v, kd, ks, kb);
     if (e != cudaSuccess) return e;
-    e = px.c.dtype == 1
-            ? launch_prio(prefill_kernel<__half, true, false, true>, dim3(num_sms), dim3(kPfThreads), kPfSmem, st, 0, true, a)
-            : launch_prio(prefill_kernel<__nv_bfloat16, true, false, true>, dim3(num_sms), dim3(kPfThreads), kPfSmem, st, 0, true, a);
-    if (e != cudaSuccess) return e;
-    const dim3 grid((unsigned)(((long long)px.batch * px.Hq + kXjWarps - 1) / kXjWarps));
-    return launch_prio(prefix_join_kernel, grid, dim3(32 * kXjWarps), 0, st, 0, true, a, num_sms);
+    return px.c.dtype == 1
+               ? launch_prio(prefill_kernel<__half, true, false, true>, dim3(num_sms), dim3(kPfThreads), kPfSmem, st, 0, true, a)
+               : launch_prio(prefill_kernel<__nv_bfloat16, true, false, true>, dim3(num_sms), dim3(kPfThreads), kPfSmem, st, 0, true, a);
 }
 
 }  // namespace kvec
