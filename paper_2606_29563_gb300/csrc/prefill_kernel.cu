@@ -66,7 +66,6 @@ constexpr int kPfTile = 128;                        // rows of a tile, keys of a
 constexpr int kPfHalf = kPfTile * 128;              // bytes of 128 rows x 64 columns
 constexpr int kPfBuf = 2 * kPfHalf;                 // a tile or block: 32 KB
 constexpr int kPfStages = 5;
-constexpr int kPfAhead = 4;                         // PAGED: blocks that are fetched into L2 before they are loaded
 constexpr int kPfItems = 4;                         // items handed out and not yet taken by every warp
 constexpr int kPfThreads = 384;
 constexpr uint32_t kPfTmem = 512;                   // S0 | S1 | O0 | O1, 128 columns each
@@ -212,7 +211,7 @@ struct GroupWalk {
     PrefixGroup gr;
     int r = 0, item = 0, i = 0;   // the next place: the i-th of an item
     long long left = 0;
-    __device__ __forceinline__ GroupWalk(const PfArgs& args) : A(args), gr(args.px.geom, args.px.geom.groups) {
+    __device__ __forceinline__ GroupWalk(const PfArgs& args, int) : A(args), gr(args.px.geom, args.px.geom.groups) {
         const GroupList list(A.px.geom);
         long long at = group_share(list.total, blockIdx.x, gridDim.x);
         left = group_share(list.total, blockIdx.x + 1, gridDim.x) - at;
@@ -254,9 +253,6 @@ struct GroupWalk {
         }
         return false;
     }
-};
-struct NoWalk {
-    __device__ __forceinline__ NoWalk(const PfArgs&) {}
 };
 
 // PAGED.  First row of KV head h from key `key` of group r's prefix on, in the pages seen as rows; -1 past it or on no page.
@@ -421,11 +417,12 @@ __device__ __forceinline__ uint32_t unbounded_mask(uint32_t w) {   // the halves
 // PARTS: a pair's blocks are divided into several items, which leave sums for prefill_join_kernel.
 // RAGGED: the CTAs share out the items, which the TMA warp finds and hands to the others, instead
 // of the places for them, of which shorter sequences leave many unused.
-// PAGED: a group's prefix instead of sequences (see the top); PARTS too.
+// PAGED: a group's prefix instead of sequences (see the top); PARTS and RAGGED too.  (Walked by every warp, the list
+// costs the softmax registers: a block of both tiles 2.1 us.)
 template <class T, bool PARTS, bool RAGGED, bool PAGED>
 __global__ void __launch_bounds__(kPfThreads, 1) prefill_kernel(const __grid_constant__ PfArgs A) {
-    static_assert(!(PARTS && RAGGED), "items that are parts have a place each");
-    static_assert(PARTS || !PAGED, "shares of a prefix are parts");
+    static_assert(!(PARTS && RAGGED) || PAGED, "items that are parts have a place each");
+    static_assert((PARTS && RAGGED) || !PAGED, "shares of a prefix are parts, and handed out");
     extern __shared__ uint8_t pf_smem_raw[];
     // 1024-byte alignment for the swizzled operand tiles.
     uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(pf_smem_raw) + 1023) & ~uintptr_t(1023));
@@ -482,9 +479,7 @@ __global__ void __launch_bounds__(kPfThreads, 1) prefill_kernel(const __grid_con
     // The next item, the same for every warp; false: none is left.
     int taken = 0;
     const int turns = (A.items + gridDim.x - 1) / gridDim.x;
-    std::conditional_t<PAGED, GroupWalk, NoWalk> walk(A);
     auto take_item = [&](Item& w) {
-        if constexpr (PAGED) return walk.next(w);
         if constexpr (!RAGGED) {
             while (taken < turns)
                 if (item_at<PARTS>(A, item_of(taken++), w)) return true;
@@ -510,11 +505,16 @@ __global__ void __launch_bounds__(kPfThreads, 1) prefill_kernel(const __grid_con
             const uint64_t policy = ptx::policy_evict_normal();
             int qloads = 0;
             // The CTA's item of a turn, handed out while the one before is loaded.
-            auto hand_out = [&, finder = std::conditional_t<RAGGED, Finder, NoFinder>(A, lane)](int turn) mutable {
+            using Source = std::conditional_t<PAGED, GroupWalk, std::conditional_t<RAGGED, Finder, NoFinder>>;
+            auto hand_out = [&, finder = Source(A, lane)](int turn) mutable {
                 if constexpr (RAGGED) {
                     const int slot = turn % kPfItems;
                     Item w{};
-                    if (!finder.find(item_of(turn), w)) w.n = -1;
+                    if constexpr (PAGED) {
+                        if (!finder.next(w)) w.n = -1;
+                    } else {
+                        if (!finder.find(item_of(turn), w)) w.n = -1;
+                    }
                     if (turn >= kPfItems && !pf_wait(&bars->item_empty[slot], (turn / kPfItems - 1) & 1, abort)) stop = true;
                     if (!stop && lane == 0) {
                         bars->items[slot] = w;
@@ -544,17 +544,6 @@ __global__ void __launch_bounds__(kPfThreads, 1) prefill_kernel(const __grid_con
                         piece = (lane >> 1) << A.page_log < kPfTile ? prefix_row(A, w.k0, w.h, key, w.off) : -1;
                     }
                 };
-                // Into L2 ahead of the ring, which holds too little to cover the memory's latency.
-                auto fetch = [&](int i) {
-                    if constexpr (PAGED) {
-                        const int at = (lane >> 1) << A.page_log;
-                        if (i >= w.n || at >= kPfTile) return;
-                        const int row = prefix_row(A, w.k0, w.h, w.block(i) * kPfTile + at, w.off);
-                        if (row < 0) return;
-                        ptx::tma_prefetch_2d(&A.kmap, (lane & 1) * 64, row);
-                        ptx::tma_prefetch_2d(&A.vmap, (lane & 1) * 64, row);
-                    }
-                };
                 find_piece(0);
                 auto load_kv = [&](int y) {   // load y of the item: K and V blocks alternate
                     const int st = x % kPfStages, round = x / kPfStages;
@@ -571,11 +560,7 @@ __global__ void __launch_bounds__(kPfThreads, 1) prefill_kernel(const __grid_con
                             ptx::tma_load_2d(ring + st * kPfBuf + (lane & 1) * kPfHalf + at * 128, y & 1 ? &A.vmap : &A.kmap,
                                              &bars->full[st], (lane & 1) * 64, piece < 0 ? A.px.rows : piece);
                         __syncwarp();
-                        if (y & 1) {
-                            fetch((y >> 1) + kPfAhead);
-                            __syncwarp();
-                            if ((y >> 1) + 1 < w.n) find_piece((y >> 1) + 1);
-                        }
+                        if ((y & 1) && (y >> 1) + 1 < w.n) find_piece((y >> 1) + 1);
                     } else if (ptx::elect_one()) {
                         const CUtensorMap* map = y & 1 ? &A.vmap : &A.kmap;
                         uint8_t* dst = ring + st * kPfBuf;
@@ -601,10 +586,6 @@ __global__ void __launch_bounds__(kPfThreads, 1) prefill_kernel(const __grid_con
                 }
                 __syncwarp();
                 ++qloads;
-                if constexpr (PAGED) {
-                    for (int i = 2; i < kPfAhead; ++i) fetch(i);
-                    __syncwarp();
-                }
                 load_kv(1);
                 if (!stop) hand_out(turn + 1);
                 for (int y = 2; y < 2 * w.n && !stop; ++y) load_kv(y);
@@ -1092,8 +1073,8 @@ cudaError_t configure_prefill() {
     one(prefill_kernel<__half, false, false, false>);
     one(prefill_kernel<__half, false, true, false>);
     one(prefill_kernel<__half, true, false, false>);
-    one(prefill_kernel<__nv_bfloat16, true, false, true>);
-    one(prefill_kernel<__half, true, false, true>);
+    one(prefill_kernel<__nv_bfloat16, true, true, true>);
+    one(prefill_kernel<__half, true, true, true>);
     return e;
 }
 
@@ -1172,8 +1153,8 @@ cudaError_t launch_prefix(const PrefixIO& px, int num_sms, cudaStream_t st) {
     if (e == cudaSuccess) e = encode_tensor_map(&a.vmap, px.c.dtype, 2, px.c.v, kd, ks, kb);
     if (e != cudaSuccess) return e;
     return px.c.dtype == 1
-               ? launch_prio(prefill_kernel<__half, true, false, true>, dim3(num_sms), dim3(kPfThreads), kPfSmem, st, 0, true, a)
-               : launch_prio(prefill_kernel<__nv_bfloat16, true, false, true>, dim3(num_sms), dim3(kPfThreads), kPfSmem, st, 0, true, a);
+               ? launch_prio(prefill_kernel<__half, true, true, true>, dim3(num_sms), dim3(kPfThreads), kPfSmem, st, 0, true, a)
+               : launch_prio(prefill_kernel<__nv_bfloat16, true, true, true>, dim3(num_sms), dim3(kPfThreads), kPfSmem, st, 0, true, a);
 }
 
 }  // namespace kvec
