@@ -444,9 +444,9 @@ KVEC_API kvec_status kvec_rotate_append_quant(kvec_handle* h, const kvec_rotate_
                                               const kvec_paged_scales* scales, kvec_stream_t stream);
 
 /* kvec_paged_decode over such a cache: keys and values count as the exact products of
- * numbers and scales.  A query enters as it is, but for at most 2^-21 of its row's largest
- * magnitude, a weight but for 2^-22 of itself.  A scale may be any fp32 number; a query row
- * that holds an infinity or NaN gives NaN.  scratch: kvec_paged_decode_quant_bytes bytes. */
+ * numbers and scales.  A query of bf16 enters as it is, but for at most 2^-39 of its row's largest
+ * magnitude, a weight but for 2^-22 of itself.  A scale may be any fp32 number.  scratch:
+ * kvec_paged_decode_quant_bytes bytes. */
 KVEC_API size_t kvec_paged_decode_quant_bytes(kvec_handle* h, int batch, int max_len, int window, int sinks,
                                               int with_weights);
 KVEC_API kvec_status kvec_paged_decode_quant(kvec_handle* h, int batch, const void* q, const kvec_paged_cache* cache,

@@ -252,16 +252,6 @@ __device__ __forceinline__ float to_range(float a) {
 }
 __device__ __forceinline__ float inverse_power(float p) { return __uint_as_float((254u << 23) - __float_as_uint(p)); }
 
-// d += A B, A 16 x 32 by rows, B 32 x 8 by columns, e4m3 with fp32 sums.
-__device__ __forceinline__ void mma_e4m3(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0,
-                                         uint32_t b1) {
-    asm volatile(
-        "mma.sync.aligned.m16n8k32.row.col.f32.e4m3.e4m3.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, "
-        "{%0, %1, %2, %3};\n"
-        : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
-        : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
-}
-
 // The products with the weights' roundings and with what these left.  Against an infinite value the rest, which is
 // zero or has either sign, would make NaN of what the roundings give alone.
 __device__ __forceinline__ float with_rest(float hi, float lo) { return fabsf(hi) < INFINITY ? hi + lo : hi; }
@@ -322,15 +312,15 @@ __device__ void add_weights(const PdArgs& A, int s, int h, const Visible<B>& v, 
 }
 
 // CL: a cluster of CTAs per pair (grid splits x Hkv x batch) instead of a share of the list.
-// E8: rows of e4m3 numbers with a scale each, which multiplies a key's logit and a value's weight.  The logits are tiles
-// of e4m3 (m16n8k32): a query row, brought to their range by a power of two, is the sum of two numbers (bf16, its 8 bits)
-// or three (fp16), so that keys go to the tiles as they are.  Values become fp16, which holds them all, on
-// their way; the weights with their scales are brought to its range by a power of two, the warp's so far.
+// E8: rows of e4m3 numbers with a scale each, which multiplies a key's logit and a value's weight.  The numbers become fp16,
+// which holds them all, on their way from shared memory to the tiles; queries of bf16 and the weights with their
+// scales are brought to its range by powers of two, a row's and the warp's so far.  (Tiles of e4m3, m16n8k32, with a
+// query as the sum of two or three numbers took more: their operands are converted too, the queries every time.)
 // OPEN: pairs' sums stay sums (own_o, own_ml), for shared_join_kernel, which adds the weights too.
 template <class T, bool CL, bool E8, bool OPEN>
 __global__ void __launch_bounds__(kPdThreads, kPdCtasPerSm) paged_decode_kernel(const __grid_constant__ PdArgs A) {
     constexpr int B = kPdBlock<E8>;
-    constexpr bool kThird = E8 && std::is_same_v<T, __half>;    // a query is the sum of three e4m3 numbers
+    constexpr bool kEarly = E8 || OPEN;                         // two blocks in flight beside the one that is worked on
     using Operand = std::conditional_t<E8, __half, T>;          // the tiles' type
     extern __shared__ uint8_t pd_smem_raw[];
     // 1024-byte alignment for the swizzled tiles.
@@ -456,43 +446,36 @@ __global__ void __launch_bounds__(kPdThreads, kPdCtasPerSm) paged_decode_kernel(
         const int len = min(count - done, v.nb - i_begin);
         const bool whole = len == v.nb;
         // The group's query rows as the upper half of the tile's row operand: head lane / 4.
-        uint32_t qa[8][2];             // E8: the lower half of it holds what the first numbers left
-        uint32_t q3[kThird ? 8 : 1];   // ... and what these left
-        float sl2 = A.sl2;             // E8: also what the row was divided by; NaN for one that holds NaN or infinities
+        uint32_t qa[8][2];
+        float sl2 = A.sl2;             // E8: also what the row was divided by
         if constexpr (E8) {
             // Columns 16 kk + 4 (lane % 4) and three more.
             const int j = lane >> 2;
             const uint2* qr =
                 reinterpret_cast<const uint2*>(A.io.q + ((size_t)s * Hq + (size_t)h * g + (j < g ? j : 0)) * kHeadDim) + (lane & 3);
-            uint2 w[8];
-            uint32_t top = 0u;         // magnitudes compare as integers, NaN the largest
 #pragma unroll
             for (int kk = 0; kk < 8; ++kk) {
-                w[kk] = j < g ? __ldg(qr + 4 * kk) : make_uint2(0u, 0u);
-                const float2 a = Half16<T>::unpack(w[kk].x), b = Half16<T>::unpack(w[kk].y);
-                top = max(max(top, __float_as_uint(fabsf(a.x))), __float_as_uint(fabsf(a.y)));
-                top = max(max(top, __float_as_uint(fabsf(b.x))), __float_as_uint(fabsf(b.y)));
+                const uint2 w = j < g ? __ldg(qr + 4 * kk) : make_uint2(0u, 0u);
+                qa[kk][0] = w.x;
+                qa[kk][1] = w.y;
             }
-            top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
-            top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
-            const float up = to_range<7>(__uint_as_float(top));
-            sl2 = __uint_as_float(top) < INFINITY ? sl2 * inverse_power(up) : __uint_as_float(0x7fc00000u);
+            if constexpr (!std::is_same_v<T, __half>) {
+                float top = 0.f;       // of the finite ones
 #pragma unroll
-            for (int kk = 0; kk < 8; ++kk) {
-                const float2 a = Half16<T>::unpack(w[kk].x), b = Half16<T>::unpack(w[kk].y);
-                float f[4] = {a.x * up, a.y * up, b.x * up, b.y * up};
-                auto part = [&]() {    // the nearest numbers; f becomes sixteen times what they leave
-                    const uint32_t n = pack_e4m3(f[0], f[1]) | pack_e4m3(f[2], f[3]) << 16;
-                    const float2 x = Half16<__half>::unpack(e4m3_to_half2(n)), y = Half16<__half>::unpack(e4m3_to_half2_upper(n));
-                    f[0] = (f[0] - x.x) * 16.f;
-                    f[1] = (f[1] - x.y) * 16.f;
-                    f[2] = (f[2] - y.x) * 16.f;
-                    f[3] = (f[3] - y.y) * 16.f;
-                    return n;
-                };
-                qa[kk][0] = part();
-                qa[kk][1] = part();
-                if constexpr (kThird) q3[kk] = part();
+                for (int kk = 0; kk < 16; ++kk) {
+                    const float2 f = Half16<T>::unpack(qa[kk >> 1][kk & 1]);
+                    top = fabsf(f.x) < INFINITY ? fmaxf(top, fabsf(f.x)) : top;
+                    top = fabsf(f.y) < INFINITY ? fmaxf(top, fabsf(f.y)) : top;
+                }
+                top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
+                top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
+                const float up = to_range<14>(top);
+                sl2 *= inverse_power(up);
+#pragma unroll
+                for (int kk = 0; kk < 16; ++kk) {
+                    const float2 f = Half16<T>::unpack(qa[kk >> 1][kk & 1]);
+                    qa[kk >> 1][kk & 1] = Half16<__half>::pack(f.x * up, f.y * up);
+                }
             }
         } else {
             const int j = lane >> 2;
@@ -520,6 +503,7 @@ __global__ void __launch_bounds__(kPdThreads, kPdCtasPerSm) paged_decode_kernel(
         for (int e = skip; e < len; e += kPdWarps) {
             const int i = i_begin + e, b = v.block(i);
             __syncwarp();
+            if constexpr (kEarly) load_next();   // into the stage that the step before freed
             const int2 rows_at = srow[warp][st];
             const int row = max(rows_at.x, rows_at.y);   // -1: nothing is there
             const uint32_t src = ring32 + st * kPdStage;
@@ -535,28 +519,20 @@ __global__ void __launch_bounds__(kPdThreads, kPdCtasPerSm) paged_decode_kernel(
 #pragma unroll
                     for (int c = 0; c < 4; ++c) x[t][c] = 0.f;
                 if constexpr (E8) {
-                    // Eight keys at a time: chunks 4 cc + lane / 8 of row lane % 8, two of them a product.
+                    // Eight keys at a time: chunks 4 cc + lane / 8 of row lane % 8.  A lane's word holds columns 4 (lane % 4) on
+                    // of a chunk: the lower two meet the tile's lower columns.
                     const int kr = lane & 7;
 #pragma unroll
-                    for (int t = 0; t < B / 8; ++t) {
-                        float y[4] = {0.f, 0.f, 0.f, 0.f};
+                    for (int cc = 0; cc < 2; ++cc)
 #pragma unroll
-                        for (int cc = 0; cc < 2; ++cc) {
+                        for (int t = 0; t < B / 8; ++t) {
                             uint32_t kb[4];
                             ldmatrix_x4(src + (8 * t + kr) * 128 + (((4 * cc + (lane >> 3)) ^ kr) << 4), kb);
 #pragma unroll
-                            for (int c = 0; c < 2; ++c) {
-                                const int kk = 4 * cc + 2 * c;
-                                mma_e4m3(x[t], qa[kk][0], qa[kk][1], qa[kk + 1][0], qa[kk + 1][1], kb[2 * c], kb[2 * c + 1]);
-                                if constexpr (kThird) mma_e4m3(y, q3[kk], 0u, q3[kk + 1], 0u, kb[2 * c], kb[2 * c + 1]);
-                            }
+                            for (int c = 0; c < 4; ++c)
+                                Half16<Operand>::mma(x[t], qa[4 * cc + c][0], 0u, qa[4 * cc + c][1], 0u, e4m3_to_half2(kb[c]),
+                                                     e4m3_to_half2_upper(kb[c]));
                         }
-#pragma unroll
-                        for (int c = 0; c < 2; ++c) {
-                            x[t][c] = fmaf(x[t][2 + c], 1.f / 16.f, x[t][c]);
-                            if constexpr (kThird) x[t][c] = fmaf(y[c], 1.f / 256.f, x[t][c]);
-                        }
-                    }
                 } else {
                     // Logits: key row (lane & 7) + 8 (lane / 16), columns 16 kk + 8 (lane / 8 % 2).
                     const int kr = (lane & 7) + ((lane >> 4) << 3);
@@ -711,7 +687,7 @@ __global__ void __launch_bounds__(kPdThreads, kPdCtasPerSm) paged_decode_kernel(
             }
             __syncwarp();   // every lane is done with the stage's tiles and row
             st = st + 1 == kPdStages ? 0 : st + 1;
-            load_next();    // into the stage that the step before freed; this step's is free now
+            if constexpr (!kEarly) load_next();    // into the stage that the step before freed; this step's is free now
         }
         // The warp's (maximum, sum, outputs), in its free stage: the one before st.
         l += __shfl_xor_sync(0xffffffffu, l, 1);
