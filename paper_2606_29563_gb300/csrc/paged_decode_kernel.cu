@@ -906,9 +906,11 @@ __global__ void __launch_bounds__(kJoinThreads, 6) paged_join_kernel(const __gri
 // (x, h, s) writes the outputs, a warp a query head, the others add the weights, kJoinRows slots each.  Sums lie as rows of
 // 128 values behind one another: the CTAs' shares of pairs, whole pairs, the prefixes' shares.  A lane reads a share's
 // maximum and sum, and eight shares' rows are read at once.
+// NT: threads, a warp for each of four heads, or of eight (64 rows of 7 heads behind 4096 slots 34.4 us with eight warps, 35.1 with
+// four; 160 of 4 heads 163 and 157).
 // one_each: every pair's own sums are whole (a cluster each); else as the list of blocks says.
-template <class T>
-__global__ void __launch_bounds__(kJoinThreads, 6) shared_join_kernel(const __grid_constant__ PdArgs A, const __grid_constant__ PrefixGeom G,
+template <class T, int NT>
+__global__ void __launch_bounds__(NT, 768 / NT) shared_join_kernel(const __grid_constant__ PdArgs A, const __grid_constant__ PrefixGeom G,
                                                                       int prefix_ctas, bool one_each) {
     constexpr int B = kPdBlock<false>;
     __shared__ float fm[kPdHeads], finv[kPdHeads];
@@ -939,7 +941,7 @@ __global__ void __launch_bounds__(kJoinThreads, 6) shared_join_kernel(const __gr
     asm volatile("griddepcontrol.launch_dependents;\n" ::: "memory");
     asm volatile("griddepcontrol.wait;\n" ::: "memory");
     if (weights && i0 >= v.nb) return;
-    for (int j = warp; j < g; j += kJoinThreads / 32) {
+    for (int j = warp; j < g; j += NT / 32) {
         float M = kNoLogit, L = 0.f;
         float4 O = make_float4(0.f, 0.f, 0.f, 0.f);
         for (int k0 = 0; k0 < n; k0 += 32) {
@@ -995,7 +997,7 @@ __global__ void __launch_bounds__(kJoinThreads, 6) shared_join_kernel(const __gr
     }
     if (!weights) return;
     __syncthreads();
-    add_weights<kJoinThreads, B>(A, s, h, v, i0, min(v.nb, i0 + kJoinRows / B), fm, finv);
+    add_weights<NT, B>(A, s, h, v, i0, min(v.nb, i0 + kJoinRows / B), fm, finv);
 }
 
 size_t round16(size_t x) { return (x + 15) & ~size_t(15); }
@@ -1055,8 +1057,11 @@ cudaError_t launch_shared_typed(const PdArgs& a, const PrefixIO& px, int num_sms
     cudaError_t e = launch_pairs<T, false, true>(a, st, &one_each);
     if (e == cudaSuccess) e = launch_prefix(px, num_sms, st);
     if (e != cudaSuccess) return e;
-    return launch_prio(shared_join_kernel<T>, dim3(1 + weight_blocks(a, kPdBlock<false>), a.io.Hkv, a.io.batch), dim3(kJoinThreads), 0,
-                       st, 0, true, a, px.geom, num_sms, one_each);
+    auto join = [&](auto kernel, int threads) {
+        return launch_prio(kernel, dim3(1 + weight_blocks(a, kPdBlock<false>), a.io.Hkv, a.io.batch), dim3(threads), 0, st, 0, true, a,
+                           px.geom, num_sms, one_each);
+    };
+    return a.g <= 4 ? join(shared_join_kernel<T, 128>, 128) : join(shared_join_kernel<T, 256>, 256);
 }
 
 // Most blocks of B slots that a sequence of up to max_len slots has in sight.
