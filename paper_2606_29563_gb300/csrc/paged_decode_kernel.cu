@@ -936,7 +936,7 @@ __global__ void __launch_bounds__(NT, 768 / NT) shared_join_kernel(const __grid_
         }
     }
     const PrefixParts parts(G, s, h, prefix_ctas);
-    const int n = own + parts.c1 - parts.c0 + 1;
+    const int n = own + parts.n;
     const int own_rows = A.ctas * 2 * kPdHeads, prefix_rows = own_rows + A.io.batch * A.io.Hq;
     asm volatile("griddepcontrol.launch_dependents;\n" ::: "memory");
     asm volatile("griddepcontrol.wait;\n" ::: "memory");
@@ -953,7 +953,7 @@ __global__ void __launch_bounds__(NT, 768 / NT) shared_join_kernel(const __grid_
                 else if (k == 0) row = (cta * 2 + (share_start(total, c0, A.ctas) < p0 ? 1 : 0)) * kPdHeads + j;
                 else if (total >= A.ctas || share_start(total, cta, A.ctas) < share_start(total, cta + 1, A.ctas)) row = cta * 2 * kPdHeads + j;
             } else if (k < n) {
-                row = parts.row(parts.c0 + k - own, prefix_ctas);
+                row = parts.row(k - own);
                 if (row >= 0) row += prefix_rows + j;
             }
             const float2 ml = row < 0 ? make_float2(kNoLogit, 0.f) : A.part_ml[row];

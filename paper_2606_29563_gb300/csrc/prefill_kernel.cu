@@ -48,8 +48,8 @@
 //
 // The same products without the causal order serve shared_decode (PAGED): the queries of the sequences
 // that share a prefix are the rows, each of which sees all of it, and K and V blocks come from the
-// prefix's pages.  The blocks of all (group, KV head, pair of tiles) form one list, as the lengths
-// are on the device; every CTA takes an even share and leaves sums for shared_join_kernel.
+// prefix's pages.  The lengths are on the device, and the CTAs share the blocks by them (prefix_list.cuh);
+// they leave sums for shared_join_kernel.
 #include <algorithm>
 #include <type_traits>
 
@@ -211,20 +211,38 @@ struct GroupWalk {
     PrefixGroup gr;
     int r = 0, item = 0, i = 0;   // the next place: the i-th of an item
     long long left = 0;
+    int chunk = -1, chunks = 0;   // or the one chunk of an item
     __device__ __forceinline__ GroupWalk(const PfArgs& args, int) : A(args), gr(args.px.geom, args.px.geom.groups) {
-        const GroupList list(A.px.geom);
-        long long at = group_share(list.total, blockIdx.x, gridDim.x);
-        left = group_share(list.total, blockIdx.x + 1, gridDim.x) - at;
+        const PrefixGeom& G = A.px.geom;
+        const GroupList list(G, gridDim.x);
+        long long at = blockIdx.x;
+        if (list.longest) {
+            left = at < list.total ? 1 : 0;
+        } else {
+            at = group_share(list.total, blockIdx.x, gridDim.x);
+            left = group_share(list.total, blockIdx.x + 1, gridDim.x) - at;
+        }
         if (left == 0) return;
-        r = list.group_at(A.px.geom, at);
-        gr = PrefixGroup(A.px.geom, r);
-        item = (int)(at / gr.places());
-        i = (int)(at - (long long)item * gr.places());
+        r = list.group_at(G, at);
+        gr = PrefixGroup(G, r);
+        if (list.longest) {
+            chunks = GroupList::chunks(gr, list.longest);
+            const int pair = (int)at % gr.pairs, hc = (int)at / gr.pairs, h = hc / chunks;
+            item = h * gr.pairs + pair;
+            chunk = hc - h * chunks;
+        } else {
+            item = (int)(at / gr.places());
+            i = (int)(at - (long long)item * gr.places());
+        }
     }
     __device__ __forceinline__ bool next(Item& w) {
         while (left > 0 && r < A.px.geom.groups) {
             const int take = (int)min((long long)(gr.places() - i), left);
-            const int b0 = max(i - PrefixGroup::kCost, 0), b1 = max(i + take - PrefixGroup::kCost, 0);
+            int b0 = max(i - PrefixGroup::kCost, 0), b1 = max(i + take - PrefixGroup::kCost, 0);
+            if (chunk >= 0) {
+                b0 = (int)((long long)gr.nb * chunk / chunks);
+                b1 = (int)((long long)gr.nb * (chunk + 1) / chunks);
+            }
             const int pair = item % gr.pairs;
             w.h = item / gr.pairs;
             w.q0 = gr.q0;
@@ -236,7 +254,7 @@ struct GroupWalk {
             w.nsink = w.lo = 0;
             w.i0 = b0;
             w.n = b1 - b0;
-            w.place = gr.first_row(A.px.geom, w.h, pair) + 2 * kPfTile * (int)blockIdx.x;
+            w.place = 2 * kPfTile * (int)blockIdx.x + (chunk >= 0 ? 0 : gr.first_row(A.px.geom, w.h, pair));
             w.whole_lo = -b0;
             w.whole_hi = gr.len / kPfTile - b0;
             left -= take;
@@ -814,6 +832,9 @@ __global__ void __launch_bounds__(kPfThreads, 1) prefill_kernel(const __grid_con
         const uint32_t lanes = (uint32_t)(quad * 32) << 16;
         const uint32_t tS = tmem + lanes + t * 128, tO = tmem + lanes + 256 + t * 128;
         const float sl2f = A.sl2;
+        // PAGED: in bf16, which holds larger ones, m moves hardly ever (a move costs 0.75 us, half a block; keys of different
+        // sizes moved it in a third of the blocks).  2^80 less 24 bits is still far from fp32's ends, in the join too.
+        constexpr float kMost = PAGED && kType<T> ? 1.2089258196146292e24f : kMostWeight;
         const uint64_t sl2 = ptx::pack_f32x2(sl2f, sl2f);
         // The infinities and NaN that a row sees in the blocks of partial sight: their weights
         // are positive, so each makes its output infinite or NaN.
@@ -904,13 +925,13 @@ __global__ void __launch_bounds__(kPfThreads, 1) prefill_kernel(const __grid_con
                 }
                 float z = weights(0);
                 z += weights(1);
-                if (__any_sync(0xffffffffu, live && !(z < kMostWeight))) {
+                if (__any_sync(0xffffffffu, live && !(z < kMost))) {
                     // The row's first logits, ones far above m, or NaN: m moves to the largest.
                     tmem_wait_st();   // these weights are written again
                     float mx = m;
 #pragma unroll
                     for (int e = 0; e < 128; e += 2) mx = max3(mx, s[e] * sl2f, s[e + 1] * sl2f);
-                    if (z < kMostWeight || !live) mx = m;
+                    if (z < kMost || !live) mx = m;
                     const float f = ptx::ex2(m - mx);
                     l *= f;
                     m = mx;
