@@ -58,17 +58,19 @@ struct GroupList {
             f(first);
             for (int k = 1; k < per; ++k) f(PrefixGroup(A, lane * per + k));
         };
-        long long blocks = 0;
-        each([&](const PrefixGroup& gr) { blocks += (long long)gr.nb * gr.pairs * A.Hkv; });
-#pragma unroll
-        for (int o = 16; o; o >>= 1) blocks += __shfl_xor_sync(0xffffffffu, blocks, o);
+        // In 32 bits: a lane's sums end at kMany, far more than there may be chunks.
+        constexpr int kMany = 1 << 25;
+        auto items = [&](const PrefixGroup& gr) { return gr.nb ? min(gr.pairs * A.Hkv, 4096) : 0; };   // of 8192 blocks at most: 2^25
+        int own = 0;
+        each([&](const PrefixGroup& gr) { own = min(own + items(gr) * gr.nb, kMany); });
+        const unsigned blocks = __reduce_add_sync(0xffffffffu, (unsigned)own);
         auto fits = [&](int length) {   // chunks of that length, a CTA each
             int n = 0;
-            each([&](const PrefixGroup& gr) { n += min((long long)chunks(gr, length) * gr.pairs * A.Hkv, 1ll << 16); });
-            return __reduce_add_sync(0xffffffffu, (unsigned)min(n, 1 << 16)) <= (unsigned)ctas;
+            each([&](const PrefixGroup& gr) { n = min(n + items(gr) * chunks(gr, length), kMany); });
+            return __reduce_add_sync(0xffffffffu, (unsigned)n) <= (unsigned)ctas;
         };
-        const int mean = (int)(blocks / ctas);   // at most 65536 groups of 8192 blocks, 256 heads and 32768 pairs: it fits
-        if (blocks > 0 && fits(mean + mean / 4 + 1)) {
+        const int mean = (int)(blocks / (unsigned)ctas);
+        if (blocks && fits(mean + mean / 4 + 1)) {
             int lo = mean > 0 ? mean : 1, hi = mean + mean / 4 + 1;
             while (lo < hi) {
                 const int mid = (lo + hi) >> 1;
