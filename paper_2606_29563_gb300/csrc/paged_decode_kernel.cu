@@ -110,17 +110,25 @@ __device__ __forceinline__ int slot_row(const PdArgs& A, int s, int h, int slot)
     return (int)((((unsigned)page * (unsigned)A.io.Hkv + (unsigned)h) << A.c.log_page) +
                  (unsigned)(slot & ((1 << A.c.log_page) - 1)));
 }
-// Rows of block b's first slot and, of two halves, of the second's (-1: it lies behind the table, or in the bound's last
-// block behind that).
+// A block's first rows, -1 where there is none: of its 16 slots, or of two halves, of which the second may lie behind the bound
+// and the table.
 template <int B>
-__device__ __forceinline__ int2 block_rows(const PdArgs& A, int s, int h, int b) {
-    int2 r = make_int2(slot_row(A, s, h, b * B), -1);
+using BlockRows = std::conditional_t<(B > kPdHalf), int2, int>;
+template <int B>
+__device__ __forceinline__ BlockRows<B> no_rows() {
+    if constexpr (B > kPdHalf) return make_int2(-1, -1);
+    else return -1;
+}
+template <int B>
+__device__ __forceinline__ BlockRows<B> block_rows(const PdArgs& A, int s, int h, int b) {
+    const int first = slot_row(A, s, h, b * B);
     if constexpr (B > kPdHalf) {
         const int slot = b * B + kPdHalf;
-        if (A.box == B) r.y = r.x < 0 ? -1 : r.x + kPdHalf;
-        else if (slot < A.io.max_len) r.y = slot_row(A, s, h, slot);
+        if (A.box == B) return make_int2(first, first < 0 ? -1 : first + kPdHalf);
+        return make_int2(first, slot < A.io.max_len ? slot_row(A, s, h, slot) : -1);
+    } else {
+        return first;
     }
-    return r;
 }
 
 // A place in the list of blocks: block i of pair (s, h).
@@ -266,10 +274,11 @@ struct SlotWeights {
     // The e-th four slots of the pair's blocks from block i0 on.
     __device__ __forceinline__ void load(const PdArgs& A, int s, int h, const Visible<B>& v, int i0, int e) {
         const int i = i0 + e / (B / 4), r = e % (B / 4) * 4, slot = v.block(i) * B + r;
+        row = slot < A.io.max_len ? slot_row(A, s, h, slot) : -1;   // past the bound the table may end
         bool any = false;
 #pragma unroll
         for (int k = 0; k < 4; ++k) any |= seen[k] = v.sees(slot + k);
-        row = any ? slot_row(A, s, h, slot) : -1;
+        row = any ? row : -1;
         if (row < 0) return;
         const float* lg = A.logits + (((size_t)s * A.io.Hkv + h) * A.nbmax + i) * (size_t)(A.g * B) + r;
 #pragma unroll
@@ -326,7 +335,7 @@ __global__ void __launch_bounds__(kPdThreads, kPdCtasPerSm) paged_decode_kernel(
     // 1024-byte alignment for the swizzled tiles.
     uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(pd_smem_raw) + 1023) & ~uintptr_t(1023));
     __shared__ __align__(8) uint64_t full[kPdWarps][kPdStages];
-    __shared__ int2 srow[kPdWarps][kPdStages];                  // first rows of the staged block's halves, -1: none
+    __shared__ BlockRows<B> srow[kPdWarps][kPdStages];          // the staged block's
     __shared__ __align__(16) float scales[kPdWarps][E8 ? kPdStages : 1][2][B];   // of the staged block's K and V
     __shared__ float wm[kPdWarps][kPdHeads], wl[kPdWarps][kPdHeads];
     __shared__ float* wacc[kPdWarps];                           // the warps' outputs, each in its free stage
@@ -384,13 +393,13 @@ __global__ void __launch_bounds__(kPdThreads, kPdCtasPerSm) paged_decode_kernel(
     int ld_at = warp, row_at = warp;      // the next load, the next row to fetch
     if (row_at < count) ld.advance(A, warp);
     auto next_row = [&]() {
-        if (row_at >= count) return make_int2(-1, -1);
-        const int2 row = block_rows<B>(A, ld.s, ld.h, ld.v.block(ld.i));
+        if (row_at >= count) return no_rows<B>();
+        const BlockRows<B> row = block_rows<B>(A, ld.s, ld.h, ld.v.block(ld.i));
         row_at += kPdWarps;
         if (row_at < count) ld.advance(A, kPdWarps);
         return row;
     };
-    int2 rows[2];
+    BlockRows<B> rows[2];
     rows[0] = next_row();
     rows[1] = next_row();
     int ld_stage = 0;
@@ -398,14 +407,14 @@ __global__ void __launch_bounds__(kPdThreads, kPdCtasPerSm) paged_decode_kernel(
     auto load_next = [&]() {
         if (ld_at < count && !failed) {
             // Warp-uniform operands: else each TMA instruction moves its own to uniform registers.
-            const int row = ptx::warp_uniform(rows[0].x), upper = E8 ? ptx::warp_uniform(rows[0].y) : -1,
-                      at = ptx::warp_uniform(ld_stage);
-            if (ptx::elect_one()) {
-                srow[warp][at] = make_int2(row, upper);
-                if ((row >= 0 || upper >= 0) && !(A.fault && warp == 0 && blockIdx.x == 0)) {
-                    uint8_t* dst = ring + at * kPdStage;
-                    uint64_t* bar = &full[warp][at];
-                    if constexpr (E8) {
+            const int at = ptx::warp_uniform(ld_stage);
+            if constexpr (E8) {
+                const int row = ptx::warp_uniform(rows[0].x), upper = ptx::warp_uniform(rows[0].y);
+                if (ptx::elect_one()) {
+                    srow[warp][at] = make_int2(row, upper);
+                    if ((row >= 0 || upper >= 0) && !(A.fault && warp == 0 && blockIdx.x == 0)) {
+                        uint8_t* dst = ring + at * kPdStage;
+                        uint64_t* bar = &full[warp][at];
                         constexpr uint32_t kHalfBytes = 2 * (kPdTile + kPdHalf * 4);
                         auto load = [&](int r, int from) {   // rows from r on, behind `from` slots of the block
                             ptx::tma_load_2d(dst + from * 128, &A.kmap, bar, 0, r);
@@ -416,7 +425,15 @@ __global__ void __launch_bounds__(kPdThreads, kPdCtasPerSm) paged_decode_kernel(
                         ptx::mbar_arrive_expect_tx(bar, row >= 0 && upper >= 0 ? 2 * kHalfBytes : kHalfBytes);
                         if (row >= 0) load(row, 0);
                         if (upper >= 0 && A.box == kPdHalf) load(upper, kPdHalf);
-                    } else {
+                    }
+                }
+            } else {
+                const int row = ptx::warp_uniform(rows[0]);
+                if (ptx::elect_one()) {
+                    srow[warp][at] = row;
+                    if (row >= 0 && !(A.fault && warp == 0 && blockIdx.x == 0)) {
+                        uint8_t* dst = ring + at * kPdStage;
+                        uint64_t* bar = &full[warp][at];
                         ptx::mbar_arrive_expect_tx(bar, kPdStage);
                         ptx::tma_load_2d(dst, &A.kmap, bar, 0, row);
                         ptx::tma_load_2d(dst + kPdTile, &A.kmap, bar, 64, row);
@@ -504,8 +521,17 @@ __global__ void __launch_bounds__(kPdThreads, kPdCtasPerSm) paged_decode_kernel(
             const int i = i_begin + e, b = v.block(i);
             __syncwarp();
             if constexpr (kEarly) load_next();   // into the stage that the step before freed
-            const int2 rows_at = srow[warp][st];
-            const int row = max(rows_at.x, rows_at.y);   // -1: nothing is there
+            const BlockRows<B> rows_at = srow[warp][st];
+            int row;                       // -1: nothing is there
+            bool here[B / kPdHalf];        // by halves
+            if constexpr (E8) {
+                row = max(rows_at.x, rows_at.y);
+                here[0] = rows_at.x >= 0;
+                here[1] = rows_at.y >= 0;
+            } else {
+                row = rows_at;
+                here[0] = row >= 0;
+            }
             const uint32_t src = ring32 + st * kPdStage;
             float x[B / 8][4];
             if (row >= 0) {
@@ -547,8 +573,7 @@ __global__ void __launch_bounds__(kPdThreads, kPdCtasPerSm) paged_decode_kernel(
                 }
             }
             // This lane's slots: 8 t + 2 (lane % 4) + c.
-            const bool here[2] = {rows_at.x >= 0, rows_at.y >= 0};       // by halves
-            const bool all = here[0] && (!E8 || here[1]) && v.whole(b);
+            const bool all = here[0] && here[B / kPdHalf - 1] && v.whole(b);
             float vs[E8 ? B / 8 : 1][2];   // the values' scales, 0 where no one sees them
             if constexpr (E8) {
 #pragma unroll
