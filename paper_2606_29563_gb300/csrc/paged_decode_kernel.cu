@@ -388,25 +388,52 @@ __global__ void __launch_bounds__(kPdThreads, kPdCtasPerSm) paged_decode_kernel(
     const uint32_t ring32 = ptx::smem_u32(ring);
     // Loads: this warp's blocks are warp, warp + 4, ... of the CTA's; load number k goes to
     // stage k % kPdStages, and one stage is free while a block is worked on.
-    // The rows of the next two are fetched ahead: a page's number takes as long as its rows.
+    // The rows of the next two are fetched ahead: a page's number takes as long as its rows.  kEarly: those of 32 at
+    // once, a lane each.
     Walker<B> ld = cur;
     int ld_at = warp, row_at = warp;      // the next load, the next row to fetch
     if (row_at < count) ld.advance(A, warp);
+    BlockRows<B> ahead = no_rows<B>();    // kEarly: of the load lane loads on from the last fetch
+    int taken = 32;
     auto next_row = [&]() {
-        if (row_at >= count) return no_rows<B>();
-        const BlockRows<B> row = block_rows<B>(A, ld.s, ld.h, ld.v.block(ld.i));
-        row_at += kPdWarps;
-        if (row_at < count) ld.advance(A, kPdWarps);
-        return row;
+        if constexpr (kEarly) {
+            if (taken == 32) {
+                taken = 0;
+                const int mine = row_at + lane * kPdWarps;
+                ahead = no_rows<B>();
+                if (mine < count) {
+                    Walker<B> w = ld;
+                    w.advance(A, lane * kPdWarps);
+                    ahead = block_rows<B>(A, w.s, w.h, w.v.block(w.i));
+                }
+                row_at += 32 * kPdWarps;
+                if (row_at < count) ld.advance(A, 32 * kPdWarps);
+                __syncwarp();
+            }
+            BlockRows<B> row;
+            if constexpr (E8) row = make_int2(__shfl_sync(0xffffffffu, ahead.x, taken), __shfl_sync(0xffffffffu, ahead.y, taken));
+            else row = __shfl_sync(0xffffffffu, ahead, taken);
+            ++taken;
+            return row;
+        } else {
+            if (row_at >= count) return no_rows<B>();
+            const BlockRows<B> row = block_rows<B>(A, ld.s, ld.h, ld.v.block(ld.i));
+            row_at += kPdWarps;
+            if (row_at < count) ld.advance(A, kPdWarps);
+            return row;
+        }
     };
     BlockRows<B> rows[2];
-    rows[0] = next_row();
-    rows[1] = next_row();
+    if constexpr (!kEarly) {
+        rows[0] = next_row();
+        rows[1] = next_row();
+    }
     int ld_stage = 0;
     bool failed = false;      // a wait gave up: no further loads and waits, outputs are invalid
     auto load_next = [&]() {
         if (ld_at < count && !failed) {
             // Warp-uniform operands: else each TMA instruction moves its own to uniform registers.
+            if constexpr (kEarly) rows[0] = next_row();
             const int at = ptx::warp_uniform(ld_stage);
             if constexpr (E8) {
                 const int row = ptx::warp_uniform(rows[0].x), upper = ptx::warp_uniform(rows[0].y);
@@ -443,8 +470,10 @@ __global__ void __launch_bounds__(kPdThreads, kPdCtasPerSm) paged_decode_kernel(
                 }
             }
             ld_at += kPdWarps;
-            rows[0] = rows[1];
-            rows[1] = next_row();
+            if constexpr (!kEarly) {
+                rows[0] = rows[1];
+                rows[1] = next_row();
+            }
         }
         ld_stage = ld_stage + 1 == kPdStages ? 0 : ld_stage + 1;
     };
