@@ -194,7 +194,9 @@ struct List {
     // block takes a CTA alone 0.25 us, all places together take 0.0013 us each, and the join and the shares'
     // ends about 5 us.  Measured, by pair and by share: 64 rows of 1024 to 2048 slots 48 and 54, 64 of
     // 200 to 3200 65 and 54, 30 of 100 to 3100 58 and 44, one of 8000 beside 31 of 500 129 and 28.
+    // 8 bits (32 slots a block): 0.43 and 0.0014 us; 64 rows of 1024 to 2048 37.9 and 39.4, 32 of 100 to 4000 50 and 39.
     __device__ __forceinline__ bool whole_pairs(const PdArgs& A) const {
+        if constexpr (B == kPdBlock<true>) return A.pairs && (long long)longest * 300 <= total + 14 * 300;
         return A.pairs && (long long)longest * 190 <= total + 20 * 190;
     }
     // The first block from place `at` on; returns how many are before it.
