@@ -1472,6 +1472,7 @@ kvec_status kvec_paged_read(kvec_handle* h, int batch, const kvec_paged_cache* c
     if (s != KVEC_OK) return s;
     if (num_rows == 0) return KVEC_OK;
     if (!cu_rows || !k_out || !v_out) return fail(KVEC_ERR_INVALID_ARG, "a device pointer is NULL");
+    if (k_out == v_out) return fail(KVEC_ERR_INVALID_ARG, "k_out and v_out must not be the same");
     if (!aligned16(k_out) || !aligned16(v_out)) return fail(KVEC_ERR_INVALID_ARG, "k_out and v_out must be 16-byte aligned");
     if (reinterpret_cast<uintptr_t>(first) % 4 || reinterpret_cast<uintptr_t>(cu_rows) % 4)
         return fail(KVEC_ERR_INVALID_ARG, "first and cu_rows must be 4-byte aligned");

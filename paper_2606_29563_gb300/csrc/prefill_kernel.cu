@@ -225,7 +225,9 @@ struct GroupWalk {
         if (left == 0) return;
         r = list.group_at(G, at);
         gr = PrefixGroup(G, r);
-        if (list.longest) {
+        if (gr.places() == 0) {
+            left = 0;
+        } else if (list.longest) {
             chunks = GroupList::chunks(gr, list.longest);
             const int pair = (int)at % gr.pairs, hc = (int)at / gr.pairs, h = hc / chunks;
             item = h * gr.pairs + pair;
@@ -234,9 +236,10 @@ struct GroupWalk {
             item = (int)(at / gr.places());
             i = (int)(at - (long long)item * gr.places());
         }
+        if (item >= gr.pairs * A.io.Hkv) left = 0;
     }
     __device__ __forceinline__ bool next(Item& w) {
-        while (left > 0 && r < A.px.geom.groups) {
+        while (left > 0 && gr.places() > i) {
             const int take = (int)min((long long)(gr.places() - i), left);
             int b0 = max(i - PrefixGroup::kCost, 0), b1 = max(i + take - PrefixGroup::kCost, 0);
             if (chunk >= 0) {

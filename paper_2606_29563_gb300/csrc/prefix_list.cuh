@@ -88,15 +88,18 @@ struct GroupList {
         before = upto - mine;
         total = __shfl_sync(0xffffffffu, upto, 31);
     }
-    // The group of chunk or place `at` < total, which becomes that within the group.
+    // The group of chunk or place `at` < total, which becomes that within the group.  (It ends whatever the lengths say: they
+    // may be written meanwhile by a program that does not wait for the call.)
     __device__ __forceinline__ int group_at(const PrefixGeom& A, long long& at) const {
         const int l = __ffs(__ballot_sync(0xffffffffu, at < before + mine)) - 1;
         at -= __shfl_sync(0xffffffffu, before, l);
-        for (int r = l * per;; ++r) {
+        int r = l * per;
+        for (; r < A.groups; ++r) {
             const long long here = part(A, PrefixGroup(A, r));
-            if (at < here) return r;
+            if (at < here) break;
             at -= here;
         }
+        return r;
     }
     // Chunks or places of the groups before r.
     __device__ __forceinline__ long long parts_before(const PrefixGeom& A, int r) const {

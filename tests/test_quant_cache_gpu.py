@@ -503,14 +503,17 @@ def test_read_matches_the_definition(dtype, Hkv, page, lens, first, extra, eight
             assert np.array_equal(f64(x), r)
 
 
-def test_read_refuses_nothing_it_need_not():
+def test_read_of_no_rows_and_of_slots_before_the_first():
     cache, _ = make_cache([5], 2, 16, torch.bfloat16, torch.Generator().manual_seed(0))
     cu = torch.tensor([0, 0], dtype=torch.int32).cuda()
     k, v = selector(4, 2).paged_read(cache, cu, 0)
     assert k.shape == v.shape == (0, 2, D)
     before = torch.tensor([-3], dtype=torch.int32).cuda()    # slots below 0 are zeros
-    k, _ = selector(4, 2).paged_read(cache, torch.tensor([0, 5], dtype=torch.int32).cuda(), 5, first=before)
+    five = torch.tensor([0, 5], dtype=torch.int32).cuda()
+    k, _ = selector(4, 2).paged_read(cache, five, 5, first=before)
     assert torch.all(k[:3] == 0) and torch.all(torch.isfinite(k)) and torch.any(k[3:] != 0)
+    with pytest.raises(kvec.KvecError):   # one place for both
+        selector(4, 2).paged_read(cache, five, 5, k_out=k, v_out=k)
 
 
 # ---------------------------------------------------------------- together, captured, on other streams

@@ -133,6 +133,14 @@ def test_the_binding_checks_a_read():
         selector(8, 4).paged_read(c, cu, 4)
 
 
+def test_the_header_names_every_entry_point():
+    header = open(kvec.os.path.join(kvec.os.path.dirname(kvec._HERE), "include", "kvec.h")).read()
+    for name in ("kvec_rotate_append_quant", "kvec_paged_decode_quant_bytes", "kvec_paged_decode_quant", "kvec_paged_evict_quant",
+                 "kvec_paged_read", "kvec_shared_decode_bytes", "kvec_shared_decode"):
+        assert name in kvec.EXPORTED and f" {name}(" in header and callable(getattr(kvec, name))
+    assert kvec.kvec_paged_decode_quant_bytes(None, 1, 64, 0, 0, True) == 0
+
+
 def test_the_binding_checks_queries_of_an_eight_bit_cache():
     sel, c = selector(), kvec.PagedCache(**tensors())
     refused(lambda: sel.paged_decode(torch.zeros((2, 8, 128), dtype=BF), c), BAD, "handle is NULL")
