@@ -49,7 +49,9 @@
 // The same products without the causal order serve shared_decode (PAGED): the queries of the sequences
 // that share a prefix are the rows, each of which sees all of it, and K and V blocks come from the
 // prefix's pages.  The lengths are on the device, and the CTAs share the blocks by them (prefix_list.cuh);
-// they leave sums for shared_join_kernel.
+// they leave sums for shared_join_kernel.  A block of both tiles takes 1.5 to 1.7 us there, as above (2.1 where bf16 maxima
+// moved at 2^14); the first S comes 4 to 6 us after the start (lengths, shares, pages, keys), and the sums of a pair of
+// tiles (128 KB a CTA) take 3 us to store.  Copies into L2 three to eight blocks ahead of the ring made it slower (164 us for 158).
 #include <algorithm>
 #include <type_traits>
 
