@@ -408,7 +408,7 @@ typedef struct {
  * but a prefix's keys and values are read for all queries of its group at once.  Keys are
  * rotated by their positions before they are stored, so own slots continue after the prefix.
  * With cache.weights the own slots' weights grow by their p_j, as there; a prefix's do not
- * (its sequences would not agree on what to evict).  The rows of 16 bits only; no window.
+ * (its sequences would not agree on what to evict).  Rows of 16 bits; no window.
  * The weights of a prefix's slots are rounded to dtype before they meet the values, as in
  * kvec_prefill_attention, those of own slots as in kvec_paged_decode.
  *   q, out     device cache.dtype [batch][H_q][d], 16-byte aligned.
@@ -458,6 +458,18 @@ KVEC_API kvec_status kvec_paged_evict_quant(kvec_handle* h, int batch, const kve
                                             const kvec_paged_scales* scales, const int32_t* new_table,
                                             int new_max_pages, int max_len, int budget, int sinks, int recent,
                                             int32_t* new_lens, int32_t* kept, kvec_stream_t stream);
+
+/* kvec_shared_decode where the sequences' own slots lie in such a cache.  The prefixes, which
+ * all queries of a group read together, stay rows of 16 bits, in a pool of their own:
+ *   pool     of the cache's dtype, its k_pages, v_pages, page_size and num_pages those that prefix's
+ *            page_table means (for instance the cache that a prefix was appended to; its other
+ *            pointers are checked as ever, and not read).
+ *   scratch  kvec_shared_decode_quant_bytes bytes, 256-byte aligned. */
+KVEC_API size_t kvec_shared_decode_quant_bytes(kvec_handle* h, int batch, int max_len, int with_weights);
+KVEC_API kvec_status kvec_shared_decode_quant(kvec_handle* h, int batch, const void* q, const kvec_paged_cache* cache,
+                                              const kvec_paged_scales* scales, const kvec_paged_cache* pool,
+                                              const kvec_shared_prefix* prefix, int max_len, int max_prefix, void* out,
+                                              void* scratch, size_t scratch_bytes, kvec_stream_t stream);
 
 /* Slots of a paged cache as packed rows of dtype, [num_rows][H_kv][d], as
  * kvec_prefill_attention takes keys and values: what a prompt's next chunk attends to.  Row

@@ -110,30 +110,33 @@ def paged_decode(q, k_pages, v_pages, weights, table, lens, max_len, window, sin
     return out
 
 
-def shared_decode(q, k_pages, v_pages, weights, table, lens, max_len, prefix_table, prefix_lens, cu, max_prefix, scale):
-    """paged_decode where sequences cu[r] .. cu[r + 1] - 1 see the slots of row r of prefix_table before their own."""
+def shared_decode(q, k_pages, v_pages, weights, table, lens, max_len, prefix_table, prefix_lens, cu, max_prefix, scale,
+                  pool=None):
+    """paged_decode where sequences cu[r] .. cu[r + 1] - 1 see the slots of row r of prefix_table before their own; these are
+    in the same pages, or in those of pool, (k, v)."""
     num_pages, Hkv, page_size, d = k_pages.shape
+    pk, pv = (k_pages, v_pages) if pool is None else pool
     batch, Hq, _ = q.shape
     g = Hq // Hkv
     out = np.zeros((batch, Hq, d))
     for s in range(batch):
         group = [r for r in range(len(cu) - 1) if cu[r] <= s < cu[r + 1]]
-        at = []
+        before = []
         if group:
             n = min(max(int(prefix_lens[group[0]]), 0), max_prefix)
-            at = [place(prefix_table[group[0]], j, page_size, num_pages) for j in range(n)]
-        shared = len([p for p in at if p is not None])
-        at += [place(table[s], j, page_size, num_pages) for j in range(min(max(int(lens[s]), 0), max_len))]
-        at = [p for p in at if p is not None]
-        if not at:
+            before = [place(prefix_table[group[0]], j, pk.shape[2], pk.shape[0]) for j in range(n)]
+        own = [place(table[s], j, page_size, num_pages) for j in range(min(max(int(lens[s]), 0), max_len))]
+        before, own = ([p for p in x if p is not None] for x in (before, own))
+        if not before and not own:
             continue
-        pages, ofs = np.array(at).T
         for h in range(Hkv):
-            k, v = k_pages[pages, h, ofs], v_pages[pages, h, ofs]
+            k = np.array([pk[p, h, o] for p, o in before] + [k_pages[p, h, o] for p, o in own])
+            v = np.array([pv[p, h, o] for p, o in before] + [v_pages[p, h, o] for p, o in own])
             p, _ = softmax(scale * (q[s, h * g:(h + 1) * g] @ k.T))
             out[s, h * g:(h + 1) * g] = p @ v
-            if weights is not None:
-                weights[pages[shared:], h, ofs[shared:]] += p.sum(axis=0)[shared:]
+            if weights is not None and own:
+                pages, ofs = np.array(own).T
+                weights[pages, h, ofs] += p.sum(axis=0)[len(before):]
     return out
 
 

@@ -1495,43 +1495,49 @@ kvec_status kvec_paged_read(kvec_handle* h, int batch, const kvec_paged_cache* c
 
 size_t kvec_shared_decode_bytes(kvec_handle* h, int batch, int max_len, int with_weights) {
     if (!h || batch < 1 || batch > h->p.max_batch || max_len < 1 || max_len > kPagedMaxLen) return 0;
-    return shared_decode_scratch(batch, h->p.num_q_heads, max_len, with_weights != 0, h->num_sms);
+    return shared_decode_scratch(batch, h->p.num_q_heads, max_len, with_weights != 0, false, h->num_sms);
 }
 
-kvec_status kvec_shared_decode(kvec_handle* h, int batch, const void* q, const kvec_paged_cache* cache,
-                               const kvec_shared_prefix* prefix, int max_len, int max_prefix, void* out, void* scratch,
-                               size_t scratch_bytes, kvec_stream_t stream) {
-    PagedCacheView v{};
-    kvec_status s = view_cache(cache, &v);
-    if (s != KVEC_OK) return s;
+size_t kvec_shared_decode_quant_bytes(kvec_handle* h, int batch, int max_len, int with_weights) {
+    if (!h || batch < 1 || batch > h->p.max_batch || max_len < 1 || max_len > kPagedMaxLen) return 0;
+    return shared_decode_scratch(batch, h->p.num_q_heads, max_len, with_weights != 0, true, h->num_sms);
+}
+
+namespace {
+
+// v: of the sequences' own slots; pool: of the prefixes, rows of 16 bits.
+kvec_status shared_decode(kvec_handle* h, int batch, const void* q, const PagedCacheView& v, const PagedCacheView& pool,
+                          const kvec_shared_prefix* prefix, int max_len, int max_prefix, void* out, void* scratch,
+                          size_t scratch_bytes, kvec_stream_t stream) {
     if (!prefix) return fail(KVEC_ERR_INVALID_ARG, "prefix is NULL");
     if (max_len < 1 || max_len > v.capacity)
         return fail(KVEC_ERR_INVALID_ARG, "max_len %d outside [1, max_pages * page_size = %d]", max_len, v.capacity);
     if (prefix->num_groups < 1 || prefix->num_groups > kMaxGridBatch)
         return fail(KVEC_ERR_INVALID_ARG, "num_groups %d outside [1, %d]", prefix->num_groups, kMaxGridBatch);
-    if (prefix->max_pages < 1 || ((long long)prefix->max_pages << v.log_page) > kPagedMaxLen)
+    if (prefix->max_pages < 1 || ((long long)prefix->max_pages << pool.log_page) > kPagedMaxLen)
         return fail(KVEC_ERR_INVALID_ARG, "need 1 <= max_pages * page_size <= %d of a prefix", kPagedMaxLen);
-    if (max_prefix < 1 || max_prefix > prefix->max_pages << v.log_page)
+    if (max_prefix < 1 || max_prefix > prefix->max_pages << pool.log_page)
         return fail(KVEC_ERR_INVALID_ARG, "max_prefix %d outside [1, max_pages * page_size = %d]", max_prefix,
-                    prefix->max_pages << v.log_page);
+                    prefix->max_pages << pool.log_page);
     if (!prefix->page_table || !prefix->lens || !prefix->cu_seqs) return fail(KVEC_ERR_INVALID_ARG, "a device pointer of the prefix is NULL");
     for (const int32_t* p : {prefix->page_table, prefix->lens, prefix->cu_seqs})
         if (reinterpret_cast<uintptr_t>(p) % 4) return fail(KVEC_ERR_INVALID_ARG, "the prefix's page_table, lens and cu_seqs must be 4-byte aligned");
-    s = check_paged_handle(h, batch, &v);
+    kvec_status s = check_paged_handle(h, batch, &v);
+    if (s == KVEC_OK) s = check_paged_handle(h, batch, &pool);
     if (s != KVEC_OK) return s;
     if (h->g > 8)
         return fail(KVEC_ERR_UNSUPPORTED, "decode attention supports up to 8 query heads per KV head (g = %d)", h->g);
     if (!q || !out || !scratch) return fail(KVEC_ERR_INVALID_ARG, "a device pointer is NULL");
     if (!aligned16(q) || !aligned16(out) || reinterpret_cast<uintptr_t>(scratch) % 256)
         return fail(KVEC_ERR_INVALID_ARG, "q and out must be 16-byte and scratch 256-byte aligned");
-    const size_t need = kvec_shared_decode_bytes(h, batch, max_len, v.weights != nullptr);
+    const size_t need = (v.k_scales ? kvec_shared_decode_quant_bytes : kvec_shared_decode_bytes)(h, batch, max_len, v.weights != nullptr);
     if (scratch_bytes < need)
         return fail(KVEC_ERR_INVALID_ARG, "scratch of %zu bytes, %zu are needed", scratch_bytes, need);
     const kvec_params& p = h->p;
     PrefixIO px{};
     px.geom = {prefix->lens, prefix->cu_seqs, prefix->num_groups, max_prefix, batch, p.num_q_heads, p.num_kv_heads, h->g, 128 / h->g};
     px.q = static_cast<const uint16_t*>(q);
-    px.c = v;
+    px.c = pool;
     px.table = prefix->page_table;
     px.max_pages = prefix->max_pages;
     px.scale = softmax_scale_of(p);
@@ -1553,6 +1559,28 @@ kvec_status kvec_shared_decode(kvec_handle* h, int batch, const void* q, const k
     cudaError_t e = launch_shared_decode(io, v, px, h->num_sms, reinterpret_cast<cudaStream_t>(stream));
     if (e != cudaSuccess) return cuda_fail(e, "shared decode launch");
     return KVEC_OK;
+}
+
+}  // namespace
+
+kvec_status kvec_shared_decode(kvec_handle* h, int batch, const void* q, const kvec_paged_cache* cache,
+                               const kvec_shared_prefix* prefix, int max_len, int max_prefix, void* out, void* scratch,
+                               size_t scratch_bytes, kvec_stream_t stream) {
+    PagedCacheView v{};
+    kvec_status s = view_cache(cache, &v);
+    return s != KVEC_OK ? s : shared_decode(h, batch, q, v, v, prefix, max_len, max_prefix, out, scratch, scratch_bytes, stream);
+}
+
+kvec_status kvec_shared_decode_quant(kvec_handle* h, int batch, const void* q, const kvec_paged_cache* cache,
+                                     const kvec_paged_scales* scales, const kvec_paged_cache* pool,
+                                     const kvec_shared_prefix* prefix, int max_len, int max_prefix, void* out, void* scratch,
+                                     size_t scratch_bytes, kvec_stream_t stream) {
+    PagedCacheView v{}, p{};
+    kvec_status s = view_quant_cache(cache, scales, &v);
+    if (s == KVEC_OK) s = view_cache(pool, &p);
+    if (s != KVEC_OK) return s;
+    if (p.dtype != v.dtype) return fail(KVEC_ERR_INVALID_ARG, "the pool's dtype differs from the cache's");
+    return shared_decode(h, batch, q, v, p, prefix, max_len, max_prefix, out, scratch, scratch_bytes, stream);
 }
 
 namespace {

@@ -196,7 +196,7 @@ struct PrefixGeom {
 struct PrefixIO {
     PrefixGeom geom;
     const uint16_t* q;        // [batch][Hq][d]
-    PagedCacheView c;         // the pool; its table and lengths are the sequences' own
+    PagedCacheView c;         // the pool, of 16 bits; its table and lengths are not looked at
     const int* table;         // [groups][max_pages]
     int max_pages;
     float scale;
@@ -341,7 +341,7 @@ cudaError_t launch_ada(const Geometry& g, const LayerIO& io, const Scratch& sc, 
 cudaError_t launch_decode(const DecodeIO& io, int num_sms, cudaStream_t st);
 cudaError_t launch_rotate(const RotateIO& io, const PagedCacheView& c, cudaStream_t st);
 cudaError_t launch_paged_decode(const PagedDecodeIO& io, const PagedCacheView& c, int num_sms, cudaStream_t st);
-size_t shared_decode_scratch(int batch, int Hq, int max_len, bool weights, int num_sms);
+size_t shared_decode_scratch(int batch, int Hq, int max_len, bool weights, bool e8, int num_sms);
 // px: but for the places of its sums.
 cudaError_t launch_shared_decode(const PagedDecodeIO& io, const PagedCacheView& c, const PrefixIO& px, int num_sms, cudaStream_t st);
 size_t paged_decode_scratch(int batch, int Hq, int max_len, int window, int sinks, bool weights, bool e8, int num_sms);

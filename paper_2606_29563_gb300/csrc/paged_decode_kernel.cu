@@ -979,10 +979,9 @@ __global__ void __launch_bounds__(kJoinThreads, 6) paged_join_kernel(const __gri
 // NT: threads, a warp for each of four heads, or of eight (64 rows of 7 heads behind 4096 slots 34.4 us with eight warps, 35.1 with
 // four; 160 of 4 heads 163 and 157).
 // one_each: every pair's own sums are whole (a cluster each); else as the list of blocks says.
-template <class T, int NT>
+template <class T, int NT, int B>
 __global__ void __launch_bounds__(NT, 768 / NT) shared_join_kernel(const __grid_constant__ PdArgs A, const __grid_constant__ PrefixGeom G,
                                                                       int prefix_ctas, bool one_each) {
-    constexpr int B = kPdBlock<false>;
     __shared__ float fm[kPdHeads], finv[kPdHeads];
     const int h = blockIdx.y, s = blockIdx.z, lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = A.g;
     // The lengths were complete before the call.
@@ -1121,17 +1120,18 @@ cudaError_t launch_typed(const PdArgs& a, cudaStream_t st) {
                        a.ctas * kPdHeads * sizeof(float2), st, 0, true, a);
 }
 
-template <class T>
+template <class T, bool E8>
 cudaError_t launch_shared_typed(const PdArgs& a, const PrefixIO& px, int num_sms, cudaStream_t st) {
+    constexpr int B = kPdBlock<E8>;
     bool one_each = false;
-    cudaError_t e = launch_pairs<T, false, true>(a, st, &one_each);
+    cudaError_t e = launch_pairs<T, E8, true>(a, st, &one_each);
     if (e == cudaSuccess) e = launch_prefix(px, num_sms, st);
     if (e != cudaSuccess) return e;
     auto join = [&](auto kernel, int threads) {
-        return launch_prio(kernel, dim3(1 + weight_blocks(a, kPdBlock<false>), a.io.Hkv, a.io.batch), dim3(threads), 0, st, 0, true, a,
+        return launch_prio(kernel, dim3(1 + weight_blocks(a, B), a.io.Hkv, a.io.batch), dim3(threads), 0, st, 0, true, a,
                            px.geom, num_sms, one_each);
     };
-    return a.g <= 4 ? join(shared_join_kernel<T, 128>, 128) : join(shared_join_kernel<T, 256>, 256);
+    return a.g <= 4 ? join(shared_join_kernel<T, 128, B>, 128) : join(shared_join_kernel<T, 256, B>, 256);
 }
 
 // Most blocks of B slots that a sequence of up to max_len slots has in sight.
@@ -1154,10 +1154,11 @@ size_t paged_decode_scratch(int batch, int Hq, int max_len, int window, int sink
 }
 
 // Rows of sums: the CTAs' shares, whole pairs, and the prefixes'.
-size_t shared_decode_scratch(int batch, int Hq, int max_len, bool weights, int num_sms) {
+size_t shared_decode_scratch(int batch, int Hq, int max_len, bool weights, bool e8, int num_sms) {
+    const int B = e8 ? kPdBlock<true> : kPdBlock<false>;
     const size_t rows = (size_t)share_ctas(num_sms) * 2 * kPdHeads + (size_t)batch * Hq * 2 + (size_t)2 * kPrefixTile * num_sms;
     size_t b = rows * kHeadDim * sizeof(float) + round16(rows * sizeof(float2));
-    if (weights) b += (size_t)batch * Hq * visible_blocks(kPdBlock<false>, max_len, 0, 0) * kPdBlock<false> * sizeof(float);
+    if (weights) b += (size_t)batch * Hq * visible_blocks(B, max_len, 0, 0) * B * sizeof(float);
     return b;
 }
 
@@ -1174,6 +1175,8 @@ cudaError_t configure_paged_decode() {
         one(paged_decode_kernel<T, false, true, false>);
         one(paged_decode_kernel<T, true, false, true>);
         one(paged_decode_kernel<T, false, false, true>);
+        one(paged_decode_kernel<T, true, true, true>);
+        one(paged_decode_kernel<T, false, true, true>);
     };
     both(__nv_bfloat16{});
     both(__half{});
@@ -1238,7 +1241,11 @@ cudaError_t launch_shared_decode(const PagedDecodeIO& io, const PagedCacheView& 
     PrefixIO px = prefix;
     px.part_o = a.own_o + pairs * kHeadDim;
     px.part_ml = a.own_ml + pairs;
-    return c.dtype == 1 ? launch_shared_typed<__half>(a, px, num_sms, st) : launch_shared_typed<__nv_bfloat16>(a, px, num_sms, st);
+    auto launch = [&](auto type) {
+        using T = decltype(type);
+        return c.k_scales ? launch_shared_typed<T, true>(a, px, num_sms, st) : launch_shared_typed<T, false>(a, px, num_sms, st);
+    };
+    return c.dtype == 1 ? launch(__half{}) : launch(__nv_bfloat16{});
 }
 
 }  // namespace kvec

@@ -33,7 +33,8 @@ EXPORTED = ("kvec_create", "kvec_destroy", "kvec_state_bytes", "kvec_reset", "kv
             "kvec_rotate_append", "kvec_paged_decode_bytes", "kvec_paged_decode_window_bytes", "kvec_paged_decode",
             "kvec_paged_evict", "kvec_prefill_bytes", "kvec_prefill_attention", "kvec_rotate_append_quant",
             "kvec_paged_decode_quant", "kvec_paged_evict_quant", "kvec_paged_read", "kvec_shared_decode_bytes",
-            "kvec_shared_decode", "kvec_paged_decode_quant_bytes")
+            "kvec_shared_decode", "kvec_paged_decode_quant_bytes", "kvec_shared_decode_quant_bytes",
+            "kvec_shared_decode_quant")
 
 KVEC_BF16 = 0
 KVEC_FP16 = 1
@@ -157,6 +158,10 @@ def load() -> ctypes.CDLL:
                                         i, i, i, i, i, _vp, _vp, _vp], st),
             "kvec_paged_decode_quant_bytes": ([_vp, i, i, i, i, i], ctypes.c_size_t),
             "kvec_shared_decode_bytes": ([_vp, i, i, i], ctypes.c_size_t),
+            "kvec_shared_decode_quant_bytes": ([_vp, i, i, i], ctypes.c_size_t),
+            "kvec_shared_decode_quant": ([_vp, i, _vp, ctypes.POINTER(kvec_paged_cache), ctypes.POINTER(kvec_paged_scales),
+                                          ctypes.POINTER(kvec_paged_cache), ctypes.POINTER(kvec_shared_prefix), i, i, _vp,
+                                          _vp, ctypes.c_size_t, _vp], st),
             "kvec_shared_decode": ([_vp, i, _vp, ctypes.POINTER(kvec_paged_cache), ctypes.POINTER(kvec_shared_prefix), i, i,
                                     _vp, _vp, ctypes.c_size_t, _vp], st),
             "kvec_paged_read": ([_vp, i, ctypes.POINTER(kvec_paged_cache), ctypes.POINTER(kvec_paged_scales), _vp, _vp, i,
@@ -299,6 +304,17 @@ def kvec_shared_decode(handle: int, batch: int, q: int, cache: kvec_paged_cache,
                        max_prefix: int, out: int, scratch: int, scratch_bytes: int, stream: int = 0) -> None:
     _check(load().kvec_shared_decode(handle, batch, q, cache, prefix, max_len, max_prefix, out, scratch, scratch_bytes,
                                      stream))
+
+
+def kvec_shared_decode_quant_bytes(handle: int, batch: int, max_len: int, with_weights: bool) -> int:
+    return int(load().kvec_shared_decode_quant_bytes(handle, batch, max_len, 1 if with_weights else 0))
+
+
+def kvec_shared_decode_quant(handle: int, batch: int, q: int, cache: kvec_paged_cache, scales: kvec_paged_scales,
+                             pool: kvec_paged_cache, prefix: kvec_shared_prefix, max_len: int, max_prefix: int, out: int,
+                             scratch: int, scratch_bytes: int, stream: int = 0) -> None:
+    _check(load().kvec_shared_decode_quant(handle, batch, q, cache, scales, pool, prefix, max_len, max_prefix, out, scratch,
+                                           scratch_bytes, stream))
 
 
 def kvec_rotate_append_quant(handle: int, args: kvec_rotate_args, batch: int, cu_tokens: Optional[int],
@@ -451,10 +467,13 @@ class SharedPrefix:
     """Prefixes that groups of consecutive sequences share (kvec_shared_prefix): holds its tensors, computes nothing.
 
     page_table int32 [num_groups][max_pages] of pages of the cache's pool; lens int32 [num_groups]; cu_seqs int32
-    [num_groups + 1]: group r's sequences are cu_seqs[r] .. cu_seqs[r + 1] - 1.  All contiguous, on the cache's device."""
+    [num_groups + 1]: group r's sequences are cu_seqs[r] .. cu_seqs[r + 1] - 1.  All contiguous, on the cache's device.
 
-    def __init__(self, page_table, lens, cu_seqs):
+    pool: for a cache of 8 bits, the PagedCache of 16 bits whose pages page_table means (None: the cache's own pages)."""
+
+    def __init__(self, page_table, lens, cu_seqs, pool=None):
         import torch as t
+        _want(pool is None or not pool.eight, "a prefix's pool must be a cache of 16 bits")
         _want(page_table.dim() == 2 and page_table.dtype == t.int32 and page_table.shape[1] >= 1,
               "page_table must be int32 [num_groups][max_pages]")
         groups = page_table.shape[0]
@@ -463,6 +482,7 @@ class SharedPrefix:
         parts = (page_table, lens, cu_seqs)
         _want(all(x.is_contiguous() for x in parts), "a prefix's tensors must be contiguous")
         _want(all(x.device == lens.device for x in parts), "a prefix's tensors must be on one device")
+        self.pool = pool
         self.page_table, self.lens, self.cu_seqs = parts
         self.max_pages, self.device = page_table.shape[1], lens.device
         self.c = kvec_shared_prefix(groups, self.max_pages, page_table.data_ptr(), lens.data_ptr(), cu_seqs.data_ptr())
@@ -716,18 +736,25 @@ class KvecSelector:
 
     def shared_decode(self, q, cache, prefix, max_len: Optional[int] = None, max_prefix: Optional[int] = None, out=None,
                       stream=None):
-        """One new token per sequence where groups of sequences share a prefix (kvec_shared_decode); adds to cache.weights,
-        where it has them, for the sequences' own slots.
+        """One new token per sequence where groups of sequences share a prefix (kvec_shared_decode, or kvec_shared_decode_quant
+        where cache is one of 8 bits); adds to cache.weights, where it has them, for the sequences' own slots.
 
-        q [batch][H_q][d] of the cache's type (16 bits), contiguous; cache: the sequences' own slots, prefix a
-        SharedPrefix of pages of the same pool.  max_len bounds the own lengths, max_prefix those of the prefixes (the
+        q [batch][H_q][d] of the cache's dtype, contiguous; cache: the sequences' own slots, prefix a SharedPrefix of
+        pages of the same pool, or with a cache of 8 bits of its own pool's.  max_len bounds the own lengths, max_prefix those of the prefixes (the
         capacities): give the least bounds that are known."""
         p = self.params
         batch, dtype = cache.batch, cache.dtype
         shape = (batch, p.num_q_heads, p.head_dim)
         self._check_cache(cache)
+        pool = prefix.pool
         if cache.eight:
-            raise KvecError(KVEC_ERR_UNSUPPORTED, "shared_decode takes caches of 16 bits")
+            if pool is None:
+                raise KvecError(KVEC_ERR_UNSUPPORTED, "behind a cache of 8 bits a prefix needs a pool of 16 bits")
+            self._check_cache(pool)
+        else:
+            _want(pool is None or (pool.k_pages is cache.k_pages and pool.v_pages is cache.v_pages),
+                  "a prefix before a cache of 16 bits lies in the same pages")
+            pool = cache
         _want(prefix.device == self.device, "the prefix must be on the handle's device")
         self._check("q", q, shape, dtype)
         if out is None:
@@ -737,17 +764,22 @@ class KvecSelector:
         if max_len is None:
             max_len = cache.capacity
         if max_prefix is None:
-            max_prefix = prefix.max_pages * cache.page_size
+            max_prefix = prefix.max_pages * pool.page_size
         if (max_len | max_prefix) >> 31:
             raise KvecError(KVEC_ERR_INVALID_ARG, "max_len and max_prefix must be in [0, 2^31)")
-        need = self._scratch_bytes(kvec_shared_decode_bytes, batch, max_len, cache.weights is not None)
+        need = self._scratch_bytes(kvec_shared_decode_quant_bytes if cache.eight else kvec_shared_decode_bytes, batch, max_len,
+                                   cache.weights is not None)
         scratch = self._empty(max(need, 16), self._torch.uint8, stream)
-        st = self._lib.kvec_shared_decode(self.handle, batch, q.data_ptr(), cache.c, prefix.c, max_len, max_prefix,
-                                          out.data_ptr(), scratch.data_ptr(), need, self._raw(stream))
+        tail = (prefix.c, max_len, max_prefix, out.data_ptr(), scratch.data_ptr(), need, self._raw(stream))
+        if cache.eight:
+            st = self._lib.kvec_shared_decode_quant(self.handle, batch, q.data_ptr(), cache.c, cache.scales, pool.c, *tail)
+        else:
+            st = self._lib.kvec_shared_decode(self.handle, batch, q.data_ptr(), cache.c, *tail)
         if st:
             _check(st)
         if stream is not None:
             self._used(stream, cache, q, out, prefix.page_table, prefix.lens, prefix.cu_seqs)
+            self._used(stream, pool)
         return out
 
     def paged_evict(self, cache, new_table, budget: int, sinks: int = 0, recent: int = 0, max_len: Optional[int] = None,

@@ -336,6 +336,95 @@ def test_steps_of_a_batch_behind_a_prefix():
     assert new_lens.tolist() == [24] * batch
 
 
+# ---------------------------------------------------------------- own slots of 8 bits
+
+def make_eight(prefixes, groups, lens, Hkv, page, pool_page, dtype, gen, weights=True):
+    """Prefixes in a pool of 16 bits, own slots of 8; NaN numbers and scales past the lengths."""
+    pool, prefix = make(prefixes, groups, [0] * len(prefixes), Hkv, pool_page, dtype, gen, weights=False)
+    counts = [-(-n // page) for n in lens]
+    pages = sum(counts) + 1
+    perm = torch.randperm(pages, generator=gen).to(torch.int32)
+    table = torch.full((len(lens), max(1, max(counts))), -1, dtype=torch.int32)
+    hole = torch.ones((pages, page), dtype=torch.bool)
+    at = 0
+    for s, c in enumerate(counts):
+        table[s, :c] = perm[at:at + c]
+        at += c
+        for j in range(lens[s]):
+            hole[table[s, j // page], j % page] = False
+    hole = hole[:, None, :].expand(pages, Hkv, page)
+    parts = []
+    for _ in range(2):
+        x = torch.randn((pages, Hkv, page, D), generator=gen)
+        scale = x.abs().amax(-1) / 448
+        x = (x / scale[..., None]).to(torch.float8_e4m3fn)
+        x.view(torch.uint8)[hole] = 0x7f
+        scale[hole] = float("nan")
+        parts += [x.cuda(), scale.cuda()]
+    w = torch.randn((pages, Hkv, page), generator=gen).exp().cuda() if weights else None
+    cache = kvec.PagedCache(parts[0], parts[2], table.cuda(), torch.tensor(lens, dtype=torch.int32).cuda(), w,
+                            k_scales=parts[1], v_scales=parts[3], dtype=dtype)
+    return cache, kvec.SharedPrefix(prefix.page_table, prefix.lens, prefix.cu_seqs, pool=pool)
+
+
+def check_eight(sel, q, cache, prefix):
+    dtype, u = q.dtype, half_step(q.dtype)
+    pool = prefix.pool
+    with np.errstate(invalid="ignore"):
+        kp, vp = (f64(x) * f64(s)[..., None] for x, s in ((cache.k_pages, cache.k_scales), (cache.v_pages, cache.v_scales)))
+    w0 = f64(cache.weights)
+    w = None if w0 is None else w0.copy()
+    lens, plens, pv = cache.lens.tolist(), prefix.lens.tolist(), f64(pool.v_pages)
+    ref = serving.shared_decode(f64(q), kp, vp, w, cache.page_table.cpu().numpy(), lens, cache.capacity,
+                                prefix.page_table.cpu().numpy(), plens, prefix.cu_seqs.tolist(),
+                                prefix.max_pages * pool.page_size, 1 / np.sqrt(D), pool=(f64(pool.k_pages), pv))
+    out = sel.shared_decode(q, cache, prefix)
+    kvec.kvec_sync_status(sel.handle)
+    vmax = max(np.abs(x[np.isfinite(x)]).max(initial=0.0) for x in (vp, pv))
+    n = max(plens) + max(lens)
+    tol = u * np.abs(ref) + (u + 4e-5 + (n * 2.0 ** -25 if dtype == torch.float16 else 0.0)) * vmax
+    assert np.all(np.abs(f64(out) - ref) <= tol)
+    if w is not None:
+        assert np.all(np.abs(f64(cache.weights) - w) <= 4e-5 * (w - w0) + 2.0 ** -24 * np.abs(w) + 1e-9)
+    return out
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("Hq,Hkv,page,pool_page,prefixes,groups,lens,weights", [
+    (32, 8, 16, 64, [128], [3], [1, 40, 16], True),
+    (28, 4, 64, 16, [500, 0], [4, 1], [1, 17, 0, 23, 5], True),
+    (16, 2, 128, 256, [700, 33], [20, 30], [(11 * i) % 190 for i in range(55)], False),
+    (8, 4, 32, 32, [333], [41], [600 + (37 * b) % 100 for b in range(60)], True),            # a CTA a pair
+    (8, 4, 16, 128, [333, 64], [41, 14], [5000] + [0, 30] * 29 + [7], True),                 # shares
+    (8, 1, 256, 128, [40], [6], [0] * 6, True),
+])
+def test_own_slots_of_eight_bits(dtype, Hq, Hkv, page, pool_page, prefixes, groups, lens, weights):
+    gen = torch.Generator().manual_seed(sum(lens) + page)
+    cache, prefix = make_eight(prefixes, groups, lens, Hkv, page, pool_page, dtype, gen, weights)
+    q = queries(len(lens), Hq, dtype, gen)
+    check_eight(selector(Hq, Hkv), q, cache, prefix)
+    check_eight(selector(Hq, Hkv), q, cache, prefix)
+
+
+def test_own_slots_of_eight_bits_captured_and_on_another_stream():
+    gen = torch.Generator().manual_seed(91)
+    cache, prefix = make_eight([700, 100], [9, 4], [(17 * b) % 99 for b in range(15)], 4, 64, 32, torch.bfloat16, gen, weights=False)
+    q, sel = queries(15, 28, torch.bfloat16, gen), selector(28, 4)
+    want = check_eight(sel, q, cache, prefix)
+    stream = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    for _ in range(10):
+        other = sel.shared_decode(q, cache, prefix, stream=stream)
+        torch.cuda.synchronize()
+        assert torch.equal(other, want) and torch.equal(sel.shared_decode(q, cache, prefix), want)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        out = sel.shared_decode(q, cache, prefix)
+    graph.replay()
+    torch.cuda.synchronize()
+    assert torch.equal(out, want)
+
+
 def test_a_wait_that_runs_out_is_reported():
     gen = torch.Generator().manual_seed(2)
     cache, prefix = make([300], [2], [20, 4], 2, 16, torch.bfloat16, gen)

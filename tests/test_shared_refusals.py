@@ -98,6 +98,28 @@ def test_the_binding_checks_a_call():
     refused(lambda: sel.shared_decode(q, eight, p), UNSUPPORTED, "16 bits")
 
 
+    other = kvec.PagedCache(k.clone(), k.clone(), c.page_table, c.lens)
+    refused(lambda: sel.shared_decode(q, eight, kvec.SharedPrefix(**tensors(), pool=other)), BAD, "handle is NULL")
+    refused(lambda: sel.shared_decode(q, c, kvec.SharedPrefix(**tensors(), pool=other)), BAD, "same pages")
+    refused(lambda: sel.shared_decode(q, c, kvec.SharedPrefix(**tensors(), pool=c)), BAD, "handle is NULL")
+    with pytest.raises(kvec.KvecError):
+        kvec.SharedPrefix(**tensors(), pool=eight)
+    half = kvec.PagedCache(k.half(), k.half(), c.page_table, c.lens)
+    refused(lambda: sel.shared_decode(q, eight, kvec.SharedPrefix(**tensors(), pool=half)), BAD, "dtype")
+
+
+def test_bad_calls_over_eight_bits():
+    scales = kvec.kvec_paged_scales(16, 32)
+    call = lambda c=cache(), s=scales, pool=cache(), p=prefix(), most=64: kvec.kvec_shared_decode_quant(
+        None, 2, 16, c, s, pool, p, 64, most, 16, 256, 0)
+    for bad, words in ((dict(s=None), "k_scales"), (dict(s=kvec.kvec_paged_scales(8, 16)), "16-byte"), (dict(pool=None), "cache is NULL"),
+                       (dict(pool=cache(dtype=kvec.KVEC_FP16)), "dtype"), (dict(pool=cache(k_pages=None)), "NULL"),
+                       (dict(p=None), "prefix is NULL"), (dict(most=193), "max_prefix"), (dict(pool=cache(page_size=16), most=49), "max_prefix"),
+                       ({}, "handle is NULL")):
+        refused(lambda: call(**bad), BAD, words)
+    assert kvec.kvec_shared_decode_quant_bytes(None, 2, 64, True) == 0
+
+
 def test_struct_layouts_match_the_header():
     assert ctypes.sizeof(kvec.kvec_shared_prefix) == 8 + 3 * 8
 
