@@ -192,6 +192,14 @@ struct PrefixGeom {
     int g, nq;                // query heads of a KV head, queries of a 128-row tile
 };
 
+// Where the sums over a sequence's prefix are, of KV head h (PrefixParts).
+struct alignas(16) PrefixPlan {
+    long long at, at_step;    // at + h * at_step: the first CTA, or place in the list of `total` places
+    long long total;          // 0: a CTA for each chunk
+    int n, step;              // chunks, one every `step` CTAs; or blocks (0: no prefix)
+    int base, base_step;      // base + h * base_step: the first query's row, without what goes by the CTA
+};
+
 // Attention of all queries of each group over its prefix in pages, as sums (prefill_kernel.cu).
 struct PrefixIO {
     PrefixGeom geom;
@@ -203,6 +211,7 @@ struct PrefixIO {
     int* err;
     float* part_o;            // [batch * Hq + 256 * SMs][d], by rows as PrefixGroup::first_row says
     float2* part_ml;          // maxima and sums of weights
+    PrefixPlan* plan;         // [batch], for the join
     int rows;                 // of the pages
 };
 

@@ -86,6 +86,8 @@ struct PdArgs {
     float2* part_ml;          // [2 * ctas][8] their maxima and sums
     float* own_o;             // shared_decode: [pair][g][128] sums of whole pairs, in the rows behind part_o's, and
     float2* own_ml;           // [pair][g] behind part_ml's; then come the prefixes'
+    longlong2* own_plan;      // [batch] (places before the sequence, -), and (all places, whether each pair is a CTA's)
+    const PrefixPlan* prefix_plan;   // [batch]
     int ctas;                 // that share the list of blocks
     int pairs;                // batch * Hkv where a CTA each may do, else 0
     int nbmax;                // most visible blocks of a pair
@@ -387,6 +389,14 @@ __global__ void __launch_bounds__(kPdThreads, kPdCtasPerSm) paged_decode_kernel(
     } else {
         List<B> list;
         list.init(A);
+        if constexpr (OPEN) {   // for the join, which would take as long for each block to find them
+            if (warp == 1)
+                for (int s = blockIdx.x; s < A.io.batch; s += A.ctas) {
+                    const long long at = list.places_before(A, s);
+                    if (lane == 0) A.own_plan[s] = make_longlong2(at, 0);
+                }
+            if (blockIdx.x == 0 && tid == 0) A.own_plan[A.io.batch] = make_longlong2(list.total, list.whole_pairs(A) ? 1 : 0);
+        }
         if (list.whole_pairs(A)) {
             cur.s = blockIdx.x / Hkv;
             cur.h = blockIdx.x - cur.s * Hkv;
@@ -980,8 +990,7 @@ __global__ void __launch_bounds__(kJoinThreads, 6) paged_join_kernel(const __gri
 // four; 160 of 4 heads 163 and 157).
 // one_each: every pair's own sums are whole (a cluster each); else as the list of blocks says.
 template <class T, int NT, int B>
-__global__ void __launch_bounds__(NT, 768 / NT) shared_join_kernel(const __grid_constant__ PdArgs A, const __grid_constant__ PrefixGeom G,
-                                                                      int prefix_ctas, bool one_each) {
+__global__ void __launch_bounds__(NT, 768 / NT) shared_join_kernel(const __grid_constant__ PdArgs A, int prefix_ctas, bool one_each) {
     __shared__ float fm[kPdHeads], finv[kPdHeads];
     const int h = blockIdx.y, s = blockIdx.z, lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = A.g;
     // The lengths were complete before the call.
@@ -989,27 +998,26 @@ __global__ void __launch_bounds__(NT, 768 / NT) shared_join_kernel(const __grid_
     v.init(A, s);
     const bool weights = blockIdx.x > 0;
     const int i0 = ((int)blockIdx.x - 1) * (kJoinRows / B);
+    const int own_rows = A.ctas * 2 * kPdHeads, prefix_rows = own_rows + A.io.batch * A.io.Hq;
+    asm volatile("griddepcontrol.launch_dependents;\n" ::: "memory");
+    asm volatile("griddepcontrol.wait;\n" ::: "memory");
+    if (weights && i0 >= v.nb) return;
     int own = v.nb ? 1 : 0, c0 = 0;   // the pair's own shares, of CTAs c0 on
     long long total = 0, p0 = 0;
     bool whole = true;
     if (!one_each && v.nb) {
-        List<B> list;
-        list.init(A);
-        whole = list.whole_pairs(A);
-        total = list.total;
+        const longlong2 all = A.own_plan[A.io.batch];
+        total = all.x;
+        whole = all.y != 0;
+        p0 = A.own_plan[s].x + (long long)h * List<B>::places(v);
         if (!whole) {
-            p0 = list.places_before(A, s) + (long long)h * List<B>::places(v);
             c0 = (int)quotient((p0 + kPairCost + 1) * A.ctas - 1, total);
             own = (int)quotient((p0 + kPairCost + v.nb) * A.ctas - 1, total) - c0 + 1;
             whole = own == 1;
         }
     }
-    const PrefixParts parts(G, s, h, prefix_ctas);
+    const PrefixParts parts(A.prefix_plan[s], h, prefix_ctas);
     const int n = own + parts.n;
-    const int own_rows = A.ctas * 2 * kPdHeads, prefix_rows = own_rows + A.io.batch * A.io.Hq;
-    asm volatile("griddepcontrol.launch_dependents;\n" ::: "memory");
-    asm volatile("griddepcontrol.wait;\n" ::: "memory");
-    if (weights && i0 >= v.nb) return;
     for (int j = warp; j < g; j += NT / 32) {
         float M = kNoLogit, L = 0.f;
         float4 O = make_float4(0.f, 0.f, 0.f, 0.f);
@@ -1129,7 +1137,7 @@ cudaError_t launch_shared_typed(const PdArgs& a, const PrefixIO& px, int num_sms
     if (e != cudaSuccess) return e;
     auto join = [&](auto kernel, int threads) {
         return launch_prio(kernel, dim3(1 + weight_blocks(a, B), a.io.Hkv, a.io.batch), dim3(threads), 0, st, 0, true, a,
-                           px.geom, num_sms, one_each);
+                           num_sms, one_each);
     };
     return a.g <= 4 ? join(shared_join_kernel<T, 128, B>, 128) : join(shared_join_kernel<T, 256, B>, 256);
 }
@@ -1157,7 +1165,7 @@ size_t paged_decode_scratch(int batch, int Hq, int max_len, int window, int sink
 size_t shared_decode_scratch(int batch, int Hq, int max_len, bool weights, bool e8, int num_sms) {
     const int B = e8 ? kPdBlock<true> : kPdBlock<false>;
     const size_t rows = (size_t)share_ctas(num_sms) * 2 * kPdHeads + (size_t)batch * Hq * 2 + (size_t)2 * kPrefixTile * num_sms;
-    size_t b = rows * kHeadDim * sizeof(float) + round16(rows * sizeof(float2));
+    size_t b = rows * kHeadDim * sizeof(float) + round16(rows * sizeof(float2)) + batch * sizeof(PrefixPlan) + (batch + 1) * sizeof(longlong2);
     if (weights) b += (size_t)batch * Hq * visible_blocks(B, max_len, 0, 0) * B * sizeof(float);
     return b;
 }
@@ -1237,8 +1245,11 @@ cudaError_t launch_shared_decode(const PagedDecodeIO& io, const PagedCacheView& 
     a.part_ml = reinterpret_cast<float2*>(a.part_o + rows * kHeadDim);
     a.own_o = a.part_o + shares * kHeadDim;
     a.own_ml = a.part_ml + shares;
-    a.logits = reinterpret_cast<float*>(reinterpret_cast<char*>(a.part_ml) + round16(rows * sizeof(float2)));
     PrefixIO px = prefix;
+    px.plan = reinterpret_cast<PrefixPlan*>(reinterpret_cast<char*>(a.part_ml) + round16(rows * sizeof(float2)));
+    a.prefix_plan = px.plan;
+    a.own_plan = reinterpret_cast<longlong2*>(px.plan + io.batch);
+    a.logits = reinterpret_cast<float*>(a.own_plan + io.batch + 1);
     px.part_o = a.own_o + pairs * kHeadDim;
     px.part_ml = a.own_ml + pairs;
     auto launch = [&](auto type) {

@@ -785,6 +785,14 @@ __global__ void __launch_bounds__(kPfThreads, 1) prefill_kernel(const __grid_con
             ptx::mbar_wait(&bars->mma_done, 0, 50000000ull);
         } else {
             // -------------------------------------------------------- V blocks of partial sight
+            if constexpr (PAGED) {
+                // Nothing has landed yet: meanwhile where the sums of every sequence will be, for the join.
+                const GroupList list(A.px.geom, gridDim.x);
+                for (int s = blockIdx.x; s < A.px.geom.batch; s += gridDim.x) {
+                    const PrefixPlan plan = plan_of(A.px.geom, list, s);
+                    if (lane == 0) A.px.plan[s] = plan;
+                }
+            }
             // Every load is passed in turn: a parity says nothing of a stage several rounds ahead.
             Item w{};
             while (!stop && take_item(w)) {

@@ -111,39 +111,54 @@ struct GroupList {
 };
 __device__ __forceinline__ long long group_share(long long total, int cta, int ctas) { return total * cta / ctas; }
 
+// Where the sums of sequence s are.
+__device__ __forceinline__ PrefixPlan plan_of(const PrefixGeom& A, const GroupList& list, int s) {
+    PrefixPlan p{};
+    int lo = 0, hi = A.groups;   // the last group that begins at or before s
+    while (lo < hi) {
+        const int mid = (lo + hi + 1) >> 1;
+        if (__ldg(&A.cu[mid]) <= s) lo = mid; else hi = mid - 1;
+    }
+    const PrefixGroup gr(A, lo);
+    if (gr.places() == 0 || s < gr.q0 || s >= gr.q0 + gr.n) return p;   // behind the last group there is none
+    const int seat = s - gr.q0, pair = seat / (2 * A.nq);
+    const long long before = list.parts_before(A, lo);
+    p.base = (seat - pair * 2 * A.nq) * A.g;
+    if (list.longest) {
+        p.n = GroupList::chunks(gr, list.longest);
+        p.step = gr.pairs;
+        p.at = before + pair;
+        p.at_step = (long long)p.n * gr.pairs;
+    } else {
+        p.n = gr.nb;
+        p.total = list.total;
+        p.at = before + (long long)pair * gr.places() + PrefixGroup::kCost;
+        p.at_step = (long long)gr.pairs * gr.places();
+        p.base += gr.first_row(A, 0, pair);
+        p.base_step = gr.n * A.g;
+    }
+    return p;
+}
+
 // The sums of the first query row of (sequence, KV head): n of them, each in a row of its own.
 struct PrefixParts {
-    int n = 0, longest, c0 = 0, step = 1, base = 0, ctas;   // of CTAs c0, c0 + step, ..
+    int n, c0, step, base, ctas;   // of CTAs c0, c0 + step, ..
     long long total;
-    __device__ __forceinline__ PrefixParts(const PrefixGeom& A, int s, int h, int num_ctas) : ctas(num_ctas) {
-        const GroupList list(A, num_ctas);
-        total = list.total;
-        longest = list.longest;
-        int lo = 0, hi = A.groups;   // the last group that begins at or before s
-        while (lo < hi) {
-            const int mid = (lo + hi + 1) >> 1;
-            if (__ldg(&A.cu[mid]) <= s) lo = mid; else hi = mid - 1;
-        }
-        const PrefixGroup gr(A, lo);
-        if (gr.places() == 0 || s < gr.q0 || s >= gr.q0 + gr.n) return;   // behind the last group there is none
-        const int seat = s - gr.q0, pair = seat / (2 * A.nq);
-        const long long before = list.parts_before(A, lo);
-        base = (seat - pair * 2 * A.nq) * A.g;
-        if (longest) {
-            n = GroupList::chunks(gr, longest);
-            c0 = (int)before + h * n * gr.pairs + pair;
-            step = gr.pairs;
+    __device__ __forceinline__ PrefixParts(const PrefixPlan& p, int h, int num_ctas)
+        : n(p.n), c0(0), step(1), base(p.base + h * p.base_step), ctas(num_ctas), total(p.total) {
+        const long long at = p.at + h * p.at_step;
+        if (total == 0) {
+            c0 = (int)at;
+            step = p.step;
         } else {
-            const long long at = before + (long long)(h * gr.pairs + pair) * gr.places() + PrefixGroup::kCost;
             c0 = (int)(((at + 1) * ctas - 1) / total);
-            n = (int)(((at + gr.nb) * ctas - 1) / total) - c0 + 1;
-            base += gr.first_row(A, h, pair);
+            n = (int)(((at + p.n) * ctas - 1) / total) - c0 + 1;
         }
     }
     // Row of the k-th; -1: the CTA's share is empty, as there are more CTAs than blocks.
     __device__ __forceinline__ int row(int k) const {
         const int cta = c0 + k * step;
-        return longest || group_share(total, cta, ctas) < group_share(total, cta + 1, ctas) ? base + 2 * kPrefixTile * cta : -1;
+        return total == 0 || group_share(total, cta, ctas) < group_share(total, cta + 1, ctas) ? base + 2 * kPrefixTile * cta : -1;
     }
 };
 

@@ -143,6 +143,20 @@ def test_many_groups(groups, length):
     check(selector(8, 2), queries(len(lens), 8, torch.float16, gen), cache, prefix)
 
 
+@pytest.mark.parametrize("Hkv,prefixes,groups", [
+    (8, [1280] * 13, [1, 2] * 6 + [3]),          # 104 items of ten blocks: shares of a list
+    (8, [1280] * 9 + [100], [1] * 10),           # 80 items: a chunk a CTA would be a fourth longer than the mean
+    (4, [4000, 128, 129], [70, 1, 40]),          # chunks of several pairs
+    (1, [20000], [130]),                         # more CTAs than an item of each length needs
+    (2, [16], [300 // 4]),                       # one block each
+])
+def test_divisions_of_the_prefixes(Hkv, prefixes, groups):
+    gen = torch.Generator().manual_seed(sum(prefixes) + Hkv)
+    lens = [(3 * b) % 20 for b in range(sum(groups) + 1)]
+    cache, prefix = make(prefixes, groups, lens, Hkv, 64, torch.bfloat16, gen)
+    check(selector(4 * Hkv, Hkv), queries(len(lens), 4 * Hkv, torch.bfloat16, gen), cache, prefix)
+
+
 def test_missing_pages_and_bounds():
     gen = torch.Generator().manual_seed(4)
     cache, prefix = make([200, 1000], [3, 4], [20, 0, 33, 50, 1, 2, 3], 2, 16, torch.bfloat16, gen, own_pages=8)
