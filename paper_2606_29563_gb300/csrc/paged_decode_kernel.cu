@@ -38,9 +38,9 @@
 //
 // Behind prefixes that groups of sequences share (OPEN): a sequence's own slots as above, then the prefixes as tiles of the prefill
 // kernel (prefill_kernel.cu), whose CTAs begin where this kernel's end, and one join of all their sums.  160 sequences
-// of 1 to 1000 slots (328 MB) in three groups of 101, 42 and 17 behind 32768, 8001 and 20000 (249 MB), 8 heads, in 141 us: the own
-// slots 60, the prefixes 79, the join 10, each a little beside the one before; 64 of 16 to 527 behind 4096 34 us; 4 behind 500
-// 14 us, three launches' chains of loads.
+// of 1 to 1000 slots (328 MB) in three groups of 101, 42 and 17 behind 32768, 8001 and 20000 (249 MB), 8 heads, in 140 us: the own
+// slots 59, the prefixes 73 more, the join 8; 64 of 16 to 527 behind 4096 34 us; 4 behind 500 14 us, three launches'
+// chains of loads.
 #include "half_types.cuh"
 #include "kvec_internal.cuh"
 #include "prefix_list.cuh"

@@ -846,8 +846,8 @@ __global__ void __launch_bounds__(kPfThreads, 1) prefill_kernel(const __grid_con
         const uint32_t tS = tmem + lanes + t * 128, tO = tmem + lanes + 256 + t * 128;
         const float sl2f = A.sl2;
         // PAGED: in bf16, which holds larger ones, m moves hardly ever (a move costs 0.75 us, half a block; keys of different
-        // sizes moved it in a third of the blocks).  2^80 less 24 bits is still far from fp32's ends, in the join too.
-        constexpr float kMost = PAGED && kType<T> ? 1.2089258196146292e24f : kMostWeight;
+        // sizes moved it in a third of the blocks).  2^40, so that sums of values up to 2^80 stay in fp32's range.
+        constexpr float kMost = PAGED && kType<T> ? 1099511627776.f : kMostWeight;
         const uint64_t sl2 = ptx::pack_f32x2(sl2f, sl2f);
         // The infinities and NaN that a row sees in the blocks of partial sight: their weights
         // are positive, so each makes its output infinite or NaN.

@@ -217,6 +217,21 @@ def test_logits_far_apart():
     check(selector(8, 2), q * 3, cache, prefix)
 
 
+@pytest.mark.parametrize("dtype,size", [(torch.bfloat16, 2.0 ** 80), (torch.float16, 2.0 ** 10)])
+@pytest.mark.parametrize("rise", [20.0, 35.0, 60.0, 200.0])
+def test_logits_that_rise_along_the_prefix_and_large_values(dtype, size, rise):
+    # Each row's logits grow by `rise` powers of two from the first keys to the last: sums relative to the first maximum, which
+    # moves or not, times values that leave little room.
+    gen = torch.Generator().manual_seed(int(rise))
+    cache, prefix = make([1000], [3], [5, 0, 20], 2, 16, dtype, gen, weights=False)
+    for j in range(1000):
+        cache.k_pages[int(prefix.page_table[0, j // 16]), :, j % 16, 0] = rise * j / 1000
+    cache.v_pages[torch.isfinite(cache.v_pages)] *= size
+    q = queries(3, 8, dtype, gen) * 0.25
+    q[:, :, 0] = np.sqrt(D) * np.log(2.0)
+    check(selector(8, 2), q, cache, prefix)
+
+
 def test_as_one_cache_of_prefix_and_own_slots():
     # A prefix that fills its pages, read once for all or by every sequence on its own: the same within the roundings.
     gen = torch.Generator().manual_seed(12)
