@@ -205,7 +205,7 @@ __global__ void __launch_bounds__(32 * kRotWarps, 8) rotate_kernel(const __grid_
 // granules are such that a pair of the rotation lies in one lane, of either layout, without shuffles.
 // The norm's factor r is common to a row: numbers are y' (448 / max|y'|) of y' = y / r, and the scale is r max|y'| / 448.
 // The products are off by 2^-22 of a quotient at most, which moves a number only where that lies as near to the middle
-// of two.  82676 tokens of 32 + 2 x 8 heads (1.91 GB) 329 us, 5.8 TB/s, 86 % of the measured copy rate: a token's rows are
+// of two.  82676 tokens of 32 + 2 x 8 heads (1.91 GB) 321 us, 6.0 TB/s, 88 % of the measured copy rate: a token's rows are
 // not loaded while the one before is stored.  One token 3.2 us.
 constexpr float kMostE4m3 = 448.f, kLeastScale = 1.1754943508222875e-38f;
 constexpr int kQuantRows = 32 * kRotWarps / 8;      // rows of a block at a time
@@ -242,8 +242,9 @@ __device__ __forceinline__ float scale_row(float (&y)[16], float top, float r) {
     return s;
 }
 
-template <class T, int NR, int NT, bool IL>
-__global__ void __launch_bounds__(32 * kRotWarps, 6) rotate_quant_kernel(const __grid_constant__ RotateArgs A) {
+// MB: blocks that are resident on an SM.
+template <class T, int NR, int NT, bool IL, int MB>
+__global__ void __launch_bounds__(32 * kRotWarps, MB) rotate_quant_kernel(const __grid_constant__ RotateArgs A) {
     __shared__ Place places[NT];
     __shared__ __align__(16) float weight[2][kHeadDim];   // the norms' of queries and keys
     const int lane = threadIdx.x & 31, l8 = lane & 7;
@@ -374,11 +375,11 @@ __global__ void __launch_bounds__(32 * kRotWarps, 6) rotate_quant_kernel(const _
     }
 }
 
-template <class T, int NR, int NT>
+template <class T, int NR, int NT, int MB = 6>
 cudaError_t launch_quant_rows(const RotateArgs& a, cudaStream_t st) {
     const dim3 grid((unsigned)((a.io.num_tokens + NT - 1) / NT), (unsigned)((a.heads + kQuantRows * NR - 1) / (kQuantRows * NR)));
-    if (a.io.interleaved) return launch_prio(rotate_quant_kernel<T, NR, NT, true>, grid, dim3(32 * kRotWarps), 0, st, 0, true, a);
-    return launch_prio(rotate_quant_kernel<T, NR, NT, false>, grid, dim3(32 * kRotWarps), 0, st, 0, true, a);
+    if (a.io.interleaved) return launch_prio(rotate_quant_kernel<T, NR, NT, true, MB>, grid, dim3(32 * kRotWarps), 0, st, 0, true, a);
+    return launch_prio(rotate_quant_kernel<T, NR, NT, false, MB>, grid, dim3(32 * kRotWarps), 0, st, 0, true, a);
 }
 
 template <class T, int NR, int NT>
@@ -399,11 +400,14 @@ cudaError_t launch_typed(const RotateArgs& a, cudaStream_t st) {
     if (a.c.k_scales) {
         // By the rows, as below; 48 heads, in us: 200 tokens a row each 3.6 (three rows 4.6), 400 both 5.0, 800 7.3 and
         // 5.4 (of two tokens 8.1); 1600 10.8 and 10.3, 3200 19.4 and 18.1 (of four tokens 17.1); 12800 65.0, 59.9 and
-        // 58.9; 82676 390, 349 and 330.  (Two rows 408, six 418: the registers of more than three leave fewer warps.)
+        // 58.9; 82676 390, 349 and 330.  (Two rows 408, six 418: the registers of more than three leave fewer warps.)  Seven
+        // blocks an SM instead of six, at the price of a few registers: 3200 tokens 19.4, 12800 58.5, 25600 106.4 for 108.4,
+        // 82676 321.  (The next token's rows loaded before the present one's are stored: 366 and more.)
         if (rows <= 16000) return launch_quant_rows<T, 1, 1>(a, st);
         if (rows <= 60000) return launch_quant_rows<T, 3, 1>(a, st);
         if (rows <= 120000) return launch_quant_rows<T, 3, 2>(a, st);
-        return launch_quant_rows<T, 3, 4>(a, st);
+        if (rows <= 800000) return launch_quant_rows<T, 3, 4>(a, st);
+        return launch_quant_rows<T, 3, 4, 7>(a, st);
     }
     if (rows <= 12000) return launch_rows<T, 1, 1>(a, st);
     if (rows <= 150000) return launch_rows<T, 3, 1>(a, st);

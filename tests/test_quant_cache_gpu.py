@@ -226,10 +226,10 @@ def test_rows_at_the_ends_of_the_range(dtype):
         assert torch.all(torch.isnan(got[5:7])) and torch.all(torch.isfinite(got[fine]))
 
 
-@pytest.mark.parametrize("Hq,Hkv,T", [(8, 2, 1333), (8, 2, 1334), (32, 8, 1250), (32, 8, 1251), (28, 4, 3333), (28, 4, 3334), (40, 8, 12000)])
+@pytest.mark.parametrize("Hq,Hkv,T", [(8, 2, 1333), (8, 2, 1334), (32, 8, 1250), (32, 8, 1251), (28, 4, 3333), (28, 4, 3334), (40, 8, 14285), (40, 8, 14286)])
 @pytest.mark.parametrize("interleaved", [False, True])
 def test_append_on_both_sides_of_the_layout_rule(Hq, Hkv, T, interleaved):
-    # Every layout stores the same bytes as a few tokens at a time: 16000, 60000 and 120000 rows.
+    # Every layout stores the same bytes as a few tokens at a time: 16000, 60000, 120000 and 800000 rows.
     gen = torch.Generator(device="cuda").manual_seed(T)
     dtype, page, new = torch.bfloat16, 32, [T // 3, T - T // 3]
     counts = [-(-n // page) for n in new]
