@@ -740,8 +740,8 @@ class KvecSelector:
         where cache is one of 8 bits); adds to cache.weights, where it has them, for the sequences' own slots.
 
         q [batch][H_q][d] of the cache's dtype, contiguous; cache: the sequences' own slots, prefix a SharedPrefix of
-        pages of the same pool, or with a cache of 8 bits of its own pool's.  max_len bounds the own lengths, max_prefix those of the prefixes (the
-        capacities): give the least bounds that are known."""
+        pages of the same pool, or with a cache of 8 bits of its own pool's.  max_len bounds the own lengths, max_prefix
+        those of the prefixes (the capacities): give the least bounds that are known."""
         p = self.params
         batch, dtype = cache.batch, cache.dtype
         shape = (batch, p.num_q_heads, p.head_dim)

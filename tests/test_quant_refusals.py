@@ -1,5 +1,6 @@
 """What the entry points of the 8-bit cache refuse, without a GPU, and the definitions that they are tested with."""
 import ctypes
+import pathlib
 
 import numpy as np
 import pytest
@@ -134,9 +135,10 @@ def test_the_binding_checks_a_read():
 
 
 def test_the_header_names_every_entry_point():
-    header = open(kvec.os.path.join(kvec.os.path.dirname(kvec._HERE), "include", "kvec.h")).read()
+    header = (pathlib.Path(__file__).parents[1] / "include" / "kvec.h").read_text()
     for name in ("kvec_rotate_append_quant", "kvec_paged_decode_quant_bytes", "kvec_paged_decode_quant", "kvec_paged_evict_quant",
-                 "kvec_paged_read", "kvec_shared_decode_bytes", "kvec_shared_decode"):
+                 "kvec_paged_read", "kvec_shared_decode_bytes", "kvec_shared_decode", "kvec_shared_decode_quant_bytes",
+                 "kvec_shared_decode_quant"):
         assert name in kvec.EXPORTED and f" {name}(" in header and callable(getattr(kvec, name))
     assert kvec.kvec_paged_decode_quant_bytes(None, 1, 64, 0, 0, True) == 0
 
