@@ -445,8 +445,10 @@ KVEC_API kvec_status kvec_rotate_append_quant(kvec_handle* h, const kvec_rotate_
 
 /* kvec_paged_decode over such a cache: keys and values count as the exact products of
  * numbers and scales.  A query of bf16 enters as it is, but for at most 2^-39 of its row's largest
- * magnitude, a weight but for 2^-22 of itself.  A scale may be any fp32 number.  scratch:
- * kvec_paged_decode_quant_bytes bytes. */
+ * magnitude; a weight times its value's scale, p_j s_j, but for 2^-22 of itself or 2^-39 of the query
+ * head's largest such product in sight, whichever is more.  So a row takes nothing from the others unless
+ * it outweighs them with its scale counted in.  A scale may be any fp32 number (weights and products are
+ * fp32 too, with fewer bits or none below 2^-126).  scratch: kvec_paged_decode_quant_bytes bytes. */
 KVEC_API size_t kvec_paged_decode_quant_bytes(kvec_handle* h, int batch, int max_len, int window, int sinks,
                                               int with_weights);
 KVEC_API kvec_status kvec_paged_decode_quant(kvec_handle* h, int batch, const void* q, const kvec_paged_cache* cache,

@@ -277,6 +277,10 @@ __device__ __forceinline__ float to_range(float a) {
     return __uint_as_float((uint32_t)min(254 + E - (int)(__float_as_uint(a) >> 23), 253) << 23);
 }
 __device__ __forceinline__ float inverse_power(float p) { return __uint_as_float((254u << 23) - __float_as_uint(p)); }
+// a / b of two such, within the range of normal numbers.
+__device__ __forceinline__ float power_ratio(float a, float b) {
+    return __uint_as_float((uint32_t)min(max(127 + (int)(__float_as_uint(a) >> 23) - (int)(__float_as_uint(b) >> 23), 1), 254) << 23);
+}
 
 // The products with the weights' roundings and with what these left.  Against an infinite value the rest, which is
 // zero or has either sign, would make NaN of what the roundings give alone.
@@ -341,7 +345,7 @@ __device__ void add_weights(const PdArgs& A, int s, int h, const Visible<B>& v, 
 // CL: a cluster of CTAs per pair (grid splits x Hkv x batch) instead of a share of the list.
 // E8: rows of e4m3 numbers with a scale each, which multiplies a key's logit and a value's weight.  The numbers become fp16,
 // which holds them all, on their way from shared memory to the tiles; queries of bf16 and the weights with their
-// scales are brought to its range by powers of two, a row's and the warp's so far.  (Tiles of e4m3, m16n8k32, with a
+// scales are brought to its range by powers of two, a row's and that of a head's largest product so far.  (Tiles of e4m3, m16n8k32, with a
 // query as the sum of two or three numbers took more: their operands are converted too, the queries every time.)
 // OPEN: pairs' sums stay sums (own_o, own_ml), for shared_join_kernel, which adds the weights too.
 template <class T, bool CL, bool E8, bool OPEN>
@@ -569,7 +573,9 @@ __global__ void __launch_bounds__(kPdThreads, kPdCtasPerSm) paged_decode_kernel(
 #pragma unroll
             for (int c = 0; c < 4; ++c) acc[d][c] = 0.f;
         float m = kNoLogit, l = 0.f;   // head lane / 4; l of this lane's slots
-        float up = to_range<14>(0.f);  // E8: acc is this times the sums
+        // E8: head lane / 4's largest weight times scale so far, relative to m; acc's columns are the sums times the power of two
+        // that brings it to fp16's range.
+        float peak = 0.f, up = to_range<14>(0.f);
         // The warp's first block of the segment: its blocks are warp mod kPdWarps of the CTA's.
         const int skip = (warp - done % kPdWarps + kPdWarps) % kPdWarps;
         for (int e = skip; e < len; e += kPdWarps) {
@@ -677,62 +683,75 @@ __global__ void __launch_bounds__(kPdThreads, kPdCtasPerSm) paged_decode_kernel(
                 t = fmaxf(t, __shfl_xor_sync(0xffffffffu, t, 1));
                 t = fmaxf(t, __shfl_xor_sync(0xffffffffu, t, 2));
                 const float mn = fmaxf(m, t);
-                bool unbounded = false;   // E8: a scale is infinite or NaN
+                // The sums so far refer to the new maximum; c0, c1: what E8's columns are multiplied by.
+                auto rescale = [&](float c0, float c1) {
+#pragma unroll
+                    for (int d = 0; d < kAcc; ++d)
+#pragma unroll
+                        for (int c = 0; c < 4; ++c) acc[d][c] *= c & 1 ? c1 : c0;
+                };
+                uint32_t hi[B / 8], lo[B / 8];
+                // Two slots' factors, rounded, and what that left.
+                auto split = [&](int t2, float p0, float p1) {
+                    hi[t2] = Half16<Operand>::pack(p0, p1);
+                    const float2 r = Half16<Operand>::unpack(hi[t2]);
+                    lo[t2] = Half16<Operand>::pack(p0 - r.x, p1 - r.y);
+                    return r;
+                };
                 if constexpr (E8) {
-                    // The block's largest scale, the same for every lane, may lower the power of two.  (Magnitudes compare
-                    // as integers, infinities and NaN as the largest.)
+                    const float corr = ptx::ex2(m - mn);   // 0 from kNoLogit on
+                    l *= corr;
+                    // Weights times scales, in x, and the largest of the head's (magnitudes compare as integers, infinities
+                    // and NaN as the largest).
                     uint32_t top = 0u;
 #pragma unroll
-                    for (int k = 0; k < B / 4; ++k) top = max(top, __float_as_uint(fabsf(vs[k >> 1][k & 1])));
+                    for (int k = 0; k < B / 8; ++k) {
+                        const float p0 = ptx::ex2(x[k][0] - mn), p1 = ptx::ex2(x[k][1] - mn);
+                        l += p0 + p1;
+                        x[k][0] = p0 * vs[k][0];
+                        x[k][1] = p1 * vs[k][1];
+                        top = max(top, max(__float_as_uint(fabsf(x[k][0])), __float_as_uint(fabsf(x[k][1]))));
+                    }
                     top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
                     top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
-                    unbounded = top >= 0x7f800000u;
+                    const bool unbounded = __any_sync(0xffffffffu, top >= 0x7f800000u);
                     if (unbounded) {   // the largest finite one
                         top = 0u;
 #pragma unroll
                         for (int k = 0; k < B / 4; ++k) {
-                            const uint32_t a = __float_as_uint(fabsf(vs[k >> 1][k & 1]));
+                            const uint32_t a = __float_as_uint(fabsf(x[k >> 1][k & 1]));
                             top = a < 0x7f800000u ? max(top, a) : top;
                         }
                         top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
                         top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
                     }
-                    const float to = to_range<14>(__uint_as_float(top));
-                    if (to < up) {
-                        const float down = to * inverse_power(up);
+                    peak = fmaxf(peak * corr, __uint_as_float(top));
+                    const float to = to_range<14>(peak);
+                    if (__any_sync(0xffffffffu, mn != m || to != up)) {
+                        const float f = corr * power_ratio(to, up);
+                        m = mn;
                         up = to;
-#pragma unroll
-                        for (int d = 0; d < kAcc; ++d)
-#pragma unroll
-                            for (int c = 0; c < 4; ++c) acc[d][c] *= down;
+                        rescale(__shfl_sync(0xffffffffu, f, (lane & 3) * 8), __shfl_sync(0xffffffffu, f, (lane & 3) * 8 + 4));
                     }
-                }
-                if (__any_sync(0xffffffffu, mn != m)) {
-                    const float corr = ptx::ex2(m - mn);   // 0 from kNoLogit on
-                    l *= corr;
-                    m = mn;
-                    // (E8: those of the lane's columns)
-                    const float c0 = E8 ? __shfl_sync(0xffffffffu, corr, (lane & 3) * 8) : corr;
-                    const float c1 = E8 ? __shfl_sync(0xffffffffu, corr, (lane & 3) * 8 + 4) : corr;
 #pragma unroll
-                    for (int d = 0; d < kAcc; ++d)
-#pragma unroll
-                        for (int c = 0; c < 4; ++c) acc[d][c] *= c & 1 ? c1 : c0;
-                }
-                uint32_t hi[B / 8], lo[B / 8];
-#pragma unroll
-                for (int t2 = 0; t2 < B / 8; ++t2) {
-                    float p0 = ptx::ex2(x[t2][0] - m), p1 = ptx::ex2(x[t2][1] - m);
-                    l += p0 + p1;
-                    if constexpr (E8) {
-                        p0 *= vs[t2][0] * up;
-                        p1 *= vs[t2][1] * up;
+                    for (int k = 0; k < B / 8; ++k) {
+                        const float2 r = split(k, x[k][0] * up, x[k][1] * up);
+                        if (unbounded)   // an infinite weight leaves no rest, where infinity less infinity gave NaN
+                            lo[k] &= (fabsf(r.x) < INFINITY ? 0xffffu : 0u) | (fabsf(r.y) < INFINITY ? 0xffff0000u : 0u);
                     }
-                    hi[t2] = Half16<Operand>::pack(p0, p1);
-                    const float2 r = Half16<Operand>::unpack(hi[t2]);
-                    lo[t2] = Half16<Operand>::pack(p0 - r.x, p1 - r.y);
-                    if (E8 && unbounded)   // an infinite weight leaves no rest, where infinity less infinity gave NaN
-                        lo[t2] &= (fabsf(r.x) < INFINITY ? 0xffffu : 0u) | (fabsf(r.y) < INFINITY ? 0xffff0000u : 0u);
+                } else {
+                    if (__any_sync(0xffffffffu, mn != m)) {
+                        const float corr = ptx::ex2(m - mn);
+                        l *= corr;
+                        m = mn;
+                        rescale(corr, corr);
+                    }
+#pragma unroll
+                    for (int k = 0; k < B / 8; ++k) {
+                        const float p0 = ptx::ex2(x[k][0] - m), p1 = ptx::ex2(x[k][1] - m);
+                        l += p0 + p1;
+                        split(k, p0, p1);
+                    }
                 }
                 // Values: row (lane & 7) + 8 (lane / 8 % 2), columns 16 dd + 8 (lane / 16).
                 const int vr = (lane & 7) + (((lane >> 3) & 1) << 3);
@@ -782,11 +801,12 @@ __global__ void __launch_bounds__(kPdThreads, kPdCtasPerSm) paged_decode_kernel(
             if (lane == 0) wacc[warp] = mine;
             if constexpr (E8) {
                 const float down = inverse_power(up);
+                const float d0 = __shfl_sync(0xffffffffu, down, (lane & 3) * 8), d1 = __shfl_sync(0xffffffffu, down, (lane & 3) * 8 + 4);
 #pragma unroll
                 for (int d = 0; d < kAcc; ++d) {
                     float* const to = mine + (lane & 3) * 2 * kHeadDim + d * 16 + 2 * j;   // j = lane / 4
-                    *reinterpret_cast<float2*>(to) = make_float2(acc[d][0] * down, acc[d][2] * down);
-                    *reinterpret_cast<float2*>(to + kHeadDim) = make_float2(acc[d][1] * down, acc[d][3] * down);
+                    *reinterpret_cast<float2*>(to) = make_float2(acc[d][0] * d0, acc[d][2] * d0);
+                    *reinterpret_cast<float2*>(to + kHeadDim) = make_float2(acc[d][1] * d1, acc[d][3] * d1);
                 }
             } else {
 #pragma unroll

@@ -363,6 +363,73 @@ def test_scales_of_any_size(dtype, n):
     check_decode(selector(8, 2), q.to(dtype).cuda(), cache, [n, n, n])
 
 
+# Each output against its own size: sum_j p_j |s_j v8_j|, not the largest value in the cache.  A weight times its value's scale
+# counts but for 2^-22 of itself, or 2^-39 of the head's largest such product: with sum_j p_j |s_j| for that one, n slots
+# and numbers up to 448, n 448 2^-39 of it.  Then the logits' 2e-5, and the rounding to the type (fp16 below its normal numbers half
+# of their step, 2^-25).
+
+def check_each_output(sel, q, cache, lens):
+    kp, vp = values(cache.k_pages, cache.k_scales), values(cache.v_pages, cache.v_scales)
+    scales = np.broadcast_to(np.abs(f64(cache.v_scales))[..., None], vp.shape)
+    ref, size, top = (serving.paged_decode(f64(q), kp, x, None, cache.page_table.cpu().numpy(), lens, cache.capacity, 0, 0,
+                                           1 / np.sqrt(D)) for x in (vp, np.abs(vp), scales))
+    out = f64(sel.paged_decode(q, cache))
+    kvec.kvec_sync_status(sel.handle)
+    n = max(lens)
+    tol = half_step(q.dtype) * np.abs(ref) + (2.0 ** -22 + 2e-5) * size + n * 448 * 2.0 ** -39 * top
+    tol += 2.0 ** -25 if q.dtype == torch.float16 else 0.0
+    past = np.abs(ref) >= 2.0 * torch.finfo(q.dtype).max      # rounded to the type, these are infinite
+    assert np.array_equal(out[past], np.sign(ref[past]) * np.inf)
+    bad = ~(np.abs(out - ref) <= tol) & ~past
+    assert not bad.any(), f"{bad.sum()} outputs off, by up to {np.abs((out - ref) / size)[bad].max():.3e} of their size"
+
+
+def set_slot(cache, s, j, key, value_scale):
+    """Slot j of sequence s: a key of `key` in column 0 and zeros, and a factor on its value's scale."""
+    at, ofs = int(cache.page_table[s, j // cache.page_size]), j % cache.page_size
+    numbers = torch.zeros(D)
+    numbers[0] = 1.0
+    cache.k_pages.view(torch.uint8)[at, :, ofs] = numbers.to(E4M3).view(torch.uint8).cuda()
+    cache.k_scales[at, :, ofs] = key
+    cache.v_scales[at, :, ofs] *= value_scale
+
+
+ON_EVERY_PATH = [(8, 2, [40]), (8, 2, [700, 1]), (28, 4, [9000]), (8, 4, [600 + (37 * b) % 100 for b in range(60)])]
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("Hq,Hkv,lens", ON_EVERY_PATH)
+@pytest.mark.parametrize("where", ["before", "behind", "between"])
+def test_a_large_scale_without_weight_costs_the_others_nothing(dtype, Hq, Hkv, lens, where):
+    # Some slots' scales are 2^40 times the others', their logits 104 (base 2) below: what they add is 2^-64 of the rest.
+    gen = torch.Generator().manual_seed(sum(lens) + len(where))
+    cache, _ = make_cache(lens, Hkv, 32, dtype, gen, weights=False)
+    for s, n in enumerate(lens):
+        few = min(n // 3, 100)
+        for j in {"before": range(few), "behind": range(n - few, n), "between": range(3, n, max(7, n // 60))}[where]:
+            set_slot(cache, s, j, -104.0, 2.0 ** 40)
+    q = torch.randn((len(lens), Hq, D), generator=gen)
+    q[:, :, 0] = np.sqrt(D) * np.log(2.0)
+    check_each_output(selector(Hq, Hkv), q.to(dtype).cuda(), cache, lens)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("Hq,Hkv,lens", ON_EVERY_PATH)
+@pytest.mark.parametrize("rise", [60.0, 90.0, -90.0])
+def test_weights_and_scales_that_make_up_for_each_other(dtype, Hq, Hkv, lens, rise):
+    # Logits that rise (or fall) along the sequence by so many powers of two, scales that fall by as many: every slot adds as much
+    # as every other, whatever maximum the weights refer to.  (The logits' five roundings are off by 5 2^-24 90 ln 2 = 1.9e-5 at most.)
+    gen = torch.Generator().manual_seed(sum(lens) + int(rise))
+    cache, _ = make_cache(lens, Hkv, 32, dtype, gen, weights=False, spread=0.1)
+    for s, n in enumerate(lens):
+        for j in range(n):
+            x = rise * (j + 1) / n
+            set_slot(cache, s, j, x, 2.0 ** (max(rise, 0.0) - x - 4.0))
+    q = torch.zeros((len(lens), Hq, D))
+    q[:, :, 0] = np.sqrt(D) * np.log(2.0)
+    check_each_output(selector(Hq, Hkv), q.to(dtype).cuda(), cache, lens)
+
+
 def test_queries_of_any_size():
     # bf16 queries far outside fp16's range, with keys' scales that bring the logits back.
     gen = torch.Generator().manual_seed(9)

@@ -434,6 +434,43 @@ def test_own_slots_of_eight_bits(dtype, Hq, Hkv, page, pool_page, prefixes, grou
     check_eight(selector(Hq, Hkv), q, cache, prefix)
     check_eight(selector(Hq, Hkv), q, cache, prefix)
 
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("lens", [[40, 0, 700], [9000, 3, 1], [600 + (37 * b) % 100 for b in range(75)]])
+def test_a_large_scale_without_weight_costs_the_others_nothing(dtype, lens):
+    """Own slots whose values' scales are 2^40 times the others' and whose logits are 104 (base 2) below.  Each output against its
+    own size, sum_j p_j |v_j|: u for a prefix's weights, 4e-5 and a rounding as above, and 2^-22 of a product of weight and
+    scale or 2^-39 of the largest, n 448 2^-39 of sum_j p_j |s_j| for n slots of numbers up to 448 (a prefix's slots, whose
+    values are below 8, count as scales of 8)."""
+    gen = torch.Generator().manual_seed(sum(lens))
+    cache, prefix = make_eight([300], [len(lens)], lens, 4, 32, 64, dtype, gen, weights=False)
+    numbers = torch.zeros(D)
+    numbers[0] = 1.0
+    numbers = numbers.to(torch.float8_e4m3fn).view(torch.uint8).cuda()
+    for s, n in enumerate(lens):
+        for j in [*range(min(n // 4, 50)), *range(n - n // 5, n, 7)]:
+            at, ofs = int(cache.page_table[s, j // 32]), j % 32
+            cache.k_pages.view(torch.uint8)[at, :, ofs] = numbers
+            cache.k_scales[at, :, ofs] = -104.0
+            cache.v_scales[at, :, ofs] *= 2.0 ** 40
+    q = torch.randn((len(lens), 8, D), generator=gen)
+    q[:, :, 0] = np.sqrt(D) * np.log(2.0)
+    q, pool, sel = q.to(dtype).cuda(), prefix.pool, selector(8, 4)
+    with np.errstate(invalid="ignore"):
+        kp, vp = (f64(x) * f64(s)[..., None] for x, s in ((cache.k_pages, cache.k_scales), (cache.v_pages, cache.v_scales)))
+    scales, pv = np.broadcast_to(np.abs(f64(cache.v_scales))[..., None], vp.shape), f64(pool.v_pages)
+    assert np.abs(pv[np.isfinite(pv)]).max() < 8
+    ref, size, top = (serving.shared_decode(f64(q), kp, own, None, cache.page_table.cpu().numpy(), lens, cache.capacity,
+                                            prefix.page_table.cpu().numpy(), prefix.lens.tolist(), prefix.cu_seqs.tolist(),
+                                            300, 1 / np.sqrt(D), pool=(f64(pool.k_pages), x))
+                      for own, x in ((vp, pv), (np.abs(vp), np.abs(pv)), (scales, np.full_like(pv, 8.0))))
+    out = f64(sel.shared_decode(q, cache, prefix, max_prefix=300))
+    kvec.kvec_sync_status(sel.handle)
+    u = half_step(dtype)
+    tol = u * np.abs(ref) + (u + 4e-5 + 2.0 ** -22) * size + max(lens) * 448 * 2.0 ** -39 * top
+    tol += 300 * 2.0 ** -25 * 8 + 2.0 ** -25 if dtype == torch.float16 else 0.0
+    assert np.all(np.abs(out - ref) <= tol)
+
+
 
 def test_own_slots_of_eight_bits_captured_and_on_another_stream():
     gen = torch.Generator().manual_seed(91)
