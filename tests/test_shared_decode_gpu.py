@@ -194,6 +194,38 @@ def test_unbounded_values_in_sight():
     out[:3, 4:, [3, 9, 70]] = 0
     assert np.isfinite(out).all()
 
+def device_time(call):
+    """Milliseconds: the least of several."""
+    call()
+    times = []
+    for _ in range(8):
+        a, b = (torch.cuda.Event(enable_timing=True) for _ in range(2))
+        a.record()
+        for _ in range(4):
+            call()
+        b.record()
+        b.synchronize()
+        times.append(a.elapsed_time(b) / 4)
+    return min(times)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("bad", [float("inf"), float("nan")])
+def test_what_lies_behind_a_prefix_costs_no_time(dtype, bad):
+    # The rest of a page may hold anything: the same bits, and no walk for its infinities (which took 60 times the call's time).
+    gen = torch.Generator().manual_seed(17)
+    cache, prefix = make([500, 140], [4, 3], [1, 17, 40, 23, 5, 6, 7], 8, 256, dtype, gen, weights=False)
+    q, sel = queries(7, 32, dtype, gen), selector(32, 8)
+    outs, times = [], []
+    for fill in (0.0, bad):
+        for r, n in enumerate(prefix.lens.tolist()):
+            cache.v_pages[int(prefix.page_table[r, (n - 1) // 256]), :, (n - 1) % 256 + 1:] = fill
+        outs.append(check(sel, q, cache, prefix))
+        times.append(device_time(lambda: sel.shared_decode(q, cache, prefix)))
+    assert torch.equal(*outs)
+    assert times[1] < 4 * times[0], f"{times[1]:.4f} ms behind infinities, {times[0]:.4f} without"
+
+
 
 def test_minus_infinite_logits_have_no_weight():
     gen = torch.Generator().manual_seed(5)
