@@ -410,7 +410,9 @@ typedef struct {
  * With cache.weights the own slots' weights grow by their p_j, as there; a prefix's do not
  * (its sequences would not agree on what to evict).  Rows of 16 bits; no window.
  * The weights of a prefix's slots are rounded to dtype before they meet the values, as in
- * kvec_prefill_attention, those of own slots as in kvec_paged_decode.
+ * kvec_prefill_attention, those of own slots as in kvec_paged_decode.  Sums are fp32, divided last:
+ * finite values of up to 2^100 give finite outputs behind any prefix (and in kvec_prefill_attention),
+ * and bf16 values of a prefix below 2^-100 may lose bits.
  *   q, out     device cache.dtype [batch][H_q][d], 16-byte aligned.
  *   max_len    host bound on the own lengths, max_prefix one on the prefixes'.
  *   scratch    device, kvec_shared_decode_bytes bytes, 256-byte aligned: written and read

@@ -51,7 +51,7 @@
 // that share a prefix are the rows, each of which sees all of it, and K and V blocks come from the
 // prefix's pages.  The lengths are on the device, and the CTAs share the blocks by them (prefix_list.cuh);
 // they leave sums for shared_join_kernel.  A block of both tiles takes 1.5 to 1.7 us there, as above (2.1 where bf16 maxima
-// moved at 2^14); the first S comes 4 to 6 us after the start (lengths, shares, pages, keys), and the sums of a pair of
+// moved at 2^14 times the first); the first S comes 4 to 6 us after the start (lengths, shares, pages, keys), and the sums of a pair of
 // tiles (128 KB a CTA) take 3 us to store.  Copies into L2 three to eight blocks ahead of the ring made it slower (164 us for 158).
 #include <algorithm>
 #include <type_traits>
@@ -848,9 +848,11 @@ __global__ void __launch_bounds__(kPfThreads, 1) prefill_kernel(const __grid_con
         const uint32_t lanes = (uint32_t)(quad * 32) << 16;
         const uint32_t tS = tmem + lanes + t * 128, tO = tmem + lanes + 256 + t * 128;
         const float sl2f = A.sl2;
-        // PAGED: in bf16, which holds larger ones, m moves hardly ever (a move costs 0.75 us, half a block; keys of different
-        // sizes moved it in a third of the blocks).  2^40, so that sums of values up to 2^80 stay in fp32's range.
-        constexpr float kMost = PAGED && kType<T> ? 1099511627776.f : kMostWeight;
+        // PAGED: bf16 holds weights of any size, so that m begins 2^26 above the first maximum and moves hardly ever (a move
+        // costs 0.75 us, half a block; keys of different sizes moved it in a third of the blocks, 163 us for 140 of the case
+        // in paged_decode_kernel.cu).  From below, so that a share's sums, of up to 2^13 blocks, have the room that they have
+        // elsewhere: 2^27 times the largest value.  (Values from 2^-100 on lose nothing of it.)
+        constexpr float kAbove = PAGED && kType<T> ? 26.f : 0.f;
         const uint64_t sl2 = ptx::pack_f32x2(sl2f, sl2f);
         // The infinities and NaN that a row sees in the blocks of partial sight: their weights
         // are positive, so each makes its output infinite or NaN.
@@ -938,16 +940,18 @@ __global__ void __launch_bounds__(kPfThreads, 1) prefill_kernel(const __grid_con
                 if (i == 0) {   // the row's first maximum
 #pragma unroll
                     for (int e = 0; e < 128; e += 2) m = max3(m, s[e] * sl2f, s[e + 1] * sl2f);
+                    m += kAbove;
                 }
                 float z = weights(0);
                 z += weights(1);
-                if (__any_sync(0xffffffffu, live && !(z < kMost))) {
+                if (__any_sync(0xffffffffu, live && !(z < kMostWeight))) {
                     // The row's first logits, ones far above m, or NaN: m moves to the largest.
                     tmem_wait_st();   // these weights are written again
                     float mx = m;
 #pragma unroll
                     for (int e = 0; e < 128; e += 2) mx = max3(mx, s[e] * sl2f, s[e + 1] * sl2f);
-                    if (z < kMost || !live) mx = m;
+                    mx += kAbove;
+                    if (z < kMostWeight || !live) mx = m;
                     const float f = ptx::ex2(m - mx);
                     l *= f;
                     m = mx;

@@ -263,6 +263,45 @@ def test_logits_that_rise_along_the_prefix_and_large_values(dtype, size, rise):
     q[:, :, 0] = np.sqrt(D) * np.log(2.0)
     check(selector(8, 2), q, cache, prefix)
 
+@pytest.mark.parametrize("size", [2.0 ** 100, 2.0 ** -100])
+@pytest.mark.parametrize("rise", [0.0, 20.0, 35.0, 45.0, 60.0, 200.0])
+def test_values_at_the_ends_of_the_range(size, rise):
+    # As above, in bf16, with values near the largest and the least that the sums have room for.
+    gen = torch.Generator().manual_seed(int(rise) + 1)
+    cache, prefix = make([1000], [3], [5, 0, 20], 2, 16, torch.bfloat16, gen, weights=False)
+    for j in range(1000):
+        cache.k_pages[int(prefix.page_table[0, j // 16]), :, j % 16, 0] = rise * j / 1000
+    cache.v_pages[torch.isfinite(cache.v_pages)] *= size / 8     # (below 8 before)
+    assert cache.v_pages[torch.isfinite(cache.v_pages)].abs().max() < size
+    q = queries(3, 8, torch.bfloat16, gen) * 0.25
+    q[:, :, 0] = np.sqrt(D) * np.log(2.0)
+    check(selector(8, 2), q, cache, prefix)
+
+
+@pytest.mark.parametrize("dtype,size", [(torch.bfloat16, 2.0 ** 100), (torch.bfloat16, 2.0 ** 80), (torch.float16, 60000.0)])
+@pytest.mark.parametrize("rise", [6.5, 20.0, 32.5, 33.5, 39.5, 46.5])
+def test_long_shares_of_large_values_have_room(dtype, size, rise):
+    """Four prefixes of 2^17 slots and eight heads, 221 blocks a CTA: the first block's logits `rise` powers of two below all
+    others', so that these meet sums relative to a maximum far below them.  Values are one number, and so are the outputs:
+    weights rounded to the type (u), sums and exponentials (4e-5), the type (u)."""
+    page, n = 128, 1 << 17
+    k = torch.zeros((3, 8, page, D), dtype=dtype, device="cuda")
+    v = torch.full_like(k, size)
+    k[1:, :, :, 0] = rise
+    ints = lambda x: torch.tensor(x, dtype=torch.int32).cuda()
+    table = torch.ones((4, n // page), dtype=torch.int32, device="cuda")
+    table[:, 0] = 0                                               # pages are only read: many entries may name one
+    prefix = kvec.SharedPrefix(table, ints([n] * 4), ints(range(5)))
+    cache = kvec.PagedCache(k, v, torch.full((4, 1), 2, dtype=torch.int32).cuda(), ints([3, 0, 100, 1]))
+    q = torch.zeros((4, 32, D), dtype=dtype, device="cuda")
+    q[:, :, 0] = np.sqrt(D) * np.log(2.0)
+    sel = selector(32, 8)
+    out = f64(sel.shared_decode(q, cache, prefix))
+    kvec.kvec_sync_status(sel.handle)
+    want, u = float(v[0, 0, 0, 0]), half_step(dtype)
+    assert np.all(np.abs(out - want) <= (2 * u + 4e-5) * want)
+
+
 
 def test_as_one_cache_of_prefix_and_own_slots():
     # A prefix that fills its pages, read once for all or by every sequence on its own: the same within the roundings.
