@@ -238,16 +238,14 @@ struct List {
         w.i = max(i - kPairCost, 0);
         return whole - (long long)(p + w.h) * kPairCost - min(i, kPairCost);
     }
-    // Places of the sequences before s.
+    // Places of the sequences before s, by a whole warp.
     __device__ __forceinline__ long long places_before(const PdArgs& A, int s) const {
         const int l = s / per;
-        long long b = __shfl_sync(0xffffffffu, before, l);
-        for (int k = l * per; k < s; ++k) {
-            Visible<B> v;
-            v.init(A, k);
-            b += (long long)places(v) * A.io.Hkv;
-        }
-        return b;
+        return __shfl_sync(0xffffffffu, before, l) + sum_by_lanes(l * per, s, [&](int k) {
+                   Visible<B> v;
+                   v.init(A, k);
+                   return (long long)places(v) * A.io.Hkv;
+               });
     }
 };
 

@@ -32,6 +32,21 @@ struct PrefixGroup {
     }
 };
 
+// The sum of f over [from, to), by a whole warp: a lane each 32nd where there are more than a few.  (Up to 2048 are asked for
+// for each sequence: 8192 sequences in as many groups take 719 us, and 1762 with one after the other by every lane.)
+template <class F>
+__device__ __forceinline__ long long sum_by_lanes(int from, int to, F f) {
+    long long sum = 0;
+    if (to - from <= 4) {
+        for (int k = from; k < to; ++k) sum += f(k);
+        return sum;
+    }
+    for (int k = from + (int)(threadIdx.x & 31); k < to; k += 32) sum += f(k);
+#pragma unroll
+    for (int o = 16; o; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+    return sum;
+}
+
 // How the CTAs share the work, as a warp sees it: lane l holds the groups l * per .. l * per + per - 1.
 //
 // If no item's blocks need to be cut into chunks much shorter than the mean share (a fourth above it at most), and there
@@ -101,12 +116,11 @@ struct GroupList {
         }
         return r;
     }
-    // Chunks or places of the groups before r.
+    // Chunks or places of the groups before r, by a whole warp.
     __device__ __forceinline__ long long parts_before(const PrefixGeom& A, int r) const {
         const int l = r / per;
-        long long b = __shfl_sync(0xffffffffu, before, l);
-        for (int k = l * per; k < r; ++k) b += part(A, PrefixGroup(A, k));
-        return b;
+        return __shfl_sync(0xffffffffu, before, l) +
+               sum_by_lanes(l * per, r, [&](int k) { return part(A, PrefixGroup(A, k)); });
     }
 };
 __device__ __forceinline__ long long group_share(long long total, int cta, int ctas) { return total * cta / ctas; }

@@ -142,6 +142,51 @@ def test_many_groups(groups, length):
     cache, prefix = make(prefixes, sizes, lens, 2, 16, torch.float16, gen)
     check(selector(8, 2), queries(len(lens), 8, torch.float16, gen), cache, prefix)
 
+def many_groups(n, gen, Hkv=1, size=lambda r: 1):
+    """n groups behind prefixes that fill their pages, of pages that many of them share (they are only read)."""
+    dtype, pages = torch.bfloat16, 200
+    sel = kvec.KvecSelector(kvec.make_params(4 * Hkv, Hkv, num_ext_heads=1, max_batch=n, max_seqlen=64, max_layers=1))
+    k, v = (torch.randn((pages, Hkv, 16, D), generator=gen).to(dtype).cuda() for _ in range(2))
+    sizes = [size(r) for r in range(n)]
+    batch = sum(sizes)
+    prefixes = torch.tensor([16 * (r % 4) for r in range(n)], dtype=torch.int32)
+    lens = torch.tensor([(7 * b) % 40 for b in range(batch)], dtype=torch.int32).cuda()
+    prefix = kvec.SharedPrefix(torch.randint(pages, (n, 3), generator=gen, dtype=torch.int32).cuda(), prefixes.cuda(),
+                               torch.tensor([0] + np.cumsum(sizes).tolist(), dtype=torch.int32).cuda())
+    cache = kvec.PagedCache(k, v, torch.randint(pages, (batch, 3), generator=gen, dtype=torch.int32).cuda(), lens)
+    return sel, queries(batch, 4 * Hkv, dtype, gen), cache, prefix, sizes
+
+
+@pytest.mark.parametrize("n,size", [(700, lambda r: r % 3), (5000, lambda r: 1), (3000, lambda r: (r % 700 == 5) * 300 + (r < 50))])
+def test_thousands_of_groups(n, size):
+    # Against every sequence on its own over its prefix's pages and then its own: the same within the roundings.
+    gen = torch.Generator().manual_seed(n)
+    sel, q, cache, prefix, sizes = many_groups(n, gen, 2, size)
+    of = torch.repeat_interleave(torch.arange(n), torch.tensor(sizes)).cuda()
+    held = prefix.lens[of]
+    at, own = torch.arange(6, device="cuda")[None, :], held[:, None] // 16
+    table = torch.where(at < own, prefix.page_table[of].gather(1, at.clamp(max=2).expand(len(of), -1)),
+                        cache.page_table.gather(1, (at - own).clamp(0, 2))).to(torch.int32).contiguous()
+    whole = kvec.PagedCache(cache.k_pages, cache.v_pages, table, cache.lens + held)
+    a, b = f64(sel.shared_decode(q, cache, prefix)), f64(sel.paged_decode(q, whole))
+    kvec.kvec_sync_status(sel.handle)
+    u = half_step(q.dtype)
+    vmax = float(cache.v_pages.float().abs().max())
+    assert np.all(np.abs(a - b) <= 2 * u * np.abs(b) + (u + 6e-5) * vmax)
+    sel.close()
+
+
+def test_time_grows_with_the_groups():
+    # Eight times as many take eight times as long (17 where each sequence's place was summed up by every lane alone).
+    times = []
+    for n in (1024, 8192):
+        sel, q, cache, prefix, _ = many_groups(n, torch.Generator().manual_seed(n))
+        times.append(device_time(lambda: sel.shared_decode(q, cache, prefix)))
+        kvec.kvec_sync_status(sel.handle)
+        sel.close()
+    assert times[1] < 13 * times[0], times
+
+
 
 @pytest.mark.parametrize("Hkv,prefixes,groups", [
     (8, [1280] * 13, [1, 2] * 6 + [3]),          # 104 items of ten blocks: shares of a list
