@@ -439,8 +439,10 @@ typedef struct {
 /* kvec_rotate_append into such a cache (which is needed here).  A key or value row y, in
  * fp32 as it comes from the norm and the rotation, is stored as
  *   scale = max(max |y| / 448, 2^-126),  numbers = y / scale rounded to nearest even,
- * so that a number is off by 1/16 of itself or 2^-10 scale at most.  A row that holds an
- * infinity or NaN gets such a scale, and reads as NaN.  q_out and k_out are dtype as ever. */
+ * so that a number is off by 1/16 of itself or 2^-10 scale at most.  Both are formed in fp32 to 2^-21
+ * of themselves: a quotient that lies so near the middle of two numbers may become either (bf16 rows
+ * have exact middles, a few numbers in a thousand).  A row that holds an infinity or NaN gets such a
+ * scale, and reads as NaN.  q_out and k_out are dtype as ever. */
 KVEC_API kvec_status kvec_rotate_append_quant(kvec_handle* h, const kvec_rotate_args* args, int batch,
                                               const int32_t* cu_tokens, const kvec_paged_cache* cache,
                                               const kvec_paged_scales* scales, kvec_stream_t stream);
