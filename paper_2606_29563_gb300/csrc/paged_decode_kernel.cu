@@ -29,18 +29,21 @@
 // by the bound on the lengths: the 64 rows take 51 us under one of 8192, 57 of 32768 and 82 of 131072.
 //
 // Rows of 8 bits (E8): blocks of 32 slots, whose numbers a warp turns into fp16 for the same tiles.  131072 slots of 8 heads (277
-// MB) in 53 us, 5.2 TB/s; the 64 rows above (107 MB) in 37.5 us; 512 slots 7.5.  Bound by what a warp does for a block, not by
-// the memory: 3000 cycles for 8.4 KB and eight warps on an SM, of which a third are the conversions (128 of two numbers
+// MB) in 53 us, 5.2 TB/s; the 64 rows above (107 MB) in 38.3 us; 512 slots 7.6.  A block takes a warp 1.6 us, 3000 cycles for 8.4
+// KB: eight warps on each of 148 SMs read at the copy rate (304 equal pairs: 6.7 to 7.1 TB/s for each slot more).  What lies
+// above the floor is the start (6.5 us of the 131072 slots) and the join (3), and of the 64 rows the pairs' lengths: the
+// longest CTA's warps have 16 blocks, 10.4 would be even.  A third of a block's cycles are the conversions (128 of two numbers
 // each, two cycles of a scheduler).  What that took, 131072 slots and the 64 rows: blocks of 16 slots 72 and 49;
 // eight warps of 128 registers a CTA 73 and 42; 32 slots, the logits as tiles of e4m3 57 and 46; as tiles of fp16, copies
-// issued before a block is worked on 54 and 39.5; the rows of 32 loads found at once 53 and 37.6.
+// issued before a block is worked on 54 and 39.5; the rows of 32 loads found at once 52.6 and 37.6 (a head's power of two by
+// its products, where a warp's scales alone had lost small values beside a large one without weight: 52.9 and 38.3).
 // Slower: three CTAs an SM with rings of two blocks (61 and 42).
 //
 // Behind prefixes that groups of sequences share (OPEN): a sequence's own slots as above, then the prefixes as tiles of the prefill
 // kernel (prefill_kernel.cu), whose CTAs begin where this kernel's end, and one join of all their sums.  160 sequences
 // of 1 to 1000 slots (328 MB) in three groups of 101, 42 and 17 behind 32768, 8001 and 20000 (249 MB), 8 heads, in 140 us: the own
-// slots 59, the prefixes 73 more, the join 8; 64 of 16 to 527 behind 4096 34 us; 4 behind 500 14 us, three launches'
-// chains of loads.
+// slots 60, the prefixes 75 more, the join 5 (own slots of 8 bits 132 in all); 64 of 16 to 527 behind 4096 34 us (12, 15 and 8);
+// 4 behind 500 14 us (4, 7 and 3), three launches' chains of loads.
 #include "half_types.cuh"
 #include "kvec_internal.cuh"
 #include "prefix_list.cuh"

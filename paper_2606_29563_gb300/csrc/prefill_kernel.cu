@@ -51,8 +51,8 @@
 // that share a prefix are the rows, each of which sees all of it, and K and V blocks come from the
 // prefix's pages.  The lengths are on the device, and the CTAs share the blocks by them (prefix_list.cuh);
 // they leave sums for shared_join_kernel.  A block of both tiles takes 1.5 to 1.7 us there, as above (2.1 where bf16 maxima
-// moved at 2^14 times the first); the first S comes 4 to 6 us after the start (lengths, shares, pages, keys), and the sums of a pair of
-// tiles (128 KB a CTA) take 3 us to store.  Copies into L2 three to eight blocks ahead of the ring made it slower (164 us for 158).
+// moved at 2^14 times the first); the first S comes 4 to 6 us after the start (lengths, shares, pages, keys), and the sums of
+// a pair of tiles (128 KB a CTA) take 3 us to store.  Copies into L2 three to eight blocks ahead of the ring made it slower (164 us for 158).
 #include <algorithm>
 #include <type_traits>
 
@@ -73,7 +73,7 @@ constexpr int kPfItems = 4;                         // items handed out and not 
 constexpr int kPfThreads = 384;
 constexpr uint32_t kPfTmem = 512;                   // S0 | S1 | O0 | O1, 128 columns each
 // Registers of a thread: at launch (the most that 384 threads may have), and after the split.
-// The compiler spills one or two words, and eight in the variant of ragged lengths (-Xptxas -v).
+// The compiler spills one or two words, eight in the variant of ragged lengths and six in that of pages (-Xptxas -v).
 constexpr int kPfRegs = 168, kPfSoftmaxRegs = 216, kPfOtherRegs = 72;
 static_assert(256 * kPfSoftmaxRegs + 128 * kPfOtherRegs <= kPfThreads * kPfRegs, "the split fits what the block was launched with");
 // A row's weights of a block that sum up to less are taken as they are; fp16 holds them.

@@ -52,8 +52,8 @@ __device__ __forceinline__ long long sum_by_lanes(int from, int to, F f) {
 // If no item's blocks need to be cut into chunks much shorter than the mean share (a fourth above it at most), and there
 // are CTAs enough, CTA c takes chunk c of them in the order (group, head, chunk, pair): the pairs of a group and head read the
 // same keys and values at the same time, which then come from memory once.  Else the CTAs take even shares of the list of
-// all items' blocks (longest = 0).  Three groups of 101, 42 and 17 sequences behind 32768, 8001 and 20000 slots: 143.5 us by
-// chunks (251 MB read for the prefixes), 149 by shares (401 MB), at the time.
+// all items' blocks (longest = 0).  Three groups of 101, 42 and 17 sequences behind 32768, 8001 and 20000 slots: 140.4 us by
+// chunks (251 MB read for the prefixes), 142.3 by shares (401 MB); four sequences behind 500 slots 14.3 and 18.1.
 struct GroupList {
     int per, longest;                // blocks of a chunk at most
     long long before, mine, total;   // chunks or places: of the lanes before, of this lane, of all

@@ -4,8 +4,8 @@
 // A block takes a few tokens, whose places (sequence, page) a thread each finds first; then a half-warp moves a
 // (token, head)'s rows of K and of V, eight values a lane, several in flight.
 //
-// HBM-bound: 82676 rows of 8 heads (513 MB) from 8 bits in 79.4 us, 6.5 TB/s, 95 % of the measured copy rate; 1057 rows of 4
-// heads 3.3 us, the launch and a chain of look-ups (sequence, page, row).
+// HBM-bound: 82676 rows of 8 heads (513 MB) from 8 bits in 79.5 us, 6.5 TB/s, 95 % of the measured copy rate, from 16 bits
+// (677 MB) in 101.4 us, 6.7 TB/s, 98 %; 1057 rows of 4 heads 3.4 us, the launch and a chain of look-ups (sequence, page, row).
 #include "half_types.cuh"
 #include "kvec_internal.cuh"
 

@@ -205,7 +205,7 @@ __global__ void __launch_bounds__(32 * kRotWarps, 8) rotate_kernel(const __grid_
 // granules are such that a pair of the rotation lies in one lane, of either layout, without shuffles.
 // The norm's factor r is common to a row: numbers are y' (448 / max|y'|) of y' = y / r, and the scale is r max|y'| / 448.
 // The products are off by 2^-22 of a quotient at most, which moves a number only where that lies as near to the middle
-// of two.  82676 tokens of 32 + 2 x 8 heads (1.91 GB) 321 us, 6.0 TB/s, 88 % of the measured copy rate: a token's rows are
+// of two.  82676 tokens of 32 + 2 x 8 heads (1.91 GB) 323 us, 5.9 TB/s, 87 % of the measured copy rate: a token's rows are
 // not loaded while the one before is stored.  One token 3.2 us.
 constexpr float kMostE4m3 = 448.f, kLeastScale = 1.1754943508222875e-38f;
 constexpr int kQuantRows = 32 * kRotWarps / 8;      // rows of a block at a time
@@ -401,8 +401,8 @@ cudaError_t launch_typed(const RotateArgs& a, cudaStream_t st) {
         // By the rows, as below; 48 heads, in us: 200 tokens a row each 3.6 (three rows 4.6), 400 both 5.0, 800 7.3 and
         // 5.4 (of two tokens 8.1); 1600 10.8 and 10.3, 3200 19.4 and 18.1 (of four tokens 17.1); 12800 65.0, 59.9 and
         // 58.9; 82676 390, 349 and 330.  (Two rows 408, six 418: the registers of more than three leave fewer warps.)  Seven
-        // blocks an SM instead of six, at the price of a few registers: 3200 tokens 19.4, 12800 58.5, 25600 106.4 for 108.4,
-        // 82676 321.  (The next token's rows loaded before the present one's are stored: 366 and more.)
+        // blocks an SM instead of six have 72 registers, which spills 28 to 40 bytes: 3200 tokens 19.4, 12800 58.5, 25600 106.4 for
+        // 108.4, 82676 321 to 323.  (The next token's rows loaded before the present one's are stored: 366 and more.)
         if (rows <= 16000) return launch_quant_rows<T, 1, 1>(a, st);
         if (rows <= 60000) return launch_quant_rows<T, 3, 1>(a, st);
         if (rows <= 120000) return launch_quant_rows<T, 3, 2>(a, st);
